@@ -295,6 +295,78 @@ int moe_dispatch_noalloc(const int32_t* topk_idx, const int32_t* tenant_id, cons
                          int32_t* tenant_expert_count, int32_t* expert_off, int32_t* group_off,
                          int32_t* status_out, void* stream);
 
+/* element types of the calls that take more than one */
+enum { MOE_TYPE_F32 = 0, MOE_TYPE_BF16 = 1 };
+
+/*
+ * Gating rules beyond moe_route's (Sec. 2.1: a gating network picks the k best experts of a token), from router logits z:
+ *   s[e] = softmax(z)[e] over all E experts, or sigmoid(z[e])
+ *   v[e] = s[e] + balance_bias[m][e]      (the bias takes part in the choice only, not in the weights)
+ *   the E experts form n_groups groups of E / n_groups consecutive ids; the keep_groups groups of the largest score stay,
+ *   a group's score being its largest v or the sum of its two largest (of its only one if it has one)
+ *   the k experts of largest v in the groups that stay, ordered by (v descending, id ascending)
+ *   w[j] = s[idx[j]] * scale, or s[idx[j]] / sum_i s[idx[i]] * scale with renormalize
+ * The choice is that of double precision: s, v and the group scores are compared as their 64-bit values, whatever the kernel
+ * computes them in.  Without a bias experts are ordered by z itself (s grows with z), and so are groups by their largest.
+ * Ties go to the lower expert (group) id.  A NaN logit or bias counts as -inf, a logit of +inf as the largest finite
+ * fp32 value.  A chosen expert of logit -inf has weight 0; with renormalize the others share the whole, and if all
+ * chosen logits are -inf all weights are 0.
+ */
+enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
+enum { MOE_GROUP_MAX = 0, MOE_GROUP_TOP2 = 1 };
+typedef struct {
+    int32_t score;          /* MOE_SCORE_* */
+    int32_t n_groups;       /* 1 (no groups) .. 32, divides E */
+    int32_t keep_groups;    /* 1 .. n_groups; keep_groups * (E / n_groups) >= k */
+    int32_t group_score;    /* MOE_GROUP_* */
+    int32_t renormalize;    /* 0: raw scores, 1: divided by the sum of the chosen ones */
+    float   scale;          /* factor of every weight; finite */
+} moe_gating;
+
+/*
+ * The choice and its weights from given logits, without a context (what moe_route does for a layer with a rule set by
+ * moe_set_gating, for callers that compute the logits themselves).  Its outputs are what moe_dispatch and moe_combine take.
+ *   logits       f32 or bf16 (logits_type) [T, E], rows ld >= E elements apart
+ *   rule         host pointer, read during the call
+ *   balance_bias f32 [M, E] or NULL
+ *   tenant_id    int32 [T] or NULL (every token uses model 0); model_of_tenant int32 [n_tenants] (DEVICE) or NULL (model
+ *                0); both are needed if M > 1.  An entry of model_of_tenant outside [0, M) counts as model 0.
+ *   topk_idx     int32 [T,k]; topk_w f32 [T,k]
+ *   tie_flag     u8 [T] or NULL: 1 if two neighbours among ranks 1..k+1 differ by less than 1e-5 relative (in v; without
+ *                a bias in s), or 32 bits could not decide the choice
+ *   status_out   device int32 or NULL: MOE_DEV_BAD_TENANT is OR-ed into it for a tenant id outside [0, n_tenants) (the
+ *                token gets experts 0..k-1 with weight 0); the caller clears it
+ * 1 <= E <= 256, 1 <= k <= min(E, 8).  One launch, no workspace; results do not depend on what else runs.
+ */
+int moe_gate(const void* logits, int logits_type, int64_t ld, int T, int E, int k, const moe_gating* rule,
+             const float* balance_bias, const int32_t* tenant_id, const int32_t* model_of_tenant, int n_tenants, int M,
+             int32_t* topk_idx, float* topk_w, uint8_t* tie_flag, int32_t* status_out, void* stream);
+
+/*
+ * Makes moe_route, and with it every call that runs the layer, use a gating rule in layer `layer` (all its models):
+ * z = x . router_w^T + router_bias as before, then the rule above with balance_bias (device f32 [M, E] or NULL, used in
+ * place).  rule is a host pointer and is copied; NULL returns to moe_route's own rule (softmax, raw probabilities).
+ * Set between calls, not while one may still run.
+ */
+int moe_set_gating(moe_ctx* ctx, int layer, const moe_gating* rule, const float* balance_bias);
+
+/*
+ * The residual's addition and the RMSNorm in front of a layer, without a context: for callers that run other blocks
+ * (attention) between the layers of moe_stack_forward.
+ *   h = bf16(x + residual)              (h = x if residual is NULL)     bf16 [T, H] each
+ *   residual_out = h                    bf16 [T, H] or NULL; may be residual or x itself (same row distance)
+ *   y = h / sqrt(mean(h^2) + eps) * weight                              fp32; weight bf16 [H]
+ *   out = bf16(y)                       bf16 [T, H] or NULL; may be x itself (same row distance)
+ *   out_q = e4m3(y / s)                 8-bit floats [T, H] or NULL, saturating; s = max |y| / 448 (0 where y is 0)
+ *   q_scale = s                         f32 [T] with group = 0 (one scale per row), f32 [T, ceil(H/128)] with group = 128
+ * Rows of every matrix are ld_* >= H elements apart; ld_* of a NULL matrix is not looked at.  At least one output.
+ * 1 <= H <= 16384.  Any alignment of whole elements; rows on 16-byte boundaries are fastest.  A row with an infinity or
+ * a NaN makes its own outputs NaN (or 0), no other row's.
+ */
+int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld_residual, const void* weight, float eps,
+                    int T, int H, void* residual_out, int64_t ld_residual_out, void* out, int64_t ld_out, void* out_q,
+                    int64_t ld_q, float* q_scale, int group, void* stream);
+
 /* route -> dispatch -> experts -> combine on the context's workspace; bit-identical to
  * the four calls above.  out bf16 [T,H]. */
 int moe_layer_forward(moe_ctx* ctx, int layer, const void* x, const int32_t* tenant_id, int T, int G,

@@ -34,11 +34,15 @@ MOE_OPT_FUSED_DISPATCH = 11
 MOE_OPT_HEAD_UNITS = 12
 MOE_DISPATCH_SHARED, MOE_DISPATCH_PRIVATE = 0, 1
 MOE_PATH_AUTO, MOE_PATH_FMA, MOE_PATH_TCGEN05 = 0, 1, 2
+MOE_TYPE_F32, MOE_TYPE_BF16 = 0, 1
+MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID = 0, 1
+MOE_GROUP_MAX, MOE_GROUP_TOP2 = 0, 1
 
 EXPORTS = ["moe_create", "moe_destroy", "moe_set_expert_pool", "moe_set_model_weights", "moe_set_slot_table",
            "moe_set_tenant_models", "moe_set_option", "moe_form_blocks", "moe_set_block_table", "moe_route", "moe_dispatch", "moe_experts", "moe_combine",
            "moe_layer_forward", "moe_residency_enable", "moe_layer_forward_paged", "moe_layer_forward_host", "moe_layer_forward_host_submit", "moe_layer_forward_host_wait", "moe_layer_forward_timed", "moe_stack_forward",
-           "moe_get_workspace", "moe_last_status", "moe_last_plan", "moe_launch_count", "moe_strerror", "moe_dispatch_noalloc"]
+           "moe_get_workspace", "moe_last_status", "moe_last_plan", "moe_launch_count", "moe_strerror", "moe_dispatch_noalloc",
+           "moe_gate", "moe_set_gating", "moe_add_rmsnorm"]
 MOE_DISPATCH_NOALLOC_MAX_WORDS = 1 << 18
 
 STAGES = ["route", "dispatch", "plan", "experts_gateup", "experts_down", "combine"]
@@ -48,6 +52,11 @@ class MoeConfig(ctypes.Structure):
     _fields_ = [("hidden", c_int32), ("n_experts", c_int32), ("inter", c_int32), ("top_k", c_int32),
                 ("shared_inter", c_int32), ("n_models", c_int32), ("n_tenants", c_int32), ("n_slots", c_int32),
                 ("max_tokens", c_int32), ("n_layers", c_int32), ("rms_eps", c_float)]
+
+
+class MoeGating(ctypes.Structure):
+    _fields_ = [("score", c_int32), ("n_groups", c_int32), ("keep_groups", c_int32), ("group_score", c_int32),
+                ("renormalize", c_int32), ("scale", c_float)]
 
 
 class MoeError(RuntimeError):
@@ -98,6 +107,11 @@ def load_library(path: str | None = None):
                                                 POINTER(c_float), c_void_p]
         lib.moe_stack_forward.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p, c_void_p, c_void_p]
         lib.moe_dispatch_noalloc.argtypes = [c_void_p] * 3 + [c_int] * 6 + [c_void_p] * 7
+        lib.moe_gate.argtypes = ([c_void_p, c_int, c_int64, c_int, c_int, c_int, POINTER(MoeGating)] + [c_void_p] * 3 +
+                                 [c_int, c_int] + [c_void_p] * 5)
+        lib.moe_set_gating.argtypes = [c_void_p, c_int, POINTER(MoeGating), c_void_p]
+        lib.moe_add_rmsnorm.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_float, c_int, c_int, c_void_p,
+                                        c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int, c_void_p]
         lib.moe_get_workspace.argtypes = [c_void_p] + [POINTER(c_void_p)] * 8
         lib.moe_last_status.argtypes = [c_void_p, POINTER(c_int32), POINTER(c_int32)]
         lib.moe_last_plan.argtypes = [c_void_p, c_int, POINTER(c_int32)]
@@ -277,6 +291,130 @@ def moe_stack_forward(ctx, x_inout, tenant_id, T, G, dbg_layer_inputs=None, dbg_
     _check("moe_stack_forward", load_library().moe_stack_forward(ctx, _ptr(x_inout), _ptr(tenant_id), T, G,
                                                                  _ptr(dbg_layer_inputs), _ptr(dbg_layer_outputs),
                                                                  _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Calls without a context.  They take strided matrices (last dimension contiguous), check types, shapes and devices, and
+# run on the tensors' own device: on `stream`, or on that device's current stream.
+
+_RAW_STREAM = torch._C._cuda_getCurrentRawStream
+
+
+def _need(ok, fn, what):
+    if not ok:
+        raise ValueError(f"{fn}: {what}")
+
+
+def _matrix(t, fn, name, rows, cols, dtypes, dev):
+    """Address and row distance of a [rows, cols] matrix (None: 0, 0)."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype not in dtypes or t.device != dev:
+        raise ValueError(f"{fn}: {name} must be [{rows}, {cols}] of {'/'.join(str(d)[6:] for d in dtypes)} on {dev}, "
+                         f"not {list(t.shape)} of {str(t.dtype)[6:]} on {t.device}")
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"{fn}: the columns of {name} must be contiguous (stride 1, not {inner})")
+    if rows <= 1:
+        ld = max(ld, cols)
+    if ld < cols:
+        raise ValueError(f"{fn}: the rows of {name} overlap (stride {ld} < {cols} columns)")
+    return t.data_ptr(), ld
+
+
+def _flat(t, fn, name, n, dtype, dev):
+    """Address of a contiguous array of n elements (n < 0: any number; None: 0)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != dev or not t.is_contiguous() or (n >= 0 and t.numel() != n):
+        raise ValueError(f"{fn}: {name} must be contiguous {str(dtype)[6:]} on {dev}" + (f", {n} elements" if n >= 0 else "") +
+                         f", not {list(t.shape)} of {str(t.dtype)[6:]} on {t.device}")
+    return t.data_ptr()
+
+
+def _call_on(dev, stream, fn, f, *args):
+    """f(*args, stream) with `dev` as the current device."""
+    if dev.type != "cuda":
+        raise ValueError(f"{fn}: tensors must be on a CUDA device, not {dev}")
+    if stream is not None:
+        _need(stream.device == dev, fn, f"the stream belongs to {stream.device}, the tensors to {dev}")
+        raw = stream.cuda_stream
+    else:
+        raw = _RAW_STREAM(dev.index)
+    if torch.cuda.current_device() == dev.index:
+        status = f(*args, raw)
+    else:
+        with torch.cuda.device(dev):
+            status = f(*args, raw)
+    if status != MOE_OK:
+        raise MoeError(fn, status)
+
+
+_SCORES = {"softmax": MOE_SCORE_SOFTMAX, "sigmoid": MOE_SCORE_SIGMOID}
+_GROUP_SCORES = {"max": MOE_GROUP_MAX, "top2": MOE_GROUP_TOP2}
+
+
+def moe_gating(*, score="softmax", n_groups=1, keep_groups=None, group_score="max", renormalize=False, scale=1.0) -> MoeGating:
+    """A gating rule (struct moe_gating of include/faasmoe.h) for moe_gate and moe_set_gating."""
+    return MoeGating(_SCORES[score], n_groups, n_groups if keep_groups is None else keep_groups, _GROUP_SCORES[group_score],
+                     1 if renormalize else 0, scale)
+
+
+_LOGITS_TYPES = {torch.float32: MOE_TYPE_F32, torch.bfloat16: MOE_TYPE_BF16}
+
+
+def moe_gate(logits, rule, topk_idx, topk_w, *, balance_bias=None, tenant_id=None, model_of_tenant=None, tie_flag=None,
+             status_out=None, stream=None):
+    """Chooses k experts per token from logits [T, E] (fp32 or bf16, rows may be strided) by `rule` (moe_gating()).
+
+    topk_idx [T, k] int32 and topk_w [T, k] float32 receive the choice; k is their width.  balance_bias [M, E] float32;
+    tenant_id [T] and model_of_tenant [n_tenants] int32 (device) pick the bias row.  See include/faasmoe.h."""
+    fn, dev = "moe_gate", logits.device
+    _need(logits.dim() == 2 and topk_idx.dim() == 2 and isinstance(rule, MoeGating), fn, "logits [T, E], a moe_gating() rule and topk_idx [T, k] are needed")
+    (T, E), k = logits.shape, topk_idx.shape[1]
+    p_logits, ld = _matrix(logits, fn, "logits", T, E, _LOGITS_TYPES, dev)
+    M = 1
+    if balance_bias is not None:
+        M = balance_bias.shape[0] if balance_bias.dim() == 2 else 1
+    _call_on(dev, stream, fn, load_library().moe_gate, p_logits, _LOGITS_TYPES[logits.dtype], ld, T, E, k, byref(rule),
+             _flat(balance_bias, fn, "balance_bias", M * E, torch.float32, dev), _flat(tenant_id, fn, "tenant_id", T, torch.int32, dev),
+             _flat(model_of_tenant, fn, "model_of_tenant", -1, torch.int32, dev),
+             model_of_tenant.numel() if model_of_tenant is not None else 1 << 30, M,
+             _flat(topk_idx, fn, "topk_idx", T * k, torch.int32, dev), _flat(topk_w, fn, "topk_w", T * k, torch.float32, dev),
+             _flat(tie_flag, fn, "tie_flag", T, torch.uint8, dev), _flat(status_out, fn, "status_out", 1, torch.int32, dev))
+
+
+def moe_set_gating(ctx, layer, rule, balance_bias=None):
+    """Makes the layer choose its experts by `rule` (None: moe_route's own rule).  balance_bias [M, E] float32 on the device is
+    used in place: keep it alive."""
+    _check("moe_set_gating", load_library().moe_set_gating(ctx, layer, byref(rule) if rule is not None else None, _ptr(balance_bias)))
+
+
+_BF16 = (torch.bfloat16,)
+_E4M3 = (torch.float8_e4m3fn,)
+
+
+def moe_add_rmsnorm(x, weight, eps, *, residual=None, residual_out=None, out=None, out_q=None, q_scale=None, stream=None):
+    """residual_out = h = bf16(x + residual); out = bf16(RMSNorm(h) * weight); out_q = e4m3 of the same with scales.
+
+    x, residual, residual_out, out: bf16 [T, H], rows may be strided; out_q float8_e4m3fn [T, H]; q_scale float32 [T, 1]
+    (one scale per row) or [T, ceil(H/128)] (one per 128 columns).  residual_out may be residual or x; out may be x."""
+    fn, dev = "moe_add_rmsnorm", x.device
+    _need(x.dim() == 2, fn, "x must be [T, H]")
+    T, H = x.shape
+    px, ldx = _matrix(x, fn, "x", T, H, _BF16, dev)
+    pr, ldr = _matrix(residual, fn, "residual", T, H, _BF16, dev)
+    pro, ldro = _matrix(residual_out, fn, "residual_out", T, H, _BF16, dev)
+    po, ldo = _matrix(out, fn, "out", T, H, _BF16, dev)
+    pq, ldq = _matrix(out_q, fn, "out_q", T, H, _E4M3, dev)
+    group = 0
+    _need((out_q is None) == (q_scale is None), fn, "out_q and q_scale go together")
+    if q_scale is not None:
+        n = -(-H // 128)
+        _need(q_scale.dim() == 2 and q_scale.shape[0] == T and q_scale.shape[1] in (1, n), fn, f"q_scale must be [{T}, 1] or [{T}, {n}]")
+        group = 0 if q_scale.shape[1] == 1 else 128       # (one group of at most 128 columns is the row)
+    _call_on(dev, stream, fn, load_library().moe_add_rmsnorm, px, ldx, pr, ldr, _flat(weight, fn, "weight", H, torch.bfloat16, dev), eps,
+             T, H, pro, ldro, po, ldo, pq, ldq, _flat(q_scale, fn, "q_scale", -1, torch.float32, dev), group)
 
 
 def moe_get_workspace(ctx):

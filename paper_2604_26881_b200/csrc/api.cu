@@ -255,6 +255,17 @@ __global__ void mark_active_kernel(const int32_t* __restrict__ topk_idx, const i
 
 }  // namespace
 
+namespace faasmoe {
+
+int cuda_result(const char* what, cudaError_t e)
+{
+    if (e == cudaSuccess) return MOE_OK;
+    snprintf(g_last_cuda_error, sizeof(g_last_cuda_error), "%s: %s", what, cudaGetErrorString(e));
+    return MOE_ERR_CUDA;
+}
+
+}  // namespace faasmoe
+
 extern "C" {
 
 int moe_create(const moe_config* cfg, moe_ctx** out)
@@ -300,6 +311,8 @@ int moe_create(const moe_config* cfg, moe_ctx** out)
     c->d_models = nullptr; c->d_slot = nullptr; c->d_model_of_tenant = nullptr; c->d_tenant_local = nullptr;
     c->d_bin_base = nullptr; c->d_tenants_in_model = nullptr;
     c->d_block_table = nullptr; c->table_blocks = 0;
+    c->gating.assign(g.n_layers, LayerGating());
+    c->d_logits = nullptr;
     int rc = MOE_OK;
     cudaError_t e = cudaGetDevice(&c->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, c->device);
@@ -376,7 +389,7 @@ int moe_destroy(moe_ctx* c)
     if (c->copy_in) cudaStreamDestroy(c->copy_in);
     if (c->copy_out) cudaStreamDestroy(c->copy_out);
     void* ptrs[] = {c->d_models, c->d_slot, c->d_model_of_tenant, c->d_tenant_local, c->d_bin_base,
-                    c->d_tenants_in_model, c->d_block_table};
+                    c->d_tenants_in_model, c->d_block_table, c->d_logits};
     for (void* p : ptrs) if (p) cudaFree(p);
     if (c->res.d_active) cudaFree(c->res.d_active);
     if (c->res.h_active) cudaFreeHost(c->res.h_active);
@@ -486,6 +499,23 @@ int moe_set_block_table(moe_ctx* c, const int32_t* block_of_expert, int n_blocks
     if (!c->d_block_table) MOE_CUDA(c, dev_alloc(&c->d_block_table, ME));
     MOE_CUDA(c, cudaMemcpy(c->d_block_table, block_of_expert, ME * sizeof(int32_t), cudaMemcpyHostToDevice));
     c->table_blocks = n_blocks;
+    return MOE_OK;
+}
+
+int moe_set_gating(moe_ctx* c, int layer, const moe_gating* rule, const float* balance_bias)
+{
+    if (!c) return MOE_ERR_NULL;
+    if (layer < 0 || layer >= c->cfg.n_layers) return MOE_ERR_SHAPE;
+    if (!rule) {
+        c->gating[layer] = LayerGating();
+        return MOE_OK;
+    }
+    if ((uintptr_t)balance_bias & 3) return MOE_ERR_SHAPE;
+    const int rc = check_gating(rule, c->cfg.n_experts, c->cfg.top_k);
+    if (rc != MOE_OK) return rc;
+    if (!c->d_logits) MOE_CUDA(c, dev_alloc(&c->d_logits, (size_t)c->cfg.max_tokens * c->cfg.n_experts));
+    LayerGating& g = c->gating[layer];
+    g.on = true; g.rule = *rule; g.bias = balance_bias;
     return MOE_OK;
 }
 

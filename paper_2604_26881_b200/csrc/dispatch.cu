@@ -287,14 +287,14 @@ cudaError_t launch_route_dispatch(moe_ctx* c, int layer, const bf16* x, const in
     // One CTA routes the batch (at most 128 tokens of one model): it holds every routed row when its top-k step ends
     // and goes on to the dispatch and the plan -- one launch and one round trip through global memory fewer on the
     // latency chain of a small batch.
-    if (tc && c->fused_dispatch_enabled && T <= kFusedDispatchTokens && g.n_models == 1 && T * g.top_k <= kSmallRows) {
+    if (tc && !c->gating[layer].on && c->fused_dispatch_enabled && T <= kFusedDispatchTokens && g.n_models == 1 && T * g.top_k <= kSmallRows) {
         SmallDispatchArgs a;
         size_t smem_small = 0;
         bool gather_inside = false;
         small_dispatch_args(c, x, topk_idx, tenant_id, T, G, perm, inv_perm, tenant_expert_count, expert_off, group_off,
                             x_perm, true, plan_shared, &a, &smem_small, &gather_inside);
         if (smem_small <= kFusedDispatchSmem) {
-            const cudaError_t e = launch_route_tc(c, layer, x, tenant_id, T, topk_idx, topk_w, shared_gate, tie_flag, st,
+            const cudaError_t e = launch_route_tc(c, layer, x, tenant_id, T, topk_idx, topk_w, shared_gate, tie_flag, nullptr, st,
                                                   &a, smem_small);
             if (e != cudaSuccess) return e;
             *fused = true;

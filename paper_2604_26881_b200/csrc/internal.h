@@ -57,6 +57,13 @@ struct Unit {
     int32_t colblock;
 };
 
+// Gating rule of a layer (moe_set_gating); off: moe_route's own rule.
+struct LayerGating {
+    bool on = false;
+    moe_gating rule;
+    const float* bias = nullptr;     // [M, E] or null
+};
+
 struct TensorMaps;   // defined in experts_tc.cu
 
 // On-demand residency of the routed experts (one layer): all experts are parked in host memory, the pool slots on
@@ -152,6 +159,8 @@ struct moe_ctx {
     int32_t* d_slot;              // [M*E]
     int32_t* d_model_of_tenant;   // [Nt]
     int32_t* d_tenant_local;      // [Nt] index of the tenant among the tenants of its model
+    std::vector<faasmoe::LayerGating> gating;   // [L]
+    float* d_logits;              // [max_tokens, E] router logits of layers with a gating rule (allocated with the first rule)
     faasmoe::Residency res;       // on-demand residency of the routed experts
     int32_t* d_block_table;       // [M*E] block of every expert (load-aware formation), null: blocks of G consecutive experts
     int table_blocks;             // blocks per model of that table
@@ -215,6 +224,11 @@ cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t sme
 }
 #endif
 
+// MOE_OK or MOE_ERR_CUDA with the message kept for moe_strerror (entry points that have no context)
+int cuda_result(const char* what, cudaError_t e);
+// MOE_OK or the reason why the rule cannot choose k of E experts
+int check_gating(const moe_gating* rule, int E, int k);
+
 // --- launchers (each returns a cudaError_t from the launch) -------------------------------
 
 cudaError_t launch_route(moe_ctx* c, int layer, const bf16* x, const int32_t* tenant_id, int T, int32_t* topk_idx,
@@ -225,13 +239,14 @@ cudaError_t launch_dispatch(moe_ctx* c, const bf16* x, const int32_t* topk_idx, 
                             int32_t* group_off, bf16* x_perm, cudaStream_t st, bool with_plan = false,
                             bool plan_shared = false, bool* plan_done = nullptr);
 
+// logits f32 [T, E], not null: the router stores its logits (bias added) there and leaves topk_idx, topk_w and tie_flag alone
 cudaError_t launch_route_fma(moe_ctx* c, int layer, const bf16* x, const int32_t* tenant_id, int T, int32_t* topk_idx,
-                             float* topk_w, float* shared_gate, uint8_t* tie_flag, cudaStream_t st);
+                             float* topk_w, float* shared_gate, uint8_t* tie_flag, float* logits, cudaStream_t st);
 struct SmallDispatchArgs;
 // fused: arguments of the one-block dispatch that the router's CTA runs behind its top-k step (one-tile batch of one
 // model; fused_smem bytes of scratch), or null
 cudaError_t launch_route_tc(moe_ctx* c, int layer, const bf16* x, const int32_t* tenant_id, int T, int32_t* topk_idx,
-                            float* topk_w, float* shared_gate, uint8_t* tie_flag, cudaStream_t st,
+                            float* topk_w, float* shared_gate, uint8_t* tie_flag, float* logits, cudaStream_t st,
                             const SmallDispatchArgs* fused = nullptr, size_t fused_smem = 0);
 // Router, then -- where one CTA routes the whole batch -- dispatch and work plan in the same launch.  *fused tells the
 // caller whether the dispatch has been done (and *plan_done whether the plan has); if not, launch_dispatch follows.

@@ -1,0 +1,85 @@
+// C-ABI entry points that need no context: argument checks, then one launcher each.
+#include <cmath>
+
+#include "addnorm.cuh"
+#include "gate.cuh"
+
+using namespace faasmoe;
+
+namespace {
+
+constexpr int kMaxRows = 1 << 28;
+
+bool off(const void* p, size_t align) { return ((uintptr_t)p & (align - 1)) != 0; }
+
+}  // namespace
+
+namespace faasmoe {
+
+int check_gating(const moe_gating* rule, int E, int k)
+{
+    if (!rule) return MOE_ERR_NULL;
+    if (rule->score != MOE_SCORE_SOFTMAX && rule->score != MOE_SCORE_SIGMOID) return MOE_ERR_SHAPE;
+    if (rule->group_score != MOE_GROUP_MAX && rule->group_score != MOE_GROUP_TOP2) return MOE_ERR_SHAPE;
+    if (rule->n_groups < 1 || rule->n_groups > 32 || E % rule->n_groups) return MOE_ERR_SHAPE;
+    if (rule->keep_groups < 1 || rule->keep_groups > rule->n_groups) return MOE_ERR_SHAPE;
+    if (k > rule->keep_groups * (E / rule->n_groups)) return MOE_ERR_SHAPE;
+    if (!std::isfinite(rule->scale)) return MOE_ERR_SHAPE;
+    return MOE_OK;
+}
+
+void apply_gating(GateArgs& a, const moe_gating& rule)
+{
+    a.score = rule.score; a.n_groups = rule.n_groups; a.keep = rule.keep_groups; a.group_score = rule.group_score;
+    a.renormalize = rule.renormalize != 0; a.scale = rule.scale;
+}
+
+}  // namespace faasmoe
+
+extern "C" {
+
+int moe_gate(const void* logits, int logits_type, int64_t ld, int T, int E, int k, const moe_gating* rule,
+             const float* balance_bias, const int32_t* tenant_id, const int32_t* model_of_tenant, int n_tenants, int M,
+             int32_t* topk_idx, float* topk_w, uint8_t* tie_flag, int32_t* status_out, void* stream)
+{
+    if (!rule) return MOE_ERR_NULL;
+    if (T < 0 || T > kMaxRows || E < 1 || E > kMaxExperts || k < 1 || k > kMaxTopK || k > E || ld < E) return MOE_ERR_SHAPE;
+    if (M < 1 || M > kMaxExperts || (tenant_id && n_tenants < 1)) return MOE_ERR_SHAPE;
+    if (logits_type != MOE_TYPE_F32 && logits_type != MOE_TYPE_BF16) return MOE_ERR_UNSUPPORTED;
+    if (off(logits, logits_type == MOE_TYPE_BF16 ? 2 : 4) || off(balance_bias, 4) || off(tenant_id, 4) || off(model_of_tenant, 4) ||
+        off(topk_idx, 4) || off(topk_w, 4) || off(status_out, 4))
+        return MOE_ERR_SHAPE;
+    const int rc = check_gating(rule, E, k);
+    if (rc != MOE_OK) return rc;
+    if (T == 0) return MOE_OK;
+    if (!logits || !topk_idx || !topk_w || (M > 1 && (!tenant_id || !model_of_tenant))) return MOE_ERR_NULL;
+    GateArgs a = {};
+    a.logits = logits; a.bf16_logits = logits_type == MOE_TYPE_BF16; a.ld = ld; a.T = T; a.E = E; a.k = k;
+    apply_gating(a, *rule);
+    a.bias = balance_bias; a.tenant_id = tenant_id; a.model_of_tenant = model_of_tenant; a.n_tenants = n_tenants; a.M = M;
+    a.topk_idx = topk_idx; a.topk_w = topk_w; a.tie_flag = tie_flag; a.status = status_out;
+    return cuda_result("moe_gate", launch_gate(a, (cudaStream_t)stream));
+}
+
+int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld_residual, const void* weight, float eps,
+                    int T, int H, void* residual_out, int64_t ld_residual_out, void* out, int64_t ld_out, void* out_q,
+                    int64_t ld_q, float* q_scale, int group, void* stream)
+{
+    if (T < 0 || T > kMaxRows || H < 1) return MOE_ERR_SHAPE;
+    if (H > kAddNormMaxH) return MOE_ERR_UNSUPPORTED;
+    if (ldx < H || (residual && ld_residual < H) || (residual_out && ld_residual_out < H) || (out && ld_out < H) || (out_q && ld_q < H))
+        return MOE_ERR_SHAPE;
+    if (!(eps >= 0.f) || (out_q && group != 0 && group != 128)) return MOE_ERR_SHAPE;
+    if (off(x, 2) || off(residual, 2) || off(weight, 2) || off(residual_out, 2) || off(out, 2) || off(q_scale, 4)) return MOE_ERR_SHAPE;
+    if (T == 0) return MOE_OK;
+    if (!x || !weight || (!residual_out && !out && !out_q) || (out_q && !q_scale)) return MOE_ERR_NULL;
+    AddNormArgs a = {};
+    a.x = (const bf16*)x; a.residual = (const bf16*)residual; a.residual_out = (bf16*)residual_out; a.weight = (const bf16*)weight;
+    a.out = (bf16*)out; a.q = (uint8_t*)out_q; a.q_scale = q_scale;
+    a.ldx = ldx; a.ldr = residual ? ld_residual : 0; a.ldro = residual_out ? ld_residual_out : 0; a.ldo = out ? ld_out : 0;
+    a.ldq = out_q ? ld_q : 0;
+    a.group = group; a.n_groups = group ? (H + group - 1) / group : 1; a.T = T; a.H = H; a.eps = eps;
+    return cuda_result("moe_add_rmsnorm", launch_addnorm(a, (cudaStream_t)stream));
+}
+
+}  // extern "C"

@@ -1,6 +1,7 @@
 // Gating network: router logits, fp32 softmax, top-k by warp shuffles, shared-expert gate.
 // (Paper Sec. 2.1: the gating network selects the top-k experts of each token; Sec. 3: it
 // runs in the orchestrator, ahead of the expert blocks.)
+#include "gate.cuh"
 #include "internal.h"
 
 namespace faasmoe {
@@ -40,7 +41,8 @@ __global__ void __launch_bounds__(kRouteWarps * 32)
 route_kernel(const bf16* __restrict__ x, const int32_t* __restrict__ tenant_id, int T, int H, int E, int k,
              int n_tenants, int n_models, const int32_t* __restrict__ model_of_tenant,
              const ModelWeights* __restrict__ models, int32_t* __restrict__ topk_idx, float* __restrict__ topk_w,
-             float* __restrict__ shared_gate, uint8_t* __restrict__ tie_flag, int32_t* __restrict__ status)
+             float* __restrict__ shared_gate, uint8_t* __restrict__ tie_flag, float* __restrict__ logits,
+             int32_t* __restrict__ status)
 {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     bf16* w_s = reinterpret_cast<bf16*>(smem_raw);                       // [kExpertsPerStage][H]
@@ -132,8 +134,13 @@ route_kernel(const bf16* __restrict__ x, const int32_t* __restrict__ tenant_id, 
 #pragma unroll
         for (int c = 0; c < kMaxChunks; ++c) p[c] = ((c * 32 + lane) < E && c < nchunks) ? p[c] / den : -1.f;
 
-        // k (+1) rounds of warp arg-max; ties go to the lower expert id
-        const int rounds = (k < E) ? k + 1 : k;
+        if (logits) {
+#pragma unroll
+            for (int c = 0; c < kMaxChunks; ++c)
+                if (c < nchunks && c * 32 + lane < E) logits[(size_t)t * E + c * 32 + lane] = z[i][c];
+        }
+        // k (+1) rounds of warp arg-max; ties go to the lower expert id (none if a gating rule makes the choice)
+        const int rounds = logits ? 0 : ((k < E) ? k + 1 : k);
         float prev = 0.f;
         uint8_t flag = 0;
         for (int j = 0; j < rounds; ++j) {
@@ -160,7 +167,7 @@ route_kernel(const bf16* __restrict__ x, const int32_t* __restrict__ tenant_id, 
                 for (int c = 0; c < kMaxChunks; ++c) if (c == (bi >> 5)) p[c] = -1.f;   // taken
             }
         }
-        if (tie_flag && lane == 0) tie_flag[t] = flag;
+        if (tie_flag && !logits && lane == 0) tie_flag[t] = flag;
         if (shared_gate) {
             float g = 0.f;
             const bf16* sg = models[model[i]].shared_gate_w;
@@ -186,12 +193,24 @@ cudaError_t launch_route(moe_ctx* c, int layer, const bf16* x, const int32_t* te
                          float* topk_w, float* shared_gate, uint8_t* tie_flag, cudaStream_t st)
 {
     const bool tc = c->route_path != MOE_PATH_FMA && route_tc_supported(c);      // (x is 16-byte aligned: checked at the ABI)
-    return tc ? launch_route_tc(c, layer, x, tenant_id, T, topk_idx, topk_w, shared_gate, tie_flag, st)
-              : launch_route_fma(c, layer, x, tenant_id, T, topk_idx, topk_w, shared_gate, tie_flag, st);
+    const LayerGating& rule = c->gating[layer];
+    float* logits = rule.on ? c->d_logits : nullptr;
+    const cudaError_t e = tc ? launch_route_tc(c, layer, x, tenant_id, T, topk_idx, topk_w, shared_gate, tie_flag, logits, st)
+                             : launch_route_fma(c, layer, x, tenant_id, T, topk_idx, topk_w, shared_gate, tie_flag, logits, st);
+    if (e != cudaSuccess || !rule.on) return e;
+    // a layer with a gating rule: the router has left its logits, the rule makes the choice
+    const moe_config& g = c->cfg;
+    GateArgs a = {};
+    a.logits = logits; a.ld = g.n_experts; a.T = T; a.E = g.n_experts; a.k = g.top_k;
+    apply_gating(a, rule.rule);
+    a.bias = rule.bias; a.tenant_id = tenant_id; a.model_of_tenant = c->d_model_of_tenant; a.n_tenants = g.n_tenants; a.M = g.n_models;
+    a.topk_idx = topk_idx; a.topk_w = topk_w; a.tie_flag = tie_flag; a.status = c->ws.status;
+    c->launches += 1;
+    return launch_gate(a, st);
 }
 
 cudaError_t launch_route_fma(moe_ctx* c, int layer, const bf16* x, const int32_t* tenant_id, int T, int32_t* topk_idx,
-                             float* topk_w, float* shared_gate, uint8_t* tie_flag, cudaStream_t st)
+                             float* topk_w, float* shared_gate, uint8_t* tie_flag, float* logits, cudaStream_t st)
 {
     const moe_config& g = c->cfg;
     const ModelWeights* models = c->d_models + (size_t)layer * g.n_models;
@@ -205,11 +224,11 @@ cudaError_t launch_route_fma(moe_ctx* c, int layer, const bf16* x, const int32_t
     if (small) {
         cudaFuncSetAttribute(route_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         route_kernel<1><<<blocks, kRouteWarps * 32, smem, st>>>(x, tenant_id, T, g.hidden, g.n_experts, g.top_k,
-            g.n_tenants, g.n_models, c->d_model_of_tenant, models, topk_idx, topk_w, shared_gate, tie_flag, c->ws.status);
+            g.n_tenants, g.n_models, c->d_model_of_tenant, models, topk_idx, topk_w, shared_gate, tie_flag, logits, c->ws.status);
     } else {
         cudaFuncSetAttribute(route_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         route_kernel<4><<<blocks, kRouteWarps * 32, smem, st>>>(x, tenant_id, T, g.hidden, g.n_experts, g.top_k,
-            g.n_tenants, g.n_models, c->d_model_of_tenant, models, topk_idx, topk_w, shared_gate, tie_flag, c->ws.status);
+            g.n_tenants, g.n_models, c->d_model_of_tenant, models, topk_idx, topk_w, shared_gate, tie_flag, logits, c->ws.status);
     }
     c->launches += 1;
     return cudaGetLastError();

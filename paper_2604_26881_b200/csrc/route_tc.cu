@@ -52,6 +52,7 @@ struct RouteParams {
     float* topk_w;
     float* shared_gate;
     uint8_t* tie_flag;
+    float* logits;                 // [T, E] or null: the logits are stored and the choice is left to the gating-rule kernel
     int32_t* status;
 };
 
@@ -290,7 +291,11 @@ route_tc_kernel(const RouteParams p, const __grid_constant__ RouteMaps maps, con
                     if (m == model && valid && p.models[m].shared_gate_w) gate = 1.f / (1.f + expf(-gl));
                 }
             }
-            if (valid) {
+            if (valid && p.logits) {
+#pragma unroll
+                for (int e = 0; e < kRMaxE; ++e) if (e < p.E) p.logits[(size_t)t * p.E + e] = z[e];
+                if (p.shared_gate) p.shared_gate[t] = bad ? 0.f : gate;
+            } else if (valid) {
                 // Softmax is monotone, so the ranking is done on the logits themselves; the
                 // probabilities are exp2((z - zmax) * log2 e) / sum.  Four independent chains keep
                 // the one warp per scheduler busy.
@@ -385,7 +390,7 @@ void route_tc_destroy(moe_ctx* c)
 }
 
 cudaError_t launch_route_tc(moe_ctx* c, int layer, const bf16* x, const int32_t* tenant_id, int T, int32_t* topk_idx,
-                            float* topk_w, float* shared_gate, uint8_t* tie_flag, cudaStream_t st,
+                            float* topk_w, float* shared_gate, uint8_t* tie_flag, float* logits, cudaStream_t st,
                             const SmallDispatchArgs* fused, size_t fused_smem)
 {
     const moe_config& g = c->cfg;
@@ -432,6 +437,7 @@ cudaError_t launch_route_tc(moe_ctx* c, int layer, const bf16* x, const int32_t*
     p.models = c->d_models + (size_t)layer * M;
     p.gate_mma = (shared_gate && rm->gate_mma[layer]) ? 1 : 0;
     p.topk_idx = topk_idx; p.topk_w = topk_w; p.shared_gate = shared_gate; p.tie_flag = tie_flag;
+    p.logits = logits;
     p.status = c->ws.status;
     p.a_bytes = (a_rows * kRBK * 2 + 1023) & ~1023;
     // several models: a CTA per (token tile, model) computes that model's logits only (4x the CTAs for a quarter of

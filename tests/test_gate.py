@@ -1,0 +1,388 @@
+"""Gating rules (moe_gate, moe_set_gating) against a plain statement of the rules in 64 bits.
+
+The choice is defined in double precision, so the expert ids must be equal wherever the 64-bit values of two experts are not
+within a few double ulps of each other (random fp32 inputs never are).  Weights are fp32: an exponential (2 ulp), a sum of
+at most 8 + 5 terms, a quotient and a product, below 32 roundings of 2^-24 relative; the argument z - ref of the exponential is
+rounded too, which costs 2^-24 |z - ref| relative (at most 40 units for the logits used here where a weight matters).
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from harness import GpuLayer
+from paper_2604_26881_b200 import binding as B
+from paper_2604_26881_b200 import workloads as W
+
+FMAX = float(np.finfo(np.float32).max)
+W_RTOL = 2.0 ** -24 * (32 + 40)
+
+
+def reference(z, k, *, score, n_groups=1, keep=1, group_score="max", renorm=False, scale=1.0, bias=None):
+    """One row at a time, as the rules read.  z [T, E] float64; bias [T, E] or None.  (idx [T, k], w [T, k])."""
+    T, E = z.shape
+    idx, w = np.zeros((T, k), np.int64), np.zeros((T, k))
+    size = E // n_groups
+    for t in range(T):
+        zt = np.where(np.isnan(z[t]), -np.inf, np.minimum(z[t], FMAX))
+        with np.errstate(over="ignore", under="ignore", invalid="ignore"):
+            if score == "softmax":
+                s = np.where(np.isneginf(zt), 0.0, np.exp(zt - zt.max()))
+                s = s / s.sum() if s.sum() > 0 else s
+            else:
+                s = np.where(zt >= 0, 1 / (1 + np.exp(-np.abs(zt))), np.exp(-np.abs(zt)) / (1 + np.exp(-np.abs(zt))))
+        v = zt if bias is None else s + np.where(np.isnan(bias[t]), -np.inf, bias[t])
+        vg = v if bias is not None or group_score == "max" or size == 1 else s
+        groups = []
+        for g in range(n_groups):
+            best = sorted(vg[g * size:(g + 1) * size], reverse=True)
+            groups.append(best[0] + (best[1] if group_score == "top2" and size > 1 else 0.0))
+        kept = sorted(range(n_groups), key=lambda g: (-groups[g], g))[:keep]
+        allowed = [e for e in range(E) if e // size in kept]
+        chosen = sorted(allowed, key=lambda e: (-v[e], e))[:k]
+        idx[t] = chosen
+        if renorm:
+            # relative to the largest chosen score, so that nothing underflows
+            zc = zt[chosen]
+            logs = zc if score == "softmax" else -np.logaddexp(0.0, -zc)
+            if np.isneginf(logs).all():
+                continue
+            x = np.exp(logs - logs.max())
+            w[t] = x / x.sum() * scale
+        else:
+            w[t] = s[chosen] * scale
+    return idx, w
+
+
+def run(z, k, dev="cuda:0", bias=None, tenant=None, mot=None, dtype=torch.float32, pad=0, tie=False, **rule):
+    T, E = z.shape
+    full = torch.full((T, E + pad), 9.0, dtype=dtype, device=dev)
+    full[:, :E] = torch.as_tensor(z, dtype=torch.float64).to(dtype).to(dev)
+    n = 64
+    idx_flat = torch.full((T * k + n,), -7, dtype=torch.int32, device=dev)
+    w_flat = torch.full((T * k + n,), -7.0, dtype=torch.float32, device=dev)
+    idx, w = idx_flat[:T * k].view(T, k), w_flat[:T * k].view(T, k)
+    flag = torch.full((T,), 9, dtype=torch.uint8, device=dev) if tie else None
+    status = torch.zeros(1, dtype=torch.int32, device=dev)
+    r = B.moe_gating(score=rule.get("score", "softmax"), n_groups=rule.get("n_groups", 1), keep_groups=rule.get("keep", 1),
+                     group_score=rule.get("group_score", "max"), renormalize=rule.get("renorm", False), scale=rule.get("scale", 1.0))
+    as_dev = lambda t, d: None if t is None else torch.as_tensor(t).to(d).to(dev)
+    B.moe_gate(full[:, :E], r, idx, w, balance_bias=as_dev(bias, torch.float32), tenant_id=as_dev(tenant, torch.int32),
+               model_of_tenant=as_dev(mot, torch.int32), tie_flag=flag, status_out=status)
+    torch.cuda.synchronize()
+    assert (idx_flat[T * k:] == -7).all() and (w_flat[T * k:] == -7).all(), "written past the end"
+    return idx.cpu().numpy(), w.double().cpu().numpy(), (flag.cpu().numpy() if tie else None), int(status.item())
+
+
+def check(z, k, bias=None, dtype=torch.float32, pad=0, **rule):
+    zr = torch.as_tensor(z, dtype=torch.float64).to(dtype).double().numpy()
+    br = None if bias is None else np.broadcast_to(torch.as_tensor(bias).float().double().numpy().reshape(1, -1), zr.shape)
+    scale = float(np.float32(rule.get("scale", 1.0)))
+    ref_idx, ref_w = reference(zr, k, bias=br, **{**rule, "scale": scale})
+    idx, w, _, status = run(z, k, bias=None if bias is None else np.asarray(bias).reshape(1, -1), dtype=dtype, pad=pad, **rule)
+    assert status == 0
+    bad = np.nonzero((idx != ref_idx).any(1))[0]
+    assert bad.size == 0, f"{bad.size} rows differ, first {bad[:3]}: got {idx[bad[:3]]}, want {ref_idx[bad[:3]]}"
+    np.testing.assert_allclose(w, ref_w, rtol=W_RTOL, atol=1e-37)
+    return idx
+
+
+gpu = pytest.mark.gpu
+RULES = [
+    dict(score="softmax"),
+    dict(score="softmax", renorm=True, scale=2.5),
+    dict(score="sigmoid", renorm=True),
+    dict(score="sigmoid", scale=0.5),
+]
+
+
+@gpu
+@pytest.mark.parametrize("E,k", [(1, 1), (2, 2), (7, 3), (8, 8), (60, 4), (63, 8), (64, 1), (65, 8), (100, 5), (128, 8), (129, 2), (200, 8), (255, 8), (256, 8)])
+@pytest.mark.parametrize("with_bias", [False, True])
+def test_every_router_width(E, k, with_bias):
+    g = np.random.default_rng(E * 10 + k)
+    z = g.standard_normal((37, E)) * 2
+    bias = g.standard_normal(E) * 0.1 if with_bias else None
+    for i, rule in enumerate(RULES):
+        check(z, k, bias=bias, pad=(0, 1, 4, 8)[i], **rule)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("E,n_groups,keep", [(256, 8, 4), (256, 32, 8), (256, 1, 1), (64, 8, 3), (60, 4, 2), (60, 12, 5), (252, 6, 3),
+                                             (32, 32, 9), (96, 3, 1), (248, 31, 30), (128, 2, 1), (16, 2, 2)])
+@pytest.mark.parametrize("group_score", ["max", "top2"])
+def test_groups(dtype, E, n_groups, keep, group_score):
+    g = np.random.default_rng(E + n_groups)
+    k = min(8, keep * (E // n_groups))
+    z = g.standard_normal((65, E))
+    for score in ("softmax", "sigmoid"):
+        for bias in (None, g.standard_normal(E) * 0.05):
+            check(z, k, bias=bias, dtype=dtype, score=score, n_groups=n_groups, keep=keep, group_score=group_score, renorm=True)
+
+
+@gpu
+@pytest.mark.parametrize("T", [0, 1, 2, 3, 4, 5, 127, 1000, 4099])
+def test_numbers_of_tokens(T):
+    g = np.random.default_rng(T)
+    z = g.standard_normal((T, 60))
+    if T == 0:
+        idx, w, _, _ = run(z, 4, score="softmax")
+        assert idx.shape == (0, 4)
+        return
+    check(z, 4, bias=g.standard_normal(60) * 0.1, score="sigmoid", n_groups=4, keep=2, group_score="top2", renorm=True)
+
+
+@gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_equal_values_take_the_lower_id(score, with_bias, dtype):
+    """Few distinct logits: nearly every neighbour is an exact tie, inside a lane, between lanes and at the k-th rank."""
+    g = np.random.default_rng(5)
+    for E, n_groups, keep in [(60, 1, 1), (256, 8, 3), (96, 6, 2)]:
+        z = g.integers(-2, 3, (50, E)).astype(float)
+        z[0] = 0.0
+        z[1] = -0.0
+        z[2, ::2] = 0.0
+        z[2, 1::2] = -0.0
+        bias = np.full(E, 0.25) if with_bias else None
+        check(z, 8, bias=bias, dtype=dtype, score=score, n_groups=n_groups, keep=keep, renorm=True)
+        if with_bias:
+            check(z, 8, bias=g.integers(0, 2, E) * 0.5, dtype=dtype, score=score, n_groups=n_groups, keep=keep, renorm=True)
+
+
+@gpu
+def test_order_is_decided_in_64_bits():
+    """Pairs whose values differ by less than fp32 can hold: v = sigmoid(z) + b with b stepping by one fp32 ulp of 1."""
+    g = np.random.default_rng(9)
+    T, E = 64, 256
+    z = np.zeros((T, E))
+    z += g.integers(0, 4, (T, E)) * 1e-7
+    bias = 1.0 + g.integers(0, 3, E) * 2.0 ** -23
+    for score in ("sigmoid", "softmax"):
+        check(z, 8, bias=bias, score=score, n_groups=8, keep=3, group_score="top2")
+        check(z, 8, bias=bias, score=score)
+    # neighbouring fp32 logits without a bias
+    base = np.float32(1.5)
+    steps = g.integers(0, 30, (T, E))
+    zz = (base + steps * np.spacing(base)).astype(np.float64)
+    check(zz, 8, score="sigmoid")
+    check(zz, 8, score="softmax", n_groups=8, keep=2)
+
+
+@gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renorm", [False, True])
+def test_masked_and_extreme_logits(score, renorm):
+    g = np.random.default_rng(3)
+    E, k = 60, 4
+    z = g.standard_normal((16, E))
+    z[0] = -np.inf                                  # nothing is left
+    z[1, :] = -np.inf
+    z[1, [7, 33]] = [0.5, 1.5]                      # fewer than k are left
+    z[2, ::2] = -np.inf
+    z[3, ::3] = -FMAX                               # the lowest finite value as a mask
+    z[4, :] = -FMAX
+    z[5, 10] = np.nan
+    z[5, 11] = 50.0
+    z[6, :] = np.nan
+    z[7, 20] = np.inf
+    z[8, [3, 30]] = np.inf
+    z[9] = 1e30 * np.sign(z[9])
+    z[10] = -200.0 + z[10]                          # scores below the smallest fp32 number
+    z[11] = 200.0 + z[11]
+    z[12] = z[12] * 1e-42                           # denormal logits
+    z[13, 5:] = -np.inf
+    z[14] = -1000.0
+    z[15, :] = -np.inf
+    z[15, 59] = -FMAX
+    check(z, k, score=score, renorm=renorm)
+    check(z, k, score=score, renorm=renorm, n_groups=6, keep=3)
+    check(z, k, score=score, renorm=renorm, n_groups=6, keep=3, bias=g.standard_normal(E) * 0.1, group_score="top2")
+    bias = g.standard_normal(E) * 0.1
+    bias[[4, 9]] = -np.inf
+    bias[12] = np.nan
+    check(z, k, score=score, renorm=renorm, bias=bias)
+
+
+@gpu
+def test_models_and_bad_tenants():
+    g = np.random.default_rng(11)
+    T, E, M, k = 130, 60, 3, 4
+    z = g.standard_normal((T, E))
+    tenant = g.integers(0, 6, T)
+    mot = np.arange(6) % M
+    bias = g.standard_normal((M, E)) * 0.3
+    rule = dict(score="sigmoid", renorm=True, n_groups=4, keep=2, group_score="top2")
+    tenant[[5, 90]] = [-1, 6]
+    idx, w, _, status = run(z, k, bias=bias, tenant=tenant, mot=mot, **rule)
+    assert status == B.MOE_DEV_BAD_TENANT
+    safe = np.where((tenant < 0) | (tenant >= 6), 0, tenant)
+    ref_idx, ref_w = reference(z.astype(np.float32).astype(float), k, bias=bias.astype(np.float32).astype(float)[mot[safe]], **rule)
+    ok = (tenant >= 0) & (tenant < 6)
+    assert np.array_equal(idx[ok], ref_idx[ok])
+    np.testing.assert_allclose(w[ok], ref_w[ok], rtol=W_RTOL)
+    assert (idx[~ok] == np.arange(k)).all() and (w[~ok] == 0).all()
+
+
+@gpu
+def test_tie_flag():
+    z = np.linspace(-3, 3, 60)[None].repeat(3, 0).copy()
+    z[1, 57] = z[1, 58]                     # ranks 2 and 3 equal
+    z[2, 0] = z[2, 1]                       # equal far behind the choice
+    for score in ("softmax", "sigmoid"):
+        _, _, flag, _ = run(z, 4, tie=True, score=score)
+        assert flag.tolist() == [0, 1, 0]
+
+
+@gpu
+def test_graph_stream_and_repeated_calls_agree():
+    g = np.random.default_rng(2)
+    dev = torch.device("cuda:0")
+    T, E, k = 513, 256, 8
+    z = torch.from_numpy(g.standard_normal((T, E))).float().to(dev)
+    bias = torch.from_numpy(g.standard_normal((1, E)) * 0.05).float().to(dev)
+    rule = B.moe_gating(score="sigmoid", n_groups=8, keep_groups=4, group_score="top2", renormalize=True)
+    mk = lambda: (torch.empty(T, k, dtype=torch.int32, device=dev), torch.empty(T, k, device=dev))
+    a, b, c = mk(), mk(), mk()
+    B.moe_gate(z, rule, *a, balance_bias=bias)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    B.moe_gate(z, rule, *b, balance_bias=bias, stream=side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.moe_gate(z, rule, *c, balance_bias=bias)
+    graph.replay()
+    torch.cuda.synchronize()
+    for o in (b, c):
+        assert torch.equal(a[0], o[0]) and torch.equal(a[1], o[1])
+    z2 = z.roll(1, 0).contiguous()
+    z.copy_(z2)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(c[0], a[0].roll(1, 0)) and torch.equal(c[1], a[1].roll(1, 0))
+
+
+def _layer(E, k, M, T, seed=0, Is=128, H=256):
+    wl = W.MoEWorkload("rule", T=T, H=H, E=E, I=128, k=k, Is=Is, M=M, n_tenants=2 * M, G=3, zipf_bias=True, tenant_layout="uniform")
+    return wl, W.make_weights(wl, seed=seed)
+
+
+@gpu
+@pytest.mark.parametrize("E,M,path", [(60, 1, B.MOE_PATH_AUTO), (12, 3, B.MOE_PATH_AUTO), (60, 2, B.MOE_PATH_FMA), (96, 1, B.MOE_PATH_AUTO)])
+def test_layer_with_a_rule(E, M, path):
+    """moe_set_gating: the layer's own logits, then the rule.  The router without a rule (raw softmax) gives the logits' order
+    of the same kernels; the rule's choice is checked against the 64-bit rule wherever fp32 logits decide it."""
+    T, k = 200, 4
+    wl, wts = _layer(E, k, M, T)
+    x, tenant, mot = W.make_tokens(wl, seed=1)
+    gl = GpuLayer(wl, [wts], max_tokens=T, model_of_tenant=mot)
+    try:
+        B.moe_set_option(gl.ctx, B.MOE_OPT_ROUTE_PATH, path)
+        G = 3
+        before = gl.forward(x, tenant, G)
+        dev = gl.dev
+        bias = (torch.randn(M, E, generator=torch.Generator().manual_seed(4)) * 0.1)
+        n_groups, keep = (4, 2)
+        rule = B.moe_gating(score="sigmoid", n_groups=n_groups, keep_groups=keep, group_score="top2", renormalize=True, scale=1.5)
+        bias_dev = bias.to(dev)
+        B.moe_set_gating(gl.ctx, 0, rule, bias_dev)
+        o = gl.four_calls(x, tenant, G)
+        assert o["status"] == 0
+        # logits in 64 bits from the exact bf16 values
+        model = mot.long()[tenant.long()]
+        z = torch.einsum("th,teh->te", x.double(), wts["router_w"].double()[model]) + wts["router_bias"].double()[model]
+        bt = bias.double()[model].numpy()
+        s = torch.sigmoid(z).numpy() + bt
+        ref_idx, ref_w = reference(z.numpy(), k, score="sigmoid", n_groups=n_groups, keep=keep, group_score="top2", renorm=True,
+                                   scale=1.5, bias=bt)
+        # fp32 logits: H products summed in fp32, |z| of a few units: 1e-4 is far above their error; rows without a
+        # closer call anywhere among their values and group scores must agree
+        size = E // n_groups
+        srt = np.sort(s, 1)
+        grp = np.sort(np.sort(s.reshape(T, n_groups, size), 2)[:, :, -2:].sum(2), 1)
+        clear = (np.diff(srt, axis=1)[:, -3 * k:].min(1) > 1e-4) & (np.diff(grp, axis=1).min(1) > 2e-4)
+        idx = o["topk_idx"].cpu().numpy()
+        assert clear.sum() > T // 4
+        assert np.array_equal(idx[clear], ref_idx[clear])
+        np.testing.assert_allclose(o["topk_w"].cpu().numpy()[clear], ref_w[clear], rtol=1e-3)
+        # the whole layer runs on it: fused call = four calls, bit for bit
+        out = gl.forward(x, tenant, G)
+        assert torch.equal(out, o["out"])
+        assert not torch.equal(out, before)
+        # every token's weights sum to the scale
+        torch.testing.assert_close(o["topk_w"].sum(1).cpu(), torch.full((T,), 1.5), rtol=1e-5, atol=0)
+        # and back: the layer's own rule, the same bits as before
+        B.moe_set_gating(gl.ctx, 0, None)
+        assert torch.equal(gl.forward(x, tenant, G), before)
+    finally:
+        gl.close()
+
+
+@gpu
+def test_softmax_rule_without_anything_is_the_layers_own_rule():
+    T = 300
+    wl, wts = _layer(60, 4, 1, T)
+    x, tenant, mot = W.make_tokens(wl, seed=2)
+    gl = GpuLayer(wl, [wts], max_tokens=T, model_of_tenant=mot)
+    try:
+        a = gl.four_calls(x, tenant, 3)
+        B.moe_set_gating(gl.ctx, 0, B.moe_gating(score="softmax"))
+        b = gl.four_calls(x, tenant, 3)
+        assert torch.equal(a["topk_idx"], b["topk_idx"])
+        torch.testing.assert_close(a["topk_w"], b["topk_w"], rtol=2e-6, atol=0)
+        assert torch.equal(a["shared_gate"], b["shared_gate"])
+    finally:
+        gl.close()
+
+
+def _raw(**kw):
+    """moe_gate's C arguments; pointers are never followed by a refused call."""
+    a = dict(logits=64, type=0, ld=8, T=4, E=8, k=2, rule=B.moe_gating(), bias=None, tenant=None, mot=None, n_tenants=1, M=1, idx=64,
+             w=64, tie=None, status=None)
+    a.update(kw)
+    rule = a["rule"]
+    return B.load_library().moe_gate(a["logits"], a["type"], a["ld"], a["T"], a["E"], a["k"], ctypes.byref(rule) if rule else None,
+                                     a["bias"], a["tenant"], a["mot"], a["n_tenants"], a["M"], a["idx"], a["w"], a["tie"], a["status"], None)
+
+
+def test_refusals_need_no_gpu():
+    assert _raw(logits=None) == B.MOE_ERR_NULL
+    assert _raw(rule=None) == B.MOE_ERR_NULL
+    assert _raw(idx=None) == B.MOE_ERR_NULL
+    assert _raw(w=None) == B.MOE_ERR_NULL
+    assert _raw(M=2, tenant=None) == B.MOE_ERR_NULL
+    for bad in (dict(T=-1), dict(E=0, ld=0), dict(E=257, ld=257), dict(k=0), dict(k=9, E=64, ld=64), dict(k=3, E=2, ld=2), dict(ld=7), dict(M=0),
+                dict(M=257, tenant=64, mot=64), dict(tenant=64, n_tenants=0), dict(logits=66), dict(idx=66), dict(w=65), dict(status=2),
+                dict(bias=66), dict(type=1, logits=65)):
+        assert _raw(**bad) == B.MOE_ERR_SHAPE, bad
+    assert _raw(type=7) == B.MOE_ERR_UNSUPPORTED
+    for rule in (B.moe_gating(n_groups=3), B.moe_gating(n_groups=0, keep_groups=0), B.moe_gating(n_groups=4, keep_groups=5),
+                 B.moe_gating(n_groups=4, keep_groups=0), B.moe_gating(scale=math.inf), B.moe_gating(scale=math.nan), B.MoeGating(2, 1, 1, 0, 0, 1.0),
+                 B.MoeGating(0, 1, 1, 2, 0, 1.0)):
+        assert _raw(rule=rule) == B.MOE_ERR_SHAPE
+    assert _raw(rule=B.moe_gating(n_groups=8, keep_groups=1), k=2) == B.MOE_ERR_SHAPE      # one expert is left for k = 2
+    assert _raw(rule=B.moe_gating(n_groups=64, keep_groups=64), E=64, ld=64) == B.MOE_ERR_SHAPE
+    assert _raw(T=0) == B.MOE_OK
+    assert B.load_library().moe_set_gating(None, 0, None, None) == B.MOE_ERR_NULL
+
+
+def test_binding_checks_tensors():
+    z, idx, w = torch.zeros(4, 8), torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2)
+    rule = B.moe_gating()
+    with pytest.raises(ValueError, match="CUDA"):
+        B.moe_gate(z, rule, idx, w)
+    for bad in (dict(logits=z.double()), dict(logits=z.t()), dict(topk_idx=idx.long()), dict(topk_w=w[:3]), dict(logits=z[0]), dict(rule=None)):
+        a = dict(logits=z, rule=rule, topk_idx=idx, topk_w=w)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            B.moe_gate(a["logits"], a["rule"], a["topk_idx"], a["topk_w"])
+    with pytest.raises(ValueError):
+        B.moe_gate(z, rule, idx, w, balance_bias=torch.zeros(1, 7))
+    with pytest.raises(ValueError):
+        B.moe_gate(z, rule, idx, w, tenant_id=torch.zeros(4))
+    with pytest.raises(KeyError):
+        B.moe_gating(score="tanh")
