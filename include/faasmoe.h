@@ -58,6 +58,7 @@ enum {
 enum {
     MOE_DEV_BAD_TENANT = 1,   /* tenant id outside [0, n_tenants): the token's output is zero */
     MOE_DEV_BAD_EXPERT = 2,   /* expert id outside [0, n_experts) in a caller-supplied topk_idx */
+    MOE_DEV_BAD_ADAPTER = 4,  /* adapter_of_tenant entry >= n_adapters: the token is served without an adapter */
     MOE_DEV_TIMEOUT = 8       /* a bounded wait inside a kernel ran out; outputs are invalid */
 };
 
@@ -366,6 +367,33 @@ int moe_set_gating(moe_ctx* ctx, int layer, const moe_gating* rule, const float*
 int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld_residual, const void* weight, float eps,
                     int T, int H, void* residual_out, int64_t ld_residual_out, void* out, int64_t ld_out, void* out_q,
                     int64_t ld_q, float* q_scale, int group, void* stream);
+
+/*
+ * A projection that all tenants share, with each tenant's own low-rank adapter beside it, without a context:
+ *   out[t] = base[t] + x[t] . w^T + scale[a] * (x[t] . a[a]^T) . b[a]^T,    a = adapter_of_tenant[tenant_id[t]]
+ * for all tokens of a batch in one call, in whatever order their tenants come.  bf16 operands, fp32 sums (the inner product of
+ * an adapter stays fp32, or a pair of bf16 numbers that hold 16 bits of it), one rounding to out's type.
+ *   x      bf16 [T, K], rows ldx apart            w      bf16 [N, K], rows ldw apart, or NULL (no product with w)
+ *   base   [T, N] of out's type, rows ld_base apart, or NULL; may be out itself (same row distance)
+ *   a      bf16 [n_adapters, rank, K]             b      bf16 [n_adapters, N, rank]         scale f32 [n_adapters] or NULL (1)
+ *   tenant_id int32 [T];  adapter_of_tenant int32 [n_tenants] (DEVICE; a negative entry: no adapter) or NULL (tenant u uses
+ *          adapter u, none if u >= n_adapters)
+ *   out    f32 or bf16 (out_type) [T, N], rows ld_out apart
+ *   workspace  moe_project_workspace() bytes of device memory, 256-byte aligned, that no other call uses meanwhile
+ *   status_out device int32 or NULL: MOE_DEV_BAD_TENANT (tenant id outside [0, n_tenants): no adapter), MOE_DEV_BAD_ADAPTER and
+ *          MOE_DEV_TIMEOUT are OR-ed into it; the caller clears it
+ * n_adapters = 0: no adapters; a, b, scale, tenant_id, adapter_of_tenant and n_tenants are not looked at.
+ * K a multiple of 8; rank a multiple of 8 up to 128 (adapters of a smaller rank are padded with zeros); ldx and ldw multiples
+ * of 8; x, w, a and b 16-byte aligned; T <= 2^22.  out may not overlap x, w, a or b.  The results depend on the shapes, not
+ * on what else runs: the sums have a fixed order.
+ */
+int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, int K, int N, const void* a, const void* b,
+                const float* scale, int n_adapters, int rank, const int32_t* tenant_id, const int32_t* adapter_of_tenant,
+                int n_tenants, const void* base, int64_t ld_base, void* out, int64_t ld_out, int out_type, void* workspace,
+                int64_t workspace_bytes, int32_t* status_out, void* stream);
+
+/* Bytes of device memory that moe_project needs for T tokens (negative: MOE_ERR_SHAPE). */
+int64_t moe_project_workspace(int T, int K, int rank, int n_adapters);
 
 /* route -> dispatch -> experts -> combine on the context's workspace; bit-identical to
  * the four calls above.  out bf16 [T,H]. */

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_HERE, "lib", "libfaasmoe.so")
 MOE_OK = 0
 MOE_ERR_NULL, MOE_ERR_SHAPE, MOE_ERR_G, MOE_ERR_STATE = -1, -2, -3, -4
 MOE_ERR_CUDA, MOE_ERR_ALLOC, MOE_ERR_UNSUPPORTED = -5, -6, -7
-MOE_DEV_BAD_TENANT, MOE_DEV_BAD_EXPERT, MOE_DEV_TIMEOUT = 1, 2, 8
+MOE_DEV_BAD_TENANT, MOE_DEV_BAD_EXPERT, MOE_DEV_BAD_ADAPTER, MOE_DEV_TIMEOUT = 1, 2, 4, 8
 MOE_OPT_EXPERT_PATH = 1
 MOE_OPT_ROUTE_PATH = 2
 MOE_OPT_PAIR_MODE = 3
@@ -42,7 +42,8 @@ EXPORTS = ["moe_create", "moe_destroy", "moe_set_expert_pool", "moe_set_model_we
            "moe_set_tenant_models", "moe_set_option", "moe_form_blocks", "moe_set_block_table", "moe_route", "moe_dispatch", "moe_experts", "moe_combine",
            "moe_layer_forward", "moe_residency_enable", "moe_layer_forward_paged", "moe_layer_forward_host", "moe_layer_forward_host_submit", "moe_layer_forward_host_wait", "moe_layer_forward_timed", "moe_stack_forward",
            "moe_get_workspace", "moe_last_status", "moe_last_plan", "moe_launch_count", "moe_strerror", "moe_dispatch_noalloc",
-           "moe_gate", "moe_set_gating", "moe_add_rmsnorm"]
+           "moe_gate", "moe_set_gating", "moe_add_rmsnorm",
+           "moe_project", "moe_project_workspace"]
 MOE_DISPATCH_NOALLOC_MAX_WORDS = 1 << 18
 
 STAGES = ["route", "dispatch", "plan", "experts_gateup", "experts_down", "combine"]
@@ -112,6 +113,11 @@ def load_library(path: str | None = None):
         lib.moe_set_gating.argtypes = [c_void_p, c_int, POINTER(MoeGating), c_void_p]
         lib.moe_add_rmsnorm.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_float, c_int, c_int, c_void_p,
                                         c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int, c_void_p]
+        lib.moe_project.argtypes = ([c_void_p, c_int64, c_void_p, c_int64, c_int, c_int, c_int] + [c_void_p] * 3 + [c_int, c_int] +
+                                    [c_void_p] * 2 + [c_int, c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64] +
+                                    [c_void_p] * 2)
+        lib.moe_project_workspace.argtypes = [c_int, c_int, c_int, c_int]
+        lib.moe_project_workspace.restype = c_int64
         lib.moe_get_workspace.argtypes = [c_void_p] + [POINTER(c_void_p)] * 8
         lib.moe_last_status.argtypes = [c_void_p, POINTER(c_int32), POINTER(c_int32)]
         lib.moe_last_plan.argtypes = [c_void_p, c_int, POINTER(c_int32)]
@@ -415,6 +421,62 @@ def moe_add_rmsnorm(x, weight, eps, *, residual=None, residual_out=None, out=Non
         group = 0 if q_scale.shape[1] == 1 else 128       # (one group of at most 128 columns is the row)
     _call_on(dev, stream, fn, load_library().moe_add_rmsnorm, px, ldx, pr, ldr, _flat(weight, fn, "weight", H, torch.bfloat16, dev), eps,
              T, H, pro, ldro, po, ldo, pq, ldq, _flat(q_scale, fn, "q_scale", -1, torch.float32, dev), group)
+
+
+_OUT_TYPES = {torch.float32: MOE_TYPE_F32, torch.bfloat16: MOE_TYPE_BF16}
+
+
+def moe_project_workspace(T, K, rank=0, n_adapters=0) -> int:
+    """Bytes of workspace that moe_project needs."""
+    n = load_library().moe_project_workspace(T, K, rank, n_adapters)
+    if n < 0:
+        raise MoeError("moe_project_workspace", n)
+    return n
+
+
+def moe_project(x, w, out, *, base=None, a=None, b=None, scale=None, tenant_id=None, adapter_of_tenant=None, n_tenants=None,
+                workspace=None, status_out=None, stream=None):
+    """out = base + x . w^T + scale[a] * (x . a[a]^T) . b[a]^T with a = the adapter of each token's tenant.
+
+    x bf16 [T, K], w bf16 [N, K] or None, out float32 or bf16 [T, N], base like out or None: rows may be strided.  a bf16
+    [n, rank, K], b bf16 [n, N, rank], scale float32 [n] or None; tenant_id int32 [T]; adapter_of_tenant int32 [n_tenants]
+    on the device (None: tenant u has adapter u; n_tenants then defaults to n).  workspace: uint8 tensor, by default
+    allocated for the call on its stream.  See include/faasmoe.h."""
+    fn, dev = "moe_project", x.device
+    _need(x.dim() == 2 and out.dim() == 2, fn, "x must be [T, K] and out [T, N]")
+    (T, K), N = x.shape, out.shape[1]
+    px, ldx = _matrix(x, fn, "x", T, K, _BF16, dev)
+    pw, ldw = _matrix(w, fn, "w", N, K, _BF16, dev)
+    po, ldo = _matrix(out, fn, "out", T, N, _OUT_TYPES, dev)
+    pb, ldb = _matrix(base, fn, "base", T, N, (out.dtype,), dev)
+    n = rank = 0
+    pa = pbb = ps = pt = pm = None
+    _need((a is None) == (b is None), fn, "a and b go together")
+    if a is not None:
+        _need(a.dim() == 3, fn, "a must be [n_adapters, rank, K]")
+        n, rank = a.shape[0], a.shape[1]
+        pa, pbb = _flat(a, fn, "a", n * rank * K, torch.bfloat16, dev), _flat(b, fn, "b", n * N * rank, torch.bfloat16, dev)
+        _need(a.shape[2] == K and b.dim() == 3 and b.shape[1] == N and b.shape[2] == rank, fn, f"a must be [n, rank, {K}] and b [n, {N}, rank]")
+        ps, pt = _flat(scale, fn, "scale", n, torch.float32, dev), _flat(tenant_id, fn, "tenant_id", T, torch.int32, dev)
+        pm = _flat(adapter_of_tenant, fn, "adapter_of_tenant", -1, torch.int32, dev)
+        if adapter_of_tenant is not None:
+            n_tenants = adapter_of_tenant.numel()
+        elif n_tenants is None:
+            n_tenants = n
+    lib = load_library()
+    if workspace is None:
+        size = lib.moe_project_workspace(T, K, rank, n)
+        if size > 0 and dev.type == "cuda":
+            if stream is None:
+                workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+            else:
+                with torch.cuda.stream(stream):
+                    workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+    pws, ws_bytes = None, 0
+    if workspace is not None:
+        pws, ws_bytes = _flat(workspace, fn, "workspace", -1, torch.uint8, dev), workspace.numel()
+    _call_on(dev, stream, fn, lib.moe_project, px, ldx, pw, ldw, T, K, N, pa, pbb, ps, n, rank, pt, pm, n_tenants or 0, pb, ldb, po, ldo,
+             _OUT_TYPES[out.dtype], pws, ws_bytes, _flat(status_out, fn, "status_out", 1, torch.int32, dev))
 
 
 def moe_get_workspace(ctx):

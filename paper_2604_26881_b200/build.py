@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "lib", "libfaasmoe.so")
 SOURCES = ["api.cu", "route.cu", "route_tc.cu", "dispatch.cu", "plan.cu", "experts_fma.cu", "experts_tc.cu", "combine.cu",
-           "gate.cu", "addnorm.cu", "operators.cu"]
+           "gate.cu", "addnorm.cu", "project.cu", "operators.cu"]
 
 
 def _newest_source_mtime() -> float:

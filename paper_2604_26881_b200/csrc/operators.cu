@@ -3,12 +3,14 @@
 
 #include "addnorm.cuh"
 #include "gate.cuh"
+#include "project.cuh"
 
 using namespace faasmoe;
 
 namespace {
 
 constexpr int kMaxRows = 1 << 28;
+constexpr int kProjectMaxTokens = 1 << 22;
 
 bool off(const void* p, size_t align) { return ((uintptr_t)p & (align - 1)) != 0; }
 
@@ -80,6 +82,46 @@ int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld
     a.ldq = out_q ? ld_q : 0;
     a.group = group; a.n_groups = group ? (H + group - 1) / group : 1; a.T = T; a.H = H; a.eps = eps;
     return cuda_result("moe_add_rmsnorm", launch_addnorm(a, (cudaStream_t)stream));
+}
+
+int64_t moe_project_workspace(int T, int K, int rank, int n_adapters)
+{
+    if (T < 0 || T > kProjectMaxTokens || K < 1 || n_adapters < 0) return MOE_ERR_SHAPE;
+    if (n_adapters > 0 && (rank < 1 || rank > kAdapterMaxRank)) return MOE_ERR_SHAPE;
+    return project_workspace(T, K, rank, n_adapters);
+}
+
+int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, int K, int N, const void* a, const void* b,
+                const float* scale, int n_adapters, int rank, const int32_t* tenant_id, const int32_t* adapter_of_tenant,
+                int n_tenants, const void* base, int64_t ld_base, void* out, int64_t ld_out, int out_type, void* workspace,
+                int64_t workspace_bytes, int32_t* status_out, void* stream)
+{
+    const bool adapters = n_adapters > 0;
+    if (T < 0 || T > kProjectMaxTokens || K < 1 || N < 1 || n_adapters < 0 || ld_out < N || (base && ld_base < N)) return MOE_ERR_SHAPE;
+    if ((w || adapters) && ldx < K) return MOE_ERR_SHAPE;
+    if (w && ldw < K) return MOE_ERR_SHAPE;
+    if (adapters && (rank < 1 || rank > kAdapterMaxRank || n_tenants < 1)) return MOE_ERR_SHAPE;
+    if (out_type != MOE_TYPE_F32 && out_type != MOE_TYPE_BF16) return MOE_ERR_UNSUPPORTED;
+    // the operands travel as TMA tiles: rows on 16-byte boundaries
+    if (K % 8 || ((w || adapters) && ldx % 8) || (w && ldw % 8) || (adapters && rank % 8)) return MOE_ERR_UNSUPPORTED;
+    const size_t out_align = out_type == MOE_TYPE_F32 ? 4 : 2;
+    if (((w || adapters) && off(x, 16)) || off(w, 16) || off(out, out_align) || off(base, out_align) || off(status_out, 4)) return MOE_ERR_SHAPE;
+    if (adapters && (off(a, 16) || off(b, 16) || off(scale, 4) || off(tenant_id, 4) || off(adapter_of_tenant, 4))) return MOE_ERR_SHAPE;
+    if (off(workspace, 256)) return MOE_ERR_SHAPE;
+    if (T == 0) return MOE_OK;
+    if (!out || !workspace || (!w && !adapters && !base)) return MOE_ERR_NULL;
+    if (((w || adapters) && !x) || (adapters && (!a || !b || !tenant_id))) return MOE_ERR_NULL;
+    if (workspace_bytes < project_workspace(T, K, rank, n_adapters)) return MOE_ERR_ALLOC;
+    ProjectArgs p = {};
+    p.x = (const bf16*)x; p.w = (const bf16*)w; p.ldx = ldx; p.ldw = ldw; p.T = T; p.K = K; p.N = N;
+    if (adapters) {
+        p.a = (const bf16*)a; p.b = (const bf16*)b; p.scale = scale; p.n_adapters = n_adapters; p.rank = rank;
+        p.tenant_id = tenant_id; p.adapter_of_tenant = adapter_of_tenant; p.n_tenants = n_tenants;
+    }
+    p.base = base; p.ldbase = ld_base; p.out = out; p.ldo = ld_out; p.out_f32 = out_type == MOE_TYPE_F32;
+    p.workspace = (unsigned char*)workspace;
+    p.status = status_out ? status_out : (int32_t*)workspace;
+    return cuda_result("moe_project", launch_project(p, (cudaStream_t)stream));
 }
 
 }  // extern "C"

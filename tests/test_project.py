@@ -1,0 +1,331 @@
+"""moe_project (shared projection with the tenants' low-rank adapters) against the formula in 64 bits.
+
+Tolerances.  A sum over K on the tensor cores is rounded or cut at most once per 16 products and once per part of K that is
+added up: (K/16 + 16) * 2^-23 of the sum of the terms' absolute values.  An adapter's inner product u carries that error, the
+factor's rounding, and at most 2^-16 relative where it is held as a pair of bf16 numbers; the outer product adds (rank + 4)
+fp32 roundings.  The last addition and base: 3 * 2^-24 of the absolute values.  A bf16 output adds half a bf16 step (2^-8).
+All of it is propagated through the absolute values of the very inputs.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_26881_b200 import binding as B
+
+gpu = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def reference(x, w, base, a, b, scale, adapter):
+    """(y, error bound) in 64 bits; adapter [T] holds each token's adapter or -1."""
+    x = x.double()
+    K = x.shape[1]
+    T, N = x.shape[0], (w if w is not None else base if base is not None else b[0]).shape[0 if w is not None else 1 if base is not None else 0]
+    e_sum = (K / 16 + 16) * 2.0 ** -23
+    y = torch.zeros(T, N, dtype=torch.float64)
+    mag = torch.zeros(T, N, dtype=torch.float64)
+    err = torch.zeros(T, N, dtype=torch.float64)
+    if w is not None:
+        y += x @ w.double().t()
+        m = x.abs() @ w.double().abs().t()
+        mag += m
+        err += e_sum * m
+    if a is not None:
+        for i in sorted(set(adapter.tolist()) - {-1}):
+            t = adapter == i
+            s = 1.0 if scale is None else float(scale[i].double())
+            ai, bi = a[i].double(), b[i].double()
+            u, um = s * (x[t] @ ai.t()), abs(s) * (x[t].abs() @ ai.abs().t())
+            u_err = e_sum * um + (2.0 ** -16 + 2.0 ** -22) * u.abs()
+            y[t] += u @ bi.t()
+            m = (u.abs() + u_err) @ bi.abs().t()
+            mag[t] += m
+            err[t] += u_err @ bi.abs().t() + (ai.shape[0] + 4 + ai.shape[0] / 8) * 2.0 ** -23 * m
+    if base is not None:
+        y += base.double()
+        mag += base.double().abs()
+    return y, err + 3 * 2.0 ** -23 * mag
+
+
+def view(t, pad, fill=3.0):
+    """t on the device as the first columns of a wider matrix."""
+    if t is None:
+        return None
+    s = torch.full((t.shape[0], t.shape[1] + pad), fill, dtype=t.dtype, device=DEV)
+    s[:, :t.shape[1]] = t.to(DEV)
+    return s[:, :t.shape[1]]
+
+
+def inputs(T, K, N, rank, n, seed, weight=True, base=False, out=torch.bfloat16, scale=True):
+    g = torch.Generator().manual_seed(seed)
+    rnd = lambda *s, std=1.0: (torch.randn(*s, generator=g) * std).to(torch.bfloat16)
+    return dict(x=rnd(T, K), w=rnd(N, K, std=0.05) if weight else None, base=torch.randn(T, N, generator=g).to(out) if base else None,
+                a=rnd(n, rank, K, std=0.05) if n else None, b=rnd(n, N, rank, std=0.05) if n else None,
+                scale=(torch.rand(n, generator=g) + 0.5) if n and scale else None)
+
+
+def tenants(T, n_tenants, layout, seed):
+    g = np.random.default_rng(seed)
+    if layout == "uniform":
+        t = g.integers(0, n_tenants, T)
+    elif layout == "contiguous":
+        t = np.arange(T) * n_tenants // max(T, 1)
+    else:
+        t = np.sort(g.integers(0, n_tenants, T) ** 2 // n_tenants)
+    return torch.from_numpy(t.astype(np.int32))
+
+
+def check(T, K, N, rank=16, n=4, n_tenants=None, layout="uniform", out=torch.float32, pads=(0, 0, 0, 0), table="some", seed=0, mutate=None, **kw):
+    d = inputs(T, K, N, rank, n, seed + T + K + N, out=out, **kw)
+    if mutate:
+        mutate(d)
+    n_tenants = n_tenants or max(n, 1)
+    tenant = tenants(T, n_tenants, layout, seed)
+    mot = None
+    adapter = tenant.long()
+    if n and table:
+        mot = torch.tensor([(u * 7 + 1) % (n + 1) - 1 for u in range(n_tenants)], dtype=torch.int32)       # -1 now and then
+        adapter = mot.long()[adapter]
+    elif n:
+        adapter = torch.where(adapter < n, adapter, torch.full_like(adapter, -1))
+    y, err = reference(d["x"], d["w"], d["base"], d["a"], d["b"], d["scale"], adapter)
+    store = torch.full((T + 2, N + pads[3] + 3), 7.0, dtype=out, device=DEV)
+    o = store[1:T + 1, :N]
+    dev = lambda t: None if t is None else t.to(DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.moe_project(view(d["x"], pads[0], float("nan")), view(d["w"], pads[1], float("nan")), o, base=view(d["base"], pads[2]), a=dev(d["a"]), b=dev(d["b"]),
+                  scale=dev(d["scale"]), tenant_id=dev(tenant) if n else None, adapter_of_tenant=dev(mot), status_out=status,
+                  **({"n_tenants": n_tenants} if n and mot is None else {}))
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    keep = torch.ones_like(store, dtype=torch.bool)
+    keep[1:T + 1, :N] = False
+    assert (store[keep] == 7.0).all(), "written outside the output"
+    got = o.double().cpu()
+    assert torch.equal(got.isnan(), y.isnan()), "NaN where none belongs, or missing"
+    ok = y.isfinite() & err.isfinite()
+    lim = err + (2.0 ** -8 * (y.abs() + err) if out == torch.bfloat16 else 0) + 1e-30
+    bad = ((got - y).abs() > lim) & ok
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, worst {((got - y).abs() / lim)[ok].max():.2f} of the bound at {bad.nonzero()[0].tolist()}"
+    return o
+
+
+@gpu
+@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 31, 64, 65, 127, 128, 129, 255, 256, 257, 300, 513])
+@pytest.mark.parametrize("K,N", [(64, 128), (200, 129), (1024, 260)])
+def test_numbers_of_tokens(T, K, N):
+    check(T, K, N, out=torch.float32)
+    check(T, K, N, out=torch.bfloat16, base=True)
+
+
+@gpu
+@pytest.mark.parametrize("K,N", [(8, 1), (8, 300), (16, 127), (72, 64), (120, 255), (136, 256), (2048, 7), (2048, 1411), (5632, 130), (1408, 2048)])
+def test_shapes(K, N):
+    for T in (5, 140, 600):
+        check(T, K, N, rank=8)
+
+
+@gpu
+@pytest.mark.parametrize("rank", [8, 16, 24, 40, 64, 72, 104, 128])
+@pytest.mark.parametrize("n,layout", [(1, "uniform"), (3, "contiguous"), (40, "uniform"), (200, "uniform"), (17, "ragged")])
+def test_ranks_and_adapters(rank, n, layout):
+    for T in (1, 33, 130, 700):
+        check(T, 192, 200, rank=rank, n=n, layout=layout)
+        check(T, 320, 130, rank=rank, n=n, layout=layout, weight=False, base=True, table=None, n_tenants=n + 2)
+
+
+@gpu
+def test_parts_can_be_left_out():
+    for T in (3, 200, 1000):
+        check(T, 256, 256, n=0)
+        check(T, 256, 256, n=0, base=True, out=torch.bfloat16)
+        check(T, 256, 256, weight=False)
+        check(T, 256, 256, weight=False, scale=False, out=torch.bfloat16)
+        check(T, 256, 256, weight=False, n=0, base=True)
+        check(T, 256, 300, scale=False)
+
+
+@gpu
+@pytest.mark.parametrize("pads", [(8, 0, 0, 0), (0, 16, 3, 1), (40, 8, 1, 5), (8, 8, 8, 8)])
+def test_strides(pads):
+    for T in (17, 150, 520):
+        for out in (torch.float32, torch.bfloat16):
+            check(T, 136, 261, pads=pads, base=True, out=out)
+
+
+@gpu
+def test_long_batches_and_long_sums():
+    check(4096, 512, 512, rank=16, n=16, layout="ragged", out=torch.bfloat16)
+    check(2048, 2048, 1411, rank=64, n=13, layout="ragged", out=torch.float32)
+    check(1126, 5632, 2048, rank=16, n=4, layout="contiguous", out=torch.bfloat16)
+    check(3000, 256, 640, rank=32, n=200, layout="uniform", out=torch.float32)
+
+
+@gpu
+@pytest.mark.parametrize("T", [20, 130, 300, 900])
+def test_one_tenants_numbers_do_not_reach_another(T):
+    """Infinities and NaN in one adapter, in one token, in one row of w: they stay in their tokens and columns."""
+    def bad_adapter(d):
+        d["a"][1, 3, 5] = float("nan")
+        d["b"][2, 7, :] = float("inf")
+        d["b"][3, :, 0] = float("nan")
+
+    def bad_tokens(d):
+        d["x"][T // 2, 0] = float("nan")
+        d["x"][3, 4] = float("inf")
+
+    def bad_w(d):
+        d["w"][9, 1] = float("nan")
+    for layout in ("uniform", "contiguous"):
+        check(T, 128, 200, rank=16, n=5, layout=layout, mutate=bad_adapter)
+        check(T, 128, 200, rank=72, n=5, layout=layout, mutate=bad_adapter, weight=False)
+        check(T, 128, 200, rank=16, n=5, layout=layout, mutate=bad_tokens)
+        check(T, 128, 200, rank=16, n=5, layout=layout, mutate=bad_w)
+
+
+@gpu
+@pytest.mark.parametrize("T", [4, 40, 260])
+def test_bad_ids_are_reported_and_have_no_adapter(T):
+    d = inputs(T, 64, 96, 8, 3, seed=1)
+    tenant = torch.arange(T, dtype=torch.int32) % 5
+    table = torch.tensor([0, 3, -1, 2, -7], dtype=torch.int32)          # tenant 1 names an adapter that is not there
+    bad = tenant.clone()
+    bad[2] = 5
+    bad[0] = -1
+    adapter = table.long()[tenant.long()]
+    adapter[tenant == 1] = -1
+    adapter[adapter < 0] = -1
+    for ids, want in ((tenant, B.MOE_DEV_BAD_ADAPTER), (bad, B.MOE_DEV_BAD_ADAPTER | B.MOE_DEV_BAD_TENANT)):
+        ad = adapter.clone()
+        ad[(ids < 0) | (ids > 4)] = -1
+        y, err = reference(d["x"], d["w"], None, d["a"], d["b"], d["scale"], ad)
+        o = torch.empty(T, 96, device=DEV)
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        B.moe_project(d["x"].to(DEV), d["w"].to(DEV), o, a=d["a"].to(DEV), b=d["b"].to(DEV), scale=d["scale"].to(DEV), tenant_id=ids.to(DEV),
+                      adapter_of_tenant=table.to(DEV), status_out=status)
+        torch.cuda.synchronize()
+        assert int(status) == want
+        assert ((o.double().cpu() - y).abs() <= err).all()
+
+
+@gpu
+def test_no_tokens():
+    e = torch.empty(0, 64, dtype=torch.bfloat16, device=DEV)
+    B.moe_project(e, torch.zeros(32, 64, dtype=torch.bfloat16, device=DEV), torch.empty(0, 32, device=DEV))
+
+
+@gpu
+@pytest.mark.parametrize("T", [9, 200, 800])
+def test_base_in_place_streams_graphs_and_repeats(T):
+    d = inputs(T, 256, 320, 16, 6, seed=5, base=True, out=torch.float32)
+    tenant = tenants(T, 6, "uniform", 3).to(DEV)
+    g = {k: (v.to(DEV) if v is not None else None) for k, v in d.items()}
+    kw = dict(a=g["a"], b=g["b"], scale=g["scale"], tenant_id=tenant)
+    ref = torch.empty(T, 320, device=DEV)
+    B.moe_project(g["x"], g["w"], ref, base=g["base"], **kw)
+    torch.cuda.synchronize()
+    # in place, on another stream, back to back, in a graph: the same bits
+    o = g["base"].clone()
+    B.moe_project(g["x"], g["w"], o, base=o, **kw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    o2 = torch.empty_like(ref)
+    B.moe_project(g["x"], g["w"], o2, base=g["base"], stream=side, **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(o, ref) and torch.equal(o2, ref)
+    many = [torch.empty_like(ref) for _ in range(10)]
+    ws = torch.empty(B.moe_project_workspace(T, 256, 16, 6), dtype=torch.uint8, device=DEV)
+    for m in many:                                                  # one workspace, one stream
+        B.moe_project(g["x"], g["w"], m, base=g["base"], workspace=ws, **kw)
+    torch.cuda.synchronize()
+    for m in many:
+        assert torch.equal(m, ref)
+    # two graphs, each with a workspace of its own, replayed side by side on two streams
+    outs, graphs = [torch.empty_like(ref), torch.empty_like(ref)], []
+    for i in range(2):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            B.moe_project(g["x"], g["w"], outs[i], base=g["base"], **kw)
+        graphs.append(gr)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        for i, s in enumerate((s1, s2)):
+            with torch.cuda.stream(s):
+                graphs[i].replay()
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], ref) and torch.equal(outs[1], ref)
+
+
+@gpu
+def test_weights_written_just_before_the_call_are_the_ones_used():
+    """The call starts early (programmatic dependent launch): what the stream's earlier work wrote must still be seen, x and w
+    of a plain copy as well as x from another call of the library."""
+    T, K, N = 24, 1024, 1024
+    d = inputs(T, K, N, 16, 4, seed=9)
+    g = {k: (v.to(DEV) if v is not None else None) for k, v in d.items()}
+    tenant = tenants(T, 4, "uniform", 3).to(DEV)
+    mid, out = torch.empty(T, K, dtype=torch.bfloat16, device=DEV), torch.empty(T, N, device=DEV)
+    w2 = (torch.randn(N, K, device=DEV) * 0.05).to(torch.bfloat16)
+    w, x = torch.zeros_like(g["w"]), torch.zeros_like(g["x"])
+    gamma = torch.ones(K, dtype=torch.bfloat16, device=DEV)
+    for with_adapters in (False, True):
+        kw = dict(a=g["a"], b=g["b"], scale=g["scale"], tenant_id=tenant) if with_adapters else {}
+        first = None
+        xn = torch.empty_like(x)
+        for rep in range(20):
+            w.zero_(); x.zero_(); xn.zero_()
+            x.copy_(g["x"])
+            w.copy_(g["w"])
+            B.moe_add_rmsnorm(x, gamma, 1e-6, out=xn)
+            B.moe_project(xn, w, mid, **kw)
+            B.moe_project(mid, w2, out, **kw)
+            torch.cuda.synchronize()
+            if first is None:
+                first = out.clone()
+                ad = tenant.cpu().long() if with_adapters else torch.full((T,), -1)
+                a = (d["a"], d["b"], d["scale"]) if with_adapters else (None, None, None)
+                y, err = reference(xn.cpu(), d["w"], None, *a, ad)
+                assert ((mid.double().cpu() - y).abs() <= err + 2.0 ** -8 * (y.abs() + err)).all()
+                y, err = reference(mid.cpu(), w2.cpu(), None, *a, ad)
+                assert ((out.double().cpu() - y).abs() <= err).all()
+            assert torch.equal(out, first)
+
+
+def _raw(**kw):
+    a = dict(x=256, ldx=64, w=256, ldw=64, T=4, K=64, N=32, a=256, b=256, scale=None, n=2, rank=8, tenant=256, table=None, n_tenants=2, base=None, ldb=0,
+             out=256, ldo=32, out_type=0, ws=256, ws_bytes=1 << 20, status=None)
+    a.update(kw)
+    return B.load_library().moe_project(*a.values(), None)
+
+
+def test_refusals_need_no_gpu():
+    for bad in (dict(x=None), dict(out=None), dict(ws=None), dict(a=None), dict(b=None), dict(tenant=None), dict(w=None, n=0), dict(x=None, n=0)):
+        assert _raw(**bad) == B.MOE_ERR_NULL, bad
+    for bad in (dict(T=-1), dict(T=(1 << 22) + 1), dict(K=0), dict(N=0), dict(n=-1), dict(ldx=56), dict(ldw=56), dict(ldo=31), dict(base=256, ldb=31), dict(rank=0),
+                dict(rank=136), dict(n_tenants=0), dict(x=264), dict(w=264), dict(a=264), dict(b=260), dict(scale=258), dict(tenant=258), dict(table=258),
+                dict(out=258), dict(out=257, out_type=1), dict(base=258, ldb=32), dict(ws=128), dict(status=258)):
+        assert _raw(**bad) == B.MOE_ERR_SHAPE, bad
+    for bad in (dict(K=60), dict(ldx=68), dict(ldw=68), dict(rank=12), dict(out_type=2)):
+        assert _raw(**bad) == B.MOE_ERR_UNSUPPORTED, bad
+    assert _raw(ws_bytes=255) == B.MOE_ERR_ALLOC
+    assert _raw(T=0) == B.MOE_OK
+    lib = B.load_library()
+    assert lib.moe_project_workspace(-1, 64, 8, 1) == B.MOE_ERR_SHAPE
+    assert lib.moe_project_workspace(4, 64, 129, 1) == B.MOE_ERR_SHAPE
+    assert lib.moe_project_workspace(4, 64, 0, 0) >= 0
+    assert lib.moe_project_workspace(100, 2048, 16, 3) >= 100 * 16 * 4
+
+
+def test_binding_checks_tensors():
+    bf = torch.bfloat16
+    x, w, out = torch.zeros(4, 64, dtype=bf), torch.zeros(32, 64, dtype=bf), torch.zeros(4, 32)
+    a, b, t = torch.zeros(2, 8, 64, dtype=bf), torch.zeros(2, 32, 8, dtype=bf), torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(ValueError, match="CUDA"):
+        B.moe_project(x, w, out, a=a, b=b, tenant_id=t)
+    for kw in (dict(a=a), dict(b=b), dict(a=a, b=b[:1], tenant_id=t), dict(a=a, b=b.transpose(1, 2), tenant_id=t), dict(a=a, b=b, tenant_id=t.long()),
+               dict(a=a, b=b, tenant_id=t[:3]), dict(base=out.to(bf)), dict(a=a, b=b, tenant_id=t, scale=torch.ones(3)), dict(workspace=torch.zeros(300))):
+        with pytest.raises(ValueError):
+            B.moe_project(x, w, out, **kw)
+    for bad in ((x.float(), w, out), (x, w[:, :32], out), (x, w, out.double()), (x[0], w, out), (x, w.t(), out)):
+        with pytest.raises(ValueError):
+            B.moe_project(*bad)
