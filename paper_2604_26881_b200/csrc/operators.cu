@@ -88,7 +88,7 @@ int64_t moe_project_workspace(int T, int K, int rank, int n_adapters)
 {
     if (T < 0 || T > kProjectMaxTokens || K < 1 || n_adapters < 0) return MOE_ERR_SHAPE;
     if (n_adapters > 0 && (rank < 1 || rank > kAdapterMaxRank)) return MOE_ERR_SHAPE;
-    return project_workspace(T, K, rank, n_adapters);
+    return project_workspace(T, rank, n_adapters);
 }
 
 int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, int K, int N, const void* a, const void* b,
@@ -111,7 +111,7 @@ int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, i
     if (T == 0) return MOE_OK;
     if (!out || !workspace || (!w && !adapters && !base)) return MOE_ERR_NULL;
     if (((w || adapters) && !x) || (adapters && (!a || !b || !tenant_id))) return MOE_ERR_NULL;
-    if (workspace_bytes < project_workspace(T, K, rank, n_adapters)) return MOE_ERR_ALLOC;
+    if (workspace_bytes < project_workspace(T, rank, n_adapters)) return MOE_ERR_ALLOC;
     ProjectArgs p = {};
     p.x = (const bf16*)x; p.w = (const bf16*)w; p.ldx = ldx; p.ldw = ldw; p.T = T; p.K = K; p.N = N;
     if (adapters) {

@@ -7,6 +7,7 @@
 // the columns of its own adapter.  K is cut over CTAs; the parts of u are stored apart in fp32 and summed in a
 // fixed order by the second launch, which is resident and streams W meanwhile (programmatic dependent launch) and adds
 // u . B^T behind its main loop.
+#include <cstdlib>
 #include <cstring>
 
 #include "project.cuh"
@@ -73,25 +74,90 @@ __device__ __forceinline__ int adapter_of(const ProjectArgs& p, int t, bool repo
     return a;
 }
 
+// The distinct adapters of a tile of 32 * G tokens, in the order of their first token; four warps work on it, warp w on the
+// groups of 32 tokens w and w + 4.  `sync` is a barrier of (at least) those warps.
+template <int G>
+struct AdapterList {
+    int adapter[32 * G];        // of every token, -1: none
+    int list[32 * G];
+    int candidate[32 * G];      // per group: its distinct adapters
+    int n_candidates[G], n_new[G];
+    int count;
+};
+template <int G, typename Sync>
+__device__ __forceinline__ void list_adapters(const ProjectArgs& p, AdapterList<G>& s, int t0, int w, int lane, bool report, Sync sync, int (&slot)[G / 4])
+{
+    uint32_t same[G / 4], fresh[G / 4];
+    bool lead[G / 4];
+#pragma unroll
+    for (int i = 0; i < G / 4; ++i) {
+        const int g = w + 4 * i, t = t0 + g * 32 + lane;
+        const int a = t < p.T ? adapter_of(p, t, report) : -1;
+        s.adapter[g * 32 + lane] = a;
+        same[i] = __match_any_sync(kFull, a);
+        lead[i] = a >= 0 && lane == __ffs(same[i]) - 1;
+        const uint32_t c = __ballot_sync(kFull, lead[i]);
+        if (lead[i]) s.candidate[g * 32 + __popc(c & ((1u << lane) - 1))] = a;
+        if (lane == 0) s.n_candidates[g] = __popc(c);
+    }
+    sync();
+#pragma unroll
+    for (int i = 0; i < G / 4; ++i) {
+        const int g = w + 4 * i, a = s.adapter[g * 32 + lane];
+        bool first = lead[i];                               // (of the tile: no earlier group has it)
+        for (int h = 0; h < g && first; ++h)
+            for (int j = 0; j < s.n_candidates[h] && first; ++j) first = s.candidate[h * 32 + j] != a;
+        fresh[i] = __ballot_sync(kFull, first);
+        if (lane == 0) s.n_new[g] = __popc(fresh[i]);
+    }
+    sync();
+    int at = 0;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+#pragma unroll
+        for (int i = 0; i < G / 4; ++i)
+            if (g == w + 4 * i && (fresh[i] >> lane & 1)) s.list[at + __popc(fresh[i] & ((1u << lane) - 1))] = s.adapter[g * 32 + lane];
+        at += s.n_new[g];
+    }
+    if (w == 0 && lane == 0) s.count = at;
+    sync();
+    // every token's place in the list: its group's first token of the adapter looks it up
+#pragma unroll
+    for (int i = 0; i < G / 4; ++i) {
+        const int a = s.adapter[(w + 4 * i) * 32 + lane];
+        int j = -1;
+        if (lead[i]) for (j = 0; s.list[j] != a; ++j) {}
+        slot[i] = __shfl_sync(kFull, j, __ffs(same[i]) - 1);
+        if (a < 0) slot[i] = -1;
+    }
+}
+
 struct UMaps { CUtensorMap x, a; };
 
-// blockIdx: x = token tile, y = chunk of the tile's distinct adapters, z = part of K
+// blockIdx: x = token tile, y = every gridDim.y-th chunk of the tile's distinct adapters, z = part of K (a cluster holds the
+// parts of one tile and adds them up in a fixed order)
 __global__ void __launch_bounds__(kUThreads)
 adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
 {
     extern __shared__ unsigned char smem_dyn[];
     const uint32_t ring = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-    __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 1];
+    __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 2];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_abort, s_count;
-    __shared__ int s_adapter[kTok], s_first[kTok], s_list[kTok], s_warp_count[4];
-    const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * kMaxStages, bar_done = bar_full + 16 * kMaxStages;
+    __shared__ int s_abort;
+    __shared__ AdapterList<4> s_al;
+    __shared__ int s_slot[kTok];
+    const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * kMaxStages, bar_done = bar_full + 16 * kMaxStages,
+                   bar_free = bar_done + 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int t0 = blockIdx.x * kTok;
+    const int pitch = p.rank + 4;
+    // this part's sums of the tile's tokens, behind the ring (and the rows that the MMA of a short tile may read)
+    float* const su = reinterpret_cast<float*>(smem_dyn + (ring - smem_u32(smem_dyn)) + p.n_stages * p.stage_bytes + kTok * kBK * 2);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.n_stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
         mbar_init(bar_done, 1);
+        mbar_init(bar_free, 4);
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -103,51 +169,37 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
     pdl_wait();
     pdl_launch_dependents();        // (after the wait: the projection may read x before it waits itself)
 
-    // the tile's distinct adapters, in the order of their first token
-    const int tok = threadIdx.x - 64, t = t0 + tok;
-    if (warp >= 2) s_adapter[tok] = t < p.T ? adapter_of(p, t, blockIdx.y == 0 && blockIdx.z == 0) : -1;
-    __syncthreads();
-    int mine = -1, first = kTok;
-    bool leads = false;
-    uint32_t leaders = 0;
     if (warp >= 2) {
-        mine = s_adapter[tok];
-        for (int j = kTok - 1; j >= 0; --j) if (s_adapter[j] == mine) first = j;
-        leads = mine >= 0 && first == tok;
-        leaders = __ballot_sync(kFull, leads);
-        if (lane == 0) s_warp_count[warp - 2] = __popc(leaders);
-    }
-    __syncthreads();
-    if (warp >= 2) {
-        int at = 0;
-        for (int w = 0; w < warp - 2; ++w) at += s_warp_count[w];
-        at += __popc(leaders & ((1u << lane) - 1));
-        if (leads) { s_list[at] = mine; s_first[tok] = at; }
-        if (threadIdx.x == 64) s_count = s_warp_count[0] + s_warp_count[1] + s_warp_count[2] + s_warp_count[3];
+        int slot[1];
+        list_adapters<4>(p, s_al, t0, warp - 2, lane, blockIdx.y == 0 && blockIdx.z == 0,
+                         [] { asm volatile("bar.sync 1, 128;" ::: "memory"); }, slot);
+        s_slot[threadIdx.x - 64] = slot[0];
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
-    const int slot0 = blockIdx.y * p.slots;
-    const int n_slots = min(p.slots, s_count - slot0);                 // adapters of this CTA
-    if (n_slots > 0) {
+    const int count = s_al.count, n_chunks = (count + p.slots - 1) / p.slots;
+    const bool work = (int)blockIdx.y < n_chunks;                       // (the same for the whole cluster)
+    if (work) {
         const int k0 = (int)((long long)p.ksteps * blockIdx.z / p.u_splits), k1 = (int)((long long)p.ksteps * (blockIdx.z + 1) / p.u_splits);
-        const int cols = (n_slots * p.rank + 15) & ~15;                 // (rank 8 and an odd number: eight stale columns, never read)
         if (warp == 0) {
             if (lane == 0) {
                 uint32_t stage = 0, phase = 0, armed = 0, armed_phase = 0;
                 bool ok = true;
-                for (int ks = k0; ks < k1; ++ks) {
-                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, p.status)) { ok = false; break; }
-                    const uint32_t sa = ring + stage * p.stage_bytes, sb = sa + p.a_bytes, full = bar_full + 8 * stage;
-                    armed |= 1u << stage;
-                    armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
-                    mbar_expect_tx(full, (p.a_rows + n_slots * p.rank) * kBK * 2);
-                    tma_load_2d(sa, &maps.x, full, ks * kBK, t0);
-                    for (int j = 0; j < n_slots; ++j)
-                        tma_load_2d(sb + j * p.rank * kBK * 2, &maps.a, full, ks * kBK, s_list[slot0 + j] * p.rank);
-                    if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
+                for (int c = blockIdx.y; c < n_chunks && ok; c += gridDim.y) {
+                    const int n_slots = min(p.slots, count - c * p.slots);
+                    for (int ks = k0; ks < k1; ++ks) {
+                        if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, p.status)) { ok = false; break; }
+                        const uint32_t sa = ring + stage * p.stage_bytes, sb = sa + p.a_bytes, full = bar_full + 8 * stage;
+                        armed |= 1u << stage;
+                        armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
+                        mbar_expect_tx(full, (p.a_rows + n_slots * p.rank) * kBK * 2);
+                        tma_load_2d(sa, &maps.x, full, ks * kBK, t0);
+                        for (int j = 0; j < n_slots; ++j)
+                            tma_load_2d(sb + j * p.rank * kBK * 2, &maps.a, full, ks * kBK, s_al.list[c * p.slots + j] * p.rank);
+                        if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
+                    }
                 }
                 if (!ok)
                     for (int s = 0; s < p.n_stages; ++s)
@@ -156,38 +208,43 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
             __syncwarp();
         } else if (warp == 1) {
             if (lane == 0) {
-                uint32_t stage = 0, phase = 0, acc = 0;
+                uint32_t stage = 0, phase = 0;
                 bool ok = true;
-                const uint32_t idesc = idesc_bf16(cols);
-                for (int ks = k0; ks < k1; ++ks) {
-                    if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, p.status)) { ok = false; break; }
+                int it = 0;
+                for (int c = blockIdx.y; c < n_chunks && ok; c += gridDim.y, ++it) {
+                    // (rank 8 and an odd number of adapters: eight stale columns, never read)
+                    const int cols = (min(p.slots, count - c * p.slots) * p.rank + 15) & ~15;
+                    const uint32_t idesc = idesc_bf16(cols);
+                    if (!mbar_wait(bar_free, (it & 1) ^ 1, &s_abort, p.status)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t lo_a = smem_desc_lo(ring + stage * p.stage_bytes), lo_b = lo_a + (p.a_bytes >> 4);
+                    uint32_t acc = 0;
+                    for (int ks = k0; ks < k1; ++ks) {
+                        if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, p.status)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t lo_a = smem_desc_lo(ring + stage * p.stage_bytes), lo_b = lo_a + (p.a_bytes >> 4);
 #pragma unroll
-                    for (int kk = 0; kk < kBK / 16; ++kk) {
-                        umma_bf16(tmem, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, acc);
-                        acc = 1;
+                        for (int kk = 0; kk < kBK / 16; ++kk) {
+                            umma_bf16(tmem, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, acc);
+                            acc = 1;
+                        }
+                        umma_commit(bar_empty + 8 * stage);
+                        if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
                     }
-                    umma_commit(bar_empty + 8 * stage);
-                    if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
+                    if (ok) umma_commit(bar_done);
                 }
-                if (ok) umma_commit(bar_done);
             }
             __syncwarp();
         } else {
             // thread <-> token; a warp reads the TMEM lanes of its quarter
-            const int quarter = warp & 3, row = quarter * 32 + lane, tr = t0 + row;
-            const int a = s_adapter[row];
-            int f = 0;
-            if (a >= 0) {
-                while (s_adapter[f] != a) ++f;                          // the adapter's first token knows its place in the list
-                f = s_first[f] - slot0;
-            }
-            const bool live = a >= 0 && f >= 0 && f < n_slots;
-            const float s = live ? (p.scale ? p.scale[a] : 1.f) : 0.f;
-            float* dst = p.u + ((size_t)blockIdx.z * p.T + tr) * p.rank;
-            const int c_lo = live ? f * p.rank : cols, c_hi = live ? c_lo + p.rank : 0;
-            if (__all_sync(kFull, mbar_wait(bar_done, 0, &s_abort, p.status))) {
+            const int quarter = warp & 3, row = quarter * 32 + lane;
+            float* dst = su + row * pitch;
+            int it = 0;
+            for (int c0 = blockIdx.y; c0 < n_chunks; c0 += gridDim.y, ++it) {
+                const int f = s_slot[row] - c0 * p.slots;
+                const bool live = s_slot[row] >= 0 && f >= 0 && f < p.slots;
+                const int cols = min(p.slots, count - c0 * p.slots) * p.rank;
+                const int c_lo = live ? f * p.rank : cols, c_hi = live ? c_lo + p.rank : 0;
+                if (!__all_sync(kFull, mbar_wait(bar_done, it & 1, &s_abort, p.status))) break;
                 tc_fence_after();
                 for (int c = 0; c < cols; c += 16) {
                     if (!__any_sync(kFull, c + 16 > c_lo && c < c_hi)) continue;
@@ -198,12 +255,49 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
                     for (int h = 0; h < 16; h += 8)
                         if (c + h >= c_lo && c + h < c_hi) {
                             float4* o = reinterpret_cast<float4*>(dst + (c + h - c_lo));
-                            o[0] = make_float4(s * __uint_as_float(r[h]), s * __uint_as_float(r[h + 1]), s * __uint_as_float(r[h + 2]), s * __uint_as_float(r[h + 3]));
-                            o[1] = make_float4(s * __uint_as_float(r[h + 4]), s * __uint_as_float(r[h + 5]), s * __uint_as_float(r[h + 6]), s * __uint_as_float(r[h + 7]));
+                            o[0] = make_float4(__uint_as_float(r[h]), __uint_as_float(r[h + 1]), __uint_as_float(r[h + 2]), __uint_as_float(r[h + 3]));
+                            o[1] = make_float4(__uint_as_float(r[h + 4]), __uint_as_float(r[h + 5]), __uint_as_float(r[h + 6]), __uint_as_float(r[h + 7]));
                         }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_free);
+            }
+        }
+        tc_fence_before();
+        if (p.u_splits > 1) cluster_sync_all(); else __syncthreads();
+        // this CTA adds up a share of the tokens over the parts
+        if (!s_abort) {
+            const int r0 = kTok * blockIdx.z / p.u_splits, r1 = kTok * (blockIdx.z + 1) / p.u_splits;
+            const uint32_t su_addr = smem_u32(su);
+            for (int e = r0 * p.rank + threadIdx.x; e < r1 * p.rank; e += kUThreads) {
+                const int row = e / p.rank, c = e - row * p.rank, slot = s_slot[row];
+                if (slot < 0 || (slot / p.slots) % gridDim.y != blockIdx.y) continue;
+                float v = 0.f;
+                if (p.u_splits > 1) {
+                    float q[8];
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) q[z] = z < p.u_splits ? ld_cluster_f32(map_to_cta(su_addr + 4 * (row * pitch + c), z)) : 0.f;
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) v += q[z];
+                } else {
+                    v = su[row * pitch + c];
+                }
+                if (p.scale) v *= p.scale[s_al.adapter[row]];
+                const size_t at = (size_t)(t0 + row) * p.rank + c;
+                if (p.u_pair) {
+                    // hi + lo hold 16 bits of v (what rounds to an infinity, or is one, has no remainder)
+                    const bf16 hi = __float2bfloat16_rn(v);
+                    const float f = __bfloat162float(hi);
+                    bf16* u = reinterpret_cast<bf16*>(p.u);
+                    u[at] = hi;
+                    u[(size_t)p.T * p.rank + at] = __float2bfloat16_rn(isinf(f) ? 0.f : v - f);
+                } else {
+                    p.u[at] = v;
                 }
             }
         }
+        if (p.u_splits > 1) cluster_sync_all();                         // nobody leaves while a peer may still read its sums
     }
     tc_fence_before();
     __syncthreads();
@@ -304,6 +398,18 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
             __syncwarp();
         } else {
             const int quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane;
+            if (adapters) {
+                // The rows of the adapters' B that this CTA will multiply come into L2 while the product runs; every token asks
+                // for its own adapter's (the ids are complete: see above), the first of a warp for all that share it.
+                const int c0 = n0 + kPN * rank / S, c1 = min(n0 + (int)(kPN * (rank + 1) / S), p.N);
+                const int a = row < rows ? adapter_of(p, t0 + row, false) : -1;
+                const uint32_t same = __match_any_sync(kFull, a);
+                if (half == 0 && a >= 0 && lane == __ffs(same) - 1 && c0 < c1) {
+                    const char* lo = reinterpret_cast<const char*>(p.b + ((size_t)a * p.N + c0) * p.rank);
+                    const char* hi = reinterpret_cast<const char*>(p.b + ((size_t)a * p.N + c1) * p.rank);
+                    for (const char* q = lo; q < hi; q += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q));
+                }
+            }
             if (__all_sync(kFull, mbar_wait(bar_done, 0, &s_abort, p.status)) && quarter * 32 < rows) {
                 tc_fence_after();
 #pragma unroll
@@ -326,59 +432,76 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    float* const su = part + (size_t)kPN * pitch;          // u of the tile's tokens, summed over the parts of K
+    float* const su = part + (size_t)kPN * pitch;          // u of the tile's tokens
     if (adapters) {
-        for (int i = threadIdx.x; i < rows * p.rank; i += kPThreads) {
-            const int r = i / p.rank;
-            float v = 0.f;
-            if (s_adapter[r] >= 0) {
-                const float* src = p.u + (size_t)t0 * p.rank + i;
-                for (int s = 0; s < p.u_splits; ++s) v += __ldcg(src + (size_t)s * p.T * p.rank);
-            }
-            su[i] = v;
-        }
+        for (int i = threadIdx.x; i < rows * p.rank; i += kPThreads)
+            su[i] = s_adapter[i / p.rank] >= 0 ? __ldcg(p.u + (size_t)t0 * p.rank + i) : 0.f;
     }
     if (S > 1) cluster_sync_all(); else __syncthreads();
     if (!s_abort) {
-        const int nc = kPN / S, c0 = rank * nc;            // this CTA's columns of the tile
+        const int c0 = kPN * rank / S, nc = kPN * (rank + 1) / S - c0;          // this CTA's columns of the tile
         const uint32_t part_addr = smem_u32(part);
-        for (int e = threadIdx.x; e < rows * nc; e += kPThreads) {
-            const int c = c0 + (e & (nc - 1)), r = e / nc, n = n0 + c;
-            if (n >= p.N) continue;
-            float v = 0.f;
-            if (product) {
-                if (S > 1) {
-                    for (int s = 0; s < S; ++s) v += ld_cluster_f32(map_to_cta(part_addr + 4 * (c * pitch + r), s));
-                } else {
-                    v = part[c * pitch + r];
+        const int total = rows * nc;
+        // four outputs of a thread at a time, so that their loads overlap
+        for (int e0 = threadIdx.x; e0 < total; e0 += 4 * kPThreads) {
+            float v[4];
+            int r[4], n[4], a[4];
+            bool on[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int e = e0 + q * kPThreads;
+                r[q] = e / nc;
+                const int c = c0 + e - r[q] * nc;
+                n[q] = n0 + c;
+                on[q] = e < total && n[q] < p.N;
+                a[q] = on[q] && adapters ? s_adapter[r[q]] : -1;
+                v[q] = 0.f;
+                if (on[q] && product) {
+                    if (S > 1) {
+                        float t[8];
+#pragma unroll
+                        for (int z = 0; z < 8; ++z) t[z] = z < S ? ld_cluster_f32(map_to_cta(part_addr + 4 * (c * pitch + r[q]), z)) : 0.f;
+#pragma unroll
+                        for (int z = 0; z < 8; ++z) v[q] += t[z];
+                    } else {
+                        v[q] = part[c * pitch + r[q]];
+                    }
                 }
             }
             if (adapters) {
-                const int a = s_adapter[r];
-                if (a >= 0) {
-                    const uint4* bp = reinterpret_cast<const uint4*>(p.b + ((size_t)a * p.N + n) * p.rank);
-                    const float* up = su + r * p.rank;
-                    float d = 0.f;
-                    for (int i = 0; i < p.rank / 8; ++i) {
-                        const uint4 q = __ldg(bp + i);
-                        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&q);
+                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int i = 0; i < p.rank / 8; ++i) {
+                    uint4 bq[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        bq[q] = a[q] >= 0 ? __ldg(reinterpret_cast<const uint4*>(p.b + ((size_t)a[q] * p.N + n[q]) * p.rank) + i) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (a[q] < 0) continue;
+                        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&bq[q]);
+                        const float* up = su + r[q] * p.rank + 8 * i;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float2 f = __bfloat1622float2(h[j]);
-                            d = fmaf(up[8 * i + 2 * j], f.x, d);
-                            d = fmaf(up[8 * i + 2 * j + 1], f.y, d);
+                            d[q] = fmaf(up[2 * j], f.x, d[q]);
+                            d[q] = fmaf(up[2 * j + 1], f.y, d[q]);
                         }
                     }
-                    v += d;
                 }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] += d[q];
             }
-            const size_t row = t0 + r;
-            if (p.out_f32) {
-                if (p.base) v += ((const float*)p.base)[row * p.ldbase + n];
-                ((float*)p.out)[row * p.ldo + n] = v;
-            } else {
-                if (p.base) v += __bfloat162float(((const bf16*)p.base)[row * p.ldbase + n]);
-                ((bf16*)p.out)[row * p.ldo + n] = __float2bfloat16_rn(v);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (!on[q]) continue;
+                const size_t row = t0 + r[q];
+                if (p.out_f32) {
+                    if (p.base) v[q] += ((const float*)p.base)[row * p.ldbase + n[q]];
+                    ((float*)p.out)[row * p.ldo + n[q]] = v[q];
+                } else {
+                    if (p.base) v[q] += __bfloat162float(((const bf16*)p.base)[row * p.ldbase + n[q]]);
+                    ((bf16*)p.out)[row * p.ldo + n[q]] = __float2bfloat16_rn(v[q]);
+                }
             }
         }
     }
@@ -388,6 +511,321 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
         __syncwarp();
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kPN) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Many tokens: 256 tokens x 256 weight rows per pair of CTAs (tcgen05.mma.cta_group::2; each CTA holds 128 of either), pairs
+// that walk over the tiles, two accumulators of 256 TMEM columns so that a tile's epilogue runs behind the next tile's MMAs.
+//
+// The adapters' second products go into the same accumulator: u of the tile's tokens is one more M operand (a pair of
+// bf16 tiles, hi and lo, that hold 16 bits of the fp32 value: a single bf16 would cost 2^-9 of the adapter's share), and
+// for every distinct adapter of the tile the rows of its B are one more N operand.  Which tokens that MMA may change is said by
+// its disable-output-lane mask, so u needs no masked copy per adapter and an infinity or a NaN in one tenant's B
+// cannot reach another's tokens (a zeroed row of u would: 0 * inf).
+constexpr int kMStages = 5;
+constexpr int kMStageBytes = 2 * kTok * kBK * 2;       // 16 KB of tokens, 16 KB of weight rows per CTA
+constexpr int kMTile = 256;
+constexpr int kMThreads = 480;                         // warp 0: TMA (weights), 1: MMA, 2..9: epilogue, 10: TMA (tokens), 11..14: u
+constexpr int kUTile = kTok * kBK * 2;                 // one bf16 tile of 64 columns of u
+
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar & 0xFEFFFFFFu), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar & 0xFEFFFFFFu), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void umma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// lanes (tokens of the pair) whose bit is set are left as they are
+__device__ __forceinline__ void umma_pair_masked(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, const uint32_t* m)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%5, %6, %7, %8, %9, %10, %11, %12}, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(m[0]), "r"(m[1]), "r"(m[2]), "r"(m[3]), "r"(m[4]), "r"(m[5]),
+                 "r"(m[6]), "r"(m[7]) : "memory");
+}
+// arrives on the barrier at the same offset in both CTAs of the pair
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((unsigned short)3) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ void builders_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+struct MMaps { CUtensorMap x, w, b, u; };
+
+// 32 outputs of one token: columns n .. n+31
+template <typename T>
+__device__ __forceinline__ void store32(const ProjectArgs& p, size_t row, int n, float* v, bool vec)
+{
+    T* out = (T*)p.out + row * p.ldo + n;
+    const T* base = p.base ? (const T*)p.base + row * p.ldbase + n : nullptr;
+    constexpr int kPer = 16 / sizeof(T);                // elements of a 16-byte vector
+    if (vec && n + 32 <= p.N) {
+        if (base) {
+            uint4 q[32 / kPer];
+#pragma unroll
+            for (int i = 0; i < 32 / kPer; ++i) q[i] = reinterpret_cast<const uint4*>(base)[i];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                T e;
+                if constexpr (sizeof(T) == 4) e = __uint_as_float((&q[i / 4].x)[i % 4]);
+                else e = __ushort_as_bfloat16((unsigned short)((&q[i / 8].x)[(i % 8) / 2] >> (16 * (i & 1))));
+                v[i] += (float)e;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 32 / kPer; ++i) {
+            uint4 o;
+            if constexpr (sizeof(T) == 4) {
+                o = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+            } else {
+                __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&o);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(v[8 * i + 2 * j], v[8 * i + 2 * j + 1]);
+            }
+            reinterpret_cast<uint4*>(out)[i] = o;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (n + i < p.N) out[i] = (T)(v[i] + (base ? (float)base[i] : 0.f));
+    }
+}
+
+__global__ void __launch_bounds__(kMThreads, 1)
+project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
+{
+    extern __shared__ unsigned char smem_dyn[];
+    const uint32_t ring = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+    unsigned char* const ring_ptr = smem_dyn + (ring - smem_u32(smem_dyn));
+    const int n_stages = p.n_stages;
+    const uint32_t ua = ring + n_stages * kMStageBytes;                 // u: [64-column chunk][hi, lo] tiles
+    __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 8];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort;
+    __shared__ AdapterList<8> s_al;
+    __shared__ uint32_t s_mask[kMTile][8];
+    const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * kMaxStages, bar_tfull = bar_full + 16 * kMaxStages,
+                   bar_tempty = bar_tfull + 16, bar_ufull = bar_tfull + 32, bar_uempty = bar_tfull + 40, bar_list = bar_tfull + 48;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const bool leader = rank == 0;
+    const bool adapters = p.n_adapters > 0;
+    const int n_tiles = (p.N + kMTile - 1) / kMTile, m_tiles = (p.T + kMTile - 1) / kMTile, total = n_tiles * m_tiles;
+    const int pair0 = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int chunks = (p.rank + kBK - 1) / kBK;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < n_stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(bar_tfull + 8 * b, 1); mbar_init(bar_tempty + 8 * b, 2 * 8); }
+        mbar_init(bar_ufull, 1);
+        mbar_init(bar_uempty, 1);
+        mbar_init(bar_list, 4);
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        __syncwarp();
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                     // the peer's barriers are there before anything is signalled on them
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    // (with adapters the kernel before this one is adapter_kernel: see project_kernel)
+    if (!adapters) pdl_wait();
+    pdl_launch_dependents();
+
+    if (warp == 0 || warp == 10) {
+        // ---- TMA: one lane for the weight rows (and the adapters' B), one for the tokens; a lane needs about 430 cycles per
+        // stage (140 for a load, 290 for the barrier), the MMAs of a stage 512
+        if (lane == 0) {
+            uint32_t stage = 0, phase = 0, armed = 0, armed_phase = 0;
+            bool ok = true;
+            int it = 0, u_loads = 0;
+            for (int tile = pair0; tile < total && ok; tile += pairs, ++it) {
+                const int n0 = (tile / m_tiles) * kMTile + rank * kTok, t0 = (tile % m_tiles) * kMTile + rank * kTok;
+                const int steps = p.ksteps;
+                int extra = -1;                             // stages of adapters' B behind the product's
+                for (int ks = 0; ok; ++ks) {
+                    if (ks >= steps && extra < 0) {
+                        extra = 0;
+                        if (adapters) {
+                            if (!mbar_wait(bar_list, it & 1, &s_abort, p.status)) { ok = false; break; }
+                            extra = s_al.count * chunks;
+                            if (warp == 10) {
+                                // u of this CTA's tokens, hi and lo tiles (rows of tokens without an adapter hold anything)
+                                if (it == 0) pdl_wait();
+                                if (!mbar_wait(bar_uempty, (it & 1) ^ 1, &s_abort, p.status)) { ok = false; break; }
+                                if (leader) mbar_expect_tx(bar_ufull, 4 * chunks * kUTile);
+                                u_loads = it + 1;
+                                for (int c = 0; c < 2 * chunks; ++c)
+                                    tma_load_3d_pair(ua + c * kUTile, &maps.u, bar_ufull, (c >> 1) * kBK, t0, c & 1);
+                            }
+                        }
+                    }
+                    if (ks >= steps && ks >= steps + extra) break;
+                    const uint32_t sa = ring + stage * kMStageBytes, full = bar_full + 8 * stage;
+                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, p.status)) { ok = false; break; }
+                    if (warp == 0) {
+                        armed |= 1u << stage;
+                        armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
+                        if (ks < steps) {
+                            if (leader) mbar_expect_tx(full, 2 * kMStageBytes);
+                            tma_load_2d_pair(sa + kTok * kBK * 2, &maps.w, full, ks * kBK, n0);
+                        } else {
+                            const int j = (ks - steps) / chunks, c = (ks - steps) - j * chunks;
+                            if (leader) mbar_expect_tx(full, kMStageBytes);
+                            tma_load_3d_pair(sa + kTok * kBK * 2, &maps.b, full, c * kBK, n0, s_al.list[j]);
+                        }
+                    } else if (ks < steps) {
+                        tma_load_2d_pair(sa, &maps.x, full, ks * kBK, t0);
+                    }
+                    if (++stage == (uint32_t)n_stages) { stage = 0; phase ^= 1; }
+                }
+            }
+            if (!ok && leader && warp == 0) {               // gave up: the copies in flight land before the block exits
+                for (int s = 0; s < n_stages; ++s)
+                    if (armed & (1u << s)) mbar_wait(bar_full + 8 * s, (armed_phase >> s) & 1u, &s_abort, p.status);
+            }
+            if (!ok && leader && u_loads > 0) mbar_wait(bar_ufull, (u_loads - 1) & 1, &s_abort, p.status);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0 && leader) {
+            uint32_t stage = 0, phase = 0;
+            bool ok = true;
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
+            int it = 0;
+            for (int tile = pair0; tile < total && ok; tile += pairs, ++it) {
+                const uint32_t buf = it & 1, d = tmem + buf * 256;
+                if (!mbar_wait_cluster(bar_tempty + 8 * buf, ((it >> 1) & 1) ^ 1, &s_abort, p.status)) { ok = false; break; }
+                tc_fence_after();
+                uint32_t acc = 0;
+                for (int ks = 0; ks < p.ksteps; ++ks) {
+                    if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, p.status)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t lo_a = smem_desc_lo(ring + stage * kMStageBytes), lo_b = lo_a + ((kTok * kBK * 2) >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < kBK / 16; ++kk) {
+                        umma_pair(d, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, acc);
+                        acc = 1;
+                    }
+                    umma_commit_pair(bar_empty + 8 * stage);
+                    if (++stage == (uint32_t)n_stages) { stage = 0; phase ^= 1; }
+                }
+                if (!ok) break;
+                if (adapters) {
+                    if (!mbar_wait(bar_list, it & 1, &s_abort, p.status) || !mbar_wait(bar_ufull, it & 1, &s_abort, p.status)) { ok = false; break; }
+                    tc_fence_after();
+                    const int count = s_al.count;
+                    for (int j = 0; j < count && ok; ++j) {
+                        // (without the product the first MMA of an adapter overwrites its tokens' lanes)
+                        uint32_t first = acc;
+                        for (int c = 0; c < chunks; ++c) {
+                            if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, p.status)) { ok = false; break; }
+                            tc_fence_after();
+                            const uint32_t lo_b = smem_desc_lo(ring + stage * kMStageBytes + kTok * kBK * 2);
+                            const int kks = (min(kBK, p.rank - c * kBK) + 15) >> 4;
+                            for (int h = 0; h < 2; ++h) {
+                                const uint32_t lo_a = smem_desc_lo(ua + (2 * c + h) * kUTile);
+                                for (int kk = 0; kk < kks; ++kk) {
+                                    umma_pair_masked(d, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, first, s_mask[j]);
+                                    first = 1;
+                                }
+                            }
+                            umma_commit_pair(bar_empty + 8 * stage);
+                            if (++stage == (uint32_t)n_stages) { stage = 0; phase ^= 1; }
+                        }
+                    }
+                    if (!ok) break;
+                    umma_commit_pair(bar_uempty);
+                }
+                umma_commit_pair(bar_tfull + 8 * buf);
+            }
+        }
+        __syncwarp();
+    } else if (warp < 10) {
+        // ---- epilogue: thread <-> token (TMEM lane), four warps per half of the columns ----
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t tempty_leader = map_to_cta(bar_tempty, 0);
+        const int esz = p.out_f32 ? 4 : 2;
+        const bool vec = (uintptr_t)p.out % 16 == 0 && p.ldo * esz % 16 == 0 && (!p.base || ((uintptr_t)p.base % 16 == 0 && p.ldbase * esz % 16 == 0));
+        if (adapters) pdl_wait();
+        bool ok = true;
+        int it = 0;
+        for (int tile = pair0; tile < total; tile += pairs, ++it) {
+            const int n0 = (tile / m_tiles) * kMTile + half * 128, t = (tile % m_tiles) * kMTile + (int)rank * kTok + quarter * 32 + lane;
+            const uint32_t buf = it & 1;
+            ok = __all_sync(kFull, mbar_wait(bar_tfull + 8 * buf, (it >> 1) & 1, &s_abort, p.status));
+            if (!ok) break;
+            tc_fence_after();
+            const bool live = t < p.T;
+            // a token that no MMA has written (no product, no adapter): its lane holds some earlier tile
+            const bool empty = p.ksteps == 0 && !(live && adapters && adapter_of(p, t, false) >= 0);
+#pragma unroll 1
+            for (int c = 0; c < 128; c += 32) {
+                uint32_t r[32];
+                const uint32_t from = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16) + half * 128 + c;
+                tmem_ld16(from, r);
+                tmem_ld16(from + 16, r + 16);
+                tmem_ld_wait();
+                if (c == 96) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * buf);
+                }
+                if (live && n0 + c < p.N) {
+                    float v[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = empty ? 0.f : __uint_as_float(r[i]);
+                    if (p.out_f32) store32<float>(p, t, n0 + c, v, vec); else store32<bf16>(p, t, n0 + c, v, vec);
+                }
+            }
+        }
+    } else if (adapters) {
+        // ---- four warps that list the adapters of the pair's tokens, and which lanes each MMA leaves alone ----
+        const int w = warp - 11;
+        int it = 0;
+        for (int tile = pair0; tile < total; tile += pairs, ++it) {
+            if (!__all_sync(kFull, mbar_wait(bar_uempty, (it & 1) ^ 1, &s_abort, p.status))) break;
+            int slot[2];
+            list_adapters<8>(p, s_al, (tile % m_tiles) * kMTile, w, lane, false, [] { builders_sync(); }, slot);
+            for (int j = w; j < s_al.count; j += 4) {
+                const int a = s_al.list[j];
+#pragma unroll
+                for (int g = 0; g < 8; ++g) {
+                    const uint32_t other = __ballot_sync(kFull, s_al.adapter[g * 32 + lane] != a);
+                    if (lane == g) s_mask[j][g] = other;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_list);
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                     // nobody leaves while the peer may still read this CTA's memory or signal it
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
 }
 
@@ -405,7 +843,21 @@ bool make_map_ld(CUtensorMap* m, const void* base, uint64_t rows, uint64_t k, ui
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr int kMaxSmem = 224 * 1024;
+// 3-D map over n matrices [N][rank] (the adapters' B; u's two halves); box = 64 x 128 rows of one matrix
+bool make_map_3d(CUtensorMap* m, const void* base, uint64_t n, uint64_t N, uint64_t rank)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {rank, N, n};
+    cuuint64_t strides[2] = {rank * 2, N * rank * 2};
+    cuuint32_t box[3] = {(cuuint32_t)kBK, (cuuint32_t)kTok, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int kMaxSmem = 212 * 1024;      // dynamic; with the static arrays below the 227 KB of an SM
 
 // the opt-in to large dynamic shared memory is a per-device attribute of a kernel
 template <typename K>
@@ -423,32 +875,31 @@ cudaError_t allow_smem(K kern, bool (&done)[kMaxDevices])
 
 int div_up(int a, int b) { return (a + b - 1) / b; }
 
-// Parts of K of the first product: about one CTA per SM over the token tiles, at least two slices each
-int u_parts(int T, int K)
+// The pair shape, from 257 tokens on.
+bool use_many(const ProjectArgs& p)
 {
-    const int tiles = div_up(T, kTok), steps = div_up(K, kBK);
-    int s = 1;
-    while (s < 8 && tiles * s * 2 <= 148 && steps / (s * 2) >= 2) s *= 2;
-    return s;
+    const char* f = getenv("PROJECT_SHAPE");
+    if (f) return f[0] == 'm' && p.T > 128;
+    return p.T > kMTile;
 }
 
 }  // namespace
 
-int64_t project_workspace(int T, int K, int rank, int n_adapters)
+int64_t project_workspace(int T, int rank, int n_adapters)
 {
-    if (n_adapters == 0 || T == 0) return kProjectHeader;
-    return kProjectHeader + (int64_t)u_parts(T, K) * T * rank * (int64_t)sizeof(float);
+    return kProjectHeader + (n_adapters > 0 ? (int64_t)T * rank * (int64_t)sizeof(float) : 0);
 }
 
 cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
 {
     ProjectArgs p = in;
-    static bool u_ok[kMaxDevices] = {false}, p_ok[kMaxDevices] = {false};
+    static bool u_ok[kMaxDevices] = {false}, p_ok[kMaxDevices] = {false}, m_ok[kMaxDevices] = {false};
     const int m_tiles = div_up(p.T, kTok);
+    const bool many = use_many(p);
     p.a_rows = p.T >= kTok ? kTok : ((p.T + 7) & ~7);
     p.a_bytes = (p.a_rows * kBK * 2 + 1023) & ~1023;
     p.u = reinterpret_cast<float*>(p.workspace + kProjectHeader);
-    p.u_splits = u_parts(p.T, p.K);
+    p.u_pair = many;
     if (p.n_adapters > 0) {
         cudaError_t e = allow_smem(adapter_kernel, u_ok);
         if (e != cudaSuccess) return e;
@@ -457,15 +908,56 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
             !make_map_ld(&um.a, p.a, (uint64_t)p.n_adapters * p.rank, p.K, p.K, p.rank))
             return cudaErrorInvalidValue;
         ProjectArgs q = p;
-        q.slots = kUCols / p.rank;
         q.ksteps = div_up(p.K, kBK);
-        q.stage_bytes = p.a_bytes + kUCols * kBK * 2;
+        // K is cut into as many parts as there are SMs for the token tiles, of two slices at least; then the chunks of a
+        // tile's adapters go to CTAs of their own as long as there are SMs, and are walked over beyond that
+        q.u_splits = 1;
+        while (q.u_splits < 8 && m_tiles * q.u_splits * 2 <= 148 && q.ksteps / (q.u_splits * 2) >= 2) q.u_splits *= 2;
+        const int cols = m_tiles == 1 ? kUCols / 2 : kUCols;      // (one tile: shorter chunks, a load of A's rows is issued per adapter)
+        q.slots = cols / p.rank > 0 ? cols / p.rank : 1;
+        const int most = p.T < kTok ? p.T : kTok;
+        int chunks = div_up(most < p.n_adapters ? most : p.n_adapters, q.slots);
+        const int room = 148 / (m_tiles * q.u_splits);
+        if (chunks > room) chunks = room < 1 ? 1 : room;
+        q.stage_bytes = p.a_bytes + (q.slots * p.rank > 64 ? kUCols : 64) * kBK * 2;
         q.n_stages = 4;
-        const int chunks = div_up(p.T < kTok ? (p.T < p.n_adapters ? p.T : p.n_adapters) : (kTok < p.n_adapters ? kTok : p.n_adapters), q.slots);
-        // (an MMA always reads 128 token rows: the last stage's tile is followed by the rows it may reach)
-        const size_t smem = (size_t)q.n_stages * q.stage_bytes + kTok * kBK * 2 + 1024;
-        e = launch_pdl(adapter_kernel, dim3(m_tiles, chunks, p.u_splits), dim3(kUThreads), smem, st, q, um);
+        const size_t smem = (size_t)q.n_stages * q.stage_bytes + kTok * kBK * 2 + (size_t)kTok * (p.rank + 4) * sizeof(float) + 1024;
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = 1; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = q.u_splits;
+        cfg.attrs = attr; cfg.numAttrs = q.u_splits > 1 ? 2 : 1; cfg.stream = st;
+        cfg.gridDim = dim3(m_tiles, chunks, q.u_splits); cfg.blockDim = dim3(kUThreads); cfg.dynamicSmemBytes = smem;
+        e = cudaLaunchKernelEx(&cfg, adapter_kernel, q, um);
         if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.stream = st;
+    if (many) {
+        cudaError_t e = allow_smem(project_many_kernel, m_ok);
+        if (e != cudaSuccess) return e;
+        MMaps mm;
+        memset(&mm, 0, sizeof(mm));
+        p.ksteps = p.w ? div_up(p.K, kBK) : 0;
+        if (p.w && (!make_map_ld(&mm.x, p.x, p.T, p.K, p.ldx, kTok) || !make_map_ld(&mm.w, p.w, p.N, p.K, p.ldw, kTok)))
+            return cudaErrorInvalidValue;
+        if (p.n_adapters > 0 && (!make_map_3d(&mm.b, p.b, p.n_adapters, p.N, p.rank) || !make_map_3d(&mm.u, p.u, 2, p.T, p.rank)))
+            return cudaErrorInvalidValue;
+        const int u_tiles = p.n_adapters > 0 ? 2 * div_up(p.rank, kBK) : 0;      // 32 KB up to rank 64, 64 KB beyond
+        p.n_stages = u_tiles > 2 ? kMStages - 1 : kMStages;
+        const int tiles = div_up(p.N, kMTile) * div_up(p.T, kMTile), pairs = tiles < 74 ? tiles : 74;
+        cfg.gridDim = dim3(2 * pairs); cfg.blockDim = dim3(kMThreads); cfg.numAttrs = 2;
+        cfg.dynamicSmemBytes = (size_t)p.n_stages * kMStageBytes + (size_t)u_tiles * kUTile + 1024;
+        return cudaLaunchKernelEx(&cfg, project_many_kernel, p, mm);
     }
     cudaError_t e = allow_smem(project_kernel, p_ok);
     if (e != cudaSuccess) return e;
@@ -475,8 +967,11 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
     if (p.w && (!make_map_ld(&pm.x, p.x, p.T, p.K, p.ldx, p.a_rows) || !make_map_ld(&pm.w, p.w, p.N, p.K, p.ldw, kPN)))
         return cudaErrorInvalidValue;
     const int n_tiles = div_up(p.N, kPN);
-    p.splits = 1;
-    while (p.splits < 8 && n_tiles * m_tiles * p.splits * 2 <= 148 && p.ksteps / (p.splits * 2) >= 2) p.splits *= 2;
+    // as many parts of K as there are SMs for the tiles (a cluster holds eight), of two slices at least
+    p.splits = 148 / (n_tiles * m_tiles);
+    if (p.splits > 8) p.splits = 8;
+    if (p.splits > p.ksteps / 2) p.splits = p.ksteps / 2;
+    if (p.splits < 1) p.splits = 1;
     p.stage_bytes = p.a_bytes + kPN * kBK * 2;
     p.n_stages = div_up(p.ksteps, p.splits);
     if (p.n_stages > 6) p.n_stages = 6;
@@ -485,15 +980,9 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
     const size_t scratch = ((size_t)kPN * (p.a_rows + 1) + (size_t)(p.n_adapters > 0 ? p.a_rows * p.rank : 0)) * sizeof(float);
     if (smem < scratch) smem = scratch;
     smem += 1024;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3(n_tiles * p.splits, m_tiles); cfg.blockDim = dim3(kPThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = p.splits; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = p.splits > 1 ? 2 : 1;
+    cfg.gridDim = dim3(n_tiles * p.splits, m_tiles); cfg.blockDim = dim3(kPThreads); cfg.dynamicSmemBytes = smem;
+    attr[1].val.clusterDim.x = p.splits;
+    cfg.numAttrs = p.splits > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, project_kernel, p, pm);
 }
 

@@ -21,17 +21,18 @@ struct ProjectArgs {
     int64_t ldx, ldw, ldbase, ldo;
     int out_f32;
     int T, K, N, n_adapters, rank, n_tenants;
-    unsigned char* workspace;       // kProjectHeader bytes, then u f32 [splits][T][rank]
+    unsigned char* workspace;       // kProjectHeader bytes, then u [T][rank]: f32, or two bf16 arrays hi and lo
     int32_t* status;                // the caller's, or a word of the workspace
     // set by launch_project
     float* u;
-    int u_splits;                   // parts of K whose sums of u are stored apart (added up in a fixed order by the reader)
+    int u_pair;                     // u is stored as hi and lo
+    int u_splits;                   // parts of K of the first product (a cluster)
     int ksteps, splits, n_stages, stage_bytes, a_bytes, a_rows;
     int slots;                      // adapters per CTA of the first product
 };
 
 // bytes of the workspace for T tokens (n_adapters = 0: none)
-int64_t project_workspace(int T, int K, int rank, int n_adapters);
+int64_t project_workspace(int T, int rank, int n_adapters);
 cudaError_t launch_project(const ProjectArgs& args, cudaStream_t st);
 
 }  // namespace faasmoe
