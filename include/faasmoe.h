@@ -379,7 +379,7 @@ int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld
  *   tenant_id int32 [T];  adapter_of_tenant int32 [n_tenants] (DEVICE; a negative entry: no adapter) or NULL (tenant u uses
  *          adapter u, none if u >= n_adapters)
  *   out    f32 or bf16 (out_type) [T, N], rows ld_out apart
- *   workspace  moe_project_workspace() bytes of device memory, 256-byte aligned, that no other call uses meanwhile
+ *   workspace  moe_project_workspace() bytes of device memory, 256-byte aligned, that no other call uses meanwhile (NULL if 0)
  *   status_out device int32 or NULL: MOE_DEV_BAD_TENANT (tenant id outside [0, n_tenants): no adapter), MOE_DEV_BAD_ADAPTER and
  *          MOE_DEV_TIMEOUT are OR-ed into it; the caller clears it
  * n_adapters = 0: no adapters; a, b, scale, tenant_id, adapter_of_tenant and n_tenants are not looked at.
@@ -392,8 +392,9 @@ int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, i
                 int n_tenants, const void* base, int64_t ld_base, void* out, int64_t ld_out, int out_type, void* workspace,
                 int64_t workspace_bytes, int32_t* status_out, void* stream);
 
-/* Bytes of device memory that moe_project needs for T tokens (negative: MOE_ERR_SHAPE). */
-int64_t moe_project_workspace(int T, int K, int rank, int n_adapters);
+/* Bytes of device memory that moe_project needs (negative: MOE_ERR_SHAPE); 0 for few tokens with few adapters or low ranks,
+ * and without adapters. */
+int64_t moe_project_workspace(int T, int K, int N, int rank, int n_adapters);
 
 /* route -> dispatch -> experts -> combine on the context's workspace; bit-identical to
  * the four calls above.  out bf16 [T,H]. */

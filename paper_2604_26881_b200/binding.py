@@ -3,11 +3,13 @@
 Every function here has the name of the C entry point it calls (see
 include/faasmoe.h) and passes raw device pointers of torch tensors.  Nothing is
 computed in Python and there is no CPU fallback: if the library cannot be
-loaded, or a call fails, an exception is raised.
+loaded, or a call fails, an exception is raised.  The calls that take no
+context go through a small C extension instead of ctypes (csrc/calls.c).
 """
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 from ctypes import POINTER, byref, c_char_p, c_float, c_int, c_int32, c_int64, c_void_p
 
@@ -15,6 +17,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "lib", "libfaasmoe.so")
+CALLS_PATH = os.path.join(_HERE, "lib", "_calls.so")
 
 MOE_OK = 0
 MOE_ERR_NULL, MOE_ERR_SHAPE, MOE_ERR_G, MOE_ERR_STATE = -1, -2, -3, -4
@@ -116,7 +119,7 @@ def load_library(path: str | None = None):
         lib.moe_project.argtypes = ([c_void_p, c_int64, c_void_p, c_int64, c_int, c_int, c_int] + [c_void_p] * 3 + [c_int, c_int] +
                                     [c_void_p] * 2 + [c_int, c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64] +
                                     [c_void_p] * 2)
-        lib.moe_project_workspace.argtypes = [c_int, c_int, c_int, c_int]
+        lib.moe_project_workspace.argtypes = [c_int, c_int, c_int, c_int, c_int]
         lib.moe_project_workspace.restype = c_int64
         lib.moe_get_workspace.argtypes = [c_void_p] + [POINTER(c_void_p)] * 8
         lib.moe_last_status.argtypes = [c_void_p, POINTER(c_int32), POINTER(c_int32)]
@@ -300,60 +303,36 @@ def moe_stack_forward(ctx, x_inout, tenant_id, T, G, dbg_layer_inputs=None, dbg_
 
 
 # ---------------------------------------------------------------------------------------------------------------------
-# Calls without a context.  They take strided matrices (last dimension contiguous), check types, shapes and devices, and
-# run on the tensors' own device: on `stream`, or on that device's current stream.
+# Calls without a context.  They take strided matrices (last dimension contiguous), check types, shapes and devices
+# (ValueError), and run on the tensors' own device: on `stream`, or on that device's current stream.  The checks are made
+# in C (csrc/calls.c): in Python they take longer than the kernels.
 
-_RAW_STREAM = torch._C._cuda_getCurrentRawStream
-
-
-def _need(ok, fn, what):
-    if not ok:
-        raise ValueError(f"{fn}: {what}")
+_OTHER_DEVICE = 1
+_calls = None
 
 
-def _matrix(t, fn, name, rows, cols, dtypes, dev):
-    """Address and row distance of a [rows, cols] matrix (None: 0, 0)."""
-    if t is None:
-        return None, 0
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype not in dtypes or t.device != dev:
-        raise ValueError(f"{fn}: {name} must be [{rows}, {cols}] of {'/'.join(str(d)[6:] for d in dtypes)} on {dev}, "
-                         f"not {list(t.shape)} of {str(t.dtype)[6:]} on {t.device}")
-    ld, inner = t.stride()
-    if inner != 1 and cols > 1:
-        raise ValueError(f"{fn}: the columns of {name} must be contiguous (stride 1, not {inner})")
-    if rows <= 1:
-        ld = max(ld, cols)
-    if ld < cols:
-        raise ValueError(f"{fn}: the rows of {name} overlap (stride {ld} < {cols} columns)")
-    return t.data_ptr(), ld
+def _load_calls():
+    global _calls
+    lib = load_library()
+    if not os.path.exists(CALLS_PATH):
+        raise FileNotFoundError(f"{CALLS_PATH} not found: build it with `python -m paper_2604_26881_b200.build`")
+    spec = importlib.util.spec_from_file_location("paper_2604_26881_b200._calls", CALLS_PATH)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    address = lambda f: ctypes.cast(f, c_void_p).value
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    mod.bind(address(lib.moe_gate), address(lib.moe_add_rmsnorm), address(lib.moe_project), address(lib.moe_project_workspace),
+             torch.float32, torch.bfloat16, torch.int32, torch.uint8, torch.float8_e4m3fn, raw, now,
+             lambda n, device: torch.empty(n, dtype=torch.uint8, device=device), MoeGating)
+    _calls = mod
+    return mod
 
 
-def _flat(t, fn, name, n, dtype, dev):
-    """Address of a contiguous array of n elements (n < 0: any number; None: 0)."""
-    if t is None:
-        return None
-    if t.dtype != dtype or t.device != dev or not t.is_contiguous() or (n >= 0 and t.numel() != n):
-        raise ValueError(f"{fn}: {name} must be contiguous {str(dtype)[6:]} on {dev}" + (f", {n} elements" if n >= 0 else "") +
-                         f", not {list(t.shape)} of {str(t.dtype)[6:]} on {t.device}")
-    return t.data_ptr()
-
-
-def _call_on(dev, stream, fn, f, *args):
-    """f(*args, stream) with `dev` as the current device."""
-    if dev.type != "cuda":
-        raise ValueError(f"{fn}: tensors must be on a CUDA device, not {dev}")
-    if stream is not None:
-        _need(stream.device == dev, fn, f"the stream belongs to {stream.device}, the tensors to {dev}")
-        raw = stream.cuda_stream
-    else:
-        raw = _RAW_STREAM(dev.index)
-    if torch.cuda.current_device() == dev.index:
-        status = f(*args, raw)
-    else:
-        with torch.cuda.device(dev):
-            status = f(*args, raw)
-    if status != MOE_OK:
-        raise MoeError(fn, status)
+def _on_device(fn, device, *args):
+    """A call that found its tensors on another device than the current one, again with that device current."""
+    with torch.cuda.device(device):
+        return getattr(_calls, fn)(*args)
 
 
 _SCORES = {"softmax": MOE_SCORE_SOFTMAX, "sigmoid": MOE_SCORE_SIGMOID}
@@ -366,28 +345,18 @@ def moe_gating(*, score="softmax", n_groups=1, keep_groups=None, group_score="ma
                      1 if renormalize else 0, scale)
 
 
-_LOGITS_TYPES = {torch.float32: MOE_TYPE_F32, torch.bfloat16: MOE_TYPE_BF16}
-
-
 def moe_gate(logits, rule, topk_idx, topk_w, *, balance_bias=None, tenant_id=None, model_of_tenant=None, tie_flag=None,
              status_out=None, stream=None):
     """Chooses k experts per token from logits [T, E] (fp32 or bf16, rows may be strided) by `rule` (moe_gating()).
 
     topk_idx [T, k] int32 and topk_w [T, k] float32 receive the choice; k is their width.  balance_bias [M, E] float32;
     tenant_id [T] and model_of_tenant [n_tenants] int32 (device) pick the bias row.  See include/faasmoe.h."""
-    fn, dev = "moe_gate", logits.device
-    _need(logits.dim() == 2 and topk_idx.dim() == 2 and isinstance(rule, MoeGating), fn, "logits [T, E], a moe_gating() rule and topk_idx [T, k] are needed")
-    (T, E), k = logits.shape, topk_idx.shape[1]
-    p_logits, ld = _matrix(logits, fn, "logits", T, E, _LOGITS_TYPES, dev)
-    M = 1
-    if balance_bias is not None:
-        M = balance_bias.shape[0] if balance_bias.dim() == 2 else 1
-    _call_on(dev, stream, fn, load_library().moe_gate, p_logits, _LOGITS_TYPES[logits.dtype], ld, T, E, k, byref(rule),
-             _flat(balance_bias, fn, "balance_bias", M * E, torch.float32, dev), _flat(tenant_id, fn, "tenant_id", T, torch.int32, dev),
-             _flat(model_of_tenant, fn, "model_of_tenant", -1, torch.int32, dev),
-             model_of_tenant.numel() if model_of_tenant is not None else 1 << 30, M,
-             _flat(topk_idx, fn, "topk_idx", T * k, torch.int32, dev), _flat(topk_w, fn, "topk_w", T * k, torch.float32, dev),
-             _flat(tie_flag, fn, "tie_flag", T, torch.uint8, dev), _flat(status_out, fn, "status_out", 1, torch.int32, dev))
+    args = (logits, rule, topk_idx, topk_w, balance_bias, tenant_id, model_of_tenant, tie_flag, status_out, stream)
+    status = (_calls or _load_calls()).moe_gate(*args)
+    if status:
+        if status == _OTHER_DEVICE:
+            status = _on_device("moe_gate", logits.device, *args)
+        _check("moe_gate", status)
 
 
 def moe_set_gating(ctx, layer, rule, balance_bias=None):
@@ -396,39 +365,22 @@ def moe_set_gating(ctx, layer, rule, balance_bias=None):
     _check("moe_set_gating", load_library().moe_set_gating(ctx, layer, byref(rule) if rule is not None else None, _ptr(balance_bias)))
 
 
-_BF16 = (torch.bfloat16,)
-_E4M3 = (torch.float8_e4m3fn,)
-
-
 def moe_add_rmsnorm(x, weight, eps, *, residual=None, residual_out=None, out=None, out_q=None, q_scale=None, stream=None):
     """residual_out = h = bf16(x + residual); out = bf16(RMSNorm(h) * weight); out_q = e4m3 of the same with scales.
 
     x, residual, residual_out, out: bf16 [T, H], rows may be strided; out_q float8_e4m3fn [T, H]; q_scale float32 [T, 1]
     (one scale per row) or [T, ceil(H/128)] (one per 128 columns).  residual_out may be residual or x; out may be x."""
-    fn, dev = "moe_add_rmsnorm", x.device
-    _need(x.dim() == 2, fn, "x must be [T, H]")
-    T, H = x.shape
-    px, ldx = _matrix(x, fn, "x", T, H, _BF16, dev)
-    pr, ldr = _matrix(residual, fn, "residual", T, H, _BF16, dev)
-    pro, ldro = _matrix(residual_out, fn, "residual_out", T, H, _BF16, dev)
-    po, ldo = _matrix(out, fn, "out", T, H, _BF16, dev)
-    pq, ldq = _matrix(out_q, fn, "out_q", T, H, _E4M3, dev)
-    group = 0
-    _need((out_q is None) == (q_scale is None), fn, "out_q and q_scale go together")
-    if q_scale is not None:
-        n = -(-H // 128)
-        _need(q_scale.dim() == 2 and q_scale.shape[0] == T and q_scale.shape[1] in (1, n), fn, f"q_scale must be [{T}, 1] or [{T}, {n}]")
-        group = 0 if q_scale.shape[1] == 1 else 128       # (one group of at most 128 columns is the row)
-    _call_on(dev, stream, fn, load_library().moe_add_rmsnorm, px, ldx, pr, ldr, _flat(weight, fn, "weight", H, torch.bfloat16, dev), eps,
-             T, H, pro, ldro, po, ldo, pq, ldq, _flat(q_scale, fn, "q_scale", -1, torch.float32, dev), group)
+    args = (x, weight, eps, residual, residual_out, out, out_q, q_scale, stream)
+    status = (_calls or _load_calls()).moe_add_rmsnorm(*args)
+    if status:
+        if status == _OTHER_DEVICE:
+            status = _on_device("moe_add_rmsnorm", x.device, *args)
+        _check("moe_add_rmsnorm", status)
 
 
-_OUT_TYPES = {torch.float32: MOE_TYPE_F32, torch.bfloat16: MOE_TYPE_BF16}
-
-
-def moe_project_workspace(T, K, rank=0, n_adapters=0) -> int:
-    """Bytes of workspace that moe_project needs."""
-    n = load_library().moe_project_workspace(T, K, rank, n_adapters)
+def moe_project_workspace(T, K, N, rank=0, n_adapters=0) -> int:
+    """Bytes of workspace that moe_project needs (0: none)."""
+    n = load_library().moe_project_workspace(T, K, N, rank, n_adapters)
     if n < 0:
         raise MoeError("moe_project_workspace", n)
     return n
@@ -442,41 +394,17 @@ def moe_project(x, w, out, *, base=None, a=None, b=None, scale=None, tenant_id=N
     [n, rank, K], b bf16 [n, N, rank], scale float32 [n] or None; tenant_id int32 [T]; adapter_of_tenant int32 [n_tenants]
     on the device (None: tenant u has adapter u; n_tenants then defaults to n).  workspace: uint8 tensor, by default
     allocated for the call on its stream.  See include/faasmoe.h."""
-    fn, dev = "moe_project", x.device
-    _need(x.dim() == 2 and out.dim() == 2, fn, "x must be [T, K] and out [T, N]")
-    (T, K), N = x.shape, out.shape[1]
-    px, ldx = _matrix(x, fn, "x", T, K, _BF16, dev)
-    pw, ldw = _matrix(w, fn, "w", N, K, _BF16, dev)
-    po, ldo = _matrix(out, fn, "out", T, N, _OUT_TYPES, dev)
-    pb, ldb = _matrix(base, fn, "base", T, N, (out.dtype,), dev)
-    n = rank = 0
-    pa = pbb = ps = pt = pm = None
-    _need((a is None) == (b is None), fn, "a and b go together")
-    if a is not None:
-        _need(a.dim() == 3, fn, "a must be [n_adapters, rank, K]")
-        n, rank = a.shape[0], a.shape[1]
-        pa, pbb = _flat(a, fn, "a", n * rank * K, torch.bfloat16, dev), _flat(b, fn, "b", n * N * rank, torch.bfloat16, dev)
-        _need(a.shape[2] == K and b.dim() == 3 and b.shape[1] == N and b.shape[2] == rank, fn, f"a must be [n, rank, {K}] and b [n, {N}, rank]")
-        ps, pt = _flat(scale, fn, "scale", n, torch.float32, dev), _flat(tenant_id, fn, "tenant_id", T, torch.int32, dev)
-        pm = _flat(adapter_of_tenant, fn, "adapter_of_tenant", -1, torch.int32, dev)
-        if adapter_of_tenant is not None:
-            n_tenants = adapter_of_tenant.numel()
-        elif n_tenants is None:
-            n_tenants = n
-    lib = load_library()
-    if workspace is None:
-        size = lib.moe_project_workspace(T, K, rank, n)
-        if size > 0 and dev.type == "cuda":
-            if stream is None:
-                workspace = torch.empty(size, dtype=torch.uint8, device=dev)
-            else:
-                with torch.cuda.stream(stream):
-                    workspace = torch.empty(size, dtype=torch.uint8, device=dev)
-    pws, ws_bytes = None, 0
-    if workspace is not None:
-        pws, ws_bytes = _flat(workspace, fn, "workspace", -1, torch.uint8, dev), workspace.numel()
-    _call_on(dev, stream, fn, lib.moe_project, px, ldx, pw, ldw, T, K, N, pa, pbb, ps, n, rank, pt, pm, n_tenants or 0, pb, ldb, po, ldo,
-             _OUT_TYPES[out.dtype], pws, ws_bytes, _flat(status_out, fn, "status_out", 1, torch.int32, dev))
+    if stream is not None and workspace is None and x.dim() == 2 and x.is_cuda and a is not None and a.dim() == 3:
+        n = load_library().moe_project_workspace(x.shape[0], x.shape[1], out.shape[-1], a.shape[1], a.shape[0])
+        if n > 0:
+            with torch.cuda.stream(stream):                  # (the allocator must know which stream uses it)
+                workspace = torch.empty(n, dtype=torch.uint8, device=x.device)
+    args = (x, w, out, base, a, b, scale, tenant_id, adapter_of_tenant, n_tenants, workspace, status_out, stream)
+    status = (_calls or _load_calls()).moe_project(*args)
+    if status:
+        if status == _OTHER_DEVICE:
+            status = _on_device("moe_project", x.device, *args)
+        _check("moe_project", status)
 
 
 def moe_get_workspace(ctx):

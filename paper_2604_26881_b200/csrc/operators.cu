@@ -84,11 +84,11 @@ int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld
     return cuda_result("moe_add_rmsnorm", launch_addnorm(a, (cudaStream_t)stream));
 }
 
-int64_t moe_project_workspace(int T, int K, int rank, int n_adapters)
+int64_t moe_project_workspace(int T, int K, int N, int rank, int n_adapters)
 {
-    if (T < 0 || T > kProjectMaxTokens || K < 1 || n_adapters < 0) return MOE_ERR_SHAPE;
+    if (T < 0 || T > kProjectMaxTokens || K < 1 || N < 1 || n_adapters < 0) return MOE_ERR_SHAPE;
     if (n_adapters > 0 && (rank < 1 || rank > kAdapterMaxRank)) return MOE_ERR_SHAPE;
-    return project_workspace(T, rank, n_adapters);
+    return project_workspace(T, K, N, rank, n_adapters);
 }
 
 int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, int K, int N, const void* a, const void* b,
@@ -109,9 +109,11 @@ int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, i
     if (adapters && (off(a, 16) || off(b, 16) || off(scale, 4) || off(tenant_id, 4) || off(adapter_of_tenant, 4))) return MOE_ERR_SHAPE;
     if (off(workspace, 256)) return MOE_ERR_SHAPE;
     if (T == 0) return MOE_OK;
-    if (!out || !workspace || (!w && !adapters && !base)) return MOE_ERR_NULL;
+    if (!out || (!w && !adapters && !base)) return MOE_ERR_NULL;
     if (((w || adapters) && !x) || (adapters && (!a || !b || !tenant_id))) return MOE_ERR_NULL;
-    if (workspace_bytes < project_workspace(T, rank, n_adapters)) return MOE_ERR_ALLOC;
+    const int64_t need = project_workspace(T, K, N, rank, n_adapters);
+    if (need > 0 && !workspace) return MOE_ERR_NULL;
+    if (workspace_bytes < need) return MOE_ERR_ALLOC;
     ProjectArgs p = {};
     p.x = (const bf16*)x; p.w = (const bf16*)w; p.ldx = ldx; p.ldw = ldw; p.T = T; p.K = K; p.N = N;
     if (adapters) {
@@ -119,8 +121,8 @@ int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, i
         p.tenant_id = tenant_id; p.adapter_of_tenant = adapter_of_tenant; p.n_tenants = n_tenants;
     }
     p.base = base; p.ldbase = ld_base; p.out = out; p.ldo = ld_out; p.out_f32 = out_type == MOE_TYPE_F32;
-    p.workspace = (unsigned char*)workspace;
-    p.status = status_out ? status_out : (int32_t*)workspace;
+    p.u = (float*)workspace;
+    p.status = status_out;
     return cuda_result("moe_project", launch_project(p, (cudaStream_t)stream));
 }
 

@@ -19,12 +19,14 @@ namespace {
 
 using namespace tc;
 
+__device__ int32_t g_project_status;      // where the status bits go of calls that did not ask for them
+
 constexpr uint32_t kFull = 0xffffffffu;
 constexpr int kTok = 128;               // tokens per tile: the M operand, one TMEM lane each
 constexpr int kBK = 64;                 // K elements per slice: one 128-byte row of a swizzled tile
 constexpr int kMaxStages = 8;
 constexpr int kUCols = 128;             // columns of one CTA of the first product
-constexpr int kUThreads = 192;          // warp 0: TMA, 1: MMA, 2..5: lists and epilogue
+constexpr int kUThreads = 224;          // warp 0: TMA (tokens), 1: MMA, 2..5: lists and epilogue, 6: TMA (rows of A)
 constexpr int kPN = 128;                // weight rows per tile of the projection
 constexpr int kPThreads = 352;          // warp 0: TMA (weights), 1: MMA, 2..9: epilogue, 10: TMA (tokens)
 
@@ -40,12 +42,16 @@ __device__ __forceinline__ uint32_t map_to_cta(uint32_t local_addr, uint32_t ran
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local_addr), "r"(rank));
     return r;
 }
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr)
+// Copies shared memory of this CTA to another of the cluster; the bytes are counted on a barrier of the receiver.  (Single
+// remote stores were measured at about 30 cycles each, one after the other: 4 us for one token's sums in a cluster of eight.)
+__device__ __forceinline__ void send_bulk(uint32_t dst, uint32_t src, uint32_t bytes, uint32_t bar)
 {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "r"(src), "r"(bytes), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync_all()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -58,17 +64,18 @@ __device__ __forceinline__ uint32_t idesc_bf16(int n)
 }
 
 // Adapter of token t, or -1.  Ids outside their range set a status bit and count as none.
+__device__ __forceinline__ int32_t* status_of(const ProjectArgs& p) { return p.status ? p.status : &g_project_status; }
 __device__ __forceinline__ int adapter_of(const ProjectArgs& p, int t, bool report)
 {
     const int u = p.tenant_id[t];
     if (u < 0 || u >= p.n_tenants) {
-        if (report) atomicOr(p.status, MOE_DEV_BAD_TENANT);
+        if (report) atomicOr(status_of(p), MOE_DEV_BAD_TENANT);
         return -1;
     }
     const int a = p.adapter_of_tenant ? p.adapter_of_tenant[u] : u;
     if (a < 0) return -1;
     if (a >= p.n_adapters) {
-        if (report && p.adapter_of_tenant) atomicOr(p.status, MOE_DEV_BAD_ADAPTER);
+        if (report && p.adapter_of_tenant) atomicOr(status_of(p), MOE_DEV_BAD_ADAPTER);
         return -1;
     }
     return a;
@@ -140,24 +147,28 @@ __global__ void __launch_bounds__(kUThreads)
 adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
 {
     extern __shared__ unsigned char smem_dyn[];
+    int32_t* const status = status_of(p);
     const uint32_t ring = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-    __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 2];
+    __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 4];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     __shared__ AdapterList<4> s_al;
     __shared__ int s_slot[kTok];
     const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * kMaxStages, bar_done = bar_full + 16 * kMaxStages,
-                   bar_free = bar_done + 8;
+                   bar_free = bar_done + 8, bar_list = bar_done + 16, bar_got = bar_done + 24;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int t0 = blockIdx.x * kTok;
-    const int pitch = p.rank + 4;
-    // this part's sums of the tile's tokens, behind the ring (and the rows that the MMA of a short tile may read)
-    float* const su = reinterpret_cast<float*>(smem_dyn + (ring - smem_u32(smem_dyn)) + p.n_stages * p.stage_bytes + kTok * kBK * 2);
-
+    // Behind the ring (and the rows that the MMA of a short tile may read): this part's sums, [owner][column][token of the
+    // owner], and those that the cluster's CTAs send here, [part][column][own token].  A CTA owns a share of the tokens.
+    const int own = p.u_own, pitch = own + 4, block = p.rank * pitch;
+    float* const sums = reinterpret_cast<float*>(smem_dyn + (ring - smem_u32(smem_dyn)) + p.scratch);
+    float* const got = p.u_splits > 1 ? sums + p.u_splits * block : sums;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < p.n_stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+        for (int s = 0; s < p.n_stages; ++s) { mbar_init(bar_full + 8 * s, 2); mbar_init(bar_empty + 8 * s, 1); }
         mbar_init(bar_done, 1);
         mbar_init(bar_free, 4);
+        mbar_init(bar_list, 4);
+        mbar_init(bar_got, 1);
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -166,123 +177,156 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"((uint32_t)kUCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (p.u_splits > 1) cluster_arrive();       // (waited for before anything is sent: the peers run and their barriers are there)
+    const uint32_t tmem = s_tmem;
     pdl_wait();
     pdl_launch_dependents();        // (after the wait: the projection may read x before it waits itself)
 
-    if (warp >= 2) {
+    const int k0 = (int)((long long)p.ksteps * blockIdx.z / p.u_splits), k1 = (int)((long long)p.ksteps * (blockIdx.z + 1) / p.u_splits);
+    int count = 0, n_chunks = 0;
+    auto know_list = [&] {                      // (every role but the listing warps)
+        if (!mbar_wait(bar_list, 0, &s_abort, status)) return false;
+        count = s_al.count;
+        n_chunks = (count + p.slots - 1) / p.slots;
+        return true;
+    };
+    if (warp == 0 || warp == 6) {
+        // two lanes in two warps, so that the tokens need not wait for the list and the loads of a stage are issued side by side
+        if (lane == 0) {
+            uint32_t stage = 0, phase = 0, armed = 0, armed_phase = 0;
+            bool ok = true;
+            // the tokens of the first slices, before the list is known (it is empty only if no token has an adapter)
+            if (warp == 6) ok = know_list();
+            bool known = warp == 6;
+            for (int c = blockIdx.y; ok && (!known || c < n_chunks); c += gridDim.y) {
+                for (int ks = k0; ks < k1; ++ks) {
+                    if (!known && (ks - k0 == p.n_stages || blockIdx.y > 0)) {
+                        if (!know_list()) { ok = false; break; }
+                        known = true;
+                        if (c >= n_chunks) break;
+                    }
+                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, status)) { ok = false; break; }
+                    const uint32_t sa = ring + stage * p.stage_bytes, sb = sa + p.a_bytes, full = bar_full + 8 * stage;
+                    armed |= 1u << stage;
+                    armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
+                    if (warp == 0) {
+                        mbar_expect_tx(full, p.a_rows * kBK * 2);
+                        tma_load_2d(sa, &maps.x, full, ks * kBK, t0);
+                    } else {
+                        const int n_slots = min(p.slots, count - c * p.slots);
+                        mbar_expect_tx(full, n_slots * p.rank * kBK * 2);
+                        for (int j = 0; j < n_slots; ++j)
+                            tma_load_2d(sb + j * p.rank * kBK * 2, &maps.a, full, ks * kBK, s_al.list[c * p.slots + j] * p.rank);
+                    }
+                    if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
+                }
+                if (ok && !known) {
+                    ok = know_list();
+                    known = true;
+                }
+            }
+            if (ok && warp == 0 && n_chunks <= (int)blockIdx.y) {
+                // no adapter to work on: the slices that were asked for early still have to land before the block exits; the
+                // other lane's arrival, which completes a stage, is made here
+                for (int s = 0; s < p.n_stages; ++s)
+                    if (armed & (1u << s)) { mbar_arrive(bar_full + 8 * s); mbar_wait(bar_full + 8 * s, 0, &s_abort, status); }
+            }
+            if (!ok && warp == 0)
+                for (int s = 0; s < p.n_stages; ++s)
+                    if (armed & (1u << s)) mbar_wait(bar_full + 8 * s, (armed_phase >> s) & 1u, &s_abort, status);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            uint32_t stage = 0, phase = 0;
+            bool ok = know_list();
+            int it = 0;
+            for (int c = blockIdx.y; c < n_chunks && ok; c += gridDim.y, ++it) {
+                // (rank 8 and an odd number of adapters: eight stale columns, never read)
+                const int cols = (min(p.slots, count - c * p.slots) * p.rank + 15) & ~15;
+                const uint32_t idesc = idesc_bf16(cols);
+                if (!mbar_wait(bar_free, (it & 1) ^ 1, &s_abort, status)) { ok = false; break; }
+                tc_fence_after();
+                uint32_t acc = 0;
+                for (int ks = k0; ks < k1; ++ks) {
+                    if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, status)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t lo_a = smem_desc_lo(ring + stage * p.stage_bytes), lo_b = lo_a + (p.a_bytes >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < kBK / 16; ++kk) {
+                        umma_bf16(tmem, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, acc);
+                        acc = 1;
+                    }
+                    umma_commit(bar_empty + 8 * stage);
+                    if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
+                }
+                if (ok) umma_commit(bar_done);
+            }
+        }
+        __syncwarp();
+    } else {
         int slot[1];
         list_adapters<4>(p, s_al, t0, warp - 2, lane, blockIdx.y == 0 && blockIdx.z == 0,
                          [] { asm volatile("bar.sync 1, 128;" ::: "memory"); }, slot);
         s_slot[threadIdx.x - 64] = slot[0];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_list);
+        __all_sync(kFull, know_list());
+        // thread <-> token; a warp reads the TMEM lanes of its quarter
+        const int quarter = warp & 3, row = quarter * 32 + lane, my_slot = s_slot[row];
+        float* const dst = sums + (row / own) * block + row % own;
+        int it = 0;
+        for (int c0 = blockIdx.y; c0 < n_chunks; c0 += gridDim.y, ++it) {
+            const int f = my_slot - c0 * p.slots;
+            const bool live = my_slot >= 0 && f >= 0 && f < p.slots;
+            const int cols = min(p.slots, count - c0 * p.slots) * p.rank;
+            const int c_lo = live ? f * p.rank : cols, c_hi = live ? c_lo + p.rank : 0;
+            if (!__all_sync(kFull, mbar_wait(bar_done, it & 1, &s_abort, status))) break;
+            tc_fence_after();
+            for (int c = 0; c < cols; c += 16) {
+                if (!__any_sync(kFull, c + 16 > c_lo && c < c_hi)) continue;
+                uint32_t r[16];
+                tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + c, r);
+                tmem_ld_wait();
+#pragma unroll
+                for (int h = 0; h < 16; h += 8)
+                    if (c + h >= c_lo && c + h < c_hi) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) dst[(c + h + i - c_lo) * pitch] = __uint_as_float(r[h + i]);
+                    }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_free);
+        }
+        fence_async_shared();                   // (the sums leave by bulk copies)
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = s_tmem;
-    const int count = s_al.count, n_chunks = (count + p.slots - 1) / p.slots;
-    const bool work = (int)blockIdx.y < n_chunks;                       // (the same for the whole cluster)
-    if (work) {
-        const int k0 = (int)((long long)p.ksteps * blockIdx.z / p.u_splits), k1 = (int)((long long)p.ksteps * (blockIdx.z + 1) / p.u_splits);
-        if (warp == 0) {
-            if (lane == 0) {
-                uint32_t stage = 0, phase = 0, armed = 0, armed_phase = 0;
-                bool ok = true;
-                for (int c = blockIdx.y; c < n_chunks && ok; c += gridDim.y) {
-                    const int n_slots = min(p.slots, count - c * p.slots);
-                    for (int ks = k0; ks < k1; ++ks) {
-                        if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, p.status)) { ok = false; break; }
-                        const uint32_t sa = ring + stage * p.stage_bytes, sb = sa + p.a_bytes, full = bar_full + 8 * stage;
-                        armed |= 1u << stage;
-                        armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
-                        mbar_expect_tx(full, (p.a_rows + n_slots * p.rank) * kBK * 2);
-                        tma_load_2d(sa, &maps.x, full, ks * kBK, t0);
-                        for (int j = 0; j < n_slots; ++j)
-                            tma_load_2d(sb + j * p.rank * kBK * 2, &maps.a, full, ks * kBK, s_al.list[c * p.slots + j] * p.rank);
-                        if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
-                    }
-                }
-                if (!ok)
-                    for (int s = 0; s < p.n_stages; ++s)
-                        if (armed & (1u << s)) mbar_wait(bar_full + 8 * s, (armed_phase >> s) & 1u, &s_abort, p.status);
-            }
-            __syncwarp();
-        } else if (warp == 1) {
-            if (lane == 0) {
-                uint32_t stage = 0, phase = 0;
-                bool ok = true;
-                int it = 0;
-                for (int c = blockIdx.y; c < n_chunks && ok; c += gridDim.y, ++it) {
-                    // (rank 8 and an odd number of adapters: eight stale columns, never read)
-                    const int cols = (min(p.slots, count - c * p.slots) * p.rank + 15) & ~15;
-                    const uint32_t idesc = idesc_bf16(cols);
-                    if (!mbar_wait(bar_free, (it & 1) ^ 1, &s_abort, p.status)) { ok = false; break; }
-                    tc_fence_after();
-                    uint32_t acc = 0;
-                    for (int ks = k0; ks < k1; ++ks) {
-                        if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, p.status)) { ok = false; break; }
-                        tc_fence_after();
-                        const uint32_t lo_a = smem_desc_lo(ring + stage * p.stage_bytes), lo_b = lo_a + (p.a_bytes >> 4);
-#pragma unroll
-                        for (int kk = 0; kk < kBK / 16; ++kk) {
-                            umma_bf16(tmem, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, acc);
-                            acc = 1;
-                        }
-                        umma_commit(bar_empty + 8 * stage);
-                        if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
-                    }
-                    if (ok) umma_commit(bar_done);
-                }
-            }
-            __syncwarp();
-        } else {
-            // thread <-> token; a warp reads the TMEM lanes of its quarter
-            const int quarter = warp & 3, row = quarter * 32 + lane;
-            float* dst = su + row * pitch;
-            int it = 0;
-            for (int c0 = blockIdx.y; c0 < n_chunks; c0 += gridDim.y, ++it) {
-                const int f = s_slot[row] - c0 * p.slots;
-                const bool live = s_slot[row] >= 0 && f >= 0 && f < p.slots;
-                const int cols = min(p.slots, count - c0 * p.slots) * p.rank;
-                const int c_lo = live ? f * p.rank : cols, c_hi = live ? c_lo + p.rank : 0;
-                if (!__all_sync(kFull, mbar_wait(bar_done, it & 1, &s_abort, p.status))) break;
-                tc_fence_after();
-                for (int c = 0; c < cols; c += 16) {
-                    if (!__any_sync(kFull, c + 16 > c_lo && c < c_hi)) continue;
-                    uint32_t r[16];
-                    tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + c, r);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int h = 0; h < 16; h += 8)
-                        if (c + h >= c_lo && c + h < c_hi) {
-                            float4* o = reinterpret_cast<float4*>(dst + (c + h - c_lo));
-                            o[0] = make_float4(__uint_as_float(r[h]), __uint_as_float(r[h + 1]), __uint_as_float(r[h + 2]), __uint_as_float(r[h + 3]));
-                            o[1] = make_float4(__uint_as_float(r[h + 4]), __uint_as_float(r[h + 5]), __uint_as_float(r[h + 6]), __uint_as_float(r[h + 7]));
-                        }
-                }
-                tc_fence_before();
+    if (p.u_splits > 1) cluster_wait();
+    if (p.slots * (int)blockIdx.y < s_al.count) {           // there was a chunk for this cluster
+        if (p.u_splits > 1) {
+            if (warp == 0) {
+                if (lane == 0) mbar_expect_tx(bar_got, p.u_splits * block * 4);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar_free);
+                if (lane < p.u_splits)
+                    send_bulk(map_to_cta(smem_u32(got + blockIdx.z * block), lane), smem_u32(sums + lane * block), block * 4, map_to_cta(bar_got, lane));
             }
+            mbar_wait(bar_got, 0, &s_abort, status);
+            __syncwarp();
+            cluster_arrive();                   // (waited for below: nobody leaves while its copies may still be on their way)
         }
-        tc_fence_before();
-        if (p.u_splits > 1) cluster_sync_all(); else __syncthreads();
-        // this CTA adds up a share of the tokens over the parts
+        // this CTA adds up its share of the tokens over the parts, in their order
         if (!s_abort) {
-            const int r0 = kTok * blockIdx.z / p.u_splits, r1 = kTok * (blockIdx.z + 1) / p.u_splits;
-            const uint32_t su_addr = smem_u32(su);
-            for (int e = r0 * p.rank + threadIdx.x; e < r1 * p.rank; e += kUThreads) {
-                const int row = e / p.rank, c = e - row * p.rank, slot = s_slot[row];
+            for (int e = threadIdx.x; e < own * p.rank; e += kUThreads) {
+                const int r = e / p.rank, c = e - r * p.rank, row = own * blockIdx.z + r, slot = s_slot[row];
                 if (slot < 0 || (slot / p.slots) % gridDim.y != blockIdx.y) continue;
                 float v = 0.f;
-                if (p.u_splits > 1) {
-                    float q[8];
-#pragma unroll
-                    for (int z = 0; z < 8; ++z) q[z] = z < p.u_splits ? ld_cluster_f32(map_to_cta(su_addr + 4 * (row * pitch + c), z)) : 0.f;
-#pragma unroll
-                    for (int z = 0; z < 8; ++z) v += q[z];
-                } else {
-                    v = su[row * pitch + c];
-                }
+                for (int z = 0; z < p.u_splits; ++z) v += got[z * block + c * pitch + r];
                 if (p.scale) v *= p.scale[s_al.adapter[row]];
                 const size_t at = (size_t)(t0 + row) * p.rank + c;
                 if (p.u_pair) {
@@ -297,7 +341,7 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
                 }
             }
         }
-        if (p.u_splits > 1) cluster_sync_all();                         // nobody leaves while a peer may still read its sums
+        if (p.u_splits > 1) cluster_wait();
     }
     tc_fence_before();
     __syncthreads();
@@ -308,64 +352,99 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
     }
 }
 
-struct PMaps { CUtensorMap x, w; };
+struct PMaps { CUtensorMap x, w, a; };
 
-// One cluster of `splits` CTAs per tile of 128 tokens x 128 weight rows; each CTA contracts over its share of K into its
-// own TMEM accumulator, leaves the sums in shared memory, and adds up a share of the columns over the cluster (distributed
-// shared memory, ranks in order: the same bits every time).  The adapters' second product and the base are added there, in fp32.
-__global__ void __launch_bounds__(kPThreads)
+// Few tokens: one cluster of `splits` CTAs per tile of 128 tokens x 128 weight rows; each CTA contracts over its share of K
+// into its own TMEM accumulator and sends every column's sums to the CTA that adds that column up (distributed shared
+// memory; the parts are added in their order: the same bits every time).  The adapters' second product and the base
+// are added there, in fp32 on the CUDA cores: with few tokens that is a few hundred thousand products, and every token may
+// have an adapter of its own.
+//
+// FUSED: the rows of A of the tile's adapters ride as further columns of the same MMA, so u comes out of the same pass (every
+// cluster computes it for itself) and there is no first launch.
+template <bool FUSED>
+__global__ void __launch_bounds__(kPThreads, 2)
 project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
 {
-    extern __shared__ unsigned char smem_dyn[];
+    extern __shared__ __align__(16) unsigned char smem_dyn[];
+    int32_t* const status = status_of(p);
     const uint32_t ring = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-    float* const part = reinterpret_cast<float*>(smem_dyn + (ring - smem_u32(smem_dyn)));      // the ring, when its stages are done
-    __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 1];
+    __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 3];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     __shared__ int s_adapter[kTok];
-    const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * kMaxStages, bar_done = bar_full + 16 * kMaxStages;
+    __shared__ AdapterList<4> s_al;
+    __shared__ int s_slot[kTok];
+    const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * kMaxStages, bar_done = bar_full + 16 * kMaxStages,
+                   bar_list = bar_done + 8, bar_got = bar_done + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int S = p.splits;
     const uint32_t rank = S > 1 ? cluster_ctarank() : 0u;
     const int n0 = (blockIdx.x / S) * kPN, t0 = blockIdx.y * kTok;
     const int rows = min(kTok, p.T - t0);
-    const int pitch = p.a_rows + 1;                       // part[column][token], odd pitch: no bank conflicts either way
-    const bool product = p.ksteps > 0, adapters = p.n_adapters > 0;
+    const bool product = p.w != nullptr, adapters = p.n_adapters > 0;
+    const int w_rows = product ? kPN : 0;
+    constexpr uint32_t kTmem = FUSED ? 256u : (uint32_t)kPN;
+    // Behind the ring (and the rows that the MMA of a short tile may read): the sums sent here, [part][own column][token], then
+    // (fused) the parts of u, [part][rank][token], then u itself, [token][rank].  This CTA's own sums, [column][token] of
+    // the product and of u, are put together in the ring when its stages are done.
+    const int c0 = (int)(kPN * rank) / S, nc = (int)(kPN * (rank + 1)) / S - c0, nc_max = (kPN + S - 1) / S;
+    const int pitch = p.a_rows + 4;
+    float* const own = reinterpret_cast<float*>(smem_dyn + (ring - smem_u32(smem_dyn)));
+    float* const own_u = own + kPN * pitch;
+    float* const part = reinterpret_cast<float*>(smem_dyn + (ring - smem_u32(smem_dyn)) + p.scratch);
+    float* const u_part = part + S * nc_max * pitch;
+    float* const su = u_part + (FUSED ? S * p.rank * pitch : 0);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < p.n_stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+        for (int s = 0; s < p.n_stages; ++s) { mbar_init(bar_full + 8 * s, FUSED ? 2 : 1); mbar_init(bar_empty + 8 * s, 1); }
         mbar_init(bar_done, 1);
+        mbar_init(bar_list, 4);
+        mbar_init(bar_got, 1);
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
         __syncwarp();
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"((uint32_t)kPN) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(kTmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
+    if (S > 1) cluster_arrive();                            // (waited for before anything is sent: the peers run and their barriers are there)
     tc_fence_after();
     const uint32_t tmem = s_tmem;
-    // With adapters the launch before this one is adapter_kernel, which had waited for everything before it when it let this
-    // kernel start: x, W and the tenant ids are complete.  Without, it is some other kernel.
-    if (!adapters) pdl_wait();
+    // With a first launch that one is adapter_kernel, which had waited for everything before it when it let this kernel start:
+    // x, W and the tenant ids are complete.  Otherwise the kernel before this one is some other's.
+    if (FUSED || !adapters) pdl_wait();
     pdl_launch_dependents();
 
-    if (product) {
-        const int k0 = (int)((long long)p.ksteps * rank / S), k1 = (int)((long long)p.ksteps * (rank + 1) / S);
+    const int ks_n = product || FUSED ? p.ksteps : 0;
+    const int k0 = (int)((long long)ks_n * rank / S), k1 = (int)((long long)ks_n * (rank + 1) / S);
+    if (k1 > k0) {
         if (warp == 0 || warp == 10) {
             if (lane == 0) {
                 uint32_t stage = 0, phase = 0, armed = 0, armed_phase = 0;
                 bool ok = true;
+                int count = -1;
                 for (int ks = k0; ks < k1; ++ks) {
-                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, p.status)) { ok = false; break; }
+                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, status)) { ok = false; break; }
                     const uint32_t sa = ring + stage * p.stage_bytes, full = bar_full + 8 * stage;
-                    armed |= 1u << stage;
-                    armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
                     if (warp == 0) {
-                        mbar_expect_tx(full, (p.a_rows + kPN) * kBK * 2);
-                        tma_load_2d(sa + p.a_bytes, &maps.w, full, ks * kBK, n0);
+                        armed |= 1u << stage;
+                        armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
+                        mbar_expect_tx(full, (p.a_rows + w_rows) * kBK * 2);
+                        if (product) tma_load_2d(sa + p.a_bytes, &maps.w, full, ks * kBK, n0);
+                        if (FUSED) tma_load_2d(sa, &maps.x, full, ks * kBK, t0);
+                    } else if (FUSED) {
+                        if (count < 0) {
+                            if (!mbar_wait(bar_list, 0, &s_abort, status)) { ok = false; break; }
+                            count = s_al.count;
+                        }
+                        const uint32_t sb = sa + p.a_bytes + w_rows * kBK * 2;
+                        mbar_expect_tx(full, count * p.rank * kBK * 2);
+                        for (int j = 0; j < count; ++j)
+                            tma_load_2d(sb + j * p.rank * kBK * 2, &maps.a, full, ks * kBK, s_al.list[j] * p.rank);
                     } else {
                         tma_load_2d(sa, &maps.x, full, ks * kBK, t0);
                     }
@@ -373,16 +452,22 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
                 }
                 if (!ok && warp == 0)
                     for (int s = 0; s < p.n_stages; ++s)
-                        if (armed & (1u << s)) mbar_wait(bar_full + 8 * s, (armed_phase >> s) & 1u, &s_abort, p.status);
+                        if (armed & (1u << s)) mbar_wait(bar_full + 8 * s, (armed_phase >> s) & 1u, &s_abort, status);
             }
             __syncwarp();
         } else if (warp == 1) {
             if (lane == 0) {
                 uint32_t stage = 0, phase = 0, acc = 0;
                 bool ok = true;
-                const uint32_t idesc = idesc_bf16(kPN);
-                for (int ks = k0; ks < k1; ++ks) {
-                    if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, p.status)) { ok = false; break; }
+                uint32_t idesc = idesc_bf16(kPN);
+                if (FUSED) {
+                    ok = mbar_wait(bar_list, 0, &s_abort, status);
+                    // (rank 8 and an odd number of adapters: eight stale columns, never read; no adapter and no product: none used)
+                    const int cols = w_rows + ((s_al.count * p.rank + 15) & ~15);
+                    idesc = idesc_bf16(cols > 0 ? cols : 16);
+                }
+                for (int ks = k0; ks < k1 && ok; ++ks) {
+                    if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, status)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t lo_a = smem_desc_lo(ring + stage * p.stage_bytes), lo_b = lo_a + (p.a_bytes >> 4);
 #pragma unroll
@@ -397,94 +482,172 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
             }
             __syncwarp();
         } else {
+            // thread <-> token (TMEM lane); two groups of four warps take half of the columns each
             const int quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane;
-            if (adapters) {
-                // The rows of the adapters' B that this CTA will multiply come into L2 while the product runs; every token asks
-                // for its own adapter's (the ids are complete: see above), the first of a warp for all that share it.
-                const int c0 = n0 + kPN * rank / S, c1 = min(n0 + (int)(kPN * (rank + 1) / S), p.N);
-                const int a = row < rows ? adapter_of(p, t0 + row, false) : -1;
+            int a = -1;
+            if (FUSED) {
+                if (half == 0) {
+                    int slot[1];
+                    list_adapters<4>(p, s_al, t0, warp - 2, lane, blockIdx.x == 0, [] { asm volatile("bar.sync 1, 128;" ::: "memory"); }, slot);
+                    s_slot[(warp - 2) * 32 + lane] = slot[0];
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_list);
+                }
+                __all_sync(kFull, mbar_wait(bar_list, 0, &s_abort, status));
+                a = s_al.adapter[row];
+            } else if (adapters) {
+                a = row < rows ? adapter_of(p, t0 + row, false) : -1;
+            }
+            if (adapters && half == 0) {
+                // The rows of the adapters' B that this CTA will multiply come into L2 while the product runs; every token asks for
+                // its own adapter's, the first of a warp for all that share it.
+                const int n_lo = n0 + c0, n_hi = min(n0 + c0 + nc, p.N);
                 const uint32_t same = __match_any_sync(kFull, a);
-                if (half == 0 && a >= 0 && lane == __ffs(same) - 1 && c0 < c1) {
-                    const char* lo = reinterpret_cast<const char*>(p.b + ((size_t)a * p.N + c0) * p.rank);
-                    const char* hi = reinterpret_cast<const char*>(p.b + ((size_t)a * p.N + c1) * p.rank);
+                if (a >= 0 && lane == __ffs(same) - 1 && n_lo < n_hi) {
+                    const char* lo = reinterpret_cast<const char*>(p.b + ((size_t)a * p.N + n_lo) * p.rank);
+                    const char* hi = reinterpret_cast<const char*>(p.b + ((size_t)a * p.N + n_hi) * p.rank);
                     for (const char* q = lo; q < hi; q += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q));
                 }
             }
-            if (__all_sync(kFull, mbar_wait(bar_done, 0, &s_abort, p.status)) && quarter * 32 < rows) {
+            if (__all_sync(kFull, mbar_wait(bar_done, 0, &s_abort, status)) && quarter * 32 < rows) {
                 tc_fence_after();
+                const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+                if (product) {
 #pragma unroll
-                for (int c = 0; c < kPN / 2; c += 16) {
-                    uint32_t r[16];
-                    tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + half * (kPN / 2) + c, r);
-                    tmem_ld_wait();
-                    if (row < rows) {
+                    for (int c = 0; c < kPN / 2; c += 16) {
+                        uint32_t r[16];
+                        tmem_ld16(tmem + lanes + half * (kPN / 2) + c, r);
+                        tmem_ld_wait();
+                        if (row < rows) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) part[(half * (kPN / 2) + c + i) * pitch + row] = __uint_as_float(r[i]);
+                            for (int i = 0; i < 16; ++i) own[(half * (kPN / 2) + c + i) * pitch + row] = __uint_as_float(r[i]);
+                        }
                     }
                 }
+                if (FUSED && half == 1) {
+                    const int slot = s_slot[row], cols = s_al.count * p.rank;
+                    const int c_lo = slot >= 0 ? slot * p.rank : cols, c_hi = slot >= 0 ? c_lo + p.rank : 0;
+                    for (int c = 0; c < cols; c += 16) {
+                        if (!__any_sync(kFull, c + 16 > c_lo && c < c_hi)) continue;
+                        uint32_t r[16];
+                        tmem_ld16(tmem + lanes + w_rows + c, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int h = 0; h < 16; h += 8)
+                            if (c + h >= c_lo && c + h < c_hi) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) own_u[(c + h + i - c_lo) * pitch + row] = __uint_as_float(r[h + i]);
+                            }
+                    }
+                }
+                fence_async_shared();                       // (the sums leave by bulk copies)
             }
         }
     }
-    if (adapters) {
+    if (S > 1) {
+        __syncthreads();
+        cluster_wait();
+        if (warp == 0) {
+            // every CTA gets its columns of the product, and (fused) u whole
+            if (lane == 0) mbar_expect_tx(bar_got, S * ((product ? nc : 0) + (FUSED ? p.rank : 0)) * pitch * 4);
+            __syncwarp();
+            if (lane < S) {
+                const int to = lane, d0 = kPN * to / S, dn = kPN * (to + 1) / S - d0;
+                const uint32_t bar = map_to_cta(bar_got, to);
+                if (product)
+                    send_bulk(map_to_cta(smem_u32(part + (int)rank * nc_max * pitch), to), smem_u32(own + d0 * pitch), dn * pitch * 4, bar);
+                if (FUSED) send_bulk(map_to_cta(smem_u32(u_part + (int)rank * p.rank * pitch), to), smem_u32(own_u), p.rank * pitch * 4, bar);
+            }
+        }
+    }
+    if (!FUSED && adapters) {
         pdl_wait();                                        // u
         for (int i = threadIdx.x; i < rows; i += kPThreads) s_adapter[i] = adapter_of(p, t0 + i, false);
+        // (rows of tokens without an adapter hold anything and are not looked at)
+        const float* src = p.u + (size_t)t0 * p.rank;
+        for (int i = threadIdx.x; i < rows * p.rank / 4; i += kPThreads)
+            reinterpret_cast<float4*>(su)[i] = __ldcg(reinterpret_cast<const float4*>(src) + i);
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    float* const su = part + (size_t)kPN * pitch;          // u of the tile's tokens
-    if (adapters) {
-        for (int i = threadIdx.x; i < rows * p.rank; i += kPThreads)
-            su[i] = s_adapter[i / p.rank] >= 0 ? __ldcg(p.u + (size_t)t0 * p.rank + i) : 0.f;
+
+    // The outputs: four of a thread at a time, so that their loads overlap.  The first rows of B are asked for before the sums
+    // have arrived.
+    const int* const adapter = FUSED ? s_al.adapter : s_adapter;
+    const int total = rows * nc, vecs = p.rank / 8;
+    const float* const got = S > 1 ? part : own;
+    int r[4], c[4], a[4];
+    bool on[4];
+    uint4 bq[4][2];
+    auto pick = [&](int e0) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int e = e0 + q * kPThreads;
+            r[q] = e / nc;
+            c[q] = e - r[q] * nc;
+            on[q] = e < total && n0 + c0 + c[q] < p.N;
+            a[q] = on[q] && adapters ? adapter[r[q]] : -1;
+        }
+    };
+    auto load_b = [&](int i) {                             // vectors i and i + 1 of the four rows of B
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                bq[q][h] = a[q] >= 0 && i + h < vecs ? __ldg(reinterpret_cast<const uint4*>(p.b + ((size_t)a[q] * p.N + n0 + c0 + c[q]) * p.rank) + i + h)
+                                                     : make_uint4(0, 0, 0, 0);
+    };
+    pick(threadIdx.x);
+    if (adapters) load_b(0);
+    if (S > 1) {
+        mbar_wait(bar_got, 0, &s_abort, status);
+        __syncwarp();
+        cluster_arrive();                                  // (waited for at the end: nobody leaves while its copies may still be on their way)
     }
-    if (S > 1) cluster_sync_all(); else __syncthreads();
+    if (FUSED) {
+        const float* const up = S > 1 ? u_part : own_u;
+        for (int i = threadIdx.x; i < rows * p.rank; i += kPThreads) {
+            const int ur = i / p.rank, uc = i - ur * p.rank, ua = s_al.adapter[ur];
+            float v = 0.f;
+            if (ua >= 0) {
+                for (int z = 0; z < S; ++z) v += up[(z * p.rank + uc) * pitch + ur];
+                if (p.scale) v *= p.scale[ua];
+            }
+            su[i] = v;
+        }
+        __syncthreads();
+    }
     if (!s_abort) {
-        const int c0 = kPN * rank / S, nc = kPN * (rank + 1) / S - c0;          // this CTA's columns of the tile
-        const uint32_t part_addr = smem_u32(part);
-        const int total = rows * nc;
-        // four outputs of a thread at a time, so that their loads overlap
         for (int e0 = threadIdx.x; e0 < total; e0 += 4 * kPThreads) {
+            if (e0 != threadIdx.x) {
+                pick(e0);
+                if (adapters) load_b(0);
+            }
             float v[4];
-            int r[4], n[4], a[4];
-            bool on[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int e = e0 + q * kPThreads;
-                r[q] = e / nc;
-                const int c = c0 + e - r[q] * nc;
-                n[q] = n0 + c;
-                on[q] = e < total && n[q] < p.N;
-                a[q] = on[q] && adapters ? s_adapter[r[q]] : -1;
                 v[q] = 0.f;
-                if (on[q] && product) {
-                    if (S > 1) {
-                        float t[8];
-#pragma unroll
-                        for (int z = 0; z < 8; ++z) t[z] = z < S ? ld_cluster_f32(map_to_cta(part_addr + 4 * (c * pitch + r[q]), z)) : 0.f;
-#pragma unroll
-                        for (int z = 0; z < 8; ++z) v[q] += t[z];
-                    } else {
-                        v[q] = part[c * pitch + r[q]];
-                    }
-                }
+                if (on[q] && product)
+                    for (int z = 0; z < S; ++z) v[q] += got[(z * nc_max + c[q]) * pitch + r[q]];
             }
             if (adapters) {
                 float d[4] = {0.f, 0.f, 0.f, 0.f};
-                for (int i = 0; i < p.rank / 8; ++i) {
-                    uint4 bq[4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        bq[q] = a[q] >= 0 ? __ldg(reinterpret_cast<const uint4*>(p.b + ((size_t)a[q] * p.N + n[q]) * p.rank) + i) : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < vecs; i += 2) {
+                    if (i > 0) load_b(i);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         if (a[q] < 0) continue;
-                        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&bq[q]);
-                        const float* up = su + r[q] * p.rank + 8 * i;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float2 f = __bfloat1622float2(h[j]);
-                            d[q] = fmaf(up[2 * j], f.x, d[q]);
-                            d[q] = fmaf(up[2 * j + 1], f.y, d[q]);
+                        for (int h = 0; h < 2; ++h) {
+                            if (i + h >= vecs) break;
+                            const __nv_bfloat162* b2 = reinterpret_cast<const __nv_bfloat162*>(&bq[q][h]);
+                            const float4* up = reinterpret_cast<const float4*>(su + r[q] * p.rank + 8 * (i + h));
+                            const float4 u0 = up[0], u1 = up[1];
+                            const float2 f0 = __bfloat1622float2(b2[0]), f1 = __bfloat1622float2(b2[1]), f2 = __bfloat1622float2(b2[2]),
+                                         f3 = __bfloat1622float2(b2[3]);
+                            d[q] = fmaf(u0.x, f0.x, d[q]); d[q] = fmaf(u0.y, f0.y, d[q]); d[q] = fmaf(u0.z, f1.x, d[q]); d[q] = fmaf(u0.w, f1.y, d[q]);
+                            d[q] = fmaf(u1.x, f2.x, d[q]); d[q] = fmaf(u1.y, f2.y, d[q]); d[q] = fmaf(u1.z, f3.x, d[q]); d[q] = fmaf(u1.w, f3.y, d[q]);
                         }
                     }
                 }
@@ -495,22 +658,24 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
             for (int q = 0; q < 4; ++q) {
                 if (!on[q]) continue;
                 const size_t row = t0 + r[q];
+                const int n = n0 + c0 + c[q];
                 if (p.out_f32) {
-                    if (p.base) v[q] += ((const float*)p.base)[row * p.ldbase + n[q]];
-                    ((float*)p.out)[row * p.ldo + n[q]] = v[q];
+                    if (p.base) v[q] += ((const float*)p.base)[row * p.ldbase + n];
+                    ((float*)p.out)[row * p.ldo + n] = v[q];
                 } else {
-                    if (p.base) v[q] += __bfloat162float(((const bf16*)p.base)[row * p.ldbase + n[q]]);
-                    ((bf16*)p.out)[row * p.ldo + n[q]] = __float2bfloat16_rn(v[q]);
+                    if (p.base) v[q] += __bfloat162float(((const bf16*)p.base)[row * p.ldbase + n]);
+                    ((bf16*)p.out)[row * p.ldo + n] = __float2bfloat16_rn(v[q]);
                 }
             }
         }
     }
+    if (S > 1) cluster_wait();
     tc_fence_before();
-    if (S > 1) cluster_sync_all(); else __syncthreads();   // nobody leaves while a peer may still read its sums
+    __syncthreads();
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kPN) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmem) : "memory");
     }
 }
 
@@ -609,6 +774,7 @@ __global__ void __launch_bounds__(kMThreads, 1)
 project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
 {
     extern __shared__ unsigned char smem_dyn[];
+    int32_t* const status = status_of(p);
     const uint32_t ring = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     unsigned char* const ring_ptr = smem_dyn + (ring - smem_u32(smem_dyn));
     const int n_stages = p.n_stages;
@@ -666,12 +832,12 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
                     if (ks >= steps && extra < 0) {
                         extra = 0;
                         if (adapters) {
-                            if (!mbar_wait(bar_list, it & 1, &s_abort, p.status)) { ok = false; break; }
+                            if (!mbar_wait(bar_list, it & 1, &s_abort, status)) { ok = false; break; }
                             extra = s_al.count * chunks;
                             if (warp == 10) {
                                 // u of this CTA's tokens, hi and lo tiles (rows of tokens without an adapter hold anything)
                                 if (it == 0) pdl_wait();
-                                if (!mbar_wait(bar_uempty, (it & 1) ^ 1, &s_abort, p.status)) { ok = false; break; }
+                                if (!mbar_wait(bar_uempty, (it & 1) ^ 1, &s_abort, status)) { ok = false; break; }
                                 if (leader) mbar_expect_tx(bar_ufull, 4 * chunks * kUTile);
                                 u_loads = it + 1;
                                 for (int c = 0; c < 2 * chunks; ++c)
@@ -681,7 +847,7 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
                     }
                     if (ks >= steps && ks >= steps + extra) break;
                     const uint32_t sa = ring + stage * kMStageBytes, full = bar_full + 8 * stage;
-                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, p.status)) { ok = false; break; }
+                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, status)) { ok = false; break; }
                     if (warp == 0) {
                         armed |= 1u << stage;
                         armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
@@ -701,9 +867,9 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
             }
             if (!ok && leader && warp == 0) {               // gave up: the copies in flight land before the block exits
                 for (int s = 0; s < n_stages; ++s)
-                    if (armed & (1u << s)) mbar_wait(bar_full + 8 * s, (armed_phase >> s) & 1u, &s_abort, p.status);
+                    if (armed & (1u << s)) mbar_wait(bar_full + 8 * s, (armed_phase >> s) & 1u, &s_abort, status);
             }
-            if (!ok && leader && u_loads > 0) mbar_wait(bar_ufull, (u_loads - 1) & 1, &s_abort, p.status);
+            if (!ok && leader && u_loads > 0) mbar_wait(bar_ufull, (u_loads - 1) & 1, &s_abort, status);
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -714,11 +880,11 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
             int it = 0;
             for (int tile = pair0; tile < total && ok; tile += pairs, ++it) {
                 const uint32_t buf = it & 1, d = tmem + buf * 256;
-                if (!mbar_wait_cluster(bar_tempty + 8 * buf, ((it >> 1) & 1) ^ 1, &s_abort, p.status)) { ok = false; break; }
+                if (!mbar_wait_cluster(bar_tempty + 8 * buf, ((it >> 1) & 1) ^ 1, &s_abort, status)) { ok = false; break; }
                 tc_fence_after();
                 uint32_t acc = 0;
                 for (int ks = 0; ks < p.ksteps; ++ks) {
-                    if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, p.status)) { ok = false; break; }
+                    if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, status)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t lo_a = smem_desc_lo(ring + stage * kMStageBytes), lo_b = lo_a + ((kTok * kBK * 2) >> 4);
 #pragma unroll
@@ -731,14 +897,14 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
                 }
                 if (!ok) break;
                 if (adapters) {
-                    if (!mbar_wait(bar_list, it & 1, &s_abort, p.status) || !mbar_wait(bar_ufull, it & 1, &s_abort, p.status)) { ok = false; break; }
+                    if (!mbar_wait(bar_list, it & 1, &s_abort, status) || !mbar_wait(bar_ufull, it & 1, &s_abort, status)) { ok = false; break; }
                     tc_fence_after();
                     const int count = s_al.count;
                     for (int j = 0; j < count && ok; ++j) {
                         // (without the product the first MMA of an adapter overwrites its tokens' lanes)
                         uint32_t first = acc;
                         for (int c = 0; c < chunks; ++c) {
-                            if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, p.status)) { ok = false; break; }
+                            if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, status)) { ok = false; break; }
                             tc_fence_after();
                             const uint32_t lo_b = smem_desc_lo(ring + stage * kMStageBytes + kTok * kBK * 2);
                             const int kks = (min(kBK, p.rank - c * kBK) + 15) >> 4;
@@ -772,7 +938,7 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
         for (int tile = pair0; tile < total; tile += pairs, ++it) {
             const int n0 = (tile / m_tiles) * kMTile + half * 128, t = (tile % m_tiles) * kMTile + (int)rank * kTok + quarter * 32 + lane;
             const uint32_t buf = it & 1;
-            ok = __all_sync(kFull, mbar_wait(bar_tfull + 8 * buf, (it >> 1) & 1, &s_abort, p.status));
+            ok = __all_sync(kFull, mbar_wait(bar_tfull + 8 * buf, (it >> 1) & 1, &s_abort, status));
             if (!ok) break;
             tc_fence_after();
             const bool live = t < p.T;
@@ -803,7 +969,7 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
         const int w = warp - 11;
         int it = 0;
         for (int tile = pair0; tile < total; tile += pairs, ++it) {
-            if (!__all_sync(kFull, mbar_wait(bar_uempty, (it & 1) ^ 1, &s_abort, p.status))) break;
+            if (!__all_sync(kFull, mbar_wait(bar_uempty, (it & 1) ^ 1, &s_abort, status))) break;
             int slot[2];
             list_adapters<8>(p, s_al, (tile % m_tiles) * kMTile, w, lane, false, [] { builders_sync(); }, slot);
             for (int j = w; j < s_al.count; j += 4) {
@@ -875,6 +1041,32 @@ cudaError_t allow_smem(K kern, bool (&done)[kMaxDevices])
 
 int div_up(int a, int b) { return (a + b - 1) / b; }
 
+// Parts of K, stages and shared memory of project_kernel; false if it does not fit.  `behind`: bytes behind the last stage
+// that the MMA of a short token tile may read.
+bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind)
+{
+    const int tiles = div_up(p.N, kPN) * div_up(p.T, kTok), pitch = p.a_rows + 4;
+    // as many parts as there are SMs for the tiles (a cluster holds eight), of two slices at least
+    p.splits = 148 / tiles;
+    if (p.splits > 8) p.splits = 8;
+    if (p.splits > p.ksteps / 2) p.splits = p.ksteps / 2;
+    if (p.splits < 1 || !(p.w || fused)) p.splits = 1;
+    if (p.splits == 5 || p.splits == 7) p.splits -= 1;      // (clusters of 7 pack badly: 18.5 against 9.6 us with 8 and 9.9 with 6, one token, 2048 x 2048)
+    p.stage_bytes = p.a_bytes + (p.w ? kPN * kBK * 2 : 0) + ((u_rows + 15) & ~15) * kBK * 2;
+    // received: the parts of this CTA's columns, (fused) the parts of u; and u itself
+    p.sums_bytes = (p.splits * div_up(kPN, p.splits) * pitch + (fused ? p.splits * p.rank * pitch : 0) + p.a_rows * p.rank) * (int)sizeof(float);
+    const int room = kMaxSmem - 1024 - p.sums_bytes;
+    p.n_stages = p.w || fused ? div_up(p.ksteps, p.splits) : 1;
+    const int most = (room - behind) / p.stage_bytes;
+    if (p.n_stages > most) p.n_stages = most;
+    if (p.n_stages > 6) p.n_stages = 6;
+    // the ring, or this CTA's own sums that are put together in it, whichever is larger
+    const int own = (kPN + (fused ? p.rank : 0)) * pitch * (int)sizeof(float);
+    p.scratch = p.n_stages * p.stage_bytes + behind;
+    if (p.scratch < own) p.scratch = own;
+    return p.scratch <= room && (p.n_stages >= 2 || p.ksteps <= 1);
+}
+
 // The pair shape, from 257 tokens on.
 bool use_many(const ProjectArgs& p)
 {
@@ -883,24 +1075,54 @@ bool use_many(const ProjectArgs& p)
     return p.T > kMTile;
 }
 
+// Tile sizes, and for few tokens the shape of project_kernel.  Whether u comes out of the same pass (fused): where all
+// adapters that the tokens may have fit 128 columns beside the product's, and the parts of u that every CTA of a cluster then
+// receives fit its shared memory beside two stages.
+bool plan_few(ProjectArgs& p)
+{
+    const bool adapters = p.n_adapters > 0;
+    p.a_rows = p.T >= kTok ? kTok : ((p.T + 7) & ~7);
+    p.a_bytes = (p.a_rows * kBK * 2 + 1023) & ~1023;
+    p.ksteps = p.w || adapters ? div_up(p.K, kBK) : 0;
+    const int behind = kTok * kBK * 2 - p.a_bytes;          // an MMA reads 128 token rows, also of a short tile in the last stage
+    if (use_many(p)) return false;
+    p.u_rows = adapters ? (p.T < p.n_adapters ? p.T : p.n_adapters) * (p.rank <= kUCols ? p.rank : kUCols) : 0;
+    if (adapters && p.T <= kTok && p.u_rows <= kUCols && few_geometry(p, true, p.u_rows, behind)) return true;
+    few_geometry(p, false, 0, behind);
+    return false;
+}
+
 }  // namespace
 
-int64_t project_workspace(int T, int rank, int n_adapters)
+int64_t project_workspace(int T, int K, int N, int rank, int n_adapters)
 {
-    return kProjectHeader + (n_adapters > 0 ? (int64_t)T * rank * (int64_t)sizeof(float) : 0);
+    if (n_adapters == 0 || T == 0) return 0;
+    ProjectArgs p = {};
+    p.T = T; p.K = K; p.N = N; p.rank = rank; p.n_adapters = n_adapters;
+    if (plan_few(p) && (p.w = reinterpret_cast<const bf16*>(16), plan_few(p))) return 0;      // (with w and without)
+    return (int64_t)T * rank * (int64_t)sizeof(float);
 }
 
 cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
 {
     ProjectArgs p = in;
-    static bool u_ok[kMaxDevices] = {false}, p_ok[kMaxDevices] = {false}, m_ok[kMaxDevices] = {false};
-    const int m_tiles = div_up(p.T, kTok);
-    const bool many = use_many(p);
-    p.a_rows = p.T >= kTok ? kTok : ((p.T + 7) & ~7);
-    p.a_bytes = (p.a_rows * kBK * 2 + 1023) & ~1023;
-    p.u = reinterpret_cast<float*>(p.workspace + kProjectHeader);
+    static bool u_ok[kMaxDevices] = {false}, p_ok[kMaxDevices] = {false}, f_ok[kMaxDevices] = {false}, m_ok[kMaxDevices] = {false};
+    const int m_tiles = div_up(p.T, kTok), n_tiles = div_up(p.N, kPN);
+    const bool many = use_many(p), adapters = p.n_adapters > 0;
+    const bool fused = plan_few(p);
     p.u_pair = many;
-    if (p.n_adapters > 0) {
+    const int behind = kTok * kBK * 2 - p.a_bytes;
+
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.stream = st;
+
+    if (adapters && !fused) {
         cudaError_t e = allow_smem(adapter_kernel, u_ok);
         if (e != cudaSuccess) return e;
         UMaps um;
@@ -908,7 +1130,6 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
             !make_map_ld(&um.a, p.a, (uint64_t)p.n_adapters * p.rank, p.K, p.K, p.rank))
             return cudaErrorInvalidValue;
         ProjectArgs q = p;
-        q.ksteps = div_up(p.K, kBK);
         // K is cut into as many parts as there are SMs for the token tiles, of two slices at least; then the chunks of a
         // tile's adapters go to CTAs of their own as long as there are SMs, and are walked over beyond that
         q.u_splits = 1;
@@ -920,70 +1141,54 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
         const int room = 148 / (m_tiles * q.u_splits);
         if (chunks > room) chunks = room < 1 ? 1 : room;
         q.stage_bytes = p.a_bytes + (q.slots * p.rank > 64 ? kUCols : 64) * kBK * 2;
-        q.n_stages = 4;
-        const size_t smem = (size_t)q.n_stages * q.stage_bytes + kTok * kBK * 2 + (size_t)kTok * (p.rank + 4) * sizeof(float) + 1024;
-        cudaLaunchConfig_t cfg;
-        memset(&cfg, 0, sizeof(cfg));
-        cudaLaunchAttribute attr[2];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = 1; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = q.u_splits;
-        cfg.attrs = attr; cfg.numAttrs = q.u_splits > 1 ? 2 : 1; cfg.stream = st;
-        cfg.gridDim = dim3(m_tiles, chunks, q.u_splits); cfg.blockDim = dim3(kUThreads); cfg.dynamicSmemBytes = smem;
+        // shared memory: the ring, and the sums of a_rows tokens twice (sent and received); at high ranks fewer parts, then fewer stages
+        size_t sums;
+        for (;; q.u_splits /= 2) {
+            q.u_own = (div_up(p.a_rows, q.u_splits) + 3) & ~3;
+            sums = (size_t)q.u_splits * (q.u_own + 4) * p.rank * sizeof(float) * (q.u_splits > 1 ? 2 : 1);
+            if (q.u_splits == 1 || 2 * q.stage_bytes + behind + sums + 1024 <= kMaxSmem) break;
+        }
+        q.n_stages = (int)((kMaxSmem - 1024 - behind - sums) / q.stage_bytes);
+        if (q.n_stages > 4) q.n_stages = 4;
+        q.scratch = q.n_stages * q.stage_bytes + behind;
+        cfg.attrs[1].val.clusterDim.z = q.u_splits;
+        cfg.numAttrs = q.u_splits > 1 ? 2 : 1;
+        cfg.gridDim = dim3(m_tiles, chunks, q.u_splits); cfg.blockDim = dim3(kUThreads);
+        cfg.dynamicSmemBytes = q.scratch + sums + 1024;
         e = cudaLaunchKernelEx(&cfg, adapter_kernel, q, um);
         if (e != cudaSuccess) return e;
+        attr[1].val.clusterDim.z = 1;
     }
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.stream = st;
     if (many) {
         cudaError_t e = allow_smem(project_many_kernel, m_ok);
         if (e != cudaSuccess) return e;
         MMaps mm;
         memset(&mm, 0, sizeof(mm));
-        p.ksteps = p.w ? div_up(p.K, kBK) : 0;
+        if (!p.w) p.ksteps = 0;
         if (p.w && (!make_map_ld(&mm.x, p.x, p.T, p.K, p.ldx, kTok) || !make_map_ld(&mm.w, p.w, p.N, p.K, p.ldw, kTok)))
             return cudaErrorInvalidValue;
-        if (p.n_adapters > 0 && (!make_map_3d(&mm.b, p.b, p.n_adapters, p.N, p.rank) || !make_map_3d(&mm.u, p.u, 2, p.T, p.rank)))
+        if (adapters && (!make_map_3d(&mm.b, p.b, p.n_adapters, p.N, p.rank) || !make_map_3d(&mm.u, p.u, 2, p.T, p.rank)))
             return cudaErrorInvalidValue;
-        const int u_tiles = p.n_adapters > 0 ? 2 * div_up(p.rank, kBK) : 0;      // 32 KB up to rank 64, 64 KB beyond
+        const int u_tiles = adapters ? 2 * div_up(p.rank, kBK) : 0;              // 32 KB up to rank 64, 64 KB beyond
         p.n_stages = u_tiles > 2 ? kMStages - 1 : kMStages;
         const int tiles = div_up(p.N, kMTile) * div_up(p.T, kMTile), pairs = tiles < 74 ? tiles : 74;
+        attr[1].val.clusterDim.x = 2;
         cfg.gridDim = dim3(2 * pairs); cfg.blockDim = dim3(kMThreads); cfg.numAttrs = 2;
         cfg.dynamicSmemBytes = (size_t)p.n_stages * kMStageBytes + (size_t)u_tiles * kUTile + 1024;
         return cudaLaunchKernelEx(&cfg, project_many_kernel, p, mm);
     }
-    cudaError_t e = allow_smem(project_kernel, p_ok);
-    if (e != cudaSuccess) return e;
     PMaps pm;
     memset(&pm, 0, sizeof(pm));
-    p.ksteps = p.w ? div_up(p.K, kBK) : 0;
-    if (p.w && (!make_map_ld(&pm.x, p.x, p.T, p.K, p.ldx, p.a_rows) || !make_map_ld(&pm.w, p.w, p.N, p.K, p.ldw, kPN)))
-        return cudaErrorInvalidValue;
-    const int n_tiles = div_up(p.N, kPN);
-    // as many parts of K as there are SMs for the tiles (a cluster holds eight), of two slices at least
-    p.splits = 148 / (n_tiles * m_tiles);
-    if (p.splits > 8) p.splits = 8;
-    if (p.splits > p.ksteps / 2) p.splits = p.ksteps / 2;
-    if (p.splits < 1) p.splits = 1;
-    p.stage_bytes = p.a_bytes + kPN * kBK * 2;
-    p.n_stages = div_up(p.ksteps, p.splits);
-    if (p.n_stages > 6) p.n_stages = 6;
-    if (p.n_stages < 1) p.n_stages = 1;
-    size_t smem = (size_t)p.n_stages * p.stage_bytes + kTok * kBK * 2;
-    const size_t scratch = ((size_t)kPN * (p.a_rows + 1) + (size_t)(p.n_adapters > 0 ? p.a_rows * p.rank : 0)) * sizeof(float);
-    if (smem < scratch) smem = scratch;
-    smem += 1024;
-    cfg.gridDim = dim3(n_tiles * p.splits, m_tiles); cfg.blockDim = dim3(kPThreads); cfg.dynamicSmemBytes = smem;
+    if ((p.w || fused) && !make_map_ld(&pm.x, p.x, p.T, p.K, p.ldx, p.a_rows)) return cudaErrorInvalidValue;
+    if (p.w && !make_map_ld(&pm.w, p.w, p.N, p.K, p.ldw, kPN)) return cudaErrorInvalidValue;
+    if (fused && !make_map_ld(&pm.a, p.a, (uint64_t)p.n_adapters * p.rank, p.K, p.K, p.rank)) return cudaErrorInvalidValue;
+    cfg.gridDim = dim3(n_tiles * p.splits, m_tiles); cfg.blockDim = dim3(kPThreads);
+    cfg.dynamicSmemBytes = (size_t)p.scratch + p.sums_bytes + 1024;
     attr[1].val.clusterDim.x = p.splits;
     cfg.numAttrs = p.splits > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, project_kernel, p, pm);
+    cudaError_t e = fused ? allow_smem(project_kernel<true>, f_ok) : allow_smem(project_kernel<false>, p_ok);
+    if (e != cudaSuccess) return e;
+    return fused ? cudaLaunchKernelEx(&cfg, project_kernel<true>, p, pm) : cudaLaunchKernelEx(&cfg, project_kernel<false>, p, pm);
 }
 
 }  // namespace faasmoe

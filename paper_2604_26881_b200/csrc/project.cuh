@@ -6,7 +6,6 @@
 namespace faasmoe {
 
 constexpr int kAdapterMaxRank = 128;
-constexpr int kProjectHeader = 256;       // bytes of the workspace in front of the adapters' first products
 
 struct ProjectArgs {
     const bf16* x;                  // [T, ldx]
@@ -21,18 +20,21 @@ struct ProjectArgs {
     int64_t ldx, ldw, ldbase, ldo;
     int out_f32;
     int T, K, N, n_adapters, rank, n_tenants;
-    unsigned char* workspace;       // kProjectHeader bytes, then u [T][rank]: f32, or two bf16 arrays hi and lo
-    int32_t* status;                // the caller's, or a word of the workspace
+    float* u;                       // workspace: [T][rank], f32 or two bf16 arrays hi and lo; not used where the first product is fused
+    int32_t* status;                // the caller's, or null
     // set by launch_project
-    float* u;
     int u_pair;                     // u is stored as hi and lo
     int u_splits;                   // parts of K of the first product (a cluster)
     int ksteps, splits, n_stages, stage_bytes, a_bytes, a_rows;
+    int u_own;                      // tokens of a tile that one CTA of such a cluster adds up
+    int u_rows;                     // most rows of A that the tokens may need (fused)
+    int scratch;                    // bytes of the ring (or of the sums put together in it) in front of the sums received
+    int sums_bytes;                 // of the sums received
     int slots;                      // adapters per CTA of the first product
 };
 
-// bytes of the workspace for T tokens (n_adapters = 0: none)
-int64_t project_workspace(int T, int rank, int n_adapters);
+// bytes of the workspace (0: none is needed)
+int64_t project_workspace(int T, int K, int N, int rank, int n_adapters);
 cudaError_t launch_project(const ProjectArgs& args, cudaStream_t st);
 
 }  // namespace faasmoe

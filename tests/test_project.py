@@ -234,7 +234,7 @@ def test_base_in_place_streams_graphs_and_repeats(T):
     torch.cuda.synchronize()
     assert torch.equal(o, ref) and torch.equal(o2, ref)
     many = [torch.empty_like(ref) for _ in range(10)]
-    ws = torch.empty(B.moe_project_workspace(T, 256, 16, 6), dtype=torch.uint8, device=DEV)
+    ws = torch.empty(max(1, B.moe_project_workspace(T, 256, 320, 16, 6)), dtype=torch.uint8, device=DEV)
     for m in many:                                                  # one workspace, one stream
         B.moe_project(g["x"], g["w"], m, base=g["base"], workspace=ws, **kw)
     torch.cuda.synchronize()
@@ -299,7 +299,7 @@ def _raw(**kw):
 
 
 def test_refusals_need_no_gpu():
-    for bad in (dict(x=None), dict(out=None), dict(ws=None), dict(a=None), dict(b=None), dict(tenant=None), dict(w=None, n=0), dict(x=None, n=0)):
+    for bad in (dict(x=None), dict(out=None), dict(T=300, ws=None), dict(a=None), dict(b=None), dict(tenant=None), dict(w=None, n=0), dict(x=None, n=0)):
         assert _raw(**bad) == B.MOE_ERR_NULL, bad
     for bad in (dict(T=-1), dict(T=(1 << 22) + 1), dict(K=0), dict(N=0), dict(n=-1), dict(ldx=56), dict(ldw=56), dict(ldo=31), dict(base=256, ldb=31), dict(rank=0),
                 dict(rank=136), dict(n_tenants=0), dict(x=264), dict(w=264), dict(a=264), dict(b=260), dict(scale=258), dict(tenant=258), dict(table=258),
@@ -307,13 +307,15 @@ def test_refusals_need_no_gpu():
         assert _raw(**bad) == B.MOE_ERR_SHAPE, bad
     for bad in (dict(K=60), dict(ldx=68), dict(ldw=68), dict(rank=12), dict(out_type=2)):
         assert _raw(**bad) == B.MOE_ERR_UNSUPPORTED, bad
-    assert _raw(ws_bytes=255) == B.MOE_ERR_ALLOC
+    assert _raw(T=300, ws_bytes=255) == B.MOE_ERR_ALLOC
     assert _raw(T=0) == B.MOE_OK
     lib = B.load_library()
-    assert lib.moe_project_workspace(-1, 64, 8, 1) == B.MOE_ERR_SHAPE
-    assert lib.moe_project_workspace(4, 64, 129, 1) == B.MOE_ERR_SHAPE
-    assert lib.moe_project_workspace(4, 64, 0, 0) >= 0
-    assert lib.moe_project_workspace(100, 2048, 16, 3) >= 100 * 16 * 4
+    assert lib.moe_project_workspace(-1, 64, 32, 8, 1) == B.MOE_ERR_SHAPE
+    assert lib.moe_project_workspace(4, 64, 32, 129, 1) == B.MOE_ERR_SHAPE
+    assert lib.moe_project_workspace(4, 64, 0, 8, 1) == B.MOE_ERR_SHAPE
+    assert lib.moe_project_workspace(4, 64, 32, 0, 0) == 0
+    assert lib.moe_project_workspace(1, 2048, 2048, 16, 3) == 0               # one pass, no workspace
+    assert lib.moe_project_workspace(1000, 2048, 2048, 16, 3) == 1000 * 16 * 4
 
 
 def test_binding_checks_tensors():
