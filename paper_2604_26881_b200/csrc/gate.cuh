@@ -21,7 +21,7 @@ struct GateArgs {
     uint8_t* tie_flag;              // or null
     int32_t* status;                // or null
     // set by launch_gate
-    int aligned_groups, eligible, vec;
+    int group_size, lanes_per_group, eligible, vec, vec_bias;
 };
 
 void apply_gating(GateArgs& args, const moe_gating& rule);
