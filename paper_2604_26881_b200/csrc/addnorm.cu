@@ -5,7 +5,8 @@
 //   out = bf16(y);   q = e4m3(y / s),  s = max |y| / 448 over the row or over each 128 columns
 //
 // Bound by HBM: every element is read and written once, kept in registers in between (W warps hold a row, up to four
-// 16-byte vectors a lane), so the only other cost is the latency of one or two reductions per row.  The sum of
+// 16-byte vectors a lane).  16384 x 2048 with both outputs and a scale per row: 302 MB in 52 us, 5.8 TB/s (0.89 of the
+// measured copy bandwidth); 4096 x 8192 with 128-column scales the same; 32 x 2048: 1.9 us, launch and latency.  The sum of
 // squares, the scales and the quotients are fp32; h is rounded once because it is the residual stream that the caller
 // keeps (the norm is that of the stored value), out and q are each one rounding of the same fp32 y.
 #include <cuda_fp8.h>
@@ -18,35 +19,44 @@ namespace {
 
 constexpr uint32_t kFull = 0xffffffffu;
 
-// max |y| that keeps a NaN, as the row's outputs do
-__device__ __forceinline__ float max_nan(float a, float b)
-{
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
+// |y| as an unsigned number: of the same order, and a NaN is above everything, as it is to be in the outputs
+__device__ __forceinline__ uint32_t magnitude(float y) { return __float_as_uint(y) & 0x7fffffffu; }
 
-// eight consecutive elements of a row, of which the first n are there
-__device__ __forceinline__ void load8(const bf16* p, int n, bool vec, float* f)
+__device__ __forceinline__ void unpack8(const uint4& v, float* f)
 {
-    if (vec) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { const float2 t = __bfloat1622float2(h[i]); f[2 * i] = t.x; f[2 * i + 1] = t.y; }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = i < n ? __bfloat162float(p[i]) : 0.f;
-    }
+    for (int i = 0; i < 4; ++i) { const float2 t = __bfloat1622float2(h[i]); f[2 * i] = t.x; f[2 * i + 1] = t.y; }
 }
-__device__ __forceinline__ void store8(bf16* p, int n, bool vec, const float* f)
+__device__ __forceinline__ uint4 pack8(const float* f)
 {
-    if (vec) {
-        uint4 v;
-        __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+    uint4 v;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-        *reinterpret_cast<uint4*>(p) = v;
+    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    return v;
+}
+// Eight consecutive elements of a row, of which the first n (possibly none) are there; the others read as zero.  VEC: n is
+// 8 or not positive and the address is on a 16-byte boundary.
+template <bool VEC>
+__device__ __forceinline__ uint4 load8(const bf16* p, int n)
+{
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (VEC) {
+        if (n > 0) v = *reinterpret_cast<const uint4*>(p);
+    } else {
+        unsigned short e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < n ? reinterpret_cast<const unsigned short*>(p)[i] : (unsigned short)0;
+        v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+    }
+    return v;
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(bf16* p, int n, const float* f)
+{
+    if (VEC) {
+        if (n > 0) *reinterpret_cast<uint4*>(p) = pack8(f);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) if (i < n) p[i] = __float2bfloat16_rn(f[i]);
@@ -57,121 +67,161 @@ __device__ __forceinline__ uint16_t e4m3x2(float a, float b)
     return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
 
-// R rows per block, W warps per row, V vectors of 8 elements per lane
-template <int V, bool QUANT>
+// e4m3 of eight values of one scale
+template <bool VEC>
+__device__ __forceinline__ void store_q(uint8_t* dst, int n, bool vec_q, const float* h, float scale)
+{
+    float y[8];
+    if (scale >= 1e-37f || scale != scale) {
+        const float inv = 1.f / scale;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = h[i] * inv;
+    } else {                                                  // (the reciprocal would not be a finite number)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = scale > 0.f ? h[i] / scale : 0.f;
+    }
+    if (VEC && vec_q) {
+        uint2 o;
+        o.x = e4m3x2(y[0], y[1]) | ((uint32_t)e4m3x2(y[2], y[3]) << 16);
+        o.y = e4m3x2(y[4], y[5]) | ((uint32_t)e4m3x2(y[6], y[7]) << 16);
+        *reinterpret_cast<uint2*>(dst) = o;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < n) dst[i] = (uint8_t)(e4m3x2(y[i], 0.f) & 0xff);
+    }
+}
+
+// W warps per row, V vectors of 8 elements per lane, blockDim / (32 W) rows at a time; a block goes on with every gridDim-th set
+// of rows and has the next set's loads in flight while it works on this one.  All loads of a row are issued before the first is
+// used (a load inside a branch of its own waits for the one before it: 78 us instead of 58 for 16384 x 2048 with V = 2).
+template <int V, bool QUANT, bool VEC>
 __global__ void __launch_bounds__(512)
 addnorm_kernel(const AddNormArgs p, int W)
 {
-    __shared__ float s_part[2][16];
+    __shared__ float s_sum[2][16];
+    __shared__ uint32_t s_top[2][16];
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int row_in_block = warp / W, wr = warp - row_in_block * W;
-    const int t = blockIdx.x * (blockDim.x / (32 * W)) + row_in_block;
-    const bool live = t < p.T;
-    float h[V][8];
-    float ss = 0.f;
+    const int rows = blockDim.x / (32 * W);
+    const int first = (wr * 32 + lane) * 8, step = W * 256;               // this lane's columns: first + v * step ...
+    uint4 gv[V], xv[V], rv[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int col = ((v * W + wr) * 32 + lane) * 8, n = p.H - col;
-        if (live && n > 0) {
-            load8(p.x + (size_t)t * p.ldx + col, n, p.vec && n >= 8, h[v]);
+        const int col = first + v * step;
+        gv[v] = p.vec_weight ? load8<VEC>(p.weight + col, p.H - col) : load8<false>(p.weight + col, p.H - col);
+        rv[v] = make_uint4(0, 0, 0, 0);
+    }
+    auto fetch = [&](int t) {
+        const int H = t < p.T ? p.H : 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) xv[v] = load8<VEC>(p.x + (size_t)t * p.ldx + first + v * step, H - first - v * step);
+        if (p.residual) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) rv[v] = load8<VEC>(p.residual + (size_t)t * p.ldr + first + v * step, H - first - v * step);
+        }
+    };
+    int t = blockIdx.x * rows + row_in_block;
+    fetch(t);
+    int buf = 0;
+    for (int set = blockIdx.x; set * rows < p.T; set += gridDim.x, t += gridDim.x * rows, buf ^= 1) {
+        const bool live = t < p.T;
+        float h[V][8];
+        float ss = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            unpack8(xv[v], h[v]);
             if (p.residual) {
                 float r[8];
-                load8(p.residual + (size_t)t * p.ldr + col, n, p.vec && n >= 8, r);
+                unpack8(rv[v], r);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[v][i] = __bfloat162float(__float2bfloat16_rn(h[v][i] + r[i]));
+                for (int i = 0; i < 8; ++i) h[v][i] += r[i];
+                const uint4 sum = pack8(h[v]);                // (rounded: the residual stream that is stored)
+                unpack8(sum, h[v]);
+            }
+        }
+        if (set + gridDim.x < (p.T + rows - 1) / rows) fetch(t + gridDim.x * rows);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (p.residual_out) store8<VEC>(p.residual_out + (size_t)t * p.ldro + first + v * step, live ? p.H - first - v * step : 0, h[v]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss = fmaf(h[v][i], h[v][i], ss);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(kFull, ss, o);
+        if (W > 1) {
+            // (two sets of partial sums in turn: a warp may be one set ahead of another, never two)
+            if (lane == 0) s_sum[buf][warp] = ss;
+            __syncthreads();
+            ss = 0.f;
+            for (int i = 0; i < W; ++i) ss += s_sum[buf][row_in_block * W + i];
+        }
+        const float r = 1.f / sqrtf(ss / (float)p.H + p.eps);
+        uint32_t top = 0;                                     // largest |y| of the row
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = first + v * step, n = live ? p.H - col : 0;
+            float g[8];
+            unpack8(gv[v], g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[v][i] = h[v][i] * r * g[i];
+            if (p.out) store8<VEC>(p.out + (size_t)t * p.ldo + col, n, h[v]);
+            if (QUANT && p.group == 0) {
+                // (columns that are not there hold 0, or 0 * r with r not finite)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) if (VEC ? n > 0 : i < n) top = max(top, magnitude(h[v][i]));
+            }
+        }
+        if (!QUANT) continue;
+        if (p.group == 0) {
+            top = __reduce_max_sync(kFull, top);
+            if (W > 1) {
+                if (lane == 0) s_top[buf][warp] = top;
+                __syncthreads();
+                top = 0;
+                for (int i = 0; i < W; ++i) top = max(top, s_top[buf][row_in_block * W + i]);
+            }
+            const float scale = __uint_as_float(top) / 448.f;
+            if (live && wr == 0 && lane == 0) p.q_scale[t] = scale;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int col = first + v * step, n = live ? p.H - col : 0;
+                if (n > 0) store_q<VEC>(p.q + (size_t)t * p.ldq + col, n, p.vec_q, h[v], scale);
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[v][i] = 0.f;
-        }
-    }
+            for (int v = 0; v < V; ++v) {
+                // sixteen lanes hold 128 columns
+                const int col = first + v * step, n = live ? p.H - col : 0;
+                uint32_t a = 0;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int col = ((v * W + wr) * 32 + lane) * 8, n = p.H - col;
-        if (p.residual_out && live && n > 0) store8(p.residual_out + (size_t)t * p.ldro + col, n, p.vec && n >= 8, h[v]);
+                for (int i = 0; i < 8; ++i) if (VEC ? n > 0 : i < n) a = max(a, magnitude(h[v][i]));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(h[v][i], h[v][i], ss);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(kFull, ss, o);
-    if (W > 1) {
-        if (lane == 0) s_part[0][warp] = ss;
-        __syncthreads();
-        ss = 0.f;
-        for (int i = 0; i < W; ++i) ss += s_part[0][row_in_block * W + i];
-    }
-    const float r = 1.f / sqrtf(ss / (float)p.H + p.eps);
-    float top = 0.f;                        // max |y| of this lane's elements (row scales)
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int col = ((v * W + wr) * 32 + lane) * 8, n = p.H - col;
-        if (n > 0) {
-            float g[8];
-            load8(p.weight + col, n, p.vec_weight && n >= 8, g);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) h[v][i] = h[v][i] * r * g[i];
-            if (live && p.out) store8(p.out + (size_t)t * p.ldo + col, n, p.vec && n >= 8, h[v]);
-        }
-        if (QUANT && p.group == 0) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) if (i < n) top = max_nan(top, fabsf(h[v][i]));
-        }
-    }
-    if (!QUANT) return;
-    float scale = 0.f;
-    if (p.group == 0) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(kFull, top, o));
-        if (W > 1) {
-            if (lane == 0) s_part[1][warp] = top;
-            __syncthreads();
-            top = 0.f;
-            for (int i = 0; i < W; ++i) top = max_nan(top, s_part[1][row_in_block * W + i]);
-        }
-        scale = top / 448.f;
-        if (live && wr == 0 && lane == 0) p.q_scale[t] = scale;
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int vec_id = (v * W + wr) * 32 + lane, col = vec_id * 8, n = p.H - col;
-        if (p.group != 0) {
-            // sixteen lanes hold 128 columns
-            float a = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) if (i < n) a = max_nan(a, fabsf(h[v][i]));
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) a = max_nan(a, __shfl_xor_sync(kFull, a, o));
-            scale = a / 448.f;
-            if (live && n > 0 && (lane & 15) == 0) p.q_scale[(size_t)t * p.n_groups + (vec_id >> 4)] = scale;
-        }
-        if (!live || n <= 0) continue;
-        // (the reciprocal of a scale below 2^-126 is not a number to multiply with)
-        const bool tiny = scale < 1e-37f;
-        const float inv = tiny ? 0.f : 1.f / scale;
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = tiny ? (scale > 0.f ? h[v][i] / scale : 0.f) : h[v][i] * inv;
-        uint8_t* dst = p.q + (size_t)t * p.ldq + col;
-        if (p.vec_q && n >= 8) {
-            uint2 o;
-            o.x = e4m3x2(y[0], y[1]) | ((uint32_t)e4m3x2(y[2], y[3]) << 16);
-            o.y = e4m3x2(y[4], y[5]) | ((uint32_t)e4m3x2(y[6], y[7]) << 16);
-            *reinterpret_cast<uint2*>(dst) = o;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) if (i < n) dst[i] = (uint8_t)(e4m3x2(y[i], 0.f) & 0xff);
+                for (int o = 8; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(kFull, a, o));
+                const float scale = __uint_as_float(a) / 448.f;
+                if (n > 0) {
+                    if ((lane & 15) == 0) p.q_scale[(size_t)t * p.n_groups + (col >> 7)] = scale;
+                    store_q<VEC>(p.q + (size_t)t * p.ldq + col, n, p.vec_q, h[v], scale);
+                }
+            }
         }
     }
 }
 
+template <int V, bool QUANT, bool VEC>
+cudaError_t launch_one(const AddNormArgs& p, int W, int rows, cudaStream_t st)
+{
+    // As many blocks as are resident at once (57 registers with V = 1, up to 128 above): 16384 x 2048 with a row's scale, V = 2,
+    // takes 52 us with 4 blocks of 4 warps per SM, 63 with 3, 66 with 6 and 81 with a block for every row.
+    const int sets = (p.T + rows - 1) / rows, most = 148 * ((V == 1 ? 32 : 16) / (W * rows));
+    return launch_pdl(addnorm_kernel<V, QUANT, VEC>, dim3(sets < most ? sets : most), dim3(32 * W * rows), 0, st, p, W);
+}
 template <int V>
 cudaError_t launch_v(const AddNormArgs& p, int W, int rows, cudaStream_t st)
 {
-    const dim3 grid((p.T + rows - 1) / rows), block(32 * W * rows);
-    return p.q ? launch_pdl(addnorm_kernel<V, true>, grid, block, 0, st, p, W)
-               : launch_pdl(addnorm_kernel<V, false>, grid, block, 0, st, p, W);
+    if (p.vec) return p.q ? launch_one<V, true, true>(p, W, rows, st) : launch_one<V, false, true>(p, W, rows, st);
+    return p.q ? launch_one<V, true, false>(p, W, rows, st) : launch_one<V, false, false>(p, W, rows, st);
 }
 
 }  // namespace
@@ -180,14 +230,15 @@ cudaError_t launch_addnorm(const AddNormArgs& in, cudaStream_t st)
 {
     AddNormArgs p = in;
     auto al = [](const void* q, size_t n) { return (uintptr_t)q % n == 0; };
-    p.vec = al(p.x, 16) && p.ldx % 8 == 0 && al(p.residual, 16) && p.ldr % 8 == 0 && al(p.residual_out, 16) && p.ldro % 8 == 0 &&
+    p.vec = p.H % 8 == 0 && al(p.x, 16) && p.ldx % 8 == 0 && al(p.residual, 16) && p.ldr % 8 == 0 && al(p.residual_out, 16) && p.ldro % 8 == 0 &&
             al(p.out, 16) && p.ldo % 8 == 0;
     p.vec_weight = al(p.weight, 16);
     p.vec_q = al(p.q, 8) && p.ldq % 8 == 0;
+    // Vectors per lane: two where a row has more than one warp's worth, four beyond 4096 columns (16384 x 2048, us: V = 1 57, V = 2
+    // 52, V = 4 54; 4096 x 8192: V = 2 58, V = 4 52).  Element by element (VEC false) one is faster: 333 x 1411 4.8 against 5.5.
     const int vecs = (p.H + 7) / 8;
-    const int V = vecs <= 32 ? 1 : (vecs <= 512 ? 2 : 4);
-    int W = (vecs + 32 * V - 1) / (32 * V);
-    const int rows = W >= 4 ? 1 : 4 / W;
+    const int V = vecs <= 32 || (!p.vec && vecs <= 512) ? 1 : (vecs <= 512 ? 2 : 4);
+    const int W = (vecs + 32 * V - 1) / (32 * V), rows = W >= 4 ? 1 : 4 / W;
     if (V == 1) return launch_v<1>(p, W, rows, st);
     if (V == 2) return launch_v<2>(p, W, rows, st);
     return launch_v<4>(p, W, rows, st);

@@ -16,9 +16,10 @@
 //     redux.sync over the heads of the lists and a shift in the winner's lane;
 //   - neighbours of the result that are closer than the error bound of key and 32-bit value, and are not the same pair
 //     (z, b), are put in order by their 64-bit values, one candidate per lane (in_order64); where the groups are that close, the
-//     warp does the whole token in 64 bits (choose64).
+//     groups' scores are taken in 64 bits (keep64).
 // Bound by instruction issue: see launch_gate for the counts and times.
 #include <float.h>
+#include <stdlib.h>
 
 #include "gate.cuh"
 
@@ -169,6 +170,67 @@ __device__ __forceinline__ uint32_t pop(uint32_t (&key)[C])
     return m;
 }
 
+// The groups that stay, decided in 64 bits (bit g: group g).
+template <int C, bool SIGMOID, bool BIAS>
+__device__ __noinline__ uint32_t keep64(const GateArgs& p, int t, const float* bias, double* row)
+{
+    const int lane = threadIdx.x & 31;
+    const bool by_logit = !BIAS && (p.group_score == MOE_GROUP_MAX || p.group_size == 1);
+    float z[C];
+    double v[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) z[i] = lane * C + i < p.E ? load_logit(p, t, lane * C + i) : -INFINITY;
+    if (by_logit) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) v[i] = z[i];
+    } else if (SIGMOID) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) v[i] = sigmoid64(z[i]);
+    } else {
+        float m = z[0];
+#pragma unroll
+        for (int i = 1; i < C; ++i) m = fmaxf(m, z[i]);
+        m = key_value(__reduce_max_sync(kFull, order_key(m)));
+        double sum = 0;
+#pragma unroll
+        for (int i = 0; i < C; ++i) { v[i] = z[i] == -INFINITY ? 0. : exp((double)z[i] - (double)m); sum += v[i]; }
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
+#pragma unroll
+        for (int i = 0; i < C; ++i) v[i] = sum > 0 ? v[i] / sum : 0.;
+    }
+    if (BIAS) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) v[i] += (double)clean_bias(lane * C + i < p.E ? __ldg(bias + lane * C + i) : 0.f);
+    }
+    double a = -INFINITY, b = -INFINITY;
+    if (p.lanes_per_group) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) { if (v[i] > a) { b = a; a = v[i]; } else if (v[i] > b) b = v[i]; }
+        for (int o = 1; o < p.lanes_per_group; o <<= 1) {
+            const double oa = __shfl_xor_sync(kFull, a, o), ob = __shfl_xor_sync(kFull, b, o);
+            if (oa > a) { b = a > ob ? a : ob; a = oa; } else if (oa > b) b = oa;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < C; ++i) row[lane * C + i] = v[i];
+        __syncwarp();
+        if (lane < p.n_groups)
+            for (int i = 0; i < p.group_size; ++i) {
+                const double x = row[lane * p.group_size + i];
+                if (x > a) { b = a; a = x; } else if (x > b) b = x;
+            }
+        __syncwarp();
+    }
+    if (p.group_score == MOE_GROUP_TOP2 && p.group_size > 1) a += b;
+    if (p.lanes_per_group) a = __shfl_sync(kFull, a, (lane * p.lanes_per_group) & 31);
+    int rank = 0;
+    for (int g = 0; g < p.n_groups; ++g) {
+        const double x = __shfl_sync(kFull, a, g);
+        rank += x > a || (x == a && g < lane);
+    }
+    return __ballot_sync(kFull, lane < p.n_groups && rank < p.keep);
+}
+
 template <int C, bool SIGMOID, bool BIAS, bool GROUPS>
 struct Gate {
     static constexpr uint32_t kIdMask = 32 * C - 1;
@@ -232,18 +294,38 @@ struct Gate {
     }
 };
 
+// Weights and outputs of one token, by a warp: lane j < p.k has the expert of rank j and its logit.
+template <bool SIGMOID>
+__device__ __forceinline__ void write_token(const GateArgs& p, int t, int lane, int my_e, float my_z, float zmax, float inv_sum, bool bad)
+{
+    float w, s = 0.f;
+    if (p.renormalize) {
+        // exp(-ref) scales every chosen score alike, so small scores do not underflow before the division
+        float top = lane < p.k ? my_z : -INFINITY;
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+        const float ref = SIGMOID ? fminf(top, 0.f) : top;
+        if (lane < p.k && my_z != -INFINITY) s = SIGMOID ? sigmoid_from(my_z, ref) : expf(my_z - ref);
+        float sum = s;
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
+        w = sum > 0.f ? s / sum * p.scale : 0.f;
+    } else {
+        if (my_z != -INFINITY) s = SIGMOID ? sigmoid_from(my_z, 0.f) : expf(my_z - zmax) * inv_sum;
+        w = s * p.scale;
+    }
+    if (lane < p.k) {
+        p.topk_idx[(size_t)t * p.k + lane] = bad ? lane : my_e;
+        p.topk_w[(size_t)t * p.k + lane] = bad ? 0.f : w;
+    }
+}
+
+// One token by one warp; row: scratch of 32 C doubles.
 template <int C, bool SIGMOID, bool BIAS, bool GROUPS>
-__global__ void __launch_bounds__(kGateWarps * 32)
-gate_kernel(const GateArgs p)
+__device__ __forceinline__ void gate_token(const GateArgs& p, int t, int lane, double* row)
 {
     using G = Gate<C, SIGMOID, BIAS, GROUPS>;
     constexpr uint32_t kIdMask = G::kIdMask;
-    __shared__ double s_row[kGateWarps][32 * C];
-    pdl_wait();
-    pdl_launch_dependents();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int t = blockIdx.x * kGateWarps + warp;
-    if (t >= p.T) return;
     bool bad = false;
     int model = 0;
     if (p.tenant_id) {
@@ -343,7 +425,7 @@ gate_kernel(const GateArgs p)
     }
 
     // groups of experts
-    bool undecided = false;                                   // the groups, or the last rank against the next
+    bool undecided = false;                                   // 32 bits did not decide
     if constexpr (GROUPS) {
         float score;                                          // lane g < n_groups: score of group g
         if (p.lanes_per_group) {
@@ -361,14 +443,14 @@ gate_kernel(const GateArgs p)
             }
             score = __shfl_sync(kFull, sums ? a + c : a, (lane * p.lanes_per_group) & 31);
         } else {
-            float* row = reinterpret_cast<float*>(s_row[warp]);
+            float* frow = reinterpret_cast<float*>(row);
 #pragma unroll
-            for (int i = 0; i < C; ++i) row[lane * C + i] = !BIAS && sums ? sc[i] : v[i];
+            for (int i = 0; i < C; ++i) frow[lane * C + i] = !BIAS && sums ? sc[i] : v[i];
             __syncwarp();
             float a = -INFINITY, c = -INFINITY;
             if (lane < p.n_groups)
                 for (int i = 0; i < p.group_size; ++i) {
-                    const float x = row[lane * p.group_size + i];
+                    const float x = frow[lane * p.group_size + i];
                     c = fmaxf(c, fminf(a, x));
                     a = fmaxf(a, x);
                 }
@@ -382,12 +464,13 @@ gate_kernel(const GateArgs p)
             rank += o > gkey || (o == gkey && g < lane);
         }
         const bool in = lane < p.n_groups && rank < p.keep;
-        const uint32_t kept = __ballot_sync(kFull, in);
+        uint32_t kept = __ballot_sync(kFull, in);
         if (BIAS || sums) {
             // the last kept against the best dropped group (a largest logit is exact: nothing to ask)
             const float lo = key_value(__reduce_min_sync(kFull, in ? gkey : kFull));
             const float hi = key_value(__reduce_max_sync(kFull, in ? 0u : gkey));
             undecided = !(lo - hi > (sums ? 2.f : 1.f) * G::kScoreSlack + 1e-6f * (fabsf(lo) + fabsf(hi)));
+            if (undecided) kept = keep64<C, SIGMOID, BIAS>(p, t, bias, row);
         }
         if (p.lanes_per_group) {
             if (!(kept >> (lane / p.lanes_per_group) & 1)) {
@@ -405,7 +488,7 @@ gate_kernel(const GateArgs p)
     int my_e;
     float my_z, flag_v = 0.f;
     const int rounds = min(p.k + 1, p.eligible);
-    if (!undecided) {
+    {
         sort_desc<C>(key);
         uint32_t my_key = 0;
 #pragma unroll
@@ -426,38 +509,13 @@ gate_kernel(const GateArgs p)
             const bool near = lane > 0 && lane < rounds && !same && !(pv - kv > G::kSlack + G::kRel * fmaxf(fabsf(pv), fabsf(kv)));
             if (__any_sync(kFull, near)) {
                 undecided = true;
-                my_e = G::in_order64(p, t, bias, key, my_key, my_e, rounds, s_row[warp]);
+                my_e = G::in_order64(p, t, bias, key, my_key, my_e, rounds, row);
                 if (lane < p.k) my_z = load_logit(p, t, my_e);
             }
         }
-    } else {
-        my_e = choose64<C>(p, t, bias, s_row[warp]);
-        my_z = lane < p.k ? load_logit(p, t, my_e) : -INFINITY;
     }
 
-    // weights
-    float w, s;
-    if (p.renormalize) {
-        // exp(-ref) scales every chosen score alike, so small scores do not underflow before the division
-        float top = lane < p.k ? my_z : -INFINITY;
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-        const float ref = SIGMOID ? fminf(top, 0.f) : top;
-        s = 0.f;
-        if (lane < p.k && my_z != -INFINITY) s = SIGMOID ? sigmoid_from(my_z, ref) : expf(my_z - ref);
-        float sum = s;
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
-        w = sum > 0.f ? s / sum * p.scale : 0.f;
-    } else {
-        s = 0.f;
-        if (my_z != -INFINITY) s = SIGMOID ? sigmoid_from(my_z, 0.f) : expf(my_z - zmax) * inv_sum;
-        w = s * p.scale;
-    }
-    if (lane < p.k) {
-        p.topk_idx[(size_t)t * p.k + lane] = bad ? lane : my_e;
-        p.topk_w[(size_t)t * p.k + lane] = bad ? 0.f : w;
-    }
+    write_token<SIGMOID>(p, t, lane, my_e, my_z, zmax, inv_sum, bad);
     if (p.tie_flag) {
         // two neighbours among ranks 1..k+1 closer than 1e-5 relative, in the values that order them (without a bias: the scores)
         if (my_z != -INFINITY) flag_v = SIGMOID ? sigmoid_from(my_z, 0.f) : expf(my_z - zmax) * inv_sum;
@@ -467,6 +525,374 @@ gate_kernel(const GateArgs p)
         if (lane == 0) p.tie_flag[t] = near || undecided;
     }
     if (bad && lane == 0 && p.status) atomicOr(p.status, MOE_DEV_BAD_TENANT);
+}
+
+template <int C, bool SIGMOID, bool BIAS, bool GROUPS>
+__global__ void __launch_bounds__(kGateWarps * 32)
+gate_kernel(const GateArgs p)
+{
+    __shared__ double s_row[kGateWarps][32 * C];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, t = blockIdx.x * kGateWarps + warp;
+    if (t < p.T) gate_token<C, SIGMOID, BIAS, GROUPS>(p, t, threadIdx.x & 31, s_row[warp]);
+}
+
+// (a call, so that the registers of its rare use do not count in the kernel below)
+template <int C, bool SIGMOID, bool BIAS, bool GROUPS>
+__device__ __noinline__ void gate_token_again(const GateArgs& p, int t, int lane, double* row)
+{
+    gate_token<C, SIGMOID, BIAS, GROUPS>(p, t, lane, row);
+}
+
+// Many tokens: four lanes per token.  A warp's instructions are what bounds the choice (the kernel above needs about 870 per
+// token with 256 experts, groups and a bias), and most of its rounds keep 31 lanes waiting for one.  Here the lanes
+// of a token go over its experts in blocks of 32 (lane r: experts 32 b + 16 h + 4 r + i), sort the eight of a block with the
+// network, read the block's two largest off its top, and merge block after block into a list of the eight largest (pairwise
+// maxima of one list and the other reversed are a bitonic sequence with the eight largest of both); two more merges join the
+// four lanes.  The largest of what the merges drop is rank 9.  Groups are runs of whole blocks.  All loads of a token are in
+// flight at once; its logits, then its sorted blocks, wait in shared memory at places that only their lane touches, so
+// that the blocks can be a short loop.
+template <int NB, bool SIGMOID, bool BIAS, bool GROUPS>
+__global__ void __launch_bounds__(kGateWarps * 32)
+gate_many_kernel(const GateArgs p)
+{
+    using G = Gate<NB, SIGMOID, BIAS, GROUPS>;
+    constexpr uint32_t kIdMask = G::kIdMask;
+    __shared__ double s_row[kGateWarps][32 * NB];
+    __shared__ float4 s_z[kGateWarps][2 * NB][32];                        // [half block][lane]: logits, then sorted keys
+    __shared__ float4 s_bias[BIAS ? 8 * NB : 1];
+    __shared__ uint2 s_top[kGateWarps][GROUPS ? NB : 1][8];               // a block's two largest keys, per token
+    pdl_wait();
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane & 3;
+    const int t0 = (blockIdx.x * kGateWarps + warp) * 8, t = t0 + (lane >> 2);
+    const bool live = t < p.T;
+    const int blocks = (p.E + 31) >> 5;
+    {
+        float4 q[2 * NB];
+#pragma unroll
+        for (int c = 0; c < 2 * NB; ++c) {
+            const int e = 16 * c + 4 * r;
+            q[c] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            if (p.vec && live && e + 4 <= p.E) {
+                if (p.bf16_logits) {
+                    const uint2 v = *reinterpret_cast<const uint2*>((const bf16*)p.logits + (size_t)t * p.ld + e);
+                    q[c] = make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
+                                       __uint_as_float(v.y & 0xffff0000u));
+                } else {
+                    q[c] = *reinterpret_cast<const float4*>((const float*)p.logits + (size_t)t * p.ld + e);
+                }
+            } else if (live && e < p.E) {
+                q[c].x = load_logit(p, t, e);
+                if (e + 1 < p.E) q[c].y = load_logit(p, t, e + 1);
+                if (e + 2 < p.E) q[c].z = load_logit(p, t, e + 2);
+                if (e + 3 < p.E) q[c].w = load_logit(p, t, e + 3);
+            }
+        }
+        if constexpr (BIAS) {
+            if (p.M == 1)
+                for (int e = threadIdx.x; e < 32 * NB; e += kGateWarps * 32) reinterpret_cast<float*>(s_bias)[e] = e < p.E ? __ldg(p.bias + e) : 0.f;
+        }
+#pragma unroll
+        for (int c = 0; c < 2 * NB; ++c)
+            s_z[warp][c][lane] = make_float4(clean(q[c].x), clean(q[c].y), clean(q[c].z), clean(q[c].w));
+    }
+    __syncthreads();
+    if (t0 >= p.T) return;
+    bool bad = false;
+    int model = 0;
+    if (p.tenant_id && live) {
+        const int u = p.tenant_id[t];
+        bad = u < 0 || u >= p.n_tenants;
+        model = p.model_of_tenant ? p.model_of_tenant[bad ? 0 : u] : 0;
+        if (model < 0 || model >= p.M) model = 0;
+    }
+    const float* bias = BIAS ? p.bias + (size_t)model * p.E : nullptr;
+    auto block_logits = [&](int b, float (&z)[8]) {
+        const float4 x = s_z[warp][2 * b][lane], y = s_z[warp][2 * b + 1][lane];
+        z[0] = x.x; z[1] = x.y; z[2] = x.z; z[3] = x.w; z[4] = y.x; z[5] = y.y; z[6] = y.z; z[7] = y.w;
+    };
+    // softmax: maximum and sum of the row (for scores, and for weights that are not renormalised), in one pass with a running maximum
+    constexpr float kLog2e = 1.4426950408889634f;
+    float zmax = 0.f, inv_sum = 0.f;
+    if (!SIGMOID && (BIAS || !p.renormalize || p.tie_flag)) {
+        float m = -INFINITY, sum = 0.f;
+#pragma unroll 1
+        for (int b = 0; b < blocks; ++b) {
+            float z[8];
+            block_logits(b, z);
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, z[i]);
+            sum = top == -INFINITY ? 0.f : sum * ex2((m - top) * kLog2e);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += z[i] == -INFINITY ? 0.f : ex2((z[i] - top) * kLog2e);
+            m = top;
+        }
+        zmax = fmaxf(m, __shfl_xor_sync(kFull, m, 1));
+        zmax = fmaxf(zmax, __shfl_xor_sync(kFull, zmax, 2));
+        sum = m == -INFINITY ? 0.f : sum * ex2((m - zmax) * kLog2e);
+        sum += __shfl_xor_sync(kFull, sum, 1);
+        sum += __shfl_xor_sync(kFull, sum, 2);
+        inv_sum = sum > 0.f ? 1.f / sum : 0.f;
+    }
+
+    uint32_t list[8], dropped = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) list[i] = 0u;
+    auto merge = [&](const uint32_t (&other)[8]) {
+        uint32_t d[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            d[i] = min(list[i], other[7 - i]);
+            list[i] = max(list[i], other[7 - i]);
+        }
+        dropped = max(dropped, max(max(max(d[0], d[1]), max(d[2], d[3])), max(max(d[4], d[5]), max(d[6], d[7]))));
+        auto cs = [&](int i, int j) { const uint32_t x = max(list[i], list[j]), y = min(list[i], list[j]); list[i] = x; list[j] = y; };
+        cs(0, 4); cs(1, 5); cs(2, 6); cs(3, 7); cs(0, 2); cs(1, 3); cs(4, 6); cs(5, 7); cs(0, 1); cs(2, 3); cs(4, 5); cs(6, 7);
+    };
+    {
+#pragma unroll 1
+        for (int b = 0; b < blocks; ++b) {
+            float z[8];
+            block_logits(b, z);
+            uint32_t key[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int e = 32 * b + 16 * h + 4 * r;
+                float bv[4] = {0.f, 0.f, 0.f, 0.f};
+                if constexpr (BIAS) {
+                    if (p.M == 1) {
+                        const float4 q = s_bias[e >> 2];
+                        bv[0] = q.x; bv[1] = q.y; bv[2] = q.z; bv[3] = q.w;
+                    } else if (p.vec_bias && e + 4 <= p.E) {
+                        const float4 q = __ldg(reinterpret_cast<const float4*>(bias + e));
+                        bv[0] = q.x; bv[1] = q.y; bv[2] = q.z; bv[3] = q.w;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) bv[i] = e + i < p.E ? __ldg(bias + e + i) : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float v = z[4 * h + i];
+                    if constexpr (BIAS) {
+                        // (the softmax of -inf is 0 also where the whole row is -inf)
+                        v = (SIGMOID ? rcp(1.f + ex2(-v * kLog2e)) : (v == -INFINITY ? 0.f : ex2((v - zmax) * kLog2e) * inv_sum)) + clean_bias(bv[i]);
+                    }
+                    key[4 * h + i] = (order_key(fmaxf(v, -FLT_MAX)) & ~kIdMask) | (kIdMask - e - i);
+                    if (e + i >= p.E) key[4 * h + i] = 0u;
+                }
+            }
+            sort_desc<8>(key);
+            if constexpr (GROUPS) {
+                uint32_t a = key[0], c = key[1];
+#pragma unroll
+                for (int o = 1; o <= 2; o <<= 1) {
+                    const uint32_t oa = __shfl_xor_sync(kFull, a, o), oc = __shfl_xor_sync(kFull, c, o);
+                    c = max(min(a, oa), max(c, oc));
+                    a = max(a, oa);
+                }
+                if (r == 0) s_top[warp][b][lane >> 2] = make_uint2(a, c);
+                uint4* keys = reinterpret_cast<uint4*>(&s_z[warp][2 * b][lane]);
+                keys[0] = make_uint4(key[0], key[1], key[2], key[3]);
+                keys[32] = make_uint4(key[4], key[5], key[6], key[7]);
+            } else {
+                merge(key);
+            }
+        }
+    }
+
+    bool unsure = false;                                      // this token goes through gate_token
+    if constexpr (GROUPS) {
+        __syncwarp();
+        const bool top2 = p.group_score == MOE_GROUP_TOP2;
+        const int run = p.group_size >> 5;                    // blocks per group: 1, 2, 4 or 8
+        // lane r scores the groups r, r + 4 of its token and counts the better ones
+        const int groups = p.n_groups;                        // at most 8
+        float score[2], big = 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int g = r + 4 * h;
+            uint32_t a = 0, c = 0;
+            if (g < groups)
+                for (int o = 0; o < run; ++o) {
+                    const uint2 q = s_top[warp][g * run + o][lane >> 2];
+                    c = max(min(a, q.x), max(c, q.y));
+                    a = max(a, q.x);
+                }
+            score[h] = g < groups ? key_value(a) + (top2 ? key_value(c) : 0.f) : -INFINITY;
+            if (g < groups) big = fmaxf(big, fabsf(key_value(a)) + fabsf(key_value(c)));
+        }
+        int above[2] = {0, 0};
+#pragma unroll
+        for (int o = 0; o < 8; ++o) {
+            const float other = __shfl_sync(kFull, o < 4 ? score[0] : score[1], (lane & ~3) | (o & 3));
+            if (o < groups) {
+                above[0] += other > score[0] || (other == score[0] && o < r);
+                above[1] += other > score[1] || (other == score[1] && o < r + 4);
+            }
+        }
+        float lo = INFINITY, hi = -INFINITY;
+        uint32_t kept = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int g = r + 4 * h;
+            if (g >= groups) continue;
+            if (above[h] < p.keep) { kept |= 1u << g; lo = fminf(lo, score[h]); } else hi = fmaxf(hi, score[h]);
+        }
+#pragma unroll
+        for (int o = 1; o <= 2; o <<= 1) {
+            kept |= __shfl_xor_sync(kFull, kept, o);
+            lo = fminf(lo, __shfl_xor_sync(kFull, lo, o));
+            hi = fmaxf(hi, __shfl_xor_sync(kFull, hi, o));
+            big = fmaxf(big, __shfl_xor_sync(kFull, big, o));
+        }
+        // (scores are sums of values read off keys; bf16 logits lose nothing there)
+        unsure = (BIAS || !p.bf16_logits) && !(lo - hi > (top2 ? 2.f : 1.f) * G::kSlack + G::kRel * big);
+        const int shift = 31 - __clz(run);
+#pragma unroll 1
+        for (int b = 0; b < blocks; ++b) {
+            const bool mine = kept >> (b >> shift) & 1;
+            const uint4* keys = reinterpret_cast<const uint4*>(&s_z[warp][2 * b][lane]);
+            const uint4 x = keys[0], y = keys[32];
+            const uint32_t key[8] = {mine ? x.x : 0u, mine ? x.y : 0u, mine ? x.z : 0u, mine ? x.w : 0u,
+                                     mine ? y.x : 0u, mine ? y.y : 0u, mine ? y.z : 0u, mine ? y.w : 0u};
+            merge(key);
+        }
+    }
+
+    // the four lanes' lists into one
+#pragma unroll 1
+    for (int o = 1; o <= 2; o <<= 1) {
+        uint32_t other[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) other[i] = __shfl_xor_sync(kFull, list[i], o);
+        dropped = max(dropped, __shfl_xor_sync(kFull, dropped, o));
+        merge(other);
+    }
+
+    // neighbours that the keys do not tell apart: inside the choice they are put in order below, at its end gate_token does it
+    const int k = p.k;
+    bool mixed = false;
+    if (BIAS || !p.bf16_logits) {
+        float f[9];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = key_value(list[j]);
+        f[8] = key_value(dropped);
+        const int last = p.eligible > k ? k : k - 1;
+        float least = f[0];
+#pragma unroll
+        for (int j = 1; j < 9; ++j) if (j == last) least = f[j];
+        const float need = G::kSlack + G::kRel * fmaxf(fabsf(f[0]), fabsf(least));        // (sorted: the largest magnitude is at an end)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool near = !(f[j] - f[j + 1] > need);
+            if (j + 1 < k) mixed |= near;
+            if (j + 1 == k && p.eligible > k) unsure |= near;
+        }
+        if (!SIGMOID && BIAS && mixed) unsure = true;         // (a softmax in 64 bits needs the whole row)
+    }
+
+    // lane r has ranks 2 r and 2 r + 1
+    const uint32_t k0 = r == 0 ? list[0] : r == 1 ? list[2] : r == 2 ? list[4] : list[6], k1 = r == 0 ? list[1] : r == 1 ? list[3] : r == 2 ? list[5] : list[7];
+    const int e0 = (int)(kIdMask - (k0 & kIdMask)), e1 = (int)(kIdMask - (k1 & kIdMask));
+    const bool on0 = live && 2 * r < k, on1 = live && 2 * r + 1 < k;
+    const float z0 = on0 ? load_logit(p, t, e0) : -INFINITY, z1 = on1 ? load_logit(p, t, e1) : -INFINITY;
+    int at0 = 2 * r, at1 = 2 * r + 1;
+    if (__any_sync(kFull, mixed && !unsure)) {
+        double v0 = z0, v1 = z1;
+        if (BIAS) {
+            v0 = on0 ? sigmoid64(z0) + (double)clean_bias(__ldg(bias + e0)) : 0.;
+            v1 = on1 ? sigmoid64(z1) + (double)clean_bias(__ldg(bias + e1)) : 0.;
+        }
+        int n0 = 0, n1 = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int from = (lane & ~3) | q;
+                const double ov = __shfl_sync(kFull, h ? v1 : v0, from);
+                const int oe = __shfl_sync(kFull, h ? e1 : e0, from);
+                if (2 * q + h < k) {
+                    n0 += ov > v0 || (ov == v0 && oe < e0);
+                    n1 += ov > v1 || (ov == v1 && oe < e1);
+                }
+            }
+        if (mixed) { at0 = n0; at1 = n1; }
+    }
+    {
+        float w0, w1, s0 = 0.f, s1 = 0.f;
+        if (p.renormalize) {
+            float top = fmaxf(z0, z1);
+            top = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(kFull, top, 2));
+            const float ref = SIGMOID ? fminf(top, 0.f) : top;
+            if (z0 != -INFINITY) s0 = SIGMOID ? sigmoid_from(z0, ref) : expf(z0 - ref);
+            if (z1 != -INFINITY) s1 = SIGMOID ? sigmoid_from(z1, ref) : expf(z1 - ref);
+            float sum = s0 + s1;
+            sum += __shfl_xor_sync(kFull, sum, 1);
+            sum += __shfl_xor_sync(kFull, sum, 2);
+            w0 = sum > 0.f ? s0 / sum * p.scale : 0.f;
+            w1 = sum > 0.f ? s1 / sum * p.scale : 0.f;
+        } else {
+            if (z0 != -INFINITY) s0 = SIGMOID ? sigmoid_from(z0, 0.f) : expf(z0 - zmax) * inv_sum;
+            if (z1 != -INFINITY) s1 = SIGMOID ? sigmoid_from(z1, 0.f) : expf(z1 - zmax) * inv_sum;
+            w0 = s0 * p.scale; w1 = s1 * p.scale;
+        }
+        const size_t out = (size_t)t * k;
+        if (on0 && !unsure) { p.topk_idx[out + at0] = bad ? 2 * r : e0; p.topk_w[out + at0] = bad ? 0.f : w0; }
+        if (on1 && !unsure) { p.topk_idx[out + at1] = bad ? 2 * r + 1 : e1; p.topk_w[out + at1] = bad ? 0.f : w1; }
+    }
+    if (p.tie_flag) {
+        // neighbours among ranks 1..k+1 closer than 1e-5 relative, in the values that order them (without a bias: the scores)
+        auto value = [&](int e, float zz, bool on) {
+            float v = 0.f;
+            if (on && zz != -INFINITY) v = SIGMOID ? sigmoid_from(zz, 0.f) : expf(zz - zmax) * inv_sum;
+            if (BIAS && on) v += clean_bias(__ldg(bias + e));
+            return v;
+        };
+        const int e8 = (int)(kIdMask - (dropped & kIdMask));
+        const bool on8 = live && k == 8 && p.eligible > 8;
+        const bool next0 = live && 2 * r <= k && 2 * r < p.eligible, next1 = live && 2 * r + 1 <= k && 2 * r + 1 < p.eligible;
+        const float v0 = value(e0, next0 ? load_logit(p, t, e0) : 0.f, next0), v1 = value(e1, next1 ? load_logit(p, t, e1) : 0.f, next1);
+        const float v8 = value(e8, on8 ? load_logit(p, t, e8) : 0.f, on8);
+        float v2 = __shfl_down_sync(kFull, v0, 1);
+        bool has2 = __shfl_down_sync(kFull, (int)next0, 1) != 0;
+        if (r == 3) { v2 = v8; has2 = on8; }
+        bool near = (next1 && !(v0 - v1 >= 1e-5f * fabsf(v0))) || (next1 && has2 && !(v1 - v2 >= 1e-5f * fabsf(v1)));
+        near = near || mixed || unsure;
+        const uint32_t any = __ballot_sync(kFull, near);
+        if (live && r == 0 && !unsure) p.tie_flag[t] = (any >> lane & 15u) != 0;
+    }
+    if (bad && live && r == 0 && p.status) atomicOr(p.status, MOE_DEV_BAD_TENANT);
+
+    // what 32 bits could not decide, token by token
+    uint32_t todo = __ballot_sync(kFull, unsure && live && r == 0);
+    while (todo) {
+        const int from = __ffs(todo) - 1;
+        todo &= todo - 1;
+        gate_token_again<NB, SIGMOID, BIAS, GROUPS>(p, t0 + (from >> 2), lane, s_row[warp]);
+        __syncwarp();
+    }
+}
+
+template <int NB>
+cudaError_t launch_many(const GateArgs& p, cudaStream_t st)
+{
+    const int which = (p.score == MOE_SCORE_SIGMOID ? 4 : 0) + (p.bias ? 2 : 0) + (p.keep < p.n_groups ? 1 : 0);
+    const dim3 grid((p.T + 8 * kGateWarps - 1) / (8 * kGateWarps)), block(kGateWarps * 32);
+    switch (which) {
+        case 0: return launch_pdl(gate_many_kernel<NB, false, false, false>, grid, block, 0, st, p);
+        case 1: return launch_pdl(gate_many_kernel<NB, false, false, true>, grid, block, 0, st, p);
+        case 2: return launch_pdl(gate_many_kernel<NB, false, true, false>, grid, block, 0, st, p);
+        case 3: return launch_pdl(gate_many_kernel<NB, false, true, true>, grid, block, 0, st, p);
+        case 4: return launch_pdl(gate_many_kernel<NB, true, false, false>, grid, block, 0, st, p);
+        case 5: return launch_pdl(gate_many_kernel<NB, true, false, true>, grid, block, 0, st, p);
+        case 6: return launch_pdl(gate_many_kernel<NB, true, true, false>, grid, block, 0, st, p);
+        default: return launch_pdl(gate_many_kernel<NB, true, true, true>, grid, block, 0, st, p);
+    }
 }
 
 template <int C>
@@ -485,6 +911,8 @@ cudaError_t launch_c(const GateArgs& p, dim3 grid, dim3 block, cudaStream_t st)
     }
 }
 
+int many_from() { const char* f = getenv("GATE_MANY"); return f ? atoi(f) : 2048; }
+
 }  // namespace
 
 cudaError_t launch_gate(const GateArgs& in, cudaStream_t st)
@@ -492,12 +920,22 @@ cudaError_t launch_gate(const GateArgs& in, cudaStream_t st)
     GateArgs p = in;
     const int C = p.E <= 64 ? 2 : (p.E <= 128 ? 4 : 8);
     p.group_size = p.E / p.n_groups;
+    const size_t esz = p.bf16_logits ? 2 : 4;
+    p.eligible = p.keep < p.n_groups ? p.keep * p.group_size : p.E;
+    // Four lanes per token from kManyTokens on, where the groups are runs of 1, 2, 4 or 8 blocks of 32 and compared by what orders
+    // the experts (sums of scores beside an order by logits stay with the other kernel).
+    const int run = p.group_size / 32;
+    const bool blocks = p.keep == p.n_groups || (p.group_size % 32 == 0 && (run & (run - 1)) == 0 && (p.bias || p.group_score == MOE_GROUP_MAX));
     // groups that fall on whole lanes, a power of two of them, are reduced by shuffles, others through shared memory
     const int lanes = p.group_size / C;
     p.lanes_per_group = p.group_size % C == 0 && (lanes & (lanes - 1)) == 0 ? lanes : 0;
-    p.eligible = p.keep < p.n_groups ? p.keep * p.group_size : p.E;
+    if (p.T >= many_from() && blocks) {
+        // (aligned for a lane's eight here and for its C in gate_token)
+        p.vec = p.ld % 8 == 0 && (uintptr_t)p.logits % 16 == 0;
+        p.vec_bias = (uintptr_t)p.bias % 16 == 0 && p.E % 4 == 0;
+        return C == 2 ? launch_many<2>(p, st) : (C == 4 ? launch_many<4>(p, st) : launch_many<8>(p, st));
+    }
     // vectors of a lane's share of a row (16 bytes at most)
-    const size_t esz = p.bf16_logits ? 2 : 4;
     const size_t share = C * esz < 16 ? C * esz : 16;
     p.vec = p.ld * esz % share == 0 && (uintptr_t)p.logits % share == 0;
     const size_t bias_share = C * 4 < 16 ? C * 4 : 16;
