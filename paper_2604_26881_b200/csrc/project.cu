@@ -26,7 +26,7 @@ constexpr int kTok = 128;               // tokens per tile: the M operand, one T
 constexpr int kBK = 64;                 // K elements per slice: one 128-byte row of a swizzled tile
 constexpr int kMaxStages = 8;
 constexpr int kUCols = 128;             // columns of one CTA of the first product
-constexpr int kUThreads = 224;          // warp 0: TMA (tokens), 1: MMA, 2..5: lists and epilogue, 6: TMA (rows of A)
+constexpr int kUThreads = 288;          // warp 0: TMA (tokens), 1, 7: MMA, 2..5: lists and epilogue, 6, 8: TMA (rows of A)
 constexpr int kPN = 128;                // weight rows per tile of the projection
 constexpr int kPThreads = 352;          // warp 0: TMA (weights), 1: MMA, 2..9: epilogue, 10: TMA (tokens)
 
@@ -154,18 +154,19 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
     __shared__ int s_abort;
     __shared__ AdapterList<4> s_al;
     __shared__ int s_slot[kTok];
+    __shared__ float s_scale[kTok];
     const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * kMaxStages, bar_done = bar_full + 16 * kMaxStages,
                    bar_free = bar_done + 8, bar_list = bar_done + 16, bar_got = bar_done + 24;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int t0 = blockIdx.x * kTok;
     // Behind the ring (and the rows that the MMA of a short tile may read): this part's sums, [owner][column][token of the
     // owner], and those that the cluster's CTAs send here, [part][column][own token].  A CTA owns a share of the tokens.
-    const int own = p.u_own, pitch = own + 4, block = p.rank * pitch;
+    const int own = p.u_own, pitch = own + 1, block = p.rank * pitch;     // (own is even: an odd pitch has no bank conflicts)
     float* const sums = reinterpret_cast<float*>(smem_dyn + (ring - smem_u32(smem_dyn)) + p.scratch);
     float* const got = p.u_splits > 1 ? sums + p.u_splits * block : sums;
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.n_stages; ++s) { mbar_init(bar_full + 8 * s, 2); mbar_init(bar_empty + 8 * s, 1); }
-        mbar_init(bar_done, 1);
+        mbar_init(bar_done, 2);
         mbar_init(bar_free, 4);
         mbar_init(bar_list, 4);
         mbar_init(bar_got, 1);
@@ -186,6 +187,8 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
     pdl_launch_dependents();        // (after the wait: the projection may read x before it waits itself)
 
     const int k0 = (int)((long long)p.ksteps * blockIdx.z / p.u_splits), k1 = (int)((long long)p.ksteps * (blockIdx.z + 1) / p.u_splits);
+    const int kb = p.kb, per_chunk = (k1 - k0 + kb - 1) / kb;           // slices per stage, stages per chunk
+    const uint32_t b_bytes = (uint32_t)(p.stage_bytes / kb) - p.a_bytes;
     int count = 0, n_chunks = 0;
     auto know_list = [&] {                      // (every role but the listing warps)
         if (!mbar_wait(bar_list, 0, &s_abort, status)) return false;
@@ -193,33 +196,38 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
         n_chunks = (count + p.slots - 1) / p.slots;
         return true;
     };
-    if (warp == 0 || warp == 6) {
-        // two lanes in two warps, so that the tokens need not wait for the list and the loads of a stage are issued side by side
+    if (warp == 0 || warp == 6 || warp == 8) {
+        // One lane loads tokens, two load rows of A, even and odd stages (a load costs its lane about 140 cycles, a barrier 290);
+        // the tokens need not wait for the list.
         if (lane == 0) {
             uint32_t stage = 0, phase = 0, armed = 0, armed_phase = 0;
             bool ok = true;
-            // the tokens of the first slices, before the list is known (it is empty only if no token has an adapter)
-            if (warp == 6) ok = know_list();
-            bool known = warp == 6;
+            int i = 0;                          // stages so far
+            if (warp != 0) ok = know_list();
+            bool known = warp != 0;
             for (int c = blockIdx.y; ok && (!known || c < n_chunks); c += gridDim.y) {
-                for (int ks = k0; ks < k1; ++ks) {
-                    if (!known && (ks - k0 == p.n_stages || blockIdx.y > 0)) {
+                for (int ks = k0; ks < k1; ks += kb, ++i) {
+                    if (!known && (i == p.n_stages || blockIdx.y > 0)) {
                         if (!know_list()) { ok = false; break; }
                         known = true;
                         if (c >= n_chunks) break;
                     }
-                    if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, status)) { ok = false; break; }
-                    const uint32_t sa = ring + stage * p.stage_bytes, sb = sa + p.a_bytes, full = bar_full + 8 * stage;
-                    armed |= 1u << stage;
-                    armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
-                    if (warp == 0) {
-                        mbar_expect_tx(full, p.a_rows * kBK * 2);
-                        tma_load_2d(sa, &maps.x, full, ks * kBK, t0);
-                    } else {
-                        const int n_slots = min(p.slots, count - c * p.slots);
-                        mbar_expect_tx(full, n_slots * p.rank * kBK * 2);
-                        for (int j = 0; j < n_slots; ++j)
-                            tma_load_2d(sb + j * p.rank * kBK * 2, &maps.a, full, ks * kBK, s_al.list[c * p.slots + j] * p.rank);
+                    if (warp == 0 || (i & 1) == (warp == 8)) {
+                        if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, status)) { ok = false; break; }
+                        const uint32_t sa = ring + stage * p.stage_bytes, sb = sa + kb * p.a_bytes, full = bar_full + 8 * stage;
+                        const int n = min(kb, k1 - ks);
+                        armed |= 1u << stage;
+                        armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
+                        if (warp == 0) {
+                            mbar_expect_tx(full, n * p.a_rows * kBK * 2);
+                            for (int q = 0; q < n; ++q) tma_load_2d(sa + q * p.a_bytes, &maps.x, full, (ks + q) * kBK, t0);
+                        } else {
+                            const int n_slots = min(p.slots, count - c * p.slots);
+                            mbar_expect_tx(full, n * n_slots * p.rank * kBK * 2);
+                            for (int q = 0; q < n; ++q)
+                                for (int j = 0; j < n_slots; ++j)
+                                    tma_load_2d(sb + q * b_bytes + j * p.rank * kBK * 2, &maps.a, full, (ks + q) * kBK, s_al.list[c * p.slots + j] * p.rank);
+                        }
                     }
                     if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
                 }
@@ -239,28 +247,37 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
                     if (armed & (1u << s)) mbar_wait(bar_full + 8 * s, (armed_phase >> s) & 1u, &s_abort, status);
         }
         __syncwarp();
-    } else if (warp == 1) {
+    } else if (warp == 1 || warp == 7) {
+        // Two lanes issue the MMAs, even and odd stages into accumulators of their own (TMEM columns 0.. and 64..): a narrow MMA
+        // costs its lane about 100 cycles, a wait and a commit some 500, whatever its width.
         if (lane == 0) {
+            const int mine = warp == 7;
             uint32_t stage = 0, phase = 0;
             bool ok = know_list();
-            int it = 0;
+            int it = 0, i = 0;
             for (int c = blockIdx.y; c < n_chunks && ok; c += gridDim.y, ++it) {
                 // (rank 8 and an odd number of adapters: eight stale columns, never read)
                 const int cols = (min(p.slots, count - c * p.slots) * p.rank + 15) & ~15;
-                const uint32_t idesc = idesc_bf16(cols);
+                const uint32_t idesc = idesc_bf16(cols), d = tmem + mine * (kUCols / 2) * (p.slots * p.rank <= kUCols / 2);
                 if (!mbar_wait(bar_free, (it & 1) ^ 1, &s_abort, status)) { ok = false; break; }
                 tc_fence_after();
                 uint32_t acc = 0;
-                for (int ks = k0; ks < k1; ++ks) {
-                    if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, status)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t lo_a = smem_desc_lo(ring + stage * p.stage_bytes), lo_b = lo_a + (p.a_bytes >> 4);
+                for (int ks = k0; ks < k1; ks += kb, ++i) {
+                    if (p.lanes == 1 ? mine == 0 : (i & 1) == mine) {
+                        if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, status)) { ok = false; break; }
+                        tc_fence_after();
+                        uint32_t lo_a = smem_desc_lo(ring + stage * p.stage_bytes), lo_b = lo_a + ((kb * p.a_bytes) >> 4);
+                        const int n = min(kb, k1 - ks);
+                        for (int q = 0; q < n; ++q) {
 #pragma unroll
-                    for (int kk = 0; kk < kBK / 16; ++kk) {
-                        umma_bf16(tmem, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, acc);
-                        acc = 1;
+                            for (int kk = 0; kk < kBK / 16; ++kk) {
+                                umma_bf16(d, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, acc);
+                                acc = 1;
+                            }
+                            lo_a += p.a_bytes >> 4; lo_b += b_bytes >> 4;
+                        }
+                        umma_commit(bar_empty + 8 * stage);
                     }
-                    umma_commit(bar_empty + 8 * stage);
                     if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
                 }
                 if (ok) umma_commit(bar_done);
@@ -277,6 +294,7 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
         __all_sync(kFull, know_list());
         // thread <-> token; a warp reads the TMEM lanes of its quarter
         const int quarter = warp & 3, row = quarter * 32 + lane, my_slot = s_slot[row];
+        s_scale[row] = my_slot >= 0 && p.scale ? p.scale[s_al.adapter[row]] : 1.f;
         float* const dst = sums + (row / own) * block + row % own;
         int it = 0;
         for (int c0 = blockIdx.y; c0 < n_chunks; c0 += gridDim.y, ++it) {
@@ -286,11 +304,19 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
             const int c_lo = live ? f * p.rank : cols, c_hi = live ? c_lo + p.rank : 0;
             if (!__all_sync(kFull, mbar_wait(bar_done, it & 1, &s_abort, status))) break;
             tc_fence_after();
+            // (a chunk of one stage has filled one accumulator only: that of its stage's lane)
+            const int lone = per_chunk == 1 ? (it * per_chunk) & 1 : -1;
             for (int c = 0; c < cols; c += 16) {
                 if (!__any_sync(kFull, c + 16 > c_lo && c < c_hi)) continue;
-                uint32_t r[16];
-                tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + c, r);
+                uint32_t r[16], r2[16];
+                const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + c;
+                tmem_ld16(p.lanes == 2 && lone == 1 ? from + kUCols / 2 : from, r);
+                if (p.lanes == 2 && lone < 0) tmem_ld16(from + kUCols / 2, r2);
                 tmem_ld_wait();
+                if (p.lanes == 2 && lone < 0) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __uint_as_float(r2[i]));
+                }
 #pragma unroll
                 for (int h = 0; h < 16; h += 8)
                     if (c + h >= c_lo && c + h < c_hi) {
@@ -322,22 +348,28 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
         }
         // this CTA adds up its share of the tokens over the parts, in their order
         if (!s_abort) {
-            for (int e = threadIdx.x; e < own * p.rank; e += kUThreads) {
-                const int r = e / p.rank, c = e - r * p.rank, row = own * blockIdx.z + r, slot = s_slot[row];
+            const int pairs = p.rank >> 1;                   // two columns at a time
+            for (int e = threadIdx.x; e < own * pairs; e += kUThreads) {
+                const int r = e / pairs, c = 2 * (e - r * pairs), row = own * blockIdx.z + r, slot = s_slot[row];
                 if (slot < 0 || (slot / p.slots) % gridDim.y != blockIdx.y) continue;
-                float v = 0.f;
-                for (int z = 0; z < p.u_splits; ++z) v += got[z * block + c * pitch + r];
-                if (p.scale) v *= p.scale[s_al.adapter[row]];
+                float v = 0.f, w = 0.f;
+                for (int z = 0; z < p.u_splits; ++z) {
+                    v += got[z * block + c * pitch + r];
+                    w += got[z * block + (c + 1) * pitch + r];
+                }
+                v *= s_scale[row];
+                w *= s_scale[row];
                 const size_t at = (size_t)(t0 + row) * p.rank + c;
                 if (p.u_pair) {
                     // hi + lo hold 16 bits of v (what rounds to an infinity, or is one, has no remainder)
-                    const bf16 hi = __float2bfloat16_rn(v);
-                    const float f = __bfloat162float(hi);
+                    const __nv_bfloat162 hi = __floats2bfloat162_rn(v, w);
+                    const float2 f = __bfloat1622float2(hi);
                     bf16* u = reinterpret_cast<bf16*>(p.u);
-                    u[at] = hi;
-                    u[(size_t)p.T * p.rank + at] = __float2bfloat16_rn(isinf(f) ? 0.f : v - f);
+                    *reinterpret_cast<__nv_bfloat162*>(u + at) = hi;
+                    *reinterpret_cast<__nv_bfloat162*>(u + (size_t)p.T * p.rank + at) =
+                        __floats2bfloat162_rn(isinf(f.x) ? 0.f : v - f.x, isinf(f.y) ? 0.f : w - f.y);
                 } else {
-                    p.u[at] = v;
+                    *reinterpret_cast<float2*>(p.u + at) = make_float2(v, w);
                 }
             }
         }
@@ -379,10 +411,11 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
                    bar_list = bar_done + 8, bar_got = bar_done + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int S = p.splits;
-    const uint32_t rank = S > 1 ? cluster_ctarank() : 0u;
+    const uint32_t rank = blockIdx.x % S;                   // (in a cluster: its rank there)
     const int n0 = (blockIdx.x / S) * kPN, t0 = blockIdx.y * kTok;
     const int rows = min(kTok, p.T - t0);
     const bool product = p.w != nullptr, adapters = p.n_adapters > 0;
+    const bool joint = S > 1 && (product || FUSED);         // a cluster that shares the sums over K; otherwise S CTAs only share the columns
     const int w_rows = product ? kPN : 0;
     constexpr uint32_t kTmem = FUSED ? 256u : (uint32_t)kPN;
     // Behind the ring (and the rows that the MMA of a short tile may read): the sums sent here, [part][own column][token], then
@@ -411,7 +444,7 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
     }
     tc_fence_before();
     __syncthreads();
-    if (S > 1) cluster_arrive();                            // (waited for before anything is sent: the peers run and their barriers are there)
+    if (joint) cluster_arrive();                            // (waited for before anything is sent: the peers run and their barriers are there)
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     // With a first launch that one is adapter_kernel, which had waited for everything before it when it let this kernel start:
@@ -544,7 +577,7 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
             }
         }
     }
-    if (S > 1) {
+    if (joint) {
         __syncthreads();
         cluster_wait();
         if (warp == 0) {
@@ -576,7 +609,7 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
     // have arrived.
     const int* const adapter = FUSED ? s_al.adapter : s_adapter;
     const int total = rows * nc, vecs = p.rank / 8;
-    const float* const got = S > 1 ? part : own;
+    const float* const got = joint ? part : own;
     int r[4], c[4], a[4];
     bool on[4];
     uint4 bq[4][2];
@@ -600,13 +633,13 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
     };
     pick(threadIdx.x);
     if (adapters) load_b(0);
-    if (S > 1) {
+    if (joint) {
         mbar_wait(bar_got, 0, &s_abort, status);
         __syncwarp();
         cluster_arrive();                                  // (waited for at the end: nobody leaves while its copies may still be on their way)
     }
     if (FUSED) {
-        const float* const up = S > 1 ? u_part : own_u;
+        const float* const up = joint ? u_part : own_u;
         for (int i = threadIdx.x; i < rows * p.rank; i += kPThreads) {
             const int ur = i / p.rank, uc = i - ur * p.rank, ua = s_al.adapter[ur];
             float v = 0.f;
@@ -669,7 +702,7 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
             }
         }
     }
-    if (S > 1) cluster_wait();
+    if (joint) cluster_wait();
     tc_fence_before();
     __syncthreads();
     if (warp == 1) {
@@ -731,43 +764,97 @@ __device__ __forceinline__ void builders_sync() { asm volatile("bar.sync 1, 128;
 
 struct MMaps { CUtensorMap x, w, b, u; };
 
-// 32 outputs of one token: columns n .. n+31
+constexpr int kOutPitch = 36;                          // floats per row of a warp's staging area (32 columns, 16-byte rows)
+constexpr size_t kOutStage = 8 * 32 * kOutPitch * sizeof(float);
+
+// 32 tokens x 32 columns (from row t, column n) by a warp, out of its staging area: a row's columns are read, added to the base
+// and written by neighbouring lanes, `kLanes` of them per row.
 template <typename T>
-__device__ __forceinline__ void store32(const ProjectArgs& p, size_t row, int n, float* v, bool vec)
-{
-    T* out = (T*)p.out + row * p.ldo + n;
-    const T* base = p.base ? (const T*)p.base + row * p.ldbase + n : nullptr;
-    constexpr int kPer = 16 / sizeof(T);                // elements of a 16-byte vector
-    if (vec && n + 32 <= p.N) {
-        if (base) {
-            uint4 q[32 / kPer];
+struct Block {
+    static constexpr int kPer = 16 / sizeof(T);         // columns of a 16-byte vector: 4 or 8
+    static constexpr int kLanes = 32 / kPer;            // lanes per row, and vectors per lane: 8 or 4
+    uint4 q[kLanes];                                    // the base
+
+    __device__ __forceinline__ void load_base(const ProjectArgs& p, int t, int n, int lane, bool vec)
+    {
+        if (!p.base || !vec || n + 32 > p.N) return;
 #pragma unroll
-            for (int i = 0; i < 32 / kPer; ++i) q[i] = reinterpret_cast<const uint4*>(base)[i];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                T e;
-                if constexpr (sizeof(T) == 4) e = __uint_as_float((&q[i / 4].x)[i % 4]);
-                else e = __ushort_as_bfloat16((unsigned short)((&q[i / 8].x)[(i % 8) / 2] >> (16 * (i & 1))));
-                v[i] += (float)e;
-            }
+        for (int i = 0; i < kLanes; ++i) {
+            const int r = t + i * (32 / kLanes) + lane / kLanes;
+            q[i] = r < p.T ? *reinterpret_cast<const uint4*>((const T*)p.base + (size_t)r * p.ldbase + n + (lane % kLanes) * kPer) : make_uint4(0, 0, 0, 0);
         }
-#pragma unroll
-        for (int i = 0; i < 32 / kPer; ++i) {
-            uint4 o;
-            if constexpr (sizeof(T) == 4) {
-                o = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-            } else {
-                __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&o);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(v[8 * i + 2 * j], v[8 * i + 2 * j + 1]);
-            }
-            reinterpret_cast<uint4*>(out)[i] = o;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (n + i < p.N) out[i] = (T)(v[i] + (base ? (float)base[i] : 0.f));
     }
+    __device__ __forceinline__ void store(const ProjectArgs& p, const float* stage, int t, int n, int lane, bool vec)
+    {
+        if (vec && n + 32 <= p.N) {
+            const int c = (lane % kLanes) * kPer;
+#pragma unroll
+            for (int i = 0; i < kLanes; ++i) {
+                const int r = i * (32 / kLanes) + lane / kLanes;
+                const float4* from = reinterpret_cast<const float4*>(stage + r * kOutPitch + c);
+                float v[kPer];
+#pragma unroll
+                for (int j = 0; j < kPer / 4; ++j) { const float4 f = from[j]; v[4 * j] = f.x; v[4 * j + 1] = f.y; v[4 * j + 2] = f.z; v[4 * j + 3] = f.w; }
+                uint4 o;
+                if constexpr (sizeof(T) == 4) {
+                    if (p.base) {
+                        v[0] += __uint_as_float(q[i].x); v[1] += __uint_as_float(q[i].y); v[2] += __uint_as_float(q[i].z); v[3] += __uint_as_float(q[i].w);
+                    }
+                    o = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+                } else {
+                    if (p.base) {
+                        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&q[i]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) { const float2 f = __bfloat1622float2(h[j]); v[2 * j] += f.x; v[2 * j + 1] += f.y; }
+                    }
+                    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&o);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+                }
+                if (t + r < p.T) *reinterpret_cast<uint4*>((T*)p.out + (size_t)(t + r) * p.ldo + n + c) = o;
+            }
+        } else if (n + lane < p.N) {
+            for (int r = 0; r < 32 && t + r < p.T; ++r) {
+                float v = stage[r * kOutPitch + lane];
+                if (p.base) v += (float)((const T*)p.base)[(size_t)(t + r) * p.ldbase + n + lane];
+                ((T*)p.out)[(size_t)(t + r) * p.ldo + n + lane] = (T)v;
+            }
+        }
+    }
+};
+
+// One tile's 32 tokens (from t) x 128 columns (from n0) of a warp: out of TMEM, through the staging area, into the output.
+template <typename T>
+__device__ __forceinline__ bool write_tile(const ProjectArgs& p, uint32_t from, float* stage, int t, int n0, int lane, bool vec, bool empty, uint32_t bar_full,
+                                           uint32_t parity, uint32_t bar_read, volatile int* abort_flag, int32_t* status)
+{
+    if (!__all_sync(kFull, mbar_wait(bar_full, parity, abort_flag, status))) return false;
+    tc_fence_after();
+#pragma unroll 1
+    for (int c = 0; c < 128; c += 32) {
+        Block<T> base;
+        if (n0 + c < p.N) base.load_base(p, t, n0 + c, lane, vec);
+        uint32_t r[32];
+        tmem_ld16(from + c, r);
+        tmem_ld16(from + c + 16, r + 16);
+        tmem_ld_wait();
+        if (c == 96) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(bar_read);
+        }
+        if (n0 + c < p.N) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                reinterpret_cast<float4*>(stage + lane * kOutPitch)[i] =
+                    empty ? make_float4(0.f, 0.f, 0.f, 0.f)
+                          : make_float4(__uint_as_float(r[4 * i]), __uint_as_float(r[4 * i + 1]), __uint_as_float(r[4 * i + 2]), __uint_as_float(r[4 * i + 3]));
+            __syncwarp();
+            base.store(p, stage, t, n0 + c, lane, vec);
+            __syncwarp();
+        }
+    }
+    return true;
 }
 
 __global__ void __launch_bounds__(kMThreads, 1)
@@ -778,21 +865,22 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
     const uint32_t ring = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     unsigned char* const ring_ptr = smem_dyn + (ring - smem_u32(smem_dyn));
     const int n_stages = p.n_stages;
-    const uint32_t ua = ring + n_stages * kMStageBytes;                 // u: [64-column chunk][hi, lo] tiles
-    __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 8];
+    // u: [64-column chunk][hi, lo] tiles; once the tile's MMAs have read it, its memory is the epilogue's staging area
+    const uint32_t ua = ring + n_stages * kMStageBytes;
+    __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 9];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     __shared__ AdapterList<8> s_al;
     __shared__ uint32_t s_mask[kMTile][8];
     const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * kMaxStages, bar_tfull = bar_full + 16 * kMaxStages,
-                   bar_tempty = bar_tfull + 16, bar_ufull = bar_tfull + 32, bar_uempty = bar_tfull + 40, bar_list = bar_tfull + 48;
+                   bar_tempty = bar_tfull + 16, bar_ufull = bar_tfull + 32, bar_uempty = bar_tfull + 40, bar_list = bar_tfull + 48, bar_staged = bar_tfull + 56;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const bool leader = rank == 0;
     const bool adapters = p.n_adapters > 0;
     const int n_tiles = (p.N + kMTile - 1) / kMTile, m_tiles = (p.T + kMTile - 1) / kMTile, total = n_tiles * m_tiles;
     const int pair0 = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int chunks = (p.rank + kBK - 1) / kBK;
+    const int chunks = (p.rank + kBK - 1) / kBK;                        // of u and of the adapters' B (0 without adapters)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < n_stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
@@ -800,6 +888,7 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
         mbar_init(bar_ufull, 1);
         mbar_init(bar_uempty, 1);
         mbar_init(bar_list, 4);
+        mbar_init(bar_staged, 8);
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -837,7 +926,9 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
                             if (warp == 10) {
                                 // u of this CTA's tokens, hi and lo tiles (rows of tokens without an adapter hold anything)
                                 if (it == 0) pdl_wait();
-                                if (!mbar_wait(bar_uempty, (it & 1) ^ 1, &s_abort, status)) { ok = false; break; }
+                                // (the MMAs of the tile before have read theirs, and its epilogue is through with the memory)
+                                if (!mbar_wait(bar_uempty, (it & 1) ^ 1, &s_abort, status) ||
+                                    !mbar_wait(bar_staged, (it & 1) ^ 1, &s_abort, status)) { ok = false; break; }
                                 if (leader) mbar_expect_tx(bar_ufull, 4 * chunks * kUTile);
                                 u_loads = it + 1;
                                 for (int c = 0; c < 2 * chunks; ++c)
@@ -932,37 +1023,22 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
         const uint32_t tempty_leader = map_to_cta(bar_tempty, 0);
         const int esz = p.out_f32 ? 4 : 2;
         const bool vec = (uintptr_t)p.out % 16 == 0 && p.ldo * esz % 16 == 0 && (!p.base || ((uintptr_t)p.base % 16 == 0 && p.ldbase * esz % 16 == 0));
+        float* const stage = reinterpret_cast<float*>(ring_ptr + n_stages * kMStageBytes) + (warp - 2) * 32 * kOutPitch;
         if (adapters) pdl_wait();
         bool ok = true;
         int it = 0;
         for (int tile = pair0; tile < total; tile += pairs, ++it) {
             const int n0 = (tile / m_tiles) * kMTile + half * 128, t = (tile % m_tiles) * kMTile + (int)rank * kTok + quarter * 32 + lane;
             const uint32_t buf = it & 1;
-            ok = __all_sync(kFull, mbar_wait(bar_tfull + 8 * buf, (it >> 1) & 1, &s_abort, status));
-            if (!ok) break;
-            tc_fence_after();
-            const bool live = t < p.T;
             // a token that no MMA has written (no product, no adapter): its lane holds some earlier tile
-            const bool empty = p.ksteps == 0 && !(live && adapters && adapter_of(p, t, false) >= 0);
-#pragma unroll 1
-            for (int c = 0; c < 128; c += 32) {
-                uint32_t r[32];
-                const uint32_t from = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16) + half * 128 + c;
-                tmem_ld16(from, r);
-                tmem_ld16(from + 16, r + 16);
-                tmem_ld_wait();
-                if (c == 96) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * buf);
-                }
-                if (live && n0 + c < p.N) {
-                    float v[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = empty ? 0.f : __uint_as_float(r[i]);
-                    if (p.out_f32) store32<float>(p, t, n0 + c, v, vec); else store32<bf16>(p, t, n0 + c, v, vec);
-                }
-            }
+            const bool empty = p.ksteps == 0 && !(t < p.T && adapters && adapter_of(p, t, false) >= 0);
+            const uint32_t from = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16) + half * 128, parity = (it >> 1) & 1;
+            ok = p.out_f32 ? write_tile<float>(p, from, stage, t - lane, n0, lane, vec, empty, bar_tfull + 8 * buf, parity, tempty_leader + 8 * buf, &s_abort, status)
+                           : write_tile<bf16>(p, from, stage, t - lane, n0, lane, vec, empty, bar_tfull + 8 * buf, parity, tempty_leader + 8 * buf, &s_abort, status);
+            if (!ok) break;
+            fence_async_shared();                           // (u of the next tile comes into the staging area by TMA)
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_staged);
         }
     } else if (adapters) {
         // ---- four warps that list the adapters of the pair's tokens, and which lanes each MMA leaves alone ----
@@ -1041,38 +1117,77 @@ cudaError_t allow_smem(K kern, bool (&done)[kMaxDevices])
 
 int div_up(int a, int b) { return (a + b - 1) / b; }
 
+constexpr int kHalfSmem = 108 * 1024;      // dynamic shared memory up to which two CTAs share an SM
+
+// How many clusters of `size` CTAs run at once, with one CTA per SM or two.  The SMs of a cluster belong to one GPC, so a few of
+// each GPC stay unused: on the part measured 15 clusters of eight, not 18, with one CTA per SM (and 33 with two), 33 of
+// four, 45 of three.  A cluster more is a second wave: 20 us instead of 10 for 16 clusters of eight.
+int cluster_room(int size, bool two)
+{
+    static int room[kMaxDevices][9][2] = {};
+    int dev = 0;
+    if (size < 2 || size > 8 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return size == 1 ? 148 * (two ? 2 : 1) : 0;
+    int& n = room[dev][size][two];
+    if (n == 0) {
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = size; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cfg.gridDim = dim3(size * 148); cfg.blockDim = dim3(kPThreads); cfg.dynamicSmemBytes = two ? kHalfSmem : kMaxSmem;
+        cfg.attrs = &attr; cfg.numAttrs = 1;
+        int most = 0;
+        if (cudaOccupancyMaxActiveClusters(&most, project_kernel<false>, &cfg) != cudaSuccess || most < 1) {
+            cudaGetLastError();
+            most = (two ? 256 : 112) / size;                // (no answer: a cautious guess)
+        }
+        n = most;
+    }
+    return n;
+}
+
 // Parts of K, stages and shared memory of project_kernel; false if it does not fit.  `behind`: bytes behind the last stage
 // that the MMA of a short token tile may read.
 bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind)
 {
     const int tiles = div_up(p.N, kPN) * div_up(p.T, kTok), pitch = p.a_rows + 4;
-    // as many parts as there are SMs for the tiles (a cluster holds eight), of two slices at least
-    p.splits = 148 / tiles;
-    if (p.splits > 8) p.splits = 8;
-    if (p.splits > p.ksteps / 2) p.splits = p.ksteps / 2;
-    if (p.splits < 1 || !(p.w || fused)) p.splits = 1;
-    if (p.splits == 5 || p.splits == 7) p.splits -= 1;      // (clusters of 7 pack badly: 18.5 against 9.6 us with 8 and 9.9 with 6, one token, 2048 x 2048)
+    const bool joint = p.w || fused;                        // (otherwise the parts only share the columns)
     p.stage_bytes = p.a_bytes + (p.w ? kPN * kBK * 2 : 0) + ((u_rows + 15) & ~15) * kBK * 2;
-    // received: the parts of this CTA's columns, (fused) the parts of u; and u itself
-    p.sums_bytes = (p.splits * div_up(kPN, p.splits) * pitch + (fused ? p.splits * p.rank * pitch : 0) + p.a_rows * p.rank) * (int)sizeof(float);
-    const int room = kMaxSmem - 1024 - p.sums_bytes;
-    p.n_stages = p.w || fused ? div_up(p.ksteps, p.splits) : 1;
-    const int most = (room - behind) / p.stage_bytes;
-    if (p.n_stages > most) p.n_stages = most;
-    if (p.n_stages > 6) p.n_stages = 6;
-    // the ring, or this CTA's own sums that are put together in it, whichever is larger
-    const int own = (kPN + (fused ? p.rank : 0)) * pitch * (int)sizeof(float);
-    p.scratch = p.n_stages * p.stage_bytes + behind;
-    if (p.scratch < own) p.scratch = own;
-    return p.scratch <= room && (p.n_stages >= 2 || p.ksteps <= 1);
+    // as many parts as there are SMs for the tiles (a cluster holds eight), of two slices at least, all clusters at once
+    for (p.splits = 8; ; --p.splits) {
+        if (p.splits > 1 && (p.splits == 5 || p.splits == 7 || p.splits * tiles > 148 || (joint && p.splits > p.ksteps / 2))) continue;
+        // received: the parts of this CTA's columns, (fused) the parts of u; and u itself
+        p.sums_bytes = (p.splits * div_up(kPN, p.splits) * pitch + (fused ? p.splits * p.rank * pitch : 0) + p.a_rows * p.rank) * (int)sizeof(float);
+        const int own = (kPN + (fused ? p.rank : 0)) * pitch * (int)sizeof(float);
+        const int want = joint ? div_up(p.ksteps, p.splits) : 1;
+        auto stages = [&](int bytes) {                      // the ring, or this CTA's own sums that are put together in it
+            const int room = bytes - 1024 - p.sums_bytes;
+            int n = (room - behind) / p.stage_bytes;
+            if (n > want) n = want;
+            if (n > 6) n = 6;
+            return room < own || n < 0 ? 0 : n;
+        };
+        // two CTAs per SM if three stages (or all there are) fit, so that the next launch of a chain finds room beside this one
+        const int half = stages(kHalfSmem), full = stages(kMaxSmem);
+        const bool two = half >= 3 || (half >= 1 && half == want);
+        p.n_stages = two ? half : full;
+        p.scratch = p.n_stages * p.stage_bytes + behind;
+        if (p.scratch < own) p.scratch = own;
+        const bool fits = p.n_stages >= 2 || (p.n_stages == 1 && want == 1);
+        if (p.splits == 1) return fits;
+        if (fits && (!joint || tiles <= cluster_room(p.splits, two))) return true;
+    }
 }
 
-// The pair shape, from 257 tokens on.
+// The pair shape for more than 256 tokens, and for more than 128 unless the product is small enough for four parts of K and the
+// ranks low (us, few / many, 200 tokens: 2048 -> 2048 rank 16 22 / 28, 2048 -> 5632 rank 16 41 / 29, 5632 -> 2048 rank 64
+// 50 / 50, adapters alone 2048 -> 2048 rank 64 116 / 33; at 300 tokens 31 / 27, 42 / 30, 74 / 48, 117 / 32).
 bool use_many(const ProjectArgs& p)
 {
     const char* f = getenv("PROJECT_SHAPE");
-    if (f) return f[0] == 'm' && p.T > 128;
-    return p.T > kMTile;
+    if (f) return f[0] == 'm';
+    if (p.T <= kTok) return false;
+    return p.T > kMTile || !p.w || p.rank > 32 || 4 * div_up(p.N, kPN) * div_up(p.T, kTok) > 148;
 }
 
 // Tile sizes, and for few tokens the shape of project_kernel.  Whether u comes out of the same pass (fused): where all
@@ -1131,25 +1246,48 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
             return cudaErrorInvalidValue;
         ProjectArgs q = p;
         // K is cut into as many parts as there are SMs for the token tiles, of two slices at least; then the chunks of a
-        // tile's adapters go to CTAs of their own as long as there are SMs, and are walked over beyond that
+        // tile's adapters go to CTAs of their own as long as there are SMs, and are walked over beyond that.  Beside a product of
+        // many tokens the SMs that count are those that the product leaves: it starts on the others at once and needs u only
+        // at the end of its first tiles (4096 tokens, 5632 -> 2048: 32 CTAs on all of K instead of 128 on quarters).
+        int sms = 148;
+        if (many && p.w) {
+            const int busy = 2 * div_up(p.N, kMTile) * div_up(p.T, kMTile);
+            sms = busy > 148 - 36 ? 36 : 148 - busy;
+        }
         q.u_splits = 1;
-        while (q.u_splits < 8 && m_tiles * q.u_splits * 2 <= 148 && q.ksteps / (q.u_splits * 2) >= 2) q.u_splits *= 2;
-        const int cols = m_tiles == 1 ? kUCols / 2 : kUCols;      // (one tile: shorter chunks, a load of A's rows is issued per adapter)
-        q.slots = cols / p.rank > 0 ? cols / p.rank : 1;
+        while (q.u_splits < (m_tiles == 1 ? 8 : 4) && m_tiles * q.u_splits * 2 <= sms && q.ksteps / (q.u_splits * 2) >= 2) q.u_splits *= 2;
+        // (chunks of 64 columns: with one tile they are more CTAs, with many the ring has more stages for x, which is what is read)
+        q.slots = 64 / p.rank > 0 ? 64 / p.rank : 1;
         const int most = p.T < kTok ? p.T : kTok;
-        int chunks = div_up(most < p.n_adapters ? most : p.n_adapters, q.slots);
-        const int room = 148 / (m_tiles * q.u_splits);
-        if (chunks > room) chunks = room < 1 ? 1 : room;
-        q.stage_bytes = p.a_bytes + (q.slots * p.rank > 64 ? kUCols : 64) * kBK * 2;
+        const int all = div_up(most < p.n_adapters ? most : p.n_adapters, q.slots);      // chunks that a tile may have
+        // (beyond rank 64 one accumulator takes all columns, and one lane issues the MMAs)
+        q.lanes = q.slots * p.rank <= kUCols / 2 ? 2 : 1;
         // shared memory: the ring, and the sums of a_rows tokens twice (sent and received); at high ranks fewer parts, then fewer stages
         size_t sums;
         for (;; q.u_splits /= 2) {
             q.u_own = (div_up(p.a_rows, q.u_splits) + 3) & ~3;
-            sums = (size_t)q.u_splits * (q.u_own + 4) * p.rank * sizeof(float) * (q.u_splits > 1 ? 2 : 1);
+            sums = (size_t)q.u_splits * (q.u_own + 1) * p.rank * sizeof(float) * (q.u_splits > 1 ? 2 : 1);
+            // two slices per stage where a CTA has many: its lanes wait and commit half as often
+            q.kb = div_up(q.ksteps, q.u_splits) >= 16 ? 2 : 1;
+            q.stage_bytes = q.kb * (p.a_bytes + (q.lanes == 2 ? kUCols / 2 : kUCols) * kBK * 2);
+            if (2 * q.stage_bytes + behind + sums + 1024 > kMaxSmem && q.kb == 2) { q.kb = 1; q.stage_bytes /= 2; }
             if (q.u_splits == 1 || 2 * q.stage_bytes + behind + sums + 1024 <= kMaxSmem) break;
         }
-        q.n_stages = (int)((kMaxSmem - 1024 - behind - sums) / q.stage_bytes);
-        if (q.n_stages > 4) q.n_stages = 4;
+        // two CTAs per SM where four stages (or all of a chunk, two at least) fit
+        const int per_chunk = div_up(div_up(q.ksteps, q.u_splits), q.kb);
+        auto fit = [&](int bytes) { const int n = (bytes - 1024 - behind - (int)sums) / q.stage_bytes; return n < 0 ? 0 : (n > kMaxStages ? kMaxStages : n); };
+        const bool two = fit(kHalfSmem) >= (per_chunk < 2 ? 2 : (per_chunk < 4 ? per_chunk : 4));
+        q.n_stages = two ? fit(kHalfSmem) : fit(kMaxSmem);
+        // chunks with CTAs of their own: as many as run at once
+        int room = q.u_splits > 1 ? cluster_room(q.u_splits, two) : 148 * (two ? 2 : 1);
+        if (room > sms / q.u_splits) room = sms / q.u_splits;
+        room /= m_tiles;
+        const int chunks = all < room ? all : (room < 1 ? 1 : room);
+        const int steps = per_chunk * div_up(all, chunks);
+        if (q.n_stages > steps) q.n_stages = steps;
+        // (an even number where the ring wraps: a stage then belongs to the same loading and issuing lanes every time around.  With
+        // an odd one they would take turns on its barriers, and a lane that is ahead could take an older phase for its own.)
+        if (q.n_stages < steps) q.n_stages &= ~1;
         q.scratch = q.n_stages * q.stage_bytes + behind;
         cfg.attrs[1].val.clusterDim.z = q.u_splits;
         cfg.numAttrs = q.u_splits > 1 ? 2 : 1;
@@ -1158,6 +1296,7 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
         e = cudaLaunchKernelEx(&cfg, adapter_kernel, q, um);
         if (e != cudaSuccess) return e;
         attr[1].val.clusterDim.z = 1;
+
     }
     if (many) {
         cudaError_t e = allow_smem(project_many_kernel, m_ok);
@@ -1171,10 +1310,12 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
             return cudaErrorInvalidValue;
         const int u_tiles = adapters ? 2 * div_up(p.rank, kBK) : 0;              // 32 KB up to rank 64, 64 KB beyond
         p.n_stages = u_tiles > 2 ? kMStages - 1 : kMStages;
+        size_t behind_ring = (size_t)u_tiles * kUTile;
+        if (behind_ring < kOutStage) behind_ring = kOutStage;
         const int tiles = div_up(p.N, kMTile) * div_up(p.T, kMTile), pairs = tiles < 74 ? tiles : 74;
         attr[1].val.clusterDim.x = 2;
         cfg.gridDim = dim3(2 * pairs); cfg.blockDim = dim3(kMThreads); cfg.numAttrs = 2;
-        cfg.dynamicSmemBytes = (size_t)p.n_stages * kMStageBytes + (size_t)u_tiles * kUTile + 1024;
+        cfg.dynamicSmemBytes = (size_t)p.n_stages * kMStageBytes + behind_ring + 1024;
         return cudaLaunchKernelEx(&cfg, project_many_kernel, p, mm);
     }
     PMaps pm;
@@ -1185,7 +1326,7 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
     cfg.gridDim = dim3(n_tiles * p.splits, m_tiles); cfg.blockDim = dim3(kPThreads);
     cfg.dynamicSmemBytes = (size_t)p.scratch + p.sums_bytes + 1024;
     attr[1].val.clusterDim.x = p.splits;
-    cfg.numAttrs = p.splits > 1 ? 2 : 1;
+    cfg.numAttrs = p.splits > 1 && (p.w || fused) ? 2 : 1;
     cudaError_t e = fused ? allow_smem(project_kernel<true>, f_ok) : allow_smem(project_kernel<false>, p_ok);
     if (e != cudaSuccess) return e;
     return fused ? cudaLaunchKernelEx(&cfg, project_kernel<true>, p, pm) : cudaLaunchKernelEx(&cfg, project_kernel<false>, p, pm);

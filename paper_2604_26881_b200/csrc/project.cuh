@@ -27,6 +27,7 @@ struct ProjectArgs {
     int u_splits;                   // parts of K of the first product (a cluster)
     int ksteps, splits, n_stages, stage_bytes, a_bytes, a_rows;
     int u_own;                      // tokens of a tile that one CTA of such a cluster adds up
+    int kb, lanes;                  // first product: slices of 64 per stage, lanes that issue MMAs
     int u_rows;                     // most rows of A that the tokens may need (fused)
     int scratch;                    // bytes of the ring (or of the sums put together in it) in front of the sums received
     int sums_bytes;                 // of the sums received

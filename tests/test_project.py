@@ -162,6 +162,15 @@ def test_long_batches_and_long_sums():
 
 
 @gpu
+@pytest.mark.parametrize("rank", [16, 40, 64, 72, 128])
+def test_rings_that_wrap_many_times(rank):
+    """Long sums over K in one CTA, at every ring depth that the rank leaves room for, with several chunks of adapters."""
+    for T, n in ((140, 16), (128, 40), (257, 3), (640, 16)):
+        check(T, 5632, 200, rank=rank, n=n, layout="ragged")
+        check(T, 2048, 130, rank=rank, n=n, layout="uniform", weight=False, base=True)
+
+
+@gpu
 @pytest.mark.parametrize("T", [20, 130, 300, 900])
 def test_one_tenants_numbers_do_not_reach_another(T):
     """Infinities and NaN in one adapter, in one token, in one row of w: they stay in their tokens and columns."""
