@@ -17,9 +17,11 @@
 //   - neighbours of the result that are closer than the error bound of key and 32-bit value, and are not the same pair
 //     (z, b), are put in order by their 64-bit values, one candidate per lane (in_order64); where the groups are that close, the
 //     groups' scores are taken in 64 bits (keep64).
-// Bound by instruction issue: see launch_gate for the counts and times.
+// Bound by instruction issue and, for few tokens, by the length of one token's chain, not by the logits' bytes (16384 x 256 in
+// fp32 are 2.7 us of HBM time): about 870 instructions per token with 256 experts in groups with a bias (gate_kernel), 470 in
+// gate_many_kernel.  One token: 2.0 us, 32 tokens of the widest rule 3.0 us, both launch and latency; more at launch_gate.
+// With random logits about 3 % of the tokens of that rule have neighbours that the keys leave undecided.
 #include <float.h>
-#include <stdlib.h>
 
 #include "gate.cuh"
 
@@ -65,7 +67,7 @@ __device__ __forceinline__ float load_logit(const GateArgs& p, int t, int e)
 // sigmoid(z) = exp(min(z, 0) - ref) / (1 + exp(-|z|)) for ref = 0; another ref scales it by exp(-ref) without underflow
 __device__ __forceinline__ float sigmoid_from(float z, float ref)
 {
-    return expf(fminf(z, 0.f) - ref) / (1.f + expf(-fabsf(z)));
+    return __fdividef(expf(fminf(z, 0.f) - ref), 1.f + expf(-fabsf(z)));
 }
 __device__ __forceinline__ double sigmoid64(double z)
 {
@@ -240,7 +242,7 @@ struct Gate {
     //   sigmoid: the exponential below 2^-21 + 2^-24 |z| relative, times s (1 - s) <= 1/4, and a reciprocal of 1 ulp: below 4e-7;
     // twice that for two, with room.  Ordered by logits the values are exact (1e-37: the key of a denormal has cleared bits too).
     static constexpr float kSlack = !BIAS ? 1e-37f : (SIGMOID ? 2e-6f : 4e-6f);
-    static constexpr float kScoreSlack = SIGMOID ? 2e-6f : 4e-6f;
+    static constexpr __device__ float score_slack() { return SIGMOID ? 2e-6f : 4e-6f; }
     // the cleared bits of two keys (32 C ulp each at most) and the rounding of s + b
     static constexpr float kRel = 2.f * 32 * C / 8388608.f + 5e-7f;
 
@@ -309,7 +311,7 @@ __device__ __forceinline__ void write_token(const GateArgs& p, int t, int lane, 
         float sum = s;
 #pragma unroll
         for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
-        w = sum > 0.f ? s / sum * p.scale : 0.f;
+        w = sum > 0.f ? s * (p.scale / sum) : 0.f;
     } else {
         if (my_z != -INFINITY) s = SIGMOID ? sigmoid_from(my_z, 0.f) : expf(my_z - zmax) * inv_sum;
         w = s * p.scale;
@@ -318,6 +320,59 @@ __device__ __forceinline__ void write_token(const GateArgs& p, int t, int lane, 
         p.topk_idx[(size_t)t * p.k + lane] = bad ? lane : my_e;
         p.topk_w[(size_t)t * p.k + lane] = bad ? 0.f : w;
     }
+}
+
+// a lane's share of a row of logits (as they are) and of biases, with vector loads where the rows allow them
+template <int C>
+__device__ __forceinline__ void load_logits(const GateArgs& p, int t, int lane, int held, float (&z)[C])
+{
+    if (p.vec && held == C) {
+        if (p.bf16_logits) {
+            const bf16* src = (const bf16*)p.logits + (size_t)t * p.ld + lane * C;
+            uint32_t h[C / 2];
+            if constexpr (C == 8) { const uint4 q = *reinterpret_cast<const uint4*>(src); h[0] = q.x; h[1] = q.y; h[2] = q.z; h[3] = q.w; }
+            else if constexpr (C == 4) { const uint2 q = *reinterpret_cast<const uint2*>(src); h[0] = q.x; h[1] = q.y; }
+            else h[0] = *reinterpret_cast<const uint32_t*>(src);
+#pragma unroll
+            for (int i = 0; i < C; ++i) z[i] = __uint_as_float(i & 1 ? h[i / 2] & 0xffff0000u : h[i / 2] << 16);
+        } else {
+            const float* src = (const float*)p.logits + (size_t)t * p.ld + lane * C;
+            if constexpr (C >= 4) {
+#pragma unroll
+                for (int i = 0; i < C; i += 4) {
+                    const float4 q = *reinterpret_cast<const float4*>(src + i);
+                    z[i] = q.x; z[i + 1] = q.y; z[i + 2] = q.z; z[i + 3] = q.w;
+                }
+            } else {
+                const float2 q = *reinterpret_cast<const float2*>(src);
+                z[0] = q.x; z[1] = q.y;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < C; ++i) z[i] = i < held ? load_logit(p, t, lane * C + i) : -INFINITY;
+    }
+}
+template <int C>
+__device__ __forceinline__ void load_bias(const GateArgs& p, const float* bias, int lane, int held, float (&b)[C])
+{
+    if (p.vec_bias && held == C) {
+        if constexpr (C >= 4) {
+#pragma unroll
+            for (int i = 0; i < C; i += 4) {
+                const float4 q = __ldg(reinterpret_cast<const float4*>(bias + lane * C + i));
+                b[i] = q.x; b[i + 1] = q.y; b[i + 2] = q.z; b[i + 3] = q.w;
+            }
+        } else {
+            const float2 q = __ldg(reinterpret_cast<const float2*>(bias + lane * C));
+            b[0] = q.x; b[1] = q.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < C; ++i) b[i] = i < held ? __ldg(bias + lane * C + i) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i) b[i] = clean_bias(b[i]);
 }
 
 // One token by one warp; row: scratch of 32 C doubles.
@@ -335,55 +390,12 @@ __device__ __forceinline__ void gate_token(const GateArgs& p, int t, int lane, d
         if (model < 0 || model >= p.M) model = 0;
     }
     const float* bias = BIAS ? p.bias + (size_t)model * p.E : nullptr;
-
-    // the logits and biases of this lane's experts (vector loads where the rows allow them)
-    float z[C], b[C];
     const int held = min(max(p.E - lane * C, 0), C);          // experts of this lane
-    if (p.vec && held == C) {
-        if (p.bf16_logits) {
-            const bf16* src = (const bf16*)p.logits + (size_t)t * p.ld + lane * C;
-            uint32_t h[C / 2];
-            if constexpr (C == 8) *reinterpret_cast<uint4*>(h) = *reinterpret_cast<const uint4*>(src);
-            else if constexpr (C == 4) *reinterpret_cast<uint2*>(h) = *reinterpret_cast<const uint2*>(src);
-            else h[0] = *reinterpret_cast<const uint32_t*>(src);
+    float z[C], b[C];
+    load_logits<C>(p, t, lane, held, z);
+    if (BIAS) load_bias<C>(p, bias, lane, held, b);
 #pragma unroll
-            for (int i = 0; i < C; ++i) z[i] = __uint_as_float(i & 1 ? h[i / 2] & 0xffff0000u : h[i / 2] << 16);
-        } else {
-            const float* src = (const float*)p.logits + (size_t)t * p.ld + lane * C;
-            if constexpr (C >= 4) {
-#pragma unroll
-                for (int i = 0; i < C; i += 4) {
-                    const float4 q = *reinterpret_cast<const float4*>(src + i);
-                    z[i] = q.x; z[i + 1] = q.y; z[i + 2] = q.z; z[i + 3] = q.w;
-                }
-            } else {
-                const float2 q = *reinterpret_cast<const float2*>(src);
-                z[0] = q.x; z[1] = q.y;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < C; ++i) z[i] = clean(z[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < C; ++i) z[i] = i < held ? load_logit(p, t, lane * C + i) : -INFINITY;
-    }
-    if constexpr (BIAS) {
-        if (p.vec_bias && held == C) {
-            if constexpr (C >= 4) {
-#pragma unroll
-                for (int i = 0; i < C; i += 4) {
-                    const float4 q = __ldg(reinterpret_cast<const float4*>(bias + lane * C + i));
-                    b[i] = q.x; b[i + 1] = q.y; b[i + 2] = q.z; b[i + 3] = q.w;
-                }
-            } else {
-                const float2 q = __ldg(reinterpret_cast<const float2*>(bias + lane * C));
-                b[0] = q.x; b[1] = q.y;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < C; ++i) b[i] = i < held ? __ldg(bias + lane * C + i) : 0.f;
-        }
-    }
+    for (int i = 0; i < C; ++i) z[i] = clean(z[i]);
     // scores: softmax needs the maximum and the sum of the whole row; sigmoids only if they are compared
     float zmax = 0.f, inv_sum = 0.f;
     constexpr float kLog2e = 1.4426950408889634f;
@@ -414,7 +426,7 @@ __device__ __forceinline__ void gate_token(const GateArgs& p, int t, int lane, d
         for (int i = 0; i < C; ++i) sc[i] = 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < C; ++i) v[i] = BIAS ? sc[i] + clean_bias(b[i]) : z[i];
+    for (int i = 0; i < C; ++i) v[i] = BIAS ? sc[i] + b[i] : z[i];
 
     uint32_t key[C];
 #pragma unroll
@@ -469,7 +481,7 @@ __device__ __forceinline__ void gate_token(const GateArgs& p, int t, int lane, d
             // the last kept against the best dropped group (a largest logit is exact: nothing to ask)
             const float lo = key_value(__reduce_min_sync(kFull, in ? gkey : kFull));
             const float hi = key_value(__reduce_max_sync(kFull, in ? 0u : gkey));
-            undecided = !(lo - hi > (sums ? 2.f : 1.f) * G::kScoreSlack + 1e-6f * (fabsf(lo) + fabsf(hi)));
+            undecided = !(lo - hi > (sums ? 2.f : 1.f) * G::score_slack() + 1e-6f * (fabsf(lo) + fabsf(hi)));
             if (undecided) kept = keep64<C, SIGMOID, BIAS>(p, t, bias, row);
         }
         if (p.lanes_per_group) {
@@ -550,7 +562,7 @@ __device__ __noinline__ void gate_token_again(const GateArgs& p, int t, int lane
 // of a token go over its experts in blocks of 32 (lane r: experts 32 b + 16 h + 4 r + i), sort the eight of a block with the
 // network, read the block's two largest off its top, and merge block after block into a list of the eight largest (pairwise
 // maxima of one list and the other reversed are a bitonic sequence with the eight largest of both); two more merges join the
-// four lanes.  The largest of what the merges drop is rank 9.  Groups are runs of whole blocks.  All loads of a token are in
+// four lanes.  The two largest of what the merges drop are ranks 9 and 10.  Groups are runs of whole blocks.  All loads of a token are in
 // flight at once; its logits, then its sorted blocks, wait in shared memory at places that only their lane touches, so
 // that the blocks can be a short loop.
 template <int NB, bool SIGMOID, bool BIAS, bool GROUPS>
@@ -638,7 +650,7 @@ gate_many_kernel(const GateArgs p)
         inv_sum = sum > 0.f ? 1.f / sum : 0.f;
     }
 
-    uint32_t list[8], dropped = 0;
+    uint32_t list[8], dropped = 0, dropped2 = 0;              // the eight largest, and the next two
 #pragma unroll
     for (int i = 0; i < 8; ++i) list[i] = 0u;
     auto merge = [&](const uint32_t (&other)[8]) {
@@ -648,7 +660,13 @@ gate_many_kernel(const GateArgs p)
             d[i] = min(list[i], other[7 - i]);
             list[i] = max(list[i], other[7 - i]);
         }
-        dropped = max(dropped, max(max(max(d[0], d[1]), max(d[2], d[3])), max(max(d[4], d[5]), max(d[6], d[7]))));
+        auto top2 = [](uint32_t& a, uint32_t& b, uint32_t c, uint32_t e) { b = max(min(a, c), max(b, e)); a = max(a, c); };
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) { const uint32_t x = max(d[i], d[i + 1]); d[i + 1] = min(d[i], d[i + 1]); d[i] = x; }
+        top2(d[0], d[1], d[2], d[3]);
+        top2(d[4], d[5], d[6], d[7]);
+        top2(d[0], d[1], d[4], d[5]);
+        top2(dropped, dropped2, d[0], d[1]);
         auto cs = [&](int i, int j) { const uint32_t x = max(list[i], list[j]), y = min(list[i], list[j]); list[i] = x; list[j] = y; };
         cs(0, 4); cs(1, 5); cs(2, 6); cs(3, 7); cs(0, 2); cs(1, 3); cs(4, 6); cs(5, 7); cs(0, 1); cs(2, 3); cs(4, 5); cs(6, 7);
     };
@@ -712,6 +730,7 @@ gate_many_kernel(const GateArgs p)
         // lane r scores the groups r, r + 4 of its token and counts the better ones
         const int groups = p.n_groups;                        // at most 8
         float score[2], big = 0.f;
+        uint32_t best[2], second[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int g = r + 4 * h;
@@ -722,6 +741,7 @@ gate_many_kernel(const GateArgs p)
                     c = max(min(a, q.x), max(c, q.y));
                     a = max(a, q.x);
                 }
+            best[h] = a; second[h] = c;
             score[h] = g < groups ? key_value(a) + (top2 ? key_value(c) : 0.f) : -INFINITY;
             if (g < groups) big = fmaxf(big, fabsf(key_value(a)) + fabsf(key_value(c)));
         }
@@ -750,7 +770,56 @@ gate_many_kernel(const GateArgs p)
             big = fmaxf(big, __shfl_xor_sync(kFull, big, o));
         }
         // (scores are sums of values read off keys; bf16 logits lose nothing there)
-        unsure = (BIAS || !p.bf16_logits) && !(lo - hi > (top2 ? 2.f : 1.f) * G::kSlack + G::kRel * big);
+        const bool close = (BIAS || !p.bf16_logits) && !(lo - hi > (top2 ? 2.f : 1.f) * G::kSlack + G::kRel * big);
+        if (!SIGMOID && BIAS) unsure = close;                 // (a softmax in 64 bits needs the whole row)
+        if ((SIGMOID || !BIAS) && __any_sync(kFull, close)) {
+            // The groups' scores in 64 bits, from the group's best (two); a group with a further expert that close to them
+            // sends the token through gate_token.
+            bool more = false;
+            double part[2][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int g = r + 4 * h;
+                const bool here = g < groups && live;
+                if (here) {
+                    const float least = key_value(top2 ? second[h] : best[h]);
+                    const uint32_t edge = order_key(least - (G::kSlack + G::kRel * fabsf(least)));
+                    int near = 0;
+                    for (int o = 0; o < run; ++o)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {         // the four lanes' eight keys of the block
+                            const uint4 k4 = reinterpret_cast<const uint4*>(&s_z[warp][2 * (g * run + o) + (i >> 2)][(lane & ~3) + (i & 3)])[0];
+                            near += (k4.x >= edge) + (k4.y >= edge) + (k4.z >= edge) + (k4.w >= edge);
+                        }
+                    more |= near > (top2 ? 2 : 1);
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int e = (int)(kIdMask - ((j ? second[h] : best[h]) & kIdMask));
+                    const bool on = here && (j == 0 || top2);
+                    const double z = on ? load_logit(p, t, e) : 0.f;
+                    part[h][j] = BIAS ? sigmoid64(z) + (double)(on ? clean_bias(__ldg(bias + e)) : 0.f) : z;
+                    if (!on) part[h][j] = 0.;
+                }
+            }
+            const double exact[2] = {r < groups ? part[0][0] + part[0][1] : -INFINITY, r + 4 < groups ? part[1][0] + part[1][1] : -INFINITY};
+            int rank[2] = {0, 0};
+#pragma unroll
+            for (int o = 0; o < 8; ++o) {
+                const double other = __shfl_sync(kFull, o < 4 ? exact[0] : exact[1], (lane & ~3) | (o & 3));
+                if (o < groups) {
+                    rank[0] += other > exact[0] || (other == exact[0] && o < r);
+                    rank[1] += other > exact[1] || (other == exact[1] && o < r + 4);
+                }
+            }
+            uint32_t again = (r < groups && rank[0] < p.keep ? 1u << r : 0u) | (r + 4 < groups && rank[1] < p.keep ? 16u << r : 0u);
+#pragma unroll
+            for (int o = 1; o <= 2; o <<= 1) {
+                again |= __shfl_xor_sync(kFull, again, o);
+                more |= __shfl_xor_sync(kFull, (int)more, o) != 0;
+            }
+            if (close) { kept = again; unsure = more; }
+        }
         const int shift = 31 - __clz(run);
 #pragma unroll 1
         for (int b = 0; b < blocks; ++b) {
@@ -769,45 +838,59 @@ gate_many_kernel(const GateArgs p)
         uint32_t other[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) other[i] = __shfl_xor_sync(kFull, list[i], o);
-        dropped = max(dropped, __shfl_xor_sync(kFull, dropped, o));
+        {
+            const uint32_t od = __shfl_xor_sync(kFull, dropped, o), od2 = __shfl_xor_sync(kFull, dropped2, o);
+            dropped2 = max(min(dropped, od), max(dropped2, od2));
+            dropped = max(dropped, od);
+        }
         merge(other);
     }
 
-    // neighbours that the keys do not tell apart: inside the choice they are put in order below, at its end gate_token does it
+    // Neighbours that the keys do not tell apart are put in order below, in 64 bits, the first rank behind the choice among them;
+    // if the one behind that is as close, gate_token does it.
     const int k = p.k;
     bool mixed = false;
     if (BIAS || !p.bf16_logits) {
-        float f[9];
+        float f[10];
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] = key_value(list[j]);
         f[8] = key_value(dropped);
-        const int last = p.eligible > k ? k : k - 1;
+        f[9] = key_value(dropped2);
+        const int last = min(k + 1, p.eligible - 1);          // the last rank looked at, from 0
         float least = f[0];
 #pragma unroll
-        for (int j = 1; j < 9; ++j) if (j == last) least = f[j];
+        for (int j = 1; j < 10; ++j) if (j == last) least = f[j];
         const float need = G::kSlack + G::kRel * fmaxf(fabsf(f[0]), fabsf(least));        // (sorted: the largest magnitude is at an end)
+        bool edge = false, behind = false;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool near = !(f[j] - f[j + 1] > need);
+        for (int j = 0; j < 9; ++j) {
+            const bool near = j + 1 <= last && !(f[j] - f[j + 1] > need);
             if (j + 1 < k) mixed |= near;
-            if (j + 1 == k && p.eligible > k) unsure |= near;
+            if (j + 1 == k) edge = near;
+            if (j == k) behind = near;
         }
+        mixed |= edge;
+        unsure |= edge && behind;
         if (!SIGMOID && BIAS && mixed) unsure = true;         // (a softmax in 64 bits needs the whole row)
     }
 
-    // lane r has ranks 2 r and 2 r + 1
+    // lane r has ranks 2 r and 2 r + 1 (and every lane the first rank behind the eight)
     const uint32_t k0 = r == 0 ? list[0] : r == 1 ? list[2] : r == 2 ? list[4] : list[6], k1 = r == 0 ? list[1] : r == 1 ? list[3] : r == 2 ? list[5] : list[7];
-    const int e0 = (int)(kIdMask - (k0 & kIdMask)), e1 = (int)(kIdMask - (k1 & kIdMask));
-    const bool on0 = live && 2 * r < k, on1 = live && 2 * r + 1 < k;
-    const float z0 = on0 ? load_logit(p, t, e0) : -INFINITY, z1 = on1 ? load_logit(p, t, e1) : -INFINITY;
-    int at0 = 2 * r, at1 = 2 * r + 1;
+    const int e0 = (int)(kIdMask - (k0 & kIdMask)), e1 = (int)(kIdMask - (k1 & kIdMask)), e8 = (int)(kIdMask - (dropped & kIdMask));
+    const int ranks = min(k + 1, p.eligible);                 // ranks that may take part in the order
+    bool on0 = live && 2 * r < k, on1 = live && 2 * r + 1 < k;
+    float z0 = live && 2 * r < ranks ? load_logit(p, t, e0) : -INFINITY, z1 = live && 2 * r + 1 < ranks ? load_logit(p, t, e1) : -INFINITY;
+    int at0 = 2 * r, at1 = 2 * r + 1, at8 = 8;
+    float z8 = -INFINITY;
     if (__any_sync(kFull, mixed && !unsure)) {
-        double v0 = z0, v1 = z1;
+        if (live && ranks > 8) z8 = load_logit(p, t, e8);
+        double v0 = z0, v1 = z1, v8 = z8;
         if (BIAS) {
-            v0 = on0 ? sigmoid64(z0) + (double)clean_bias(__ldg(bias + e0)) : 0.;
-            v1 = on1 ? sigmoid64(z1) + (double)clean_bias(__ldg(bias + e1)) : 0.;
+            v0 = live && 2 * r < ranks ? sigmoid64(z0) + (double)clean_bias(__ldg(bias + e0)) : 0.;
+            v1 = live && 2 * r + 1 < ranks ? sigmoid64(z1) + (double)clean_bias(__ldg(bias + e1)) : 0.;
+            v8 = live && ranks > 8 ? sigmoid64(z8) + (double)clean_bias(__ldg(bias + e8)) : 0.;
         }
-        int n0 = 0, n1 = 0;
+        int n0 = 0, n1 = 0, n8 = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -815,35 +898,51 @@ gate_many_kernel(const GateArgs p)
                 const int from = (lane & ~3) | q;
                 const double ov = __shfl_sync(kFull, h ? v1 : v0, from);
                 const int oe = __shfl_sync(kFull, h ? e1 : e0, from);
-                if (2 * q + h < k) {
+                if (2 * q + h < ranks) {
                     n0 += ov > v0 || (ov == v0 && oe < e0);
                     n1 += ov > v1 || (ov == v1 && oe < e1);
+                    n8 += ov > v8 || (ov == v8 && oe < e8);
                 }
             }
-        if (mixed) { at0 = n0; at1 = n1; }
+        if (ranks > 8) {
+            n0 += v8 > v0 || (v8 == v0 && e8 < e0);
+            n1 += v8 > v1 || (v8 == v1 && e8 < e1);
+        }
+        if (mixed) {
+            at0 = n0; at1 = n1; at8 = n8;
+            on0 = live && 2 * r < ranks && n0 < k;
+            on1 = live && 2 * r + 1 < ranks && n1 < k;
+        }
     }
+    const bool on8 = mixed && live && ranks > 8 && at8 < k && r == 0;     // (rank 9 has moved up: lane 0 writes it)
+    if (!on0) z0 = -INFINITY;
+    if (!on1) z1 = -INFINITY;
+    if (!on8) z8 = -INFINITY;
     {
-        float w0, w1, s0 = 0.f, s1 = 0.f;
+        float w0, w1, w8, s0 = 0.f, s1 = 0.f, s8 = 0.f;
         if (p.renormalize) {
-            float top = fmaxf(z0, z1);
+            float top = fmaxf(fmaxf(z0, z1), z8);
             top = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
             top = fmaxf(top, __shfl_xor_sync(kFull, top, 2));
             const float ref = SIGMOID ? fminf(top, 0.f) : top;
             if (z0 != -INFINITY) s0 = SIGMOID ? sigmoid_from(z0, ref) : expf(z0 - ref);
             if (z1 != -INFINITY) s1 = SIGMOID ? sigmoid_from(z1, ref) : expf(z1 - ref);
-            float sum = s0 + s1;
+            if (z8 != -INFINITY) s8 = SIGMOID ? sigmoid_from(z8, ref) : expf(z8 - ref);
+            float sum = s0 + s1 + s8;
             sum += __shfl_xor_sync(kFull, sum, 1);
             sum += __shfl_xor_sync(kFull, sum, 2);
-            w0 = sum > 0.f ? s0 / sum * p.scale : 0.f;
-            w1 = sum > 0.f ? s1 / sum * p.scale : 0.f;
+            const float share = sum > 0.f ? p.scale / sum : 0.f;
+            w0 = s0 * share; w1 = s1 * share; w8 = s8 * share;
         } else {
             if (z0 != -INFINITY) s0 = SIGMOID ? sigmoid_from(z0, 0.f) : expf(z0 - zmax) * inv_sum;
             if (z1 != -INFINITY) s1 = SIGMOID ? sigmoid_from(z1, 0.f) : expf(z1 - zmax) * inv_sum;
-            w0 = s0 * p.scale; w1 = s1 * p.scale;
+            if (z8 != -INFINITY) s8 = SIGMOID ? sigmoid_from(z8, 0.f) : expf(z8 - zmax) * inv_sum;
+            w0 = s0 * p.scale; w1 = s1 * p.scale; w8 = s8 * p.scale;
         }
         const size_t out = (size_t)t * k;
-        if (on0 && !unsure) { p.topk_idx[out + at0] = bad ? 2 * r : e0; p.topk_w[out + at0] = bad ? 0.f : w0; }
-        if (on1 && !unsure) { p.topk_idx[out + at1] = bad ? 2 * r + 1 : e1; p.topk_w[out + at1] = bad ? 0.f : w1; }
+        if (on0 && !unsure) { p.topk_idx[out + at0] = bad ? at0 : e0; p.topk_w[out + at0] = bad ? 0.f : w0; }
+        if (on1 && !unsure) { p.topk_idx[out + at1] = bad ? at1 : e1; p.topk_w[out + at1] = bad ? 0.f : w1; }
+        if (on8 && !unsure) { p.topk_idx[out + at8] = bad ? at8 : e8; p.topk_w[out + at8] = bad ? 0.f : w8; }
     }
     if (p.tie_flag) {
         // neighbours among ranks 1..k+1 closer than 1e-5 relative, in the values that order them (without a bias: the scores)
@@ -853,14 +952,13 @@ gate_many_kernel(const GateArgs p)
             if (BIAS && on) v += clean_bias(__ldg(bias + e));
             return v;
         };
-        const int e8 = (int)(kIdMask - (dropped & kIdMask));
-        const bool on8 = live && k == 8 && p.eligible > 8;
+        const bool has8 = live && k == 8 && p.eligible > 8;
         const bool next0 = live && 2 * r <= k && 2 * r < p.eligible, next1 = live && 2 * r + 1 <= k && 2 * r + 1 < p.eligible;
         const float v0 = value(e0, next0 ? load_logit(p, t, e0) : 0.f, next0), v1 = value(e1, next1 ? load_logit(p, t, e1) : 0.f, next1);
-        const float v8 = value(e8, on8 ? load_logit(p, t, e8) : 0.f, on8);
+        const float v8 = value(e8, has8 ? load_logit(p, t, e8) : 0.f, has8);
         float v2 = __shfl_down_sync(kFull, v0, 1);
         bool has2 = __shfl_down_sync(kFull, (int)next0, 1) != 0;
-        if (r == 3) { v2 = v8; has2 = on8; }
+        if (r == 3) { v2 = v8; has2 = has8; }
         bool near = (next1 && !(v0 - v1 >= 1e-5f * fabsf(v0))) || (next1 && has2 && !(v1 - v2 >= 1e-5f * fabsf(v1)));
         near = near || mixed || unsure;
         const uint32_t any = __ballot_sync(kFull, near);
@@ -911,8 +1009,6 @@ cudaError_t launch_c(const GateArgs& p, dim3 grid, dim3 block, cudaStream_t st)
     }
 }
 
-int many_from() { const char* f = getenv("GATE_MANY"); return f ? atoi(f) : 2048; }
-
 }  // namespace
 
 cudaError_t launch_gate(const GateArgs& in, cudaStream_t st)
@@ -922,14 +1018,19 @@ cudaError_t launch_gate(const GateArgs& in, cudaStream_t st)
     p.group_size = p.E / p.n_groups;
     const size_t esz = p.bf16_logits ? 2 : 4;
     p.eligible = p.keep < p.n_groups ? p.keep * p.group_size : p.E;
-    // Four lanes per token from kManyTokens on, where the groups are runs of 1, 2, 4 or 8 blocks of 32 and compared by what orders
-    // the experts (sums of scores beside an order by logits stay with the other kernel).
+    // Four lanes per token where there are tokens enough for its longer chain, and the groups are runs of 1, 2, 4 or 8 blocks of
+    // 32 compared by what orders the experts (sums of scores beside an order by logits stay with the other kernel).  Measured, one
+    // warp per token / four lanes per token, us: 60 experts, softmax: 4096 tokens 5.4 / 4.8, 8192 8.1 / 5.8, 32768 24 / 11;
+    // 128, sigmoid, bias: 4096 6.6 / 6.1, 8192 10.1 / 7.6, 32768 31 / 15; 128 in 4 groups: 4096 7.1 / 8.3, 8192 10.9 / 9.7;
+    // 256 in 8 groups: 8192 14.8 / 18.0, 16384 25.2 / 24.0, 32768 47 / 38; 256, softmax, bias (ties through gate_token):
+    // 16384 24.8 / 31.1, 32768 45.2 / 44.3.
     const int run = p.group_size / 32;
     const bool blocks = p.keep == p.n_groups || (p.group_size % 32 == 0 && (run & (run - 1)) == 0 && (p.bias || p.group_score == MOE_GROUP_MAX));
+    const int many_from = p.E <= 128 ? 8192 : (p.score == MOE_SCORE_SOFTMAX && p.bias ? 32768 : 16384);
     // groups that fall on whole lanes, a power of two of them, are reduced by shuffles, others through shared memory
     const int lanes = p.group_size / C;
     p.lanes_per_group = p.group_size % C == 0 && (lanes & (lanes - 1)) == 0 ? lanes : 0;
-    if (p.T >= many_from() && blocks) {
+    if (p.T >= many_from && blocks) {
         // (aligned for a lane's eight here and for its C in gate_token)
         p.vec = p.ld % 8 == 0 && (uintptr_t)p.logits % 16 == 0;
         p.vec_bias = (uintptr_t)p.bias % 16 == 0 && p.E % 4 == 0;

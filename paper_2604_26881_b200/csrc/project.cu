@@ -7,7 +7,6 @@
 // the columns of its own adapter.  K is cut over CTAs; the parts of u are stored apart in fp32 and summed in a
 // fixed order by the second launch, which is resident and streams W meanwhile (programmatic dependent launch) and adds
 // u . B^T behind its main loop.
-#include <cstdlib>
 #include <cstring>
 
 #include "project.cuh"
@@ -1184,8 +1183,6 @@ bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind)
 // 50 / 50, adapters alone 2048 -> 2048 rank 64 116 / 33; at 300 tokens 31 / 27, 42 / 30, 74 / 48, 117 / 32).
 bool use_many(const ProjectArgs& p)
 {
-    const char* f = getenv("PROJECT_SHAPE");
-    if (f) return f[0] == 'm';
     if (p.T <= kTok) return false;
     return p.T > kMTile || !p.w || p.rank > 32 || 4 * div_up(p.N, kPN) * div_up(p.T, kTok) > 148;
 }

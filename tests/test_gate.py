@@ -208,6 +208,91 @@ def test_masked_and_extreme_logits(score, renorm):
     check(z, k, score=score, renorm=renorm, bias=bias)
 
 
+def check_repeated(rows, T, k, bias=None, dtype=torch.float32, pad=0, seed=0, **rule):
+    """A long batch: `rows` in random order, many times over.  The reference looks at every row once."""
+    pick = np.random.default_rng(seed).integers(0, len(rows), T)
+    pick[:len(rows)] = np.arange(len(rows))
+    zr = torch.as_tensor(rows, dtype=torch.float64).to(dtype).double().numpy()
+    br = None if bias is None else np.broadcast_to(torch.as_tensor(bias).float().double().numpy().reshape(1, -1), zr.shape)
+    ref_idx, ref_w = reference(zr, k, bias=br, **{**rule, "scale": float(np.float32(rule.get("scale", 1.0)))})
+    idx, w, flag, status = run(rows[pick], k, bias=None if bias is None else np.asarray(bias).reshape(1, -1), dtype=dtype, pad=pad, tie=True, **rule)
+    assert status == 0
+    bad = np.nonzero((idx != ref_idx[pick]).any(1))[0]
+    assert bad.size == 0, f"{bad.size} tokens differ, first {bad[:3]}: got {idx[bad[:3]]}, want {ref_idx[pick[bad[:3]]]}"
+    np.testing.assert_allclose(w, ref_w[pick], rtol=W_RTOL, atol=1e-37)
+    # what a token gets does not depend on the token beside it
+    for i in range(len(rows)):
+        assert len(np.unique(w[pick == i], axis=0)) == 1 and len(set(flag[pick == i])) == 1
+
+
+# batches that four lanes per token work on: from 8192 tokens with up to 128 experts, from 16384 or 32768 beyond
+LONG = [(8192, 60, 4, {}), (8199, 64, 8, {}), (8192, 7, 3, {}), (8193, 1, 1, {}), (8200, 100, 8, {}), (8192, 128, 8, dict(n_groups=4, keep=2)),
+        (8195, 128, 5, dict(n_groups=2, keep=1)), (8192, 96, 8, dict(n_groups=3, keep=2)), (8192, 60, 4, dict(n_groups=4, keep=2)),
+        (8192, 8, 8, {}), (8192, 64, 7, dict(n_groups=2, keep=1)), (16387, 256, 8, {}), (16384, 256, 8, dict(n_groups=8, keep=4)), (16390, 200, 6, {}),
+        (16384, 256, 7, dict(n_groups=4, keep=1)), (16384, 256, 1, dict(n_groups=2, keep=1)), (32768, 256, 8, dict(n_groups=8, keep=3))]
+
+
+@gpu
+@pytest.mark.parametrize("T,E,k,groups", LONG)
+def test_long_batches(T, E, k, groups):
+    g = np.random.default_rng(T + E + k)
+    rows = g.standard_normal((300, E)) * 1.5
+    for score in ("softmax", "sigmoid"):
+        for bias in (None, g.standard_normal(E) * 0.05):
+            for group_score in ("max", "top2") if groups else ("max",):
+                for renorm, dtype, pad in ((True, torch.float32, 0), (False, torch.bfloat16, 8), (True, torch.float32, 3)):
+                    check_repeated(rows, T, k, bias=bias, dtype=dtype, pad=pad, score=score, renorm=renorm, group_score=group_score, **groups)
+
+
+@gpu
+@pytest.mark.parametrize("T,E,groups", [(8192, 60, {}), (8192, 128, dict(n_groups=4, keep=2)), (16384, 256, dict(n_groups=8, keep=4)), (16384, 256, {}),
+                                        (32768, 256, dict(n_groups=2, keep=1))])
+@pytest.mark.parametrize("k", [1, 5, 7, 8])
+def test_long_batches_of_ties_and_near_ties(T, E, groups, k):
+    """Exact ties, values that only 64 bits tell apart, masked and extreme rows, at the k-th rank and between groups."""
+    g = np.random.default_rng(E + k)
+    ties = g.integers(-2, 3, (40, E)).astype(float)
+    near = g.integers(0, 4, (40, E)) * 1e-7
+    ulps = (np.float32(1.5) + g.integers(0, 30, (40, E)) * np.spacing(np.float32(1.5))).astype(float)
+    odd = g.standard_normal((12, E))
+    odd[0] = -np.inf
+    odd[1, 3:] = -np.inf
+    odd[2, ::2] = -FMAX
+    odd[3] = np.nan
+    odd[4, 5] = np.inf
+    odd[5] = 1e30 * np.sign(odd[5])
+    odd[6] -= 200
+    odd[7] *= 1e-42
+    odd[8] = -FMAX
+    odd[9] = 0.0
+    odd[10] += 200
+    rows = np.concatenate([ties, near, ulps, odd])
+    for score in ("softmax", "sigmoid"):
+        for bias in (None, 1.0 + g.integers(0, 3, E) * 2.0 ** -23, np.zeros(E)):
+            for group_score in ("max", "top2") if groups else ("max",):
+                check_repeated(rows, T, k, bias=bias, score=score, renorm=True, group_score=group_score, **groups)
+        check_repeated(ties, T, k, dtype=torch.bfloat16, score=score, **groups)
+
+
+@gpu
+def test_long_batches_of_several_models():
+    g = np.random.default_rng(21)
+    T, E, M, k = 8300, 60, 4, 4
+    z = g.standard_normal((T, E))
+    tenant, mot = g.integers(0, 9, T), np.arange(9) % M
+    tenant[[3, T - 1]] = [9, -2]
+    bias = g.standard_normal((M, E)) * 0.2
+    rule = dict(score="sigmoid", renorm=True)
+    idx, w, _, status = run(z, k, bias=bias, tenant=tenant, mot=mot, **rule)
+    assert status == B.MOE_DEV_BAD_TENANT
+    ok = (tenant >= 0) & (tenant < 9)
+    safe = np.where(ok, tenant, 0)
+    ref_idx, ref_w = reference(z.astype(np.float32).astype(float), k, bias=bias.astype(np.float32).astype(float)[mot[safe]], **rule)
+    assert np.array_equal(idx[ok], ref_idx[ok])
+    np.testing.assert_allclose(w[ok], ref_w[ok], rtol=W_RTOL)
+    assert (idx[~ok] == np.arange(k)).all() and (w[~ok] == 0).all()
+
+
 @gpu
 def test_models_and_bad_tenants():
     g = np.random.default_rng(11)
@@ -318,6 +403,69 @@ def test_layer_with_a_rule(E, M, path):
         # and back: the layer's own rule, the same bits as before
         B.moe_set_gating(gl.ctx, 0, None)
         assert torch.equal(gl.forward(x, tenant, G), before)
+    finally:
+        gl.close()
+
+
+@gpu
+def test_every_call_that_runs_the_layer_uses_the_rule():
+    """Fused dispatch, the timed, host, pipelined and paged calls and the stack: the same bits as the layer call."""
+    T, k = 100, 4
+    wl = W.MoEWorkload("rule", T=T, H=256, E=60, I=128, k=k, Is=128, n_tenants=3, G=3, tenant_layout="uniform")
+    wts = W.make_weights(wl, seed=5)
+    x, tenant, mot = W.make_tokens(wl, seed=5)
+    gl = GpuLayer(wl, [wts], max_tokens=T, model_of_tenant=mot)
+    try:
+        rule = B.moe_gating(score="sigmoid", n_groups=4, keep_groups=2, group_score="max", renormalize=True)
+        bias = (torch.randn(1, 60, generator=torch.Generator().manual_seed(1)) * 0.1).to(gl.dev)
+        plain = gl.forward(x, tenant, 3)
+        B.moe_set_gating(gl.ctx, 0, rule, bias)
+        ref = gl.forward(x, tenant, 3)
+        assert not torch.equal(ref, plain)
+        B.moe_set_option(gl.ctx, B.MOE_OPT_FUSED_DISPATCH, 1)
+        assert torch.equal(gl.forward(x, tenant, 3), ref)
+        B.moe_set_option(gl.ctx, B.MOE_OPT_FUSED_DISPATCH, 0)
+        assert torch.equal(gl.forward_host(x, tenant, 3), ref.cpu())
+        xd, td, out = x.to(gl.dev), tenant.to(gl.dev), torch.zeros_like(ref)
+        B.moe_layer_forward_timed(gl.ctx, 0, xd, td, T, 3, out)
+        assert torch.equal(out, ref)
+        xh, th, oh = x.pin_memory(), tenant.pin_memory(), torch.zeros_like(x).pin_memory()
+        B.moe_layer_forward_host_wait(gl.ctx, B.moe_layer_forward_host_submit(gl.ctx, 0, xh, th, T, 3, oh))
+        assert torch.equal(oh, ref.cpu())
+        # the stack's one block on inputs that its norm leaves as the layer's tokens
+        sx, dbg_in, dbg_out = xd.clone(), torch.empty(1, T, 256, dtype=torch.bfloat16, device=gl.dev), torch.empty(1, T, 256, dtype=torch.bfloat16, device=gl.dev)
+        B.moe_stack_forward(gl.ctx, sx, td, T, 3, dbg_layer_inputs=dbg_in, dbg_layer_outputs=dbg_out)
+        o = torch.zeros_like(ref)
+        B.moe_layer_forward(gl.ctx, 0, dbg_in[0], td, T, 3, o)
+        d = (sx.double() - (xd.double() + o.double())).abs()                   # (the stack rounds once, this sum twice)
+        assert (d <= 2.0 ** -8 * (o.double().abs() + sx.double().abs()) + 1e-30).all()
+        # paged residency: routes by the rule, then pages in what the rule chose
+        host = [wts[n].pin_memory() for n in ("pool_gate", "pool_up", "pool_down")]
+        pool = [torch.zeros_like(h, device=gl.dev) for h in host]
+        B.moe_residency_enable(gl.ctx, 0, *host, *pool)
+        out.zero_()
+        B.moe_layer_forward_paged(gl.ctx, 0, xd, td, T, 3, out)
+        assert torch.equal(out, ref)
+    finally:
+        gl.close()
+
+
+@gpu
+def test_a_layers_rule_is_its_own():
+    """Two layers, a rule in the second only; a layer index or a rule that does not fit is refused and changes nothing."""
+    wl = W.MoEWorkload("two", T=40, H=256, E=12, I=128, k=2, Is=128, n_tenants=2, G=3, n_layers=2)
+    wts = [W.make_weights(wl, seed=6, layer=i) for i in range(2)]
+    x, tenant, mot = W.make_tokens(wl, seed=6)
+    gl = GpuLayer(wl, wts, max_tokens=40, model_of_tenant=mot)
+    try:
+        a0, a1 = gl.forward(x, tenant, 3, 0), gl.forward(x, tenant, 3, 1)
+        B.moe_set_gating(gl.ctx, 1, B.moe_gating(score="sigmoid", renormalize=True))
+        assert torch.equal(gl.forward(x, tenant, 3, 0), a0) and not torch.equal(gl.forward(x, tenant, 3, 1), a1)
+        for layer, rule in ((2, B.moe_gating()), (-1, None), (0, B.moe_gating(n_groups=5)), (0, B.moe_gating(n_groups=12, keep_groups=1))):
+            with pytest.raises(B.MoeError) as e:
+                B.moe_set_gating(gl.ctx, layer, rule)
+            assert e.value.status == B.MOE_ERR_SHAPE
+        assert torch.equal(gl.forward(x, tenant, 3, 0), a0)
     finally:
         gl.close()
 
