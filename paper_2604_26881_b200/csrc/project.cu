@@ -612,6 +612,7 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
     int r[4], c[4], a[4];
     bool on[4];
     uint4 bq[4][2];
+    float at_base[4];
     auto pick = [&](int e0) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -620,6 +621,11 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
             c[q] = e - r[q] * nc;
             on[q] = e < total && n0 + c0 + c[q] < p.N;
             a[q] = on[q] && adapters ? adapter[r[q]] : -1;
+            at_base[q] = 0.f;
+            if (on[q] && p.base) {
+                const size_t at = (size_t)(t0 + r[q]) * p.ldbase + n0 + c0 + c[q];
+                at_base[q] = p.out_f32 ? ((const float*)p.base)[at] : __bfloat162float(((const bf16*)p.base)[at]);
+            }
         }
     };
     auto load_b = [&](int i) {                             // vectors i and i + 1 of the four rows of B
@@ -691,13 +697,9 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
                 if (!on[q]) continue;
                 const size_t row = t0 + r[q];
                 const int n = n0 + c0 + c[q];
-                if (p.out_f32) {
-                    if (p.base) v[q] += ((const float*)p.base)[row * p.ldbase + n];
-                    ((float*)p.out)[row * p.ldo + n] = v[q];
-                } else {
-                    if (p.base) v[q] += __bfloat162float(((const bf16*)p.base)[row * p.ldbase + n]);
-                    ((bf16*)p.out)[row * p.ldo + n] = __float2bfloat16_rn(v[q]);
-                }
+                v[q] += at_base[q];
+                if (p.out_f32) ((float*)p.out)[row * p.ldo + n] = v[q];
+                else ((bf16*)p.out)[row * p.ldo + n] = __float2bfloat16_rn(v[q]);
             }
         }
     }
@@ -813,10 +815,24 @@ struct Block {
                 if (t + r < p.T) *reinterpret_cast<uint4*>((T*)p.out + (size_t)(t + r) * p.ldo + n + c) = o;
             }
         } else if (n + lane < p.N) {
-            for (int r = 0; r < 32 && t + r < p.T; ++r) {
-                float v = stage[r * kOutPitch + lane];
-                if (p.base) v += (float)((const T*)p.base)[(size_t)(t + r) * p.ldbase + n + lane];
-                ((T*)p.out)[(size_t)(t + r) * p.ldo + n + lane] = (T)v;
+            // rows that are not on 16-byte boundaries: a row's 32 columns at a time, eight rows' bases on their way at once
+            T* out = (T*)p.out + (size_t)t * p.ldo + n + lane;
+            const float* from = stage + lane;
+            const int rows = min(32, p.T - t);
+            if (p.base) {
+                const T* base = (const T*)p.base + (size_t)t * p.ldbase + n + lane;
+#pragma unroll 1
+                for (int r0 = 0; r0 < rows; r0 += 8) {
+                    T b[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) if (r0 + i < rows) b[i] = base[i * p.ldbase];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) if (r0 + i < rows) out[i * p.ldo] = (T)(from[i * kOutPitch] + (float)b[i]);
+                    base += 8 * p.ldbase; out += 8 * p.ldo; from += 8 * kOutPitch;
+                }
+            } else {
+#pragma unroll 8
+                for (int r = 0; r < rows; ++r, out += p.ldo, from += kOutPitch) *out = (T)*from;
             }
         }
     }
@@ -1178,13 +1194,23 @@ bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind)
     }
 }
 
-// The pair shape for more than 256 tokens, and for more than 128 unless the product is small enough for four parts of K and the
-// ranks low (us, few / many, 200 tokens: 2048 -> 2048 rank 16 22 / 28, 2048 -> 5632 rank 16 41 / 29, 5632 -> 2048 rank 64
-// 50 / 50, adapters alone 2048 -> 2048 rank 64 116 / 33; at 300 tokens 31 / 27, 42 / 30, 74 / 48, 117 / 32).
+// Which shape, by what either was measured to cost (us): the pair shape some 18 and 0.33 per slice of K and round of tiles;
+// the other 8 and, half as much again as its parts alone, 0.4 per slice and 9e-5 per product of the adapters on a thread's
+// CUDA core.  (few / many: 2048 -> 2048, rank 16: 140 tokens 20 / 28, 256 25 / 28, 300 31 / 27, 1024 47 / 23; 2048 -> 5632:
+// 140 tokens 41 / 29; 5632 -> 2048, rank 64: 140 tokens 50 / 49, 300 74 / 48; 512 -> 512: 140 tokens 17 / 24, 1024 19 / 18.)
+// Up to 128 tokens the pair shape only pays for high ranks of few adapters (2048 -> 2048, rank 64, 2 adapters: 32 tokens
+// 20 / 19, 128 tokens 48 / 20; 32 adapters: 64 tokens 30 / 53).
 bool use_many(const ProjectArgs& p)
 {
-    if (p.T <= kTok) return false;
-    return p.T > kMTile || !p.w || p.rank > 32 || 4 * div_up(p.N, kPN) * div_up(p.T, kTok) > 148;
+    if (p.T <= kTok) return p.T > 32 && p.rank >= 48 && p.n_adapters > 0 && p.n_adapters <= 4;
+    const int steps = p.w ? div_up(p.K, kBK) : 0, tiles = div_up(p.N, kPN) * div_up(p.T, kTok);
+    int parts = tiles > 0 ? 148 / tiles : 1;
+    if (parts > 8) parts = 8;
+    if (p.w && parts > steps / 2) parts = steps / 2;
+    if (parts < 1) parts = 1;
+    const int rounds = div_up(div_up(p.N, kMTile) * div_up(p.T, kMTile), 74), waves = div_up(tiles * parts, 148);
+    const float few = 8.f + 1.5f * waves * (0.4f * steps / parts + 9e-5f * kTok * kPN / parts * (p.n_adapters > 0 ? p.rank : 0));
+    return 18.f + 0.33f * steps * rounds < few;
 }
 
 // Tile sizes, and for few tokens the shape of project_kernel.  Whether u comes out of the same pass (fused): where all
