@@ -2,11 +2,12 @@
 //
 //   out[t] = base[t] + x[t] . W^T + scale[a] * (x[t] . A[a]^T) . B[a]^T,     a = adapter of token t's tenant
 //
-// Two launches.  The first computes u[t] = scale[a] * x[t] . A[a]^T (adapter_kernel): per 128 tokens the distinct adapters
-// are listed, their rows are gathered by TMA as the N operand of one tcgen05.mma per 16 elements of K, and each token keeps
-// the columns of its own adapter.  K is cut over CTAs; the parts of u are stored apart in fp32 and summed in a
-// fixed order by the second launch, which is resident and streams W meanwhile (programmatic dependent launch) and adds
-// u . B^T behind its main loop.
+// u[t] = scale[a] * x[t] . A[a]^T, the first product, comes from a launch of its own (adapter_kernel): per 128 tokens the
+// distinct adapters are listed, their rows are gathered by TMA as the N operand of one tcgen05.mma per 16 elements of K, and
+// each token keeps the columns of its own adapter; K is cut over the CTAs of a cluster, which add up their parts in a fixed
+// order.  The projection (project_kernel for few tokens, project_many_kernel for many) is resident and streams W meanwhile
+// (programmatic dependent launch) and adds u . B^T behind its main loop.  With few tokens of few adapters it computes u
+// itself, in the same pass over x, and there is one launch only.
 #include <cstring>
 
 #include "project.cuh"
@@ -1144,6 +1145,8 @@ int cluster_room(int size, bool two)
     if (size < 2 || size > 8 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return size == 1 ? 148 * (two ? 2 : 1) : 0;
     int& n = room[dev][size][two];
     if (n == 0) {
+        static bool allowed[kMaxDevices] = {false};
+        if (allow_smem(project_kernel<false>, allowed) != cudaSuccess) cudaGetLastError();      // (the query asks for that much)
         cudaLaunchConfig_t cfg;
         memset(&cfg, 0, sizeof(cfg));
         cudaLaunchAttribute attr;
