@@ -337,7 +337,7 @@ typedef struct {
  *                a bias in s), or 32 bits could not decide the choice
  *   status_out   device int32 or NULL: MOE_DEV_BAD_TENANT is OR-ed into it for a tenant id outside [0, n_tenants) (the
  *                token gets experts 0..k-1 with weight 0); the caller clears it
- * 1 <= E <= 256, 1 <= k <= min(E, 8).  One launch, no workspace; results do not depend on what else runs.
+ * 1 <= E <= 256, 1 <= k <= min(E, 8).  T = 0: nothing is done and the pointers may be NULL.  One launch, no workspace; results do not depend on what else runs.
  */
 int moe_gate(const void* logits, int logits_type, int64_t ld, int T, int E, int k, const moe_gating* rule,
              const float* balance_bias, const int32_t* tenant_id, const int32_t* model_of_tenant, int n_tenants, int M,
@@ -362,7 +362,7 @@ int moe_set_gating(moe_ctx* ctx, int layer, const moe_gating* rule, const float*
  *   q_scale = s                         f32 [T] with group = 0 (one scale per row), f32 [T, ceil(H/128)] with group = 128
  * Rows of every matrix are ld_* >= H elements apart; ld_* of a NULL matrix is not looked at.  At least one output.
  * 1 <= H <= 16384.  Any alignment of whole elements; rows on 16-byte boundaries are fastest.  A row with an infinity or
- * a NaN makes its own outputs NaN (or 0), no other row's.
+ * a NaN makes its own outputs NaN (or 0), no other row's.  T = 0: nothing is done and the pointers may be NULL.
  */
 int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld_residual, const void* weight, float eps,
                     int T, int H, void* residual_out, int64_t ld_residual_out, void* out, int64_t ld_out, void* out_q,
@@ -384,8 +384,9 @@ int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld
  *          MOE_DEV_TIMEOUT are OR-ed into it; the caller clears it
  * n_adapters = 0: no adapters; a, b, scale, tenant_id, adapter_of_tenant and n_tenants are not looked at.
  * K a multiple of 8; rank a multiple of 8 up to 128 (adapters of a smaller rank are padded with zeros); ldx and ldw multiples
- * of 8; x, w, a and b 16-byte aligned; T <= 2^22.  out may not overlap x, w, a or b.  The results depend on the shapes, not
- * on what else runs: the sums have a fixed order.
+ * of 8; x, w, a and b 16-byte aligned; T <= 2^22; K, N and n_adapters * rank <= 2^30.  out may not overlap x, w, a or b.  T = 0:
+ * nothing is done and the pointers may be NULL.  The results depend on the shapes, not on what else runs: the sums have a
+ * fixed order.
  */
 int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, int K, int N, const void* a, const void* b,
                 const float* scale, int n_adapters, int rank, const int32_t* tenant_id, const int32_t* adapter_of_tenant,

@@ -362,6 +362,10 @@ def moe_gate(logits, rule, topk_idx, topk_w, *, balance_bias=None, tenant_id=Non
 def moe_set_gating(ctx, layer, rule, balance_bias=None):
     """Makes the layer choose its experts by `rule` (None: moe_route's own rule).  balance_bias [M, E] float32 on the device is
     used in place: keep it alive."""
+    if isinstance(balance_bias, torch.Tensor) and not (balance_bias.is_cuda and balance_bias.dtype == torch.float32 and
+                                                       balance_bias.is_contiguous()):
+        raise ValueError("moe_set_gating: balance_bias must be contiguous float32 on the device, "
+                         f"not {balance_bias.dtype} on {balance_bias.device}")
     _check("moe_set_gating", load_library().moe_set_gating(ctx, layer, byref(rule) if rule is not None else None, _ptr(balance_bias)))
 
 

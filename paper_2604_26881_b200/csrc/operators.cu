@@ -11,6 +11,7 @@ namespace {
 
 constexpr int kMaxRows = 1 << 28;
 constexpr int kProjectMaxTokens = 1 << 22;
+constexpr int kProjectMaxDim = 1 << 30;      // K, N, and the rows of all adapters' A
 
 bool off(const void* p, size_t align) { return ((uintptr_t)p & (align - 1)) != 0; }
 
@@ -86,8 +87,8 @@ int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld
 
 int64_t moe_project_workspace(int T, int K, int N, int rank, int n_adapters)
 {
-    if (T < 0 || T > kProjectMaxTokens || K < 1 || N < 1 || n_adapters < 0) return MOE_ERR_SHAPE;
-    if (n_adapters > 0 && (rank < 1 || rank > kAdapterMaxRank)) return MOE_ERR_SHAPE;
+    if (T < 0 || T > kProjectMaxTokens || K < 1 || K > kProjectMaxDim || N < 1 || N > kProjectMaxDim || n_adapters < 0) return MOE_ERR_SHAPE;
+    if (n_adapters > 0 && (rank < 1 || rank > kAdapterMaxRank || n_adapters > kProjectMaxDim / rank)) return MOE_ERR_SHAPE;
     return project_workspace(T, K, N, rank, n_adapters);
 }
 
@@ -97,10 +98,11 @@ int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, i
                 int64_t workspace_bytes, int32_t* status_out, void* stream)
 {
     const bool adapters = n_adapters > 0;
-    if (T < 0 || T > kProjectMaxTokens || K < 1 || N < 1 || n_adapters < 0 || ld_out < N || (base && ld_base < N)) return MOE_ERR_SHAPE;
+    if (T < 0 || T > kProjectMaxTokens || K < 1 || K > kProjectMaxDim || N < 1 || N > kProjectMaxDim || n_adapters < 0) return MOE_ERR_SHAPE;
+    if (ld_out < N || (base && ld_base < N)) return MOE_ERR_SHAPE;
     if ((w || adapters) && ldx < K) return MOE_ERR_SHAPE;
     if (w && ldw < K) return MOE_ERR_SHAPE;
-    if (adapters && (rank < 1 || rank > kAdapterMaxRank || n_tenants < 1)) return MOE_ERR_SHAPE;
+    if (adapters && (rank < 1 || rank > kAdapterMaxRank || n_adapters > kProjectMaxDim / rank || n_tenants < 1)) return MOE_ERR_SHAPE;
     if (out_type != MOE_TYPE_F32 && out_type != MOE_TYPE_BF16) return MOE_ERR_UNSUPPORTED;
     // the operands travel as TMA tiles: rows on 16-byte boundaries
     if (K % 8 || ((w || adapters) && ldx % 8) || (w && ldw % 8) || (adapters && rank % 8)) return MOE_ERR_UNSUPPORTED;

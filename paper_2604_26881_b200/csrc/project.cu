@@ -727,6 +727,7 @@ constexpr int kMStages = 5;
 constexpr int kMStageBytes = 2 * kTok * kBK * 2;       // 16 KB of tokens, 16 KB of weight rows per CTA
 constexpr int kMTile = 256;
 constexpr int kMThreads = 480;                         // warp 0: TMA (weights), 1: MMA, 2..9: epilogue, 10: TMA (tokens), 11..14: u
+constexpr int kBRows = kTok / 2;                       // rows of an adapter's B in one load
 constexpr int kUTile = kTok * kBK * 2;                 // one bf16 tile of 64 columns of u
 
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y)
@@ -902,7 +903,7 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
         for (int s = 0; s < n_stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(bar_tfull + 8 * b, 1); mbar_init(bar_tempty + 8 * b, 2 * 8); }
         mbar_init(bar_ufull, 1);
-        mbar_init(bar_uempty, 1);
+        mbar_init(bar_uempty, 3);                           // the tile's MMAs, and both loading lanes: nobody needs its list any more
         mbar_init(bar_list, 4);
         mbar_init(bar_staged, 8);
         s_abort = 0;
@@ -923,8 +924,9 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
     pdl_launch_dependents();
 
     if (warp == 0 || warp == 10) {
-        // ---- TMA: one lane for the weight rows (and the adapters' B), one for the tokens; a lane needs about 430 cycles per
-        // stage (140 for a load, 290 for the barrier), the MMAs of a stage 512
+        // ---- TMA: one lane for the weight rows, one for the tokens; a lane needs about 430 cycles per stage (140 for a load,
+        // 290 for the barrier), the MMAs of a stage 512.  Of the adapters' B each loads half of the rows, so that neither lane
+        // can fall a turn of the ring behind the other and take a later phase of a barrier for its own.
         if (lane == 0) {
             uint32_t stage = 0, phase = 0, armed = 0, armed_phase = 0;
             bool ok = true;
@@ -968,9 +970,13 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
                         }
                     } else if (ks < steps) {
                         tma_load_2d_pair(sa, &maps.x, full, ks * kBK, t0);
+                    } else {
+                        const int j = (ks - steps) / chunks, c = (ks - steps) - j * chunks;
+                        tma_load_3d_pair(sa + (kTok + kBRows) * kBK * 2, &maps.b, full, c * kBK, n0 + kBRows, s_al.list[j]);
                     }
                     if (++stage == (uint32_t)n_stages) { stage = 0; phase ^= 1; }
                 }
+                if (ok && adapters) mbar_arrive(bar_uempty);
             }
             if (!ok && leader && warp == 0) {               // gave up: the copies in flight land before the block exits
                 for (int s = 0; s < n_stages; ++s)
@@ -1101,14 +1107,14 @@ bool make_map_ld(CUtensorMap* m, const void* base, uint64_t rows, uint64_t k, ui
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// 3-D map over n matrices [N][rank] (the adapters' B; u's two halves); box = 64 x 128 rows of one matrix
-bool make_map_3d(CUtensorMap* m, const void* base, uint64_t n, uint64_t N, uint64_t rank)
+// 3-D map over n matrices [N][rank] (the adapters' B; u's two halves); box = 64 x box_rows of one matrix
+bool make_map_3d(CUtensorMap* m, const void* base, uint64_t n, uint64_t N, uint64_t rank, uint32_t box_rows)
 {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[3] = {rank, N, n};
     cuuint64_t strides[2] = {rank * 2, N * rank * 2};
-    cuuint32_t box[3] = {(cuuint32_t)kBK, (cuuint32_t)kTok, 1};
+    cuuint32_t box[3] = {(cuuint32_t)kBK, box_rows, 1};
     cuuint32_t estr[3] = {1, 1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -1132,6 +1138,13 @@ cudaError_t allow_smem(K kern, bool (&done)[kMaxDevices])
 }
 
 int div_up(int a, int b) { return (a + b - 1) / b; }
+
+// tiles of `tile` tokens x `tile` columns (of sizes that no memory holds, which only a question for the workspace can have: many)
+int tiles_of(const ProjectArgs& p, int tile)
+{
+    const int64_t n = (int64_t)div_up(p.N, tile) * div_up(p.T, tile);
+    return n < (1 << 24) ? (int)n : 1 << 24;
+}
 
 constexpr int kHalfSmem = 108 * 1024;      // dynamic shared memory up to which two CTAs share an SM
 
@@ -1168,7 +1181,8 @@ int cluster_room(int size, bool two)
 // that the MMA of a short token tile may read.
 bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind)
 {
-    const int tiles = div_up(p.N, kPN) * div_up(p.T, kTok), pitch = p.a_rows + 4;
+    static_assert(kPN == kTok, "");
+    const int tiles = tiles_of(p, kPN), pitch = p.a_rows + 4;
     const bool joint = p.w || fused;                        // (otherwise the parts only share the columns)
     p.stage_bytes = p.a_bytes + (p.w ? kPN * kBK * 2 : 0) + ((u_rows + 15) & ~15) * kBK * 2;
     // as many parts as there are SMs for the tiles (a cluster holds eight), of two slices at least, all clusters at once
@@ -1206,12 +1220,12 @@ bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind)
 bool use_many(const ProjectArgs& p)
 {
     if (p.T <= kTok) return p.T > 32 && p.rank >= 48 && p.n_adapters > 0 && p.n_adapters <= 4;
-    const int steps = p.w ? div_up(p.K, kBK) : 0, tiles = div_up(p.N, kPN) * div_up(p.T, kTok);
+    const int steps = p.w ? div_up(p.K, kBK) : 0, tiles = tiles_of(p, kPN);
     int parts = tiles > 0 ? 148 / tiles : 1;
     if (parts > 8) parts = 8;
     if (p.w && parts > steps / 2) parts = steps / 2;
     if (parts < 1) parts = 1;
-    const int rounds = div_up(div_up(p.N, kMTile) * div_up(p.T, kMTile), 74), waves = div_up(tiles * parts, 148);
+    const int rounds = div_up(tiles_of(p, kMTile), 74), waves = div_up(tiles * parts, 148);
     const float few = 8.f + 1.5f * waves * (0.4f * steps / parts + 9e-5f * kTok * kPN / parts * (p.n_adapters > 0 ? p.rank : 0));
     return 18.f + 0.33f * steps * rounds < few;
 }
@@ -1277,7 +1291,7 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
         // at the end of its first tiles (4096 tokens, 5632 -> 2048: 32 CTAs on all of K instead of 128 on quarters).
         int sms = 148;
         if (many && p.w) {
-            const int busy = 2 * div_up(p.N, kMTile) * div_up(p.T, kMTile);
+            const int busy = 2 * tiles_of(p, kMTile);
             sms = busy > 148 - 36 ? 36 : 148 - busy;
         }
         q.u_splits = 1;
@@ -1332,13 +1346,13 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
         if (!p.w) p.ksteps = 0;
         if (p.w && (!make_map_ld(&mm.x, p.x, p.T, p.K, p.ldx, kTok) || !make_map_ld(&mm.w, p.w, p.N, p.K, p.ldw, kTok)))
             return cudaErrorInvalidValue;
-        if (adapters && (!make_map_3d(&mm.b, p.b, p.n_adapters, p.N, p.rank) || !make_map_3d(&mm.u, p.u, 2, p.T, p.rank)))
+        if (adapters && (!make_map_3d(&mm.b, p.b, p.n_adapters, p.N, p.rank, kBRows) || !make_map_3d(&mm.u, p.u, 2, p.T, p.rank, kTok)))
             return cudaErrorInvalidValue;
         const int u_tiles = adapters ? 2 * div_up(p.rank, kBK) : 0;              // 32 KB up to rank 64, 64 KB beyond
         p.n_stages = u_tiles > 2 ? kMStages - 1 : kMStages;
         size_t behind_ring = (size_t)u_tiles * kUTile;
         if (behind_ring < kOutStage) behind_ring = kOutStage;
-        const int tiles = div_up(p.N, kMTile) * div_up(p.T, kMTile), pairs = tiles < 74 ? tiles : 74;
+        const int tiles = tiles_of(p, kMTile), pairs = tiles < 74 ? tiles : 74;
         attr[1].val.clusterDim.x = 2;
         cfg.gridDim = dim3(2 * pairs); cfg.blockDim = dim3(kMThreads); cfg.numAttrs = 2;
         cfg.dynamicSmemBytes = (size_t)p.n_stages * kMStageBytes + behind_ring + 1024;

@@ -532,5 +532,7 @@ def test_binding_checks_tensors():
         B.moe_gate(z, rule, idx, w, balance_bias=torch.zeros(1, 7))
     with pytest.raises(ValueError):
         B.moe_gate(z, rule, idx, w, tenant_id=torch.zeros(4))
+    with pytest.raises(ValueError):
+        B.moe_set_gating(None, 0, rule, torch.zeros(1, 8))
     with pytest.raises(KeyError):
         B.moe_gating(score="tanh")

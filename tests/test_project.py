@@ -171,6 +171,31 @@ def test_rings_that_wrap_many_times(rank):
 
 
 @gpu
+@pytest.mark.parametrize("weight", [True, False])
+def test_tiles_of_one_run_with_all_none_and_hundreds_of_adapters(weight):
+    """More tiles than run at once; neighbouring runs of 256 tokens have 1, 0, about 200 and 3 adapters, so the loops over a tile's
+    adapters are of very different lengths one after the other."""
+    T, K, N, rank, n = 8192 - 5, 64, 1024, 16, 300
+    d = inputs(T, K, N, rank, n, 11, weight=weight, base=not weight, out=torch.float32)
+    rng = np.random.default_rng(5)
+    adapter = np.full(T, -1, dtype=np.int32)
+    for i in range(0, T, 256):
+        m, kind = min(256, T - i), (i // 256) % 4
+        adapter[i:i + m] = {0: rng.integers(0, n), 1: -1, 2: rng.integers(0, n, m), 3: rng.integers(0, 3, m)}[kind]
+    tenant = torch.from_numpy(np.where(adapter < 0, n, adapter).astype(np.int32))           # (tenant n has no adapter)
+    y, err = reference(d["x"], d["w"], d["base"], d["a"], d["b"], d["scale"], torch.from_numpy(adapter).long())
+    g = {k: None if v is None else v.to(DEV) for k, v in d.items()}
+    outs = [torch.empty(T, N, device=DEV) for _ in range(3)]
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for o in outs:
+        B.moe_project(g["x"], g["w"], o, base=g["base"], a=g["a"], b=g["b"], scale=g["scale"], tenant_id=tenant.to(DEV), n_tenants=n + 1, status_out=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    assert ((outs[0].double().cpu() - y).abs() <= err + 1e-30).all()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@gpu
 @pytest.mark.parametrize("T", [20, 130, 300, 900])
 def test_one_tenants_numbers_do_not_reach_another(T):
     """Infinities and NaN in one adapter, in one token, in one row of w: they stay in their tokens and columns."""
@@ -312,7 +337,8 @@ def test_refusals_need_no_gpu():
         assert _raw(**bad) == B.MOE_ERR_NULL, bad
     for bad in (dict(T=-1), dict(T=(1 << 22) + 1), dict(K=0), dict(N=0), dict(n=-1), dict(ldx=56), dict(ldw=56), dict(ldo=31), dict(base=256, ldb=31), dict(rank=0),
                 dict(rank=136), dict(n_tenants=0), dict(x=264), dict(w=264), dict(a=264), dict(b=260), dict(scale=258), dict(tenant=258), dict(table=258),
-                dict(out=258), dict(out=257, out_type=1), dict(base=258, ldb=32), dict(ws=128), dict(status=258)):
+                dict(out=258), dict(out=257, out_type=1), dict(K=(1 << 30) + 8, ldx=1 << 31, ldw=1 << 31), dict(N=(1 << 30) + 1, ldo=1 << 31),
+                dict(n=1 << 28), dict(base=258, ldb=32), dict(ws=128), dict(status=258)):
         assert _raw(**bad) == B.MOE_ERR_SHAPE, bad
     for bad in (dict(K=60), dict(ldx=68), dict(ldw=68), dict(rank=12), dict(out_type=2)):
         assert _raw(**bad) == B.MOE_ERR_UNSUPPORTED, bad
@@ -322,6 +348,8 @@ def test_refusals_need_no_gpu():
     assert lib.moe_project_workspace(-1, 64, 32, 8, 1) == B.MOE_ERR_SHAPE
     assert lib.moe_project_workspace(4, 64, 32, 129, 1) == B.MOE_ERR_SHAPE
     assert lib.moe_project_workspace(4, 64, 0, 8, 1) == B.MOE_ERR_SHAPE
+    assert lib.moe_project_workspace(4, 64, 32, 8, 1 << 28) == B.MOE_ERR_SHAPE
+    assert lib.moe_project_workspace(1 << 22, 64, 1 << 30, 8, 1) == 8 * 4 << 22          # (no overflow on the way)
     assert lib.moe_project_workspace(4, 64, 32, 0, 0) == 0
     assert lib.moe_project_workspace(1, 2048, 2048, 16, 3) == 0               # one pass, no workspace
     assert lib.moe_project_workspace(1000, 2048, 2048, 16, 3) == 1000 * 16 * 4
