@@ -50,6 +50,8 @@ __device__ __forceinline__ void send_bulk(uint32_t dst, uint32_t src, uint32_t b
                  ::"r"(dst), "r"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+// (nothing that was written before is handed over: only that this CTA has come so far)
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync_all()
@@ -82,61 +84,66 @@ __device__ __forceinline__ int adapter_of(const ProjectArgs& p, int t, bool repo
 }
 
 // The distinct adapters of a tile of 32 * G tokens, in the order of their first token; four warps work on it, warp w on the
-// groups of 32 tokens w and w + 4.  `sync` is a barrier of (at least) those warps.
+// groups of 32 tokens w and w + 4.  `sync` is a barrier of (at least) those warps.  Every token looks for the first one with its
+// adapter by comparing with all earlier ones, four at a time: no step depends on how many there are or whose turn it is
+// (walks along lists of the adapters found so far took up to 1 us).
 template <int G>
 struct AdapterList {
-    int adapter[32 * G];        // of every token, -1: none
+    alignas(16) int adapter[32 * G];    // of every token, -1: none
     int list[32 * G];
-    int candidate[32 * G];      // per group: its distinct adapters
-    int n_candidates[G], n_new[G];
+    uint32_t fresh[G];                  // the tokens that are the first with their adapter
     int count;
 };
 template <int G, typename Sync>
 __device__ __forceinline__ void list_adapters(const ProjectArgs& p, AdapterList<G>& s, int t0, int w, int lane, bool report, Sync sync, int (&slot)[G / 4])
 {
-    uint32_t same[G / 4], fresh[G / 4];
-    bool lead[G / 4];
+    int a[G / 4], first[G / 4];
 #pragma unroll
     for (int i = 0; i < G / 4; ++i) {
         const int g = w + 4 * i, t = t0 + g * 32 + lane;
-        const int a = t < p.T ? adapter_of(p, t, report) : -1;
-        s.adapter[g * 32 + lane] = a;
-        same[i] = __match_any_sync(kFull, a);
-        lead[i] = a >= 0 && lane == __ffs(same[i]) - 1;
-        const uint32_t c = __ballot_sync(kFull, lead[i]);
-        if (lead[i]) s.candidate[g * 32 + __popc(c & ((1u << lane) - 1))] = a;
-        if (lane == 0) s.n_candidates[g] = __popc(c);
+        a[i] = t < p.T ? adapter_of(p, t, report) : -1;
+        s.adapter[g * 32 + lane] = a[i];
+        first[i] = g * 32 + __ffs(__match_any_sync(kFull, a[i])) - 1;
     }
     sync();
 #pragma unroll
     for (int i = 0; i < G / 4; ++i) {
-        const int g = w + 4 * i, a = s.adapter[g * 32 + lane];
-        bool first = lead[i];                               // (of the tile: no earlier group has it)
-        for (int h = 0; h < g && first; ++h)
-            for (int j = 0; j < s.n_candidates[h] && first; ++j) first = s.candidate[h * 32 + j] != a;
-        fresh[i] = __ballot_sync(kFull, first);
-        if (lane == 0) s.n_new[g] = __popc(fresh[i]);
+        const int g = w + 4 * i;
+        for (int h = g - 1; h >= 0; --h) {
+#pragma unroll
+            for (int q = 7; q >= 0; --q) {
+                const int4 v = reinterpret_cast<const int4*>(s.adapter)[h * 8 + q];
+                const int at = h * 32 + q * 4;
+                if (v.w == a[i]) first[i] = at + 3;
+                if (v.z == a[i]) first[i] = at + 2;
+                if (v.y == a[i]) first[i] = at + 1;
+                if (v.x == a[i]) first[i] = at;
+            }
+        }
+        const uint32_t fresh = __ballot_sync(kFull, a[i] >= 0 && first[i] == g * 32 + lane);
+        if (lane == 0) s.fresh[g] = fresh;
     }
     sync();
-    int at = 0;
+    uint32_t fresh[G];
+    int count = 0;
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-#pragma unroll
-        for (int i = 0; i < G / 4; ++i)
-            if (g == w + 4 * i && (fresh[i] >> lane & 1)) s.list[at + __popc(fresh[i] & ((1u << lane) - 1))] = s.adapter[g * 32 + lane];
-        at += s.n_new[g];
+    for (int h = 0; h < G; ++h) {
+        fresh[h] = s.fresh[h];
+        count += __popc(fresh[h]);
     }
-    if (w == 0 && lane == 0) s.count = at;
-    sync();
-    // every token's place in the list: its group's first token of the adapter looks it up
 #pragma unroll
     for (int i = 0; i < G / 4; ++i) {
-        const int a = s.adapter[(w + 4 * i) * 32 + lane];
-        int j = -1;
-        if (lead[i]) for (j = 0; s.list[j] != a; ++j) {}
-        slot[i] = __shfl_sync(kFull, j, __ffs(same[i]) - 1);
-        if (a < 0) slot[i] = -1;
+        int at = 0;
+#pragma unroll
+        for (int h = 0; h < G; ++h) {
+            const int d = first[i] - 32 * h;                // (bits of the group that are before the first token)
+            at += __popc(d >= 32 ? fresh[h] : (d > 0 ? fresh[h] & ((1u << d) - 1) : 0u));
+        }
+        slot[i] = a[i] >= 0 ? at : -1;
+        if (a[i] >= 0 && first[i] == (w + 4 * i) * 32 + lane) s.list[at] = a[i];
     }
+    if (w == 0 && lane == 0) s.count = count;
+    sync();
 }
 
 struct UMaps { CUtensorMap x, a; };
@@ -154,6 +161,7 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
     __shared__ int s_abort;
     __shared__ AdapterList<4> s_al;
     __shared__ int s_slot[kTok];
+    __shared__ int s_mine[kTok];            // the token's adapter is in a chunk of this CTA
     __shared__ float s_scale[kTok];
     const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * kMaxStages, bar_done = bar_full + 16 * kMaxStages,
                    bar_free = bar_done + 8, bar_list = bar_done + 16, bar_got = bar_done + 24;
@@ -294,6 +302,7 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
         __all_sync(kFull, know_list());
         // thread <-> token; a warp reads the TMEM lanes of its quarter
         const int quarter = warp & 3, row = quarter * 32 + lane, my_slot = s_slot[row];
+        s_mine[row] = my_slot >= 0 && (my_slot / p.slots) % gridDim.y == blockIdx.y;
         s_scale[row] = my_slot >= 0 && p.scale ? p.scale[s_al.adapter[row]] : 1.f;
         float* const dst = sums + (row / own) * block + row % own;
         int it = 0;
@@ -344,14 +353,15 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
             }
             mbar_wait(bar_got, 0, &s_abort, status);
             __syncwarp();
-            cluster_arrive();                   // (waited for below: nobody leaves while its copies may still be on their way)
+            cluster_arrive_relaxed();           // (waited for below: nobody leaves while its copies may still be on their way)
         }
         // this CTA adds up its share of the tokens over the parts, in their order
         if (!s_abort) {
-            const int pairs = p.rank >> 1;                   // two columns at a time
-            for (int e = threadIdx.x; e < own * pairs; e += kUThreads) {
-                const int r = e / pairs, c = 2 * (e - r * pairs), row = own * blockIdx.z + r, slot = s_slot[row];
-                if (slot < 0 || (slot / p.slots) % gridDim.y != blockIdx.y) continue;
+            const int pairs = p.rank >> 1, at_once = kUThreads / pairs;      // a thread adds two columns, of every at_once-th token
+            const int r0 = threadIdx.x / pairs, c = 2 * (threadIdx.x - r0 * pairs);
+            for (int r = r0; r0 < at_once && r < own; r += at_once) {
+                const int row = own * blockIdx.z + r;
+                if (row >= kTok || !s_mine[row]) continue;
                 float v = 0.f, w = 0.f;
                 for (int z = 0; z < p.u_splits; ++z) {
                     v += got[z * block + c * pitch + r];
@@ -452,6 +462,10 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
     if (FUSED || !adapters) pdl_wait();
     pdl_launch_dependents();
 
+    if (!FUSED && adapters && warp >= 2 && warp < 6) {
+        const int row = (warp & 3) * 32 + lane;
+        s_adapter[row] = row < rows ? adapter_of(p, t0 + row, false) : -1;
+    }
     const int ks_n = product || FUSED ? p.ksteps : 0;
     const int k0 = (int)((long long)ks_n * rank / S), k1 = (int)((long long)ks_n * (rank + 1) / S);
     if (k1 > k0) {
@@ -528,8 +542,8 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
                 }
                 __all_sync(kFull, mbar_wait(bar_list, 0, &s_abort, status));
                 a = s_al.adapter[row];
-            } else if (adapters) {
-                a = row < rows ? adapter_of(p, t0 + row, false) : -1;
+            } else if (adapters && half == 0) {
+                a = s_adapter[row];
             }
             if (adapters && half == 0) {
                 // The rows of the adapters' B that this CTA will multiply come into L2 while the product runs; every token asks for
@@ -577,8 +591,8 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
             }
         }
     }
+    __syncthreads();
     if (joint) {
-        __syncthreads();
         cluster_wait();
         if (warp == 0) {
             // every CTA gets its columns of the product, and (fused) u whole
@@ -593,20 +607,8 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
             }
         }
     }
-    if (!FUSED && adapters) {
-        pdl_wait();                                        // u
-        for (int i = threadIdx.x; i < rows; i += kPThreads) s_adapter[i] = adapter_of(p, t0 + i, false);
-        // (rows of tokens without an adapter hold anything and are not looked at)
-        const float* src = p.u + (size_t)t0 * p.rank;
-        for (int i = threadIdx.x; i < rows * p.rank / 4; i += kPThreads)
-            reinterpret_cast<float4*>(su)[i] = __ldcg(reinterpret_cast<const float4*>(src) + i);
-    }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-
-    // The outputs: four of a thread at a time, so that their loads overlap.  The first rows of B are asked for before the sums
-    // have arrived.
+    // The outputs: four of a thread at a time, so that their loads overlap.  The first rows of B and of the base are asked for
+    // before u and the sums have arrived.
     const int* const adapter = FUSED ? s_al.adapter : s_adapter;
     const int total = rows * nc, vecs = p.rank / 8;
     const float* const got = joint ? part : own;
@@ -639,10 +641,20 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
     };
     pick(threadIdx.x);
     if (adapters) load_b(0);
+    if (!FUSED && adapters) {
+        pdl_wait();                                        // u
+        // (rows of tokens without an adapter hold anything and are not looked at)
+        const float* src = p.u + (size_t)t0 * p.rank;
+        for (int i = threadIdx.x; i < rows * p.rank / 4; i += kPThreads)
+            reinterpret_cast<float4*>(su)[i] = __ldcg(reinterpret_cast<const float4*>(src) + i);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
     if (joint) {
         mbar_wait(bar_got, 0, &s_abort, status);
         __syncwarp();
-        cluster_arrive();                                  // (waited for at the end: nobody leaves while its copies may still be on their way)
+        cluster_arrive_relaxed();                          // (waited for at the end: nobody leaves while its copies may still be on their way)
     }
     if (FUSED) {
         const float* const up = joint ? u_part : own_u;
@@ -1046,7 +1058,17 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
         const int esz = p.out_f32 ? 4 : 2;
         const bool vec = (uintptr_t)p.out % 16 == 0 && p.ldo * esz % 16 == 0 && (!p.base || ((uintptr_t)p.base % 16 == 0 && p.ldbase * esz % 16 == 0));
         float* const stage = reinterpret_cast<float*>(ring_ptr + n_stages * kMStageBytes) + (warp - 2) * 32 * kOutPitch;
-        if (adapters) pdl_wait();
+        if (adapters) {
+            // the base of the first tile comes into L2 while u is being computed (a tile's epilogue of 4 blocks of columns, one
+            // after the other, waits for it otherwise)
+            const int n0 = (pair0 / m_tiles) * kMTile + half * 128, t = (pair0 % m_tiles) * kMTile + (int)rank * kTok + quarter * 32 + lane;
+            if (p.base && t < p.T && n0 < p.N) {
+                const char* row = (const char*)p.base + ((size_t)t * p.ldbase + n0) * esz;
+                const int bytes = min(128, p.N - n0) * esz;
+                for (int b = 0; b < bytes; b += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + b));
+            }
+            pdl_wait();
+        }
         bool ok = true;
         int it = 0;
         for (int tile = pair0; tile < total; tile += pairs, ++it) {
