@@ -1027,7 +1027,9 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
                     const int count = s_al.count;
                     for (int j = 0; j < count && ok; ++j) {
                         // (without the product the first MMA of an adapter overwrites its tokens' lanes)
-                        uint32_t first = acc;
+                        uint32_t first = acc, mask[8];
+#pragma unroll
+                        for (int g = 0; g < 8; ++g) mask[g] = s_mask[j][g];
                         for (int c = 0; c < chunks; ++c) {
                             if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, status)) { ok = false; break; }
                             tc_fence_after();
@@ -1036,7 +1038,7 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
                             for (int h = 0; h < 2; ++h) {
                                 const uint32_t lo_a = smem_desc_lo(ua + (2 * c + h) * kUTile);
                                 for (int kk = 0; kk < kks; ++kk) {
-                                    umma_pair_masked(d, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, first, s_mask[j]);
+                                    umma_pair_masked(d, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, first, mask);
                                     first = 1;
                                 }
                             }
@@ -1168,6 +1170,7 @@ int tiles_of(const ProjectArgs& p, int tile)
     return n < (1 << 24) ? (int)n : 1 << 24;
 }
 
+constexpr int kSmSmem = 228 * 1024, kStaticSmem = 8 * 1024;     // of an SM; of one CTA of either launch, static and reserved
 constexpr int kHalfSmem = 108 * 1024;      // dynamic shared memory up to which two CTAs share an SM
 
 // How many clusters of `size` CTAs run at once, with one CTA per SM or two.  The SMs of a cluster belong to one GPC, so a few of
@@ -1200,8 +1203,8 @@ int cluster_room(int size, bool two)
 }
 
 // Parts of K, stages and shared memory of project_kernel; false if it does not fit.  `behind`: bytes behind the last stage
-// that the MMA of a short token tile may read.
-bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind)
+// that the MMA of a short token tile may read; `beside`: shared memory of a CTA of the first launch, 0 without one.
+bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind, int beside = 0)
 {
     static_assert(kPN == kTok, "");
     const int tiles = tiles_of(p, kPN), pitch = p.a_rows + 4;
@@ -1223,8 +1226,11 @@ bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind)
         };
         // two CTAs per SM if three stages (or all there are) fit, so that the next launch of a chain finds room beside this one
         const int half = stages(kHalfSmem), full = stages(kMaxSmem);
-        const bool two = half >= 3 || (half >= 1 && half == want);
+        bool two = half >= 3 || (half >= 1 && half == want);
         p.n_stages = two ? half : full;
+        // (behind a first launch what has to fit beside a CTA is one of that launch, not a second one of these)
+        const int left = beside > 0 ? stages(min(kMaxSmem, kSmSmem - kStaticSmem - beside)) : 0;
+        if (two && left > half) { two = false; p.n_stages = left; }
         p.scratch = p.n_stages * p.stage_bytes + behind;
         if (p.scratch < own) p.scratch = own;
         const bool fits = p.n_stages >= 2 || (p.n_stages == 1 && want == 1);
@@ -1250,6 +1256,63 @@ bool use_many(const ProjectArgs& p)
     const int rounds = div_up(tiles_of(p, kMTile), 74), waves = div_up(tiles * parts, 148);
     const float few = 8.f + 1.5f * waves * (0.4f * steps / parts + 9e-5f * kTok * kPN / parts * (p.n_adapters > 0 ? p.rank : 0));
     return 18.f + 0.33f * steps * rounds < few;
+}
+
+// Parts of K, chunks of adapters, stages and shared memory (returned) of adapter_kernel.
+size_t adapter_geometry(const ProjectArgs& p, bool many, ProjectArgs& q, int& chunks)
+{
+    const int m_tiles = div_up(p.T, kTok), behind = kTok * kBK * 2 - p.a_bytes;
+    q = p;
+    // K is cut into as many parts as there are SMs for the token tiles, of two slices at least.  Beside a product of many
+    // tokens the SMs that count are those that the product leaves: it starts on the others at once and needs u only at the
+    // end of its first tiles (4096 tokens, 5632 -> 2048: 32 CTAs on all of K instead of 128 on quarters).
+    int sms = 148;
+    if (many && p.w) {
+        const int busy = 2 * tiles_of(p, kMTile);
+        sms = busy > 148 - 36 ? 36 : 148 - busy;
+    }
+    q.u_splits = 1;
+    while (q.u_splits < (m_tiles == 1 ? 8 : 4) && m_tiles * q.u_splits * 2 <= sms && q.ksteps / (q.u_splits * 2) >= 2) q.u_splits *= 2;
+    // Chunks of 64 columns: with one tile they are more CTAs, with many the ring has more stages for x, which is what is read.
+    // From rank 32 on they would hold one or two adapters, so that beside a product, where CTAs are few, x would be read often:
+    // 128 columns.  (64 / 128 columns, us, 4096 tokens, 5632 -> 2048: 4 adapters of rank 16 75 / 90, 16 of rank 32 162 / 135,
+    // 13 of rank 64 113 / 103; 2048 tokens: 53 / 63, 91 / 76, 65 / 66.)
+    const int columns = many && p.w && p.rank >= 32 ? kUCols : kUCols / 2;
+    q.slots = columns / p.rank > 0 ? columns / p.rank : 1;
+    const int most = p.T < kTok ? p.T : kTok;
+    const int all = div_up(most < p.n_adapters ? most : p.n_adapters, q.slots);      // chunks that a tile may have
+    // (beyond rank 64 one accumulator takes all columns, and one lane issues the MMAs)
+    q.lanes = q.slots * p.rank <= kUCols / 2 ? 2 : 1;
+    // shared memory: the ring, and the sums of a_rows tokens twice (sent and received); at high ranks fewer parts, then fewer stages
+    size_t sums;
+    for (;; q.u_splits /= 2) {
+        q.u_own = (div_up(p.a_rows, q.u_splits) + 3) & ~3;
+        sums = (size_t)q.u_splits * (q.u_own + 1) * p.rank * sizeof(float) * (q.u_splits > 1 ? 2 : 1);
+        // two slices per stage where a CTA has many: its lanes wait and commit half as often
+        q.kb = div_up(q.ksteps, q.u_splits) >= 16 ? 2 : 1;
+        q.stage_bytes = q.kb * (p.a_bytes + (q.lanes == 2 ? kUCols / 2 : kUCols) * kBK * 2);
+        if (2 * q.stage_bytes + behind + sums + 1024 > kMaxSmem && q.kb == 2) { q.kb = 1; q.stage_bytes /= 2; }
+        if (q.u_splits == 1 || 2 * q.stage_bytes + behind + sums + 1024 <= kMaxSmem) break;
+    }
+    // two CTAs per SM where four stages (or all of a chunk, two at least) fit
+    const int per_chunk = div_up(div_up(q.ksteps, q.u_splits), q.kb);
+    auto fit = [&](int bytes) { const int n = (bytes - 1024 - behind - (int)sums) / q.stage_bytes; return n < 0 ? 0 : (n > kMaxStages ? kMaxStages : n); };
+    const bool two = fit(kHalfSmem) >= (per_chunk < 2 ? 2 : (per_chunk < 4 ? per_chunk : 4));
+    q.n_stages = two ? fit(kHalfSmem) : fit(kMaxSmem);
+    // Chunks have CTAs of their own, as many as run at once, and are walked over beyond that.  A CTA whose tile has no such chunk
+    // ends at once, so they are counted for all SMs also beside a product.  (4096 tokens, 5632 -> 2048, 32 adapters of rank 16,
+    // every token another: 304 us with the SMs that the product leaves, 166 with all; the same in runs of one tenant: 88, 78.)
+    int room = q.u_splits > 1 ? cluster_room(q.u_splits, two) : 148 * (two ? 2 : 1);
+    if (room > 148 / q.u_splits) room = 148 / q.u_splits;
+    room /= m_tiles;
+    chunks = all < room ? all : (room < 1 ? 1 : room);
+    const int steps = per_chunk * div_up(all, chunks);
+    if (q.n_stages > steps) q.n_stages = steps;
+    // (an even number where the ring wraps: a stage then belongs to the same loading and issuing lanes every time around.  With
+    // an odd one they would take turns on its barriers, and a lane that is ahead could take an older phase for its own.)
+    if (q.n_stages < steps) q.n_stages &= ~1;
+    q.scratch = q.n_stages * q.stage_bytes + behind;
+    return q.scratch + sums + 1024;
 }
 
 // Tile sizes, and for few tokens the shape of project_kernel.  Whether u comes out of the same pass (fused): where all
@@ -1288,7 +1351,10 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
     const bool many = use_many(p), adapters = p.n_adapters > 0;
     const bool fused = plan_few(p);
     p.u_pair = many;
-    const int behind = kTok * kBK * 2 - p.a_bytes;
+    ProjectArgs q;
+    int chunks = 0;
+    const size_t u_smem = adapters && !fused ? adapter_geometry(p, many, q, chunks) : 0;
+    if (u_smem && !many) few_geometry(p, false, 0, kTok * kBK * 2 - p.a_bytes, (int)u_smem);
 
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
@@ -1306,55 +1372,9 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
         if (!make_map_ld(&um.x, p.x, p.T, p.K, p.ldx, p.a_rows) ||
             !make_map_ld(&um.a, p.a, (uint64_t)p.n_adapters * p.rank, p.K, p.K, p.rank))
             return cudaErrorInvalidValue;
-        ProjectArgs q = p;
-        // K is cut into as many parts as there are SMs for the token tiles, of two slices at least; then the chunks of a
-        // tile's adapters go to CTAs of their own as long as there are SMs, and are walked over beyond that.  Beside a product of
-        // many tokens the SMs that count are those that the product leaves: it starts on the others at once and needs u only
-        // at the end of its first tiles (4096 tokens, 5632 -> 2048: 32 CTAs on all of K instead of 128 on quarters).
-        int sms = 148;
-        if (many && p.w) {
-            const int busy = 2 * tiles_of(p, kMTile);
-            sms = busy > 148 - 36 ? 36 : 148 - busy;
-        }
-        q.u_splits = 1;
-        while (q.u_splits < (m_tiles == 1 ? 8 : 4) && m_tiles * q.u_splits * 2 <= sms && q.ksteps / (q.u_splits * 2) >= 2) q.u_splits *= 2;
-        // (chunks of 64 columns: with one tile they are more CTAs, with many the ring has more stages for x, which is what is read)
-        q.slots = 64 / p.rank > 0 ? 64 / p.rank : 1;
-        const int most = p.T < kTok ? p.T : kTok;
-        const int all = div_up(most < p.n_adapters ? most : p.n_adapters, q.slots);      // chunks that a tile may have
-        // (beyond rank 64 one accumulator takes all columns, and one lane issues the MMAs)
-        q.lanes = q.slots * p.rank <= kUCols / 2 ? 2 : 1;
-        // shared memory: the ring, and the sums of a_rows tokens twice (sent and received); at high ranks fewer parts, then fewer stages
-        size_t sums;
-        for (;; q.u_splits /= 2) {
-            q.u_own = (div_up(p.a_rows, q.u_splits) + 3) & ~3;
-            sums = (size_t)q.u_splits * (q.u_own + 1) * p.rank * sizeof(float) * (q.u_splits > 1 ? 2 : 1);
-            // two slices per stage where a CTA has many: its lanes wait and commit half as often
-            q.kb = div_up(q.ksteps, q.u_splits) >= 16 ? 2 : 1;
-            q.stage_bytes = q.kb * (p.a_bytes + (q.lanes == 2 ? kUCols / 2 : kUCols) * kBK * 2);
-            if (2 * q.stage_bytes + behind + sums + 1024 > kMaxSmem && q.kb == 2) { q.kb = 1; q.stage_bytes /= 2; }
-            if (q.u_splits == 1 || 2 * q.stage_bytes + behind + sums + 1024 <= kMaxSmem) break;
-        }
-        // two CTAs per SM where four stages (or all of a chunk, two at least) fit
-        const int per_chunk = div_up(div_up(q.ksteps, q.u_splits), q.kb);
-        auto fit = [&](int bytes) { const int n = (bytes - 1024 - behind - (int)sums) / q.stage_bytes; return n < 0 ? 0 : (n > kMaxStages ? kMaxStages : n); };
-        const bool two = fit(kHalfSmem) >= (per_chunk < 2 ? 2 : (per_chunk < 4 ? per_chunk : 4));
-        q.n_stages = two ? fit(kHalfSmem) : fit(kMaxSmem);
-        // chunks with CTAs of their own: as many as run at once
-        int room = q.u_splits > 1 ? cluster_room(q.u_splits, two) : 148 * (two ? 2 : 1);
-        if (room > sms / q.u_splits) room = sms / q.u_splits;
-        room /= m_tiles;
-        const int chunks = all < room ? all : (room < 1 ? 1 : room);
-        const int steps = per_chunk * div_up(all, chunks);
-        if (q.n_stages > steps) q.n_stages = steps;
-        // (an even number where the ring wraps: a stage then belongs to the same loading and issuing lanes every time around.  With
-        // an odd one they would take turns on its barriers, and a lane that is ahead could take an older phase for its own.)
-        if (q.n_stages < steps) q.n_stages &= ~1;
-        q.scratch = q.n_stages * q.stage_bytes + behind;
         cfg.attrs[1].val.clusterDim.z = q.u_splits;
         cfg.numAttrs = q.u_splits > 1 ? 2 : 1;
-        cfg.gridDim = dim3(m_tiles, chunks, q.u_splits); cfg.blockDim = dim3(kUThreads);
-        cfg.dynamicSmemBytes = q.scratch + sums + 1024;
+        cfg.gridDim = dim3(m_tiles, chunks, q.u_splits); cfg.blockDim = dim3(kUThreads); cfg.dynamicSmemBytes = u_smem;
         e = cudaLaunchKernelEx(&cfg, adapter_kernel, q, um);
         if (e != cudaSuccess) return e;
         attr[1].val.clusterDim.z = 1;
