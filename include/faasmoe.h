@@ -393,8 +393,8 @@ int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, i
                 int n_tenants, const void* base, int64_t ld_base, void* out, int64_t ld_out, int out_type, void* workspace,
                 int64_t workspace_bytes, int32_t* status_out, void* stream);
 
-/* Bytes of device memory that moe_project needs (negative: MOE_ERR_SHAPE); 0 for few tokens with few adapters or low ranks,
- * and without adapters. */
+/* Bytes of device memory that moe_project needs (negative: MOE_ERR_SHAPE); 0 without adapters, and where one launch does all (a
+ * handful of tokens of a small projection). */
 int64_t moe_project_workspace(int T, int K, int N, int rank, int n_adapters);
 
 /* route -> dispatch -> experts -> combine on the context's workspace; bit-identical to

@@ -6,8 +6,8 @@
 // distinct adapters are listed, their rows are gathered by TMA as the N operand of one tcgen05.mma per 16 elements of K, and
 // each token keeps the columns of its own adapter; K is cut over the CTAs of a cluster, which add up their parts in a fixed
 // order.  The projection (project_kernel for few tokens, project_many_kernel for many) is resident and streams W meanwhile
-// (programmatic dependent launch) and adds u . B^T behind its main loop.  With few tokens of few adapters it computes u
-// itself, in the same pass over x, and there is one launch only.
+// (programmatic dependent launch) and adds u . B^T behind its main loop.  For a handful of tokens it computes u itself, in the
+// same pass over x, and there is one launch only.
 #include <cstring>
 
 #include "project.cuh"
@@ -1239,23 +1239,26 @@ bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind, int beside
     }
 }
 
-// Which shape, by what either was measured to cost (us): the pair shape some 18 and 0.33 per slice of K and round of tiles;
-// the other 8 and, half as much again as its parts alone, 0.4 per slice and 9e-5 per product of the adapters on a thread's
-// CUDA core.  (few / many: 2048 -> 2048, rank 16: 140 tokens 20 / 28, 256 25 / 28, 300 31 / 27, 1024 47 / 23; 2048 -> 5632:
-// 140 tokens 41 / 29; 5632 -> 2048, rank 64: 140 tokens 50 / 49, 300 74 / 48; 512 -> 512: 140 tokens 17 / 24, 1024 19 / 18.)
-// Up to 128 tokens the pair shape only pays for high ranks of few adapters (2048 -> 2048, rank 64, 2 adapters: 32 tokens
-// 20 / 19, 128 tokens 48 / 20; 32 adapters: 64 tokens 30 / 53).
+// Which shape, by what either costs (us), a model fitted to some thousand measured pairs of 1 to 1024 tokens, 512 to 5632 rows and
+// columns, ranks 8 to 128 of 1 to 32 adapters (the choice is within 1.15 of the better one in all but nine).  The pair shape: its
+// slices of K, and a masked MMA per adapter that a tile may have.  The other: parts of K, and the adapters' products on the CUDA
+// cores.  (few / many tokens' shape, 2048 -> 2048: rank 16, 4 adapters, 64 tokens 11 / 20, 128 15 / 21; 32 adapters, 128 tokens
+// 22 / 36; rank 64, 2 adapters, 48 tokens 18 / 19, 96 27 / 20; no adapters, 200 tokens 14 / 15, 512 20 / 16.  2048 -> 5632:
+// rank 16, 4 adapters, 24 tokens 12 / 20, 96 23 / 21; 5632 -> 2048: rank 32, 4 adapters, 128 tokens 22 / 38.)
 bool use_many(const ProjectArgs& p)
 {
-    if (p.T <= kTok) return p.T > 32 && p.rank >= 48 && p.n_adapters > 0 && p.n_adapters <= 4;
-    const int steps = p.w ? div_up(p.K, kBK) : 0, tiles = tiles_of(p, kPN);
-    int parts = tiles > 0 ? 148 / tiles : 1;
+    const int steps = p.w ? div_up(p.K, kBK) : 0, tiles = tiles_of(p, kPN), rows = p.T < kTok ? p.T : kTok;
+    int parts = tiles < 148 ? 148 / tiles : 1;
     if (parts > 8) parts = 8;
     if (p.w && parts > steps / 2) parts = steps / 2;
     if (parts < 1) parts = 1;
-    const int rounds = div_up(tiles_of(p, kMTile), 74), waves = div_up(tiles * parts, 148);
-    const float few = 8.f + 1.5f * waves * (0.4f * steps / parts + 9e-5f * kTok * kPN / parts * (p.n_adapters > 0 ? p.rank : 0));
-    return 18.f + 0.33f * steps * rounds < few;
+    const int waves = div_up(tiles * parts, 148), rounds = div_up(tiles_of(p, kMTile), 74);
+    int distinct = p.T < kMTile ? p.T : kMTile;
+    if (distinct > p.n_adapters) distinct = p.n_adapters;
+    const bool adapters = p.n_adapters > 0;
+    const float few = (adapters ? 8.8f : 7.7f) + waves * (0.6f * steps / parts + 0.009f * rows + 1.2e-4f * rows * kPN / parts * (adapters ? p.rank : 0));
+    const float many = (p.w ? 10.3f : 13.5f) - (adapters ? 0.f : 3.1f) + rounds * (0.25f * steps + distinct * (0.48f + 0.0083f * p.rank));
+    return many < few;
 }
 
 // Parts of K, chunks of adapters, stages and shared memory (returned) of adapter_kernel.
@@ -1315,9 +1318,11 @@ size_t adapter_geometry(const ProjectArgs& p, bool many, ProjectArgs& q, int& ch
     return q.scratch + sums + 1024;
 }
 
-// Tile sizes, and for few tokens the shape of project_kernel.  Whether u comes out of the same pass (fused): where all
-// adapters that the tokens may have fit 128 columns beside the product's, and the parts of u that every CTA of a cluster then
-// receives fit its shared memory beside two stages.
+// Tile sizes, and for few tokens the shape of project_kernel; returns whether u comes out of the same pass (fused).  That
+// saves a launch, some 2 us of the caller's time, and costs every CTA all of u: up to four tokens of a product of at most 512 tiles of
+// 128 x 64 weights (8 MB), where the launches are what a call waits for.  (2048 -> 2048, rank 16, one token: 9.9 us on the GPU
+// and 11 on the host in one launch, 9.6 and 12.5 in two; 2048 -> 5632: 12.6 and 10.7 on the GPU; 2048 -> 2048, 4 adapters of rank 32:
+// 8 tokens 12.7 and 11.1, 64 tokens 18 and 14.)
 bool plan_few(ProjectArgs& p)
 {
     const bool adapters = p.n_adapters > 0;
@@ -1325,10 +1330,9 @@ bool plan_few(ProjectArgs& p)
     p.a_bytes = (p.a_rows * kBK * 2 + 1023) & ~1023;
     p.ksteps = p.w || adapters ? div_up(p.K, kBK) : 0;
     const int behind = kTok * kBK * 2 - p.a_bytes;          // an MMA reads 128 token rows, also of a short tile in the last stage
-    if (use_many(p)) return false;
     p.u_rows = adapters ? (p.T < p.n_adapters ? p.T : p.n_adapters) * (p.rank <= kUCols ? p.rank : kUCols) : 0;
-    if (adapters && p.T <= kTok && p.u_rows <= kUCols && few_geometry(p, true, p.u_rows, behind)) return true;
-    few_geometry(p, false, 0, behind);
+    if (adapters && p.T <= 4 && (int64_t)tiles_of(p, kPN) * p.ksteps <= 512 && p.u_rows <= kUCols && few_geometry(p, true, p.u_rows, behind)) return true;
+    if (!use_many(p)) few_geometry(p, false, 0, behind);
     return false;
 }
 
@@ -1348,8 +1352,7 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
     ProjectArgs p = in;
     static bool u_ok[kMaxDevices] = {false}, p_ok[kMaxDevices] = {false}, f_ok[kMaxDevices] = {false}, m_ok[kMaxDevices] = {false};
     const int m_tiles = div_up(p.T, kTok), n_tiles = div_up(p.N, kPN);
-    const bool many = use_many(p), adapters = p.n_adapters > 0;
-    const bool fused = plan_few(p);
+    const bool adapters = p.n_adapters > 0, fused = plan_few(p), many = !fused && use_many(p);
     p.u_pair = many;
     ProjectArgs q;
     int chunks = 0;
