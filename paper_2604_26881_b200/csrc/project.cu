@@ -370,14 +370,16 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
                 v *= s_scale[row];
                 w *= s_scale[row];
                 const size_t at = (size_t)(t0 + row) * p.rank + c;
-                if (p.u_pair) {
-                    // hi + lo hold 16 bits of v (what rounds to an infinity, or is one, has no remainder)
-                    const __nv_bfloat162 hi = __floats2bfloat162_rn(v, w);
-                    const float2 f = __bfloat1622float2(hi);
-                    bf16* u = reinterpret_cast<bf16*>(p.u);
-                    *reinterpret_cast<__nv_bfloat162*>(u + at) = hi;
-                    *reinterpret_cast<__nv_bfloat162*>(u + (size_t)p.T * p.rank + at) =
-                        __floats2bfloat162_rn(isinf(f.x) ? 0.f : v - f.x, isinf(f.y) ? 0.f : w - f.y);
+                if (p.u_terms > 0) {
+                    // each term is what the ones before left over (what rounds to an infinity, or is one, leaves nothing)
+                    bf16* u = reinterpret_cast<bf16*>(p.u) + at;
+                    for (int h = 0; h < p.u_terms; ++h, u += (size_t)p.T * p.rank) {
+                        const __nv_bfloat162 term = __floats2bfloat162_rn(v, w);
+                        const float2 f = __bfloat1622float2(term);
+                        *reinterpret_cast<__nv_bfloat162*>(u) = term;
+                        v = isinf(f.x) ? 0.f : v - f.x;
+                        w = isinf(f.y) ? 0.f : w - f.y;
+                    }
                 } else {
                     *reinterpret_cast<float2*>(p.u + at) = make_float2(v, w);
                 }
@@ -730,8 +732,9 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
 // Many tokens: 256 tokens x 256 weight rows per pair of CTAs (tcgen05.mma.cta_group::2; each CTA holds 128 of either), pairs
 // that walk over the tiles, two accumulators of 256 TMEM columns so that a tile's epilogue runs behind the next tile's MMAs.
 //
-// The adapters' second products go into the same accumulator: u of the tile's tokens is one more M operand (a pair of
-// bf16 tiles, hi and lo, that hold 16 bits of the fp32 value: a single bf16 would cost 2^-9 of the adapter's share), and
+// The adapters' second products go into the same accumulator: u of the tile's tokens is one more M operand (bf16 tiles that
+// add up to the fp32 value: two, 16 bits of it, for a bf16 output, where a single one would cost 2^-9 of the adapter's share;
+// three, all 24 bits, for an fp32 output, which two would leave 1.7e-6 off where fp32 sums are 3e-7), and
 // for every distinct adapter of the tile the rows of its B are one more N operand.  Which tokens that MMA may change is said by
 // its disable-output-lane mask, so u needs no masked copy per adapter and an infinity or a NaN in one tenant's B
 // cannot reach another's tokens (a zeroed row of u would: 0 * inf).
@@ -894,7 +897,7 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
     const uint32_t ring = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     unsigned char* const ring_ptr = smem_dyn + (ring - smem_u32(smem_dyn));
     const int n_stages = p.n_stages;
-    // u: [64-column chunk][hi, lo] tiles; once the tile's MMAs have read it, its memory is the epilogue's staging area
+    // u: [64-column chunk][term] tiles; once the tile's MMAs have read it, its memory is the epilogue's staging area
     const uint32_t ua = ring + n_stages * kMStageBytes;
     __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 9];
     __shared__ uint32_t s_tmem;
@@ -909,7 +912,7 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
     const bool adapters = p.n_adapters > 0;
     const int n_tiles = (p.N + kMTile - 1) / kMTile, m_tiles = (p.T + kMTile - 1) / kMTile, total = n_tiles * m_tiles;
     const int pair0 = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int chunks = (p.rank + kBK - 1) / kBK;                        // of u and of the adapters' B (0 without adapters)
+    const int terms = p.u_terms, chunks = (p.rank + kBK - 1) / kBK;     // of u and of the adapters' B (0 without adapters)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < n_stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
@@ -954,15 +957,16 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
                             if (!mbar_wait(bar_list, it & 1, &s_abort, status)) { ok = false; break; }
                             extra = s_al.count * chunks;
                             if (warp == 10) {
-                                // u of this CTA's tokens, hi and lo tiles (rows of tokens without an adapter hold anything)
+                                // u of this CTA's tokens (rows of tokens without an adapter hold anything)
                                 if (it == 0) pdl_wait();
                                 // (the MMAs of the tile before have read theirs, and its epilogue is through with the memory)
                                 if (!mbar_wait(bar_uempty, (it & 1) ^ 1, &s_abort, status) ||
                                     !mbar_wait(bar_staged, (it & 1) ^ 1, &s_abort, status)) { ok = false; break; }
-                                if (leader) mbar_expect_tx(bar_ufull, 4 * chunks * kUTile);
+                                if (leader) mbar_expect_tx(bar_ufull, 2 * terms * chunks * kUTile);
                                 u_loads = it + 1;
-                                for (int c = 0; c < 2 * chunks; ++c)
-                                    tma_load_3d_pair(ua + c * kUTile, &maps.u, bar_ufull, (c >> 1) * kBK, t0, c & 1);
+                                for (int c = 0; c < chunks; ++c)
+                                    for (int h = 0; h < terms; ++h)
+                                        tma_load_3d_pair(ua + (c * terms + h) * kUTile, &maps.u, bar_ufull, c * kBK, t0, h);
                             }
                         }
                     }
@@ -1035,8 +1039,8 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
                             tc_fence_after();
                             const uint32_t lo_b = smem_desc_lo(ring + stage * kMStageBytes + kTok * kBK * 2);
                             const int kks = (min(kBK, p.rank - c * kBK) + 15) >> 4;
-                            for (int h = 0; h < 2; ++h) {
-                                const uint32_t lo_a = smem_desc_lo(ua + (2 * c + h) * kUTile);
+                            for (int h = 0; h < terms; ++h) {
+                                const uint32_t lo_a = smem_desc_lo(ua + (c * terms + h) * kUTile);
                                 for (int kk = 0; kk < kks; ++kk) {
                                     umma_pair_masked(d, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, first, mask);
                                     first = 1;
@@ -1131,7 +1135,7 @@ bool make_map_ld(CUtensorMap* m, const void* base, uint64_t rows, uint64_t k, ui
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// 3-D map over n matrices [N][rank] (the adapters' B; u's two halves); box = 64 x box_rows of one matrix
+// 3-D map over n matrices [N][rank] (the adapters' B; u's terms); box = 64 x box_rows of one matrix
 bool make_map_3d(CUtensorMap* m, const void* base, uint64_t n, uint64_t N, uint64_t rank, uint32_t box_rows)
 {
     EncodeTiledFn fn = encode_fn();
@@ -1257,7 +1261,7 @@ bool use_many(const ProjectArgs& p)
     if (distinct > p.n_adapters) distinct = p.n_adapters;
     const bool adapters = p.n_adapters > 0;
     const float few = (adapters ? 8.8f : 7.7f) + waves * (0.6f * steps / parts + 0.009f * rows + 1.2e-4f * rows * kPN / parts * (adapters ? p.rank : 0));
-    const float many = (p.w ? 10.3f : 13.5f) - (adapters ? 0.f : 3.1f) + rounds * (0.25f * steps + distinct * (0.48f + 0.0083f * p.rank));
+    const float many = (p.w ? 10.3f : 13.5f) - (adapters ? 0.f : 3.1f) + rounds * (0.25f * steps + distinct * (0.48f + 0.0083f * p.rank * (p.out_f32 ? 1.5f : 1.f)));
     return many < few;
 }
 
@@ -1344,7 +1348,7 @@ int64_t project_workspace(int T, int K, int N, int rank, int n_adapters)
     ProjectArgs p = {};
     p.T = T; p.K = K; p.N = N; p.rank = rank; p.n_adapters = n_adapters;
     if (plan_few(p) && (p.w = reinterpret_cast<const bf16*>(16), plan_few(p))) return 0;      // (with w and without)
-    return (int64_t)T * rank * (int64_t)sizeof(float);
+    return (int64_t)T * rank * 6;        // fp32, or up to three bf16 terms
 }
 
 cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
@@ -1353,7 +1357,7 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
     static bool u_ok[kMaxDevices] = {false}, p_ok[kMaxDevices] = {false}, f_ok[kMaxDevices] = {false}, m_ok[kMaxDevices] = {false};
     const int m_tiles = div_up(p.T, kTok), n_tiles = div_up(p.N, kPN);
     const bool adapters = p.n_adapters > 0, fused = plan_few(p), many = !fused && use_many(p);
-    p.u_pair = many;
+    p.u_terms = many ? (p.out_f32 ? 3 : 2) : 0;
     ProjectArgs q;
     int chunks = 0;
     const size_t u_smem = adapters && !fused ? adapter_geometry(p, many, q, chunks) : 0;
@@ -1391,10 +1395,11 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
         if (!p.w) p.ksteps = 0;
         if (p.w && (!make_map_ld(&mm.x, p.x, p.T, p.K, p.ldx, kTok) || !make_map_ld(&mm.w, p.w, p.N, p.K, p.ldw, kTok)))
             return cudaErrorInvalidValue;
-        if (adapters && (!make_map_3d(&mm.b, p.b, p.n_adapters, p.N, p.rank, kBRows) || !make_map_3d(&mm.u, p.u, 2, p.T, p.rank, kTok)))
+        if (adapters && (!make_map_3d(&mm.b, p.b, p.n_adapters, p.N, p.rank, kBRows) || !make_map_3d(&mm.u, p.u, p.u_terms, p.T, p.rank, kTok)))
             return cudaErrorInvalidValue;
-        const int u_tiles = adapters ? 2 * div_up(p.rank, kBK) : 0;              // 32 KB up to rank 64, 64 KB beyond
-        p.n_stages = u_tiles > 2 ? kMStages - 1 : kMStages;
+        const int u_tiles = adapters ? p.u_terms * div_up(p.rank, kBK) : 0;      // 32 to 96 KB, which leave five to three stages
+        p.n_stages = (kMaxSmem - 1024 - u_tiles * kUTile) / kMStageBytes;
+        if (p.n_stages > kMStages) p.n_stages = kMStages;
         size_t behind_ring = (size_t)u_tiles * kUTile;
         if (behind_ring < kOutStage) behind_ring = kOutStage;
         const int tiles = tiles_of(p, kMTile), pairs = tiles < 74 ? tiles : 74;

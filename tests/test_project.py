@@ -2,7 +2,7 @@
 
 Tolerances.  A sum over K on the tensor cores is rounded or cut at most once per 16 products and once per part of K that is
 added up: (K/16 + 16) * 2^-23 of the sum of the terms' absolute values.  An adapter's inner product u carries that error, the
-factor's rounding, and at most 2^-16 relative where it is held as a pair of bf16 numbers; the outer product adds (rank + 4)
+factor's rounding, and at most 2^-16 relative where it is held as bf16 numbers (2^-24 for an fp32 output); the outer product adds (rank + 4)
 fp32 roundings.  The last addition and base: 3 * 2^-24 of the absolute values.  A bf16 output adds half a bf16 step (2^-8).
 All of it is propagated through the absolute values of the very inputs.
 """
@@ -16,8 +16,8 @@ gpu = pytest.mark.gpu
 DEV = "cuda:0"
 
 
-def reference(x, w, base, a, b, scale, adapter):
-    """(y, error bound) in 64 bits; adapter [T] holds each token's adapter or -1."""
+def reference(x, w, base, a, b, scale, adapter, exact_u=False):
+    """(y, error bound) in 64 bits; adapter [T] holds each token's adapter or -1.  exact_u: of an fp32 output."""
     x = x.double()
     K = x.shape[1]
     T, N = x.shape[0], (w if w is not None else base if base is not None else b[0]).shape[0 if w is not None else 1 if base is not None else 0]
@@ -36,7 +36,7 @@ def reference(x, w, base, a, b, scale, adapter):
             s = 1.0 if scale is None else float(scale[i].double())
             ai, bi = a[i].double(), b[i].double()
             u, um = s * (x[t] @ ai.t()), abs(s) * (x[t].abs() @ ai.abs().t())
-            u_err = e_sum * um + (2.0 ** -16 + 2.0 ** -22) * u.abs()
+            u_err = e_sum * um + (2.0 ** -22 + (2.0 ** -24 if exact_u else 2.0 ** -16)) * u.abs()
             y[t] += u @ bi.t()
             m = (u.abs() + u_err) @ bi.abs().t()
             mag[t] += m
@@ -88,7 +88,7 @@ def check(T, K, N, rank=16, n=4, n_tenants=None, layout="uniform", out=torch.flo
         adapter = mot.long()[adapter]
     elif n:
         adapter = torch.where(adapter < n, adapter, torch.full_like(adapter, -1))
-    y, err = reference(d["x"], d["w"], d["base"], d["a"], d["b"], d["scale"], adapter)
+    y, err = reference(d["x"], d["w"], d["base"], d["a"], d["b"], d["scale"], adapter, out == torch.float32)
     store = torch.full((T + 2, N + pads[3] + 3), 7.0, dtype=out, device=DEV)
     o = store[1:T + 1, :N]
     dev = lambda t: None if t is None else t.to(DEV)
@@ -349,10 +349,10 @@ def test_refusals_need_no_gpu():
     assert lib.moe_project_workspace(4, 64, 32, 129, 1) == B.MOE_ERR_SHAPE
     assert lib.moe_project_workspace(4, 64, 0, 8, 1) == B.MOE_ERR_SHAPE
     assert lib.moe_project_workspace(4, 64, 32, 8, 1 << 28) == B.MOE_ERR_SHAPE
-    assert lib.moe_project_workspace(1 << 22, 64, 1 << 30, 8, 1) == 8 * 4 << 22          # (no overflow on the way)
+    assert lib.moe_project_workspace(1 << 22, 64, 1 << 30, 8, 1) == 8 * 6 << 22          # (no overflow on the way)
     assert lib.moe_project_workspace(4, 64, 32, 0, 0) == 0
     assert lib.moe_project_workspace(1, 2048, 2048, 16, 3) == 0               # one pass, no workspace
-    assert lib.moe_project_workspace(1000, 2048, 2048, 16, 3) == 1000 * 16 * 4
+    assert lib.moe_project_workspace(1000, 2048, 2048, 16, 3) == 1000 * 16 * 6
 
 
 def test_binding_checks_tensors():
