@@ -8,6 +8,12 @@
 // order.  The projection (project_kernel for few tokens, project_many_kernel for many) is resident and streams W meanwhile
 // (programmatic dependent launch) and adds u . B^T behind its main loop.  For a handful of tokens it computes u itself, in the
 // same pass over x, and there is one launch only.
+//
+// Few tokens are a chain of latencies (ids, list, TMA, MMA, exchange in the cluster, the launch boundary, second product), not
+// bytes: 2048 -> 2048, rank 16, one token 9.8 us (8.5 MB, 1.3 us of HBM time); 2048 -> 5632, 32 tokens of 32 adapters 14.0 us
+// (31.8 MB, 4.9 us).  Many tokens are bound by the tensor cores: 5632 -> 2048, 4096 tokens of 16 adapters of rank 16 75 to 77 us (95
+// GFLOP, 1.25 PFLOP/s, 0.76 of the measured peak); the adapters alone beside a base, 1126 tokens, 13 of rank 64: 26 us, first
+// product 12 of them.
 #include <cstring>
 
 #include "project.cuh"
