@@ -355,7 +355,7 @@ int moe_set_gating(moe_ctx* ctx, int layer, const moe_gating* rule, const float*
  * The residual's addition and the RMSNorm in front of a layer, without a context: for callers that run other blocks
  * (attention) between the layers of moe_stack_forward.
  *   h = bf16(x + residual)              (h = x if residual is NULL)     bf16 [T, H] each
- *   residual_out = h                    bf16 [T, H] or NULL; may be residual or x itself (same row distance)
+ *   residual_out = h                    bf16 [T, H] or NULL; may be residual or x itself (same row distance, else MOE_ERR_SHAPE)
  *   y = h / sqrt(mean(h^2) + eps) * weight                              fp32; weight bf16 [H]
  *   out = bf16(y)                       bf16 [T, H] or NULL; may be x itself (same row distance)
  *   out_q = e4m3(y / s)                 8-bit floats [T, H] or NULL, saturating; s = max |y| / 448 (0 where y is 0)

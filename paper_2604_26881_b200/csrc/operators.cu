@@ -15,6 +15,9 @@ constexpr int kProjectMaxDim = 1 << 30;      // K, N, and the rows of all adapte
 
 bool off(const void* p, size_t align) { return ((uintptr_t)p & (align - 1)) != 0; }
 
+// an output in the place of an input needs the input's row distance: a row would be overwritten before it is read
+bool shifted(const void* out, int64_t ld_out, const void* in, int64_t ld_in, int T) { return out && out == in && T > 1 && ld_out != ld_in; }
+
 }  // namespace
 
 namespace faasmoe {
@@ -76,6 +79,10 @@ int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld
     if (off(x, 2) || off(residual, 2) || off(weight, 2) || off(residual_out, 2) || off(out, 2) || off(q_scale, 4)) return MOE_ERR_SHAPE;
     if (T == 0) return MOE_OK;
     if (!x || !weight || (!residual_out && !out && !out_q) || (out_q && !q_scale)) return MOE_ERR_NULL;
+    if ((out && out == residual_out) || (out_q && (out_q == x || out_q == residual || out_q == out || out_q == residual_out))) return MOE_ERR_SHAPE;
+    if (shifted(out, ld_out, x, ldx, T) || shifted(out, ld_out, residual, ld_residual, T) || shifted(residual_out, ld_residual_out, x, ldx, T) ||
+        shifted(residual_out, ld_residual_out, residual, ld_residual, T))
+        return MOE_ERR_SHAPE;
     AddNormArgs a = {};
     a.x = (const bf16*)x; a.residual = (const bf16*)residual; a.residual_out = (bf16*)residual_out; a.weight = (const bf16*)weight;
     a.out = (bf16*)out; a.q = (uint8_t*)out_q; a.q_scale = q_scale;
@@ -116,6 +123,7 @@ int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, i
     const int64_t need = project_workspace(T, K, N, rank, n_adapters);
     if (need > 0 && !workspace) return MOE_ERR_NULL;
     if (workspace_bytes < need) return MOE_ERR_ALLOC;
+    if (((w || adapters) && out == x) || out == w || (adapters && (out == a || out == b)) || shifted(out, ld_out, base, ld_base, T)) return MOE_ERR_SHAPE;
     ProjectArgs p = {};
     p.x = (const bf16*)x; p.w = (const bf16*)w; p.ldx = ldx; p.ldw = ldw; p.T = T; p.K = K; p.N = N;
     if (adapters) {

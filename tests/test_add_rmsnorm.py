@@ -117,6 +117,25 @@ def test_strides_and_alignment(pads, shift):
 
 
 @gpu
+def test_rows_beyond_32_bit_offsets():
+    """Rows 2^25 elements apart: the last ones lie beyond 2^31 elements."""
+    T, H, ld = 70, 520, 1 << 25
+    g = torch.Generator().manual_seed(4)
+    far = lambda dtype: torch.empty(T * ld, dtype=dtype, device="cuda:0").as_strided((T, H), (ld, 1))
+    x0, r0, w0 = torch.randn(T, H, generator=g).to(torch.bfloat16), torch.randn(T, H, generator=g).to(torch.bfloat16), torch.ones(H, dtype=torch.bfloat16)
+    near = dict(out=torch.empty(T, H, dtype=torch.bfloat16, device="cuda:0"), out_q=torch.empty(T, H, dtype=torch.float8_e4m3fn, device="cuda:0"),
+                q_scale=torch.empty(T, 1, device="cuda:0"), residual_out=torch.empty(T, H, dtype=torch.bfloat16, device="cuda:0"))
+    B.moe_add_rmsnorm(x0.cuda(), w0.cuda(), 1e-6, residual=r0.cuda(), **near)
+    x, o, q = far(torch.bfloat16), far(torch.bfloat16), far(torch.float8_e4m3fn)
+    x.copy_(x0)
+    s = torch.empty(T, 1, device="cuda:0")
+    B.moe_add_rmsnorm(x, w0.cuda(), 1e-6, residual=r0.cuda(), residual_out=x, out=o, out_q=q, q_scale=s)
+    torch.cuda.synchronize()
+    assert torch.equal(x, near["residual_out"]) and torch.equal(o, near["out"]) and torch.equal(s, near["q_scale"])
+    assert torch.equal(q.contiguous().view(torch.uint8), near["out_q"].view(torch.uint8))
+
+
+@gpu
 def test_each_output_alone_and_without_a_residual():
     for residual in (False, True):
         check(9, 520, residual=residual, residual_out=True, out=False)
@@ -219,6 +238,8 @@ def test_refusals_need_no_gpu():
         assert _raw(**bad) == B.MOE_ERR_NULL, bad
     for bad in (dict(T=-1), dict(H=0), dict(ldx=15), dict(ldo=15), dict(r=64, ldr=15), dict(ro=64, ldro=15), dict(q=64, ldq=15, qs=64), dict(eps=-1.0),
                 dict(eps=float("nan")), dict(q=64, ldq=16, qs=64, group=64), dict(x=65), dict(o=65), dict(q=64, ldq=16, qs=66), dict(w=63)):
+        assert _raw(**bad) == B.MOE_ERR_SHAPE, bad
+    for bad in (dict(ldo=24), dict(x=128, r=64, ldr=24), dict(o=None, ro=64, ldro=24), dict(x=128, ro=64, ldro=16), dict(q=64, ldq=16, qs=64)):      # overlapping
         assert _raw(**bad) == B.MOE_ERR_SHAPE, bad
     assert _raw(H=16385, ldx=16385, ldo=16385) == B.MOE_ERR_UNSUPPORTED
     assert _raw(T=0) == B.MOE_OK

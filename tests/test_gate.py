@@ -124,6 +124,23 @@ def test_groups(dtype, E, n_groups, keep, group_score):
 
 
 @gpu
+@pytest.mark.parametrize("T,ld,E", [(140, 1 << 24, 60), (9000, 1 << 18, 60), (16400, 1 << 18, 256)])
+def test_rows_beyond_32_bit_offsets(T, ld, E):
+    g = np.random.default_rng(T)
+    z = torch.as_tensor(g.standard_normal((T, E))).to(torch.bfloat16)
+    far = torch.empty(T * ld, dtype=torch.bfloat16, device="cuda:0").as_strided((T, E), (ld, 1))
+    far.copy_(z)
+    rule = B.moe_gating(score="sigmoid", renormalize=True)
+    outs = []
+    for logits in (z.to("cuda:0"), far):
+        idx, w = torch.empty(T, 4, dtype=torch.int32, device="cuda:0"), torch.empty(T, 4, device="cuda:0")
+        B.moe_gate(logits, rule, idx, w)
+        outs.append((idx, w))
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
+@gpu
 @pytest.mark.parametrize("T", [0, 1, 2, 3, 4, 5, 127, 1000, 4099])
 def test_numbers_of_tokens(T):
     g = np.random.default_rng(T)

@@ -171,6 +171,55 @@ def test_rings_that_wrap_many_times(rank):
 
 
 @gpu
+@pytest.mark.parametrize("T,what", [(100, "x"), (100, "w"), (100, "out"), (600, "x"), (600, "w"), (600, "out")])
+def test_rows_beyond_32_bit_offsets(T, what):
+    """Rows so far apart that the last ones lie beyond 2^31 elements, of each matrix in turn, in either shape."""
+    K, N, rank, n = 128, 260, 16, 4
+    d = inputs(T, K, N, rank, n, 3, base=True)
+    g = {k: v.to(DEV) for k, v in d.items()}
+    tenant = tenants(T, n, "uniform", 1).to(DEV)
+    kw = dict(a=g["a"], b=g["b"], scale=g["scale"], tenant_id=tenant)
+    near = torch.empty(T, N, dtype=torch.bfloat16, device=DEV)
+    B.moe_project(g["x"], g["w"], near, base=g["base"], **kw)
+
+    def far(t):
+        ld = -(-(1 << 32) // t.shape[0] // 8) * 8
+        v = torch.empty(t.shape[0] * ld + 1024, dtype=t.dtype, device=DEV).as_strided(t.shape, (ld, 1))
+        v.copy_(t)
+        return v
+    x, w, out, base = g["x"], g["w"], torch.empty_like(near), g["base"]
+    if what == "x":
+        x = far(x)
+    elif what == "w":
+        w = far(w)
+    else:
+        out = base = far(base)                                       # (in place)
+    B.moe_project(x, w, out, base=base, **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(out, near)
+
+
+@gpu
+@pytest.mark.parametrize("T", [3, 40, 600])
+def test_adapters_beyond_32_bit_offsets(T):
+    """a and b of more than 2^31 elements: the last adapters give what they give alone."""
+    K, N, rank, n = 4096, 4096, 128, 4100
+    g = torch.Generator(device=DEV).manual_seed(2)
+    rnd = lambda *s: (torch.randn(*s, generator=g, device=DEV) * 0.05).to(torch.bfloat16)
+    x, a2, b2 = rnd(T, K), rnd(2, rank, K), rnd(2, N, rank)
+    a, b = torch.empty(n, rank, K, dtype=torch.bfloat16, device=DEV), torch.empty(n, N, rank, dtype=torch.bfloat16, device=DEV)
+    a[n - 2:], b[n - 2:] = a2, b2
+    pick = torch.arange(T, dtype=torch.int32, device=DEV) % 2
+    one, two = (torch.empty(T, N, device=DEV) for _ in range(2))
+    B.moe_project(x, None, one, a=a2, b=b2, tenant_id=pick)
+    B.moe_project(x, None, two, a=a, b=b, tenant_id=pick + (n - 2))
+    torch.cuda.synchronize()
+    y, err = reference(x.cpu(), None, None, a2.cpu(), b2.cpu(), None, pick.cpu().long())
+    for o in (one, two):                                             # (of other numbers of adapters: other shapes, other orders of the sums)
+        assert ((o.double().cpu() - y).abs() <= err + 1e-30).all()
+
+
+@gpu
 @pytest.mark.parametrize("weight", [True, False])
 def test_tiles_of_one_run_with_all_none_and_hundreds_of_adapters(weight):
     """More tiles than run at once; neighbouring runs of 256 tokens have 1, 0, about 200 and 3 adapters, so the loops over a tile's
@@ -339,6 +388,8 @@ def test_refusals_need_no_gpu():
                 dict(rank=136), dict(n_tenants=0), dict(x=264), dict(w=264), dict(a=264), dict(b=260), dict(scale=258), dict(tenant=258), dict(table=258),
                 dict(out=258), dict(out=257, out_type=1), dict(K=(1 << 30) + 8, ldx=1 << 31, ldw=1 << 31), dict(N=(1 << 30) + 1, ldo=1 << 31),
                 dict(n=1 << 28), dict(base=258, ldb=32), dict(ws=128), dict(status=258)):
+        assert _raw(**bad) == B.MOE_ERR_SHAPE, bad
+    for bad in (dict(), dict(x=512, w=256), dict(x=512, w=512, b=512), dict(x=512, w=512, a=512), dict(x=512, w=512, n=0, base=256, ldb=40)):      # overlapping
         assert _raw(**bad) == B.MOE_ERR_SHAPE, bad
     for bad in (dict(K=60), dict(ldx=68), dict(ldw=68), dict(rank=12), dict(out_type=2)):
         assert _raw(**bad) == B.MOE_ERR_UNSUPPORTED, bad
