@@ -19,7 +19,7 @@
 //     groups' scores are taken in 64 bits (keep64).
 // Bound by instruction issue and, for few tokens, by the length of one token's chain, not by the logits' bytes (16384 x 256 in
 // fp32 are 2.7 us of HBM time): about 870 instructions per token with 256 experts in groups with a bias (gate_kernel), 470 in
-// gate_many_kernel.  One token: 2.0 us, 32 tokens of the widest rule 3.0 us, both launch and latency; more at launch_gate.
+// gate_many_kernel (22.7 us).  One token: 2.0 us, 32 tokens of the widest rule 3.0 us, both launch and latency; more at launch_gate.
 // With random logits about 3 % of the tokens of that rule have neighbours that the keys leave undecided.
 #include <float.h>
 
@@ -581,6 +581,7 @@ gate_many_kernel(const GateArgs p)
     const int t0 = (blockIdx.x * kGateWarps + warp) * 8, t = t0 + (lane >> 2);
     const bool live = t < p.T;
     const int blocks = (p.E + 31) >> 5;
+    const bool whole = (p.E & 31) == 0;
     {
         float4 q[2 * NB];
 #pragma unroll
@@ -700,7 +701,7 @@ gate_many_kernel(const GateArgs p)
                         v = (SIGMOID ? rcp(1.f + ex2(-v * kLog2e)) : (v == -INFINITY ? 0.f : ex2((v - zmax) * kLog2e) * inv_sum)) + clean_bias(bv[i]);
                     }
                     key[4 * h + i] = (order_key(fmaxf(v, -FLT_MAX)) & ~kIdMask) | (kIdMask - e - i);
-                    if (e + i >= p.E) key[4 * h + i] = 0u;
+                    if (!whole && e + i >= p.E) key[4 * h + i] = 0u;
                 }
             }
             sort_desc<8>(key);
@@ -820,15 +821,17 @@ gate_many_kernel(const GateArgs p)
             }
             if (close) { kept = again; unsure = more; }
         }
-        const int shift = 31 - __clz(run);
+        // (every token goes over its own groups, keep of them: the places of a lane in s_z are its own in any block)
 #pragma unroll 1
-        for (int b = 0; b < blocks; ++b) {
-            const bool mine = kept >> (b >> shift) & 1;
-            const uint4* keys = reinterpret_cast<const uint4*>(&s_z[warp][2 * b][lane]);
-            const uint4 x = keys[0], y = keys[32];
-            const uint32_t key[8] = {mine ? x.x : 0u, mine ? x.y : 0u, mine ? x.z : 0u, mine ? x.w : 0u,
-                                     mine ? y.x : 0u, mine ? y.y : 0u, mine ? y.z : 0u, mine ? y.w : 0u};
-            merge(key);
+        for (uint32_t left = kept; left; left &= left - 1) {
+            const int first = (__ffs(left) - 1) * run;
+#pragma unroll 1
+            for (int o = 0; o < run; ++o) {
+                const uint4* keys = reinterpret_cast<const uint4*>(&s_z[warp][2 * (first + o)][lane]);
+                const uint4 x = keys[0], y = keys[32];
+                const uint32_t key[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                merge(key);
+            }
         }
     }
 
@@ -1020,13 +1023,15 @@ cudaError_t launch_gate(const GateArgs& in, cudaStream_t st)
     p.eligible = p.keep < p.n_groups ? p.keep * p.group_size : p.E;
     // Four lanes per token where there are tokens enough for its longer chain, and the groups are runs of 1, 2, 4 or 8 blocks of
     // 32 compared by what orders the experts (sums of scores beside an order by logits stay with the other kernel).  Measured, one
-    // warp per token / four lanes per token, us: 60 experts, softmax: 4096 tokens 5.4 / 4.8, 8192 8.1 / 5.8, 32768 24 / 11;
-    // 128, sigmoid, bias: 4096 6.6 / 6.1, 8192 10.1 / 7.6, 32768 31 / 15; 128 in 4 groups: 4096 7.1 / 8.3, 8192 10.9 / 9.7;
-    // 256 in 8 groups: 8192 14.8 / 18.0, 16384 25.2 / 24.0, 32768 47 / 38; 256, softmax, bias (ties through gate_token):
-    // 16384 24.8 / 31.1, 32768 45.2 / 44.3.
+    // warp per token / four lanes per token, us: 60 experts, softmax: 2048 tokens 3.8 / 4.4, 4096 5.0 / 4.6, 32768 24 / 11; 96, sigmoid,
+    // bias: 4096 6.7 / 5.5; 128 in 4 groups, sigmoid, bias: 4096 7.0 / 7.8, 8192 10.8 / 9.0; 256, softmax: 4096 7.3 / 7.6, 8192
+    // 12.1 / 9.7; 256 in 8 groups, sigmoid, bias: 8192 14.8 / 17.6, 16384 25.2 / 22.7, 32768 47 / 36.  With a softmax and a bias, whose
+    // near ties go through gate_token: 128 in 4 groups 8192 12.4 / 15.4, 16384 20.8 / 18.8; 256: 16384 24.8 / 30.3, 32768 45.5 / 44.3.
     const int run = p.group_size / 32;
-    const bool blocks = p.keep == p.n_groups || (p.group_size % 32 == 0 && (run & (run - 1)) == 0 && (p.bias || p.group_score == MOE_GROUP_MAX));
-    const int many_from = p.E <= 128 ? 8192 : (p.score == MOE_SCORE_SOFTMAX && p.bias ? 32768 : 16384);
+    const bool grouped = p.keep < p.n_groups;
+    const bool blocks = !grouped || (p.group_size % 32 == 0 && (run & (run - 1)) == 0 && (p.bias || p.group_score == MOE_GROUP_MAX));
+    int many_from = p.E <= 128 ? (grouped ? 8192 : 4096) : (p.bias ? 16384 : 8192);
+    if (p.score == MOE_SCORE_SOFTMAX && p.bias) many_from = p.E <= 128 ? 16384 : 32768;
     // groups that fall on whole lanes, a power of two of them, are reduced by shuffles, others through shared memory
     const int lanes = p.group_size / C;
     p.lanes_per_group = p.group_size % C == 0 && (lanes & (lanes - 1)) == 0 ? lanes : 0;

@@ -246,7 +246,8 @@ def check_repeated(rows, T, k, bias=None, dtype=torch.float32, pad=0, seed=0, **
 LONG = [(8192, 60, 4, {}), (8199, 64, 8, {}), (8192, 7, 3, {}), (8193, 1, 1, {}), (8200, 100, 8, {}), (8192, 128, 8, dict(n_groups=4, keep=2)),
         (8195, 128, 5, dict(n_groups=2, keep=1)), (8192, 96, 8, dict(n_groups=3, keep=2)), (8192, 60, 4, dict(n_groups=4, keep=2)),
         (8192, 8, 8, {}), (8192, 64, 7, dict(n_groups=2, keep=1)), (16387, 256, 8, {}), (16384, 256, 8, dict(n_groups=8, keep=4)), (16390, 200, 6, {}),
-        (16384, 256, 7, dict(n_groups=4, keep=1)), (16384, 256, 1, dict(n_groups=2, keep=1)), (32768, 256, 8, dict(n_groups=8, keep=3))]
+        (16384, 256, 7, dict(n_groups=4, keep=1)), (16384, 256, 1, dict(n_groups=2, keep=1)), (32768, 256, 8, dict(n_groups=8, keep=3)),
+        (16385, 60, 4, {}), (16391, 128, 8, dict(n_groups=4, keep=3)), (4097, 64, 8, {}), (4100, 128, 6, {}), (8193, 256, 8, dict(n_groups=8, keep=2))]
 
 
 @gpu
@@ -263,7 +264,7 @@ def test_long_batches(T, E, k, groups):
 
 @gpu
 @pytest.mark.parametrize("T,E,groups", [(8192, 60, {}), (8192, 128, dict(n_groups=4, keep=2)), (16384, 256, dict(n_groups=8, keep=4)), (16384, 256, {}),
-                                        (32768, 256, dict(n_groups=2, keep=1))])
+                                        (32768, 256, dict(n_groups=2, keep=1)), (16384, 60, {}), (16384, 128, dict(n_groups=4, keep=2))])
 @pytest.mark.parametrize("k", [1, 5, 7, 8])
 def test_long_batches_of_ties_and_near_ties(T, E, groups, k):
     """Exact ties, values that only 64 bits tell apart, masked and extreme rows, at the k-th rank and between groups."""
@@ -292,14 +293,15 @@ def test_long_batches_of_ties_and_near_ties(T, E, groups, k):
 
 
 @gpu
-def test_long_batches_of_several_models():
+@pytest.mark.parametrize("T,score", [(8300, "sigmoid"), (16400, "softmax")])
+def test_long_batches_of_several_models(T, score):
     g = np.random.default_rng(21)
-    T, E, M, k = 8300, 60, 4, 4
+    E, M, k = 60, 4, 4
     z = g.standard_normal((T, E))
     tenant, mot = g.integers(0, 9, T), np.arange(9) % M
     tenant[[3, T - 1]] = [9, -2]
     bias = g.standard_normal((M, E)) * 0.2
-    rule = dict(score="sigmoid", renorm=True)
+    rule = dict(score=score, renorm=True)
     idx, w, _, status = run(z, k, bias=bias, tenant=tenant, mot=mot, **rule)
     assert status == B.MOE_DEV_BAD_TENANT
     ok = (tenant >= 0) & (tenant < 9)
