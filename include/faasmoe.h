@@ -347,7 +347,7 @@ int moe_gate(const void* logits, int logits_type, int64_t ld, int T, int E, int 
  * Makes moe_route, and with it every call that runs the layer, use a gating rule in layer `layer` (all its models):
  * z = x . router_w^T + router_bias as before, then the rule above with balance_bias (device f32 [M, E] or NULL, used in
  * place).  rule is a host pointer and is copied; NULL returns to moe_route's own rule (softmax, raw probabilities).
- * Set between calls, not while one may still run.
+ * Set between calls, not while one may still run; a captured graph keeps the rule that it was captured with.
  */
 int moe_set_gating(moe_ctx* ctx, int layer, const moe_gating* rule, const float* balance_bias);
 

@@ -235,6 +235,7 @@ static PyObject* call_gate(PyObject* self, PyObject* const* a, Py_ssize_t n)
         flat(&c, a[8], "status_out", 1, t_i32, &status, NULL) < 0)
         goto done;
     if (!mot) n_tenants = 1 << 30;
+    if (too_large(&c, n_tenants, M)) goto done;
     const int where = stream_of(&c, a[9], &raw);
     if (where < 0 || PyObject_GetBuffer(a[1], &rule, PyBUF_SIMPLE) < 0) goto done;
     const int rc = where ? kOtherDevice

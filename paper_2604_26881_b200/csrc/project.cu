@@ -27,6 +27,9 @@ using namespace tc;
 
 __device__ int32_t g_project_status;      // where the status bits go of calls that did not ask for them
 
+// TMEM: the CTAs of these kernels that fit one SM together ask for 512 columns at most (by registers two of project_kernel, 256
+// columns each at most, or one and two of adapter_kernel, 128, or four of those), and a kernel that takes all 512 leaves no
+// shared memory for a cluster of either.  So an allocation never waits for a cluster that waits for it, whatever other streams run.
 constexpr uint32_t kFull = 0xffffffffu;
 constexpr int kTok = 128;               // tokens per tile: the M operand, one TMEM lane each
 constexpr int kBK = 64;                 // K elements per slice: one 128-byte row of a swizzled tile

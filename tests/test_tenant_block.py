@@ -5,6 +5,10 @@ Checked against the formulas in 64 bits at the layer's own tolerances (rtol 2e-2
 intermediates, fp32 accumulation); the choice of experts must equal the 64-bit rule wherever its values are not closer than the
 fp32 logits can tell (1e-4, far above the rounding of sums of 256 products of order one).
 """
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -116,3 +120,67 @@ def test_block_with_tenants_adapters(T, graph):
     ys = projected(c["act"].double(), "down")
     assert close(c["ys"], ys)
     assert close(c["out"], routed + ys)
+
+
+FIRST_CALLS = """
+import torch
+from paper_2604_26881_b200 import binding as B
+dev = "cuda:0"
+rnd = lambda *s: torch.randn(*s, device=dev).bfloat16()
+w, a, b = rnd(320, 256), rnd(3, 16, 256), rnd(3, 320, 16)
+calls = []
+for T in (2, 40, 700, 9000):
+    x, out, y, z = rnd(T, 256), torch.zeros(T, 320, device=dev), rnd(T, 256), torch.randn(T, 64, device=dev)
+    idx, wt, tenant = torch.zeros(T, 4, dtype=torch.int32, device=dev), torch.zeros(T, 4, device=dev), (torch.arange(T, device=dev) % 3).int()
+    calls.append((lambda x=x, out=out, tenant=tenant: B.moe_project(x, w, out, a=a, b=b, tenant_id=tenant), out))
+    calls.append((lambda z=z, idx=idx, wt=wt: B.moe_gate(z, B.moe_gating(), idx, wt), wt))
+    calls.append((lambda x=x, y=y: B.moe_add_rmsnorm(x, w.view(-1)[:256], 1e-6, out=y), y))
+torch.cuda.synchronize()
+for run, out in calls:
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    replayed = out.clone()
+    run()
+    torch.cuda.synchronize()
+    assert torch.equal(replayed, out) and out.float().abs().sum() > 0
+print("captured")
+"""
+
+
+def test_first_calls_of_a_process_may_be_captured():
+    """Kernels are loaded, and launch shapes looked up, inside the capture."""
+    done = subprocess.run([sys.executable, "-c", FIRST_CALLS], capture_output=True, text=True, timeout=300,
+                          cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert done.returncode == 0 and "captured" in done.stdout, done.stdout + done.stderr
+
+
+def test_calls_on_three_streams_at_once():
+    """Launches of different shapes share the SMs, their tensor memory included; each gives what it gives alone."""
+    g = torch.Generator(device="cuda:0").manual_seed(5)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda:0").mul_(0.1).bfloat16()
+    w, a, b = rnd(1408, 1024), rnd(40, 16, 1024), rnd(40, 1408, 16)
+    sizes = (3, 50, 200, 700, 2000, 4)
+    work = []
+    for T in sizes:
+        x, tenant = rnd(T, 1024), (torch.arange(T, device="cuda:0") % 40).int()
+        alone, out = torch.empty(T, 1408, device="cuda:0"), torch.empty(T, 1408, device="cuda:0")
+        call = lambda o, x=x, tenant=tenant: B.moe_project(x, w, o, a=a, b=b, tenant_id=tenant)
+        call(alone)
+        work.append((call, alone, out))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for rep in range(20):
+        for i, (call, alone, out) in enumerate(work):
+            out.zero_()
+        torch.cuda.synchronize()
+        for i, (call, alone, out) in enumerate(work):
+            with torch.cuda.stream(streams[(i + rep) % 3]):
+                for _ in range(3):
+                    call(out)
+        torch.cuda.synchronize()
+        for call, alone, out in work:
+            assert torch.equal(alone, out)
