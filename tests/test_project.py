@@ -171,6 +171,27 @@ def test_rings_that_wrap_many_times(rank):
 
 
 @gpu
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [2, 20, 130, 300, 900])
+def test_what_the_workspace_held_does_not_matter(T, out):
+    """Tokens without an adapter leave their rows of the workspace as they were: NaN there reaches nobody."""
+    K, N, rank, n = 512, 300, 24, 5
+    d = inputs(T, K, N, rank, n, 8, base=True, out=out)
+    g = {k: v.to(DEV) for k, v in d.items()}
+    tenant = tenants(T, n + 3, "uniform", 2).to(DEV)                # (three tenants have no adapter)
+    results = []
+    for weight in (g["w"], None):
+        for fill in (0, 255):
+            ws = torch.full((max(256, B.moe_project_workspace(T, K, N, rank, n)),), fill, dtype=torch.uint8, device=DEV)
+            o = torch.empty(T, N, dtype=out, device=DEV)
+            B.moe_project(g["x"], weight, o, base=g["base"], a=g["a"], b=g["b"], scale=g["scale"], tenant_id=tenant, n_tenants=n + 3, workspace=ws)
+            results.append(o)
+    torch.cuda.synchronize()
+    assert torch.equal(results[0], results[1]) and torch.equal(results[2], results[3])
+    assert all(bool(o.isfinite().all()) for o in results)
+
+
+@gpu
 @pytest.mark.parametrize("T,what", [(100, "x"), (100, "w"), (100, "out"), (600, "x"), (600, "w"), (600, "out")])
 def test_rows_beyond_32_bit_offsets(T, what):
     """Rows so far apart that the last ones lie beyond 2^31 elements, of each matrix in turn, in either shape."""
