@@ -10,7 +10,7 @@
 // same pass over x, and there is one launch only.
 //
 // Few tokens are a chain of latencies (ids, list, TMA, MMA, exchange in the cluster, the launch boundary, second product), not
-// bytes: 2048 -> 2048, rank 16, one token 9.8 us (8.5 MB, 1.3 us of HBM time); 2048 -> 5632, 32 tokens of 32 adapters 14.0 us
+// bytes: 2048 -> 2048, rank 16, one token 9.8 us (8.5 MB, 1.3 us of HBM time); 2048 -> 5632, 32 tokens of 32 adapters 13.6 us
 // (31.8 MB, 4.9 us).  Many tokens are bound by the tensor cores: 5632 -> 2048, 4096 tokens of 16 adapters of rank 16 75 to 77 us (95
 // GFLOP, 1.25 PFLOP/s, 0.76 of the measured peak); the adapters alone beside a base, 1126 tokens, 13 of rank 64: 26 us, first
 // product 12 of them.
@@ -407,6 +407,10 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
 
 struct PMaps { CUtensorMap x, w, a; };
 
+// The columns of a tile that CTA i of n adds up and writes.
+__host__ __device__ constexpr int first_column(int i, int n) { return kPN / 2 * i / n * 2; }
+__host__ __device__ constexpr int most_columns(int n) { return (kPN / 2 + n - 1) / n * 2; }
+
 // Few tokens: one cluster of `splits` CTAs per tile of 128 tokens x 128 weight rows; each CTA contracts over its share of K
 // into its own TMEM accumulator and sends every column's sums to the CTA that adds that column up (distributed shared
 // memory; the parts are added in their order: the same bits every time).  The adapters' second product and the base
@@ -442,8 +446,10 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
     // Behind the ring (and the rows that the MMA of a short tile may read): the sums sent here, [part][own column][token], then
     // (fused) the parts of u, [part][rank][token], then u itself, [token][rank].  This CTA's own sums, [column][token] of
     // the product and of u, are put together in the ring when its stages are done.
-    const int c0 = (int)(kPN * rank) / S, nc = (int)(kPN * (rank + 1)) / S - c0, nc_max = (kPN + S - 1) / S;
-    const int pitch = p.a_rows + 4;
+    // (columns in twos and a pitch of twice an odd number: a CTA's share is whole 16 bytes, and neighbouring columns meet in a bank in
+    // pairs only; in fours and with an odd pitch never, but the largest share would be an extra round of outputs for 64 tokens)
+    const int c0 = first_column((int)rank, S), nc = first_column((int)rank + 1, S) - c0, nc_max = most_columns(S);
+    const int pitch = p.a_rows + 2;
     float* const own = reinterpret_cast<float*>(smem_dyn + (ring - smem_u32(smem_dyn)));
     float* const own_u = own + kPN * pitch;
     float* const part = reinterpret_cast<float*>(smem_dyn + (ring - smem_u32(smem_dyn)) + p.scratch);
@@ -610,7 +616,7 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
             if (lane == 0) mbar_expect_tx(bar_got, S * ((product ? nc : 0) + (FUSED ? p.rank : 0)) * pitch * 4);
             __syncwarp();
             if (lane < S) {
-                const int to = lane, d0 = kPN * to / S, dn = kPN * (to + 1) / S - d0;
+                const int to = lane, d0 = first_column(to, S), dn = first_column(to + 1, S) - d0;
                 const uint32_t bar = map_to_cta(bar_got, to);
                 if (product)
                     send_bulk(map_to_cta(smem_u32(part + (int)rank * nc_max * pitch), to), smem_u32(own + d0 * pitch), dn * pitch * 4, bar);
@@ -1220,14 +1226,14 @@ int cluster_room(int size, bool two)
 bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind, int beside = 0)
 {
     static_assert(kPN == kTok, "");
-    const int tiles = tiles_of(p, kPN), pitch = p.a_rows + 4;
+    const int tiles = tiles_of(p, kPN), pitch = p.a_rows + 2;
     const bool joint = p.w || fused;                        // (otherwise the parts only share the columns)
     p.stage_bytes = p.a_bytes + (p.w ? kPN * kBK * 2 : 0) + ((u_rows + 15) & ~15) * kBK * 2;
     // as many parts as there are SMs for the tiles (a cluster holds eight), of two slices at least, all clusters at once
     for (p.splits = 8; ; --p.splits) {
         if (p.splits > 1 && (p.splits == 5 || p.splits == 7 || p.splits * tiles > 148 || (joint && p.splits > p.ksteps / 2))) continue;
         // received: the parts of this CTA's columns, (fused) the parts of u; and u itself
-        p.sums_bytes = (p.splits * div_up(kPN, p.splits) * pitch + (fused ? p.splits * p.rank * pitch : 0) + p.a_rows * p.rank) * (int)sizeof(float);
+        p.sums_bytes = (p.splits * most_columns(p.splits) * pitch + (fused ? p.splits * p.rank * pitch : 0) + p.a_rows * p.rank) * (int)sizeof(float);
         const int own = (kPN + (fused ? p.rank : 0)) * pitch * (int)sizeof(float);
         const int want = joint ? div_up(p.ksteps, p.splits) : 1;
         auto stages = [&](int bytes) {                      // the ring, or this CTA's own sums that are put together in it
