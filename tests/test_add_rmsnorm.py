@@ -256,3 +256,24 @@ def test_binding_checks_tensors():
             B.moe_add_rmsnorm(x, w, 1e-6, **kw)
     with pytest.raises(ValueError):
         B.moe_add_rmsnorm(x, w.float(), 1e-6, out=x)
+
+
+@gpu
+@pytest.mark.parametrize("q", ["row", "group"])
+def test_quotients_are_rounded_once_to_8_bits(q):
+    """out_q = e4m3(y / s) of the fp32 y and s, bit for bit.  With h = +-1 and eps = 0 the mean is 1 and y = +-weight, both exact,
+    so y / s is an fp32 quotient of known numbers; some of them are in the middle of two 8-bit floats, or an fp32 step beside it."""
+    g = torch.Generator().manual_seed(0)
+    H, size = 16384, 16384 if q == "row" else 128
+    for _ in range(8 if q == "row" else 3):
+        w = (torch.randn(H, generator=g) * 2).to(torch.bfloat16)
+        x = torch.where(torch.rand(2, H, generator=g) < 0.5, -1.0, 1.0).to(torch.bfloat16)
+        y = (x.float() * w.float()).view(2, H // size, size)
+        s = y.abs().amax(2) / 448
+        want = (y / s[:, :, None]).view(2, H).to(torch.float8_e4m3fn)
+        out_q, scale = torch.empty(2, H, dtype=torch.float8_e4m3fn, device="cuda:0"), torch.empty(2, H // size, device="cuda:0")
+        B.moe_add_rmsnorm(x.cuda(), w.cuda(), 0.0, out_q=out_q, q_scale=scale)
+        torch.cuda.synchronize()
+        assert torch.equal(scale.cpu(), s)
+        bad = out_q.cpu().view(torch.uint8) != want.view(torch.uint8)
+        assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} differ"
