@@ -34,6 +34,7 @@ constexpr uint32_t kFull = 0xffffffffu;
 constexpr int kTok = 128;               // tokens per tile: the M operand, one TMEM lane each
 constexpr int kBK = 64;                 // K elements per slice: one 128-byte row of a swizzled tile
 constexpr int kMaxStages = 8;
+constexpr int kUTerms = 3;              // bf16 numbers that add up to an fp32 one: 8 bits each
 constexpr int kUCols = 128;             // columns of one CTA of the first product
 constexpr int kUThreads = 288;          // warp 0: TMA (tokens), 1, 7: MMA, 2..5: lists and epilogue, 6, 8: TMA (rows of A)
 constexpr int kPN = 128;                // weight rows per tile of the projection
@@ -379,10 +380,10 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
                 v *= s_scale[row];
                 w *= s_scale[row];
                 const size_t at = (size_t)(t0 + row) * p.rank + c;
-                if (p.u_terms > 0) {
+                if (p.u_split) {
                     // each term is what the ones before left over (what rounds to an infinity, or is one, leaves nothing)
                     bf16* u = reinterpret_cast<bf16*>(p.u) + at;
-                    for (int h = 0; h < p.u_terms; ++h, u += (size_t)p.T * p.rank) {
+                    for (int h = 0; h < kUTerms; ++h, u += (size_t)p.T * p.rank) {
                         const __nv_bfloat162 term = __floats2bfloat162_rn(v, w);
                         const float2 f = __bfloat1622float2(term);
                         *reinterpret_cast<__nv_bfloat162*>(u) = term;
@@ -747,9 +748,8 @@ project_kernel(const ProjectArgs p, const __grid_constant__ PMaps maps)
 // Many tokens: 256 tokens x 256 weight rows per pair of CTAs (tcgen05.mma.cta_group::2; each CTA holds 128 of either), pairs
 // that walk over the tiles, two accumulators of 256 TMEM columns so that a tile's epilogue runs behind the next tile's MMAs.
 //
-// The adapters' second products go into the same accumulator: u of the tile's tokens is one more M operand (bf16 tiles that
-// add up to the fp32 value: two, 16 bits of it, for a bf16 output, where a single one would cost 2^-9 of the adapter's share;
-// three, all 24 bits, for an fp32 output, which two would leave 1.7e-6 off where fp32 sums are 3e-7), and
+// The adapters' second products go into the same accumulator: u of the tile's tokens is one more M operand, three bf16 tiles that
+// add up to the fp32 value, and
 // for every distinct adapter of the tile the rows of its B are one more N operand.  Which tokens that MMA may change is said by
 // its disable-output-lane mask, so u needs no masked copy per adapter and an infinity or a NaN in one tenant's B
 // cannot reach another's tokens (a zeroed row of u would: 0 * inf).
@@ -927,7 +927,7 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
     const bool adapters = p.n_adapters > 0;
     const int n_tiles = (p.N + kMTile - 1) / kMTile, m_tiles = (p.T + kMTile - 1) / kMTile, total = n_tiles * m_tiles;
     const int pair0 = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int terms = p.u_terms, chunks = (p.rank + kBK - 1) / kBK;     // of u and of the adapters' B (0 without adapters)
+    const int chunks = (p.rank + kBK - 1) / kBK;            // of u and of the adapters' B
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < n_stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
@@ -977,11 +977,11 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
                                 // (the MMAs of the tile before have read theirs, and its epilogue is through with the memory)
                                 if (!mbar_wait(bar_uempty, (it & 1) ^ 1, &s_abort, status) ||
                                     !mbar_wait(bar_staged, (it & 1) ^ 1, &s_abort, status)) { ok = false; break; }
-                                if (leader) mbar_expect_tx(bar_ufull, 2 * terms * chunks * kUTile);
+                                if (leader) mbar_expect_tx(bar_ufull, 2 * kUTerms * chunks * kUTile);
                                 u_loads = it + 1;
                                 for (int c = 0; c < chunks; ++c)
-                                    for (int h = 0; h < terms; ++h)
-                                        tma_load_3d_pair(ua + (c * terms + h) * kUTile, &maps.u, bar_ufull, c * kBK, t0, h);
+                                    for (int h = 0; h < kUTerms; ++h)
+                                        tma_load_3d_pair(ua + (c * kUTerms + h) * kUTile, &maps.u, bar_ufull, c * kBK, t0, h);
                             }
                         }
                     }
@@ -1054,8 +1054,8 @@ project_many_kernel(const ProjectArgs p, const __grid_constant__ MMaps maps)
                             tc_fence_after();
                             const uint32_t lo_b = smem_desc_lo(ring + stage * kMStageBytes + kTok * kBK * 2);
                             const int kks = (min(kBK, p.rank - c * kBK) + 15) >> 4;
-                            for (int h = 0; h < terms; ++h) {
-                                const uint32_t lo_a = smem_desc_lo(ua + (c * terms + h) * kUTile);
+                            for (int h = 0; h < kUTerms; ++h) {
+                                const uint32_t lo_a = smem_desc_lo(ua + (c * kUTerms + h) * kUTile);
                                 for (int kk = 0; kk < kks; ++kk) {
                                     umma_pair_masked(d, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, first, mask);
                                     first = 1;
@@ -1276,7 +1276,7 @@ bool use_many(const ProjectArgs& p)
     if (distinct > p.n_adapters) distinct = p.n_adapters;
     const bool adapters = p.n_adapters > 0;
     const float few = (adapters ? 8.8f : 7.7f) + waves * (0.6f * steps / parts + 0.009f * rows + 1.2e-4f * rows * kPN / parts * (adapters ? p.rank : 0));
-    const float many = (p.w ? 10.3f : 13.5f) - (adapters ? 0.f : 3.1f) + rounds * (0.25f * steps + distinct * (0.48f + 0.0083f * p.rank * (p.out_f32 ? 1.5f : 1.f)));
+    const float many = (p.w ? 10.3f : 13.5f) - (adapters ? 0.f : 3.1f) + rounds * (0.25f * steps + distinct * (0.48f + 0.0125f * p.rank));
     return many < few;
 }
 
@@ -1363,7 +1363,7 @@ int64_t project_workspace(int T, int K, int N, int rank, int n_adapters)
     ProjectArgs p = {};
     p.T = T; p.K = K; p.N = N; p.rank = rank; p.n_adapters = n_adapters;
     if (plan_few(p) && (p.w = reinterpret_cast<const bf16*>(16), plan_few(p))) return 0;      // (with w and without)
-    return (int64_t)T * rank * 6;        // fp32, or up to three bf16 terms
+    return (int64_t)T * rank * 2 * kUTerms;        // bf16 terms (fp32, which few tokens take, is less)
 }
 
 cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
@@ -1372,7 +1372,7 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
     static bool u_ok[kMaxDevices] = {false}, p_ok[kMaxDevices] = {false}, f_ok[kMaxDevices] = {false}, m_ok[kMaxDevices] = {false};
     const int m_tiles = div_up(p.T, kTok), n_tiles = div_up(p.N, kPN);
     const bool adapters = p.n_adapters > 0, fused = plan_few(p), many = !fused && use_many(p);
-    p.u_terms = many ? (p.out_f32 ? 3 : 2) : 0;
+    p.u_split = many;
     ProjectArgs q;
     int chunks = 0;
     const size_t u_smem = adapters && !fused ? adapter_geometry(p, many, q, chunks) : 0;
@@ -1410,9 +1410,9 @@ cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)
         if (!p.w) p.ksteps = 0;
         if (p.w && (!make_map_ld(&mm.x, p.x, p.T, p.K, p.ldx, kTok) || !make_map_ld(&mm.w, p.w, p.N, p.K, p.ldw, kTok)))
             return cudaErrorInvalidValue;
-        if (adapters && (!make_map_3d(&mm.b, p.b, p.n_adapters, p.N, p.rank, kBRows) || !make_map_3d(&mm.u, p.u, p.u_terms, p.T, p.rank, kTok)))
+        if (adapters && (!make_map_3d(&mm.b, p.b, p.n_adapters, p.N, p.rank, kBRows) || !make_map_3d(&mm.u, p.u, kUTerms, p.T, p.rank, kTok)))
             return cudaErrorInvalidValue;
-        const int u_tiles = adapters ? p.u_terms * div_up(p.rank, kBK) : 0;      // 32 to 96 KB, which leave five to three stages
+        const int u_tiles = adapters ? kUTerms * div_up(p.rank, kBK) : 0;      // 48 or 96 KB, which leave five or three stages
         p.n_stages = (kMaxSmem - 1024 - u_tiles * kUTile) / kMStageBytes;
         if (p.n_stages > kMStages) p.n_stages = kMStages;
         size_t behind_ring = (size_t)u_tiles * kUTile;

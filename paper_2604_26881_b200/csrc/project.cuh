@@ -20,10 +20,10 @@ struct ProjectArgs {
     int64_t ldx, ldw, ldbase, ldo;
     int out_f32;
     int T, K, N, n_adapters, rank, n_tenants;
-    float* u;                       // workspace: [T][rank], f32 or up to three bf16 arrays; not used where the first product is fused
+    float* u;                       // workspace: [T][rank], f32 or three bf16 arrays; not used where the first product is fused
     int32_t* status;                // the caller's, or null
     // set by launch_project
-    int u_terms;                    // u is stored as so many bf16 terms (0: f32)
+    int u_split;                    // u is stored as three bf16 terms, not as f32
     int u_splits;                   // parts of K of the first product (a cluster)
     int ksteps, splits, n_stages, stage_bytes, a_bytes, a_rows;
     int u_own;                      // tokens of a tile that one CTA of such a cluster adds up

@@ -440,3 +440,33 @@ def test_binding_checks_tensors():
     for bad in ((x.float(), w, out), (x, w[:, :32], out), (x, w, out.double()), (x[0], w, out), (x, w.t(), out)):
         with pytest.raises(ValueError):
             B.moe_project(*bad)
+
+
+@gpu
+@pytest.mark.parametrize("T", [3, 20, 130, 300, 900, 4000])
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("weight", [True, False])
+def test_an_inner_product_has_32_bits_in_batches_of_any_length(T, out, weight):
+    """A base that takes the adapter's share back but for its rounding: what is left shows u to its last bits.  One product per output:
+    u = scale * a is one fp32 rounding, its product with b is cut to 24 bits at most once per term it is handed over in (three) and
+    once more where the base is added: 2^-24 + 4 * 2^-23 of |u b|, below 2^-20; then the output's own half step."""
+    K, N, rank, n = 64, 200, 16, 5
+    g = torch.Generator().manual_seed(T)
+    a, b = torch.zeros(n, rank, K), torch.zeros(n, N, rank)
+    a[:, 0, 0] = torch.rand(n, generator=g) + 0.5
+    b[:, :, 0] = torch.rand(n, N, generator=g) + 0.5
+    a, b, scale = a.to(torch.bfloat16), b.to(torch.bfloat16), torch.rand(n, generator=g) + 0.5
+    x = torch.zeros(T, K)
+    x[:, 0] = torch.rand(T, generator=g) + 0.5
+    x = x.to(torch.bfloat16)
+    adapter = torch.arange(T) % n
+    share = (x[:, :1].double() * a[adapter, 0, :1].double() * scale[adapter].double()[:, None]) * b[adapter, :, 0].double()
+    base = (-share).to(torch.bfloat16).to(out)
+    y = share + base.double()
+    o, dev = torch.empty(T, N, dtype=out, device=DEV), lambda t: t.to(DEV)
+    w = torch.zeros(N, K, dtype=torch.bfloat16, device=DEV) if weight else None             # (adds nothing, but takes other shapes)
+    B.moe_project(dev(x), w, o, base=dev(base), a=dev(a), b=dev(b), scale=dev(scale), tenant_id=dev(adapter.to(torch.int32)))
+    torch.cuda.synchronize()
+    lim = 2.0 ** -20 * share.abs() + (2.0 ** -8 if out == torch.bfloat16 else 2.0 ** -24) * y.abs()
+    off = (o.double().cpu() - y).abs()
+    assert (off <= lim).all(), f"{int((off > lim).sum())} of {off.numel()}, worst {float((off / lim).max()):.1f} of the bound"
