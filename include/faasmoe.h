@@ -373,6 +373,7 @@ int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld
  *   out[t] = base[t] + x[t] . w^T + scale[a] * (x[t] . a[a]^T) . b[a]^T,    a = adapter_of_tenant[tenant_id[t]]
  * for all tokens of a batch in one call, in whatever order their tenants come.  bf16 operands, fp32 sums (the inner product of
  * an adapter stays fp32, or three bf16 numbers that add up to it), one rounding to out's type.
+ * Infinities and NaN give what they give in the formula, in their own tokens and columns.
  *   x      bf16 [T, K], rows ldx apart            w      bf16 [N, K], rows ldw apart, or NULL (no product with w)
  *   base   [T, N] of out's type, rows ld_base apart, or NULL; may be out itself (same row distance)
  *   a      bf16 [n_adapters, rank, K]             b      bf16 [n_adapters, N, rank]         scale f32 [n_adapters] or NULL (1)

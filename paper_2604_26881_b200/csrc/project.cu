@@ -381,14 +381,19 @@ adapter_kernel(const ProjectArgs p, const __grid_constant__ UMaps maps)
                 w *= s_scale[row];
                 const size_t at = (size_t)(t0 + row) * p.rank + c;
                 if (p.u_split) {
-                    // each term is what the ones before left over (what rounds to an infinity, or is one, leaves nothing)
+                    // Each term is cut, not rounded, and the next is what it left over, so all have the sign of u: with an infinity in B
+                    // terms of both signs, or a zero, would add up to NaN.  For the same reason nothing left over is handed on as
+                    // 2^-32 of u, which 24 bits do not see (but for u below 2^-101), and what is left of an infinity as that infinity.
                     bf16* u = reinterpret_cast<bf16*>(p.u) + at;
+                    const float2 trace = make_float2(v * 0x1p-32f, w * 0x1p-32f);
                     for (int h = 0; h < kUTerms; ++h, u += (size_t)p.T * p.rank) {
-                        const __nv_bfloat162 term = __floats2bfloat162_rn(v, w);
+                        const __nv_bfloat162 term = __halves2bfloat162(__float2bfloat16_rz(v), __float2bfloat16_rz(w));
                         const float2 f = __bfloat1622float2(term);
                         *reinterpret_cast<__nv_bfloat162*>(u) = term;
-                        v = isinf(f.x) ? 0.f : v - f.x;
-                        w = isinf(f.y) ? 0.f : w - f.y;
+                        if (!isinf(f.x)) v -= f.x;
+                        if (!isinf(f.y)) w -= f.y;
+                        if (v == 0.f) v = trace.x;
+                        if (w == 0.f) w = trace.y;
                     }
                 } else {
                     *reinterpret_cast<float2*>(p.u + at) = make_float2(v, w);

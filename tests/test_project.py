@@ -470,3 +470,34 @@ def test_an_inner_product_has_32_bits_in_batches_of_any_length(T, out, weight):
     lim = 2.0 ** -20 * share.abs() + (2.0 ** -8 if out == torch.bfloat16 else 2.0 ** -24) * y.abs()
     off = (o.double().cpu() - y).abs()
     assert (off <= lim).all(), f"{int((off > lim).sum())} of {off.numel()}, worst {float((off / lim).max()):.1f} of the bound"
+
+
+@gpu
+@pytest.mark.parametrize("rank", [8, 16, 72])
+@pytest.mark.parametrize("T", [3, 20, 130, 300, 900])
+@pytest.mark.parametrize("what", ["b", "u"])
+def test_single_infinities_stay_infinities(T, rank, what):
+    """One infinite element of B, or an infinite inner product: +-inf where the formula in 64 bits has it and NaN nowhere else, whatever
+    shape the batch takes and however the inner product is handed over."""
+    K, N, n = 128, 200, 4
+    for weight, out in ((True, torch.float32), (True, torch.bfloat16), (False, torch.float32), (False, torch.bfloat16)):
+        d = inputs(T, K, N, rank, n, T + rank, weight=weight, base=not weight, out=out, scale=False)
+        adapter = torch.arange(T) % n
+        if what == "b":
+            d["b"][0, 7, 3], d["b"][1, 50, 1], d["b"][2, 9, 2] = float("inf"), -float("inf"), float("inf")
+            # inner products of one bit, of which nothing is left to hand over behind the first term: 1, -2 and 2^-60
+            d["x"][:3] = 0
+            d["x"][0, 0], d["x"][1, 0], d["x"][2, 0] = 1, -2, 2.0 ** -60
+            d["a"][:3, :, 0] = 1
+        else:
+            d["a"][1, 3, 5], d["a"][2, 0, 6] = float("inf"), -float("inf")
+            d["x"][:, 5:7] = 1.0
+        y, _ = reference(d["x"], d["w"], d["base"], d["a"], d["b"], None, adapter)
+        g = {k: None if v is None else v.to(DEV) for k, v in d.items()}
+        o, status = torch.empty(T, N, dtype=out, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        B.moe_project(g["x"], g["w"], o, base=g["base"], a=g["a"], b=g["b"], tenant_id=adapter.to(torch.int32).to(DEV), status_out=status)
+        torch.cuda.synchronize()
+        got = o.double().cpu()
+        assert int(status) == 0 and bool(y.isinf().any()) and not y.isnan().any()
+        assert not got.isnan().any(), f"{int(got.isnan().sum())} NaN, first at {got.isnan().nonzero()[0].tolist()}"
+        assert torch.equal(got.isinf(), y.isinf()) and torch.equal(got[got.isinf()], y[y.isinf()])
