@@ -699,6 +699,7 @@ gate_many_kernel(const GateArgs p)
                     if constexpr (BIAS) {
                         // (the softmax of -inf is 0 also where the whole row is -inf)
                         v = (SIGMOID ? rcp(1.f + ex2(-v * kLog2e)) : (v == -INFINITY ? 0.f : ex2((v - zmax) * kLog2e) * inv_sum)) + clean_bias(bv[i]);
+                        v = fminf(v, FLT_MAX);                // (the id bits must not make a NaN of +inf either: the groups are compared by keys)
                     }
                     key[4 * h + i] = (order_key(fmaxf(v, -FLT_MAX)) & ~kIdMask) | (kIdMask - e - i);
                     if (!whole && e + i >= p.E) key[4 * h + i] = 0u;

@@ -555,3 +555,23 @@ def test_binding_checks_tensors():
         B.moe_set_gating(None, 0, rule, torch.zeros(1, 8))
     with pytest.raises(KeyError):
         B.moe_gating(score="tanh")
+
+
+@gpu
+@pytest.mark.parametrize("T,E,n_groups,keep,k", [(90, 256, 8, 4, 8), (16384, 256, 8, 4, 8), (16384, 256, 4, 1, 5), (16384, 128, 4, 2, 3), (32768, 256, 8, 2, 8)])
+def test_experts_forced_by_an_infinite_bias(T, E, n_groups, keep, k):
+    """A bias of +inf (or of the largest finite value, which is below it) puts its expert in front, ties to the lower id, and its group
+    among those that stay."""
+    g = np.random.default_rng(T + E + n_groups)
+    rows = g.standard_normal((60, E))
+    size = E // n_groups
+    for forced in ([3], [size + 1, E - 1], [5, 2 * size - 1, E - 2], list(range(0, E, size)), [2, 3, 4, 7, E - 3]):
+        for value in (np.inf, FMAX):
+            bias = g.standard_normal(E) * 0.05
+            bias[forced] = value
+            for score in ("softmax", "sigmoid"):
+                for group_score in ("max", "top2"):
+                    check_repeated(rows, T, k, bias=bias, score=score, n_groups=n_groups, keep=keep, group_score=group_score, renorm=True)
+    bias = g.standard_normal(E) * 0.05
+    bias[[1, size + 2]] = [FMAX, np.inf]
+    check_repeated(rows, T, k, bias=bias, score="sigmoid", n_groups=n_groups, keep=keep, renorm=True)
