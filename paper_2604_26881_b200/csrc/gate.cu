@@ -237,10 +237,11 @@ template <int C, bool SIGMOID, bool BIAS, bool GROUPS>
 struct Gate {
     static constexpr uint32_t kIdMask = 32 * C - 1;
     // Error bound of the difference of two 32-bit values:
-    //   softmax: (z - zmax) * log2 e rounds by 2^-24 relative (p * |ln p| <= 0.37), ex2 by 2 ulp, a sum of at most C + 5
-    //            additions in a row and the product by 1.5 ulp each: below 1.2e-6 * p;
+    //   softmax: the argument (z - zmax) * log2 e is off by 3 * 2^-24 of itself, which is at most 0.37 * 1.8e-7 in p (p |ln p| <= 0.37)
+    //            and, averaged over a row of 256, ln 256 * 1.8e-7 of the sum; ex2 by 2 ulp, 2.4e-7, in either; the sum by its C + 5
+    //            additions in a row, 7.8e-7; quotient and product 6e-8 each: below 2.5e-6 of p, and two p add up to 1 at most;
     //   sigmoid: the exponential below 2^-21 + 2^-24 |z| relative, times s (1 - s) <= 1/4, and a reciprocal of 1 ulp: below 4e-7;
-    // twice that for two, with room.  Ordered by logits the values are exact (1e-37: the key of a denormal has cleared bits too).
+    // twice that for two sigmoids, with room.  Ordered by logits the values are exact (1e-37: the key of a denormal has cleared bits too).
     static constexpr float kSlack = !BIAS ? 1e-37f : (SIGMOID ? 2e-6f : 4e-6f);
     static constexpr __device__ float score_slack() { return SIGMOID ? 2e-6f : 4e-6f; }
     // the cleared bits of two keys (32 C ulp each at most) and the rounding of s + b
@@ -626,7 +627,8 @@ gate_many_kernel(const GateArgs p)
         const float4 x = s_z[warp][2 * b][lane], y = s_z[warp][2 * b + 1][lane];
         z[0] = x.x; z[1] = x.y; z[2] = x.z; z[3] = x.w; z[4] = y.x; z[5] = y.y; z[6] = y.z; z[7] = y.w;
     };
-    // softmax: maximum and sum of the row (for scores, and for weights that are not renormalised), in one pass with a running maximum
+    // softmax: maximum, then sum of the row (for scores, and for weights that are not renormalised).  A block's eight terms are a tree, so
+    // that a sum is as many additions deep as in the kernel above, C + 5 at most: the bounds in Gate hold for both.
     constexpr float kLog2e = 1.4426950408889634f;
     float zmax = 0.f, inv_sum = 0.f;
     if (!SIGMOID && (BIAS || !p.renormalize || p.tie_flag)) {
@@ -635,17 +637,19 @@ gate_many_kernel(const GateArgs p)
         for (int b = 0; b < blocks; ++b) {
             float z[8];
             block_logits(b, z);
-            float top = m;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, z[i]);
-            sum = top == -INFINITY ? 0.f : sum * ex2((m - top) * kLog2e);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += z[i] == -INFINITY ? 0.f : ex2((z[i] - top) * kLog2e);
-            m = top;
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, z[i]);
         }
-        zmax = fmaxf(m, __shfl_xor_sync(kFull, m, 1));
-        zmax = fmaxf(zmax, __shfl_xor_sync(kFull, zmax, 2));
-        sum = m == -INFINITY ? 0.f : sum * ex2((m - zmax) * kLog2e);
+        m = fmaxf(m, __shfl_xor_sync(kFull, m, 1));
+        zmax = fmaxf(m, __shfl_xor_sync(kFull, m, 2));
+#pragma unroll 1
+        for (int b = 0; b < blocks; ++b) {
+            float z[8];
+            block_logits(b, z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = z[i] == -INFINITY ? 0.f : ex2((z[i] - zmax) * kLog2e);
+            sum += ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
+        }
         sum += __shfl_xor_sync(kFull, sum, 1);
         sum += __shfl_xor_sync(kFull, sum, 2);
         inv_sum = sum > 0.f ? 1.f / sum : 0.f;

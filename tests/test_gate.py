@@ -575,3 +575,38 @@ def test_experts_forced_by_an_infinite_bias(T, E, n_groups, keep, k):
     bias = g.standard_normal(E) * 0.05
     bias[[1, size + 2]] = [FMAX, np.inf]
     check_repeated(rows, T, k, bias=bias, score="sigmoid", n_groups=n_groups, keep=keep, renorm=True)
+
+
+@gpu
+@pytest.mark.parametrize("T,E,groups", [(40, 256, {}), (8192, 256, {}), (8192, 128, {}), (8192, 64, {}), (16384, 256, dict(n_groups=8, keep=8))])
+def test_softmax_sums_of_one_dominant_expert(T, E, groups):
+    """One expert has nearly all of the weight and the others 2^-24 of it or less, not half an fp32 step beside it: added to it one after
+    the other they would all be lost.  At most 13 additions lie between an exponential and the sum, each 2^-24 relative, then a quotient and
+    a product: below 16 * 2^-24 with the rounding of the tail's own exponentials.  (The others are 2e-3 apart, so that nothing is near a tie.)"""
+    g = np.random.default_rng(E)
+    rows = -24 * math.log(2) - 2e-3 * np.stack([g.permutation(E) for _ in range(E)])
+    rows[np.arange(E), np.arange(E)] = 0.0
+    for tie in (False, True):
+        pick = np.arange(T) % E
+        idx, w, _, _ = run(rows[pick], 2, score="softmax", tie=tie, **groups)
+        zr = rows.astype(np.float32).astype(float)
+        p = np.exp(zr) / np.exp(zr).sum(1, keepdims=True)
+        assert np.array_equal(idx[:, 0], pick)
+        np.testing.assert_allclose(w[:, 0], p[pick, pick], rtol=16 * 2.0 ** -24, atol=0)
+
+
+@gpu
+@pytest.mark.parametrize("T", [300, 32768])
+def test_softmax_scores_that_a_bias_brings_close_to_zero(T):
+    """One dominant logit early in a lane, the others 2^-24 of it, and a bias that leaves a few 1e-6 between it and the next ones: what a
+    sum in 32 bits may be off by must not decide."""
+    g = np.random.default_rng(31)
+    E, k = 256, 4
+    rows = -24 * math.log(2) - 1e-3 * g.random((256, E))
+    top = g.integers(0, 8, 256) * 32 + g.integers(0, 4, 256)
+    rows[np.arange(256), top] = 0.0
+    p = 1 / (1 + 255 * 2.0 ** -24)                  # (to 1e-8)
+    bias = g.uniform(-4e-6, 4e-6, E)
+    bias[np.unique(top)] = -p + g.uniform(-4e-6, 4e-6, np.unique(top).size)
+    for groups in ({}, dict(n_groups=8, keep=3)):
+        check_repeated(rows, T, k, bias=bias, score="softmax", renorm=True, **groups)
