@@ -141,6 +141,9 @@ typedef struct {
 int moe_create(const moe_config* cfg, moe_ctx** out);
 int moe_destroy(moe_ctx* ctx);
 
+/* What the context was created with, and (device, not NULL) the index of its device.  Host pointers. */
+int moe_get_config(moe_ctx* ctx, moe_config* cfg, int32_t* device);
+
 /*
  * Registers the routed-expert pool of one layer (Sec. 4.1: experts are
  * extracted from each MoE layer and packaged by layer and expert id).
@@ -348,6 +351,7 @@ int moe_gate(const void* logits, int logits_type, int64_t ld, int T, int E, int 
  * z = x . router_w^T + router_bias as before, then the rule above with balance_bias (device f32 [M, E] or NULL, used in
  * place).  rule is a host pointer and is copied; NULL returns to moe_route's own rule (softmax, raw probabilities).
  * Set between calls, not while one may still run; a captured graph keeps the rule that it was captured with.
+ * balance_bias is read at [model][expert] for all M * E of them, which the call cannot check (moe_get_config tells M and E).
  */
 int moe_set_gating(moe_ctx* ctx, int layer, const moe_gating* rule, const float* balance_bias);
 

@@ -41,7 +41,7 @@ MOE_TYPE_F32, MOE_TYPE_BF16 = 0, 1
 MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID = 0, 1
 MOE_GROUP_MAX, MOE_GROUP_TOP2 = 0, 1
 
-EXPORTS = ["moe_create", "moe_destroy", "moe_set_expert_pool", "moe_set_model_weights", "moe_set_slot_table",
+EXPORTS = ["moe_create", "moe_destroy", "moe_get_config", "moe_set_expert_pool", "moe_set_model_weights", "moe_set_slot_table",
            "moe_set_tenant_models", "moe_set_option", "moe_form_blocks", "moe_set_block_table", "moe_route", "moe_dispatch", "moe_experts", "moe_combine",
            "moe_layer_forward", "moe_residency_enable", "moe_layer_forward_paged", "moe_layer_forward_host", "moe_layer_forward_host_submit", "moe_layer_forward_host_wait", "moe_layer_forward_timed", "moe_stack_forward",
            "moe_get_workspace", "moe_last_status", "moe_last_plan", "moe_launch_count", "moe_strerror", "moe_dispatch_noalloc",
@@ -88,6 +88,7 @@ def load_library(path: str | None = None):
         lib.moe_launch_count.argtypes = [c_void_p]
         lib.moe_create.argtypes = [POINTER(MoeConfig), POINTER(c_void_p)]
         lib.moe_destroy.argtypes = [c_void_p]
+        lib.moe_get_config.argtypes = [c_void_p, POINTER(MoeConfig), POINTER(c_int32)]
         lib.moe_set_expert_pool.argtypes = [c_void_p, c_int, c_void_p, c_void_p, c_void_p]
         lib.moe_set_model_weights.argtypes = [c_void_p, c_int, c_int] + [c_void_p] * 7
         lib.moe_set_slot_table.argtypes = [c_void_p, c_void_p]
@@ -163,6 +164,13 @@ def moe_create(*, hidden, n_experts, inter, top_k, shared_inter=0, n_models=1, n
 
 def moe_destroy(ctx):
     _check("moe_destroy", load_library().moe_destroy(ctx))
+
+
+def moe_get_config(ctx):
+    """(MoeConfig, torch.device) of a context."""
+    cfg, device = MoeConfig(), c_int32()
+    _check("moe_get_config", load_library().moe_get_config(ctx, byref(cfg), byref(device)))
+    return cfg, torch.device("cuda", device.value)
 
 
 def moe_set_expert_pool(ctx, layer, w_gate, w_up, w_down):
@@ -360,12 +368,18 @@ def moe_gate(logits, rule, topk_idx, topk_w, *, balance_bias=None, tenant_id=Non
 
 
 def moe_set_gating(ctx, layer, rule, balance_bias=None):
-    """Makes the layer choose its experts by `rule` (None: moe_route's own rule).  balance_bias [M, E] float32 on the device is
-    used in place: keep it alive."""
+    """Makes the layer choose its experts by `rule` (None: moe_route's own rule).  balance_bias [M, E] float32 (or [E], of one model)
+    on the context's device is used in place: keep it alive."""
     if isinstance(balance_bias, torch.Tensor) and not (balance_bias.is_cuda and balance_bias.dtype == torch.float32 and
                                                        balance_bias.is_contiguous()):
         raise ValueError("moe_set_gating: balance_bias must be contiguous float32 on the device, "
                          f"not {balance_bias.dtype} on {balance_bias.device}")
+    if isinstance(balance_bias, torch.Tensor):
+        cfg, device = moe_get_config(ctx)                   # (the kernel reads all M * E of them)
+        shape = (cfg.n_models, cfg.n_experts)
+        if balance_bias.device != device or tuple(balance_bias.shape) not in (shape, shape[1:] if shape[0] == 1 else shape):
+            raise ValueError(f"moe_set_gating: balance_bias must be {list(shape)} on {device}, "
+                             f"not {list(balance_bias.shape)} on {balance_bias.device}")
     _check("moe_set_gating", load_library().moe_set_gating(ctx, layer, byref(rule) if rule is not None else None, _ptr(balance_bias)))
 
 

@@ -397,6 +397,14 @@ int moe_destroy(moe_ctx* c)
     return MOE_OK;
 }
 
+int moe_get_config(moe_ctx* c, moe_config* cfg, int32_t* device)
+{
+    if (!c || !cfg) return MOE_ERR_NULL;
+    *cfg = c->cfg;
+    if (device) *device = c->device;
+    return MOE_OK;
+}
+
 int moe_set_expert_pool(moe_ctx* c, int layer, const void* w_gate, const void* w_up, const void* w_down)
 {
     if (!c || !w_gate || !w_up || !w_down) return MOE_ERR_NULL;

@@ -610,3 +610,60 @@ def test_softmax_scores_that_a_bias_brings_close_to_zero(T):
     bias[np.unique(top)] = -p + g.uniform(-4e-6, 4e-6, np.unique(top).size)
     for groups in ({}, dict(n_groups=8, keep=3)):
         check_repeated(rows, T, k, bias=bias, score="softmax", renorm=True, **groups)
+
+
+@gpu
+def test_a_layers_bias_has_one_number_for_every_expert_of_every_model():
+    """moe_set_gating takes no bias that is shorter or longer than what the kernels read, and leaves the layer as it was."""
+    T, M, E = 40, 3, 12
+    wl, wts = _layer(E, 4, M, T)
+    x, tenant, mot = W.make_tokens(wl, seed=1)
+    gl = GpuLayer(wl, [wts], max_tokens=T, model_of_tenant=mot)
+    try:
+        cfg, device = B.moe_get_config(gl.ctx)
+        assert (cfg.n_models, cfg.n_experts, cfg.top_k, cfg.max_tokens, device) == (M, E, 4, T, torch.device(gl.dev))
+        before = gl.forward(x, tenant, 3)
+        rule = B.moe_gating(score="sigmoid", renormalize=True)
+        for shape in ((E,), (1, E), (M, E - 1), (E, M), (M, E, 1), (M * E,), (2 * M, E), (0,)):
+            with pytest.raises(ValueError, match="balance_bias"):
+                B.moe_set_gating(gl.ctx, 0, rule, torch.zeros(shape, device=gl.dev))
+        assert torch.equal(gl.forward(x, tenant, 3), before)
+        bias = torch.full((M, E), -1.0, device=gl.dev)
+        bias[:, :4] = 1.0
+        B.moe_set_gating(gl.ctx, 0, rule, bias)
+        assert (gl.four_calls(x, tenant, 3)["topk_idx"].sort(1)[0].cpu() == torch.arange(4)).all()
+    finally:
+        gl.close()
+
+
+def test_a_layers_bias_is_checked_before_the_call(monkeypatch):
+    class OnDevice(torch.Tensor):
+        is_cuda, device = True, torch.device("cuda", 0)
+
+    class Library:
+        def __init__(self, M, E, index=0):
+            self.M, self.E, self.index, self.set = M, E, index, 0
+
+        def moe_get_config(self, ctx, cfg, device):
+            cfg._obj.n_models, cfg._obj.n_experts, device._obj.value = self.M, self.E, self.index
+            return B.MOE_OK
+
+        def moe_set_gating(self, ctx, layer, rule, bias):
+            self.set += 1
+            return B.MOE_OK
+    rule = B.moe_gating()
+    for M, E, index, shape, good in ((4, 8, 0, (4, 8), True), (1, 8, 0, (8,), True), (1, 8, 0, (1, 8), True), (4, 8, 0, (8,), False), (4, 8, 0, (1, 8), False),
+                                     (4, 8, 0, (8, 4), False), (4, 8, 0, (4, 9), False), (4, 8, 0, (4, 7), False), (4, 8, 0, (32,), False), (4, 8, 1, (4, 8), False)):
+        lib = Library(M, E, index)
+        monkeypatch.setattr(B, "load_library", lambda lib=lib: lib)
+        bias = torch.zeros(shape).as_subclass(OnDevice)
+        if good:
+            B.moe_set_gating(1, 0, rule, bias)
+        else:
+            with pytest.raises(ValueError, match="balance_bias"):
+                B.moe_set_gating(1, 0, rule, bias)
+        assert lib.set == good
+
+
+def test_the_configuration_of_no_context():
+    assert B.load_library().moe_get_config(None, ctypes.byref(B.MoeConfig()), None) == B.MOE_ERR_NULL
