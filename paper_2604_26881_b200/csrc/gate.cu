@@ -45,6 +45,7 @@ __device__ __forceinline__ float key_value(uint32_t k)
 __device__ __forceinline__ float clean(float z) { return fminf(fmaxf(z, -INFINITY), FLT_MAX); }
 // a bias likewise, NaN as -inf
 __device__ __forceinline__ float clean_bias(float b) { return fmaxf(b, -INFINITY); }
+__device__ __forceinline__ float finite(float v) { return fminf(fmaxf(v, -FLT_MAX), FLT_MAX); }
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -427,13 +428,13 @@ __device__ __forceinline__ void gate_token(const GateArgs& p, int t, int lane, d
         for (int i = 0; i < C; ++i) sc[i] = 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < C; ++i) v[i] = BIAS ? sc[i] + b[i] : z[i];
+    for (int i = 0; i < C; ++i) v[i] = BIAS ? __fadd_rn(sc[i], b[i]) : z[i];       // (never fused with the product before it)
 
     uint32_t key[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-        // (from the lowest finite value up: the id bits must not make a NaN of -inf)
-        key[i] = (order_key(fmaxf(v[i], -FLT_MAX)) & ~kIdMask) | (kIdMask - lane * C - i);
+        // (finite values: the id bits must not make a NaN of an infinity)
+        key[i] = (order_key(finite(v[i])) & ~kIdMask) | (kIdMask - lane * C - i);
         if (i >= held) key[i] = 0u;
     }
 
@@ -470,7 +471,7 @@ __device__ __forceinline__ void gate_token(const GateArgs& p, int t, int lane, d
             score = sums ? a + c : a;
             __syncwarp();
         }
-        const uint32_t gkey = lane < p.n_groups ? order_key(score) : 0u;
+        const uint32_t gkey = lane < p.n_groups ? order_key(BIAS ? finite(score) : score) : 0u;      // (infinite ones are decided below)
         int rank = 0;
         for (int g = 0; g < p.n_groups; ++g) {
             const uint32_t o = __shfl_sync(kFull, gkey, g);
@@ -530,8 +531,9 @@ __device__ __forceinline__ void gate_token(const GateArgs& p, int t, int lane, d
 
     write_token<SIGMOID>(p, t, lane, my_e, my_z, zmax, inv_sum, bad);
     if (p.tie_flag) {
-        // two neighbours among ranks 1..k+1 closer than 1e-5 relative, in the values that order them (without a bias: the scores)
-        if (my_z != -INFINITY) flag_v = SIGMOID ? sigmoid_from(my_z, 0.f) : expf(my_z - zmax) * inv_sum;
+        // two neighbours among ranks 1..k+1 closer than 1e-5 relative, in the values that order them (without a bias: the scores, up
+        // to a common factor)
+        if (my_z != -INFINITY) flag_v = SIGMOID ? sigmoid_from(my_z, 0.f) : expf(my_z - zmax) * (BIAS ? inv_sum : 1.f);
         if (BIAS && lane < rounds) flag_v += clean_bias(__ldg(bias + my_e));
         const float pv = __shfl_up_sync(kFull, flag_v, 1);
         const bool near = __any_sync(kFull, lane > 0 && lane < rounds && !(pv - flag_v >= 1e-5f * fabsf(pv)));
@@ -703,9 +705,8 @@ gate_many_kernel(const GateArgs p)
                     if constexpr (BIAS) {
                         // (the softmax of -inf is 0 also where the whole row is -inf)
                         v = (SIGMOID ? rcp(1.f + ex2(-v * kLog2e)) : (v == -INFINITY ? 0.f : ex2((v - zmax) * kLog2e) * inv_sum)) + clean_bias(bv[i]);
-                        v = fminf(v, FLT_MAX);                // (the id bits must not make a NaN of +inf either: the groups are compared by keys)
                     }
-                    key[4 * h + i] = (order_key(fmaxf(v, -FLT_MAX)) & ~kIdMask) | (kIdMask - e - i);
+                    key[4 * h + i] = (order_key(finite(v)) & ~kIdMask) | (kIdMask - e - i);
                     if (!whole && e + i >= p.E) key[4 * h + i] = 0u;
                 }
             }
@@ -826,6 +827,9 @@ gate_many_kernel(const GateArgs p)
             }
             if (close) { kept = again; unsure = more; }
         }
+        // (The flag is gate_token's to say wherever it might find the groups undecided.  Its values differ from these by the cleared bits
+        // of keys, half of kRel, and with a softmax by the order of the sum, 2.1e-6.)
+        if (BIAS && p.tie_flag) unsure |= !(lo - hi > (SIGMOID ? 1.f : 2.f) * ((top2 ? 2.f : 1.f) * G::kSlack + G::kRel * big));
         // (every token goes over its own groups, keep of them: the places of a lane in s_z are its own in any block)
 #pragma unroll 1
         for (uint32_t left = kept; left; left &= left - 1) {
@@ -879,7 +883,13 @@ gate_many_kernel(const GateArgs p)
         }
         mixed |= edge;
         unsure |= edge && behind;
-        if (!SIGMOID && BIAS && mixed) unsure = true;         // (a softmax in 64 bits needs the whole row)
+        if (!SIGMOID && BIAS) {
+            unsure |= mixed;                                  // (a softmax in 64 bits needs the whole row)
+            if (p.tie_flag) {                                 // (the flag as for the groups; 2 kRel is above 1e-5 and what values differ by)
+#pragma unroll
+                for (int j = 0; j < 9; ++j) unsure |= j + 1 <= last && !(f[j] - f[j + 1] > 2.f * need);
+            }
+        }
     }
 
     // lane r has ranks 2 r and 2 r + 1 (and every lane the first rank behind the eight)
@@ -953,22 +963,34 @@ gate_many_kernel(const GateArgs p)
         if (on8 && !unsure) { p.topk_idx[out + at8] = bad ? at8 : e8; p.topk_w[out + at8] = bad ? 0.f : w8; }
     }
     if (p.tie_flag) {
-        // neighbours among ranks 1..k+1 closer than 1e-5 relative, in the values that order them (without a bias: the scores)
-        auto value = [&](int e, float zz, bool on) {
-            float v = 0.f;
-            if (on && zz != -INFINITY) v = SIGMOID ? sigmoid_from(zz, 0.f) : expf(zz - zmax) * inv_sum;
-            if (BIAS && on) v += clean_bias(__ldg(bias + e));
-            return v;
-        };
-        const bool has8 = live && k == 8 && p.eligible > 8;
-        const bool next0 = live && 2 * r <= k && 2 * r < p.eligible, next1 = live && 2 * r + 1 <= k && 2 * r + 1 < p.eligible;
-        const float v0 = value(e0, next0 ? load_logit(p, t, e0) : 0.f, next0), v1 = value(e1, next1 ? load_logit(p, t, e1) : 0.f, next1);
-        const float v8 = value(e8, has8 ? load_logit(p, t, e8) : 0.f, has8);
-        float v2 = __shfl_down_sync(kFull, v0, 1);
-        bool has2 = __shfl_down_sync(kFull, (int)next0, 1) != 0;
-        if (r == 3) { v2 = v8; has2 = has8; }
-        bool near = (next1 && !(v0 - v1 >= 1e-5f * fabsf(v0))) || (next1 && has2 && !(v1 - v2 >= 1e-5f * fabsf(v1)));
-        near = near || mixed || unsure;
+        // what gate_token looks at, in the same values: neighbours among ranks 1..k+1 that the keys leave undecided, or closer than 1e-5
+        // relative (with a softmax and a bias it has been asked wherever either may be)
+        bool near = false;
+        if (SIGMOID || !BIAS) {
+            float zz[3] = {0.f, 0.f, 0.f}, bb[3] = {0.f, 0.f, 0.f}, vv[3] = {0.f, 0.f, 0.f};      // ranks 2 r, 2 r + 1, 2 r + 2
+            float kv[3] = {key_value(k0), key_value(k1), key_value(dropped)};
+            bool in[3];
+            const int ids[3] = {e0, e1, e8};
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+                in[q] = live && 2 * r + q < ranks && (q < 2 || r == 3);
+                if (!in[q]) continue;
+                zz[q] = load_logit(p, t, ids[q]);
+                if (BIAS) bb[q] = __ldg(bias + ids[q]);
+                if (zz[q] != -INFINITY) vv[q] = SIGMOID ? sigmoid_from(zz[q], 0.f) : expf(zz[q] - zmax);
+                if (BIAS) vv[q] += clean_bias(bb[q]);
+            }
+            const float nz = __shfl_down_sync(kFull, zz[0], 1), nb = __shfl_down_sync(kFull, bb[0], 1), nv = __shfl_down_sync(kFull, vv[0], 1),
+                        nk = __shfl_down_sync(kFull, kv[0], 1);
+            const bool next = __shfl_down_sync(kFull, (int)in[0], 1) != 0;
+            if (r < 3) { zz[2] = nz; bb[2] = nb; vv[2] = nv; kv[2] = nk; in[2] = next; }
+#pragma unroll
+            for (int q = 1; q < 3; ++q) {
+                const bool same = zz[q - 1] == zz[q] && bb[q - 1] == bb[q] && 2 * r + q < k;
+                const bool apart = kv[q - 1] - kv[q] > G::kSlack + G::kRel * fmaxf(fabsf(kv[q - 1]), fabsf(kv[q]));
+                near |= in[q] && ((!apart && !same && (BIAS || !p.bf16_logits)) || !(vv[q - 1] - vv[q] >= 1e-5f * fabsf(vv[q - 1])));
+            }
+        }
         const uint32_t any = __ballot_sync(kFull, near);
         if (live && r == 0 && !unsure) p.tie_flag[t] = (any >> lane & 15u) != 0;
     }

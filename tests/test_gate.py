@@ -667,3 +667,49 @@ def test_a_layers_bias_is_checked_before_the_call(monkeypatch):
 
 def test_the_configuration_of_no_context():
     assert B.load_library().moe_get_config(None, ctypes.byref(B.MoeConfig()), None) == B.MOE_ERR_NULL
+
+
+def flagged_rows(g, E):
+    """Rows of every degree of closeness: random ones, neighbours from 1e-3 down to one fp32 step apart (of the logits, and of the scores
+    where the bias is flat), exact ties, masked rows."""
+    near = []
+    for step in 2.0 ** -np.arange(8, 25, dtype=float):
+        z = g.standard_normal((12, E))
+        z[:, 1::2] = z[:, ::2][:, :z[:, 1::2].shape[1]] + step * g.integers(-3, 4, z[:, 1::2].shape)
+        near.append(g.permuted(z, axis=1))
+    odd = g.standard_normal((6, E))
+    odd[0] = -np.inf
+    odd[1, 1:] = -np.inf
+    odd[2] = 0.0
+    odd[3] -= 200
+    odd[4, ::2] = -FMAX
+    odd[5] = g.integers(-2, 3, E)
+    return np.concatenate([g.standard_normal((60, E)), *near, odd])
+
+
+@gpu
+@pytest.mark.parametrize("T,E,k,groups", [(16384, 60, 4, {}), (16384, 64, 8, dict(n_groups=2, keep=1)), (16384, 128, 8, dict(n_groups=4, keep=2)), (16384, 128, 7, {}),
+                                          (32768, 256, 8, dict(n_groups=8, keep=4)), (32768, 256, 8, {}), (32768, 200, 1, {}), (32768, 8, 8, {})])
+def test_the_tie_flag_does_not_depend_on_the_batch(T, E, k, groups):
+    """A row has the same flag in a short batch and in a long one, whichever kernel looks at it; so have its experts."""
+    g = np.random.default_rng(E + k)
+    rows = flagged_rows(g, E)
+    pick = g.integers(0, len(rows), T)
+    pick[:len(rows)] = np.arange(len(rows))
+    # (a bias that undoes the scores in part, so that sums of the two come close to each other and to zero)
+    s = 1 / (1 + np.exp(-rows[70]))
+    odd = g.standard_normal(E) * 0.05
+    odd[[1, E // 2, 2, 3]] = np.inf, np.inf, -np.inf, np.nan
+    seen = set()
+    for score in ("softmax", "sigmoid"):
+        for bias in (None, np.zeros(E), g.standard_normal(E) * 0.05, odd, -s if score == "sigmoid" else -np.exp(rows[70]) / np.exp(rows[70]).sum()):
+            for group_score in ("max", "top2") if groups else ("max",):
+                for dtype in (torch.float32, torch.bfloat16):
+                    kw = dict(bias=None if bias is None else bias.reshape(1, -1), dtype=dtype, tie=True, score=score, group_score=group_score, renorm=True, **groups)
+                    idx, _, flag, _ = run(rows, k, **kw)
+                    long_idx, _, long_flag, _ = run(rows[pick], k, **kw)
+                    assert np.array_equal(long_idx, idx[pick])
+                    bad = np.nonzero(long_flag != flag[pick])[0]
+                    assert bad.size == 0, f"{bad.size} tokens, rows {sorted(set(pick[bad]))[:8]}: flag {long_flag[bad[0]]}, alone {flag[pick[bad[0]]]}, {kw}"
+                    seen |= set(flag.tolist())
+    assert seen == {0, 1}
