@@ -386,7 +386,7 @@ int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld
  *   out    f32 or bf16 (out_type) [T, N], rows ld_out apart
  *   workspace  moe_project_workspace() bytes of device memory, 256-byte aligned, that no other call uses meanwhile (NULL if 0)
  *   status_out device int32 or NULL: MOE_DEV_BAD_TENANT (tenant id outside [0, n_tenants): no adapter), MOE_DEV_BAD_ADAPTER and
- *          MOE_DEV_TIMEOUT are OR-ed into it; the caller clears it
+ *          MOE_DEV_TIMEOUT are OR-ed into it; the caller clears it.  NULL: into a word of the device, which moe_project_status reads
  * n_adapters = 0: no adapters; a, b, scale, tenant_id, adapter_of_tenant and n_tenants are not looked at.
  * K a multiple of 8; rank a multiple of 8 up to 128 (adapters of a smaller rank are padded with zeros); ldx and ldw multiples
  * of 8; x, w, a and b 16-byte aligned; T <= 2^22; K, N and n_adapters * rank <= 2^30.  out may not overlap x, w, a or b.  T = 0:
@@ -397,6 +397,10 @@ int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, i
                 const float* scale, int n_adapters, int rank, const int32_t* tenant_id, const int32_t* adapter_of_tenant,
                 int n_tenants, const void* base, int64_t ld_base, void* out, int64_t ld_out, int out_type, void* workspace,
                 int64_t workspace_bytes, int32_t* status_out, void* stream);
+
+/* Synchronises the current device, returns in *status_host the MOE_DEV_* bits that moe_project calls without a status_out have left
+ * there since the last such question, and clears them.  (MOE_DEV_TIMEOUT: some of those calls' outputs are invalid.) */
+int moe_project_status(int32_t* status_host);
 
 /* Bytes of device memory that moe_project needs (negative: MOE_ERR_SHAPE); 0 without adapters, and where one launch does all (a
  * handful of tokens of a small projection). */

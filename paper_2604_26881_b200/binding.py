@@ -46,7 +46,7 @@ EXPORTS = ["moe_create", "moe_destroy", "moe_get_config", "moe_set_expert_pool",
            "moe_layer_forward", "moe_residency_enable", "moe_layer_forward_paged", "moe_layer_forward_host", "moe_layer_forward_host_submit", "moe_layer_forward_host_wait", "moe_layer_forward_timed", "moe_stack_forward",
            "moe_get_workspace", "moe_last_status", "moe_last_plan", "moe_launch_count", "moe_strerror", "moe_dispatch_noalloc",
            "moe_gate", "moe_set_gating", "moe_add_rmsnorm",
-           "moe_project", "moe_project_workspace"]
+           "moe_project", "moe_project_workspace", "moe_project_status"]
 MOE_DISPATCH_NOALLOC_MAX_WORDS = 1 << 18
 
 STAGES = ["route", "dispatch", "plan", "experts_gateup", "experts_down", "combine"]
@@ -122,6 +122,7 @@ def load_library(path: str | None = None):
                                     [c_void_p] * 2)
         lib.moe_project_workspace.argtypes = [c_int, c_int, c_int, c_int, c_int]
         lib.moe_project_workspace.restype = c_int64
+        lib.moe_project_status.argtypes = [POINTER(c_int32)]
         lib.moe_get_workspace.argtypes = [c_void_p] + [POINTER(c_void_p)] * 8
         lib.moe_last_status.argtypes = [c_void_p, POINTER(c_int32), POINTER(c_int32)]
         lib.moe_last_plan.argtypes = [c_void_p, c_int, POINTER(c_int32)]
@@ -404,6 +405,15 @@ def moe_project_workspace(T, K, N, rank=0, n_adapters=0) -> int:
     return n
 
 
+def moe_project_status(device=None) -> int:
+    """Waits for the device (by default the current one) and returns the MOE_DEV_* bits that moe_project calls without a status_out
+    have left there, clearing them."""
+    status = c_int32()
+    with torch.cuda.device(device):
+        _check("moe_project_status", load_library().moe_project_status(byref(status)))
+    return status.value
+
+
 def moe_project(x, w, out, *, base=None, a=None, b=None, scale=None, tenant_id=None, adapter_of_tenant=None, n_tenants=None,
                 workspace=None, status_out=None, stream=None):
     """out = base + x . w^T + scale[a] * (x . a[a]^T) . b[a]^T with a = the adapter of each token's tenant.
@@ -411,7 +421,8 @@ def moe_project(x, w, out, *, base=None, a=None, b=None, scale=None, tenant_id=N
     x bf16 [T, K], w bf16 [N, K] or None, out float32 or bf16 [T, N], base like out or None: rows may be strided.  a bf16
     [n, rank, K], b bf16 [n, N, rank], scale float32 [n] or None; tenant_id int32 [T]; adapter_of_tenant int32 [n_tenants]
     on the device (None: tenant u has adapter u; n_tenants then defaults to n).  workspace: uint8 tensor, by default
-    allocated for the call on its stream.  See include/faasmoe.h."""
+    allocated for the call on its stream.  status_out: int32 [1] on the device; without it moe_project_status() tells of ids out
+    of range and of outputs that a time-out has left invalid.  See include/faasmoe.h."""
     if stream is not None and workspace is None and x.dim() == 2 and x.is_cuda and a is not None and a.dim() == 3:
         n = load_library().moe_project_workspace(x.shape[0], x.shape[1], out.shape[-1], a.shape[1], a.shape[0])
         if n > 0:

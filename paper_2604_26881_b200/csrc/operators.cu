@@ -99,6 +99,12 @@ int64_t moe_project_workspace(int T, int K, int N, int rank, int n_adapters)
     return project_workspace(T, K, N, rank, n_adapters);
 }
 
+int moe_project_status(int32_t* status_host)
+{
+    if (!status_host) return MOE_ERR_NULL;
+    return cuda_result("moe_project_status", take_project_status(status_host));
+}
+
 int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, int K, int N, const void* a, const void* b,
                 const float* scale, int n_adapters, int rank, const int32_t* tenant_id, const int32_t* adapter_of_tenant,
                 int n_tenants, const void* base, int64_t ld_base, void* out, int64_t ld_out, int out_type, void* workspace,

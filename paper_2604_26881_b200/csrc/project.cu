@@ -25,7 +25,9 @@ namespace {
 
 using namespace tc;
 
-__device__ int32_t g_project_status;      // where the status bits go of calls that did not ask for them
+__device__ int32_t g_project_status;      // where the status bits go of calls that have no word for them
+__device__ int32_t g_project_taken;
+__global__ void take_status_kernel() { g_project_taken = atomicExch(&g_project_status, 0); }
 
 // TMEM: the CTAs of these kernels that fit one SM together ask for 512 columns at most (by registers two of project_kernel, 256
 // columns each at most, or one and two of adapter_kernel, 128, or four of those), and a kernel that takes all 512 leaves no
@@ -1369,6 +1371,15 @@ int64_t project_workspace(int T, int K, int N, int rank, int n_adapters)
     p.T = T; p.K = K; p.N = N; p.rank = rank; p.n_adapters = n_adapters;
     if (plan_few(p) && (p.w = reinterpret_cast<const bf16*>(16), plan_few(p))) return 0;      // (with w and without)
     return (int64_t)T * rank * 2 * kUTerms;        // bf16 terms (fp32, which few tokens take, is less)
+}
+
+cudaError_t take_project_status(int32_t* status_host)
+{
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) return e;
+    take_status_kernel<<<1, 1>>>();
+    e = cudaGetLastError();
+    return e == cudaSuccess ? cudaMemcpyFromSymbol(status_host, g_project_taken, sizeof(int32_t)) : e;
 }
 
 cudaError_t launch_project(const ProjectArgs& in, cudaStream_t st)

@@ -37,5 +37,7 @@ struct ProjectArgs {
 // bytes of the workspace (0: none is needed)
 int64_t project_workspace(int T, int K, int N, int rank, int n_adapters);
 cudaError_t launch_project(const ProjectArgs& args, cudaStream_t st);
+// the status bits of the calls that had no word for them, read and cleared (waits for the device)
+cudaError_t take_project_status(int32_t* status_host);
 
 }  // namespace faasmoe

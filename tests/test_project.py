@@ -501,3 +501,38 @@ def test_single_infinities_stay_infinities(T, rank, what):
         assert int(status) == 0 and bool(y.isinf().any()) and not y.isnan().any()
         assert not got.isnan().any(), f"{int(got.isnan().sum())} NaN, first at {got.isnan().nonzero()[0].tolist()}"
         assert torch.equal(got.isinf(), y.isinf()) and torch.equal(got[got.isinf()], y[y.isinf()])
+
+
+@gpu
+def test_status_without_a_status_word():
+    """A call that passes no status_out leaves its bits in the device's own word, which is read and cleared."""
+    d = inputs(20, 64, 96, 8, 3, seed=1)
+    g = {k: None if v is None else v.to(DEV) for k, v in d.items()}
+    o = torch.empty(20, 96, device=DEV)
+    run = lambda ids, table=None: B.moe_project(g["x"], g["w"], o, a=g["a"], b=g["b"], scale=g["scale"], tenant_id=ids, adapter_of_tenant=table)
+    ids = torch.zeros(20, dtype=torch.int32, device=DEV)
+    B.moe_project_status()
+    run(ids)
+    assert B.moe_project_status() == 0
+    ids[3] = 7
+    run(ids)
+    run(ids * 0, torch.full((1,), 5, dtype=torch.int32, device=DEV))
+    assert B.moe_project_status() == B.MOE_DEV_BAD_TENANT | B.MOE_DEV_BAD_ADAPTER
+    assert B.moe_project_status() == 0
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.moe_project(g["x"], g["w"], o, a=g["a"], b=g["b"], tenant_id=ids, status_out=status)
+    assert B.moe_project_status() == 0 and int(status) == B.MOE_DEV_BAD_TENANT
+    # from another stream, and out of a graph
+    side = torch.cuda.Stream()
+    B.moe_project(g["x"], g["w"], o, a=g["a"], b=g["b"], tenant_id=ids, stream=side)
+    assert B.moe_project_status() == B.MOE_DEV_BAD_TENANT
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(ids)
+    assert B.moe_project_status() == 0
+    graph.replay()
+    assert B.moe_project_status() == B.MOE_DEV_BAD_TENANT
+
+
+def test_the_status_call_needs_somewhere_to_write():
+    assert B.load_library().moe_project_status(None) == B.MOE_ERR_NULL
