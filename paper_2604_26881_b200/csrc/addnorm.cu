@@ -7,9 +7,11 @@
 // Bound by HBM: every element is read and written once, kept in registers in between (W warps hold a row, up to four
 // 16-byte vectors a lane).  16384 x 2048 with both outputs and a scale per row: 302 MB in 52 us, 5.8 TB/s (0.89 of the
 // measured copy bandwidth); 4096 x 8192 with 128-column scales the same; 32 x 2048: 1.9 us, launch and latency.  The sum of
-// squares, the scales and the quotients are fp32; h is rounded once because it is the residual stream that the caller
-// keeps (the norm is that of the stored value), out is one rounding of the fp32 y, q one of the fp32 quotient y / s.
+// squares (of the row in units of a power of two, where its squares leave the range), the scales and the quotients are fp32; h is
+// rounded once because it is the residual stream that the caller keeps (the norm is that of the stored value), out is one rounding
+// of the fp32 y, q one of the fp32 quotient y / s.
 #include <cuda_fp8.h>
+#include <float.h>
 
 #include "addnorm.cuh"
 
@@ -102,6 +104,13 @@ __device__ __forceinline__ void store_q(uint8_t* dst, int n, bool vec_q, const f
     }
 }
 
+// a barrier of the warps of one row of the block (rows of several warps: two in a block at most)
+__device__ __forceinline__ void row_sync(int row, int W)
+{
+    if (row == 0) asm volatile("bar.sync 1, %0;" ::"r"(32 * W) : "memory");
+    else asm volatile("bar.sync 2, %0;" ::"r"(32 * W) : "memory");
+}
+
 // W warps per row, V vectors of 8 elements per lane, blockDim / (32 W) rows at a time; a block goes on with every gridDim-th set
 // of rows and has the next set's loads in flight while it works on this one.  All loads of a row are issued before the first is
 // used (a load inside a branch of its own waits for the one before it: 78 us instead of 58 for 16384 x 2048 with V = 2).
@@ -111,6 +120,8 @@ addnorm_kernel(const AddNormArgs p, int W)
 {
     __shared__ float s_sum[2][16];
     __shared__ uint32_t s_top[2][16];
+    __shared__ uint32_t s_big[16];
+    __shared__ float s_again[16];
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -168,7 +179,47 @@ addnorm_kernel(const AddNormArgs p, int W)
             ss = 0.f;
             for (int i = 0; i < W; ++i) ss += s_sum[buf][row_in_block * W + i];
         }
-        const float r = 1.f / sqrtf(ss / (float)p.H + p.eps);
+        float mean = ss / (float)p.H + p.eps;
+        // Squares beyond the range of fp32, or below it with no eps that counts beside them: the row again, in units of a power of two near
+        // its largest element (or near the root of eps).  (All warps of a row have the same sum, and so go the same way.)
+        // (16384 x 2048: 1.3 us; as a call that is not inlined 8 us.)
+        if (!(mean >= 0x1p-100f && mean <= FLT_MAX)) {
+            uint32_t big = 0;                                 // (columns that are not there hold 0)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) big = max(big, magnitude(h[v][i]));
+            big = __reduce_max_sync(kFull, big);
+            if (W > 1) {
+                if (lane == 0) s_big[warp] = big;
+                row_sync(row_in_block, W);
+                big = 0;
+                for (int i = 0; i < W; ++i) big = max(big, s_big[row_in_block * W + i]);
+            }
+            const float unit = fmaxf(__uint_as_float(big), sqrtf(p.eps));
+            if (big > 0 && big < 0x7f800000u && unit <= FLT_MAX) {       // (rows of zeros, with infinities or NaN: as they are)
+                const int e = min(max((int)(__float_as_uint(unit) >> 23) - 127, -126), 126);
+                const float scale = __uint_as_float((uint32_t)(127 - e) << 23);        // 2^-e: exact, as are its products
+                ss = 0.f;
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        h[v][i] *= scale;
+                        ss = fmaf(h[v][i], h[v][i], ss);
+                    }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(kFull, ss, o);
+                if (W > 1) {
+                    if (lane == 0) s_again[warp] = ss;
+                    row_sync(row_in_block, W);
+                    ss = 0.f;
+                    for (int i = 0; i < W; ++i) ss += s_again[row_in_block * W + i];
+                }
+                mean = ss / (float)p.H + p.eps * scale * scale;
+            }
+        }
+        const float r = 1.f / sqrtf(mean);
         uint32_t top = 0;                                     // largest |y| of the row
 #pragma unroll
         for (int v = 0; v < V; ++v) {

@@ -277,3 +277,23 @@ def test_quotients_are_rounded_once_to_8_bits(q):
         assert torch.equal(scale.cpu(), s)
         bad = out_q.cpu().view(torch.uint8) != want.view(torch.uint8)
         assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} differ"
+
+
+@gpu
+@pytest.mark.parametrize("H", [5, 300, 512, 768, 1411, 2048, 8192])
+def test_finite_rows_whose_squares_leave_the_range_of_32_bits(H):
+    """The formula holds for every finite row: squares beyond the largest fp32 number, squares that vanish and no eps beside them, and
+    an eps of either kind.  Ordinary rows between them keep their results."""
+    g = torch.Generator().manual_seed(H)
+    sizes = torch.tensor([1e18, 1.0, 3e19, 1e25, 1e-30, 1e30, 1e37, 1e-12, 1e-18, 1e-23, 2.0 ** -110, 2.0 ** -120, 1.0, 1e20])
+    x = (torch.rand(len(sizes), H, generator=g) + 0.5) * torch.where(torch.rand(len(sizes), H, generator=g) < 0.5, -1, 1)
+    x = (x * sizes[:, None]).to(torch.bfloat16)
+    x[13, 1:] = 1.0                                     # one element alone is beyond the range
+    tiny = x.clone()
+    tiny[[0, 3]] = (2.0 ** -133 * torch.randint(1, 100, (2, H), generator=g)).to(torch.bfloat16)           # (numbers below the normal ones)
+    far = torch.where(torch.rand(len(sizes), H, generator=g) < 0.5, -1, 1) * torch.finfo(torch.bfloat16).max
+    for q in (None, "row", "group"):
+        for eps in (0.0, 2.0 ** -20, 2.0 ** -110, 2.0 ** -126, 2.0 ** 126):
+            check(len(sizes), H, residual=False, q=q, x_values=x, eps=eps)
+            check(len(sizes), H, residual=True, q=q, x_values=tiny, r_values=torch.zeros_like(x), eps=eps)
+            check(len(sizes), H, residual=False, q=q, x_values=far.to(torch.bfloat16), eps=eps)
