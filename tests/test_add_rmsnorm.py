@@ -297,3 +297,36 @@ def test_finite_rows_whose_squares_leave_the_range_of_32_bits(H):
             check(len(sizes), H, residual=False, q=q, x_values=x, eps=eps)
             check(len(sizes), H, residual=True, q=q, x_values=tiny, r_values=torch.zeros_like(x), eps=eps)
             check(len(sizes), H, residual=False, q=q, x_values=far.to(torch.bfloat16), eps=eps)
+
+
+@gpu
+@pytest.mark.parametrize("H", [5, 200, 768, 2048, 5632])
+@pytest.mark.parametrize("q", [False, True])
+def test_rows_out_of_range_in_place(H, q):
+    """Rows whose squares leave the range beside ordinary ones, with every output in the place of an input that may be there: the bits
+    of a call whose outputs are elsewhere, in a batch that blocks go over several times."""
+    g = torch.Generator().manual_seed(H)
+    T = 3000
+    size = torch.tensor([1.0, 1e20, 1e-3, 3e37, 1.0, 1e-30])[torch.randint(0, 6, (T,), generator=g)]
+    x = (torch.randn(T, H, generator=g) * size[:, None]).to(torch.bfloat16).cuda()
+    r = (torch.randn(T, H, generator=g) * size[:, None]).to(torch.bfloat16).cuda()
+    w = (1 + 0.2 * torch.randn(H, generator=g)).to(torch.bfloat16).cuda()
+    for residual in (False, True):
+        for eps in (1e-6, 0.0):
+            def call(x, r, ro, o):
+                oq, s = (torch.zeros(T, H, dtype=torch.float8_e4m3fn, device="cuda:0"), torch.zeros(T, 1, device="cuda:0")) if q else (None, None)
+                B.moe_add_rmsnorm(x, w, eps, residual=r, residual_out=ro, out=o, out_q=oq, q_scale=s)
+                torch.cuda.synchronize()
+                return (oq.view(torch.uint8), s) if q else ()
+            ro, o = torch.empty_like(x), torch.empty_like(x)
+            want = call(x, r if residual else None, ro, o)
+            assert bool(o[size.cuda() > 1e19].isfinite().all()) and bool((o[size.cuda() > 1e19].abs().amax(1) > 0.1).all())
+            for place in ("out", "residual", "both", "x"):
+                x2, r2 = x.clone(), r.clone() if residual else None
+                o2 = x2 if place in ("out", "both") else torch.empty_like(x)
+                ro2 = {"out": None, "residual": r2, "both": r2, "x": x2}[place]
+                got = call(x2, r2, ro2, o2)
+                assert torch.equal(o2.view(torch.int16), o.view(torch.int16)), place
+                if ro2 is not None:
+                    assert torch.equal(ro2, ro), place
+                assert all(torch.equal(a, b) for a, b in zip(got, want)), place
