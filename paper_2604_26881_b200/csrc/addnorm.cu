@@ -7,10 +7,10 @@
 // Bound by HBM: every element is read and written once, kept in registers in between (W warps hold a row, up to four
 // 16-byte vectors a lane).  16384 x 2048 with a bf16 output alone: 268 MB in 46 us, 5.9 TB/s (0.89 of the measured copy
 // bandwidth); with both outputs and a scale per row 302 MB in 55 us, 5.5 TB/s (0.84), where the two roundings of every
-// quotient are instructions that the loads do not hide; 4096 x 8192 with 128-column scales 58 us; 32 x 2048: 2.0 us, launch and latency.  The sum of
-// squares (of the row in units of a power of two, where its squares leave the range), the scales and the quotients are fp32; h is
-// rounded once because it is the residual stream that the caller keeps (the norm is that of the stored value), out is one rounding
-// of the fp32 y, q one of the fp32 quotient y / s.
+// quotient are instructions that the loads do not hide; 4096 x 8192 with 128-column scales 58 us; 32 x 2048: 2.0 us, launch and
+// latency.  The sum of squares (of the row in units of a power of two, where its squares leave the range), the scales and the
+// quotients are fp32; h is rounded once because it is the residual stream that the caller keeps (the norm is that of the stored
+// value), out is one rounding of the fp32 y, q one of the fp32 quotient y / s.
 #include <cuda_fp8.h>
 #include <float.h>
 

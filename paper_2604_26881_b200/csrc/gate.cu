@@ -17,9 +17,10 @@
 //   - neighbours of the result that are closer than the error bound of key and 32-bit value, and are not the same pair
 //     (z, b), are put in order by their 64-bit values, one candidate per lane (in_order64); where the groups are that close, the
 //     groups' scores are taken in 64 bits (keep64).
-// Bound by instruction issue and, for few tokens, by the length of one token's chain, not by the logits' bytes (16384 x 256 in
-// fp32 are 2.7 us of HBM time): about 870 instructions per token with 256 experts in groups with a bias (gate_kernel), 470 in
-// gate_many_kernel (22.7 us).  One token: 2.0 us, 32 tokens of the widest rule 3.0 us, both launch and latency; more at launch_gate.
+// Bound by the length of a warp's chain of dependent integer steps, not by the logits' bytes (16384 x 256 in fp32 are 2.7 us of HBM
+// time) nor by issue (the SMs are busy 23 % of the time, with 19 % of their warps): about 870 instructions per token with 256
+// experts in groups with a bias (gate_kernel), 470 in gate_many_kernel (22.9 us).  One token: 1.9 us, 32 tokens of the widest
+// rule 3.0 us, both launch and latency; more at launch_gate.
 // With random logits about 3 % of the tokens of that rule have neighbours that the keys leave undecided.
 #include <float.h>
 
@@ -1050,10 +1051,11 @@ cudaError_t launch_gate(const GateArgs& in, cudaStream_t st)
     p.eligible = p.keep < p.n_groups ? p.keep * p.group_size : p.E;
     // Four lanes per token where there are tokens enough for its longer chain, and the groups are runs of 1, 2, 4 or 8 blocks of
     // 32 compared by what orders the experts (sums of scores beside an order by logits stay with the other kernel).  Measured, one
-    // warp per token / four lanes per token, us: 60 experts, softmax: 2048 tokens 3.8 / 4.4, 4096 5.0 / 4.6, 32768 24 / 11; 96, sigmoid,
-    // bias: 4096 6.7 / 5.5; 128 in 4 groups, sigmoid, bias: 4096 7.0 / 7.8, 8192 10.8 / 9.0; 256, softmax: 4096 7.3 / 7.6, 8192
-    // 12.1 / 9.7; 256 in 8 groups, sigmoid, bias: 8192 14.8 / 17.6, 16384 25.2 / 22.7, 32768 47 / 36.  With a softmax and a bias, whose
-    // near ties go through gate_token: 128 in 4 groups 8192 12.4 / 15.4, 16384 20.8 / 18.8; 256: 16384 24.8 / 30.3, 32768 45.5 / 44.3.
+    // warp per token / four lanes per token, us: 60 experts, softmax: 2048 tokens 3.7 / 4.5, 4096 5.0 / 4.7, 32768 24 / 11; 96, sigmoid,
+    // bias: 4096 6.6 / 5.7; 128 in 4 groups, sigmoid, bias: 4096 7.2 / 7.7, 8192 10.8 / 9.1; 256, softmax: 4096 7.1 / 7.7, 8192
+    // 11.7 / 9.8; 256 in 8 groups, sigmoid, bias: 8192 14.8 / 17.4, 16384 25.4 / 23.0, 32768 47 / 37.  With a softmax and a bias, whose
+    // near ties go through gate_token: 128 in 4 groups 8192 12.3 / 15.5, 16384 20.6 / 19.0; 256: 16384 24.9 / 31.5, 32768 45.5 / 45.2,
+    // in 8 groups 51.7 / 50.0.
     const int run = p.group_size / 32;
     const bool grouped = p.keep < p.n_groups;
     const bool blocks = !grouped || (p.group_size % 32 == 0 && (run & (run - 1)) == 0 && (p.bias || p.group_score == MOE_GROUP_MAX));

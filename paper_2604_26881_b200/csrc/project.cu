@@ -11,9 +11,9 @@
 //
 // Few tokens are a chain of latencies (ids, list, TMA, MMA, exchange in the cluster, the launch boundary, second product), not
 // bytes: 2048 -> 2048, rank 16, one token 9.8 us (8.5 MB, 1.3 us of HBM time); 2048 -> 5632, 32 tokens of 32 adapters 13.6 us
-// (31.8 MB, 4.9 us).  Many tokens are bound by the tensor cores: 5632 -> 2048, 4096 tokens of 16 adapters of rank 16 75 to 77 us (95
-// GFLOP, 1.25 PFLOP/s, 0.76 of the measured peak); the adapters alone beside a base, 1126 tokens, 13 of rank 64: 26 us, first
-// product 12 of them.
+// (31.8 MB, 4.9 us).  Many tokens are bound by the tensor cores: 5632 -> 2048, 4096 tokens of 16 adapters of rank 16 77 to 78 us (95
+// GFLOP, 1.23 PFLOP/s, 0.75 of the measured burst peak) in short runs, 87 to 92 back to back, where the power cap lowers the clock; the
+// adapters alone beside a base, 1126 tokens, 13 of rank 64: 28 us, first product 12 of them.
 #include <cstring>
 
 #include "project.cuh"
@@ -1266,11 +1266,11 @@ bool few_geometry(ProjectArgs& p, bool fused, int u_rows, int behind, int beside
 }
 
 // Which shape, by what either costs (us), a model fitted to some thousand measured pairs of 1 to 1024 tokens, 512 to 5632 rows and
-// columns, ranks 8 to 128 of 1 to 32 adapters (the choice is within 1.15 of the better one in all but nine).  The pair shape: its
-// slices of K, and a masked MMA per adapter that a tile may have.  The other: parts of K, and the adapters' products on the CUDA
-// cores.  (few / many tokens' shape, 2048 -> 2048: rank 16, 4 adapters, 64 tokens 11 / 20, 128 15 / 21; 32 adapters, 128 tokens
-// 22 / 36; rank 64, 2 adapters, 48 tokens 18 / 19, 96 27 / 20; no adapters, 200 tokens 14 / 15, 512 20 / 16.  2048 -> 5632:
-// rank 16, 4 adapters, 24 tokens 12 / 20, 96 23 / 21; 5632 -> 2048: rank 32, 4 adapters, 128 tokens 22 / 38.)
+// columns, ranks 8 to 128 of 1 to 32 adapters (in 110 other draws of those, the choice is within 1.15 of the better one in all but
+// two).  The pair shape: its slices of K, and a masked MMA per adapter that a tile may have.  The other: parts of K, and the
+// adapters' products on the CUDA cores.  (few / many tokens' shape, 2048 -> 2048: rank 16, 4 adapters, 64 tokens 11 / 21, 128 15 / 22, 512 27 / 21; 32 adapters, 128
+// tokens 21 / 41; rank 64, 2 adapters, 48 tokens 18 / 21, 96 28 / 21; no adapters, 200 tokens 13 / 15, 512 19 / 15.  2048 -> 5632:
+// rank 16, 4 adapters, 24 tokens 12 / 22, 96 23 / 22; 5632 -> 2048: rank 32, 4 adapters, 128 tokens 22 / 39, rank 16, 1024 tokens 69 / 38.)
 bool use_many(const ProjectArgs& p)
 {
     const int steps = p.w ? div_up(p.K, kBK) : 0, tiles = tiles_of(p, kPN), rows = p.T < kTok ? p.T : kTok;
@@ -1294,7 +1294,9 @@ size_t adapter_geometry(const ProjectArgs& p, bool many, ProjectArgs& q, int& ch
     q = p;
     // K is cut into as many parts as there are SMs for the token tiles, of two slices at least.  Beside a product of many
     // tokens the SMs that count are those that the product leaves: it starts on the others at once and needs u only at the
-    // end of its first tiles (4096 tokens, 5632 -> 2048: 32 CTAs on all of K instead of 128 on quarters).
+    // end of its first tiles (4096 tokens, 5632 -> 2048: 32 CTAs on all of K instead of 128 on quarters).  A product that leaves
+    // none gives up 36.  (At least 12 / 20 / 36 / 52 / 74, us, adapters in ragged runs: 4096 tokens, 2048 -> 5632, 16 of rank 16
+    // 91 / 96 / 94 / 96 / 99; 2048 tokens, 8 of them 61 / 57 / 52 / 53 / 58; 4096, 2048 -> 2048, 8 of rank 64 54 / 51 / 50 / 50 / 51.)
     int sms = 148;
     if (many && p.w) {
         const int busy = 2 * tiles_of(p, kMTile);
@@ -1304,8 +1306,9 @@ size_t adapter_geometry(const ProjectArgs& p, bool many, ProjectArgs& q, int& ch
     while (q.u_splits < (m_tiles == 1 ? 8 : 4) && m_tiles * q.u_splits * 2 <= sms && q.ksteps / (q.u_splits * 2) >= 2) q.u_splits *= 2;
     // Chunks of 64 columns: with one tile they are more CTAs, with many the ring has more stages for x, which is what is read.
     // From rank 32 on they would hold one or two adapters, so that beside a product, where CTAs are few, x would be read often:
-    // 128 columns.  (64 / 128 columns, us, 4096 tokens, 5632 -> 2048: 4 adapters of rank 16 75 / 90, 16 of rank 32 162 / 135,
-    // 13 of rank 64 113 / 103; 2048 tokens: 53 / 63, 91 / 76, 65 / 66.)
+    // 128 columns.  (64 / 128 columns, us, 5632 -> 2048, tokens of mixed tenants / in ragged runs of one: 4096 tokens, 4 adapters of
+    // rank 16 80 / 101 and 80 / 101, 16 of rank 32 177 / 150 and 88 / 112, 13 of rank 64 236 / 171 and 130 / 101; 2048 tokens 67 / 64
+    // and 54 / 60, 95 / 81 and 64 / 64, 120 / 95 and 67 / 67.)
     const int columns = many && p.w && p.rank >= 32 ? kUCols : kUCols / 2;
     q.slots = columns / p.rank > 0 ? columns / p.rank : 1;
     const int most = p.T < kTok ? p.T : kTok;
@@ -1330,7 +1333,7 @@ size_t adapter_geometry(const ProjectArgs& p, bool many, ProjectArgs& q, int& ch
     q.n_stages = two ? fit(kHalfSmem) : fit(kMaxSmem);
     // Chunks have CTAs of their own, as many as run at once, and are walked over beyond that.  A CTA whose tile has no such chunk
     // ends at once, so they are counted for all SMs also beside a product.  (4096 tokens, 5632 -> 2048, 32 adapters of rank 16,
-    // every token another: 304 us with the SMs that the product leaves, 166 with all; the same in runs of one tenant: 88, 78.)
+    // every token another: 290 us with the SMs that the product leaves, 170 to 195 with all; the same in runs of one tenant: 76, 79.)
     int room = q.u_splits > 1 ? cluster_room(q.u_splits, two) : 148 * (two ? 2 : 1);
     if (room > 148 / q.u_splits) room = 148 / q.u_splits;
     room /= m_tiles;
