@@ -373,6 +373,56 @@ int moe_add_rmsnorm(const void* x, int64_t ldx, const void* residual, int64_t ld
                     int64_t ld_q, float* q_scale, int group, void* stream);
 
 /*
+ * The norms behind and in front of a block, with the block's gate and the residual's scale, without a context: for models whose
+ * blocks are normed on both sides, gated, or scaled into the stream (moe_add_rmsnorm is the plain case).
+ *   a = y / sqrt(mean(y^2) + eps) * post_weight          (a = y if post_weight is NULL)     y = block_out   bf16 [T, H]
+ *   h = bf16(residual_scale * residual + block_scale * g * a)                               bf16 [T, H] each
+ *   v = h / sqrt(mean(h^2) + eps) * pre_weight           fp32; the weights are bf16 [H]
+ *   out = bf16(v)                       bf16 [T, H] or NULL
+ *   out_q = the fp32 quotient v / s, rounded to the nearest integer (ties to even)   int8 [T, H] or NULL; s = max |v| / 127
+ *   q_scale = s                         f32 [T], with out_q
+ *   g = gate, or 1 / (1 + exp(-gate)) with MOE_GATE_SIGMOID; gate is NULL (MOE_GATE_NONE), bf16 [H] (MOE_GATE_CHANNEL),
+ *       f32 [T] (MOE_GATE_TOKEN) or bf16 [T, H] with rows ld_gate apart (MOE_GATE_ELEMENT)
+ * pre_weight NULL: out and out_q are NULL too, h is the output.  Rows of every matrix are ld_* >= H elements apart; ld_* of a NULL
+ * matrix is not looked at.  1 <= H <= 16384.  Any alignment of whole elements; rows on 16-byte boundaries are fastest.  h and out may
+ * be block_out, residual or the gate itself (same row distance, else MOE_ERR_SHAPE), not each other; out_q is memory of its own.  A
+ * row with an infinity or a NaN makes its own outputs NaN (or 0; its out_q 0 and its q_scale not finite), no other row's.  T = 0:
+ * nothing is done and the pointers may be NULL.
+ */
+enum { MOE_GATE_NONE = 0, MOE_GATE_CHANNEL = 1, MOE_GATE_TOKEN = 2, MOE_GATE_ELEMENT = 3 };
+enum { MOE_GATE_RAW = 0, MOE_GATE_SIGMOID = 1 };
+typedef struct {
+    int32_t gate;            /* MOE_GATE_NONE .. MOE_GATE_ELEMENT */
+    int32_t gate_act;        /* MOE_GATE_RAW or MOE_GATE_SIGMOID */
+    float   residual_scale;  /* finite */
+    float   block_scale;     /* finite */
+    float   eps;             /* >= 0, of both norms */
+} moe_block_rule;
+int moe_block_norm(const void* block_out, int64_t ld_block, const void* residual, int64_t ld_residual, const void* post_weight,
+                   const void* pre_weight, const void* gate, int64_t ld_gate, const moe_block_rule* rule, int T, int H, void* h,
+                   int64_t ld_h, void* out, int64_t ld_out, int8_t* out_q, int64_t ld_q, float* q_scale, void* stream);
+
+/*
+ * The gradients of moe_block_norm, from those of its outputs (h rounded to bf16 passes them on as if it were not rounded; out_q has
+ * none).  block_out, pre_weight, post_weight, gate and rule are those of the forward call, h what it stored.
+ *   d_out [T, H] of out, or NULL (no gradient comes by way of out; h is not looked at)
+ *   d_h   [T, H] of h, or NULL; one of the two at least                                     bf16 each
+ *   d_block, d_residual    bf16 [T, H] or NULL
+ *   d_gate                 bf16 [T, H] (MOE_GATE_ELEMENT), f32 [T] (MOE_GATE_TOKEN), f32 [H] (MOE_GATE_CHANNEL), or NULL
+ *   d_post_weight, d_pre_weight      f32 [H] or NULL: sums over the tokens, in a fixed order
+ *   workspace  moe_block_norm_workspace(T, H) bytes, 16-byte aligned, that no other call uses meanwhile; only with d_post_weight,
+ *              d_pre_weight or a d_gate of f32 [H], else NULL
+ * At least one output; outputs are overwritten, not added to.  Those of T rows may be inputs of the same row distance.  T = 0: the
+ * sums over the tokens are set to zero.
+ */
+int moe_block_norm_backward(const void* block_out, int64_t ld_block, const void* h, int64_t ld_h, const void* post_weight,
+                            const void* pre_weight, const void* gate, int64_t ld_gate, const moe_block_rule* rule, int T, int H,
+                            const void* d_out, int64_t ld_d_out, const void* d_h, int64_t ld_d_h, void* d_block, int64_t ld_d_block,
+                            void* d_residual, int64_t ld_d_residual, void* d_gate, int64_t ld_d_gate, float* d_post_weight,
+                            float* d_pre_weight, void* workspace, int64_t workspace_bytes, void* stream);
+int64_t moe_block_norm_workspace(int T, int H);
+
+/*
  * A projection that all tenants share, with each tenant's own low-rank adapter beside it, without a context:
  *   out[t] = base[t] + x[t] . w^T + scale[a] * (x[t] . a[a]^T) . b[a]^T,    a = adapter_of_tenant[tenant_id[t]]
  * for all tokens of a batch in one call, in whatever order their tenants come.  bf16 operands, fp32 sums (the inner product of
@@ -398,13 +448,83 @@ int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, i
                 int n_tenants, const void* base, int64_t ld_base, void* out, int64_t ld_out, int out_type, void* workspace,
                 int64_t workspace_bytes, int32_t* status_out, void* stream);
 
-/* Synchronises the current device, returns in *status_host the MOE_DEV_* bits that moe_project calls without a status_out have left
- * there since the last such question, and clears them.  (MOE_DEV_TIMEOUT: some of those calls' outputs are invalid.) */
+/* Synchronises the current device, returns in *status_host the MOE_DEV_* bits that moe_project and moe_project_i8 calls without a
+ * status_out have left there since the last such question, and clears them.  (MOE_DEV_TIMEOUT: some of those calls' outputs are invalid.) */
 int moe_project_status(int32_t* status_host);
 
 /* Bytes of device memory that moe_project needs (negative: MOE_ERR_SHAPE); 0 without adapters, and where one launch does all (a
  * handful of tokens of a small projection). */
 int64_t moe_project_workspace(int T, int K, int N, int rank, int n_adapters);
+
+/*
+ * Rows as 8-bit integers with one scale each (the tokens of moe_project_i8, and once the rows of its weights), without a context:
+ *   scale[t] = max |x[t]| / 127;   q[t] = the fp32 quotient x[t] / scale[t], rounded to the nearest integer (ties to even)
+ * x bf16 [T, K], rows ldx apart; q int8 [T, K], rows ldq apart; scale f32 [T].  A row of zeros has scale 0.  A row with an infinity or a
+ * NaN has a scale that is not finite, and zeros.  1 <= K < 2^24.  Any alignment.  T = 0: nothing is done and the pointers may be NULL.
+ */
+int moe_quantize_i8(const void* x, int64_t ldx, int T, int K, int8_t* q, int64_t ldq, float* scale, void* stream);
+
+/*
+ * A projection in 8-bit integers that all tenants share, with a scale for each token and each channel, without a context:
+ *   out[t, n] = base[t, n] + bias[n] + x_scale[t] * w_scale[n] * sum_k x[t, k] * w[n, k]
+ * The sum is exact (32-bit integers); it is rounded to fp32 once, scaled and added to in fp32, and rounded once to out's type.
+ * (A scale that is not finite makes its token's or channel's outputs NaN or infinite, no other's.)  The tenants' low-rank adapters come
+ * beside it by moe_project with w NULL and this call's out as base.
+ *   x      int8 [T, K], rows ldx apart            x_scale f32 [T]
+ *   w      int8 [N, K], rows ldw apart            w_scale f32 [N]
+ *   bias   f32 [N] or NULL
+ *   base   [T, N] of out's type, rows ld_base apart, or NULL; may be out itself (same row distance)
+ *   out    f32 or bf16 (out_type) [T, N], rows ld_out apart
+ *   status_out  device int32 or NULL: MOE_DEV_TIMEOUT is OR-ed into it (the outputs are invalid); the caller clears it.  NULL: into
+ *               the word that moe_project_status reads
+ * 1 <= K <= 131071 (sums of any values fit 32 bits); ldx and ldw multiples of 16; x and w 16-byte aligned; T <= 2^22, N <= 2^30.
+ * out may not overlap x or w.  T = 0: nothing is done and the pointers may be NULL.  One launch, no workspace.
+ */
+int moe_project_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw, const float* w_scale, int T,
+                   int K, int N, const float* bias, const void* base, int64_t ld_base, void* out, int64_t ld_out, int out_type,
+                   int32_t* status_out, void* stream);
+
+/*
+ * What a router's training needs beside moe_gate: the balance loss of every model with its per-expert counts, and the gradient of
+ * the logits.  With p[t, e] = softmax(z[t])[e], or s[e] / sum s with s = sigmoid(z[t]), over the tokens t of model m that take part
+ * (tokens[m] of them):
+ *   counts[m, e]    = times that expert e is in topk_idx
+ *   mean_prob[m, e] = mean of p[t, e]
+ *   loss[m]         = E / (k * tokens[m]) * sum_e counts[m, e] * mean_prob[m, e]        (1 where both are even)
+ *   z_loss[m]       = mean of (log sum_e exp z[t, e])^2
+ * all 0 for a model without tokens.  Sums have a fixed order: the same bits every time.  A NaN logit counts as -inf, +inf as the
+ * largest finite fp32 value; a token whose logits are all -inf counts, with p = 0 and nothing for z_loss.
+ *   logits, logits_type, ld, tenant_id, model_of_tenant, n_tenants, M    as in moe_gate
+ *   topk_idx  int32 [T, k], as chosen by moe_gate (any order; the same expert twice counts twice)
+ *   score     MOE_SCORE_SOFTMAX or MOE_SCORE_SIGMOID
+ *   mask      u8 [T] or NULL: tokens with 0 take no part (padding); their logits and ids are not looked at
+ *   counts int32 [M, E], tokens int32 [M], mean_prob f32 [M, E], loss f32 [M], z_loss f32 [M] or NULL
+ *   workspace  moe_balance_workspace(T, E, M) bytes, 16-byte aligned, that no other call uses meanwhile (NULL if 0)
+ *   status_out device int32 or NULL: MOE_DEV_BAD_TENANT (the token takes no part) and MOE_DEV_BAD_EXPERT (an id outside [0, E) is
+ *              left out) are OR-ed into it; the caller clears it
+ * 1 <= E <= 256, 1 <= k <= min(E, 8), M <= 256, T <= 2^27.  T = 0: all outputs are set to zero.
+ */
+int moe_balance_loss(const void* logits, int logits_type, int64_t ld, int T, int E, int k, int score, const int32_t* topk_idx,
+                     const uint8_t* mask, const int32_t* tenant_id, const int32_t* model_of_tenant, int n_tenants, int M,
+                     int32_t* counts, int32_t* tokens, float* mean_prob, float* loss, float* z_loss, void* workspace,
+                     int64_t workspace_bytes, int32_t* status_out, void* stream);
+int64_t moe_balance_workspace(int T, int E, int M);
+
+/*
+ * The gradient of the logits, from those of the chosen experts' weights (moe_gate's topk_w by the same rule; the choice itself has
+ * none) and of both losses:
+ *   d_logits[t, e] = sum_j d_topk_w[t, j] * d w[t, j] / d z[t, e] + d_loss[m] * d loss[m] / d z[t, e] + d_z_loss[m] * d z_loss[m] / d z[t, e]
+ * counts are constants, as usual.  rule: score, renormalize and scale are read.  A balance bias takes part in the choice only and is not
+ * needed.  mask, tenants, ids out of range, NaN and infinite logits are taken as above; tokens that take no part get zeros (their
+ * d_topk_w is not looked at).
+ *   d_topk_w  f32 [T, k] or NULL;  d_loss f32 [M] or NULL, with counts and tokens of moe_balance_loss;  d_z_loss f32 [M] or NULL, with tokens
+ *   d_logits  f32 or bf16 as the logits [T, E], rows ld_d apart; may be the logits themselves (same row distance)
+ * T = 0: nothing is done and the pointers may be NULL.  One launch, no workspace.
+ */
+int moe_gate_backward(const void* logits, int logits_type, int64_t ld, int T, int E, int k, const moe_gating* rule,
+                      const int32_t* topk_idx, const float* d_topk_w, const uint8_t* mask, const int32_t* tenant_id,
+                      const int32_t* model_of_tenant, int n_tenants, int M, const int32_t* counts, const int32_t* tokens,
+                      const float* d_loss, const float* d_z_loss, void* d_logits, int64_t ld_d, int32_t* status_out, void* stream);
 
 /* route -> dispatch -> experts -> combine on the context's workspace; bit-identical to
  * the four calls above.  out bf16 [T,H]. */

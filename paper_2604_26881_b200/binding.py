@@ -40,13 +40,17 @@ MOE_PATH_AUTO, MOE_PATH_FMA, MOE_PATH_TCGEN05 = 0, 1, 2
 MOE_TYPE_F32, MOE_TYPE_BF16 = 0, 1
 MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID = 0, 1
 MOE_GROUP_MAX, MOE_GROUP_TOP2 = 0, 1
+MOE_GATE_NONE, MOE_GATE_CHANNEL, MOE_GATE_TOKEN, MOE_GATE_ELEMENT = 0, 1, 2, 3
+MOE_GATE_RAW, MOE_GATE_SIGMOID = 0, 1
 
 EXPORTS = ["moe_create", "moe_destroy", "moe_get_config", "moe_set_expert_pool", "moe_set_model_weights", "moe_set_slot_table",
            "moe_set_tenant_models", "moe_set_option", "moe_form_blocks", "moe_set_block_table", "moe_route", "moe_dispatch", "moe_experts", "moe_combine",
            "moe_layer_forward", "moe_residency_enable", "moe_layer_forward_paged", "moe_layer_forward_host", "moe_layer_forward_host_submit", "moe_layer_forward_host_wait", "moe_layer_forward_timed", "moe_stack_forward",
            "moe_get_workspace", "moe_last_status", "moe_last_plan", "moe_launch_count", "moe_strerror", "moe_dispatch_noalloc",
            "moe_gate", "moe_set_gating", "moe_add_rmsnorm",
-           "moe_project", "moe_project_workspace", "moe_project_status"]
+           "moe_project", "moe_project_workspace", "moe_project_status",
+           "moe_block_norm", "moe_block_norm_backward", "moe_block_norm_workspace", "moe_quantize_i8", "moe_project_i8",
+           "moe_balance_loss", "moe_balance_workspace", "moe_gate_backward"]
 MOE_DISPATCH_NOALLOC_MAX_WORDS = 1 << 18
 
 STAGES = ["route", "dispatch", "plan", "experts_gateup", "experts_down", "combine"]
@@ -61,6 +65,10 @@ class MoeConfig(ctypes.Structure):
 class MoeGating(ctypes.Structure):
     _fields_ = [("score", c_int32), ("n_groups", c_int32), ("keep_groups", c_int32), ("group_score", c_int32),
                 ("renormalize", c_int32), ("scale", c_float)]
+
+
+class MoeBlockRule(ctypes.Structure):
+    _fields_ = [("gate", c_int32), ("gate_act", c_int32), ("residual_scale", c_float), ("block_scale", c_float), ("eps", c_float)]
 
 
 class MoeError(RuntimeError):
@@ -123,6 +131,21 @@ def load_library(path: str | None = None):
         lib.moe_project_workspace.argtypes = [c_int, c_int, c_int, c_int, c_int]
         lib.moe_project_workspace.restype = c_int64
         lib.moe_project_status.argtypes = [POINTER(c_int32)]
+        lib.moe_block_norm.argtypes = ([c_void_p, c_int64] * 2 + [c_void_p] * 3 + [c_int64, POINTER(MoeBlockRule), c_int, c_int] +
+                                       [c_void_p, c_int64] * 3 + [c_void_p] * 2)
+        lib.moe_block_norm_backward.argtypes = ([c_void_p, c_int64] * 2 + [c_void_p] * 3 + [c_int64, POINTER(MoeBlockRule), c_int, c_int] +
+                                                [c_void_p, c_int64] * 5 + [c_void_p] * 3 + [c_int64, c_void_p])
+        lib.moe_block_norm_workspace.argtypes = [c_int, c_int]
+        lib.moe_block_norm_workspace.restype = c_int64
+        lib.moe_quantize_i8.argtypes = [c_void_p, c_int64, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p]
+        lib.moe_project_i8.argtypes = ([c_void_p, c_int64, c_void_p] * 2 + [c_int] * 3 + [c_void_p] * 2 + [c_int64, c_void_p, c_int64, c_int] +
+                                       [c_void_p] * 2)
+        lib.moe_balance_loss.argtypes = ([c_void_p, c_int, c_int64] + [c_int] * 4 + [c_void_p] * 4 + [c_int, c_int] + [c_void_p] * 6 +
+                                         [c_int64] + [c_void_p] * 2)
+        lib.moe_balance_workspace.argtypes = [c_int] * 3
+        lib.moe_balance_workspace.restype = c_int64
+        lib.moe_gate_backward.argtypes = ([c_void_p, c_int, c_int64, c_int, c_int, c_int, POINTER(MoeGating)] + [c_void_p] * 5 + [c_int, c_int] +
+                                          [c_void_p] * 5 + [c_int64] + [c_void_p] * 2)
         lib.moe_get_workspace.argtypes = [c_void_p] + [POINTER(c_void_p)] * 8
         lib.moe_last_status.argtypes = [c_void_p, POINTER(c_int32), POINTER(c_int32)]
         lib.moe_last_plan.argtypes = [c_void_p, c_int, POINTER(c_int32)]
@@ -331,8 +354,10 @@ def _load_calls():
     address = lambda f: ctypes.cast(f, c_void_p).value
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
     now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    mod.bind(address(lib.moe_gate), address(lib.moe_add_rmsnorm), address(lib.moe_project), address(lib.moe_project_workspace),
-             torch.float32, torch.bfloat16, torch.int32, torch.uint8, torch.float8_e4m3fn, raw, now,
+    mod.bind(*[address(f) for f in (lib.moe_gate, lib.moe_add_rmsnorm, lib.moe_project, lib.moe_project_workspace, lib.moe_block_norm,
+                                    lib.moe_block_norm_backward, lib.moe_block_norm_workspace, lib.moe_quantize_i8, lib.moe_project_i8,
+                                    lib.moe_balance_loss, lib.moe_balance_workspace, lib.moe_gate_backward)],
+             torch.float32, torch.bfloat16, torch.int32, torch.uint8, torch.float8_e4m3fn, torch.int8, raw, now,
              lambda n, device: torch.empty(n, dtype=torch.uint8, device=device), MoeGating)
     _calls = mod
     return mod
@@ -406,8 +431,8 @@ def moe_project_workspace(T, K, N, rank=0, n_adapters=0) -> int:
 
 
 def moe_project_status(device=None) -> int:
-    """Waits for the device (by default the current one) and returns the MOE_DEV_* bits that moe_project calls without a status_out
-    have left there, clearing them."""
+    """Waits for the device (by default the current one) and returns the MOE_DEV_* bits that moe_project and moe_project_i8 calls
+    without a status_out have left there, clearing them."""
     status = c_int32()
     with torch.cuda.device(device):
         _check("moe_project_status", load_library().moe_project_status(byref(status)))
@@ -434,6 +459,103 @@ def moe_project(x, w, out, *, base=None, a=None, b=None, scale=None, tenant_id=N
         if status == _OTHER_DEVICE:
             status = _on_device("moe_project", x.device, *args)
         _check("moe_project", status)
+
+
+def _call(fn, first, *args):
+    """A context-free call, on the device of its first tensor."""
+    status = getattr(_calls or _load_calls(), fn)(first, *args)
+    if status:
+        if status == _OTHER_DEVICE:
+            status = _on_device(fn, first.device, first, *args)
+        _check(fn, status)
+
+
+def _workspace_on(stream, device, n):
+    """A workspace for a call on another stream than the current one (the allocator must know which stream uses it)."""
+    if n <= 0:
+        return None
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+_ACTS = {"none": MOE_GATE_RAW, "sigmoid": MOE_GATE_SIGMOID}
+
+
+def moe_block_norm(block_out, residual, h, eps, *, post_weight=None, pre_weight=None, gate=None, gate_act="none", residual_scale=1.0,
+                   block_scale=1.0, out=None, out_q=None, q_scale=None, stream=None):
+    """h = bf16(residual_scale * residual + block_scale * g * RMSNorm(block_out) * post_weight); out = bf16(RMSNorm(h) * pre_weight),
+    out_q the same as int8 with one scale per row.
+
+    block_out, residual, h, out: bf16 [T, H], rows may be strided; out_q int8 [T, H], q_scale float32 [T]; the weights bf16 [H].
+    gate: bf16 [H] (per channel), float32 [T] (per token), bf16 [T, H] (per element) or None; gate_act "none" or "sigmoid".
+    post_weight None: block_out is not normed; pre_weight None: only h.  h and out may be block_out, residual or the gate."""
+    _call("moe_block_norm", block_out, residual, h, eps, post_weight, pre_weight, gate, _ACTS[gate_act], residual_scale, block_scale, out,
+          out_q, q_scale, stream)
+
+
+def moe_block_norm_workspace(T, H) -> int:
+    """Bytes of workspace that moe_block_norm_backward needs for its sums over the tokens."""
+    n = load_library().moe_block_norm_workspace(T, H)
+    if n < 0:
+        raise MoeError("moe_block_norm_workspace", n)
+    return n
+
+
+def moe_block_norm_backward(block_out, h, eps, *, post_weight=None, pre_weight=None, gate=None, gate_act="none", residual_scale=1.0,
+                            block_scale=1.0, d_out=None, d_h=None, d_block=None, d_residual=None, d_gate=None, d_post_weight=None,
+                            d_pre_weight=None, workspace=None, stream=None):
+    """Gradients of moe_block_norm from d_out and d_h (bf16 [T, H] or None); h is what the forward call stored (None without d_out).
+
+    d_block, d_residual: bf16 [T, H]; d_gate: float32 [H] or [T], or bf16 [T, H], as the gate; d_post_weight, d_pre_weight:
+    float32 [H].  Those that are None are not computed; the others are overwritten.  workspace: uint8 tensor, by default
+    allocated for the call on its stream."""
+    if stream is not None and workspace is None and block_out.dim() == 2 and block_out.is_cuda:
+        workspace = _workspace_on(stream, block_out.device, load_library().moe_block_norm_workspace(*block_out.shape))
+    _call("moe_block_norm_backward", block_out, h, eps, post_weight, pre_weight, gate, _ACTS[gate_act], residual_scale, block_scale, d_out,
+          d_h, d_block, d_residual, d_gate, d_post_weight, d_pre_weight, workspace, stream)
+
+
+def moe_quantize_i8(x, q, scale, *, stream=None):
+    """scale[t] = max |x[t]| / 127, q[t] = x[t] / scale[t] to the nearest integer: x bf16 [T, K], q int8 [T, K], scale float32 [T]."""
+    _call("moe_quantize_i8", x, q, scale, stream)
+
+
+def moe_project_i8(x, x_scale, w, w_scale, out, *, bias=None, base=None, status_out=None, stream=None):
+    """out = base + bias + x_scale * w_scale * (x . w^T), the product exact in 32-bit integers.
+
+    x int8 [T, K], w int8 [N, K] (rows may be strided, multiples of 16 apart, 16-byte aligned), x_scale float32 [T], w_scale
+    float32 [N], bias float32 [N] or None, out float32 or bf16 [T, N], base like out or None.  status_out: int32 [1] on the device;
+    without it moe_project_status() tells of a time-out.  Adapters are added by moe_project(x, None, out, base=out, a=..., b=...)."""
+    _call("moe_project_i8", x, x_scale, w, w_scale, out, bias, base, status_out, stream)
+
+
+def moe_balance_workspace(T, E, M=1) -> int:
+    """Bytes of workspace that moe_balance_loss needs (0: none)."""
+    n = load_library().moe_balance_workspace(T, E, M)
+    if n < 0:
+        raise MoeError("moe_balance_workspace", n)
+    return n
+
+
+def moe_balance_loss(logits, topk_idx, counts, tokens, mean_prob, loss, *, score="softmax", z_loss=None, mask=None, tenant_id=None,
+                     model_of_tenant=None, workspace=None, status_out=None, stream=None):
+    """The balance loss E / k * sum_e (counts / tokens) * mean_prob of every model, with its parts, and the mean of (log sum exp)^2.
+
+    logits [T, E] float32 or bf16 (rows may be strided), topk_idx [T, k] int32; counts int32 and mean_prob float32 [M, E], tokens int32,
+    loss and z_loss float32 [M].  mask uint8 [T]: 0 for tokens that take no part.  tenant_id [T] and model_of_tenant
+    [n_tenants] int32 (device) name a token's model.  workspace: uint8 tensor, by default allocated for the call on its stream."""
+    if stream is not None and workspace is None and logits.dim() == 2 and logits.is_cuda:
+        workspace = _workspace_on(stream, logits.device, load_library().moe_balance_workspace(*logits.shape, loss.numel()))
+    _call("moe_balance_loss", logits, topk_idx, counts, tokens, mean_prob, loss, _SCORES[score], z_loss, mask, tenant_id, model_of_tenant,
+          workspace, status_out, stream)
+
+
+def moe_gate_backward(logits, rule, topk_idx, d_logits, *, d_topk_w=None, counts=None, tokens=None, d_loss=None, d_z_loss=None, mask=None,
+                      tenant_id=None, model_of_tenant=None, status_out=None, stream=None):
+    """Gradient of the logits [T, E] (d_logits, of their type) by way of the chosen weights of `rule` (d_topk_w float32 [T, k]), of the
+    balance loss (d_loss float32 [M], with counts and tokens of moe_balance_loss) and of its second loss (d_z_loss float32 [M])."""
+    _call("moe_gate_backward", logits, rule, topk_idx, d_logits, d_topk_w, counts, tokens, d_loss, d_z_loss, mask, tenant_id, model_of_tenant,
+          status_out, stream)
 
 
 def moe_get_workspace(ctx):

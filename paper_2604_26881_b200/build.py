@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "lib", "libfaasmoe.so")
 CALLS = os.path.join(HERE, "lib", "_calls.so")          # marshalling of the context-free calls (CPython API only)
 SOURCES = ["api.cu", "route.cu", "route_tc.cu", "dispatch.cu", "plan.cu", "experts_fma.cu", "experts_tc.cu", "combine.cu",
-           "gate.cu", "addnorm.cu", "project.cu", "operators.cu"]
+           "gate.cu", "addnorm.cu", "project.cu", "blocknorm.cu", "project_i8.cu", "balance.cu", "operators.cu"]
 
 
 def _newest_source_mtime() -> float:

@@ -15,6 +15,7 @@
 #include <float.h>
 
 #include "addnorm.cuh"
+#include "rows.cuh"
 
 namespace faasmoe {
 
@@ -22,49 +23,6 @@ namespace {
 
 constexpr uint32_t kFull = 0xffffffffu;
 
-// |y| as an unsigned number: of the same order, and a NaN is above everything, as it is to be in the outputs
-__device__ __forceinline__ uint32_t magnitude(float y) { return __float_as_uint(y) & 0x7fffffffu; }
-
-__device__ __forceinline__ void unpack8(const uint4& v, float* f)
-{
-    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { const float2 t = __bfloat1622float2(h[i]); f[2 * i] = t.x; f[2 * i + 1] = t.y; }
-}
-__device__ __forceinline__ uint4 pack8(const float* f)
-{
-    uint4 v;
-    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-    return v;
-}
-// Eight consecutive elements of a row, of which the first n (possibly none) are there; the others read as zero.  VEC: n is
-// 8 or not positive and the address is on a 16-byte boundary.
-template <bool VEC>
-__device__ __forceinline__ uint4 load8(const bf16* p, int n)
-{
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (VEC) {
-        if (n > 0) v = *reinterpret_cast<const uint4*>(p);
-    } else {
-        unsigned short e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = i < n ? reinterpret_cast<const unsigned short*>(p)[i] : (unsigned short)0;
-        v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
-    }
-    return v;
-}
-template <bool VEC>
-__device__ __forceinline__ void store8(bf16* p, int n, const float* f)
-{
-    if (VEC) {
-        if (n > 0) *reinterpret_cast<uint4*>(p) = pack8(f);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < n) p[i] = __float2bfloat16_rn(f[i]);
-    }
-}
 __device__ __forceinline__ uint16_t e4m3x2(float a, float b)
 {
     return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
@@ -110,13 +68,6 @@ __device__ __forceinline__ void store_q(uint8_t* dst, int n, bool vec_q, const f
 #pragma unroll
         for (int i = 0; i < 8; ++i) if (i < n) dst[i] = (uint8_t)((i < 4 ? o.x : o.y) >> (8 * (i & 3)) & 0xffu);
     }
-}
-
-// a barrier of the warps of one row of the block (rows of several warps: two in a block at most)
-__device__ __forceinline__ void row_sync(int row, int W)
-{
-    if (row == 0) asm volatile("bar.sync 1, %0;" ::"r"(32 * W) : "memory");
-    else asm volatile("bar.sync 2, %0;" ::"r"(32 * W) : "memory");
 }
 
 // Mean of squares and eps of a row whose squares are beyond the range of fp32, or below it with no eps that counts beside them: of the

@@ -1,0 +1,51 @@
+// Arguments of the balance loss of a router and of the gradient of its logits (balance.cu).
+#pragma once
+
+#include "internal.h"
+
+namespace faasmoe {
+
+// what both calls read: logits, choices, and which model a token belongs to
+struct RouterBatch {
+    const void* logits;
+    int bf16_logits;
+    int64_t ld;
+    int T, E, k;
+    int score;
+    const int32_t* topk_idx;
+    const uint8_t* mask;              // or null
+    const int32_t* tenant_id;         // or null: model 0
+    const int32_t* model_of_tenant;   // or null: model 0
+    int n_tenants, M;
+    int32_t* status;                  // or null
+};
+
+struct BalanceArgs {
+    RouterBatch b;
+    int32_t* counts;                  // [M, E]
+    int32_t* tokens;                  // [M]
+    float* mean_prob;                 // [M, E]
+    float* loss;                      // [M]
+    float* z_loss;                    // [M] or null
+    float* parts;                     // [blocks][M][record]
+    int blocks;                       // blocks per model
+};
+
+struct GateGradArgs {
+    RouterBatch b;
+    int renormalize;
+    float scale;
+    const float* d_w;                 // [T, k] or null
+    const int32_t* counts;
+    const int32_t* tokens;
+    const float* d_loss;              // [M] or null
+    const float* d_z;                 // [M] or null
+    void* d_logits;
+    int64_t ld_d;
+};
+
+int64_t balance_workspace(int T, int E, int M);
+cudaError_t launch_balance(const BalanceArgs& args, cudaStream_t st);
+cudaError_t launch_gate_grad(const GateGradArgs& args, cudaStream_t st);
+
+}  // namespace faasmoe

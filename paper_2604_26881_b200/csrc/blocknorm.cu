@@ -1,0 +1,577 @@
+// The norms behind and in front of a block, with the block's gate and the residual's scale, in one pass over the rows:
+//
+//   a = y / sqrt(mean(y^2) + eps) * post                (a = y without a weight)
+//   h = bf16(residual_scale * residual + block_scale * g * a)            g: per channel, per token or per element, raw or its sigmoid
+//   v = h / sqrt(mean(h^2) + eps) * pre;   out = bf16(v);   q = int8(v / s), s = max |v| / 127 over the row
+//
+// and, row by row, the gradients of all of them (block_norm_grad_kernel).  All sums are fp32; h is rounded once because it is the
+// stream that the caller keeps, and the norm in front of the next block is that of the stored value.
+#include "blocknorm.cuh"
+#include "quant_i8.cuh"
+
+namespace faasmoe {
+
+namespace {
+
+constexpr uint32_t kFull = 0xffffffffu;
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+    return v;
+}
+
+// 1 / sqrt(mean of squares + eps) of a row held by W warps.  Where the squares are beyond the range of fp32, or below it with no
+// eps that counts beside them, the row is first multiplied (in place) by a power of two that is exact and brings them inside; the
+// factor is then that of the multiplied row, and *unit what it was multiplied with.
+template <int V>
+__device__ __forceinline__ float norm_factor(float (&x)[V][8], int H, float eps, int W, int warp, int lane, int row, float* sums, float* unit = nullptr)
+{
+    float ss = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = fmaf(x[v][i], x[v][i], ss);
+    ss = warp_sum(ss);
+    if (W > 1) {
+        if (lane == 0) sums[warp] = ss;
+        __syncthreads();
+        ss = 0.f;
+        for (int i = 0; i < W; ++i) ss += sums[row * W + i];
+    }
+    float mean = ss / (float)H + eps;
+    if (unit) *unit = 1.f;
+    // (all warps of a row have the same sum, and so go the same way)
+    if (!(mean >= 0x1p-100f && mean <= FLT_MAX)) {
+        const float scale = mean < 1.f ? 0x1p100f : 0x1p-72f;
+        if (unit) *unit = scale;
+        ss = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[v][i] *= scale;
+                ss = fmaf(x[v][i], x[v][i], ss);
+            }
+        ss = warp_sum(ss);
+        if (W > 1) {
+            row_sync(row, W);                                 // (everybody has read what was there)
+            if (lane == 0) sums[warp] = ss;
+            row_sync(row, W);
+            ss = 0.f;
+            for (int i = 0; i < W; ++i) ss += sums[row * W + i];
+        }
+        mean = ss / (float)H + eps * scale * scale;
+    }
+    return 1.f / sqrtf(mean);
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+__device__ __forceinline__ float activate(float g, int act) { return act == MOE_GATE_SIGMOID ? sigmoid(g) : g; }
+
+// What every row multiplies a column of the block's output with: block_scale, the weight behind the block, a gate per channel.
+template <int V>
+__device__ __forceinline__ void column_factors(const BlockNormArgs& p, int first, int step, float (&c)[V][8])
+{
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int col = first + v * step, n = p.H - col;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[v][i] = p.block_scale;
+        if (p.post) {
+            float w[8];
+            unpack8(p.vec_weight && n >= 8 ? load8<true>(p.post + col, n) : load8<false>(p.post + col, n), w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[v][i] *= w[i];
+        }
+        if (p.gate_form == MOE_GATE_CHANNEL) {
+            float g[8];
+            const bf16* gate = (const bf16*)p.gate + col;
+            unpack8(p.vec_weight && n >= 8 ? load8<true>(gate, n) : load8<false>(gate, n), g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[v][i] *= activate(g[i], p.gate_act);
+        }
+    }
+}
+
+// W warps per row, V vectors of 8 elements per lane, blockDim / (32 W) rows at a time; a block goes on with every gridDim-th set
+// of rows and has the next set's loads in flight while it works on this one.
+template <int V, bool ELEMENT, bool VEC>
+__global__ void __launch_bounds__(512)
+block_norm_kernel(const BlockNormArgs p, int W)
+{
+    __shared__ float s_post[2][16], s_pre[2][16];
+    __shared__ uint32_t s_top[2][16];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int row_in_block = warp / W, wr = warp - row_in_block * W;
+    const int rows = blockDim.x / (32 * W);
+    const int first = (wr * 32 + lane) * 8, step = W * 256;               // this lane's columns: first + v * step ...
+    uint4 yv[V], rv[V], gv[V], pv[V];
+    float gt = 1.f;
+    auto fetch = [&](int t) {
+        const int H = t < p.T ? p.H : 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) yv[v] = load8<VEC>(p.y + (size_t)t * p.ldy + first + v * step, H - first - v * step);
+#pragma unroll
+        for (int v = 0; v < V; ++v) rv[v] = load8<VEC>(p.residual + (size_t)t * p.ldr + first + v * step, H - first - v * step);
+        if (ELEMENT) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) gv[v] = load8<VEC>((const bf16*)p.gate + (size_t)t * p.ldg + first + v * step, H - first - v * step);
+        }
+        if (p.gate_form == MOE_GATE_TOKEN && t < p.T) gt = ((const float*)p.gate)[t];
+    };
+    int t = blockIdx.x * rows + row_in_block;
+    fetch(t);
+    float c[V][8];
+    column_factors<V>(p, first, step, c);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int col = first + v * step, n = p.pre ? p.H - col : 0;
+        pv[v] = p.vec_weight && n >= 8 ? load8<true>(p.pre + col, n) : load8<false>(p.pre + col, n);
+    }
+    int buf = 0;
+    for (int set = blockIdx.x; set * rows < p.T; set += gridDim.x, t += gridDim.x * rows, buf ^= 1) {
+        const bool live = t < p.T;
+        float x[V][8], r[V][8];
+#pragma unroll
+        for (int v = 0; v < V; ++v) unpack8(yv[v], x[v]);
+        uint4 res[V], gate[V];
+        float f = p.gate_form == MOE_GATE_TOKEN ? activate(gt, p.gate_act) : 1.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) { res[v] = rv[v]; if (ELEMENT) gate[v] = gv[v]; }
+        if (set + gridDim.x < (p.T + rows - 1) / rows) fetch(t + gridDim.x * rows);
+        // (two sets of partial sums in turn: a warp may be one set ahead of another, never two)
+        if (p.post) f *= norm_factor<V>(x, p.H, p.eps, W, warp, lane, row_in_block, s_post[buf]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = first + v * step;
+            unpack8(res[v], r[v]);
+            float g[8];
+            if (ELEMENT) unpack8(gate[v], g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float a = x[v][i] * f * c[v][i];
+                if (ELEMENT) a *= activate(g[i], p.gate_act);
+                x[v][i] = fmaf(p.residual_scale, r[v][i], a);
+            }
+            const uint4 h = pack8(x[v]);                      // (rounded: the stream that is stored)
+            unpack8(h, x[v]);
+            store8<VEC>(p.h + (size_t)t * p.ldh + col, live ? p.H - col : 0, x[v]);
+            // (columns that are not there hold 0 * f, and f need not be finite)
+            if (VEC ? col >= p.H : col + 8 > p.H) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) if (col + i >= p.H) x[v][i] = 0.f;
+            }
+        }
+        if (!p.pre) continue;
+        const float inv = norm_factor<V>(x, p.H, p.eps, W, warp, lane, row_in_block, s_pre[buf]);
+        uint32_t top = 0;                                     // largest |v| of the row
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = first + v * step, n = live ? p.H - col : 0;
+            float w[8];
+            unpack8(pv[v], w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[v][i] = x[v][i] * inv * w[i];
+            if (p.out) store8<VEC>(p.out + (size_t)t * p.ldo + col, n, x[v]);
+            if (p.q) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) if (VEC ? n > 0 : i < n) top = max(top, magnitude(x[v][i]));
+            }
+        }
+        if (!p.q) continue;
+        top = __reduce_max_sync(kFull, top);
+        if (W > 1) {
+            if (lane == 0) s_top[buf][warp] = top;
+            __syncthreads();
+            top = 0;
+            for (int i = 0; i < W; ++i) top = max(top, s_top[buf][row_in_block * W + i]);
+        }
+        const RowScale s = row_scale(__uint_as_float(top) / 127.f);
+        if (live && wr == 0 && lane == 0) p.q_scale[t] = s.scale;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = first + v * step, n = live ? p.H - col : 0;
+            if (n > 0) store_i8<VEC>(p.q + (size_t)t * p.ldq + col, n, p.vec_q, x[v], s);
+        }
+    }
+}
+
+template <int V, bool ELEMENT, bool VEC>
+cudaError_t launch_one(const BlockNormArgs& p, int W, int rows, cudaStream_t st)
+{
+    const int sets = (p.T + rows - 1) / rows, most = 148 * ((V == 1 ? 32 : 16) / (W * rows));
+    return launch_pdl(block_norm_kernel<V, ELEMENT, VEC>, dim3(sets < most ? sets : most), dim3(32 * W * rows), 0, st, p, W);
+}
+template <int V>
+cudaError_t launch_v(const BlockNormArgs& p, int W, int rows, cudaStream_t st)
+{
+    const bool element = p.gate_form == MOE_GATE_ELEMENT;
+    if (p.vec) return element ? launch_one<V, true, true>(p, W, rows, st) : launch_one<V, false, true>(p, W, rows, st);
+    return element ? launch_one<V, true, false>(p, W, rows, st) : launch_one<V, false, false>(p, W, rows, st);
+}
+
+bool al(const void* q, size_t n) { return (uintptr_t)q % n == 0; }
+bool rows16(const void* q, int64_t ld) { return !q || (al(q, 16) && ld % 8 == 0); }
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Gradients.  With d_out and d_h coming back, n = h / rms(h), m = y / rms(y):
+//
+//   d = d_h + (pre d_out - n mean(pre d_out n)) / rms(h)          d_pre = sum_t d_out n
+//   d_residual = residual_scale d                                 b = block_scale d
+//   d_g = b m post  (times g (1 - g) of a sigmoid)                e = b g post,  d_post = sum_t b g m
+//   d_y = (e - m mean(e m)) / rms(y)
+
+// the sums of `v` and `w` over a row's W warps
+__device__ __forceinline__ float row_sum(float v, int W, int warp, int lane, int row, float* sums)
+{
+    v = warp_sum(v);
+    if (W > 1) {
+        if (lane == 0) sums[warp] = v;
+        __syncthreads();
+        v = 0.f;
+        for (int i = 0; i < W; ++i) v += sums[row * W + i];
+    }
+    return v;
+}
+
+// One row at a time by W warps, V vectors per lane, blockDim / (32 W) rows at once; a lane keeps the same columns for all of the
+// block's rows and adds up their gradients (of the weights, of a gate per channel) in registers, rows in their order.
+template <int V, bool ELEMENT, bool VEC>
+__global__ void __launch_bounds__(512)
+block_norm_grad_kernel(const BlockNormArgs p, int W)
+{
+    __shared__ float s_sum[2][4][16];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int row_in_block = warp / W, wr = warp - row_in_block * W;
+    const int rows = blockDim.x / (32 * W);
+    const int first = (wr * 32 + lane) * 8, step = W * 256;
+    uint4 yv[V], hv[V], gv[V], ov[V], dv[V];
+    float gt = 1.f;
+    auto fetch = [&](int t) {
+        const int H = t < p.T ? p.H : 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) yv[v] = load8<VEC>(p.y + (size_t)t * p.ldy + first + v * step, H - first - v * step);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int n = p.d_out ? H - first - v * step : 0;
+            hv[v] = load8<VEC>(p.h + (size_t)t * p.ldh + first + v * step, n);
+            ov[v] = load8<VEC>(p.d_out + (size_t)t * p.ldout_grad + first + v * step, n);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) dv[v] = load8<VEC>(p.d_h + (size_t)t * p.ldh_grad + first + v * step, p.d_h ? H - first - v * step : 0);
+        if (ELEMENT) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) gv[v] = load8<VEC>((const bf16*)p.gate + (size_t)t * p.ldg + first + v * step, H - first - v * step);
+        }
+        if (p.gate_form == MOE_GATE_TOKEN && t < p.T) gt = ((const float*)p.gate)[t];
+    };
+    auto column = [&](const bf16* w, int v, float* f) {       // eight of a row of weights, or ones
+        const int col = first + v * step, n = p.H - col;
+        if (w) unpack8(p.vec_weight && n >= 8 ? load8<true>(w + col, n) : load8<false>(w + col, n), f);
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = 1.f;
+        }
+    };
+    float sum_pre[V][8], sum_post[V][8], sum_gate[V][8];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum_pre[v][i] = sum_post[v][i] = sum_gate[v][i] = 0.f;
+    const bool channel = p.gate_form == MOE_GATE_CHANNEL, token = p.gate_form == MOE_GATE_TOKEN;
+    const float over = 1.f / (float)p.H;
+    int t = blockIdx.x * rows + row_in_block;
+    int buf = 0;
+    for (int set = blockIdx.x; set * rows < p.T; set += gridDim.x, t += gridDim.x * rows, buf ^= 1) {
+        const bool live = t < p.T;
+        fetch(t);
+        float y[V][8], d[V][8];
+        if (p.d_out) {
+            float h[V][8], unit;
+#pragma unroll
+            for (int v = 0; v < V; ++v) unpack8(hv[v], h[v]);
+            const float inv = norm_factor<V>(h, p.H, p.eps, W, warp, lane, row_in_block, s_sum[buf][0], &unit);
+            float dot = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float o[8], w[8];
+                unpack8(ov[v], o);
+                column(p.pre, v, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    h[v][i] *= inv;                           // n
+                    if (VEC || first + v * step + i < p.H) sum_pre[v][i] = live ? fmaf(o[i], h[v][i], sum_pre[v][i]) : sum_pre[v][i];
+                    d[v][i] = o[i] * w[i];
+                    dot = fmaf(d[v][i], h[v][i], dot);
+                }
+            }
+            dot = row_sum(dot, W, warp, lane, row_in_block, s_sum[buf][1]) * over;
+            const float back = inv * unit;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[v][i] = back * (d[v][i] - h[v][i] * dot);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[v][i] = 0.f;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = first + v * step, n = live ? p.H - col : 0;
+            float u[8];
+            unpack8(dv[v], u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                d[v][i] += u[i];
+                u[i] = p.residual_scale * d[v][i];
+                d[v][i] *= p.block_scale;
+            }
+            if (p.d_residual) store8<VEC>(p.d_residual + (size_t)t * p.ldr_grad + col, n, u);
+            unpack8(yv[v], y[v]);
+        }
+        float inv = 1.f, unit = 1.f;
+        if (p.post) inv = norm_factor<V>(y, p.H, p.eps, W, warp, lane, row_in_block, s_sum[buf][2], &unit);
+        const float row_gate = token ? activate(gt, p.gate_act) : 1.f;
+        float dot = 0.f;                                      // without the token's gate, whose gradient it is too
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = first + v * step;
+            float w[8], g[8];
+            column(p.post, v, w);
+            if (channel) column((const bf16*)p.gate, v, g);
+            if (ELEMENT) unpack8(gv[v], g);
+            float dg[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float m = y[v][i] * inv;
+                y[v][i] = m;
+                const bool there = live && (VEC ? col < p.H : col + i < p.H);
+                float b = d[v][i];
+                if (channel || ELEMENT) {
+                    const float value = activate(g[i], p.gate_act);
+                    dg[i] = b * m * w[i];
+                    if (p.gate_act == MOE_GATE_SIGMOID) dg[i] *= value * sigmoid(-g[i]);
+                    b *= value;
+                    if (channel && there) sum_gate[v][i] += dg[i];
+                }
+                if (there) sum_post[v][i] = fmaf(b * row_gate, m, sum_post[v][i]);
+                d[v][i] = b * w[i];
+                if (there) dot = fmaf(d[v][i], m, dot);
+            }
+            if (ELEMENT && p.d_gate) store8<VEC>((bf16*)p.d_gate + (size_t)t * p.ldg_grad + col, live ? p.H - col : 0, dg);
+        }
+        if (p.post || token) dot = row_sum(dot, W, warp, lane, row_in_block, s_sum[buf][3]);
+        if (token && p.d_gate && live && wr == 0 && lane == 0)
+            ((float*)p.d_gate)[t] = p.gate_act == MOE_GATE_SIGMOID ? dot * (row_gate * sigmoid(-gt)) : dot;
+        if (p.d_y) {
+            const float mean = p.post ? dot * over : 0.f, back = inv * unit * row_gate;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int col = first + v * step;
+                float u[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] = p.post ? back * (d[v][i] - y[v][i] * mean) : row_gate * d[v][i];
+                store8<VEC>(p.d_y + (size_t)t * p.ldy_grad + col, live ? p.H - col : 0, u);
+            }
+        }
+    }
+    if (!p.sums) return;
+    const size_t part = (size_t)blockIdx.x * rows + row_in_block, all = (size_t)p.parts * p.H;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int col = first + v * step + i;
+            if (col >= p.H) continue;
+            if (p.d_pre) p.sums[part * p.H + col] = sum_pre[v][i];
+            if (p.d_post) p.sums[all + part * p.H + col] = sum_post[v][i];
+            if (channel && p.d_gate) p.sums[2 * all + part * p.H + col] = sum_gate[v][i];
+        }
+}
+
+// The blocks' sums, added up in a fixed order: 32 columns a block, 32 threads a column.  blockIdx.y: which of the three.
+__global__ void __launch_bounds__(1024)
+column_sum_kernel(const BlockNormArgs p)
+{
+    __shared__ float s[32][33];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int c = threadIdx.x & 31, r = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+    float* const dst = blockIdx.y == 0 ? p.d_pre : blockIdx.y == 1 ? p.d_post : p.gate_form == MOE_GATE_CHANNEL ? (float*)p.d_gate : nullptr;
+    if (!dst) return;
+    const float* src = p.sums + (size_t)blockIdx.y * p.parts * p.H;
+    float v = 0.f;
+    if (col < p.H)
+        for (int i = r; i < p.parts; i += 32) v += src[(size_t)i * p.H + col];
+    s[r][c] = v;
+    __syncthreads();
+    v = warp_sum(s[c][r]);                                    // warp r: column r
+    if (c == 0 && blockIdx.x * 32 + r < p.H) dst[blockIdx.x * 32 + r] = v;
+}
+
+// blocks of the gradients' kernel, and warps and rows of a block
+struct GradShape { int V, W, rows, blocks; };
+GradShape grad_shape(int T, int H)
+{
+    GradShape g;
+    const int vecs = (H + 7) / 8;
+    g.V = vecs <= 512 ? 1 : (vecs <= 1024 ? 2 : 4);
+    g.W = (vecs + 32 * g.V - 1) / (32 * g.V);
+    g.rows = g.W >= 4 ? 1 : 4 / g.W;
+    const int sets = (T + g.rows - 1) / g.rows;
+    int most = 148 * (16 / (g.W * g.rows));
+    g.blocks = sets < most ? sets : most;
+    return g;
+}
+
+template <int V>
+cudaError_t launch_grad(const BlockNormArgs& p, const GradShape& g, cudaStream_t st)
+{
+    const bool element = p.gate_form == MOE_GATE_ELEMENT;
+    const dim3 grid(g.blocks), block(32 * g.W * g.rows);
+    if (p.vec) return element ? launch_pdl(block_norm_grad_kernel<V, true, true>, grid, block, 0, st, p, g.W)
+                              : launch_pdl(block_norm_grad_kernel<V, false, true>, grid, block, 0, st, p, g.W);
+    return element ? launch_pdl(block_norm_grad_kernel<V, true, false>, grid, block, 0, st, p, g.W)
+                   : launch_pdl(block_norm_grad_kernel<V, false, false>, grid, block, 0, st, p, g.W);
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+
+// Rows as 8-bit integers.  Up to 16384 columns a row stays in registers; beyond, it is read twice.
+template <int V, bool VEC>
+__global__ void __launch_bounds__(512)
+quantize_kernel(const QuantizeArgs p, int W)
+{
+    __shared__ uint32_t s_top[2][16];
+    pdl_wait();
+    pdl_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int row_in_block = warp / W, wr = warp - row_in_block * W;
+    const int rows = blockDim.x / (32 * W);
+    const int first = (wr * 32 + lane) * 8, step = W * 256;
+    uint4 xv[V];
+    auto fetch = [&](int t) {
+        const int K = t < p.T ? p.K : 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) xv[v] = load8<VEC>(p.x + (size_t)t * p.ldx + first + v * step, K - first - v * step);
+    };
+    int t = blockIdx.x * rows + row_in_block;
+    fetch(t);
+    int buf = 0;
+    for (int set = blockIdx.x; set * rows < p.T; set += gridDim.x, t += gridDim.x * rows, buf ^= 1) {
+        const bool live = t < p.T;
+        float x[V][8];
+        uint32_t top = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            unpack8(xv[v], x[v]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, magnitude(x[v][i]));
+        }
+        if (set + gridDim.x < (p.T + rows - 1) / rows) fetch(t + gridDim.x * rows);
+        if (p.K > V * step)                                   // (one row a block, and more of it than the registers hold)
+            for (int col = first + V * step; live && col < p.K; col += step) {
+                float f[8];
+                unpack8(load8<VEC>(p.x + (size_t)t * p.ldx + col, p.K - col), f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = max(top, magnitude(f[i]));
+            }
+        top = __reduce_max_sync(kFull, top);
+        if (W > 1) {
+            if (lane == 0) s_top[buf][warp] = top;
+            __syncthreads();
+            top = 0;
+            for (int i = 0; i < W; ++i) top = max(top, s_top[buf][row_in_block * W + i]);
+        }
+        const RowScale s = row_scale(__uint_as_float(top) / 127.f);
+        if (live && wr == 0 && lane == 0) p.scale[t] = s.scale;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = first + v * step, n = live ? p.K - col : 0;
+            if (n > 0) store_i8<VEC>(p.q + (size_t)t * p.ldq + col, n, p.vec_q, x[v], s);
+        }
+        if (p.K > V * step)
+            for (int col = first + V * step; live && col < p.K; col += step) {
+                float f[8];
+                unpack8(load8<VEC>(p.x + (size_t)t * p.ldx + col, p.K - col), f);
+                store_i8<VEC>(p.q + (size_t)t * p.ldq + col, p.K - col, p.vec_q, f, s);
+            }
+    }
+}
+
+template <int V>
+cudaError_t launch_quantize_v(const QuantizeArgs& p, int W, int rows, cudaStream_t st)
+{
+    const int sets = (p.T + rows - 1) / rows, most = 148 * (32 / (W * rows));
+    const dim3 grid(sets < most ? sets : most), block(32 * W * rows);
+    return p.vec ? launch_pdl(quantize_kernel<V, true>, grid, block, 0, st, p, W) : launch_pdl(quantize_kernel<V, false>, grid, block, 0, st, p, W);
+}
+
+}  // namespace
+
+cudaError_t launch_block_norm(const BlockNormArgs& in, cudaStream_t st)
+{
+    BlockNormArgs p = in;
+    const bool element = p.gate_form == MOE_GATE_ELEMENT;
+    p.vec = p.H % 8 == 0 && rows16(p.y, p.ldy) && rows16(p.residual, p.ldr) && rows16(p.h, p.ldh) && rows16(p.out, p.ldo) &&
+            (!element || rows16(p.gate, p.ldg));
+    p.vec_weight = al(p.post, 16) && al(p.pre, 16) && (p.gate_form != MOE_GATE_CHANNEL || al(p.gate, 16));
+    p.vec_q = al(p.q, 8) && p.ldq % 8 == 0;
+    const int vecs = (p.H + 7) / 8;
+    const int V = vecs <= 32 || (!p.vec && vecs <= 512) ? 1 : (vecs <= 512 ? 2 : 4);
+    const int W = (vecs + 32 * V - 1) / (32 * V), rows = W >= 4 ? 1 : 4 / W;
+    if (V == 1) return launch_v<1>(p, W, rows, st);
+    if (V == 2) return launch_v<2>(p, W, rows, st);
+    return launch_v<4>(p, W, rows, st);
+}
+
+int64_t block_norm_workspace(int T, int H)
+{
+    const GradShape g = grad_shape(T, H);
+    return (int64_t)3 * g.blocks * g.rows * H * (int64_t)sizeof(float);
+}
+
+cudaError_t launch_block_norm_backward(const BlockNormArgs& in, cudaStream_t st)
+{
+    BlockNormArgs p = in;
+    const bool element = p.gate_form == MOE_GATE_ELEMENT;
+    p.vec = p.H % 8 == 0 && rows16(p.y, p.ldy) && rows16(p.h, p.ldh) && rows16(p.d_out, p.ldout_grad) && rows16(p.d_h, p.ldh_grad) &&
+            rows16(p.d_y, p.ldy_grad) && rows16(p.d_residual, p.ldr_grad) &&
+            (!element || (rows16(p.gate, p.ldg) && rows16(p.d_gate, p.ldg_grad)));
+    p.vec_weight = al(p.post, 16) && al(p.pre, 16) && (p.gate_form != MOE_GATE_CHANNEL || al(p.gate, 16));
+    const GradShape g = grad_shape(p.T, p.H);
+    p.parts = g.blocks * g.rows;
+    if (!p.d_pre && !p.d_post && !(p.d_gate && p.gate_form == MOE_GATE_CHANNEL)) p.sums = nullptr;
+    cudaError_t e = cudaSuccess;
+    if (p.T > 0) {
+        e = g.V == 1 ? launch_grad<1>(p, g, st) : g.V == 2 ? launch_grad<2>(p, g, st) : launch_grad<4>(p, g, st);
+        if (e != cudaSuccess) return e;
+    }
+    if (!p.d_pre && !p.d_post && !(p.d_gate && p.gate_form == MOE_GATE_CHANNEL)) return e;
+    return launch_pdl(column_sum_kernel, dim3((p.H + 31) / 32, 3), dim3(1024), 0, st, p);
+}
+
+cudaError_t launch_quantize_i8(const QuantizeArgs& in, cudaStream_t st)
+{
+    QuantizeArgs p = in;
+    p.vec = p.K % 8 == 0 && rows16(p.x, p.ldx);
+    p.vec_q = al(p.q, 8) && p.ldq % 8 == 0;
+    const int vecs = (p.K + 7) / 8;
+    const int V = vecs <= 32 ? 1 : (vecs <= 512 ? 2 : 4);
+    int W = (vecs + 32 * V - 1) / (32 * V);
+    if (W > 16) W = 16;
+    const int rows = W >= 4 ? 1 : 4 / W;
+    if (V == 1) return launch_quantize_v<1>(p, W, rows, st);
+    if (V == 2) return launch_quantize_v<2>(p, W, rows, st);
+    return launch_quantize_v<4>(p, W, rows, st);
+}
+
+}  // namespace faasmoe

@@ -1,0 +1,52 @@
+// Arguments of the kernels of a block's norms with gate and residual scale, and of their gradients (blocknorm.cu).
+#pragma once
+
+#include "internal.h"
+
+namespace faasmoe {
+
+constexpr int kBlockNormMaxH = 16384;      // 16 warps x 32 lanes x 4 vectors of 8 elements
+
+struct BlockNormArgs {
+    const bf16* y;             // the block's output
+    const bf16* residual;
+    const bf16* post;          // [H] or null: no norm behind the block
+    const bf16* pre;           // [H] or null: no norm in front of the next
+    const void* gate;          // bf16 [H], f32 [T] or bf16 [T, H], or null
+    bf16* h;                   // forward: the stream (may be residual or y); backward: the stored stream
+    bf16* out;                 // or null; may be y or residual
+    int8_t* q;                 // or null
+    float* q_scale;
+    // backward
+    const bf16* d_out;         // or null
+    const bf16* d_h;           // or null
+    bf16* d_y;                 // or null
+    bf16* d_residual;          // or null
+    void* d_gate;              // f32 [H], f32 [T] or bf16 [T, H], or null
+    float* d_post;             // f32 [H] or null
+    float* d_pre;              // f32 [H] or null
+    float* sums;               // partial column sums: [3][parts][H]
+    int64_t ldy, ldr, ldg, ldh, ldo, ldq, ldout_grad, ldh_grad, ldy_grad, ldr_grad, ldg_grad;
+    int T, H;
+    int gate_form, gate_act;
+    float residual_scale, block_scale, eps;
+    // set by the launchers
+    int vec, vec_weight, vec_q, parts;
+};
+
+cudaError_t launch_block_norm(const BlockNormArgs& args, cudaStream_t st);
+cudaError_t launch_block_norm_backward(const BlockNormArgs& args, cudaStream_t st);
+int64_t block_norm_workspace(int T, int H);
+
+// x bf16 [T, K] -> q int8 [T, K], one scale per row
+struct QuantizeArgs {
+    const bf16* x;
+    int8_t* q;
+    float* scale;
+    int64_t ldx, ldq;
+    int T, K;
+    int vec, vec_q;
+};
+cudaError_t launch_quantize_i8(const QuantizeArgs& args, cudaStream_t st);
+
+}  // namespace faasmoe

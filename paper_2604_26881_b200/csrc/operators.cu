@@ -2,8 +2,11 @@
 #include <cmath>
 
 #include "addnorm.cuh"
+#include "balance.cuh"
+#include "blocknorm.cuh"
 #include "gate.cuh"
 #include "project.cuh"
+#include "project_i8.cuh"
 
 using namespace faasmoe;
 
@@ -12,11 +15,42 @@ namespace {
 constexpr int kMaxRows = 1 << 28;
 constexpr int kProjectMaxTokens = 1 << 22;
 constexpr int kProjectMaxDim = 1 << 30;      // K, N, and the rows of all adapters' A
+constexpr int kRouterMaxRows = 1 << 27;      // (counts of up to 8 choices per token fit 32 bits)
+constexpr int kQuantizeMaxK = (1 << 24) - 1;
 
 bool off(const void* p, size_t align) { return ((uintptr_t)p & (align - 1)) != 0; }
 
 // an output in the place of an input needs the input's row distance: a row would be overwritten before it is read
 bool shifted(const void* out, int64_t ld_out, const void* in, int64_t ld_in, int T) { return out && out == in && T > 1 && ld_out != ld_in; }
+
+int check_block_rule(const moe_block_rule* r)
+{
+    if (!r) return MOE_ERR_NULL;
+    if (r->gate < MOE_GATE_NONE || r->gate > MOE_GATE_ELEMENT || (r->gate_act != MOE_GATE_RAW && r->gate_act != MOE_GATE_SIGMOID)) return MOE_ERR_SHAPE;
+    if (!std::isfinite(r->residual_scale) || !std::isfinite(r->block_scale) || !(r->eps >= 0.f) || !std::isfinite(r->eps)) return MOE_ERR_SHAPE;
+    return MOE_OK;
+}
+
+// what moe_balance_loss and moe_gate_backward check alike
+int check_router(const void* logits, int logits_type, int64_t ld, int T, int E, int k, const int32_t* topk_idx, const int32_t* tenant_id,
+                 const int32_t* model_of_tenant, int n_tenants, int M, const int32_t* status_out)
+{
+    if (T < 0 || T > kRouterMaxRows || E < 1 || E > kMaxExperts || k < 1 || k > kMaxTopK || k > E || ld < E) return MOE_ERR_SHAPE;
+    if (M < 1 || M > kMaxExperts || (tenant_id && n_tenants < 1)) return MOE_ERR_SHAPE;
+    if (logits_type != MOE_TYPE_F32 && logits_type != MOE_TYPE_BF16) return MOE_ERR_UNSUPPORTED;
+    if (off(logits, logits_type == MOE_TYPE_BF16 ? 2 : 4) || off(topk_idx, 4) || off(tenant_id, 4) || off(model_of_tenant, 4) || off(status_out, 4)) return MOE_ERR_SHAPE;
+    if (T > 0 && (!logits || (M > 1 && (!tenant_id || !model_of_tenant)))) return MOE_ERR_NULL;
+    return MOE_OK;
+}
+
+RouterBatch router_batch(const void* logits, int logits_type, int64_t ld, int T, int E, int k, int score, const int32_t* topk_idx,
+                         const uint8_t* mask, const int32_t* tenant_id, const int32_t* model_of_tenant, int n_tenants, int M, int32_t* status_out)
+{
+    RouterBatch b = {};
+    b.logits = logits; b.bf16_logits = logits_type == MOE_TYPE_BF16; b.ld = ld; b.T = T; b.E = E; b.k = k; b.score = score; b.topk_idx = topk_idx;
+    b.mask = mask; b.tenant_id = tenant_id; b.model_of_tenant = model_of_tenant; b.n_tenants = n_tenants; b.M = M; b.status = status_out;
+    return b;
+}
 
 }  // namespace
 
@@ -102,7 +136,11 @@ int64_t moe_project_workspace(int T, int K, int N, int rank, int n_adapters)
 int moe_project_status(int32_t* status_host)
 {
     if (!status_host) return MOE_ERR_NULL;
-    return cuda_result("moe_project_status", take_project_status(status_host));
+    cudaError_t e = take_project_status(status_host);
+    int32_t more = 0;
+    if (e == cudaSuccess) e = take_project_i8_status(&more);
+    *status_host |= more;
+    return cuda_result("moe_project_status", e);
 }
 
 int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, int K, int N, const void* a, const void* b,
@@ -140,6 +178,169 @@ int moe_project(const void* x, int64_t ldx, const void* w, int64_t ldw, int T, i
     p.u = (float*)workspace;
     p.status = status_out;
     return cuda_result("moe_project", launch_project(p, (cudaStream_t)stream));
+}
+
+int moe_block_norm(const void* block_out, int64_t ld_block, const void* residual, int64_t ld_residual, const void* post_weight,
+                   const void* pre_weight, const void* gate, int64_t ld_gate, const moe_block_rule* rule, int T, int H, void* h,
+                   int64_t ld_h, void* out, int64_t ld_out, int8_t* out_q, int64_t ld_q, float* q_scale, void* stream)
+{
+    const int rc = check_block_rule(rule);
+    if (rc != MOE_OK) return rc;
+    if (T < 0 || T > kMaxRows || H < 1) return MOE_ERR_SHAPE;
+    if (H > kBlockNormMaxH) return MOE_ERR_UNSUPPORTED;
+    const bool element = rule->gate == MOE_GATE_ELEMENT;
+    if (ld_block < H || ld_residual < H || ld_h < H || (out && ld_out < H) || (out_q && ld_q < H) || (element && ld_gate < H)) return MOE_ERR_SHAPE;
+    if (off(block_out, 2) || off(residual, 2) || off(post_weight, 2) || off(pre_weight, 2) || off(gate, rule->gate == MOE_GATE_TOKEN ? 4 : 2) ||
+        off(h, 2) || off(out, 2) || off(q_scale, 4))
+        return MOE_ERR_SHAPE;
+    if ((rule->gate == MOE_GATE_NONE && gate) || (!pre_weight && (out || out_q))) return MOE_ERR_SHAPE;
+    if (T == 0) return MOE_OK;
+    if (!block_out || !residual || !h || (rule->gate != MOE_GATE_NONE && !gate) || (pre_weight && !out && !out_q) || (out_q && !q_scale)) return MOE_ERR_NULL;
+    if (h == out || (out_q && ((const void*)out_q == block_out || (const void*)out_q == residual || (const void*)out_q == gate || (const void*)out_q == h || (const void*)out_q == out)))
+        return MOE_ERR_SHAPE;
+    for (int i = 0; i < 2; ++i) {
+        const void* o = i ? out : h;
+        const int64_t ld = i ? ld_out : ld_h;
+        if (shifted(o, ld, block_out, ld_block, T) || shifted(o, ld, residual, ld_residual, T)) return MOE_ERR_SHAPE;
+        if (o && o == gate && (!element || shifted(o, ld, gate, ld_gate, T))) return MOE_ERR_SHAPE;
+        if (o && (o == post_weight || o == pre_weight)) return MOE_ERR_SHAPE;
+    }
+    BlockNormArgs a = {};
+    a.y = (const bf16*)block_out; a.residual = (const bf16*)residual; a.post = (const bf16*)post_weight; a.pre = (const bf16*)pre_weight;
+    a.gate = gate; a.h = (bf16*)h; a.out = (bf16*)out; a.q = out_q; a.q_scale = q_scale;
+    a.ldy = ld_block; a.ldr = ld_residual; a.ldg = element ? ld_gate : 0; a.ldh = ld_h; a.ldo = out ? ld_out : 0; a.ldq = out_q ? ld_q : 0;
+    a.T = T; a.H = H; a.gate_form = rule->gate; a.gate_act = rule->gate_act;
+    a.residual_scale = rule->residual_scale; a.block_scale = rule->block_scale; a.eps = rule->eps;
+    return cuda_result("moe_block_norm", launch_block_norm(a, (cudaStream_t)stream));
+}
+
+int64_t moe_block_norm_workspace(int T, int H)
+{
+    if (T < 0 || T > kMaxRows || H < 1) return MOE_ERR_SHAPE;
+    return H > kBlockNormMaxH ? MOE_ERR_UNSUPPORTED : block_norm_workspace(T, H);
+}
+
+int moe_block_norm_backward(const void* block_out, int64_t ld_block, const void* h, int64_t ld_h, const void* post_weight,
+                            const void* pre_weight, const void* gate, int64_t ld_gate, const moe_block_rule* rule, int T, int H,
+                            const void* d_out, int64_t ld_d_out, const void* d_h, int64_t ld_d_h, void* d_block, int64_t ld_d_block,
+                            void* d_residual, int64_t ld_d_residual, void* d_gate, int64_t ld_d_gate, float* d_post_weight,
+                            float* d_pre_weight, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    const int rc = check_block_rule(rule);
+    if (rc != MOE_OK) return rc;
+    if (T < 0 || T > kMaxRows || H < 1) return MOE_ERR_SHAPE;
+    if (H > kBlockNormMaxH) return MOE_ERR_UNSUPPORTED;
+    const bool element = rule->gate == MOE_GATE_ELEMENT, channel = rule->gate == MOE_GATE_CHANNEL;
+    if (ld_block < H || (d_out && ld_h < H) || (element && ld_gate < H) || (d_out && ld_d_out < H) || (d_h && ld_d_h < H) ||
+        (d_block && ld_d_block < H) || (d_residual && ld_d_residual < H) || (element && d_gate && ld_d_gate < H))
+        return MOE_ERR_SHAPE;
+    if (off(block_out, 2) || off(h, 2) || off(post_weight, 2) || off(pre_weight, 2) || off(gate, rule->gate == MOE_GATE_TOKEN ? 4 : 2) || off(d_out, 2) ||
+        off(d_h, 2) || off(d_block, 2) || off(d_residual, 2) || off(d_gate, element ? 2 : 4) || off(d_post_weight, 4) || off(d_pre_weight, 4) ||
+        off(workspace, 16))
+        return MOE_ERR_SHAPE;
+    if ((rule->gate == MOE_GATE_NONE && (gate || d_gate)) || (!pre_weight && (d_out || d_pre_weight)) || (!post_weight && d_post_weight)) return MOE_ERR_SHAPE;
+    if (!d_block && !d_residual && !d_gate && !d_post_weight && !d_pre_weight) return T == 0 ? MOE_OK : MOE_ERR_NULL;
+    const bool sums = d_post_weight || d_pre_weight || (channel && d_gate);
+    if (T > 0) {
+        if (!block_out || (!d_out && !d_h) || (d_out && !h) || (rule->gate != MOE_GATE_NONE && !gate)) return MOE_ERR_NULL;
+        const int64_t need = sums ? block_norm_workspace(T, H) : 0;
+        if (need > 0 && !workspace) return MOE_ERR_NULL;
+        if (workspace_bytes < need) return MOE_ERR_ALLOC;
+        struct { const void* p; int64_t ld; } in[] = {{block_out, ld_block}, {d_out ? h : nullptr, ld_h}, {element ? gate : nullptr, ld_gate}, {d_out, ld_d_out}, {d_h, ld_d_h}},
+                                              out[] = {{d_block, ld_d_block}, {d_residual, ld_d_residual}, {element ? d_gate : nullptr, ld_d_gate}};
+        for (int i = 0; i < 3; ++i) {
+            for (const auto& v : in) if (shifted(out[i].p, out[i].ld, v.p, v.ld, T)) return MOE_ERR_SHAPE;
+            for (int j = 0; j < i; ++j) if (out[i].p && out[i].p == out[j].p) return MOE_ERR_SHAPE;
+        }
+    }
+    BlockNormArgs a = {};
+    a.y = (const bf16*)block_out; a.h = (bf16*)h; a.post = (const bf16*)post_weight; a.pre = (const bf16*)pre_weight; a.gate = gate;
+    a.d_out = (const bf16*)d_out; a.d_h = (const bf16*)d_h; a.d_y = (bf16*)d_block; a.d_residual = (bf16*)d_residual; a.d_gate = d_gate;
+    a.d_post = d_post_weight; a.d_pre = d_pre_weight; a.sums = sums ? (float*)workspace : nullptr;
+    a.ldy = ld_block; a.ldh = ld_h; a.ldg = element ? ld_gate : 0; a.ldout_grad = d_out ? ld_d_out : 0; a.ldh_grad = d_h ? ld_d_h : 0;
+    a.ldy_grad = d_block ? ld_d_block : 0; a.ldr_grad = d_residual ? ld_d_residual : 0; a.ldg_grad = element && d_gate ? ld_d_gate : 0;
+    a.T = T; a.H = H; a.gate_form = rule->gate; a.gate_act = rule->gate_act;
+    a.residual_scale = rule->residual_scale; a.block_scale = rule->block_scale; a.eps = rule->eps;
+    return cuda_result("moe_block_norm_backward", launch_block_norm_backward(a, (cudaStream_t)stream));
+}
+
+int moe_quantize_i8(const void* x, int64_t ldx, int T, int K, int8_t* q, int64_t ldq, float* scale, void* stream)
+{
+    if (T < 0 || T > kMaxRows || K < 1 || K > kQuantizeMaxK || ldx < K || ldq < K) return MOE_ERR_SHAPE;
+    if (off(x, 2) || off(scale, 4)) return MOE_ERR_SHAPE;
+    if (T == 0) return MOE_OK;
+    if (!x || !q || !scale) return MOE_ERR_NULL;
+    if ((const void*)q == x) return MOE_ERR_SHAPE;
+    QuantizeArgs a = {};
+    a.x = (const bf16*)x; a.q = q; a.scale = scale; a.ldx = ldx; a.ldq = ldq; a.T = T; a.K = K;
+    return cuda_result("moe_quantize_i8", launch_quantize_i8(a, (cudaStream_t)stream));
+}
+
+int moe_project_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw, const float* w_scale, int T,
+                   int K, int N, const float* bias, const void* base, int64_t ld_base, void* out, int64_t ld_out, int out_type,
+                   int32_t* status_out, void* stream)
+{
+    if (T < 0 || T > kProjectMaxTokens || K < 1 || K > kI8MaxK || N < 1 || N > kProjectMaxDim) return MOE_ERR_SHAPE;
+    if (ldx < K || ldw < K || ld_out < N || (base && ld_base < N)) return MOE_ERR_SHAPE;
+    if (out_type != MOE_TYPE_F32 && out_type != MOE_TYPE_BF16) return MOE_ERR_UNSUPPORTED;
+    // the operands travel as TMA tiles: rows on 16-byte boundaries
+    if (ldx % 16 || ldw % 16) return MOE_ERR_UNSUPPORTED;
+    const size_t out_align = out_type == MOE_TYPE_F32 ? 4 : 2;
+    if (off(x, 16) || off(w, 16) || off(x_scale, 4) || off(w_scale, 4) || off(bias, 4) || off(out, out_align) || off(base, out_align) || off(status_out, 4)) return MOE_ERR_SHAPE;
+    if (T == 0) return MOE_OK;
+    if (!x || !w || !x_scale || !w_scale || !out) return MOE_ERR_NULL;
+    if (out == (const void*)x || out == (const void*)w || shifted(out, ld_out, base, ld_base, T)) return MOE_ERR_SHAPE;
+    I8Args a = {};
+    a.x = x; a.w = w; a.x_scale = x_scale; a.w_scale = w_scale; a.bias = bias; a.base = base; a.out = out;
+    a.ldx = ldx; a.ldw = ldw; a.ldbase = base ? ld_base : 0; a.ldo = ld_out; a.T = T; a.K = K; a.N = N; a.out_f32 = out_type == MOE_TYPE_F32;
+    a.status = status_out;
+    return cuda_result("moe_project_i8", launch_project_i8(a, (cudaStream_t)stream));
+}
+
+int64_t moe_balance_workspace(int T, int E, int M)
+{
+    if (T < 0 || T > kRouterMaxRows || E < 1 || E > kMaxExperts || M < 1 || M > kMaxExperts) return MOE_ERR_SHAPE;
+    return balance_workspace(T, E, M);
+}
+
+int moe_balance_loss(const void* logits, int logits_type, int64_t ld, int T, int E, int k, int score, const int32_t* topk_idx,
+                     const uint8_t* mask, const int32_t* tenant_id, const int32_t* model_of_tenant, int n_tenants, int M,
+                     int32_t* counts, int32_t* tokens, float* mean_prob, float* loss, float* z_loss, void* workspace,
+                     int64_t workspace_bytes, int32_t* status_out, void* stream)
+{
+    const int rc = check_router(logits, logits_type, ld, T, E, k, topk_idx, tenant_id, model_of_tenant, n_tenants, M, status_out);
+    if (rc != MOE_OK) return rc;
+    if (score != MOE_SCORE_SOFTMAX && score != MOE_SCORE_SIGMOID) return MOE_ERR_SHAPE;
+    if (off(counts, 4) || off(tokens, 4) || off(mean_prob, 4) || off(loss, 4) || off(z_loss, 4) || off(workspace, 16)) return MOE_ERR_SHAPE;
+    if (!counts || !tokens || !mean_prob || !loss || (T > 0 && !topk_idx)) return MOE_ERR_NULL;
+    const int64_t need = balance_workspace(T, E, M);
+    if (need > 0 && !workspace) return MOE_ERR_NULL;
+    if (workspace_bytes < need) return MOE_ERR_ALLOC;
+    BalanceArgs a = {};
+    a.b = router_batch(logits, logits_type, ld, T, E, k, score, topk_idx, mask, tenant_id, model_of_tenant, n_tenants, M, status_out);
+    a.counts = counts; a.tokens = tokens; a.mean_prob = mean_prob; a.loss = loss; a.z_loss = z_loss; a.parts = (float*)workspace;
+    return cuda_result("moe_balance_loss", launch_balance(a, (cudaStream_t)stream));
+}
+
+int moe_gate_backward(const void* logits, int logits_type, int64_t ld, int T, int E, int k, const moe_gating* rule,
+                      const int32_t* topk_idx, const float* d_topk_w, const uint8_t* mask, const int32_t* tenant_id,
+                      const int32_t* model_of_tenant, int n_tenants, int M, const int32_t* counts, const int32_t* tokens,
+                      const float* d_loss, const float* d_z_loss, void* d_logits, int64_t ld_d, int32_t* status_out, void* stream)
+{
+    if (!rule) return MOE_ERR_NULL;
+    int rc = check_router(logits, logits_type, ld, T, E, k, topk_idx, tenant_id, model_of_tenant, n_tenants, M, status_out);
+    if (rc == MOE_OK) rc = check_gating(rule, E, k);
+    if (rc != MOE_OK) return rc;
+    if (ld_d < E) return MOE_ERR_SHAPE;
+    if (off(d_topk_w, 4) || off(counts, 4) || off(tokens, 4) || off(d_loss, 4) || off(d_z_loss, 4) || off(d_logits, logits_type == MOE_TYPE_BF16 ? 2 : 4)) return MOE_ERR_SHAPE;
+    if (T == 0) return MOE_OK;
+    if (!d_logits || (!d_topk_w && !d_loss && !d_z_loss) || (d_topk_w && !topk_idx) || (d_loss && !counts) || ((d_loss || d_z_loss) && !tokens)) return MOE_ERR_NULL;
+    if (shifted(d_logits, ld_d, logits, ld, T)) return MOE_ERR_SHAPE;
+    GateGradArgs a = {};
+    a.b = router_batch(logits, logits_type, ld, T, E, k, rule->score, topk_idx, mask, tenant_id, model_of_tenant, n_tenants, M, status_out);
+    a.renormalize = rule->renormalize != 0; a.scale = rule->scale; a.d_w = d_topk_w; a.counts = counts; a.tokens = tokens; a.d_loss = d_loss;
+    a.d_z = d_z_loss; a.d_logits = d_logits; a.ld_d = ld_d;
+    return cuda_result("moe_gate_backward", launch_gate_grad(a, (cudaStream_t)stream));
 }
 
 }  // extern "C"

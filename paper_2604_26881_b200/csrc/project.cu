@@ -16,8 +16,8 @@
 // adapters alone beside a base, 1126 tokens, 13 of rank 64: 28 us, first product 12 of them.
 #include <cstring>
 
+#include "cluster_ptx.cuh"
 #include "project.cuh"
-#include "tc_ptx.cuh"
 
 namespace faasmoe {
 
@@ -41,35 +41,6 @@ constexpr int kUCols = 128;             // columns of one CTA of the first produ
 constexpr int kUThreads = 288;          // warp 0: TMA (tokens), 1, 7: MMA, 2..5: lists and epilogue, 6, 8: TMA (rows of A)
 constexpr int kPN = 128;                // weight rows per tile of the projection
 constexpr int kPThreads = 352;          // warp 0: TMA (weights), 1: MMA, 2..9: epilogue, 10: TMA (tokens)
-
-__device__ __forceinline__ uint32_t cluster_ctarank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t map_to_cta(uint32_t local_addr, uint32_t rank)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local_addr), "r"(rank));
-    return r;
-}
-// Copies shared memory of this CTA to another of the cluster; the bytes are counted on a barrier of the receiver.  (Single
-// remote stores were measured at about 30 cycles each, one after the other: 4 us for one token's sums in a cluster of eight.)
-__device__ __forceinline__ void send_bulk(uint32_t dst, uint32_t src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "r"(src), "r"(bytes), "r"(bar) : "memory");
-}
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-// (nothing that was written before is handed over: only that this CTA has come so far)
-__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void cluster_sync_all()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 
 // instruction descriptor: bf16 x bf16 -> fp32, K-major operands, M = 128
 __device__ __forceinline__ uint32_t idesc_bf16(int n)
@@ -767,11 +738,6 @@ constexpr int kMThreads = 480;                         // warp 0: TMA (weights),
 constexpr int kBRows = kTok / 2;                       // rows of an adapter's B in one load
 constexpr int kUTile = kTok * kBK * 2;                 // one bf16 tile of 64 columns of u
 
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y)
-{
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(dst), "l"(map), "r"(bar & 0xFEFFFFFFu), "r"(x), "r"(y) : "memory");
-}
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z)
 {
     asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -789,16 +755,6 @@ __device__ __forceinline__ void umma_pair_masked(uint32_t d, uint64_t a, uint64_
                  "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%5, %6, %7, %8, %9, %10, %11, %12}, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(m[0]), "r"(m[1]), "r"(m[2]), "r"(m[3]), "r"(m[4]), "r"(m[5]),
                  "r"(m[6]), "r"(m[7]) : "memory");
-}
-// arrives on the barrier at the same offset in both CTAs of the pair
-__device__ __forceinline__ void umma_commit_pair(uint32_t bar)
-{
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((unsigned short)3) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr)
-{
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 __device__ __forceinline__ void builders_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 

@@ -1,0 +1,452 @@
+"""moe_balance_loss and moe_gate_backward against their definitions in 64 bits.
+
+Tolerances (u = 2^-24): an exponential is off by 2 ulp = 4 u of itself and by 2 u |z - max| for its rounded argument (|z - max| <= 24
+here: 48 u), a sum of 16 + 4 terms by 20 u, quotients and products by 8 u more: a share p is off by at most 100 u relative.  A mean
+adds sums of fp32 over a lane's tokens (at most 64), 8 groups, 8 warps, and of the blocks: 100 u more.  Losses are sums of those.
+A gradient is a sum of at most four terms, each within 300 u of the magnitudes that meet in it; 0.5 u or 2^-8 for its own type.
+"""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_26881_b200 import binding as B
+
+gpu = pytest.mark.gpu
+U, BF16_HALF = 2.0 ** -24, 2.0 ** -8
+
+
+def clean(z):
+    z = z.astype(np.float64)
+    z = np.where(np.isnan(z), -np.inf, z)
+    return np.minimum(z, float(np.finfo(np.float32).max))
+
+
+def scores(z, score):
+    """shares p, softmax, its log-sum, 1 - s (1 for softmax), raw scores; zeros for rows without a logit."""
+    with np.errstate(all="ignore"):
+        top = z.max(1, keepdims=True)
+        some = top[:, 0] > -np.inf
+        e = np.where(some[:, None], np.exp(z - np.where(some[:, None], top, 0)), 0)
+        total = e.sum(1)
+        soft = e / np.where(total > 0, total, 1)[:, None]
+        lse = np.where(some, top[:, 0] + np.log(np.where(total > 0, total, 1)), 0)
+        if score == "softmax":
+            return soft, soft, lse, np.ones_like(z), soft
+        a = np.exp(-np.abs(z))
+        s, slope = np.where(z >= 0, 1 / (1 + a), a / (1 + a)), np.where(z >= 0, a / (1 + a), 1 / (1 + a))
+        log_s = -np.logaddexp(0, -z)                                   # shares of far negative logits do not underflow
+        lt = log_s.max(1, keepdims=True)
+        w = np.where(some[:, None], np.exp(log_s - np.where(some[:, None], lt, 0)), 0)
+        return w / np.where(some, w.sum(1), 1)[:, None], soft, lse, slope, s
+
+
+def reference(z, idx, score, M=1, live=None, model=None):
+    T, E = z.shape
+    k = idx.shape[1]
+    live = np.ones(T, bool) if live is None else live
+    model = np.zeros(T, int) if model is None else model
+    p, _, lse, _, _ = scores(z, score)
+    out = dict(counts=np.zeros((M, E), np.int64), tokens=np.zeros(M, np.int64), mean=np.zeros((M, E)), loss=np.zeros(M), z=np.zeros(M))
+    for m in range(M):
+        t = np.nonzero(live & (model == m))[0]
+        out["tokens"][m] = t.size
+        if t.size:
+            ids = idx[t].ravel()
+            out["counts"][m] = np.bincount(ids[(ids >= 0) & (ids < E)], minlength=E)
+            out["mean"][m] = p[t].mean(0)
+            out["loss"][m] = E / (k * t.size) * (out["counts"][m] * out["mean"][m]).sum()
+            out["z"][m] = (lse[t] ** 2).mean()
+    return out
+
+
+def gradient(z, idx, gate, ref, d_w=None, d_loss=None, d_z=None, live=None, model=None):
+    """The formula's gradient and the magnitudes that meet in it."""
+    T, E = z.shape
+    k = idx.shape[1]
+    live = np.ones(T, bool) if live is None else live
+    model = np.zeros(T, int) if model is None else model
+    p, soft, lse, slope, s = scores(z, gate["score"])
+    g, size = np.zeros((T, E)), np.zeros((T, E))
+    rows = np.arange(T)
+    if d_w is not None:
+        gw = d_w.astype(np.float64) * gate.get("scale", 1.0)
+        ok = (idx >= 0) & (idx < E)
+        at = np.where(ok, idx, 0)
+        if gate.get("renorm"):
+            if gate["score"] == "softmax":
+                lw = np.where(ok, z[rows[:, None], at], -np.inf)
+            else:
+                lw = np.where(ok, -np.logaddexp(0, -z[rows[:, None], at]), -np.inf)
+            top = lw.max(1, keepdims=True)
+            w = np.where(top > -np.inf, np.exp(lw - np.where(top > -np.inf, top, 0)), 0)
+            w = w / np.where(w.sum(1) > 0, w.sum(1), 1)[:, None]
+            mean, amean = (gw * w).sum(1, keepdims=True), (np.abs(gw) * w).sum(1, keepdims=True)
+            inner, ainner = w * (gw - mean), w * (np.abs(gw) + amean)
+        else:
+            w = np.where(ok, s[rows[:, None], at], 0)
+            inner, ainner = gw * w, np.abs(gw) * w
+            if gate["score"] == "softmax":
+                g -= soft * inner.sum(1, keepdims=True)
+                size += soft * ainner.sum(1, keepdims=True)
+        for j in range(k):
+            np.add.at(g, (rows[ok[:, j]], at[ok[:, j], j]), (inner[:, j] * slope[rows, at[:, j]])[ok[:, j]])
+            np.add.at(size, (rows[ok[:, j]], at[ok[:, j], j]), (ainner[:, j] * slope[rows, at[:, j]])[ok[:, j]])
+    n = np.maximum(ref["tokens"][model], 1).astype(np.float64)
+    if d_loss is not None:
+        f = ref["counts"][model] * (d_loss.astype(np.float64)[model] * E / (k * n * n))[:, None]
+        g += p * slope * (f - (f * p).sum(1, keepdims=True))
+        size += p * slope * (np.abs(f) + (np.abs(f) * p).sum(1, keepdims=True))
+    if d_z is not None:
+        x = soft * (2 * d_z.astype(np.float64)[model] / n)[:, None] * lse[:, None]
+        g += x
+        size += np.abs(x)
+    return np.where(live[:, None], g, 0), np.where(live[:, None], size, 0)
+
+
+def check(T, E, k, score="softmax", renorm=True, scale=1.0, M=1, tenants=None, masked=False, dtype=torch.float32, pad=0, shift=0, use=("w", "loss", "z"),
+          z=None, idx=None, seed=0, tenant=None, model_of_tenant=None, bits=0, mask=None):
+    g = torch.Generator().manual_seed(seed + 3 * T + 7 * E + k)
+    rng = np.random.RandomState(seed + T + E)
+    z0 = (torch.randn(T, E, generator=g) * 1.5 if z is None else z).to(dtype)
+    if idx is None:
+        idx = torch.stack([torch.randperm(E, generator=g)[:k] for _ in range(T)]).to(torch.int32) if T < 3000 else torch.topk(z0.float(), k)[1].to(torch.int32)
+    if mask is None:
+        mask = (torch.rand(T, generator=g) < 0.7).to(torch.uint8) if masked else None
+    tenants = M if tenants is None else tenants
+    if M > 1 and tenant is None:
+        tenant = torch.from_numpy(rng.randint(0, tenants, T).astype(np.int32))
+    if model_of_tenant is None and tenant is not None:
+        model_of_tenant = (torch.arange(tenants) * 5 + 1).to(torch.int32) % M
+    store = torch.full((T * (E + pad) + shift + 8,), float("nan"), device="cuda:0", dtype=dtype)
+    zd = store[shift:shift + T * (E + pad)].view(T, E + pad)[:, :E]
+    zd.copy_(z0)
+    gs = torch.full((T * (E + pad) + shift + 8,), 7.0, device="cuda:0", dtype=dtype)
+    gd = gs[shift:shift + T * (E + pad)].view(T, E + pad)[:, :E]
+    dev = lambda t: None if t is None else t.cuda()
+    e = lambda *s, dt=torch.float32: torch.full(s, 9, dtype=dt, device="cuda:0")
+    counts, tokens, mean, loss, zl = e(M, E, dt=torch.int32), e(M, dt=torch.int32), e(M, E), e(M), e(M)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    same = dict(mask=dev(mask), tenant_id=dev(tenant), model_of_tenant=dev(model_of_tenant), status_out=status)
+    B.moe_balance_loss(zd, idx.cuda(), counts, tokens, mean, loss, score=score, z_loss=zl, **same)
+    torch.cuda.synchronize()
+    assert int(status) == bits
+    zc, ids = clean(z0.float().numpy()), idx.numpy()
+    live = np.ones(T, bool) if mask is None else mask.numpy() != 0
+    model = np.zeros(T, int)
+    if tenant is not None:
+        t = tenant.numpy()
+        good = (t >= 0) & (t < len(model_of_tenant))
+        model = model_of_tenant.numpy()[np.where(good, t, 0)]
+        model = np.where((model >= 0) & (model < M), model, 0)
+        live &= good
+    ref = reference(zc, ids, score, M, live, model)
+    np.testing.assert_array_equal(counts.cpu().numpy(), ref["counts"])
+    np.testing.assert_array_equal(tokens.cpu().numpy(), ref["tokens"])
+    np.testing.assert_allclose(mean.cpu().numpy(), ref["mean"], rtol=200 * U, atol=1e-37)
+    np.testing.assert_allclose(loss.cpu().numpy(), ref["loss"], rtol=202 * U, atol=1e-37)
+    lse_size = np.abs(zc[live]).max(initial=0) if np.isfinite(zc).all() else 1.0
+    with np.errstate(over="ignore"):                                   # (beyond 3.4e38 the output's type holds infinity)
+        want_z = ref["z"].astype(np.float32)
+    np.testing.assert_allclose(zl.cpu().numpy(), want_z, rtol=300 * U, atol=300 * U * (lse_size + 1))
+    rule = B.moe_gating(score=score, renormalize=renorm, scale=scale)
+    d_w = torch.randn(T, k, generator=g)
+    d_loss, d_z = torch.rand(M, generator=g) + 0.5, torch.rand(M, generator=g) + 0.5
+    args = dict(d_topk_w=dev(d_w) if "w" in use else None, d_loss=dev(d_loss) if "loss" in use else None, d_z_loss=dev(d_z) if "z" in use else None)
+    B.moe_gate_backward(zd, rule, idx.cuda(), gd, counts=counts, tokens=tokens, **args, **same)
+    torch.cuda.synchronize()
+    keep = torch.ones(gs.numel(), dtype=torch.bool)
+    keep[(torch.arange(T)[:, None] * (E + pad) + torch.arange(E) + shift).flatten()] = False
+    assert (gs.cpu().float()[keep] == 7).all(), "written outside the rows"
+    want, size = gradient(zc, ids, dict(score=score, renorm=renorm, scale=scale), ref, d_w.numpy() if "w" in use else None,
+                          d_loss.numpy() if "loss" in use else None, d_z.numpy() if "z" in use else None, live, model)
+    half = BF16_HALF if dtype == torch.bfloat16 else U
+    got = gd.cpu().double().numpy()
+    lim = half * np.abs(want) + 300 * U * size + 300 * U * (lse_size + 1) * (size > 0) * ("z" in use) * U + 1e-37
+    assert (np.abs(got - want) <= lim).all(), (np.abs(got - want) / lim).max()
+    return dict(counts=counts, tokens=tokens, mean=mean, loss=loss, z=zl, d=gd)
+
+
+@gpu
+@pytest.mark.parametrize("E", [1, 2, 3, 4, 7, 8, 15, 16, 17, 31, 32, 60, 63, 64, 65, 100, 127, 128, 129, 160, 200, 255, 256])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_every_number_of_experts(E, score):
+    for k in {1, min(E, 4), min(E, 8)}:
+        check(50, E, k, score, renorm=k != 4, scale=2.5)
+
+
+@gpu
+@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 31, 32, 33, 255, 256, 257, 300, 1126, 5000])
+def test_numbers_of_tokens(T):
+    check(T, 60, 4)
+    check(T, 60, 4, "sigmoid", masked=True, dtype=torch.bfloat16, pad=4)
+    check(T, 256, 8, "sigmoid", renorm=False)
+    check(T, 100, 6, "softmax", renorm=False, masked=True)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (4, 0), (3, 0), (0, 1), (8, 8), (1, 3)])
+def test_strides_and_alignment(dtype, pad, shift):
+    for E, k in ((60, 4), (62, 4), (128, 8), (250, 8), (256, 8)):
+        check(40, E, k, "sigmoid" if pad else "softmax", dtype=dtype, pad=pad, shift=shift)
+
+
+@gpu
+@pytest.mark.parametrize("M,tenants", [(2, 5), (4, 4), (7, 3), (60, 100), (256, 256)])
+def test_models(M, tenants):
+    check(700, 60, 4, M=M, tenants=tenants, masked=True)
+    check(33, 256, 8, "sigmoid", M=M, tenants=tenants)
+
+
+@gpu
+@pytest.mark.parametrize("use", [("w",), ("loss",), ("z",), ("w", "z"), ("loss", "z"), ("w", "loss")])
+def test_gradients_each_alone(use):
+    for score in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            check(70, 60, 4, score, renorm=renorm, use=use, masked=True)
+            check(70, 200, 8, score, renorm=renorm, use=use, M=3)
+
+
+@gpu
+def test_the_same_expert_twice_and_ids_out_of_range():
+    idx = torch.randint(0, 5, (90, 8), generator=torch.Generator().manual_seed(1)).to(torch.int32)
+    for E in (8, 100, 256):
+        for score, renorm in (("softmax", True), ("sigmoid", False), ("softmax", False), ("sigmoid", True)):
+            check(90, E, 8, score, renorm=renorm, idx=idx)
+    bad = idx.clone()
+    bad[3, 2], bad[50, 7], bad[60] = -1, 256, torch.arange(300, 308).to(torch.int32)
+    for E in (60, 256):
+        for renorm in (True, False):
+            check(90, E, 8, renorm=renorm, idx=bad, bits=B.MOE_DEV_BAD_EXPERT)
+
+
+@gpu
+def test_tenants_out_of_range_take_no_part():
+    tenant = torch.randint(0, 6, (200,), generator=torch.Generator().manual_seed(2)).to(torch.int32)
+    tenant[5], tenant[77], tenant[199] = -1, 6, 1 << 30
+    table = torch.tensor([0, 1, 2, -3, 9, 1], dtype=torch.int32)       # entries out of range: model 0
+    check(200, 60, 4, M=3, tenant=tenant, model_of_tenant=table, bits=B.MOE_DEV_BAD_TENANT)
+    check(200, 60, 4, M=1, tenant=tenant, model_of_tenant=table, bits=B.MOE_DEV_BAD_TENANT)
+
+
+@gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,k", [(60, 4), (256, 8)])
+def test_infinities_nan_and_far_logits(score, E, k):
+    g = torch.Generator().manual_seed(3)
+    z = torch.randn(40, E, generator=g)
+    inf, nan = float("inf"), float("nan")
+    z[0, 3], z[1, 5], z[2, :] = -inf, nan, -inf
+    z[3, 1:] = -inf
+    z[4, :] = nan
+    z[5, :] = torch.finfo(torch.float32).min
+    z[6, :] -= 100
+    z[7, :] -= 200
+    z[8, :] -= 59
+    z[9, :] += 80
+    z[10, ::2] = -inf
+    z[11, :] = -300 + 20 * torch.rand(E, generator=g)
+    for renorm in (True, False):
+        for use in (("w", "loss"), ("w",)):
+            check(40, E, k, score, renorm=renorm, z=z, use=use)
+    # the largest values: one expert has it all
+    z = torch.randn(20, E, generator=g)
+    z[0, 3], z[1, 4], z[2, 5] = inf, torch.finfo(torch.float32).max, 1e30
+    z[3, 1] = z[3, 2] = inf
+    check_far(z, E, k, score)
+
+
+def check_far(z, E, k, score):
+    """Where the second loss is infinite: everything but that."""
+    T = z.shape[0]
+    idx = torch.topk(torch.nan_to_num(z, posinf=3e38), k)[1].to(torch.int32).cuda()
+    e = lambda *s, dt=torch.float32: torch.empty(*s, dtype=dt, device="cuda:0")
+    counts, tokens, mean, loss, d = e(1, E, dt=torch.int32), e(1, dt=torch.int32), e(1, E), e(1), e(T, E)
+    B.moe_balance_loss(z.cuda(), idx, counts, tokens, mean, loss, score=score)
+    ref = reference(clean(z.numpy()), idx.cpu().numpy(), score)
+    np.testing.assert_allclose(mean.cpu().numpy(), ref["mean"], rtol=200 * U)
+    np.testing.assert_allclose(loss.cpu().numpy(), ref["loss"], rtol=200 * U)
+    dw = torch.randn(T, k, generator=torch.Generator().manual_seed(1))
+    for renorm in (True, False):
+        B.moe_gate_backward(z.cuda(), B.moe_gating(score=score, renormalize=renorm), idx, d, d_topk_w=dw.cuda(), counts=counts, tokens=tokens,
+                            d_loss=torch.ones(1, device="cuda:0"))
+        want, size = gradient(clean(z.numpy()), idx.cpu().numpy(), dict(score=score, renorm=renorm), ref, dw.numpy(), np.ones(1, np.float32))
+        assert (np.abs(d.cpu().double().numpy() - want) <= 300 * U * size + 1e-37).all()
+
+
+@gpu
+def test_masked_tokens_are_not_looked_at():
+    T, E, k = 100, 60, 4
+    z = torch.randn(T, E, generator=torch.Generator().manual_seed(1))
+    idx = torch.topk(z, k)[1].to(torch.int32)
+    mask = (torch.arange(T) % 3 != 0).to(torch.uint8)
+    clean_run = check(T, E, k, z=z, idx=idx, mask=mask)
+    z2, idx2 = z.clone(), idx.clone()
+    z2[::3], idx2[::3] = float("nan"), 10 ** 6
+    dirty = check(T, E, k, z=z2, idx=idx2, mask=mask)
+    for name in clean_run:
+        assert torch.equal(clean_run[name], dirty[name]), name
+    assert (dirty["d"][::3] == 0).all()
+    none = check(T, E, k, z=z, idx=idx, mask=torch.zeros(T, dtype=torch.uint8))
+    assert all((v == 0).all() for v in none.values())
+
+
+@gpu
+def test_no_tokens():
+    e = lambda *s, dt=torch.float32: torch.full(s, 5, dtype=dt, device="cuda:0")
+    counts, tokens, mean, loss, zl = e(3, 60, dt=torch.int32), e(3, dt=torch.int32), e(3, 60), e(3), e(3)
+    idx = e(0, 4, dt=torch.int32)
+    t = dict(tenant_id=e(0, dt=torch.int32), model_of_tenant=e(3, dt=torch.int32))
+    B.moe_balance_loss(e(0, 60), idx, counts, tokens, mean, loss, z_loss=zl, **t)
+    assert all((v == 0).all() for v in (counts, tokens, mean, loss, zl))
+    B.moe_gate_backward(e(0, 60), B.moe_gating(), idx, e(0, 60), d_loss=loss, counts=counts, tokens=tokens, **t)
+
+
+@gpu
+def test_gradient_in_the_place_of_the_logits():
+    z = torch.randn(300, 60, generator=torch.Generator().manual_seed(1)).cuda()
+    idx = torch.topk(z, 4)[1].to(torch.int32)
+    dw = torch.randn(300, 4, generator=torch.Generator().manual_seed(2)).cuda()
+    d = torch.empty_like(z)
+    B.moe_gate_backward(z, B.moe_gating(), idx, d, d_topk_w=dw)
+    B.moe_gate_backward(z, B.moe_gating(), idx, z, d_topk_w=dw)
+    assert torch.equal(z, d)
+
+
+@gpu
+def test_gradient_against_differences():
+    """Of sum(d_w w) + d_loss loss(p) + d_z z_loss with the counts held, w out of moe_gate's own rule in 64 bits."""
+    T, E, k = 6, 20, 3
+    for score in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            g = torch.Generator().manual_seed(4)
+            z = torch.randn(T, E, generator=g)
+            idx = torch.topk(z, k)[1].to(torch.int32)
+            d_w, e = torch.randn(T, k, generator=g), lambda *s, dt=torch.float32: torch.empty(*s, dtype=dt, device="cuda:0")
+            counts, tokens, mean, loss, zl, d = e(1, E, dt=torch.int32), e(1, dt=torch.int32), e(1, E), e(1), e(1), e(T, E)
+            B.moe_balance_loss(z.cuda(), idx.cuda(), counts, tokens, mean, loss, score=score, z_loss=zl)
+            B.moe_gate_backward(z.cuda(), B.moe_gating(score=score, renormalize=renorm, scale=2.5), idx.cuda(), d, d_topk_w=d_w.cuda(), counts=counts,
+                                tokens=tokens, d_loss=torch.tensor([0.7]).cuda(), d_z_loss=torch.tensor([0.3]).cuda())
+            c = counts.cpu().double().numpy()
+
+            def f(z):
+                p, _, lse, _, s = scores(z, score)
+                w = np.take_along_axis(s, idx.numpy(), 1)
+                if renorm:
+                    w = w / w.sum(1, keepdims=True)
+                return (d_w.numpy() * w * 2.5).sum() + np.float32(0.7) * E / (k * T) * (c * p.mean(0)).sum() + np.float32(0.3) * (lse ** 2).mean()
+            zz, step = z.double().numpy(), 2.0 ** -10
+            for t, x in ((0, 0), (1, int(idx[1, 0])), (2, int(idx[2, 2])), (5, E - 1), (3, 7)):
+                up, down = zz.copy(), zz.copy()
+                up[t, x] += step
+                down[t, x] -= step
+                want = (f(up) - f(down)) / (2 * step)
+                assert abs(float(d[t, x]) - want) <= 1e-5 * 10 + 1e-6, (score, renorm, t, x)      # third derivatives of order 10, step^2 / 6
+
+
+@gpu
+def test_long_batches_offsets_and_repeatability():
+    T, E, k = 40000, 256, 8
+    a = check(T, E, k, "sigmoid", scale=2.5)
+    b = check(T, E, k, "sigmoid", scale=2.5)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+    # rows far apart: offsets beyond 32 bits
+    big = torch.zeros(3, 1 << 30, device="cuda:0")
+    z = torch.randn(3, 60, generator=torch.Generator().manual_seed(1))
+    big[:, :60].copy_(z)
+    idx = torch.topk(z, 4)[1].to(torch.int32).cuda()
+    dw = torch.randn(3, 4, generator=torch.Generator().manual_seed(2)).cuda()
+    d, w = torch.empty(3, 60, device="cuda:0"), torch.empty(3, 60, device="cuda:0")
+    B.moe_gate_backward(big[:, :60], B.moe_gating(), idx, d, d_topk_w=dw)
+    B.moe_gate_backward(z.cuda(), B.moe_gating(), idx, w, d_topk_w=dw)
+    assert torch.equal(d, w)
+
+
+@gpu
+def test_streams_graphs_and_workspaces():
+    T, E, k = 9000, 60, 4
+    z = torch.randn(T, E, generator=torch.Generator().manual_seed(1)).cuda()
+    idx = torch.topk(z, k)[1].to(torch.int32)
+    dw = torch.randn(T, k, generator=torch.Generator().manual_seed(2)).cuda()
+    one = torch.ones(1, device="cuda:0")
+
+    def new():
+        e = lambda *s, dt=torch.float32: torch.zeros(*s, dtype=dt, device="cuda:0")
+        return dict(counts=e(E, dt=torch.int32), tokens=e(1, dt=torch.int32), mean=e(E), loss=e(1), z=e(1), d=e(T, E))
+
+    def call(o, ws, stream=None):
+        B.moe_balance_loss(z, idx, o["counts"], o["tokens"], o["mean"], o["loss"], z_loss=o["z"], workspace=ws, stream=stream)
+        B.moe_gate_backward(z, B.moe_gating(renormalize=True), idx, o["d"], d_topk_w=dw, counts=o["counts"], tokens=o["tokens"], d_loss=one, d_z_loss=one, stream=stream)
+    want = new()
+    call(want, None)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    n = B.moe_balance_workspace(T, E)
+    assert n > 0
+    spaces = [torch.full((n,), 255, dtype=torch.uint8, device="cuda:0") for _ in streams]
+    outs = [new() for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for o, w, s in zip(outs, spaces, streams):
+            call(o, w, s)
+    call(outs[0], None, streams[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o[name], want[name]) for o in outs for name in want)
+    graphs, outs = [], [new(), new()]
+    for o, w in zip(outs, spaces):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            call(o, w)
+        graphs.append(gr)
+    for _ in range(3):
+        for gr, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                gr.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o[name], want[name]) for o in outs for name in want)
+
+
+def test_refusals_of_the_c_entry_points():
+    lib, p = B.load_library(), ctypes.c_void_p
+    a = [p(4096 * (i + 1)) for i in range(20)]                          # (never dereferenced)
+
+    def balance(z=a[0], kind=0, ld=60, T=9000, E=60, k=4, score=0, idx=a[1], mask=None, ten=None, mot=None, nt=0, M=1, counts=a[2], tokens=a[3], mean=a[4],
+                loss=a[5], zl=a[6], ws=a[7], n=1 << 30, st=None):
+        return lib.moe_balance_loss(z, kind, ld, T, E, k, score, idx, mask, ten, mot, nt, M, counts, tokens, mean, loss, zl, ws, n, st, None)
+    for kw in (dict(T=-1), dict(T=(1 << 27) + 1), dict(E=0), dict(E=257, ld=257), dict(k=0), dict(k=9), dict(E=3, ld=3), dict(ld=59), dict(score=2), dict(M=0),
+               dict(M=257), dict(ten=a[8], nt=0), dict(z=p(4098)), dict(idx=p(4098)), dict(loss=p(4098)), dict(ws=p(4104)), dict(st=p(4098))):
+        assert balance(**kw) == B.MOE_ERR_SHAPE, kw
+    for kw in (dict(z=None), dict(idx=None), dict(counts=None), dict(tokens=None), dict(mean=None), dict(loss=None), dict(ws=None), dict(M=2),
+               dict(M=2, ten=a[8], nt=3)):
+        assert balance(**kw) == B.MOE_ERR_NULL, kw
+    assert balance(kind=2) == B.MOE_ERR_UNSUPPORTED and balance(n=8) == B.MOE_ERR_ALLOC
+    assert lib.moe_balance_workspace(-1, 60, 1) == B.MOE_ERR_SHAPE and lib.moe_balance_workspace(5, 60, 1) == 0
+
+    def back(z=a[0], kind=0, ld=60, T=10, E=60, k=4, rule=B.moe_gating(), idx=a[1], dw=a[2], mask=None, ten=None, mot=None, nt=0, M=1, counts=a[3], tokens=a[4],
+             dl=a[5], dz=a[6], d=a[7], ldd=60, st=None):
+        return lib.moe_gate_backward(z, kind, ld, T, E, k, ctypes.byref(rule) if rule else None, idx, dw, mask, ten, mot, nt, M, counts, tokens, dl, dz, d, ldd, st, None)
+    assert back(T=0, z=None, idx=None, d=None) == B.MOE_OK
+    for kw in (dict(T=-1), dict(E=257, ld=257), dict(k=9), dict(ld=59), dict(ldd=59), dict(M=0), dict(d=p(4098)), dict(dw=p(4098)), dict(d=a[0], ldd=64),
+               dict(rule=B.moe_gating(scale=float("inf")))):
+        assert back(**kw) == B.MOE_ERR_SHAPE, kw
+    for kw in (dict(rule=None), dict(z=None), dict(d=None), dict(dw=None, dl=None, dz=None), dict(idx=None), dict(counts=None), dict(tokens=None), dict(M=2)):
+        assert back(**kw) == B.MOE_ERR_NULL, kw
+
+
+def test_refusals_of_the_binding():
+    z, idx = torch.zeros(5, 8), torch.zeros(5, 2, dtype=torch.int32)
+    c, n, m, l = torch.zeros(8, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(8), torch.zeros(1)
+    for args in ((z.double(), idx, c, n, m, l), (z[0], idx, c, n, m, l), (z, idx.long(), c, n, m, l), (z, idx[:3], c, n, m, l), (z, idx, c[:7], n, m, l),
+                 (z, idx, c, n, m[:7], l), (z, idx, c, n, m, torch.zeros(2)), (z, idx, c, None, m, l), (z, idx, c, n, m, l)):
+        with pytest.raises(ValueError):
+            B.moe_balance_loss(*args)
+    with pytest.raises(KeyError):
+        B.moe_balance_loss(z, idx, c, n, m, l, score="tanh")
+    rule = B.moe_gating()
+    for kw in (dict(rule="softmax"), dict(d_logits=z[:3]), dict(d_logits=None), dict(d_topk_w=torch.zeros(5, 3)), dict(d_loss=l, counts=c[:4], tokens=n),
+               dict(d_loss=l, d_z_loss=torch.zeros(2), counts=c, tokens=n), dict(mask=torch.zeros(4, dtype=torch.uint8)), {}):
+        args = dict(logits=z, rule=rule, topk_idx=idx, d_logits=z.clone(), d_topk_w=torch.zeros(5, 2))
+        args.update(kw)
+        with pytest.raises(ValueError):
+            B.moe_gate_backward(args.pop("logits"), args.pop("rule"), args.pop("topk_idx"), args.pop("d_logits"), **args)

@@ -1,0 +1,502 @@
+"""moe_block_norm and moe_block_norm_backward against the formulas in 64 bits.
+
+Tolerances, from the roundings (u = 2^-24, half a step of fp32).  A norm's factor 1 / sqrt(mean + eps) is off by at most 32 u (sums
+at most 53 deep, halved by the root) + 3 u; a sigmoid by 8 u (expf 2 ulp, a sum, a quotient); the products up to a by 6 u, so a is
+off by 60 u relative.  h adds one fp32 rounding of each of its two terms and half a bf16 step (2^-8); out and q are compared with
+the formula on the h that was stored: 40 u, and half a step of bf16, or of the integers.
+
+A gradient is compared with the formula's, whose every sum of terms v_i of either sign is off by at most c u sum |v_i|; c = 160 covers
+the 60 u of each factor (three at most meet in a product) and sums over a row at most 53 deep.  Errors are carried along as the
+reference computes: err(x y) = err(x) |y| + |x| err(y) + u |x y|.  Sums over the tokens are at most 96 rows deep in a block and 96 over the blocks (T <= 16384 here).
+"""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_26881_b200 import binding as B
+
+gpu = pytest.mark.gpu
+U = 2.0 ** -24
+A_REL, Y_REL, BF16_HALF = 60 * U, 40 * U, 2.0 ** -8
+BF = torch.bfloat16
+
+
+def strided(t, pad, dtype, fill=7.0, shift=0):
+    """A [T, H] view on the device with rows H + pad apart, `shift` elements into its storage (filled); holds t if it is a tensor."""
+    T, H = t.shape if isinstance(t, torch.Tensor) else t
+    store = torch.full((T * (H + pad) + shift + 16,), fill, device="cuda:0").to(dtype)
+    view = store[shift:shift + T * (H + pad)].view(T, H + pad)[:, :H]
+    if isinstance(t, torch.Tensor):
+        view.copy_(t)
+    return view, store
+
+
+def untouched(view, store, shift=0, fill=7.0):
+    T, H = view.shape
+    keep = torch.ones(store.numel(), dtype=torch.bool)
+    keep[(torch.arange(T)[:, None] * view.stride(0) + torch.arange(H) + shift).flatten()] = False
+    assert (store.cpu().float()[keep] == fill).all(), "written outside the rows"
+
+
+def gate_tensor(form, T, H, g):
+    return {"none": lambda: None, "channel": lambda: torch.randn(H, generator=g).to(BF), "token": lambda: torch.randn(T, generator=g),
+            "element": lambda: (2 * torch.randn(T, H, generator=g)).to(BF)}[form]()
+
+
+def gate_value(gate, form, act):
+    if gate is None:
+        return torch.ones(1, dtype=torch.float64)
+    v = gate.double()
+    if form == "token":
+        v = v[:, None]
+    return torch.sigmoid(v) if act == "sigmoid" else v
+
+
+def norm(x, eps):
+    return x / torch.sqrt((x * x).mean(1, keepdim=True) + eps)
+
+
+def inputs(T, H, form, seed=0, post=True, pre=True):
+    g = torch.Generator().manual_seed(seed + 7 * T + H)
+    rnd = lambda std: (torch.randn(T, H, generator=g) * std).to(BF)
+    w = lambda: (1 + 0.2 * torch.randn(H, generator=g)).to(BF)
+    return dict(y=rnd(0.5), r=rnd(2.0), post=w() if post else None, pre=w() if pre else None, gate=gate_tensor(form, T, H, g))
+
+
+def cuda(t):
+    return None if t is None else t.cuda()
+
+
+def check_forward(T, H, form="none", act="none", post=True, pre=True, out=True, q=False, rs=1.0, bs=1.0, eps=1e-6, pads=(0,) * 6, shift=0, seed=0, i=None):
+    i = inputs(T, H, form, seed, post, pre) if i is None else i
+    y, _ = strided(i["y"], pads[0], BF, shift=shift)
+    r, _ = strided(i["r"], pads[1], BF, shift=shift)
+    h, h_s = strided((T, H), pads[2], BF, shift=shift)
+    o, o_s = strided((T, H), pads[3], BF, shift=shift) if out and pre else (None, None)
+    qt, q_s = strided((T, H), pads[4], torch.int8, shift=shift) if q else (None, None)
+    qs = torch.full((T,), -5.0, device="cuda:0") if q else None
+    gate = strided(i["gate"], pads[5], BF, shift=shift)[0] if form == "element" else cuda(i["gate"])
+    B.moe_block_norm(y, r, h, eps, post_weight=cuda(i["post"]), pre_weight=cuda(i["pre"]), gate=gate, gate_act=act, residual_scale=rs,
+                     block_scale=bs, out=o, out_q=qt, q_scale=qs)
+    torch.cuda.synchronize()
+    for v, s in ((h, h_s), (o, o_s), (qt, q_s)):
+        if v is not None:
+            untouched(v, s, shift)
+    a = i["y"].double()
+    if post:
+        a = norm(a, eps) * i["post"].double()
+    a = a * gate_value(i["gate"], form, act) * np.float32(bs)
+    s = i["r"].double() * np.float32(rs)
+    ref, got = s + a, h.cpu().double()
+    assert torch.equal(got.isnan(), ref.isnan())
+    fine = ref.isfinite()
+    assert ((got - ref).abs() <= BF16_HALF * ref.abs() + (1 + BF16_HALF) * (2 * U * s.abs() + (A_REL + 2 * U) * a.abs()) + 1e-40)[fine].all()
+    if not pre:
+        return h, None, None, None
+    v = norm(got, eps) * i["pre"].double()
+    if out:
+        c = o.cpu().double()
+        assert torch.equal(c.isnan(), v.isnan())
+        ok = ~v.isnan()
+        assert ((c - v).abs()[ok] <= (BF16_HALF + 2 * Y_REL) * v.abs()[ok] + 1e-40).all()
+    if q:
+        scale, top = qs.cpu().double(), v.abs().amax(1) / 127
+        assert torch.equal(scale.isfinite(), top.isfinite())
+        ok = top.isfinite()
+        assert ((scale - top).abs()[ok] <= (Y_REL + 2 * U) * top[ok] + 1e-45).all()
+        qq = qt.cpu().double()
+        assert (qq.abs() <= 127).all() and (qq[~ok] == 0).all() and (qq[ok & (scale == 0)] == 0).all()
+        live = ok & (scale > 1e-30)
+        assert ((qq - v / scale[:, None]).abs()[live] <= 0.5 + 127 * 2 * Y_REL).all()
+    return h, o, qt, qs
+
+
+@gpu
+@pytest.mark.parametrize("H", [1, 2, 7, 8, 9, 127, 128, 255, 256, 257, 511, 512, 513, 1411, 2048, 4096, 4104, 8192, 8200, 16384])
+@pytest.mark.parametrize("form", ["none", "channel", "token", "element"])
+def test_every_width(H, form):
+    check_forward(5, H, form, "sigmoid" if H % 2 else "none", q=True, rs=0.5, bs=0.7)
+
+
+@gpu
+@pytest.mark.parametrize("T", [1, 2, 3, 4, 5, 33, 1126])
+def test_numbers_of_tokens(T):
+    for H in (64, 512, 768, 2048):
+        check_forward(T, H, "token", "sigmoid", q=True, seed=1)
+        check_forward(T, H, "element", post=False, seed=2)
+        check_forward(T, H, "channel", pre=False, seed=3)
+        check_forward(T, H, out=False, q=True, seed=4)
+
+
+@gpu
+@pytest.mark.parametrize("pads,shift", [((8, 0, 16, 8, 8, 0), 0), ((1, 2, 3, 4, 5, 6), 0), ((0,) * 6, 1), ((0, 0, 0, 0, 3, 0), 0), ((0, 0, 0, 0, 0, 4), 0), ((7,) * 6, 3)])
+def test_strides_and_alignment(pads, shift):
+    for H in (200, 1411, 2048):
+        check_forward(6, H, "element", "sigmoid", q=True, pads=pads, shift=shift)
+
+
+@gpu
+def test_outputs_in_the_place_of_inputs():
+    T, H = 33, 1032
+    i = inputs(T, H, "element")
+    args = dict(post_weight=cuda(i["post"]), pre_weight=cuda(i["pre"]), gate_act="sigmoid")
+    y, r, g = cuda(i["y"]), cuda(i["r"]), cuda(i["gate"])
+    h, o = torch.empty_like(y), torch.empty_like(y)
+    B.moe_block_norm(y, r, h, 1e-6, gate=g, out=o, **args)
+    for hi, oi in ((1, 0), (0, 1), (2, 1), (0, 2)):                    # of (y, r, gate)
+        t = [y.clone(), r.clone(), g.clone()]
+        B.moe_block_norm(t[0], t[1], t[hi], 1e-6, gate=t[2], out=t[oi], **args)
+        assert torch.equal(t[hi], h) and torch.equal(t[oi], o)
+
+
+@gpu
+def test_rows_with_infinities_nan_zeros_and_the_ends_of_the_range():
+    T, H = 12, 520
+    i = inputs(T, H, "none")
+    inf, nan = float("inf"), float("nan")
+    y = i["y"].float()
+    y[0, 3], y[1, 5], y[2, :] = inf, nan, 0
+    y[3] *= 2.0 ** 100
+    y[4] *= 2.0 ** -110
+    r = i["r"].float()
+    r[5, 7], r[6, 9] = -inf, nan
+    r[7], y[7] = 0, 0
+    r[8] *= 2.0 ** 90
+    i["y"], i["r"] = y.to(BF), r.to(BF)
+    for eps in (1e-6, 0.0):
+        j = dict(i)
+        if eps == 0:                                                   # (zeros over their root: NaN, as the formula)
+            j["y"] = torch.cat([i["y"][:2], i["y"][3:7], i["y"][8:]])
+            j["r"] = torch.cat([i["r"][:2], i["r"][3:7], i["r"][8:]])
+        n = j["y"].shape[0]
+        h, o, q, s = check_rows(n, H, j, eps)
+        clean = check_rows(n, H, dict(j, y=torch.nan_to_num(j["y"].float(), 1, 1, 1).to(BF), r=torch.nan_to_num(j["r"].float(), 1, 1, 1).to(BF)), eps)
+        bad = (~(j["y"].float().isfinite() & j["r"].float().isfinite())).any(1)
+        assert torch.equal(h.cpu()[~bad], clean[0].cpu()[~bad]) and torch.equal(q.cpu()[~bad], clean[2].cpu()[~bad])      # no other row's
+        assert (q.cpu()[bad] == 0).all() and not s.cpu()[bad].isfinite().any()
+
+
+def check_rows(n, H, i, eps):
+    """check_forward where rows may hold infinities: such a row's outputs are NaN or 0, so only the others are compared."""
+    y, r = cuda(i["y"]), cuda(i["r"])
+    h, o, q, s = torch.empty_like(y), torch.empty_like(y), torch.empty(n, H, dtype=torch.int8, device="cuda:0"), torch.empty(n, device="cuda:0")
+    B.moe_block_norm(y, r, h, eps, post_weight=cuda(i["post"]), pre_weight=cuda(i["pre"]), out=o, out_q=q, q_scale=s)
+    fine = (i["y"].float().isfinite() & i["r"].float().isfinite()).all(1)
+    check_forward(int(fine.sum()), H, q=True, eps=eps, i=dict(i, y=i["y"][fine], r=i["r"][fine]))
+    assert h.cpu()[fine].isfinite().all() and o.cpu()[fine].isfinite().all()
+    return h, o, q, s
+
+
+@gpu
+def test_no_tokens():
+    e = torch.empty(0, 256, dtype=BF, device="cuda:0")
+    w = torch.ones(256, dtype=BF, device="cuda:0")
+    B.moe_block_norm(e, e, e, 1e-6, post_weight=w, pre_weight=w, out=torch.empty_like(e))
+    d = [torch.full((256,), 3.0, device="cuda:0") for _ in range(3)]
+    B.moe_block_norm_backward(e, e, 1e-6, post_weight=w, pre_weight=w, gate=w, d_out=e, d_h=e, d_block=torch.empty_like(e), d_gate=d[0],
+                              d_post_weight=d[1], d_pre_weight=d[2])
+    assert all((t == 0).all() for t in d)                              # sums over no tokens
+
+
+@gpu
+def test_rows_beyond_32_bit_offsets():
+    T, H, ld = 3, 256, 1 << 30
+    i = inputs(T, H, "none")
+    big = torch.zeros(2 * ld + 4096, dtype=BF, device="cuda:0")
+    y = big.as_strided((T, H), (ld, 1))
+    y.copy_(i["y"])
+    h = big.as_strided((T, H), (ld, 1), 1024)
+    o = big.as_strided((T, H), (ld, 1), 2048)
+    B.moe_block_norm(y, cuda(i["r"]), h, 1e-6, post_weight=cuda(i["post"]), pre_weight=cuda(i["pre"]), out=o)
+    h0, o0 = torch.empty(T, H, dtype=BF, device="cuda:0"), torch.empty(T, H, dtype=BF, device="cuda:0")
+    B.moe_block_norm(cuda(i["y"]), cuda(i["r"]), h0, 1e-6, post_weight=cuda(i["post"]), pre_weight=cuda(i["pre"]), out=o0)
+    assert torch.equal(h, h0) and torch.equal(o, o0)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# gradients
+
+def gradients(i, h, form, act, rs, bs, eps, d_out, d_h):
+    """The formula's gradients in 64 bits (by way of differentiation of the forward formula), and bounds of the kernel's errors."""
+    y, gate = i["y"].double().requires_grad_(), None if i["gate"] is None else i["gate"].double().requires_grad_()
+    post = None if i["post"] is None else i["post"].double().requires_grad_()
+    pre = None if i["pre"] is None else i["pre"].double().requires_grad_()
+    H = y.shape[1]
+    total = torch.zeros_like(y) if d_h is None else d_h.double()
+    size = total.abs()                                                 # sums of magnitudes of what the kernel adds up
+    g = {}
+    sum_pre = None
+    if d_out is not None:
+        hh = h.double().requires_grad_()
+        out = norm(hh, eps) * pre
+        dh, g["pre"] = torch.autograd.grad(out, (hh, pre), d_out.double())
+        total = total + dh
+        with torch.no_grad():
+            inv = 1 / torch.sqrt((hh * hh).mean(1, keepdim=True) + eps)
+            n, d = hh * inv, d_out.double() * pre
+            size = size + inv * (d.abs() + n.abs() * (d * n).abs().mean(1, keepdim=True))
+            sum_pre = (d_out.double() * n).abs().sum(0)
+    g["residual"] = total * np.float32(rs)
+    a = y if post is None else norm(y, eps) * post
+    v = gate_value(gate, form, act)
+    stream = np.float32(bs) * v * a
+    want = [t for t in (y, post, gate) if t is not None]
+    got = dict(zip([n for n, t in (("y", y), ("post", post), ("gate", gate)) if t is not None], torch.autograd.grad(stream, want, total)))
+    g.update(got)
+    with torch.no_grad():
+        err = 160 * U * size
+        slope = v * (1 - v) if act == "sigmoid" else torch.ones(1, dtype=torch.float64)
+        inv = 1 / torch.sqrt((y * y).mean(1, keepdim=True) + eps) if post is not None else torch.ones(1, dtype=torch.float64)
+        m, w = y * inv, post if post is not None else torch.ones(1, dtype=torch.float64)
+        b = abs(bs)
+        e = b * (v * w).abs() * (err + 160 * U * size)
+        bound = {"residual": abs(rs) * err, "pre": None if sum_pre is None else 250 * U * sum_pre}
+        bound["y"] = inv * (e + m.abs() * (e * m.abs()).mean(1, keepdim=True)) if post is not None else e
+        if post is not None:
+            bound["post"] = (b * (err + 250 * U * size) * (v * m).abs()).sum(0)
+        if gate is not None:
+            dg = b * (err + 250 * U * size) * (m * w * slope).abs()
+            bound["gate"] = {"channel": lambda: dg.sum(0), "token": lambda: dg.sum(1), "element": lambda: dg}[form]()
+    return g, bound
+
+
+def run_backward(i, h, form, act, rs, bs, eps, d_out, d_h, pads=(0,) * 9, shift=0, weights=True):
+    T, H = i["y"].shape
+    put = lambda t, n: None if t is None else strided(t, pads[n], BF, shift=shift)[0]
+    d_block, d_block_s = strided((T, H), pads[5], BF, shift=shift)
+    d_res, d_res_s = strided((T, H), pads[6], BF, shift=shift)
+    d_gate = dg_s = None
+    if form == "element":
+        d_gate, dg_s = strided((T, H), pads[7], BF, shift=shift)
+    elif form != "none":
+        d_gate = torch.full((H if form == "channel" else T,), 7.0, device="cuda:0")
+    d_post = torch.full((H,), 7.0, device="cuda:0") if i["post"] is not None and weights else None
+    d_pre = torch.full((H,), 7.0, device="cuda:0") if d_out is not None and weights else None
+    gate = strided(i["gate"], pads[8], BF, shift=shift)[0] if form == "element" else cuda(i["gate"])
+    B.moe_block_norm_backward(put(i["y"], 0), put(h, 1), eps, post_weight=cuda(i["post"]), pre_weight=cuda(i["pre"]), gate=gate, gate_act=act,
+                              residual_scale=rs, block_scale=bs, d_out=put(d_out, 2), d_h=put(d_h, 3), d_block=d_block, d_residual=d_res,
+                              d_gate=d_gate, d_post_weight=d_post, d_pre_weight=d_pre)
+    torch.cuda.synchronize()
+    for v, s in ((d_block, d_block_s), (d_res, d_res_s)) + (((d_gate, dg_s),) if form == "element" else ()):
+        untouched(v, s, shift)
+    return dict(y=d_block, residual=d_res, gate=d_gate, post=d_post, pre=d_pre)
+
+
+def check_backward(T, H, form="none", act="none", post=True, pre=True, d_h=True, rs=1.0, bs=1.0, eps=1e-6, seed=0, **kw):
+    i = inputs(T, H, form, seed, post, pre)
+    g = torch.Generator().manual_seed(seed + 13 * T + H)
+    rnd = lambda std: (torch.randn(T, H, generator=g) * std).to(BF)
+    h = rnd(2.0)
+    d_out = rnd(0.1) if pre else None
+    d_hh = rnd(0.1) if d_h or not pre else None
+    got = run_backward(i, h, form, act, rs, bs, eps, d_out, d_hh, **kw)
+    ref, bound = gradients(i, h, form, act, rs, bs, eps, d_out, d_hh)
+    for name, t in got.items():
+        if t is None:
+            continue
+        c, want = t.cpu().double(), ref[name].reshape(t.shape)
+        half = BF16_HALF if t.dtype == BF else U
+        tol = (half + 4 * U) * want.abs() + (1 + half) * bound[name].reshape(t.shape) + 1e-38
+        assert ((c - want).abs() <= tol).all(), (name, ((c - want).abs() / tol).max())
+    return got
+
+
+@gpu
+@pytest.mark.parametrize("H", [1, 2, 7, 8, 9, 127, 128, 255, 256, 257, 511, 513, 1411, 2048, 4096, 4104, 8192, 8200, 16384])
+@pytest.mark.parametrize("form", ["none", "channel", "token", "element"])
+def test_gradients_of_every_width(H, form):
+    check_backward(5, H, form, "sigmoid" if H % 2 == 0 else "none", rs=0.5, bs=0.7)
+
+
+@gpu
+@pytest.mark.parametrize("T", [1, 2, 3, 4, 5, 33, 1126, 5000])
+def test_gradients_of_numbers_of_tokens(T):
+    for H in (64, 300, 512, 2048):
+        check_backward(T, H, "channel", "sigmoid", seed=1)
+        check_backward(T, H, "element", post=False, seed=2)
+        check_backward(T, H, "token", pre=False, seed=3)
+        check_backward(T, H, "none", d_h=False, seed=4)
+
+
+@gpu
+@pytest.mark.parametrize("pads,shift", [((8, 0, 16, 8, 8, 0, 8, 16, 0), 0), ((1, 2, 3, 4, 5, 6, 7, 8, 9), 0), ((0,) * 9, 1), ((0, 0, 0, 0, 0, 3, 0, 0, 0), 0), ((7,) * 9, 3)])
+def test_gradients_with_strides_and_alignment(pads, shift):
+    for H in (200, 1411, 2048):
+        check_backward(6, H, "element", "sigmoid", pads=pads, shift=shift)
+
+
+@gpu
+def test_gradients_against_differences():
+    """Of the scalar sum(d_out out) + sum(d_h h) in 64 bits, by central differences with steps of 2^-12 of order-one values."""
+    T, H, eps, rs, bs = 3, 40, 1e-3, 0.5, 0.7
+    for form in ("channel", "token", "element"):
+        i = inputs(T, H, form)
+        g = torch.Generator().manual_seed(5)
+        d_out, d_h = torch.randn(T, H, generator=g).to(BF), torch.randn(T, H, generator=g).to(BF)
+        v = {n: t.double().clone() for n, t in i.items()}
+
+        def f(v):
+            h = rs * v["r"] + bs * gate_value(v["gate"], form, "sigmoid") * norm(v["y"], eps) * v["post"]
+            return h, (d_out.double() * norm(h, eps) * v["pre"]).sum() + (d_h.double() * h).sum()
+        h = f(v)[0]
+        # the kernel takes the stream as bf16: a residual that makes it one
+        hb = h.to(BF)
+        v["r"] = v["r"] + (hb.double() - h) / rs
+        got = run_backward(i, hb, form, "sigmoid", rs, bs, eps, d_out, d_h)
+        step = 2.0 ** -12
+        for name, key in (("y", "y"), ("residual", "r"), ("gate", "gate"), ("post", "post"), ("pre", "pre")):
+            flat, grad = v[key].view(-1), got[name].cpu().double().view(-1)
+            for at in (0, flat.numel() // 2, flat.numel() - 1):
+                keep = float(flat[at])
+                flat[at] = keep + step
+                up = f(v)[1]
+                flat[at] = keep - step
+                down = f(v)[1]
+                flat[at] = keep
+                want = float((up - down) / (2 * step))
+                # third derivatives of order one times step^2 / 6, and the gradient's own rounding
+                assert abs(float(grad[at]) - want) <= 2e-6 * 10 + 2 * BF16_HALF * abs(want) + 1e-5, (form, name, at)
+
+
+@gpu
+def test_gradients_in_the_place_of_inputs_are_the_same():
+    T, H = 37, 1032
+    i = inputs(T, H, "element")
+    h, d_out, d_h = ((torch.randn(T, H, generator=torch.Generator().manual_seed(s))).to(BF) for s in (1, 2, 3))
+    want = run_backward(i, h, "element", "sigmoid", 0.5, 0.7, 1e-6, d_out, d_h)
+    y, gate, hc, do, dh = (cuda(t) for t in (i["y"], i["gate"], h, d_out, d_h))
+    d_post, d_pre = torch.empty(H, device="cuda:0"), torch.empty(H, device="cuda:0")
+    B.moe_block_norm_backward(y, hc, 1e-6, post_weight=cuda(i["post"]), pre_weight=cuda(i["pre"]), gate=gate, gate_act="sigmoid", residual_scale=0.5,
+                              block_scale=0.7, d_out=do, d_h=dh, d_block=y, d_residual=dh, d_gate=gate, d_post_weight=d_post, d_pre_weight=d_pre)
+    for name, t in (("y", y), ("residual", dh), ("gate", gate), ("post", d_post), ("pre", d_pre)):
+        assert torch.equal(t, want[name]), name
+
+
+@gpu
+def test_gradients_each_alone_are_those_of_all():
+    T, H = 20, 768
+    for form in ("channel", "token", "element"):
+        i = inputs(T, H, form)
+        h, d_out, d_h = ((torch.randn(T, H, generator=torch.Generator().manual_seed(s))).to(BF) for s in (1, 2, 3))
+        want = run_backward(i, h, form, "none", 1.0, 1.0, 1e-6, d_out, d_h)
+        for name, key in (("y", "d_block"), ("residual", "d_residual"), ("gate", "d_gate"), ("post", "d_post_weight"), ("pre", "d_pre_weight")):
+            t = torch.empty_like(want[name])
+            B.moe_block_norm_backward(cuda(i["y"]), cuda(h), 1e-6, post_weight=cuda(i["post"]), pre_weight=cuda(i["pre"]), gate=cuda(i["gate"]),
+                                      d_out=cuda(d_out), d_h=cuda(d_h), **{key: t})
+            assert torch.equal(t, want[name]), (form, name)
+
+
+@gpu
+def test_gradients_of_rows_at_the_ends_of_the_range():
+    T, H = 6, 264
+    i = inputs(T, H, "none")
+    scale = torch.tensor([1.0, 2.0 ** 90, 2.0 ** -90, 2.0 ** 70, 2.0 ** -70, 1.0])[:, None]
+    i["y"] = (i["y"].float() * scale).to(BF)
+    h = (torch.randn(T, H, generator=torch.Generator().manual_seed(1)) * scale.flip(0)).to(BF)
+    d_out = torch.randn(T, H, generator=torch.Generator().manual_seed(2)).to(BF)
+    got = run_backward(i, h, "none", "none", 1.0, 1.0, 0.0, d_out, None)
+    ref, bound = gradients(i, h, "none", "none", 1.0, 1.0, 0.0, d_out, None)
+    for name in ("residual", "pre", "post"):                            # (d_y of the smallest rows leaves the range of bf16)
+        c, want = got[name].cpu().double(), ref[name]
+        half = BF16_HALF if got[name].dtype == BF else U
+        ok = want.abs() < 1e37
+        assert ((c - want).abs() <= (half + 4 * U) * want.abs() + (1 + half) * bound[name] + 1e-38)[ok].all(), name
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# streams, graphs, refusals
+
+@gpu
+def test_streams_graphs_and_workspaces():
+    T, H = 700, 520
+    i = inputs(T, H, "channel")
+    h, d_out, d_h = ((torch.randn(T, H, generator=torch.Generator().manual_seed(s))).to(BF).cuda() for s in (1, 2, 3))
+    want = run_backward(i, h.cpu(), "channel", "sigmoid", 1.0, 1.0, 1e-6, d_out.cpu(), d_h.cpu())
+    dev = {n: cuda(t) for n, t in i.items()}
+
+    def call(d, ws, stream=None):
+        B.moe_block_norm_backward(dev["y"], h, 1e-6, post_weight=dev["post"], pre_weight=dev["pre"], gate=dev["gate"], gate_act="sigmoid", d_out=d_out,
+                                  d_h=d_h, d_block=d["y"], d_residual=d["residual"], d_gate=d["gate"], d_post_weight=d["post"], d_pre_weight=d["pre"],
+                                  workspace=ws, stream=stream)
+    new = lambda: {n: torch.full_like(t, 3.0) for n, t in want.items()}
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs = [new() for _ in streams]
+    spaces = [torch.full((B.moe_block_norm_workspace(T, H),), 255, dtype=torch.uint8, device="cuda:0") for _ in streams]   # (NaN: not read before written)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, o, w in zip(streams, outs, spaces):
+            call(o, w, s)
+    call(outs[0], None, streams[0])                                    # its own workspace, on that stream
+    torch.cuda.synchronize()
+    for o in outs:
+        assert all(torch.equal(o[n], want[n]) for n in want)
+    # two graphs with workspaces of their own, replayed at once
+    graphs, outs = [], [new(), new()]
+    for o, w in zip(outs, spaces):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            call(o, w)
+        graphs.append(gr)
+    for _ in range(3):
+        for gr, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                gr.replay()
+    torch.cuda.synchronize()
+    for o in outs:
+        assert all(torch.equal(o[n], want[n]) for n in want)
+
+
+def rule(**kw):
+    v = dict(gate=0, gate_act=0, residual_scale=1.0, block_scale=1.0, eps=1e-6)
+    v.update(kw)
+    return B.MoeBlockRule(*[v[n] for n, _ in B.MoeBlockRule._fields_])
+
+
+def test_refusals_of_the_c_entry_points():
+    lib, p = B.load_library(), ctypes.c_void_p
+    a = [p(4096 * (i + 1)) for i in range(20)]                          # (never dereferenced: every call here is refused, or has no tokens)
+
+    def fwd(T=2, H=64, ld=64, r=None, y=a[0], res=a[1], post=a[2], pre=a[3], gate=None, ldg=64, h=a[4], ldh=64, out=a[5], q=None, qs=None):
+        return lib.moe_block_norm(y, ld, res, ld, post, pre, gate, ldg, ctypes.byref(r or rule()), T, H, h, ldh, out, ld, q, ld, qs, None)
+    assert fwd(T=0, y=None, res=None, h=None, out=None) == B.MOE_OK
+    for kw in (dict(T=-1), dict(H=0), dict(ld=63), dict(ldh=63), dict(r=rule(gate=4), gate=a[6]), dict(r=rule(gate_act=2)), dict(r=rule(eps=-1.0)),
+               dict(r=rule(eps=float("nan"))), dict(r=rule(residual_scale=float("inf"))), dict(r=rule(block_scale=float("nan"))), dict(gate=a[6]),
+               dict(pre=None), dict(y=p(4097)), dict(h=a[5]), dict(h=a[0], ldh=72), dict(q=a[0], qs=a[8]), dict(r=rule(gate=3), gate=a[6], ldg=63),
+               dict(r=rule(gate=2), gate=p(4098)), dict(r=rule(gate=1), gate=a[4]), dict(h=a[2])):
+        assert fwd(**kw) == B.MOE_ERR_SHAPE, kw
+    for kw in (dict(y=None), dict(res=None), dict(h=None), dict(out=None), dict(q=a[7]), dict(r=rule(gate=1))):
+        assert fwd(**kw) == B.MOE_ERR_NULL, kw
+    assert fwd(H=16385, ld=16385, ldh=16385) == B.MOE_ERR_UNSUPPORTED
+    assert lib.moe_block_norm(a[0], 64, a[1], 64, None, None, None, 0, None, 2, 64, a[4], 64, None, 0, None, 0, None, None) == B.MOE_ERR_NULL
+
+    def bwd(T=2, H=64, ld=64, r=None, y=a[0], h=a[1], post=a[2], pre=a[3], gate=None, d_out=a[4], d_h=a[5], d_block=a[6], ldb=64, d_res=a[7], d_gate=None,
+            d_post=a[8], d_pre=a[9], ws=a[10], n=1 << 30):
+        return lib.moe_block_norm_backward(y, ld, h, ld, post, pre, gate, ld, ctypes.byref(r or rule()), T, H, d_out, ld, d_h, ld, d_block, ldb, d_res, ld,
+                                           d_gate, ld, d_post, d_pre, ws, n, None)
+    for kw in (dict(T=-1), dict(ld=63), dict(ldb=63), dict(post=None), dict(pre=None), dict(d_gate=a[11]), dict(ws=p(4104)), dict(d_block=a[7]),
+               dict(d_block=a[0], ldb=72), dict(d_post=p(4098))):
+        assert bwd(**kw) == B.MOE_ERR_SHAPE, kw
+    for kw in (dict(y=None), dict(h=None), dict(d_out=None, d_h=None, d_pre=None), dict(ws=None), dict(d_block=None, d_res=None, d_post=None, d_pre=None)):
+        assert bwd(**kw) == B.MOE_ERR_NULL, kw
+    assert bwd(n=16) == B.MOE_ERR_ALLOC
+    assert lib.moe_block_norm_workspace(-1, 64) == B.MOE_ERR_SHAPE and lib.moe_block_norm_workspace(4, 16385) == B.MOE_ERR_UNSUPPORTED
+
+
+def test_refusals_of_the_binding():
+    y = torch.zeros(4, 64, dtype=BF)
+    w = torch.ones(64, dtype=BF)
+    bad = [dict(block_out=y[0]), dict(residual=None), dict(residual=y.float()), dict(residual=y[:3]), dict(h=torch.zeros(4, 128, dtype=BF)[:, ::2]),
+           dict(post_weight=w[:63]), dict(post_weight=w.float()), dict(gate=torch.zeros(3)), dict(gate=torch.zeros(63, dtype=BF)),
+           dict(gate=torch.zeros(3, 64, dtype=BF)), dict(out_q=torch.zeros(4, 64, dtype=torch.int8)), dict(out=y.half()), {}]
+    for kw in bad:                                                      # ({}: tensors of the host)
+        args = dict(block_out=y, residual=y, h=y.clone(), eps=1e-6, post_weight=w, pre_weight=w, out=y.clone())
+        args.update(kw)
+        with pytest.raises(ValueError):
+            B.moe_block_norm(args.pop("block_out"), args.pop("residual"), args.pop("h"), args.pop("eps"), **args)
+    with pytest.raises(KeyError):
+        B.moe_block_norm(y, y, y, 1e-6, gate_act="tanh")
+    for kw in (dict(d_gate=torch.zeros(64)), dict(d_block=y[:2]), dict(d_post_weight=w), dict(workspace=y), {}):
+        with pytest.raises(ValueError):
+            B.moe_block_norm_backward(y, y, 1e-6, **{**dict(post_weight=w, pre_weight=w, d_out=y, d_block=y.clone()), **kw})

@@ -1,0 +1,315 @@
+"""moe_quantize_i8 and moe_project_i8.
+
+Quantising is exact: scale is one fp32 quotient, q the rounding of another, and numpy's are the same.  The product's integers
+are exact; what follows are roundings in fp32 (u = 2^-24): the sum to fp32, two scales, bias, base -- 4 u of the scaled sum and 2 u of
+the running total -- and one to the output's type (half a step: 2^-8 of bf16).
+"""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_26881_b200 import binding as B
+
+gpu = pytest.mark.gpu
+U, BF16_HALF = 2.0 ** -24, 2.0 ** -8
+BF = torch.bfloat16
+
+
+def rows(t, dtype, pad=0, fill=7, shift=0):
+    T, K = t.shape if isinstance(t, torch.Tensor) else t
+    store = torch.full((T * (K + pad) + shift + 16,), fill, device="cuda:0", dtype=dtype)
+    view = store[shift:shift + T * (K + pad)].view(T, K + pad)[:, :K]
+    if isinstance(t, torch.Tensor):
+        view.copy_(t)
+    return view, store
+
+
+def check_quantize(x, pad=0, qpad=0, shift=0, qshift=0):
+    T, K = x.shape
+    xd, _ = rows(x, BF, pad, shift=shift)
+    q, store = rows((T, K), torch.int8, qpad, shift=qshift)
+    s = torch.full((T + 4,), -5.0, device="cuda:0")
+    B.moe_quantize_i8(xd, q, s[:T])
+    torch.cuda.synchronize()
+    keep = torch.ones(store.numel(), dtype=torch.bool)
+    keep[(torch.arange(T)[:, None] * (K + qpad) + torch.arange(K) + qshift).flatten()] = False
+    assert (store.cpu()[keep] == 7).all() and (s[T:] == -5).all()
+    xf = x.float().numpy()
+    with np.errstate(all="ignore"):
+        scale = (np.abs(xf).max(1) / np.float32(127)).astype(np.float32)
+        scale[np.isnan(xf).any(1)] = np.nan
+        fine = np.isfinite(scale) & (scale > 0)
+        want = np.where(fine[:, None], np.clip(np.rint((xf / scale[:, None]).astype(np.float32)), -127, 127), 0).astype(np.int8)
+    got = s[:T].cpu().numpy()
+    np.testing.assert_array_equal(got[~np.isnan(scale)], scale[~np.isnan(scale)])
+    assert np.isnan(got[np.isnan(scale)]).all()
+    np.testing.assert_array_equal(q.cpu().numpy(), want)
+
+
+def normal(T, K, seed=0, std=1.0):
+    return (torch.randn(T, K, generator=torch.Generator().manual_seed(seed + 7 * T + K)) * std).to(BF)
+
+
+@gpu
+@pytest.mark.parametrize("K", [1, 2, 7, 8, 15, 16, 127, 255, 256, 257, 511, 1000, 2048, 4096, 4100, 5632, 8192, 16384, 16385, 16392, 40000])
+def test_quantize_every_width(K):
+    check_quantize(normal(5, K))
+    check_quantize(normal(3, K, 1), pad=5, qpad=3, shift=1, qshift=1)
+
+
+@gpu
+@pytest.mark.parametrize("T", [1, 2, 3, 4, 33, 1126, 9000])
+def test_quantize_numbers_of_rows(T):
+    for K in (64, 300, 768, 2048):
+        check_quantize(normal(T, K, 2), pad=8, qpad=8)
+
+
+@gpu
+def test_quantize_ties_and_the_ends_of_the_range():
+    # a largest value of 254 steps makes the scale a power of two and every odd multiple of it a tie
+    x = torch.randint(-254, 255, (64, 512), generator=torch.Generator().manual_seed(1)).float()
+    x[:, 0] = 254
+    e = torch.arange(64)[:, None].float() - 32
+    check_quantize((x * 2.0 ** e).to(BF))
+    y = normal(12, 300).float()
+    y[0, 3], y[1, 5], y[2], y[3, 0] = float("inf"), float("nan"), 0, -float("inf")
+    y[4] *= 2.0 ** -120
+    y[5] *= 2.0 ** -130                                                # (scales that are not normal numbers)
+    y[6] *= 2.0 ** 125
+    y[7] = 0
+    y[7, 9] = 2.0 ** -133                                              # the smallest bf16: its scale is 0
+    y[8] = 2.0 ** -126
+    check_quantize(y.to(BF))
+
+
+@gpu
+def test_quantize_no_rows():
+    B.moe_quantize_i8(torch.empty(0, 64, dtype=BF, device="cuda:0"), torch.empty(0, 64, dtype=torch.int8, device="cuda:0"), torch.empty(0, device="cuda:0"))
+
+
+def operands(T, K, N, seed=0, extreme=False):
+    g = torch.Generator().manual_seed(seed + T + 3 * K + 5 * N)
+    draw = lambda *s: torch.full(s, -128, dtype=torch.int8) if extreme else torch.randint(-128, 128, s, generator=g, dtype=torch.int8)
+    return draw(T, K), torch.rand(T, generator=g) + 0.5, draw(N, K), (torch.rand(N, generator=g) + 0.5) * 1e-4, g
+
+
+def product(x, w):
+    """Exact: in fp64 on the device, where sums of 131071 products of 128 * 128 are whole numbers below 2^53."""
+    return (x.cuda().double() @ w.cuda().double().t()).cpu()
+
+
+def check(T, K, N, out=BF, bias=False, base=False, xpad=None, wpad=None, opad=0, bpad=0, shift=0, in_place=False, seed=0, extreme=False, data=None):
+    x, xs, w, ws, g = operands(T, K, N, seed, extreme) if data is None else data
+    b = torch.randn(N, generator=g) if bias else None
+    base0 = torch.randn(T, N, generator=g).to(out) if base else None
+    xd, _ = rows(x, torch.int8, -K % 16 if xpad is None else xpad)
+    wd, _ = rows(w, torch.int8, -K % 16 if wpad is None else wpad)
+    o, store = rows((T, N), out, opad, shift=shift)
+    bd = None
+    if base:
+        bd = o if in_place else rows(base0, out, bpad, shift=shift)[0]
+        if in_place:
+            o.copy_(base0)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    B.moe_project_i8(xd, xs.cuda(), wd, ws.cuda(), o, bias=None if b is None else b.cuda(), base=bd, status_out=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    keep = torch.ones(store.numel(), dtype=torch.bool)
+    keep[(torch.arange(T)[:, None] * (N + opad) + torch.arange(N) + shift).flatten()] = False
+    assert (store.cpu().float()[keep] == 7).all(), "written outside the rows"
+    y = product(x, w) * xs.double()[:, None] * ws.double()
+    total = y.abs()
+    if bias:
+        y, total = y + b.double(), total + b.double().abs()
+    if base:
+        y, total = y + base0.double(), total + base0.double().abs()
+    half = BF16_HALF if out == BF else 0
+    got = o.cpu().double()
+    assert torch.equal(got.isnan(), y.isnan())
+    ok = y.isfinite()
+    assert ((got - y).abs() <= half * y.abs() + (1 + half) * 7 * U * total)[ok].all()
+    return o
+
+
+@gpu
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 31, 33, 64, 65, 100, 127, 128, 129, 200, 256, 257, 300, 513, 1126])
+def test_numbers_of_tokens(T):
+    check(T, 2048, 2048)
+    check(T, 640, 300, out=torch.float32, bias=True, base=True)
+    check(T, 5632, 200, bias=True)
+
+
+@gpu
+@pytest.mark.parametrize("K", [1, 2, 15, 16, 17, 31, 32, 33, 100, 127, 128, 129, 255, 256, 257, 400, 1000, 1024, 1411, 2048, 5632])
+def test_every_depth(K):
+    for T in (1, 40, 300):
+        check(T, K, 260, out=torch.float32)
+        check(T, K, 70, bias=True, base=True)
+
+
+@gpu
+@pytest.mark.parametrize("N", [1, 2, 7, 8, 15, 31, 32, 33, 64, 100, 127, 128, 129, 255, 256, 257, 1000, 5632, 20011])
+def test_every_number_of_channels(N):
+    for T in (1, 33, 260):
+        check(T, 512, N)
+        check(T, 2048, N, out=torch.float32, base=True, in_place=True)
+
+
+@gpu
+@pytest.mark.parametrize("opad,bpad,shift,xpad,wpad", [(8, 16, 0, 16, 32), (3, 5, 0, None, None), (0, 0, 1, None, None), (1, 0, 3, 48, 16), (0, 7, 0, None, None)])
+def test_strides_and_alignment(opad, bpad, shift, xpad, wpad):
+    for T in (5, 100, 270):
+        for out in (BF, torch.float32):
+            check(T, 320, 296, out=out, bias=True, base=True, opad=opad, bpad=bpad, shift=shift, xpad=xpad, wpad=wpad)
+
+
+@gpu
+@pytest.mark.parametrize("T", [3, 300])
+def test_largest_sums_do_not_wrap(T):
+    check(T, 131071, 130, out=torch.float32, extreme=True)              # 131071 * 128 * 128 = 2^31 - 2^14
+    x, xs, w, ws, g = operands(T, 131071, 130, extreme=True)
+    check(T, 131071, 130, out=torch.float32, data=(x, xs, torch.full_like(w, 127), ws, g))
+
+
+@gpu
+@pytest.mark.parametrize("T", [2, 30, 300])
+def test_scales_that_are_not_finite_stay_with_their_rows(T):
+    x, xs, w, ws, g = operands(T, 384, 300)
+    xs[0], xs[T - 1], ws[7], ws[280] = float("inf"), float("nan"), float("nan"), 0
+    got = check(T, 384, 300, out=torch.float32, data=(x, xs, w, ws, g)).cpu()
+    x, xs, w, ws, g = operands(T, 384, 300)
+    ws[280] = 0
+    clean = check(T, 384, 300, out=torch.float32, data=(x, xs, w, ws, g)).cpu()
+    cols = torch.arange(300) != 7
+    assert torch.equal(got[1:T - 1][:, cols], clean[1:T - 1][:, cols])
+
+
+@gpu
+def test_no_tokens():
+    e = lambda *s, dt=torch.int8: torch.empty(*s, dtype=dt, device="cuda:0")
+    B.moe_project_i8(e(0, 64), e(0, dt=torch.float32), e(32, 64), e(32, dt=torch.float32), e(0, 32, dt=BF))
+
+
+@gpu
+def test_outputs_beyond_32_bit_offsets():
+    T, K, N, ld = 3, 64, 40, 1 << 30
+    x, xs, w, ws, _ = operands(T, K, N)
+    big = torch.zeros(2 * ld + 64, dtype=BF, device="cuda:0")
+    out = big.as_strided((T, N), (ld, 1))
+    B.moe_project_i8(x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), out)
+    y = torch.empty(T, N, dtype=BF, device="cuda:0")
+    B.moe_project_i8(x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), y)
+    assert torch.equal(out, y)
+    del big
+    T = 200                                                            # tokens far apart, in the shape of many tokens
+    xw = torch.zeros(T, 1 << 24, dtype=torch.int8, device="cuda:0")
+    x, xs, w, ws, _ = operands(T, K, N)
+    xw[:, :K].copy_(x)
+    y, z = torch.empty(T, N, dtype=BF, device="cuda:0"), torch.empty(T, N, dtype=BF, device="cuda:0")
+    B.moe_project_i8(xw[:, :K], xs.cuda(), w.cuda(), ws.cuda(), y)
+    B.moe_project_i8(x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), z)
+    assert torch.equal(y, z)
+
+
+@gpu
+def test_streams_and_graphs_side_by_side():
+    shapes = [(1, 2048, 2048), (32, 2048, 5632), (128, 640, 300), (300, 1024, 700), (1126, 512, 2048)]
+    calls = []
+    for T, K, N in shapes:
+        x, xs, w, ws, _ = operands(T, K, N)
+        d = [t.cuda() for t in (x, xs, w, ws)]
+        want = torch.empty(T, N, dtype=BF, device="cuda:0")
+        B.moe_project_i8(*d, want)
+        calls.append((d, want))
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs = [[torch.empty_like(w) for _, w in calls] for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for n in range(len(calls)):
+            for j, s in enumerate(streams):
+                at = (n + 2 * j) % len(calls)
+                B.moe_project_i8(*calls[at][0], outs[j][at], stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for out in outs for o, (_, w) in zip(out, calls))
+    graph = torch.cuda.CUDAGraph()
+    for o in outs[0]:
+        o.zero_()
+    with torch.cuda.graph(graph):
+        for (d, _), o in zip(calls, outs[0]):
+            B.moe_project_i8(*d, o)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, (_, w) in zip(outs[0], calls))
+    assert B.moe_project_status() == 0
+
+
+@gpu
+def test_quantize_and_project_with_tenants_adapters_beside():
+    """8-bit shared projection, the adapters of the tenants on top by moe_project without a weight."""
+    T, K, N, n, r = 150, 512, 384, 3, 8
+    x = normal(T, K)
+    g = torch.Generator().manual_seed(3)
+    w = (torch.randn(N, K, generator=g) * 0.05).to(BF)
+    a, b = (torch.randn(n, r, K, generator=g) * 0.05).to(BF), (torch.randn(n, N, r, generator=g) * 0.05).to(BF)
+    tenant = torch.randint(0, n, (T,), generator=g, dtype=torch.int32)
+    i8 = lambda *s: torch.empty(*s, dtype=torch.int8, device="cuda:0")
+    xq, xs, wq, ws = i8(T, K), torch.empty(T, device="cuda:0"), i8(N, K), torch.empty(N, device="cuda:0")
+    B.moe_quantize_i8(w.cuda(), wq, ws)
+    B.moe_quantize_i8(x.cuda(), xq, xs)
+    out = torch.empty(T, N, device="cuda:0")
+    B.moe_project_i8(xq, xs, wq, ws, out)
+    B.moe_project(x.cuda(), None, out, base=out, a=a.cuda(), b=b.cuda(), tenant_id=tenant.cuda())
+    full = (xq.cpu().double() * xs.cpu().double()[:, None]) @ (wq.cpu().double() * ws.cpu().double()[:, None]).t()
+    ad = torch.stack([b[tenant[t]].double() @ (a[tenant[t]].double() @ x[t].double()) for t in range(T)])
+    size = full.abs() + torch.stack([b[tenant[t]].double().abs() @ (a[tenant[t]].double().abs() @ x[t].double().abs()) for t in range(T)])
+    # (the adapters' inner product is an fp32 sum of 512 terms: 520 u of their magnitudes)
+    assert ((out.cpu().double() - full - ad).abs() <= 530 * U * size).all()
+    # what 8 bits cost: half a step of x (scale / 2) against w, and of w against x
+    exact = x.double() @ w.double().t()
+    lim = 0.5001 * (xs.cpu().double()[:, None] * w.double().abs().sum(1) + x.double().abs().sum(1)[:, None] * ws.cpu().double()) + 0.25 * K * xs.cpu().double()[:, None] * ws.cpu().double()
+    assert ((full - exact).abs() <= lim).all()
+
+
+def test_refusals_of_the_c_entry_points():
+    lib, p = B.load_library(), ctypes.c_void_p
+    a = [p(4096 * (i + 1)) for i in range(10)]                          # (never dereferenced)
+
+    def project(T=2, K=64, N=32, ldx=64, ldw=64, x=a[0], xs=a[1], w=a[2], ws=a[3], bias=None, base=None, ldb=32, out=a[4], ldo=32, kind=1, status=None):
+        return lib.moe_project_i8(x, ldx, xs, w, ldw, ws, T, K, N, bias, base, ldb, out, ldo, kind, status, None)
+    assert project(T=0, x=None, xs=None, w=None, ws=None, out=None) == B.MOE_OK
+    for kw in (dict(T=-1), dict(T=(1 << 22) + 1), dict(K=0), dict(K=131072, ldx=131072, ldw=131072), dict(N=0), dict(ldx=48), dict(ldw=48), dict(ldo=31),
+               dict(base=a[5], ldb=31), dict(x=p(4104)), dict(w=p(4104)), dict(xs=p(4098)), dict(ws=p(4098)), dict(bias=p(4098)), dict(out=p(4097)),
+               dict(out=a[0]), dict(out=a[2]), dict(base=a[4], ldb=40), dict(status=p(4098))):
+        assert project(**kw) == B.MOE_ERR_SHAPE, kw
+    for kw in (dict(x=None), dict(w=None), dict(xs=None), dict(ws=None), dict(out=None)):
+        assert project(**kw) == B.MOE_ERR_NULL, kw
+    for kw in (dict(ldx=72), dict(ldw=72), dict(kind=2)):
+        assert project(**kw) == B.MOE_ERR_UNSUPPORTED, kw
+
+    def quantize(T=2, K=64, x=a[0], ldx=64, q=a[1], ldq=64, s=a[2]):
+        return lib.moe_quantize_i8(x, ldx, T, K, q, ldq, s, None)
+    assert quantize(T=0, x=None, q=None, s=None) == B.MOE_OK
+    for kw in (dict(T=-1), dict(K=0), dict(K=1 << 24, ldx=1 << 24, ldq=1 << 24), dict(ldx=63), dict(ldq=63), dict(x=p(4097)), dict(s=p(4098)), dict(q=a[0])):
+        assert quantize(**kw) == B.MOE_ERR_SHAPE, kw
+    for kw in (dict(x=None), dict(q=None), dict(s=None)):
+        assert quantize(**kw) == B.MOE_ERR_NULL, kw
+
+
+def test_refusals_of_the_binding():
+    x, w = torch.zeros(4, 64, dtype=torch.int8), torch.zeros(32, 64, dtype=torch.int8)
+    xs, ws, out = torch.zeros(4), torch.zeros(32), torch.zeros(4, 32)
+    for args in ((x.float(), xs, w, ws, out), (x, xs[:3], w, ws, out), (x, xs, w[:, :32], ws, out), (x, xs, w, ws[:31], out), (x, xs, w, ws, out.half()),
+                 (x, None, w, ws, out), (x, xs, w, ws, out[0]), (x, xs, w, ws, out)):      # (the last: tensors of the host)
+        with pytest.raises(ValueError):
+            B.moe_project_i8(*args)
+    with pytest.raises(ValueError):
+        B.moe_project_i8(x, xs, w, ws, out, base=out[:2])
+    with pytest.raises(ValueError):
+        B.moe_project_i8(x, xs, w, ws, out, bias=ws.double())
+    b = torch.zeros(4, 64, dtype=BF)
+    for args in ((b.float(), x, xs), (b, x[:2], xs), (b, x, xs[:2]), (b, x.to(torch.uint8), xs), (b, x, None), (b[0], x, xs), (b, x, xs)):
+        with pytest.raises(ValueError):
+            B.moe_quantize_i8(*args)
