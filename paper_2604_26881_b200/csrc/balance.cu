@@ -46,7 +46,7 @@ __device__ __forceinline__ float group_max(float v)
 template <int L, int VW>
 __device__ __forceinline__ int expert_of(int sub, int i) { return ((i / VW) * L + sub) * VW + i % VW; }
 
-// This lane's 16 logits of a row, -inf where there is no expert.
+// This lane's 16 logits of a row as they are, -inf where there is no expert.
 template <int L, int VW, typename TL>
 __device__ __forceinline__ void load_row(const TL* row, int E, int sub, bool live, float (&z)[kC])
 {
@@ -62,7 +62,7 @@ __device__ __forceinline__ void load_row(const TL* row, int E, int sub, bool liv
             for (int j = 0; j < VW; ++j) if (j < n) v[j] = row[e0 + j];
         }
 #pragma unroll
-        for (int j = 0; j < VW; ++j) z[q * VW + j] = j < n ? clean(to_float(v[j])) : -INFINITY;
+        for (int j = 0; j < VW; ++j) z[q * VW + j] = j < n ? to_float(v[j]) : -INFINITY;
     }
 }
 
@@ -81,40 +81,57 @@ __device__ __forceinline__ int model_of(const RouterBatch& b, int t, bool report
     return m >= 0 && m < b.M ? m : 0;
 }
 
-// The shares p of a token, out of its logits (which become p); its log of the sum of exponentials.  A token without any logit
-// above -inf has p = 0 and 0.
-template <int L, bool SIGMOID, bool LSE>
-__device__ __forceinline__ void shares(float (&z)[kC], float& lse)
+// Most rows need one exponential per expert: with x = exp(z), softmax is x / sum x, the sigmoid x / (1 + x), 1 - s is 1 / (1 + x) and
+// the log of the sum log(sum x), without the largest logit, as long as the sum of x is well inside the range of fp32 (a logit counts
+// beside others down to exp(-87)).  Rows where it is not, or not a number, are done over with shifted exponentials.
+__device__ __forceinline__ bool ordinary(float sum) { return sum > 1e-9f && sum < 1e30f; }
+__device__ __forceinline__ float rcp(float x)
 {
-    float top = z[0];
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The same for rows of any logits: from clean(z), exponentials shifted by the largest.  e: exp(z - top), of which the softmax is e *
+// inv; s: sigmoid scores, in units of the largest if that is below exp(-60).  A token without any logit above -inf has zeros.
+template <int L, bool SIGMOID>
+struct Shifted {
+    float e[kC], s[SIGMOID ? kC : 1];
+    float top, inv, lse, share_inv;
+    __device__ __forceinline__ explicit Shifted(const float (&z)[kC])
+    {
+        top = -INFINITY;
 #pragma unroll
-    for (int i = 1; i < kC; ++i) top = fmaxf(top, z[i]);
-    top = group_max<L>(top);
-    const bool some = top > -INFINITY;
-    const float from = some ? top : 0.f;
-    lse = 0.f;
-    float sum = 0.f;
-    if (!SIGMOID || LSE) {
-        float e[kC];
+        for (int i = 0; i < kC; ++i) top = fmaxf(top, clean(z[i]));
+        top = group_max<L>(top);
+        const bool some = top > -INFINITY;
+        const float from = some ? top : 0.f;
+        float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < kC; ++i) { e[i] = expf(z[i] - from); sum += e[i]; }
+        for (int i = 0; i < kC; ++i) { e[i] = expf(clean(z[i]) - from); sum += e[i]; }
         sum = group_sum<L>(sum);
-        if (LSE) lse = some ? top + logf(sum) : 0.f;
-        if (!SIGMOID) {
+        inv = some ? 1.f / sum : 0.f;
+        lse = some ? top + logf(sum) : 0.f;
+        share_inv = inv;
+        if (SIGMOID) {
+            const float ref = top > -60.f ? 0.f : from;
+            sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < kC; ++i) z[i] = e[i];
+            for (int i = 0; i < kC; ++i) { s[i] = sigmoid_from(clean(z[i]), ref); sum += s[i]; }
+            sum = group_sum<L>(sum);
+            share_inv = some ? 1.f / sum : 0.f;
         }
     }
-    if (SIGMOID) {
-        const float ref = top > -60.f ? 0.f : from;           // (sigmoids of far negative logits in units of their largest)
-        sum = 0.f;
+    __device__ __forceinline__ float share(int i) const { return (SIGMOID ? s[i] : e[i]) * share_inv; }
+};
+
+template <int L, bool SIGMOID>
+__device__ __noinline__ void shifted_shares(float (&z)[kC], float& lse)
+{
+    const Shifted<L, SIGMOID> r(z);
 #pragma unroll
-        for (int i = 0; i < kC; ++i) { z[i] = sigmoid_from(z[i], ref); sum += z[i]; }
-        sum = group_sum<L>(sum);
-    }
-    const float inv = some ? 1.f / sum : 0.f;
-#pragma unroll
-    for (int i = 0; i < kC; ++i) z[i] *= inv;
+    for (int i = 0; i < kC; ++i) z[i] = r.share(i);
+    lse = r.lse;
 }
 
 __host__ __device__ constexpr int padded(int E) { return (E + 3) & ~3; }
@@ -181,9 +198,10 @@ __device__ __forceinline__ void finish(const BalanceArgs& p, int m, const float*
     }
 }
 
-// blockIdx.y: model; the model's blocks take chunks of 32 tokens per warp in turn.  A lane keeps the sums of its 16 experts.
+// blockIdx.y: model; the model's blocks take chunks of up to 32 tokens per warp in turn, list those of the model and sum up 32 / L of
+// them at a time.  A lane keeps the sums of its 16 experts.
 template <int L, int VW, bool SIGMOID, typename TL>
-__global__ void __launch_bounds__(32 * kWarps)
+__global__ void __launch_bounds__(32 * kWarps, 4)
 balance_kernel(const BalanceArgs p)
 {
     constexpr int G = 32 / L;                                 // tokens of a warp at a time
@@ -204,10 +222,10 @@ balance_kernel(const BalanceArgs p)
 #pragma unroll
     for (int i = 0; i < kC; ++i) acc[i] = 0.f;
     int tokens = 0;
-    const int chunks = (b.T + 31) / 32;
+    const int chunks = (b.T + p.chunk - 1) / p.chunk;
     for (int chunk = blockIdx.x * kWarps + warp; chunk < chunks; chunk += gridDim.x * kWarps) {
-        const int t0 = chunk * 32, t = t0 + lane;
-        const bool mine = t < b.T && model_of(b, t, m == 0) == m;
+        const int t0 = chunk * p.chunk, t = t0 + lane;
+        const bool mine = lane < p.chunk && t < b.T && model_of(b, t, m == 0) == m;
         const uint32_t set = __ballot_sync(kFull, mine);
         const int count = __popc(set);
         tokens += count;
@@ -223,9 +241,34 @@ balance_kernel(const BalanceArgs p)
         for (int base = 0; base < count; base += G) {
             const bool live = base + group < count;
             const int row = t0 + (live ? s_list[warp][base + group] : 0);
-            float z[kC], lse;
-            load_row<L, VW>((const TL*)b.logits + (size_t)row * b.ld, b.E, sub, live, z);
-            if (p.z_loss) shares<L, SIGMOID, true>(z, lse); else shares<L, SIGMOID, false>(z, lse);
+            const TL* const logits = (const TL*)b.logits + (size_t)row * b.ld;
+            float z[kC], x = 0.f, lse;
+            load_row<L, VW>(logits, b.E, sub, live, z);
+#pragma unroll
+            for (int i = 0; i < kC; ++i) { z[i] = expf(z[i]); x += z[i]; }
+            x = group_sum<L>(x);
+            lse = logf(x);
+            const bool far = live && !ordinary(x);
+            if (SIGMOID) {
+                x = 0.f;
+#pragma unroll
+                for (int i = 0; i < kC; ++i) { z[i] *= rcp(1.f + z[i]); x += z[i]; }
+                x = group_sum<L>(x);
+            }
+            const float inv = live ? __fdividef(1.f, x) : 0.f;
+            if (!live) lse = 0.f;
+#pragma unroll
+            for (int i = 0; i < kC; ++i) z[i] *= inv;
+            if (__any_sync(kFull, far)) {
+                float again[kC], lse2;
+                load_row<L, VW>(logits, b.E, sub, far, again);
+                shifted_shares<L, SIGMOID>(again, lse2);
+                if (far) {
+                    lse = lse2;
+#pragma unroll
+                    for (int i = 0; i < kC; ++i) z[i] = again[i];
+                }
+            }
 #pragma unroll
             for (int i = 0; i < kC; ++i) acc[i] += z[i];
             z2 = fmaf(lse, lse, z2);
@@ -281,189 +324,262 @@ balance_finish_kernel(const BalanceArgs p)
 
 // ---------------------------------------------------------------------------------------------------------------------
 
-template <int L, int VW, bool SIGMOID, typename TL>
-__global__ void __launch_bounds__(32 * kWarps)
-gate_grad_kernel(const GateGradArgs p)
+// One step of a warp: the gradients of the tokens of its groups of L lanes.  FAR: those whose exponentials need a shift (`todo`);
+// otherwise all but those, which are returned.  f: the model's counts if there is one model, else they are looked up.
+template <int L, int VW, bool SIGMOID, bool MULTI, bool FAR, typename TL>
+__device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add, const float (&f1)[kC], float coef1, float z1)
 {
-    constexpr int G = 32 / L;                                 // tokens of a warp at a time
     constexpr int J = L < 8 ? 2 : 1;                          // chosen experts of a lane: j = sub and sub + L
-    __shared__ __align__(16) float s_add[kWarps][G][kC * L];  // what comes by way of the weights, at the chosen experts
-    pdl_wait();
-    pdl_launch_dependents();
     const RouterBatch& b = p.b;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane % L, group = lane / L;
-    float* const add = s_add[warp][group];
-    for (int i = sub; i < kC * L; i += L) add[i] = 0.f;
-    __syncwarp();
-    const int steps = (b.T + G - 1) / G;
-    for (int step = blockIdx.x * kWarps + warp; step < steps; step += gridDim.x * kWarps) {
-        const int t = step * G + group;
-        const int m = t < b.T ? model_of(b, t, sub == 0) : -1;
-        const bool live = m >= 0;
-        float z[kC];
-        load_row<L, VW>((const TL*)b.logits + (size_t)t * b.ld, b.E, sub, live, z);
-        // the chosen experts, their weights' gradients and their logits
-        int id[J];
-        float gw[J], zj[J];
+    const bool live = m >= 0;
+    const TL* const logits = (const TL*)b.logits + (size_t)t * b.ld;
+    int id[J];
+    float gw[J];
+#pragma unroll
+    for (int q = 0; q < J; ++q) {
+        const int j = sub + q * L;
+        id[q] = -1; gw[q] = 0.f;
+        if (p.d_w && live && j < b.k) {
+            id[q] = b.topk_idx[(size_t)t * b.k + j];
+            gw[q] = p.d_w[(size_t)t * b.k + j] * p.scale;
+        }
+    }
+    float coef = coef1, cz = z1, f[kC];
+    if (MULTI) {
+        const float n = live && (p.d_loss || p.d_z) ? (float)max(p.tokens[m], 1) : 1.f;
+        coef = live && p.d_loss ? p.d_loss[m] * ((float)b.E / (float)b.k) / n / n : 0.f;
+        cz = live && p.d_z ? 2.f * p.d_z[m] / n : 0.f;
+    }
+    float e[kC], r[SIGMOID ? kC : 1], s[SIGMOID && FAR ? kC : 1];       // exponentials; 1 - s; s
+    float inv, lse, share_inv, from = 0.f, ref = 0.f;
+    bool far = false;
+    load_row<L, VW>(logits, b.E, sub, live, e);
+    if (MULTI) {
+#pragma unroll
+        for (int i = 0; i < kC; ++i) {
+            const int at = expert_of<L, VW>(sub, i);
+            f[i] = live && p.d_loss && at < b.E ? (float)p.counts[(size_t)m * b.E + at] : 0.f;
+        }
+    }
+    // (a token's choices are as many as its lanes take; their logits are in the caches now)
+    float zj[J];
+#pragma unroll
+    for (int q = 0; q < J; ++q) {
+        if (id[q] >= b.E || (id[q] < 0 && p.d_w && live && sub + q * L < b.k)) {
+            if (b.status) atomicOr(b.status, MOE_DEV_BAD_EXPERT);
+            id[q] = -1;
+        }
+        zj[q] = id[q] >= 0 ? to_float(logits[id[q]]) : -INFINITY;
+    }
+    if constexpr (FAR) {
+        const Shifted<L, SIGMOID> x(e);
+        if (SIGMOID) {
+#pragma unroll
+            for (int i = 0; i < kC; ++i) { r[i] = sigmoid_from(-clean(e[i]), 0.f); s[i] = x.s[i]; }
+        }
+#pragma unroll
+        for (int i = 0; i < kC; ++i) e[i] = x.e[i];
+        inv = x.inv; lse = x.lse; share_inv = x.share_inv;
+        from = x.top > -INFINITY ? x.top : 0.f;
+        float best = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < J; ++q) { zj[q] = clean(zj[q]); best = fmaxf(best, zj[q]); }
+        best = group_max<L>(best);
+        if (p.renormalize && best > -INFINITY) ref = SIGMOID ? fminf(best, 0.f) : best;
+    } else {
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < kC; ++i) { e[i] = expf(e[i]); x += e[i]; }
+        x = group_sum<L>(x);
+        far = live && !ordinary(x);
+        inv = live ? __fdividef(1.f, x) : 0.f;
+        lse = live ? logf(x) : 0.f;
+        share_inv = inv;
+        if (SIGMOID) {
+            x = 0.f;
+#pragma unroll
+            for (int i = 0; i < kC; ++i) { r[i] = rcp(1.f + e[i]); x = fmaf(e[i], r[i], x); }
+            x = group_sum<L>(x);
+            share_inv = live ? __fdividef(1.f, x) : 0.f;
+        }
+    }
+    float d[kC];
+#pragma unroll
+    for (int i = 0; i < kC; ++i) d[i] = 0.f;
+    if (p.d_w) {
+        float ws[J], inner[J], sum = 0.f;
 #pragma unroll
         for (int q = 0; q < J; ++q) {
-            const int j = sub + q * L;
-            id[q] = -1; gw[q] = 0.f; zj[q] = -INFINITY;
-            if (p.d_w && live && j < b.k) {
-                const int e = b.topk_idx[(size_t)t * b.k + j];
-                if (e >= 0 && e < b.E) {
-                    id[q] = e;
-                    gw[q] = p.d_w[(size_t)t * b.k + j] * p.scale;
-                    zj[q] = clean(to_float(((const TL*)b.logits)[(size_t)t * b.ld + e]));
-                } else if (b.status) {
-                    atomicOr(b.status, MOE_DEV_BAD_EXPERT);
-                }
-            }
+            const float x = expf(zj[q]);                      // (not used where it is not in range)
+            if (FAR) ws[q] = SIGMOID ? sigmoid_from(zj[q], ref) : (p.renormalize ? expf(zj[q] - ref) : expf(zj[q] - from) * inv);
+            else ws[q] = SIGMOID ? x * rcp(1.f + x) : (p.renormalize ? x : x * inv);
+            sum += ws[q];
         }
-        float top = z[0];
-#pragma unroll
-        for (int i = 1; i < kC; ++i) top = fmaxf(top, z[i]);
-        top = group_max<L>(top);
-        const bool some = top > -INFINITY;
-        const float from = some ? top : 0.f;
-        // softmax (of sigmoid scores only where the second loss asks for it)
-        float soft[kC], soft_inv = 0.f, lse = 0.f;
-        if (!SIGMOID || p.d_z) {
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < kC; ++i) { soft[i] = expf(z[i] - from); sum += soft[i]; }
+        if (p.renormalize) {
             sum = group_sum<L>(sum);
-            soft_inv = some ? 1.f / sum : 0.f;
-            lse = some ? top + logf(sum) : 0.f;
-        }
-        float d[kC];
+            if (!FAR) far = far || (live && !(sum > 1e-30f));           // (the chosen ones alone are too small)
+            const float over = sum > 0.f ? 1.f / sum : 0.f;
+            sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < kC; ++i) d[i] = 0.f;
-        if (p.d_w) {
-            float ws[J], inner[J], s = 0.f;
-            if (p.renormalize) {
-                float best = zj[0];
-                if (J > 1) best = fmaxf(best, zj[J - 1]);
-                best = group_max<L>(best);
-                const float ref = best > -INFINITY ? (SIGMOID ? fminf(best, 0.f) : best) : 0.f;
+            for (int q = 0; q < J; ++q) { ws[q] *= over; sum = fmaf(gw[q], ws[q], sum); }
+            sum = group_sum<L>(sum);
 #pragma unroll
-                for (int q = 0; q < J; ++q) { ws[q] = SIGMOID ? sigmoid_from(zj[q], ref) : expf(zj[q] - ref); s += ws[q]; }
-                s = group_sum<L>(s);
-                const float inv = s > 0.f ? 1.f / s : 0.f;
-                s = 0.f;
+            for (int q = 0; q < J; ++q) inner[q] = ws[q] * (gw[q] - sum);
+        } else {
+            sum = 0.f;
 #pragma unroll
-                for (int q = 0; q < J; ++q) { ws[q] *= inv; s = fmaf(gw[q], ws[q], s); }
-                s = group_sum<L>(s);
+            for (int q = 0; q < J; ++q) { inner[q] = gw[q] * ws[q]; sum += inner[q]; }
+            if (!SIGMOID) {                                   // every expert has its share of the whole
+                sum = group_sum<L>(sum) * inv;
 #pragma unroll
-                for (int q = 0; q < J; ++q) inner[q] = ws[q] * (gw[q] - s);
-            } else {
-#pragma unroll
-                for (int q = 0; q < J; ++q) {
-                    ws[q] = SIGMOID ? sigmoid_from(zj[q], 0.f) : expf(zj[q] - from) * soft_inv;
-                    inner[q] = gw[q] * ws[q];
-                    s += inner[q];
-                }
-                if (!SIGMOID) {                               // every expert has its share of the whole
-                    s = group_sum<L>(s) * soft_inv;
-#pragma unroll
-                    for (int i = 0; i < kC; ++i) d[i] = -soft[i] * s;
-                }
+                for (int i = 0; i < kC; ++i) d[i] = -e[i] * sum;
             }
+        }
 #pragma unroll
-            for (int q = 0; q < J; ++q) if (SIGMOID) inner[q] *= sigmoid_from(-zj[q], 0.f);
-            // an expert that was chosen twice gets both, in the order of the choices
+        for (int q = 0; q < J; ++q) {
+            if (SIGMOID) inner[q] *= sigmoid_from(-zj[q], 0.f);
+            if (id[q] >= 0) reinterpret_cast<int*>(add)[id[q]] = sub + q * L;
+        }
+        __syncwarp();
+        bool twice = false;
+#pragma unroll
+        for (int q = 0; q < J; ++q) twice |= id[q] >= 0 && reinterpret_cast<int*>(add)[id[q]] != sub + q * L;
+        __syncwarp();
+        if (__any_sync(kFull, twice)) {
+            // an expert that was chosen more than once gets them all, in the order of the choices
             float total[J];
 #pragma unroll
             for (int q = 0; q < J; ++q) total[q] = 0.f;
             for (int j = 0; j < b.k; ++j) {
-                int other = __shfl_sync(kFull, id[0], (group * L) + (j % L));
-                float x = __shfl_sync(kFull, inner[0], (group * L) + (j % L));
+                int other = __shfl_sync(kFull, id[0], group * L + j % L);
+                float x = __shfl_sync(kFull, inner[0], group * L + j % L);
                 if (J > 1) {
-                    const int other1 = __shfl_sync(kFull, id[J - 1], (group * L) + (j % L));
-                    const float x1 = __shfl_sync(kFull, inner[J - 1], (group * L) + (j % L));
+                    const int other1 = __shfl_sync(kFull, id[J - 1], group * L + j % L);
+                    const float x1 = __shfl_sync(kFull, inner[J - 1], group * L + j % L);
                     if (j >= L) { other = other1; x = x1; }
                 }
 #pragma unroll
                 for (int q = 0; q < J; ++q) if (other == id[q]) total[q] += x;
             }
 #pragma unroll
-            for (int q = 0; q < J; ++q) if (id[q] >= 0) add[id[q]] = total[q];
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < kC; ++i) d[i] += add[expert_of<L, VW>(sub, i)];
-            __syncwarp();
-#pragma unroll
-            for (int q = 0; q < J; ++q) if (id[q] >= 0) add[id[q]] = 0.f;
-            __syncwarp();
+            for (int q = 0; q < J; ++q) inner[q] = total[q];
         }
-        const float n = live && (p.d_loss || p.d_z) ? (float)max(p.tokens[m], 1) : 1.f;
-        if (p.d_z) {
-            const float c = live ? 2.f * p.d_z[m] / n * soft_inv : 0.f;
 #pragma unroll
-            for (int i = 0; i < kC; ++i) d[i] = fmaf(soft[i] * c, lse, d[i]);      // (in this order: a share of 0 stays 0)
-        }
-        if (p.d_loss) {
-            const float coef = live ? p.d_loss[m] * ((float)b.E / (float)b.k) / n / n : 0.f;
-            float f[kC], share[kC], sum = 0.f;
+        for (int q = 0; q < J; ++q) if (id[q] >= 0) add[id[q]] = inner[q];
+        __syncwarp();
 #pragma unroll
-            for (int i = 0; i < kC; ++i) {
-                const int e = expert_of<L, VW>(sub, i);
-                f[i] = live && e < b.E ? (float)p.counts[(size_t)m * b.E + e] : 0.f;
+        for (int q = 0; q < kC / VW; ++q) {
+            const float* const from_add = add + (q * L + sub) * VW;
+            if (VW > 1) {
+#pragma unroll
+                for (int j = 0; j < VW; j += 4) {
+                    const float4 x = *reinterpret_cast<const float4*>(from_add + j);
+                    d[q * VW + j] += x.x; d[q * VW + j + 1] += x.y; d[q * VW + j + 2] += x.z; d[q * VW + j + 3] += x.w;
+                }
+            } else {
+                d[q] += *from_add;
             }
-            if (SIGMOID) {
-                const float ref = top > -60.f ? 0.f : from;
+        }
+        __syncwarp();
 #pragma unroll
-                for (int i = 0; i < kC; ++i) { share[i] = sigmoid_from(z[i], ref); sum += share[i]; }
-                sum = group_sum<L>(sum);
-                const float inv = some ? 1.f / sum : 0.f;
+        for (int q = 0; q < J; ++q) if (id[q] >= 0) add[id[q]] = 0.f;
+        __syncwarp();
+    }
+    if (p.d_z) {
+        const float c = cz * inv;
 #pragma unroll
-                for (int i = 0; i < kC; ++i) share[i] *= inv;
+        for (int i = 0; i < kC; ++i) d[i] = fmaf(e[i] * c, lse, d[i]);  // (in this order: a share of 0 stays 0)
+    }
+    if (p.d_loss) {
+        float mean = 0.f;
+#pragma unroll
+        for (int i = 0; i < kC; ++i) {
+            const float score = SIGMOID ? (FAR ? s[SIGMOID && FAR ? i : 0] : e[i] * r[SIGMOID ? i : 0]) : e[i];
+            mean = fmaf(MULTI ? f[i] : f1[i], score, mean);
+        }
+        mean = group_sum<L>(mean) * share_inv;
+        const float c = coef * share_inv;
+#pragma unroll
+        for (int i = 0; i < kC; ++i) {
+            const float score = SIGMOID ? (FAR ? s[SIGMOID && FAR ? i : 0] : e[i] * r[SIGMOID ? i : 0]) : e[i];
+            float x = score * c * ((MULTI ? f[i] : f1[i]) - mean);
+            if (SIGMOID) x *= r[i];
+            d[i] += x;
+        }
+    }
+    if (t < b.T && (FAR ? todo : !far)) {
+        TL* const row = (TL*)p.d_logits + (size_t)t * p.ld_d;
+#pragma unroll
+        for (int q = 0; q < kC / VW; ++q) {
+            const int e0 = (q * L + sub) * VW, n = b.E - e0;
+            TL v[VW];
+#pragma unroll
+            for (int j = 0; j < VW; ++j) v[j] = (TL)(live ? d[q * VW + j] : 0.f);
+            if (VW > 1 && n >= VW) {
+                uint4 u;
+                memcpy(&u, v, sizeof(v) < sizeof(u) ? sizeof(v) : sizeof(u));
+                *reinterpret_cast<uint4*>(row + e0) = u;
             } else {
 #pragma unroll
-                for (int i = 0; i < kC; ++i) share[i] = soft[i] * soft_inv;
-            }
-            float mean = 0.f;
-#pragma unroll
-            for (int i = 0; i < kC; ++i) mean = fmaf(f[i], share[i], mean);
-            mean = group_sum<L>(mean);
-#pragma unroll
-            for (int i = 0; i < kC; ++i) {
-                float x = share[i] * (f[i] - mean) * coef;
-                if (SIGMOID) x *= sigmoid_from(-z[i], 0.f);
-                d[i] += x;
+                for (int j = 0; j < VW; ++j) if (j < n) row[e0 + j] = v[j];
             }
         }
-        if (t < b.T) {
-            TL* const row = (TL*)p.d_logits + (size_t)t * p.ld_d;
+    }
+    return far;
+}
+template <int L, int VW, bool SIGMOID, bool MULTI, typename TL>
+__device__ __noinline__ void grad_step_far(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add, const float (&f1)[kC], float coef1, float z1)
+{
+    grad_step<L, VW, SIGMOID, MULTI, true, TL>(p, t, m, sub, group, todo, add, f1, coef1, z1);
+}
+
+template <int L, int VW, bool SIGMOID, bool MULTI, typename TL>
+__global__ void __launch_bounds__(32 * kWarps, 2)
+gate_grad_kernel(const __grid_constant__ GateGradArgs p)
+{
+    constexpr int G = 32 / L;                                 // tokens of a warp at a time
+    __shared__ __align__(16) float s_add[kWarps][G][kC * L];  // what comes by way of the weights, at the chosen experts
+    const RouterBatch& b = p.b;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane % L, group = lane / L;
+    float* const add = s_add[warp][group];
+    for (int i = sub; i < kC * L; i += L) add[i] = 0.f;
+    __syncwarp();
+    pdl_wait();
+    pdl_launch_dependents();
+    float f[kC], coef = 0.f, cz = 0.f;
+    if (!MULTI) {
+        const float n = p.d_loss || p.d_z ? (float)max(p.tokens[0], 1) : 1.f;
+        if (p.d_loss) coef = p.d_loss[0] * ((float)b.E / (float)b.k) / n / n;
+        if (p.d_z) cz = 2.f * p.d_z[0] / n;
+    }
 #pragma unroll
-            for (int q = 0; q < kC / VW; ++q) {
-                const int e0 = (q * L + sub) * VW, n_here = b.E - e0;
-                TL v[VW];
-#pragma unroll
-                for (int j = 0; j < VW; ++j) v[j] = (TL)(live ? d[q * VW + j] : 0.f);
-                if (VW > 1 && n_here >= VW) {
-                    uint4 u;
-                    memcpy(&u, v, sizeof(v) < sizeof(u) ? sizeof(v) : sizeof(u));
-                    *reinterpret_cast<uint4*>(row + e0) = u;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < VW; ++j) if (j < n_here) row[e0 + j] = v[j];
-                }
-            }
-        }
+    for (int i = 0; i < kC; ++i) {
+        const int e = expert_of<L, VW>(sub, i);
+        f[i] = !MULTI && p.d_loss && e < b.E ? (float)p.counts[e] : 0.f;
+    }
+    const int steps = (b.T + G - 1) / G;
+    for (int step = blockIdx.x * kWarps + warp; step < steps; step += gridDim.x * kWarps) {
+        const int t = step * G + group;
+        const int m = t < b.T ? model_of(b, t, sub == 0) : -1;
+        const bool far = grad_step<L, VW, SIGMOID, MULTI, false, TL>(p, t, m, sub, group, false, add, f, coef, cz);
+        if (__any_sync(kFull, far)) grad_step_far<L, VW, SIGMOID, MULTI, TL>(p, t, m, sub, group, far, add, f, coef, cz);
     }
 }
 
 bool wide_rows(const void* p, int64_t ld, int size) { return (uintptr_t)p % 16 == 0 && ld * size % 16 == 0; }
 
-// the block count of balance_kernel, per model
-int balance_blocks(int T, int E, int M)
+// Tokens that a warp of balance_kernel lists at once (with several models only those of one are summed up), and its blocks per model.
+struct BalanceShape { int chunk, blocks; };
+BalanceShape balance_shape(int T, int E, int M)
 {
-    const int chunks = (T + 31) / 32, all = (chunks + kWarps - 1) / kWarps;
-    int most = 148 * 2 / M;
+    BalanceShape s;
+    s.chunk = 32 / (E <= 64 ? 4 : (E <= 128 ? 8 : 16));
+    while (s.chunk < 32 && (M > 1 || T / s.chunk > 148 * 32)) s.chunk *= 2;
+    const int chunks = (T + s.chunk - 1) / s.chunk, all = (chunks + kWarps - 1) / kWarps;
+    int most = 148 * 4 / M;
     if (most < 1) most = 1;
-    const int blocks = all < most ? all : most;
-    return blocks < 1 ? 1 : blocks;
+    s.blocks = all <= 2 ? 1 : (all < most ? all : most);
+    return s;
 }
 
 template <int L, int VW, typename TL>
@@ -478,8 +594,11 @@ cudaError_t run_grad(const GateGradArgs& p, cudaStream_t st)
 {
     const int steps = (p.b.T + 32 / L - 1) / (32 / L), all = (steps + kWarps - 1) / kWarps, most = 148 * 4;
     const dim3 grid(all < most ? all : most), block(32 * kWarps);
-    return p.b.score == MOE_SCORE_SIGMOID ? launch_pdl(gate_grad_kernel<L, VW, true, TL>, grid, block, 0, st, p)
-                                          : launch_pdl(gate_grad_kernel<L, VW, false, TL>, grid, block, 0, st, p);
+    if (p.b.score == MOE_SCORE_SIGMOID)
+        return p.b.M > 1 ? launch_pdl(gate_grad_kernel<L, VW, true, true, TL>, grid, block, 0, st, p)
+                         : launch_pdl(gate_grad_kernel<L, VW, true, false, TL>, grid, block, 0, st, p);
+    return p.b.M > 1 ? launch_pdl(gate_grad_kernel<L, VW, false, true, TL>, grid, block, 0, st, p)
+                     : launch_pdl(gate_grad_kernel<L, VW, false, false, TL>, grid, block, 0, st, p);
 }
 // (a macro: the shapes of both kernels)
 #define FAASMOE_BY_SHAPE(run, E, wide, bf, ...)                                                                            \
@@ -494,7 +613,7 @@ cudaError_t run_grad(const GateGradArgs& p, cudaStream_t st)
 
 int64_t balance_workspace(int T, int E, int M)
 {
-    const int blocks = balance_blocks(T, E, M);
+    const int blocks = balance_shape(T, E, M).blocks;
     return blocks == 1 ? 0 : (int64_t)blocks * M * record(E) * (int64_t)sizeof(float);
 }
 
@@ -502,7 +621,9 @@ cudaError_t launch_balance(const BalanceArgs& in, cudaStream_t st)
 {
     BalanceArgs p = in;
     const RouterBatch& b = p.b;
-    p.blocks = balance_blocks(b.T, b.E, b.M);
+    const BalanceShape s = balance_shape(b.T, b.E, b.M);
+    p.blocks = s.blocks;
+    p.chunk = s.chunk;
     const bool wide = wide_rows(b.logits, b.ld, b.bf16_logits ? 2 : 4);
     const cudaError_t e = FAASMOE_BY_SHAPE(run_balance, b.E, wide, b.bf16_logits, p, st);
     if (e != cudaSuccess || p.blocks == 1) return e;

@@ -29,6 +29,7 @@ struct BalanceArgs {
     float* z_loss;                    // [M] or null
     float* parts;                     // [blocks][M][record]
     int blocks;                       // blocks per model
+    int chunk;                        // tokens that a warp lists at once
 };
 
 struct GateGradArgs {

@@ -67,8 +67,17 @@ __device__ __forceinline__ float norm_factor(float (&x)[V][8], int H, float eps,
     return 1.f / sqrtf(mean);
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
-__device__ __forceinline__ float activate(float g, int act) { return act == MOE_GATE_SIGMOID ? sigmoid(g) : g; }
+// The gate's value; *slope: its derivative (1 - s by way of exp(-|x|), so that neither end cancels).
+__device__ __forceinline__ float activate(float x, int act, float* slope = nullptr)
+{
+    if (act != MOE_GATE_SIGMOID) {
+        if (slope) *slope = 1.f;
+        return x;
+    }
+    const float e = expf(-fabsf(x)), r = __fdividef(1.f, 1.f + e), er = e * r;
+    if (slope) *slope = er * r;
+    return x >= 0.f ? r : (x < 0.f ? er : x);                 // (a NaN stays one)
+}
 
 // What every row multiplies a column of the block's output with: block_scale, the weight behind the block, a gate per channel.
 template <int V>
@@ -225,38 +234,129 @@ bool rows16(const void* q, int64_t ld) { return !q || (al(q, 16) && ld % 8 == 0)
 //   d_g = b m post  (times g (1 - g) of a sigmoid)                e = b g post,  d_post = sum_t b g m
 //   d_y = (e - m mean(e m)) / rms(y)
 
-// the sums of `v` and `w` over a row's W warps
-__device__ __forceinline__ float row_sum(float v, int W, int warp, int lane, int row, float* sums)
+// Up to four sums over a row's W warps at once; every lane gets all of them.  In a warp the lanes share the values out (half of them
+// after the first exchange, one after the second: 6 shuffles instead of 20), then each warp adds up all warps' sums, sixteen at most of
+// each value, by eight lanes.  `s`: 4 x 16 floats of the row, zero beyond W; used again only after another barrier of the block.
+template <int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], int W, int wr, int lane, float* s, bool block = true, int row = 0)
 {
-    v = warp_sum(v);
-    if (W > 1) {
-        if (lane == 0) sums[warp] = v;
-        __syncthreads();
-        v = 0.f;
-        for (int i = 0; i < W; ++i) v += sums[row * W + i];
+    float x;
+    if (N == 1) {
+        x = warp_sum(v[0]);
+    } else {
+        const bool hi = lane & 16, mid = lane & 8;
+        const float a = v[0], b = v[1], c = N > 2 ? v[N > 2 ? 2 : 0] : 0.f, d = N > 3 ? v[N > 3 ? 3 : 0] : 0.f;
+        const float x0 = (hi ? c : a) + __shfl_xor_sync(kFull, hi ? a : c, 16), x1 = (hi ? d : b) + __shfl_xor_sync(kFull, hi ? b : d, 16);
+        x = (mid ? x1 : x0) + __shfl_xor_sync(kFull, mid ? x0 : x1, 8);
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) x += __shfl_xor_sync(kFull, x, o);
     }
-    return v;
+    if (W > 1) {
+        if ((lane & 7) == 0 && (lane >> 3) < N) s[(lane >> 3) * 16 + wr] = x;
+        if (block) __syncthreads(); else row_sync(row, W);
+        const float2 f = *reinterpret_cast<const float2*>(s + (N == 1 ? 0 : lane >> 3) * 16 + (lane & 7) * 2);
+        x = f.x + f.y;
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) x += __shfl_xor_sync(kFull, x, o);
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = __shfl_sync(kFull, x, 8 * n);
 }
 
+constexpr int kSumsOfRow = 2 * 2 * 4 * 16;      // (two in turn) x (two steps) x values x warps
+
+__device__ __forceinline__ bool in_range(float mean) { return mean >= 0x1p-100f && mean <= FLT_MAX; }
+
+// A row whose squares leave the range of fp32: multiplied in place by a power of two that brings them inside; sums: those of its
+// squares, and of its products with d.
+template <int V>
+__device__ __noinline__ float rescale(float (&x)[V][8], const float (&d)[V][8], float mean, float (&sums)[2], int W, int wr, int lane, int row, float* s)
+{
+    const float unit = mean < 1.f ? 0x1p100f : 0x1p-72f;
+    sums[0] = sums[1] = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[v][i] *= unit;
+            sums[0] = fmaf(x[v][i], x[v][i], sums[0]);
+            sums[1] = fmaf(x[v][i], d[v][i], sums[1]);
+        }
+    if (W > 1) row_sync(row, W);                              // (everybody has read what was there)
+    row_sums<2>(sums, W, wr, lane, s, false, row);
+    return unit;
+}
+
+// A lane's sums over the block's rows, V vectors of eight columns of each of N gradients: in registers where there is one vector, else
+// in shared memory that no other lane touches (vectors of 16 bytes, neighbouring lanes side by side).
+template <int V, int N>
+struct ColumnSums {
+    float r[V == 1 ? N : 1][8];
+    float4* s;
+    __device__ __forceinline__ ColumnSums()
+    {
+        extern __shared__ __align__(16) float4 s_columns[];
+        s = s_columns + threadIdx.x;
+        if (V == 1) {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r[n][i] = 0.f;
+        } else {
+#pragma unroll
+            for (int j = 0; j < N * V * 2; ++j) s[j * blockDim.x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    }
+    __device__ __forceinline__ void get(int n, int v, float (&f)[8]) const
+    {
+        if (V == 1) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = r[n][i];
+        } else {
+            const float4 a = s[((n * V + v) * 2) * blockDim.x], b = s[((n * V + v) * 2 + 1) * blockDim.x];
+            f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+        }
+    }
+    // column i: + x[i] y[i]
+    __device__ __forceinline__ void add(int n, int v, const float (&x)[8], const float (&y)[8])
+    {
+        if (V == 1) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[n][i] = fmaf(x[i], y[i], r[n][i]);
+        } else {
+            float f[8];
+            get(n, v, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = fmaf(x[i], y[i], f[i]);
+            s[((n * V + v) * 2) * blockDim.x] = make_float4(f[0], f[1], f[2], f[3]);
+            s[((n * V + v) * 2 + 1) * blockDim.x] = make_float4(f[4], f[5], f[6], f[7]);
+        }
+    }
+};
+// (bytes of shared memory)
+size_t column_sums_bytes(int V, int N, int threads) { return V == 1 ? 0 : (size_t)N * V * 8 * sizeof(float) * threads; }
+
 // One row at a time by W warps, V vectors per lane, blockDim / (32 W) rows at once; a lane keeps the same columns for all of the
-// block's rows and adds up their gradients (of the weights, of a gate per channel) in registers, rows in their order.
-template <int V, bool ELEMENT, bool VEC>
+// block's rows and adds up their gradients (of the weights, of a gate per channel), rows in their order.  A row has two
+// barriers: the sums of squares of h and y and that of pre d_out h, then the sum that the norm behind the block needs.  Columns that
+// are not there hold zeros, and what a row without finite sums makes of those is never stored.
+template <int V, int GATE, bool VEC>
 __global__ void __launch_bounds__(512)
 block_norm_grad_kernel(const BlockNormArgs p, int W)
 {
-    __shared__ float s_sum[2][4][16];
-    pdl_wait();
-    pdl_launch_dependents();
+    __shared__ __align__(8) float s_sums[4][kSumsOfRow];      // of a block's rows (four if a row is one warp, which needs none)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int row_in_block = warp / W, wr = warp - row_in_block * W;
     const int rows = blockDim.x / (32 * W);
     const int first = (wr * 32 + lane) * 8, step = W * 256;
+    for (int i = threadIdx.x; i < 4 * kSumsOfRow; i += blockDim.x) (&s_sums[0][0])[i] = 0.f;
+    __syncthreads();
+    pdl_wait();
+    pdl_launch_dependents();
     uint4 yv[V], hv[V], gv[V], ov[V], dv[V];
     float gt = 1.f;
     auto fetch = [&](int t) {
         const int H = t < p.T ? p.H : 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) yv[v] = load8<VEC>(p.y + (size_t)t * p.ldy + first + v * step, H - first - v * step);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int n = p.d_out ? H - first - v * step : 0;
@@ -264,70 +364,95 @@ block_norm_grad_kernel(const BlockNormArgs p, int W)
             ov[v] = load8<VEC>(p.d_out + (size_t)t * p.ldout_grad + first + v * step, n);
         }
 #pragma unroll
+        for (int v = 0; v < V; ++v) yv[v] = load8<VEC>(p.y + (size_t)t * p.ldy + first + v * step, H - first - v * step);
+#pragma unroll
         for (int v = 0; v < V; ++v) dv[v] = load8<VEC>(p.d_h + (size_t)t * p.ldh_grad + first + v * step, p.d_h ? H - first - v * step : 0);
-        if (ELEMENT) {
+        if (GATE == MOE_GATE_ELEMENT) {
 #pragma unroll
             for (int v = 0; v < V; ++v) gv[v] = load8<VEC>((const bf16*)p.gate + (size_t)t * p.ldg + first + v * step, H - first - v * step);
         }
-        if (p.gate_form == MOE_GATE_TOKEN && t < p.T) gt = ((const float*)p.gate)[t];
+        if (GATE == MOE_GATE_TOKEN && t < p.T) gt = ((const float*)p.gate)[t];
     };
-    auto column = [&](const bf16* w, int v, float* f) {       // eight of a row of weights, or ones
+    auto column = [&](const bf16* w, int v) {                 // eight of a row of weights, or ones
         const int col = first + v * step, n = p.H - col;
-        if (w) unpack8(p.vec_weight && n >= 8 ? load8<true>(w + col, n) : load8<false>(w + col, n), f);
-        else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = 1.f;
-        }
+        if (!w) return make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+        return p.vec_weight && n >= 8 ? load8<true>(w + col, n) : load8<false>(w + col, n);
     };
-    float sum_pre[V][8], sum_post[V][8], sum_gate[V][8];
+    constexpr bool kKeep = V == 1;                            // the weights stay in registers
+    uint4 pre_w[V], post_w[V], gate_w[V];
+    if (kKeep) {
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum_pre[v][i] = sum_post[v][i] = sum_gate[v][i] = 0.f;
-    const bool channel = p.gate_form == MOE_GATE_CHANNEL, token = p.gate_form == MOE_GATE_TOKEN;
+        for (int v = 0; v < V; ++v) {
+            pre_w[v] = column(p.pre, v);
+            post_w[v] = column(p.post, v);
+            if (GATE == MOE_GATE_CHANNEL) gate_w[v] = column((const bf16*)p.gate, v);
+        }
+    }
+    ColumnSums<V, GATE == MOE_GATE_CHANNEL ? 3 : 2> columns;  // of d_pre, d_post, d_gate
     const float over = 1.f / (float)p.H;
     int t = blockIdx.x * rows + row_in_block;
     int buf = 0;
+    fetch(t);
     for (int set = blockIdx.x; set * rows < p.T; set += gridDim.x, t += gridDim.x * rows, buf ^= 1) {
         const bool live = t < p.T;
-        fetch(t);
-        float y[V][8], d[V][8];
-        if (p.d_out) {
-            float h[V][8], unit;
+        float* const s1 = s_sums[row_in_block] + buf * 128;
+        float* const s2 = s1 + 64;
+        float y[V][8], d[V][8], h[V][8];
+        uint4 gate_now[V], dh_now[V];
+        const float token_gate = gt;
+        float sums[3] = {0.f, 0.f, 0.f};
 #pragma unroll
-            for (int v = 0; v < V; ++v) unpack8(hv[v], h[v]);
-            const float inv = norm_factor<V>(h, p.H, p.eps, W, warp, lane, row_in_block, s_sum[buf][0], &unit);
-            float dot = 0.f;
+        for (int v = 0; v < V; ++v) {
+            float w[8];
+            unpack8(hv[v], h[v]);
+            unpack8(ov[v], d[v]);
+            unpack8(yv[v], y[v]);
+            unpack8(kKeep ? pre_w[v] : column(p.pre, v), w);
+            dh_now[v] = dv[v];
+            if (GATE == MOE_GATE_ELEMENT) gate_now[v] = gv[v];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sums[0] = fmaf(h[v][i], h[v][i], sums[0]);
+                sums[1] = fmaf(h[v][i], d[v][i] * w[i], sums[1]);
+                sums[2] = fmaf(y[v][i], y[v][i], sums[2]);
+            }
+        }
+        if (set + gridDim.x < (p.T + rows - 1) / rows) fetch(t + gridDim.x * rows);
+        row_sums<3>(sums, W, wr, lane, s1);
+        if (p.d_out) {
+            // d_out n for the weight's gradient, then what goes on to h
+            float mean = fmaf(sums[0], over, p.eps), dot = sums[1], unit = 1.f;
+            if (!in_range(mean)) {
+                float more[2], dw[V][8];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    float w[8];
+                    unpack8(kKeep ? pre_w[v] : column(p.pre, v), w);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) dw[v][i] = d[v][i] * w[i];
+                }
+                unit = rescale<V>(h, dw, mean, more, W, wr, lane, row_in_block, s1);
+                mean = fmaf(more[0], over, p.eps * unit * unit);
+                dot = more[1];
+            }
+            const float inv = live ? 1.f / sqrtf(mean) : 0.f, back = inv * unit;
+            dot *= inv * over;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                float o[8], w[8];
-                unpack8(ov[v], o);
-                column(p.pre, v, w);
+                float w[8];
+                unpack8(kKeep ? pre_w[v] : column(p.pre, v), w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    h[v][i] *= inv;                           // n
-                    if (VEC || first + v * step + i < p.H) sum_pre[v][i] = live ? fmaf(o[i], h[v][i], sum_pre[v][i]) : sum_pre[v][i];
-                    d[v][i] = o[i] * w[i];
-                    dot = fmaf(d[v][i], h[v][i], dot);
-                }
+                for (int i = 0; i < 8; ++i) h[v][i] *= inv;   // n
+                columns.add(0, v, d[v], h[v]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[v][i] = back * fmaf(-h[v][i], dot, d[v][i] * w[i]);
             }
-            dot = row_sum(dot, W, warp, lane, row_in_block, s_sum[buf][1]) * over;
-            const float back = inv * unit;
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) d[v][i] = back * (d[v][i] - h[v][i] * dot);
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) d[v][i] = 0.f;
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = first + v * step, n = live ? p.H - col : 0;
             float u[8];
-            unpack8(dv[v], u);
+            unpack8(dh_now[v], u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 d[v][i] += u[i];
@@ -335,66 +460,83 @@ block_norm_grad_kernel(const BlockNormArgs p, int W)
                 d[v][i] *= p.block_scale;
             }
             if (p.d_residual) store8<VEC>(p.d_residual + (size_t)t * p.ldr_grad + col, n, u);
-            unpack8(yv[v], y[v]);
         }
         float inv = 1.f, unit = 1.f;
-        if (p.post) inv = norm_factor<V>(y, p.H, p.eps, W, warp, lane, row_in_block, s_sum[buf][2], &unit);
-        const float row_gate = token ? activate(gt, p.gate_act) : 1.f;
-        float dot = 0.f;                                      // without the token's gate, whose gradient it is too
+        if (p.post) {
+            float mean = fmaf(sums[2], over, p.eps);
+            if (!in_range(mean)) {
+                float more[2];
+                unit = rescale<V>(y, y, mean, more, W, wr, lane, row_in_block, s1);
+                mean = fmaf(more[0], over, p.eps * unit * unit);
+            }
+            inv = live ? 1.f / sqrtf(mean) : 0.f;
+        }
+        float row_slope = 1.f;
+        const float row_gate = GATE == MOE_GATE_TOKEN ? activate(token_gate, p.gate_act, &row_slope) : 1.f;
+        float dot[1] = {0.f};                                 // without the token's gate, whose gradient it is too
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = first + v * step;
-            float w[8], g[8];
-            column(p.post, v, w);
-            if (channel) column((const bf16*)p.gate, v, g);
-            if (ELEMENT) unpack8(gv[v], g);
-            float dg[8];
+            float w[8], g[8], dg[8], bg[8];
+            unpack8(kKeep ? post_w[v] : column(p.post, v), w);
+            if (GATE == MOE_GATE_CHANNEL) unpack8(kKeep ? gate_w[v] : column((const bf16*)p.gate, v), g);
+            if (GATE == MOE_GATE_ELEMENT) unpack8(gate_now[v], g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float m = y[v][i] * inv;
                 y[v][i] = m;
-                const bool there = live && (VEC ? col < p.H : col + i < p.H);
                 float b = d[v][i];
-                if (channel || ELEMENT) {
-                    const float value = activate(g[i], p.gate_act);
-                    dg[i] = b * m * w[i];
-                    if (p.gate_act == MOE_GATE_SIGMOID) dg[i] *= value * sigmoid(-g[i]);
+                if (GATE == MOE_GATE_CHANNEL || GATE == MOE_GATE_ELEMENT) {
+                    float slope;
+                    const float value = activate(g[i], p.gate_act, &slope);
+                    dg[i] = b * m * w[i] * slope;
                     b *= value;
-                    if (channel && there) sum_gate[v][i] += dg[i];
                 }
-                if (there) sum_post[v][i] = fmaf(b * row_gate, m, sum_post[v][i]);
+                bg[i] = b * row_gate;
                 d[v][i] = b * w[i];
-                if (there) dot = fmaf(d[v][i], m, dot);
+                dot[0] = fmaf(d[v][i], m, dot[0]);
             }
-            if (ELEMENT && p.d_gate) store8<VEC>((bf16*)p.d_gate + (size_t)t * p.ldg_grad + col, live ? p.H - col : 0, dg);
+            columns.add(1, v, bg, y[v]);
+            if (GATE == MOE_GATE_CHANNEL) {
+                constexpr float one[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+                columns.add(2, v, dg, one);
+            }
+            if (GATE == MOE_GATE_ELEMENT && p.d_gate) store8<VEC>((bf16*)p.d_gate + (size_t)t * p.ldg_grad + col, live ? p.H - col : 0, dg);
         }
-        if (p.post || token) dot = row_sum(dot, W, warp, lane, row_in_block, s_sum[buf][3]);
-        if (token && p.d_gate && live && wr == 0 && lane == 0)
-            ((float*)p.d_gate)[t] = p.gate_act == MOE_GATE_SIGMOID ? dot * (row_gate * sigmoid(-gt)) : dot;
+        if (p.post || GATE == MOE_GATE_TOKEN) row_sums<1>(dot, W, wr, lane, s2);
+        if (GATE == MOE_GATE_TOKEN && p.d_gate && live && wr == 0 && lane == 0) ((float*)p.d_gate)[t] = dot[0] * row_slope;
         if (p.d_y) {
-            const float mean = p.post ? dot * over : 0.f, back = inv * unit * row_gate;
+            const float mean = p.post ? dot[0] * over : 0.f, back = inv * unit * row_gate;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int col = first + v * step;
                 float u[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) u[i] = p.post ? back * (d[v][i] - y[v][i] * mean) : row_gate * d[v][i];
-                store8<VEC>(p.d_y + (size_t)t * p.ldy_grad + col, live ? p.H - col : 0, u);
+                for (int i = 0; i < 8; ++i) u[i] = back * fmaf(-y[v][i], mean, d[v][i]);
+                store8<VEC>(p.d_y + (size_t)t * p.ldy_grad + first + v * step, live ? p.H - first - v * step : 0, u);
             }
         }
     }
     if (!p.sums) return;
     const size_t part = (size_t)blockIdx.x * rows + row_in_block, all = (size_t)p.parts * p.H;
+    auto store = [&](int n) {
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+        for (int v = 0; v < V; ++v) {
+            const int col = first + v * step;
+            float* const dst = p.sums + n * all + part * p.H + col;
+            float f[8];
+            columns.get(n, v, f);
+            if (VEC && col < p.H) {
+                reinterpret_cast<float4*>(dst)[0] = make_float4(f[0], f[1], f[2], f[3]);
+                reinterpret_cast<float4*>(dst)[1] = make_float4(f[4], f[5], f[6], f[7]);
+            } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int col = first + v * step + i;
-            if (col >= p.H) continue;
-            if (p.d_pre) p.sums[part * p.H + col] = sum_pre[v][i];
-            if (p.d_post) p.sums[all + part * p.H + col] = sum_post[v][i];
-            if (channel && p.d_gate) p.sums[2 * all + part * p.H + col] = sum_gate[v][i];
+                for (int i = 0; i < 8; ++i) if (col + i < p.H) dst[i] = f[i];
+            }
         }
+    };
+    if (p.d_pre) store(0);
+    if (p.d_post) store(1);
+    if (GATE == MOE_GATE_CHANNEL && p.d_gate) store(2);
 }
 
 // The blocks' sums, added up in a fixed order: 32 columns a block, 32 threads a column.  blockIdx.y: which of the three.
@@ -432,15 +574,42 @@ GradShape grad_shape(int T, int H)
     return g;
 }
 
+// the opt-in to large dynamic shared memory is a per-device attribute of a kernel
+template <typename K>
+cudaError_t allow_smem(K kern, bool (&done)[kMaxDevices])
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    if (done[dev]) return cudaSuccess;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+    if (e == cudaSuccess) done[dev] = true;
+    return e;
+}
+
+template <int V, int GATE>
+cudaError_t launch_grad_gate(const BlockNormArgs& p, const GradShape& g, cudaStream_t st)
+{
+    static bool ok[2][kMaxDevices] = {{false}, {false}};
+    const dim3 grid(g.blocks), block(32 * g.W * g.rows);
+    const size_t smem = column_sums_bytes(V, GATE == MOE_GATE_CHANNEL ? 3 : 2, 32 * g.W * g.rows);
+    if (smem > 40 * 1024) {
+        const cudaError_t e = p.vec ? allow_smem(block_norm_grad_kernel<V, GATE, true>, ok[1]) : allow_smem(block_norm_grad_kernel<V, GATE, false>, ok[0]);
+        if (e != cudaSuccess) return e;
+    }
+    return p.vec ? launch_pdl(block_norm_grad_kernel<V, GATE, true>, grid, block, smem, st, p, g.W)
+                 : launch_pdl(block_norm_grad_kernel<V, GATE, false>, grid, block, smem, st, p, g.W);
+}
 template <int V>
 cudaError_t launch_grad(const BlockNormArgs& p, const GradShape& g, cudaStream_t st)
 {
-    const bool element = p.gate_form == MOE_GATE_ELEMENT;
-    const dim3 grid(g.blocks), block(32 * g.W * g.rows);
-    if (p.vec) return element ? launch_pdl(block_norm_grad_kernel<V, true, true>, grid, block, 0, st, p, g.W)
-                              : launch_pdl(block_norm_grad_kernel<V, false, true>, grid, block, 0, st, p, g.W);
-    return element ? launch_pdl(block_norm_grad_kernel<V, true, false>, grid, block, 0, st, p, g.W)
-                   : launch_pdl(block_norm_grad_kernel<V, false, false>, grid, block, 0, st, p, g.W);
+    switch (p.gate_form) {
+        case MOE_GATE_CHANNEL: return launch_grad_gate<V, MOE_GATE_CHANNEL>(p, g, st);
+        case MOE_GATE_TOKEN: return launch_grad_gate<V, MOE_GATE_TOKEN>(p, g, st);
+        case MOE_GATE_ELEMENT: return launch_grad_gate<V, MOE_GATE_ELEMENT>(p, g, st);
+        default: return launch_grad_gate<V, MOE_GATE_NONE>(p, g, st);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
