@@ -527,10 +527,11 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
     }
     return far;
 }
-template <int L, int VW, bool SIGMOID, bool MULTI, typename TL>
-__device__ __noinline__ void grad_step_far(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add, const float (&f1)[kC], float coef1, float z1)
+template <int L, int VW, bool SIGMOID, typename TL>
+__device__ __noinline__ void grad_step_far(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add)
 {
-    grad_step<L, VW, SIGMOID, MULTI, true, TL>(p, t, m, sub, group, todo, add, f1, coef1, z1);
+    const float none[kC] = {};                                // (looked up: what a call may look into does not stay in registers)
+    grad_step<L, VW, SIGMOID, true, true, TL>(p, t, m, sub, group, todo, add, none, 0.f, 0.f);
 }
 
 template <int L, int VW, bool SIGMOID, bool MULTI, typename TL>
@@ -562,7 +563,7 @@ gate_grad_kernel(const __grid_constant__ GateGradArgs p)
         const int t = step * G + group;
         const int m = t < b.T ? model_of(b, t, sub == 0) : -1;
         const bool far = grad_step<L, VW, SIGMOID, MULTI, false, TL>(p, t, m, sub, group, false, add, f, coef, cz);
-        if (__any_sync(kFull, far)) grad_step_far<L, VW, SIGMOID, MULTI, TL>(p, t, m, sub, group, far, add, f, coef, cz);
+        if (__any_sync(kFull, far)) grad_step_far<L, VW, SIGMOID, TL>(p, t, m, sub, group, far, add);
     }
 }
 

@@ -22,47 +22,66 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-// 1 / sqrt(mean of squares + eps) of a row held by W warps.  Where the squares are beyond the range of fp32, or below it with no
-// eps that counts beside them, the row is first multiplied (in place) by a power of two that is exact and brings them inside; the
-// factor is then that of the multiplied row, and *unit what it was multiplied with.
-template <int V>
-__device__ __forceinline__ float norm_factor(float (&x)[V][8], int H, float eps, int W, int warp, int lane, int row, float* sums, float* unit = nullptr)
+constexpr int kWarpsOfRow = 16;
+
+__device__ __forceinline__ bool in_range(float mean) { return mean >= 0x1p-100f && mean <= FLT_MAX; }
+
+// sum over a row's W warps; a barrier of the block, or of the row's warps alone
+__device__ __forceinline__ float row_sum(float ss, int W, int warp, int lane, int row, float* sums, bool block)
 {
-    float ss = 0.f;
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(x[v][i], x[v][i], ss);
     ss = warp_sum(ss);
     if (W > 1) {
         if (lane == 0) sums[warp] = ss;
-        __syncthreads();
+        if (block) __syncthreads(); else row_sync(row, W);
         ss = 0.f;
         for (int i = 0; i < W; ++i) ss += sums[row * W + i];
     }
-    float mean = ss / (float)H + eps;
-    if (unit) *unit = 1.f;
+    return ss;
+}
+
+template <int V>
+__device__ __forceinline__ float squares(const float2 (&x)[V][4])
+{
+    float2 s = both(0.f);
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = fma2(x[v][i], x[v][i], s);
+    return s.x + s.y;
+}
+
+// A row whose mean of squares leaves the range of fp32, or is below it with no eps that counts beside it: multiplied (in place) by a
+// power of two that is exact and brings it inside; returns the mean of the multiplied row, with its eps.
+template <int V>
+__device__ __noinline__ float mean_in_units(float2 (&x)[V][4], int H, float eps, float mean, int W, int warp, int lane, int row, float* sums)
+{
+    const float unit = mean < 1.f ? 0x1p100f : 0x1p-72f;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[v][i] = mul2(x[v][i], both(unit));
+    if (W > 1) row_sync(row, W);                              // (everybody has read what was there)
+    return row_sum(squares<V>(x), W, warp, lane, row, sums, false) / (float)H + eps * unit * unit;
+}
+
+// 1 / sqrt(mean of squares + eps) of a row held by W warps (x may be multiplied by a power of two: the factor is that of x as it is
+// then)
+template <int V>
+__device__ __forceinline__ float norm_factor(float2 (&x)[V][4], int H, float eps, int W, int warp, int lane, int row, float* sums)
+{
+    float mean = row_sum(squares<V>(x), W, warp, lane, row, sums, true) / (float)H + eps;
     // (all warps of a row have the same sum, and so go the same way)
-    if (!(mean >= 0x1p-100f && mean <= FLT_MAX)) {
-        const float scale = mean < 1.f ? 0x1p100f : 0x1p-72f;
-        if (unit) *unit = scale;
-        ss = 0.f;
+    if (!in_range(mean)) {
+        float2 y[V][4];                                       // (what a call may look into does not stay in registers)
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[v][i] *= scale;
-                ss = fmaf(x[v][i], x[v][i], ss);
-            }
-        ss = warp_sum(ss);
-        if (W > 1) {
-            row_sync(row, W);                                 // (everybody has read what was there)
-            if (lane == 0) sums[warp] = ss;
-            row_sync(row, W);
-            ss = 0.f;
-            for (int i = 0; i < W; ++i) ss += sums[row * W + i];
-        }
-        mean = ss / (float)H + eps * scale * scale;
+            for (int i = 0; i < 4; ++i) y[v][i] = x[v][i];
+        mean = mean_in_units<V>(y, H, eps, mean, W, warp, lane, row, sums);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[v][i] = y[v][i];
     }
     return 1.f / sqrtf(mean);
 }
@@ -74,32 +93,36 @@ __device__ __forceinline__ float activate(float x, int act, float* slope = nullp
         if (slope) *slope = 1.f;
         return x;
     }
-    const float e = expf(-fabsf(x)), r = __fdividef(1.f, 1.f + e), er = e * r;
+    // (2^(-|x| log2 e): off by 4 + 1.5 |x| units of 2^-24, far below the steps of the bf16 values that gates are)
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(x) * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    const float er = e * r;
     if (slope) *slope = er * r;
-    return x >= 0.f ? r : (x < 0.f ? er : x);                 // (a NaN stays one)
+    return x >= 0.f ? r : er;                                 // (both are NaN for a NaN)
 }
 
 // What every row multiplies a column of the block's output with: block_scale, the weight behind the block, a gate per channel.
 template <int V>
-__device__ __forceinline__ void column_factors(const BlockNormArgs& p, int first, int step, float (&c)[V][8])
+__device__ __forceinline__ void column_factors(const BlockNormArgs& p, int first, int step, float2 (&c)[V][4])
 {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int col = first + v * step, n = p.H - col;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c[v][i] = p.block_scale;
+        for (int i = 0; i < 4; ++i) c[v][i] = both(p.block_scale);
         if (p.post) {
-            float w[8];
+            float2 w[4];
             unpack8(p.vec_weight && n >= 8 ? load8<true>(p.post + col, n) : load8<false>(p.post + col, n), w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) c[v][i] *= w[i];
+            for (int i = 0; i < 4; ++i) c[v][i] = mul2(c[v][i], w[i]);
         }
         if (p.gate_form == MOE_GATE_CHANNEL) {
-            float g[8];
+            float2 g[4];
             const bf16* gate = (const bf16*)p.gate + col;
             unpack8(p.vec_weight && n >= 8 ? load8<true>(gate, n) : load8<false>(gate, n), g);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) c[v][i] *= activate(g[i], p.gate_act);
+            for (int i = 0; i < 4; ++i) c[v][i] = mul2(c[v][i], make_float2(activate(g[i].x, p.gate_act), activate(g[i].y, p.gate_act)));
         }
     }
 }
@@ -108,10 +131,10 @@ __device__ __forceinline__ void column_factors(const BlockNormArgs& p, int first
 // of rows and has the next set's loads in flight while it works on this one.
 template <int V, bool ELEMENT, bool VEC>
 __global__ void __launch_bounds__(512)
-block_norm_kernel(const BlockNormArgs p, int W)
+block_norm_kernel(const __grid_constant__ BlockNormArgs p, int W)
 {
-    __shared__ float s_post[2][16], s_pre[2][16];
-    __shared__ uint32_t s_top[2][16];
+    __shared__ float s_post[2][kWarpsOfRow], s_pre[2][kWarpsOfRow];
+    __shared__ uint32_t s_top[2][kWarpsOfRow];
     pdl_wait();
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -134,7 +157,7 @@ block_norm_kernel(const BlockNormArgs p, int W)
     };
     int t = blockIdx.x * rows + row_in_block;
     fetch(t);
-    float c[V][8];
+    float2 c[V][4];
     column_factors<V>(p, first, step, c);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -144,35 +167,40 @@ block_norm_kernel(const BlockNormArgs p, int W)
     int buf = 0;
     for (int set = blockIdx.x; set * rows < p.T; set += gridDim.x, t += gridDim.x * rows, buf ^= 1) {
         const bool live = t < p.T;
-        float x[V][8], r[V][8];
-#pragma unroll
-        for (int v = 0; v < V; ++v) unpack8(yv[v], x[v]);
+        float2 x[V][4];
         uint4 res[V], gate[V];
         float f = p.gate_form == MOE_GATE_TOKEN ? activate(gt, p.gate_act) : 1.f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) { res[v] = rv[v]; if (ELEMENT) gate[v] = gv[v]; }
+        for (int v = 0; v < V; ++v) { unpack8(yv[v], x[v]); res[v] = rv[v]; if (ELEMENT) gate[v] = gv[v]; }
         if (set + gridDim.x < (p.T + rows - 1) / rows) fetch(t + gridDim.x * rows);
         // (two sets of partial sums in turn: a warp may be one set ahead of another, never two)
         if (p.post) f *= norm_factor<V>(x, p.H, p.eps, W, warp, lane, row_in_block, s_post[buf]);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = first + v * step;
-            unpack8(res[v], r[v]);
-            float g[8];
+            float2 r[4], g[4];
+            unpack8(res[v], r);
             if (ELEMENT) unpack8(gate[v], g);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float a = x[v][i] * f * c[v][i];
-                if (ELEMENT) a *= activate(g[i], p.gate_act);
-                x[v][i] = fmaf(p.residual_scale, r[v][i], a);
+            for (int i = 0; i < 4; ++i) {
+                float2 a = mul2(mul2(x[v][i], both(f)), c[v][i]);
+                if (ELEMENT) a = mul2(a, make_float2(activate(g[i].x, p.gate_act), activate(g[i].y, p.gate_act)));
+                x[v][i] = fma2(both(p.residual_scale), r[i], a);
             }
             const uint4 h = pack8(x[v]);                      // (rounded: the stream that is stored)
+            if (VEC) {
+                if (live && col < p.H) *reinterpret_cast<uint4*>(p.h + (size_t)t * p.ldh + col) = h;
+            } else {
+                store8<false>(p.h + (size_t)t * p.ldh + col, live ? p.H - col : 0, x[v]);
+            }
             unpack8(h, x[v]);
-            store8<VEC>(p.h + (size_t)t * p.ldh + col, live ? p.H - col : 0, x[v]);
             // (columns that are not there hold 0 * f, and f need not be finite)
             if (VEC ? col >= p.H : col + 8 > p.H) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) if (col + i >= p.H) x[v][i] = 0.f;
+                for (int i = 0; i < 4; ++i) {
+                    if (col + 2 * i >= p.H) x[v][i].x = 0.f;
+                    if (col + 2 * i + 1 >= p.H) x[v][i].y = 0.f;
+                }
             }
         }
         if (!p.pre) continue;
@@ -181,14 +209,17 @@ block_norm_kernel(const BlockNormArgs p, int W)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = first + v * step, n = live ? p.H - col : 0;
-            float w[8];
+            float2 w[4];
             unpack8(pv[v], w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[v][i] = x[v][i] * inv * w[i];
+            for (int i = 0; i < 4; ++i) x[v][i] = mul2(mul2(x[v][i], both(inv)), w[i]);
             if (p.out) store8<VEC>(p.out + (size_t)t * p.ldo + col, n, x[v]);
             if (p.q) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) if (VEC ? n > 0 : i < n) top = max(top, magnitude(x[v][i]));
+                for (int i = 0; i < 4; ++i) {
+                    if (VEC ? n > 0 : 2 * i < n) top = max(top, magnitude(x[v][i].x));
+                    if (VEC ? n > 0 : 2 * i + 1 < n) top = max(top, magnitude(x[v][i].y));
+                }
             }
         }
         if (!p.q) continue;
@@ -204,7 +235,7 @@ block_norm_kernel(const BlockNormArgs p, int W)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = first + v * step, n = live ? p.H - col : 0;
-            if (n > 0) store_i8<VEC>(p.q + (size_t)t * p.ldq + col, n, p.vec_q, x[v], s);
+            if (n > 0) store_i8<VEC>(p.q + (size_t)t * p.ldq + col, n, p.vec_q, reinterpret_cast<const float*>(x[v]), s);
         }
     }
 }
@@ -263,25 +294,24 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int W, int wr, int lane,
     for (int n = 0; n < N; ++n) v[n] = __shfl_sync(kFull, x, 8 * n);
 }
 
-constexpr int kSumsOfRow = 2 * 2 * 4 * 16;      // (two in turn) x (two steps) x values x warps
-
-__device__ __forceinline__ bool in_range(float mean) { return mean >= 0x1p-100f && mean <= FLT_MAX; }
+constexpr int kSumsOfRow = 2 * 2 * 4 * kWarpsOfRow;      // (two in turn) x (two steps) x values x warps
 
 // A row whose squares leave the range of fp32: multiplied in place by a power of two that brings them inside; sums: those of its
 // squares, and of its products with d.
 template <int V>
-__device__ __noinline__ float rescale(float (&x)[V][8], const float (&d)[V][8], float mean, float (&sums)[2], int W, int wr, int lane, int row, float* s)
+__device__ __noinline__ float rescale(float2 (&x)[V][4], const float2 (&d)[V][4], float mean, float (&sums)[2], int W, int wr, int lane, int row, float* s)
 {
     const float unit = mean < 1.f ? 0x1p100f : 0x1p-72f;
-    sums[0] = sums[1] = 0.f;
+    float2 dot = both(0.f);
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[v][i] *= unit;
-            sums[0] = fmaf(x[v][i], x[v][i], sums[0]);
-            sums[1] = fmaf(x[v][i], d[v][i], sums[1]);
+        for (int i = 0; i < 4; ++i) {
+            x[v][i] = mul2(x[v][i], both(unit));
+            dot = fma2(x[v][i], d[v][i], dot);
         }
+    sums[0] = squares<V>(x);
+    sums[1] = dot.x + dot.y;
     if (W > 1) row_sync(row, W);                              // (everybody has read what was there)
     row_sums<2>(sums, W, wr, lane, s, false, row);
     return unit;
@@ -291,7 +321,7 @@ __device__ __noinline__ float rescale(float (&x)[V][8], const float (&d)[V][8], 
 // in shared memory that no other lane touches (vectors of 16 bytes, neighbouring lanes side by side).
 template <int V, int N>
 struct ColumnSums {
-    float r[V == 1 ? N : 1][8];
+    float2 r[V == 1 ? N : 1][4];
     float4* s;
     __device__ __forceinline__ ColumnSums()
     {
@@ -301,36 +331,47 @@ struct ColumnSums {
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) r[n][i] = 0.f;
+                for (int i = 0; i < 4; ++i) r[n][i] = both(0.f);
         } else {
 #pragma unroll
             for (int j = 0; j < N * V * 2; ++j) s[j * blockDim.x] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
-    __device__ __forceinline__ void get(int n, int v, float (&f)[8]) const
+    __device__ __forceinline__ void get(int n, int v, float2 (&f)[4]) const
     {
         if (V == 1) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = r[n][i];
+            for (int i = 0; i < 4; ++i) f[i] = r[n][i];
         } else {
             const float4 a = s[((n * V + v) * 2) * blockDim.x], b = s[((n * V + v) * 2 + 1) * blockDim.x];
-            f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+            f[0] = make_float2(a.x, a.y); f[1] = make_float2(a.z, a.w); f[2] = make_float2(b.x, b.y); f[3] = make_float2(b.z, b.w);
         }
     }
-    // column i: + x[i] y[i]
-    __device__ __forceinline__ void add(int n, int v, const float (&x)[8], const float (&y)[8])
+    __device__ __forceinline__ void set(int n, int v, const float2 (&f)[4])
     {
         if (V == 1) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[n][i] = fmaf(x[i], y[i], r[n][i]);
+            for (int i = 0; i < 4; ++i) r[n][i] = f[i];
         } else {
-            float f[8];
-            get(n, v, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = fmaf(x[i], y[i], f[i]);
-            s[((n * V + v) * 2) * blockDim.x] = make_float4(f[0], f[1], f[2], f[3]);
-            s[((n * V + v) * 2 + 1) * blockDim.x] = make_float4(f[4], f[5], f[6], f[7]);
+            s[((n * V + v) * 2) * blockDim.x] = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+            s[((n * V + v) * 2 + 1) * blockDim.x] = make_float4(f[2].x, f[2].y, f[3].x, f[3].y);
         }
+    }
+    __device__ __forceinline__ void add(int n, int v, const float2 (&x)[4], const float2 (&y)[4])      // + x y
+    {
+        float2 f[4];
+        get(n, v, f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = fma2(x[i], y[i], f[i]);
+        set(n, v, f);
+    }
+    __device__ __forceinline__ void add(int n, int v, const float2 (&x)[4])
+    {
+        float2 f[4];
+        get(n, v, f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = add2(f[i], x[i]);
+        set(n, v, f);
     }
 };
 // (bytes of shared memory)
@@ -342,7 +383,7 @@ size_t column_sums_bytes(int V, int N, int threads) { return V == 1 ? 0 : (size_
 // are not there hold zeros, and what a row without finite sums makes of those is never stored.
 template <int V, int GATE, bool VEC>
 __global__ void __launch_bounds__(512)
-block_norm_grad_kernel(const BlockNormArgs p, int W)
+block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
 {
     __shared__ __align__(8) float s_sums[4][kSumsOfRow];      // of a block's rows (four if a row is one warp, which needs none)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -378,17 +419,25 @@ block_norm_grad_kernel(const BlockNormArgs p, int W)
         if (!w) return make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
         return p.vec_weight && n >= 8 ? load8<true>(w + col, n) : load8<false>(w + col, n);
     };
-    constexpr bool kKeep = V == 1;                            // the weights stay in registers
-    uint4 pre_w[V], post_w[V], gate_w[V];
+    // The weights: pre, and post times block_scale, which the gradients of the block's output have in common.  They stay in registers
+    // where a lane has one vector.
+    constexpr bool kKeep = V == 1;
+    float2 pre_w[V][4], post_w[V][4], gate_w[V][4];
+    auto load_pre = [&](int v, float2 (&w)[4]) { unpack8(column(p.pre, v), w); };
+    auto load_post = [&](int v, float2 (&w)[4]) {
+        unpack8(column(p.post, v), w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = mul2(w[i], both(p.block_scale));
+    };
     if (kKeep) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            pre_w[v] = column(p.pre, v);
-            post_w[v] = column(p.post, v);
-            if (GATE == MOE_GATE_CHANNEL) gate_w[v] = column((const bf16*)p.gate, v);
+            load_pre(v, pre_w[v]);
+            load_post(v, post_w[v]);
+            if (GATE == MOE_GATE_CHANNEL) unpack8(column((const bf16*)p.gate, v), gate_w[v]);
         }
     }
-    ColumnSums<V, GATE == MOE_GATE_CHANNEL ? 3 : 2> columns;  // of d_pre, d_post, d_gate
+    ColumnSums<V, GATE == MOE_GATE_CHANNEL ? 3 : 2> columns;  // of d_pre, d_post (without block_scale), d_gate
     const float over = 1.f / (float)p.H;
     int t = blockIdx.x * rows + row_in_block;
     int buf = 0;
@@ -397,41 +446,45 @@ block_norm_grad_kernel(const BlockNormArgs p, int W)
         const bool live = t < p.T;
         float* const s1 = s_sums[row_in_block] + buf * 128;
         float* const s2 = s1 + 64;
-        float y[V][8], d[V][8], h[V][8];
+        float2 y[V][4], d[V][4], h[V][4];
         uint4 gate_now[V], dh_now[V];
         const float token_gate = gt;
-        float sums[3] = {0.f, 0.f, 0.f};
+        float2 hh = both(0.f), hd = both(0.f), yy = both(0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            float w[8];
+            if (!kKeep) load_pre(v, pre_w[v]);
             unpack8(hv[v], h[v]);
             unpack8(ov[v], d[v]);
             unpack8(yv[v], y[v]);
-            unpack8(kKeep ? pre_w[v] : column(p.pre, v), w);
             dh_now[v] = dv[v];
             if (GATE == MOE_GATE_ELEMENT) gate_now[v] = gv[v];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                sums[0] = fmaf(h[v][i], h[v][i], sums[0]);
-                sums[1] = fmaf(h[v][i], d[v][i] * w[i], sums[1]);
-                sums[2] = fmaf(y[v][i], y[v][i], sums[2]);
+            for (int i = 0; i < 4; ++i) {
+                hh = fma2(h[v][i], h[v][i], hh);
+                hd = fma2(h[v][i], mul2(d[v][i], pre_w[v][i]), hd);
+                yy = fma2(y[v][i], y[v][i], yy);
             }
         }
+        float sums[3] = {hh.x + hh.y, hd.x + hd.y, yy.x + yy.y};
         if (set + gridDim.x < (p.T + rows - 1) / rows) fetch(t + gridDim.x * rows);
         row_sums<3>(sums, W, wr, lane, s1);
         if (p.d_out) {
             // d_out n for the weight's gradient, then what goes on to h
             float mean = fmaf(sums[0], over, p.eps), dot = sums[1], unit = 1.f;
             if (!in_range(mean)) {
-                float more[2], dw[V][8];
+                float more[2];
+                float2 dw[V][4], x[V][4];                     // (what a call may look into does not stay in registers)
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    float w[8];
-                    unpack8(kKeep ? pre_w[v] : column(p.pre, v), w);
+                    if (!kKeep) load_pre(v, pre_w[v]);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) dw[v][i] = d[v][i] * w[i];
+                    for (int i = 0; i < 4; ++i) { dw[v][i] = mul2(d[v][i], pre_w[v][i]); x[v][i] = h[v][i]; }
                 }
-                unit = rescale<V>(h, dw, mean, more, W, wr, lane, row_in_block, s1);
+                unit = rescale<V>(x, dw, mean, more, W, wr, lane, row_in_block, s1);
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) h[v][i] = x[v][i];
                 mean = fmaf(more[0], over, p.eps * unit * unit);
                 dot = more[1];
             }
@@ -439,104 +492,116 @@ block_norm_grad_kernel(const BlockNormArgs p, int W)
             dot *= inv * over;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                float w[8];
-                unpack8(kKeep ? pre_w[v] : column(p.pre, v), w);
+                if (!kKeep) load_pre(v, pre_w[v]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[v][i] *= inv;   // n
+                for (int i = 0; i < 4; ++i) h[v][i] = mul2(h[v][i], both(inv));      // n
                 columns.add(0, v, d[v], h[v]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[v][i] = back * fmaf(-h[v][i], dot, d[v][i] * w[i]);
+                for (int i = 0; i < 4; ++i) d[v][i] = mul2(fma2(h[v][i], both(-dot), mul2(d[v][i], pre_w[v][i])), both(back));
             }
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int col = first + v * step, n = live ? p.H - col : 0;
-            float u[8];
+            const int col = first + v * step;
+            float2 u[4];
             unpack8(dh_now[v], u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                d[v][i] += u[i];
-                u[i] = p.residual_scale * d[v][i];
-                d[v][i] *= p.block_scale;
+            for (int i = 0; i < 4; ++i) {
+                d[v][i] = add2(d[v][i], u[i]);
+                u[i] = mul2(d[v][i], both(p.residual_scale));
             }
-            if (p.d_residual) store8<VEC>(p.d_residual + (size_t)t * p.ldr_grad + col, n, u);
+            if (p.d_residual) store8<VEC>(p.d_residual + (size_t)t * p.ldr_grad + col, live ? p.H - col : 0, u);
         }
         float inv = 1.f, unit = 1.f;
         if (p.post) {
             float mean = fmaf(sums[2], over, p.eps);
             if (!in_range(mean)) {
                 float more[2];
-                unit = rescale<V>(y, y, mean, more, W, wr, lane, row_in_block, s1);
+                float2 x[V][4];
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[v][i] = y[v][i];
+                unit = rescale<V>(x, x, mean, more, W, wr, lane, row_in_block, s1);
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[v][i] = x[v][i];
                 mean = fmaf(more[0], over, p.eps * unit * unit);
             }
             inv = live ? 1.f / sqrtf(mean) : 0.f;
         }
         float row_slope = 1.f;
         const float row_gate = GATE == MOE_GATE_TOKEN ? activate(token_gate, p.gate_act, &row_slope) : 1.f;
-        float dot[1] = {0.f};                                 // without the token's gate, whose gradient it is too
+        float2 dd = both(0.f);                                // without the token's gate, whose gradient it is too
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = first + v * step;
-            float w[8], g[8], dg[8], bg[8];
-            unpack8(kKeep ? post_w[v] : column(p.post, v), w);
-            if (GATE == MOE_GATE_CHANNEL) unpack8(kKeep ? gate_w[v] : column((const bf16*)p.gate, v), g);
+            float2 g[4], dg[4], b[4];
+            if (!kKeep) load_post(v, post_w[v]);
+            if (GATE == MOE_GATE_CHANNEL) {
+                if (!kKeep) unpack8(column((const bf16*)p.gate, v), gate_w[v]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) g[i] = gate_w[v][i];
+            }
             if (GATE == MOE_GATE_ELEMENT) unpack8(gate_now[v], g);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float m = y[v][i] * inv;
-                y[v][i] = m;
-                float b = d[v][i];
+            for (int i = 0; i < 4; ++i) {
+                if (p.post) y[v][i] = mul2(y[v][i], both(inv));              // m
+                b[i] = d[v][i];
+                d[v][i] = mul2(d[v][i], post_w[v][i]);
                 if (GATE == MOE_GATE_CHANNEL || GATE == MOE_GATE_ELEMENT) {
-                    float slope;
-                    const float value = activate(g[i], p.gate_act, &slope);
-                    dg[i] = b * m * w[i] * slope;
-                    b *= value;
+                    float2 value, slope;
+                    value.x = activate(g[i].x, p.gate_act, &slope.x);
+                    value.y = activate(g[i].y, p.gate_act, &slope.y);
+                    dg[i] = mul2(mul2(d[v][i], y[v][i]), slope);
+                    b[i] = mul2(b[i], value);
+                    d[v][i] = mul2(d[v][i], value);
                 }
-                bg[i] = b * row_gate;
-                d[v][i] = b * w[i];
-                dot[0] = fmaf(d[v][i], m, dot[0]);
+                if (GATE == MOE_GATE_TOKEN) b[i] = mul2(b[i], both(row_gate));
+                dd = fma2(d[v][i], y[v][i], dd);
             }
-            columns.add(1, v, bg, y[v]);
-            if (GATE == MOE_GATE_CHANNEL) {
-                constexpr float one[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-                columns.add(2, v, dg, one);
-            }
+            columns.add(1, v, b, y[v]);
+            if (GATE == MOE_GATE_CHANNEL) columns.add(2, v, dg);
             if (GATE == MOE_GATE_ELEMENT && p.d_gate) store8<VEC>((bf16*)p.d_gate + (size_t)t * p.ldg_grad + col, live ? p.H - col : 0, dg);
         }
+        float dot[1] = {dd.x + dd.y};
         if (p.post || GATE == MOE_GATE_TOKEN) row_sums<1>(dot, W, wr, lane, s2);
         if (GATE == MOE_GATE_TOKEN && p.d_gate && live && wr == 0 && lane == 0) ((float*)p.d_gate)[t] = dot[0] * row_slope;
         if (p.d_y) {
             const float mean = p.post ? dot[0] * over : 0.f, back = inv * unit * row_gate;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                float u[8];
+                float2 u[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) u[i] = back * fmaf(-y[v][i], mean, d[v][i]);
+                for (int i = 0; i < 4; ++i) u[i] = mul2(fma2(y[v][i], both(-mean), d[v][i]), both(back));
                 store8<VEC>(p.d_y + (size_t)t * p.ldy_grad + first + v * step, live ? p.H - first - v * step : 0, u);
             }
         }
     }
     if (!p.sums) return;
     const size_t part = (size_t)blockIdx.x * rows + row_in_block, all = (size_t)p.parts * p.H;
-    auto store = [&](int n) {
+    auto store = [&](int n, float scale) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = first + v * step;
             float* const dst = p.sums + n * all + part * p.H + col;
-            float f[8];
+            float2 f[4];
             columns.get(n, v, f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = mul2(f[i], both(scale));
             if (VEC && col < p.H) {
-                reinterpret_cast<float4*>(dst)[0] = make_float4(f[0], f[1], f[2], f[3]);
-                reinterpret_cast<float4*>(dst)[1] = make_float4(f[4], f[5], f[6], f[7]);
+                reinterpret_cast<float4*>(dst)[0] = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+                reinterpret_cast<float4*>(dst)[1] = make_float4(f[2].x, f[2].y, f[3].x, f[3].y);
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) if (col + i < p.H) dst[i] = f[i];
+                for (int i = 0; i < 8; ++i) if (col + i < p.H) dst[i] = i & 1 ? f[i / 2].y : f[i / 2].x;
             }
         }
     };
-    if (p.d_pre) store(0);
-    if (p.d_post) store(1);
-    if (GATE == MOE_GATE_CHANNEL && p.d_gate) store(2);
+    if (p.d_pre) store(0, 1.f);
+    if (p.d_post) store(1, p.block_scale);
+    if (GATE == MOE_GATE_CHANNEL && p.d_gate) store(2, 1.f);
 }
 
 // The blocks' sums, added up in a fixed order: 32 columns a block, 32 threads a column.  blockIdx.y: which of the three.
