@@ -26,17 +26,33 @@ constexpr int kWarpsOfRow = 16;
 
 __device__ __forceinline__ bool in_range(float mean) { return mean >= 0x1p-100f && mean <= FLT_MAX; }
 
-// sum over a row's W warps; a barrier of the block, or of the row's warps alone
-__device__ __forceinline__ float row_sum(float ss, int W, int warp, int lane, int row, float* sums, bool block)
+// Sum over a row's W warps; a barrier of the block, or of the row's warps alone.  `sums`: the row's 16 floats, zero beyond W.
+__device__ __forceinline__ float row_sum(float ss, int W, int wr, int lane, int row, float* sums, bool block)
 {
     ss = warp_sum(ss);
     if (W > 1) {
-        if (lane == 0) sums[warp] = ss;
+        if (lane == 0) sums[wr] = ss;
         if (block) __syncthreads(); else row_sync(row, W);
-        ss = 0.f;
-        for (int i = 0; i < W; ++i) ss += sums[row * W + i];
+        const float4* s = reinterpret_cast<const float4*>(sums);
+        float4 q = s[0];
+        ss = (q.x + q.y) + (q.z + q.w);
+        if (W > 4) {
+            q = s[1];
+            ss += (q.x + q.y) + (q.z + q.w);
+            if (W > 8) {
+                q = s[2];
+                const float4 r = s[3];
+                ss += ((q.x + q.y) + (q.z + q.w)) + ((r.x + r.y) + (r.z + r.w));
+            }
+        }
     }
     return ss;
+}
+__device__ __forceinline__ float inverse_root(float x)       // (off by 2^-22.9 of itself at most; x is 0, at least 2^-100, infinite or NaN)
+{
+    float y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 template <int V>
@@ -53,7 +69,7 @@ __device__ __forceinline__ float squares(const float2 (&x)[V][4])
 // A row whose mean of squares leaves the range of fp32, or is below it with no eps that counts beside it: multiplied (in place) by a
 // power of two that is exact and brings it inside; returns the mean of the multiplied row, with its eps.
 template <int V>
-__device__ __noinline__ float mean_in_units(float2 (&x)[V][4], int H, float eps, float mean, int W, int warp, int lane, int row, float* sums)
+__device__ __noinline__ float mean_in_units(float2 (&x)[V][4], float over, float eps, float mean, int W, int wr, int lane, int row, float* sums)
 {
     const float unit = mean < 1.f ? 0x1p100f : 0x1p-72f;
 #pragma unroll
@@ -61,15 +77,15 @@ __device__ __noinline__ float mean_in_units(float2 (&x)[V][4], int H, float eps,
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[v][i] = mul2(x[v][i], both(unit));
     if (W > 1) row_sync(row, W);                              // (everybody has read what was there)
-    return row_sum(squares<V>(x), W, warp, lane, row, sums, false) / (float)H + eps * unit * unit;
+    return fmaf(row_sum(squares<V>(x), W, wr, lane, row, sums, false), over, eps * unit * unit);
 }
 
 // 1 / sqrt(mean of squares + eps) of a row held by W warps (x may be multiplied by a power of two: the factor is that of x as it is
 // then)
 template <int V>
-__device__ __forceinline__ float norm_factor(float2 (&x)[V][4], int H, float eps, int W, int warp, int lane, int row, float* sums)
+__device__ __forceinline__ float norm_factor(float2 (&x)[V][4], float over, float eps, int W, int wr, int lane, int row, float* sums)
 {
-    float mean = row_sum(squares<V>(x), W, warp, lane, row, sums, true) / (float)H + eps;
+    float mean = fmaf(row_sum(squares<V>(x), W, wr, lane, row, sums, true), over, eps);
     // (all warps of a row have the same sum, and so go the same way)
     if (!in_range(mean)) {
         float2 y[V][4];                                       // (what a call may look into does not stay in registers)
@@ -77,13 +93,13 @@ __device__ __forceinline__ float norm_factor(float2 (&x)[V][4], int H, float eps
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[v][i] = x[v][i];
-        mean = mean_in_units<V>(y, H, eps, mean, W, warp, lane, row, sums);
+        mean = mean_in_units<V>(y, over, eps, mean, W, wr, lane, row, sums);
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[v][i] = y[v][i];
     }
-    return 1.f / sqrtf(mean);
+    return inverse_root(mean);
 }
 
 // The gate's value; *slope: its derivative (1 - s by way of exp(-|x|), so that neither end cancels).
@@ -101,6 +117,92 @@ __device__ __forceinline__ float activate(float x, int act, float* slope = nullp
     if (slope) *slope = er * r;
     return x >= 0.f ? r : er;                                 // (both are NaN for a NaN)
 }
+
+// A row's address: 32-bit factors, so that it is one instruction.
+__device__ __forceinline__ const bf16* at(const bf16* p, int t, uint32_t ld_bytes) { return reinterpret_cast<const bf16*>(reinterpret_cast<const char*>(p) + (uint64_t)(uint32_t)t * ld_bytes); }
+__device__ __forceinline__ bf16* at(bf16* p, int t, uint32_t ld_bytes) { return reinterpret_cast<bf16*>(reinterpret_cast<char*>(p) + (uint64_t)(uint32_t)t * ld_bytes); }
+
+// The rows of up to NA matrices that a block works through, each lane's own vectors of them, on their way ahead of time: D rows in
+// shared memory that no other lane touches (asynchronous copies: no registers, and nothing to wait for but the lane's own), or, where
+// rows are not on 16-byte boundaries or D is 0, one row in registers.
+template <int NA, int V, bool VEC, int D>
+struct RowFeed {
+    static constexpr bool kShared = VEC && D > 0;
+    static constexpr int kA = kShared ? 1 : NA, kV = kShared ? 1 : V;
+    const bf16* src[NA];             // this lane's first column of row 0, or null: zeros
+    uint32_t ld[NA];
+    int n, step, T, t, t_step;       // columns from the lane's first on; the next row to ask for
+    uint4* s;
+    int stage;
+    uint4 cur[kA][kV], next[kA][kV];
+
+    __device__ __forceinline__ void ask(int to)
+    {
+        if (t < T) {
+#pragma unroll
+            for (int a = 0; a < NA; ++a) {
+                const bf16* const row = at(src[a], t, ld[a]);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    if (kShared) {
+                        uint4* const dst = s + ((to * NA + a) * V + v) * blockDim.x;
+                        if (src[a] && n > v * step)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(row + v * step) : "memory");
+                    } else {
+                        next[kShared ? 0 : a][kShared ? 0 : v] = load8<VEC>(row + v * step, src[a] ? n - v * step : 0);
+                    }
+                }
+            }
+        } else if (!kShared) {
+#pragma unroll
+            for (int a = 0; a < NA; ++a)
+#pragma unroll
+                for (int v = 0; v < V; ++v) next[kShared ? 0 : a][kShared ? 0 : v] = make_uint4(0, 0, 0, 0);
+        }
+        t += t_step;
+        if (kShared) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // src and ld are set; `first_t`: the block's first row for this lane
+    __device__ __forceinline__ void start(uint4* shared, int columns, int column_step, int rows, int first_t, int row_step)
+    {
+        n = columns; step = column_step; T = rows; t = first_t; t_step = row_step; stage = 0;
+        s = shared + threadIdx.x;
+        if (kShared) {
+            // (what is never copied, columns and matrices that are not there and rows behind the last, reads as zero or is not stored)
+#pragma unroll
+            for (int i = 0; i < D * NA * V; ++i) s[i * blockDim.x] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int d = 0; d < D; ++d) ask(d);
+        } else {
+            ask(0);
+        }
+    }
+    __device__ __forceinline__ void begin()                   // the next row is there
+    {
+        if (kShared) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kShared ? D - 1 : 0) : "memory");
+        } else {
+#pragma unroll
+            for (int a = 0; a < NA; ++a)
+#pragma unroll
+                for (int v = 0; v < V; ++v) cur[kShared ? 0 : a][kShared ? 0 : v] = next[kShared ? 0 : a][kShared ? 0 : v];
+            ask(0);
+        }
+    }
+    __device__ __forceinline__ uint4 get(int a, int v) const
+    {
+        return kShared ? s[((stage * NA + a) * V + v) * blockDim.x] : cur[kShared ? 0 : a][kShared ? 0 : v];
+    }
+    __device__ __forceinline__ void end()                     // nothing of this row is read any more
+    {
+        if (kShared) {
+            ask(stage);
+            if (++stage == D) stage = 0;
+        }
+    }
+};
+// (bytes of shared memory)
+size_t feed_bytes(int NA, int V, int D, int threads) { return (size_t)NA * V * D * 16 * threads; }
 
 // What every row multiplies a column of the block's output with: block_scale, the weight behind the block, a gate per channel.
 template <int V>
@@ -127,36 +229,38 @@ __device__ __forceinline__ void column_factors(const BlockNormArgs& p, int first
     }
 }
 
+constexpr int kForwardRows = 2;          // rows on their way (3 and 4 are no faster)
+
 // W warps per row, V vectors of 8 elements per lane, blockDim / (32 W) rows at a time; a block goes on with every gridDim-th set
-// of rows and has the next set's loads in flight while it works on this one.
+// of rows and has the next sets' loads in flight while it works on this one.
 template <int V, bool ELEMENT, bool VEC>
 __global__ void __launch_bounds__(512)
 block_norm_kernel(const __grid_constant__ BlockNormArgs p, int W)
 {
-    __shared__ float s_post[2][kWarpsOfRow], s_pre[2][kWarpsOfRow];
-    __shared__ uint32_t s_top[2][kWarpsOfRow];
-    pdl_wait();
-    pdl_launch_dependents();
+    __shared__ __align__(16) float s_sums[2][2][2][kWarpsOfRow];          // [in turn][row of the block][norm]
+    __shared__ uint32_t s_top[2][2][kWarpsOfRow];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int row_in_block = warp / W, wr = warp - row_in_block * W;
     const int rows = blockDim.x / (32 * W);
     const int first = (wr * 32 + lane) * 8, step = W * 256;               // this lane's columns: first + v * step ...
-    uint4 yv[V], rv[V], gv[V], pv[V];
-    float gt = 1.f;
-    auto fetch = [&](int t) {
-        const int H = t < p.T ? p.H : 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) yv[v] = load8<VEC>(p.y + (size_t)t * p.ldy + first + v * step, H - first - v * step);
-#pragma unroll
-        for (int v = 0; v < V; ++v) rv[v] = load8<VEC>(p.residual + (size_t)t * p.ldr + first + v * step, H - first - v * step);
-        if (ELEMENT) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) gv[v] = load8<VEC>((const bf16*)p.gate + (size_t)t * p.ldg + first + v * step, H - first - v * step);
-        }
-        if (p.gate_form == MOE_GATE_TOKEN && t < p.T) gt = ((const float*)p.gate)[t];
-    };
+    const int sets = (p.T + rows - 1) / rows;
+    for (int i = threadIdx.x; i < 8 * kWarpsOfRow; i += blockDim.x) (&s_sums[0][0][0][0])[i] = 0.f;
+    __syncthreads();
+    pdl_wait();
+    pdl_launch_dependents();
     int t = blockIdx.x * rows + row_in_block;
-    fetch(t);
+    const int t_step = gridDim.x * rows;
+    extern __shared__ __align__(16) uint4 s_feed[];
+    RowFeed<ELEMENT ? 3 : 2, V, VEC, kForwardRows> feed;
+    feed.src[0] = p.y + first; feed.ld[0] = (uint32_t)p.ldy * 2;
+    feed.src[1] = p.residual + first; feed.ld[1] = (uint32_t)p.ldr * 2;
+    if (ELEMENT) { feed.src[ELEMENT ? 2 : 0] = (const bf16*)p.gate + first; feed.ld[ELEMENT ? 2 : 0] = (uint32_t)p.ldg * 2; }
+    feed.start(s_feed, p.H - first, step, p.T, t, t_step);
+    const bool token = p.gate_form == MOE_GATE_TOKEN;
+    float gt = token && t < p.T ? ((const float*)p.gate)[t] : 1.f;
+    bf16* const h = p.h + first;
+    bf16* const o = p.out + first;
+    uint4 pv[V];
     float2 c[V][4];
     column_factors<V>(p, first, step, c);
 #pragma unroll
@@ -164,87 +268,96 @@ block_norm_kernel(const __grid_constant__ BlockNormArgs p, int W)
         const int col = first + v * step, n = p.pre ? p.H - col : 0;
         pv[v] = p.vec_weight && n >= 8 ? load8<true>(p.pre + col, n) : load8<false>(p.pre + col, n);
     }
+    const float over = 1.f / (float)p.H;
     int buf = 0;
-    for (int set = blockIdx.x; set * rows < p.T; set += gridDim.x, t += gridDim.x * rows, buf ^= 1) {
-        const bool live = t < p.T;
+    for (int set = blockIdx.x; set < sets; set += gridDim.x, t += t_step, buf ^= 1) {
+        // Columns that are not there hold zeros; in a row whose factors are not finite they become NaN, as all of that row does.
+        const int n = t < p.T ? p.H - first : 0;
         float2 x[V][4];
-        uint4 res[V], gate[V];
-        float f = p.gate_form == MOE_GATE_TOKEN ? activate(gt, p.gate_act) : 1.f;
+        float f = 1.f;
+        if (token) {
+            f = activate(gt, p.gate_act);
+            if (t + t_step < p.T) gt = ((const float*)p.gate)[t + t_step];
+        }
+        feed.begin();
 #pragma unroll
-        for (int v = 0; v < V; ++v) { unpack8(yv[v], x[v]); res[v] = rv[v]; if (ELEMENT) gate[v] = gv[v]; }
-        if (set + gridDim.x < (p.T + rows - 1) / rows) fetch(t + gridDim.x * rows);
+        for (int v = 0; v < V; ++v) unpack8(feed.get(0, v), x[v]);
         // (two sets of partial sums in turn: a warp may be one set ahead of another, never two)
-        if (p.post) f *= norm_factor<V>(x, p.H, p.eps, W, warp, lane, row_in_block, s_post[buf]);
+        if (p.post) f *= norm_factor<V>(x, over, p.eps, W, wr, lane, row_in_block, s_sums[buf][row_in_block & 1][0]);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int col = first + v * step;
-            float2 r[4], g[4];
-            unpack8(res[v], r);
-            if (ELEMENT) unpack8(gate[v], g);
+            float2 q[4], e[4];
+            unpack8(feed.get(1, v), q);
+            if (ELEMENT) unpack8(feed.get(ELEMENT ? 2 : 0, v), e);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float2 a = mul2(mul2(x[v][i], both(f)), c[v][i]);
-                if (ELEMENT) a = mul2(a, make_float2(activate(g[i].x, p.gate_act), activate(g[i].y, p.gate_act)));
-                x[v][i] = fma2(both(p.residual_scale), r[i], a);
+                if (ELEMENT) a = mul2(a, make_float2(activate(e[i].x, p.gate_act), activate(e[i].y, p.gate_act)));
+                x[v][i] = fma2(both(p.residual_scale), q[i], a);
             }
-            const uint4 h = pack8(x[v]);                      // (rounded: the stream that is stored)
-            if (VEC) {
-                if (live && col < p.H) *reinterpret_cast<uint4*>(p.h + (size_t)t * p.ldh + col) = h;
-            } else {
-                store8<false>(p.h + (size_t)t * p.ldh + col, live ? p.H - col : 0, x[v]);
-            }
-            unpack8(h, x[v]);
-            // (columns that are not there hold 0 * f, and f need not be finite)
-            if (VEC ? col >= p.H : col + 8 > p.H) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (col + 2 * i >= p.H) x[v][i].x = 0.f;
-                    if (col + 2 * i + 1 >= p.H) x[v][i].y = 0.f;
-                }
-            }
+            const uint4 stored = pack8(x[v]);                 // (rounded: the stream)
+            bf16* const dst = at(h, t, (uint32_t)p.ldh * 2) + v * step;
+            if (!VEC) store8<false>(dst, n - v * step, x[v]);
+            else if (n > v * step) *reinterpret_cast<uint4*>(dst) = stored;
+            unpack8(stored, x[v]);
         }
+        feed.end();
         if (!p.pre) continue;
-        const float inv = norm_factor<V>(x, p.H, p.eps, W, warp, lane, row_in_block, s_pre[buf]);
+        const float inv = norm_factor<V>(x, over, p.eps, W, wr, lane, row_in_block, s_sums[buf][row_in_block & 1][1]);
         uint32_t top = 0;                                     // largest |v| of the row
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int col = first + v * step, n = live ? p.H - col : 0;
             float2 w[4];
             unpack8(pv[v], w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[v][i] = mul2(mul2(x[v][i], both(inv)), w[i]);
-            if (p.out) store8<VEC>(p.out + (size_t)t * p.ldo + col, n, x[v]);
+            if (p.out) store8<VEC>(at(o, t, (uint32_t)p.ldo * 2) + v * step, n - v * step, x[v]);
             if (p.q) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (VEC ? n > 0 : 2 * i < n) top = max(top, magnitude(x[v][i].x));
-                    if (VEC ? n > 0 : 2 * i + 1 < n) top = max(top, magnitude(x[v][i].y));
-                }
+                for (int i = 0; i < 4; ++i) top = max(top, max(magnitude(x[v][i].x), magnitude(x[v][i].y)));
             }
         }
         if (!p.q) continue;
         top = __reduce_max_sync(kFull, top);
         if (W > 1) {
-            if (lane == 0) s_top[buf][warp] = top;
+            if (lane == 0) s_top[buf][row_in_block & 1][wr] = top;
             __syncthreads();
             top = 0;
-            for (int i = 0; i < W; ++i) top = max(top, s_top[buf][row_in_block * W + i]);
+            for (int i = 0; i < W; ++i) top = max(top, s_top[buf][row_in_block & 1][i]);
         }
         const RowScale s = row_scale(__uint_as_float(top) / 127.f);
-        if (live && wr == 0 && lane == 0) p.q_scale[t] = s.scale;
+        if (n > 0 && wr == 0 && lane == 0) p.q_scale[t] = s.scale;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int col = first + v * step, n = live ? p.H - col : 0;
-            if (n > 0) store_i8<VEC>(p.q + (size_t)t * p.ldq + col, n, p.vec_q, reinterpret_cast<const float*>(x[v]), s);
-        }
+        for (int v = 0; v < V; ++v)
+            if (n > v * step) store_i8<VEC>(p.q + (size_t)t * p.ldq + first + v * step, n - v * step, p.vec_q, reinterpret_cast<const float*>(x[v]), s);
     }
+}
+
+// the opt-in to large dynamic shared memory is a per-device attribute of a kernel
+template <typename K>
+cudaError_t allow_smem(K kern, bool (&done)[kMaxDevices])
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    if (done[dev]) return cudaSuccess;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+    if (e == cudaSuccess) done[dev] = true;
+    return e;
 }
 
 template <int V, bool ELEMENT, bool VEC>
 cudaError_t launch_one(const BlockNormArgs& p, int W, int rows, cudaStream_t st)
 {
     const int sets = (p.T + rows - 1) / rows, most = 148 * ((V == 1 ? 32 : 16) / (W * rows));
-    return launch_pdl(block_norm_kernel<V, ELEMENT, VEC>, dim3(sets < most ? sets : most), dim3(32 * W * rows), 0, st, p, W);
+    static bool ok[kMaxDevices] = {false};
+    const size_t smem = VEC ? feed_bytes(ELEMENT ? 3 : 2, V, kForwardRows, 32 * W * rows) : 0;
+    if (smem > 40 * 1024) {
+        const cudaError_t e = allow_smem(block_norm_kernel<V, ELEMENT, VEC>, ok);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_pdl(block_norm_kernel<V, ELEMENT, VEC>, dim3(sets < most ? sets : most), dim3(32 * W * rows), smem, st, p, W);
 }
 template <int V>
 cudaError_t launch_v(const BlockNormArgs& p, int W, int rows, cudaStream_t st)
@@ -317,19 +430,19 @@ __device__ __noinline__ float rescale(float2 (&x)[V][4], const float2 (&d)[V][4]
     return unit;
 }
 
-// A lane's sums over the block's rows, V vectors of eight columns of each of N gradients: in registers where there is one vector, else
-// in shared memory that no other lane touches (vectors of 16 bytes, neighbouring lanes side by side).
+// A lane's sums over the block's rows, V vectors of eight columns of each of N gradients: in registers up to two vectors, else in
+// shared memory that no other lane touches (vectors of 16 bytes, neighbouring lanes side by side).
 template <int V, int N>
 struct ColumnSums {
-    float2 r[V == 1 ? N : 1][4];
+    static constexpr bool kRegisters = V <= 2;
+    float2 r[kRegisters ? N * V : 1][4];
     float4* s;
-    __device__ __forceinline__ ColumnSums()
+    __device__ __forceinline__ explicit ColumnSums(float4* shared)
     {
-        extern __shared__ __align__(16) float4 s_columns[];
-        s = s_columns + threadIdx.x;
-        if (V == 1) {
+        s = shared + threadIdx.x;
+        if (kRegisters) {
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+            for (int n = 0; n < N * V; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) r[n][i] = both(0.f);
         } else {
@@ -339,9 +452,9 @@ struct ColumnSums {
     }
     __device__ __forceinline__ void get(int n, int v, float2 (&f)[4]) const
     {
-        if (V == 1) {
+        if (kRegisters) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) f[i] = r[n][i];
+            for (int i = 0; i < 4; ++i) f[i] = r[kRegisters ? n * V + v : 0][i];
         } else {
             const float4 a = s[((n * V + v) * 2) * blockDim.x], b = s[((n * V + v) * 2 + 1) * blockDim.x];
             f[0] = make_float2(a.x, a.y); f[1] = make_float2(a.z, a.w); f[2] = make_float2(b.x, b.y); f[3] = make_float2(b.z, b.w);
@@ -349,9 +462,9 @@ struct ColumnSums {
     }
     __device__ __forceinline__ void set(int n, int v, const float2 (&f)[4])
     {
-        if (V == 1) {
+        if (kRegisters) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r[n][i] = f[i];
+            for (int i = 0; i < 4; ++i) r[kRegisters ? n * V + v : 0][i] = f[i];
         } else {
             s[((n * V + v) * 2) * blockDim.x] = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
             s[((n * V + v) * 2 + 1) * blockDim.x] = make_float4(f[2].x, f[2].y, f[3].x, f[3].y);
@@ -375,7 +488,11 @@ struct ColumnSums {
     }
 };
 // (bytes of shared memory)
-size_t column_sums_bytes(int V, int N, int threads) { return V == 1 ? 0 : (size_t)N * V * 8 * sizeof(float) * threads; }
+size_t column_sums_bytes(int V, int N, int threads) { return V <= 2 ? 0 : (size_t)N * V * 8 * sizeof(float) * threads; }
+
+// Rows on their way in shared memory (0: one, in registers).
+template <int V>
+constexpr int kGradRows = V <= 2 ? 2 : 0;
 
 // One row at a time by W warps, V vectors per lane, blockDim / (32 W) rows at once; a lane keeps the same columns for all of the
 // block's rows and adds up their gradients (of the weights, of a gate per channel), rows in their order.  A row has two
@@ -394,26 +511,21 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
     __syncthreads();
     pdl_wait();
     pdl_launch_dependents();
-    uint4 yv[V], hv[V], gv[V], ov[V], dv[V];
-    float gt = 1.f;
-    auto fetch = [&](int t) {
-        const int H = t < p.T ? p.H : 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int n = p.d_out ? H - first - v * step : 0;
-            hv[v] = load8<VEC>(p.h + (size_t)t * p.ldh + first + v * step, n);
-            ov[v] = load8<VEC>(p.d_out + (size_t)t * p.ldout_grad + first + v * step, n);
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) yv[v] = load8<VEC>(p.y + (size_t)t * p.ldy + first + v * step, H - first - v * step);
-#pragma unroll
-        for (int v = 0; v < V; ++v) dv[v] = load8<VEC>(p.d_h + (size_t)t * p.ldh_grad + first + v * step, p.d_h ? H - first - v * step : 0);
-        if (GATE == MOE_GATE_ELEMENT) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) gv[v] = load8<VEC>((const bf16*)p.gate + (size_t)t * p.ldg + first + v * step, H - first - v * step);
-        }
-        if (GATE == MOE_GATE_TOKEN && t < p.T) gt = ((const float*)p.gate)[t];
-    };
+    constexpr bool kElement = GATE == MOE_GATE_ELEMENT;
+    const int sets = (p.T + rows - 1) / rows, t_step = gridDim.x * rows;
+    int t = blockIdx.x * rows + row_in_block;
+    extern __shared__ __align__(16) uint4 s_feed[];           // rows on their way, then the columns' sums
+    RowFeed<kElement ? 5 : 4, V, VEC, kGradRows<V>> feed;
+    feed.src[0] = p.y + first; feed.ld[0] = (uint32_t)p.ldy * 2;
+    feed.src[1] = p.d_out ? p.h + first : nullptr; feed.ld[1] = (uint32_t)p.ldh * 2;
+    feed.src[2] = p.d_out ? p.d_out + first : nullptr; feed.ld[2] = (uint32_t)p.ldout_grad * 2;
+    feed.src[3] = p.d_h ? p.d_h + first : nullptr; feed.ld[3] = (uint32_t)p.ldh_grad * 2;
+    if (kElement) { feed.src[kElement ? 4 : 0] = (const bf16*)p.gate + first; feed.ld[kElement ? 4 : 0] = (uint32_t)p.ldg * 2; }
+    feed.start(s_feed, p.H - first, step, p.T, t, t_step);
+    float gt = GATE == MOE_GATE_TOKEN && t < p.T ? ((const float*)p.gate)[t] : 1.f;
+    bf16* const d_y = p.d_y + first;
+    bf16* const d_residual = p.d_residual + first;
+    bf16* const d_gate = (bf16*)p.d_gate + first;
     auto column = [&](const bf16* w, int v) {                 // eight of a row of weights, or ones
         const int col = first + v * step, n = p.H - col;
         if (!w) return make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
@@ -437,27 +549,25 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
             if (GATE == MOE_GATE_CHANNEL) unpack8(column((const bf16*)p.gate, v), gate_w[v]);
         }
     }
-    ColumnSums<V, GATE == MOE_GATE_CHANNEL ? 3 : 2> columns;  // of d_pre, d_post (without block_scale), d_gate
+    ColumnSums<V, GATE == MOE_GATE_CHANNEL ? 3 : 2> columns(reinterpret_cast<float4*>(s_feed + (VEC ? kGradRows<V> * (kElement ? 5 : 4) * V * blockDim.x : 0)));  // of d_pre, d_post (without block_scale), d_gate
     const float over = 1.f / (float)p.H;
-    int t = blockIdx.x * rows + row_in_block;
     int buf = 0;
-    fetch(t);
-    for (int set = blockIdx.x; set * rows < p.T; set += gridDim.x, t += gridDim.x * rows, buf ^= 1) {
+    for (int set = blockIdx.x; set < sets; set += gridDim.x, t += t_step, buf ^= 1) {
         const bool live = t < p.T;
+        const int n = live ? p.H - first : 0;
         float* const s1 = s_sums[row_in_block] + buf * 128;
         float* const s2 = s1 + 64;
         float2 y[V][4], d[V][4], h[V][4];
-        uint4 gate_now[V], dh_now[V];
         const float token_gate = gt;
+        if (GATE == MOE_GATE_TOKEN && t + t_step < p.T) gt = ((const float*)p.gate)[t + t_step];
+        feed.begin();
         float2 hh = both(0.f), hd = both(0.f), yy = both(0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!kKeep) load_pre(v, pre_w[v]);
-            unpack8(hv[v], h[v]);
-            unpack8(ov[v], d[v]);
-            unpack8(yv[v], y[v]);
-            dh_now[v] = dv[v];
-            if (GATE == MOE_GATE_ELEMENT) gate_now[v] = gv[v];
+            unpack8(feed.get(1, v), h[v]);
+            unpack8(feed.get(2, v), d[v]);
+            unpack8(feed.get(0, v), y[v]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 hh = fma2(h[v][i], h[v][i], hh);
@@ -466,7 +576,6 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
             }
         }
         float sums[3] = {hh.x + hh.y, hd.x + hd.y, yy.x + yy.y};
-        if (set + gridDim.x < (p.T + rows - 1) / rows) fetch(t + gridDim.x * rows);
         row_sums<3>(sums, W, wr, lane, s1);
         if (p.d_out) {
             // d_out n for the weight's gradient, then what goes on to h
@@ -488,7 +597,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
                 mean = fmaf(more[0], over, p.eps * unit * unit);
                 dot = more[1];
             }
-            const float inv = live ? 1.f / sqrtf(mean) : 0.f, back = inv * unit;
+            const float inv = live ? inverse_root(mean) : 0.f, back = inv * unit;
             dot *= inv * over;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -502,15 +611,14 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int col = first + v * step;
             float2 u[4];
-            unpack8(dh_now[v], u);
+            unpack8(feed.get(3, v), u);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 d[v][i] = add2(d[v][i], u[i]);
                 u[i] = mul2(d[v][i], both(p.residual_scale));
             }
-            if (p.d_residual) store8<VEC>(p.d_residual + (size_t)t * p.ldr_grad + col, live ? p.H - col : 0, u);
+            if (p.d_residual) store8<VEC>(at(d_residual, t, (uint32_t)p.ldr_grad * 2) + v * step, n - v * step, u);
         }
         float inv = 1.f, unit = 1.f;
         if (p.post) {
@@ -529,14 +637,13 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
                     for (int i = 0; i < 4; ++i) y[v][i] = x[v][i];
                 mean = fmaf(more[0], over, p.eps * unit * unit);
             }
-            inv = live ? 1.f / sqrtf(mean) : 0.f;
+            inv = live ? inverse_root(mean) : 0.f;
         }
         float row_slope = 1.f;
         const float row_gate = GATE == MOE_GATE_TOKEN ? activate(token_gate, p.gate_act, &row_slope) : 1.f;
         float2 dd = both(0.f);                                // without the token's gate, whose gradient it is too
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int col = first + v * step;
             float2 g[4], dg[4], b[4];
             if (!kKeep) load_post(v, post_w[v]);
             if (GATE == MOE_GATE_CHANNEL) {
@@ -544,7 +651,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) g[i] = gate_w[v][i];
             }
-            if (GATE == MOE_GATE_ELEMENT) unpack8(gate_now[v], g);
+            if (kElement) unpack8(feed.get(kElement ? 4 : 0, v), g);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (p.post) y[v][i] = mul2(y[v][i], both(inv));              // m
@@ -563,8 +670,9 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
             }
             columns.add(1, v, b, y[v]);
             if (GATE == MOE_GATE_CHANNEL) columns.add(2, v, dg);
-            if (GATE == MOE_GATE_ELEMENT && p.d_gate) store8<VEC>((bf16*)p.d_gate + (size_t)t * p.ldg_grad + col, live ? p.H - col : 0, dg);
+            if (kElement && p.d_gate) store8<VEC>(at(d_gate, t, (uint32_t)p.ldg_grad * 2) + v * step, n - v * step, dg);
         }
+        feed.end();
         float dot[1] = {dd.x + dd.y};
         if (p.post || GATE == MOE_GATE_TOKEN) row_sums<1>(dot, W, wr, lane, s2);
         if (GATE == MOE_GATE_TOKEN && p.d_gate && live && wr == 0 && lane == 0) ((float*)p.d_gate)[t] = dot[0] * row_slope;
@@ -575,7 +683,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
                 float2 u[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) u[i] = mul2(fma2(y[v][i], both(-mean), d[v][i]), both(back));
-                store8<VEC>(p.d_y + (size_t)t * p.ldy_grad + first + v * step, live ? p.H - first - v * step : 0, u);
+                store8<VEC>(at(d_y, t, (uint32_t)p.ldy_grad * 2) + v * step, n - v * step, u);
             }
         }
     }
@@ -639,26 +747,13 @@ GradShape grad_shape(int T, int H)
     return g;
 }
 
-// the opt-in to large dynamic shared memory is a per-device attribute of a kernel
-template <typename K>
-cudaError_t allow_smem(K kern, bool (&done)[kMaxDevices])
-{
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
-    if (done[dev]) return cudaSuccess;
-    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-    if (e == cudaSuccess) done[dev] = true;
-    return e;
-}
-
 template <int V, int GATE>
 cudaError_t launch_grad_gate(const BlockNormArgs& p, const GradShape& g, cudaStream_t st)
 {
     static bool ok[2][kMaxDevices] = {{false}, {false}};
     const dim3 grid(g.blocks), block(32 * g.W * g.rows);
-    const size_t smem = column_sums_bytes(V, GATE == MOE_GATE_CHANNEL ? 3 : 2, 32 * g.W * g.rows);
+    const int threads = 32 * g.W * g.rows;
+    const size_t smem = column_sums_bytes(V, GATE == MOE_GATE_CHANNEL ? 3 : 2, threads) + (p.vec ? feed_bytes(GATE == MOE_GATE_ELEMENT ? 5 : 4, V, kGradRows<V>, threads) : 0);
     if (smem > 40 * 1024) {
         const cudaError_t e = p.vec ? allow_smem(block_norm_grad_kernel<V, GATE, true>, ok[1]) : allow_smem(block_norm_grad_kernel<V, GATE, false>, ok[0]);
         if (e != cudaSuccess) return e;

@@ -23,6 +23,9 @@ bool off(const void* p, size_t align) { return ((uintptr_t)p & (align - 1)) != 0
 // an output in the place of an input needs the input's row distance: a row would be overwritten before it is read
 bool shifted(const void* out, int64_t ld_out, const void* in, int64_t ld_in, int T) { return out && out == in && T > 1 && ld_out != ld_in; }
 
+// row distances of the block norms: 32 bits
+bool beyond(int64_t ld) { return ld > INT32_MAX; }
+
 int check_block_rule(const moe_block_rule* r)
 {
     if (!r) return MOE_ERR_NULL;
@@ -190,6 +193,7 @@ int moe_block_norm(const void* block_out, int64_t ld_block, const void* residual
     if (H > kBlockNormMaxH) return MOE_ERR_UNSUPPORTED;
     const bool element = rule->gate == MOE_GATE_ELEMENT;
     if (ld_block < H || ld_residual < H || ld_h < H || (out && ld_out < H) || (out_q && ld_q < H) || (element && ld_gate < H)) return MOE_ERR_SHAPE;
+    if (beyond(ld_block) || beyond(ld_residual) || beyond(ld_h) || (out && beyond(ld_out)) || (element && beyond(ld_gate))) return MOE_ERR_UNSUPPORTED;
     if (off(block_out, 2) || off(residual, 2) || off(post_weight, 2) || off(pre_weight, 2) || off(gate, rule->gate == MOE_GATE_TOKEN ? 4 : 2) ||
         off(h, 2) || off(out, 2) || off(q_scale, 4))
         return MOE_ERR_SHAPE;
@@ -234,6 +238,9 @@ int moe_block_norm_backward(const void* block_out, int64_t ld_block, const void*
     if (ld_block < H || (d_out && ld_h < H) || (element && ld_gate < H) || (d_out && ld_d_out < H) || (d_h && ld_d_h < H) ||
         (d_block && ld_d_block < H) || (d_residual && ld_d_residual < H) || (element && d_gate && ld_d_gate < H))
         return MOE_ERR_SHAPE;
+    if (beyond(ld_block) || (d_out && (beyond(ld_h) || beyond(ld_d_out))) || (element && (beyond(ld_gate) || (d_gate && beyond(ld_d_gate)))) ||
+        (d_h && beyond(ld_d_h)) || (d_block && beyond(ld_d_block)) || (d_residual && beyond(ld_d_residual)))
+        return MOE_ERR_UNSUPPORTED;
     if (off(block_out, 2) || off(h, 2) || off(post_weight, 2) || off(pre_weight, 2) || off(gate, rule->gate == MOE_GATE_TOKEN ? 4 : 2) || off(d_out, 2) ||
         off(d_h, 2) || off(d_block, 2) || off(d_residual, 2) || off(d_gate, element ? 2 : 4) || off(d_post_weight, 4) || off(d_pre_weight, 4) ||
         off(workspace, 16))

@@ -468,7 +468,7 @@ def test_refusals_of_the_c_entry_points():
         assert fwd(**kw) == B.MOE_ERR_SHAPE, kw
     for kw in (dict(y=None), dict(res=None), dict(h=None), dict(out=None), dict(q=a[7]), dict(r=rule(gate=1))):
         assert fwd(**kw) == B.MOE_ERR_NULL, kw
-    assert fwd(H=16385, ld=16385, ldh=16385) == B.MOE_ERR_UNSUPPORTED
+    assert fwd(H=16385, ld=16385, ldh=16385) == B.MOE_ERR_UNSUPPORTED and fwd(ldh=1 << 31) == B.MOE_ERR_UNSUPPORTED
     assert lib.moe_block_norm(a[0], 64, a[1], 64, None, None, None, 0, None, 2, 64, a[4], 64, None, 0, None, 0, None, None) == B.MOE_ERR_NULL
 
     def bwd(T=2, H=64, ld=64, r=None, y=a[0], h=a[1], post=a[2], pre=a[3], gate=None, d_out=a[4], d_h=a[5], d_block=a[6], ldb=64, d_res=a[7], d_gate=None,
