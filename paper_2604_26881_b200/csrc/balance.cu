@@ -10,6 +10,7 @@
 #include <float.h>
 
 #include "balance.cuh"
+#include "rows.cuh"
 
 namespace faasmoe {
 
@@ -17,7 +18,8 @@ namespace {
 
 constexpr uint32_t kFull = 0xffffffffu;
 constexpr int kC = 16;                  // experts of a lane
-constexpr int kWarps = 8;
+constexpr int kWarps = 8;              // of a block of the gradient
+constexpr int kSumWarps = 32;          // of the loss: an SM's registers
 
 // a logit as the rules see it: NaN counts as -inf, +inf as the largest finite value
 __device__ __forceinline__ float clean(float z) { return fminf(fmaxf(z, -INFINITY), FLT_MAX); }
@@ -46,23 +48,24 @@ __device__ __forceinline__ float group_max(float v)
 template <int L, int VW>
 __device__ __forceinline__ int expert_of(int sub, int i) { return ((i / VW) * L + sub) * VW + i % VW; }
 
-// This lane's 16 logits of a row as they are, -inf where there is no expert.
+// This lane's 16 logits of a row as they are, in pairs, -inf where there is no expert.
 template <int L, int VW, typename TL>
-__device__ __forceinline__ void load_row(const TL* row, int E, int sub, bool live, float (&z)[kC])
+__device__ __forceinline__ void load_row(const TL* row, int E, int sub, bool live, float2 (&z)[kC / 2])
 {
+    float* const f = reinterpret_cast<float*>(z);
 #pragma unroll
     for (int q = 0; q < kC / VW; ++q) {
         const int e0 = (q * L + sub) * VW, n = live ? E - e0 : 0;
-        TL v[VW];
         if (VW > 1 && n >= VW) {
             const uint4 u = *reinterpret_cast<const uint4*>(row + e0);
+            TL v[VW];
             memcpy(v, &u, sizeof(v) < sizeof(u) ? sizeof(v) : sizeof(u));
+#pragma unroll
+            for (int j = 0; j < VW; ++j) f[q * VW + j] = to_float(v[j]);
         } else {
 #pragma unroll
-            for (int j = 0; j < VW; ++j) if (j < n) v[j] = row[e0 + j];
+            for (int j = 0; j < VW; ++j) f[q * VW + j] = j < n ? to_float(row[e0 + j]) : -INFINITY;
         }
-#pragma unroll
-        for (int j = 0; j < VW; ++j) z[q * VW + j] = j < n ? to_float(v[j]) : -INFINITY;
     }
 }
 
@@ -91,6 +94,31 @@ __device__ __forceinline__ float rcp(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// exp of two logits: 2^t with t = z log2 e rounded, times 1 + ln 2 (z log2 e - t), the product's rounding error out of an fma
+// (Dekker's product, as the fma gives it) and the rest of log2 e -- 3.5 instructions each instead of 9, off by 3 units of 2^-24.  A
+// NaN counts as -inf; below -10^4 is 0 as well; beyond the range of fp32 it is not a number, and the row's sum neither.
+__device__ __forceinline__ float2 exp_of(float2 z)
+{
+    const float2 c = make_float2(fmaxf(z.x, -1e4f), fmaxf(z.y, -1e4f));
+    const float2 t = mul2(c, both(-1.44269502f));
+    const float2 lo = fma2(c, both(1.92596303e-8f), fma2(c, both(1.44269502f), t));
+    const float2 r = make_float2(ex2(-t.x), ex2(-t.y));
+    return fma2(mul2(r, both(0.693147182f)), lo, r);
+}
+__device__ __forceinline__ float2 rcp_of(float2 x) { return make_float2(rcp(x.x), rcp(x.y)); }
+__device__ __forceinline__ float total(const float2 (&x)[kC / 2])
+{
+    float2 s = x[0];
+#pragma unroll
+    for (int i = 1; i < kC / 2; ++i) s = add2(s, x[i]);
+    return s.x + s.y;
+}
 
 // The same for rows of any logits: from clean(z), exponentials shifted by the largest.  e: exp(z - top), of which the softmax is e *
 // inv; s: sigmoid scores, in units of the largest if that is below exp(-60).  A token without any logit above -inf has zeros.
@@ -98,8 +126,9 @@ template <int L, bool SIGMOID>
 struct Shifted {
     float e[kC], s[SIGMOID ? kC : 1];
     float top, inv, lse, share_inv;
-    __device__ __forceinline__ explicit Shifted(const float (&z)[kC])
+    __device__ __forceinline__ explicit Shifted(const float2 (&pairs)[kC / 2])
     {
+        const float* const z = reinterpret_cast<const float*>(pairs);
         top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kC; ++i) top = fmaxf(top, clean(z[i]));
@@ -126,11 +155,11 @@ struct Shifted {
 };
 
 template <int L, bool SIGMOID>
-__device__ __noinline__ void shifted_shares(float (&z)[kC], float& lse)
+__device__ __noinline__ void shifted_shares(float2 (&z)[kC / 2], float& lse)
 {
     const Shifted<L, SIGMOID> r(z);
 #pragma unroll
-    for (int i = 0; i < kC; ++i) z[i] = r.share(i);
+    for (int i = 0; i < kC / 2; ++i) z[i] = make_float2(r.share(2 * i), r.share(2 * i + 1));
     lse = r.lse;
 }
 
@@ -153,7 +182,7 @@ __device__ __forceinline__ void finish(const BalanceArgs& p, int m, const float*
     if (r < rows && c < Ep) {
         float4 sp = make_float4(0.f, 0.f, 0.f, 0.f);
         int4 sc = make_int4(0, 0, 0, 0);
-#pragma unroll 4
+#pragma unroll 5
         for (int x = r; x < n; x += rows) {
             const float4 f = *reinterpret_cast<const float4*>(rec + x * stride + c);
             const int4 q = *reinterpret_cast<const int4*>(rec + x * stride + Ep + c);
@@ -201,29 +230,30 @@ __device__ __forceinline__ void finish(const BalanceArgs& p, int m, const float*
 // blockIdx.y: model; the model's blocks take chunks of up to 32 tokens per warp in turn, list those of the model and sum up 32 / L of
 // them at a time.  A lane keeps the sums of its 16 experts.
 template <int L, int VW, bool SIGMOID, typename TL>
-__global__ void __launch_bounds__(32 * kWarps, 4)
-balance_kernel(const BalanceArgs p)
+__global__ void __launch_bounds__(32 * kSumWarps, 1)
+balance_kernel(const __grid_constant__ BalanceArgs p)
 {
     constexpr int G = 32 / L;                                 // tokens of a warp at a time
-    __shared__ __align__(16) float s_p[kWarps][kC * L];
+    __shared__ __align__(16) float s_p[kSumWarps][kC * L];
     __shared__ __align__(16) int s_count[kC * L];
-    __shared__ float s_z[kWarps];
-    __shared__ int s_n[kWarps];
-    __shared__ unsigned char s_list[kWarps][32];
+    __shared__ float s_z[kSumWarps];
+    __shared__ int s_n[kSumWarps];
+    __shared__ unsigned char s_list[kSumWarps][32];
     __shared__ __align__(16) float s_rec[record(kC * L)];
-    pdl_wait();
-    pdl_launch_dependents();
     const RouterBatch& b = p.b;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane % L, group = lane / L;
     const int m = blockIdx.y;
     for (int i = threadIdx.x; i < kC * L; i += blockDim.x) s_count[i] = 0;
     __syncthreads();
-    float acc[kC], z2 = 0.f;
+    pdl_wait();
+    pdl_launch_dependents();
+    float2 acc[kC / 2];
+    float z2 = 0.f;
 #pragma unroll
-    for (int i = 0; i < kC; ++i) acc[i] = 0.f;
+    for (int i = 0; i < kC / 2; ++i) acc[i] = both(0.f);
     int tokens = 0;
     const int chunks = (b.T + p.chunk - 1) / p.chunk;
-    for (int chunk = blockIdx.x * kWarps + warp; chunk < chunks; chunk += gridDim.x * kWarps) {
+    for (int chunk = blockIdx.x * (blockDim.x >> 5) + warp; chunk < chunks; chunk += gridDim.x * (blockDim.x >> 5)) {
         const int t0 = chunk * p.chunk, t = t0 + lane;
         const bool mine = lane < p.chunk && t < b.T && model_of(b, t, m == 0) == m;
         const uint32_t set = __ballot_sync(kFull, mine);
@@ -242,35 +272,31 @@ balance_kernel(const BalanceArgs p)
             const bool live = base + group < count;
             const int row = t0 + (live ? s_list[warp][base + group] : 0);
             const TL* const logits = (const TL*)b.logits + (size_t)row * b.ld;
-            float z[kC], x = 0.f, lse;
+            float2 z[kC / 2];
             load_row<L, VW>(logits, b.E, sub, live, z);
 #pragma unroll
-            for (int i = 0; i < kC; ++i) { z[i] = expf(z[i]); x += z[i]; }
-            x = group_sum<L>(x);
-            lse = logf(x);
+            for (int i = 0; i < kC / 2; ++i) z[i] = exp_of(z[i]);
+            float x = group_sum<L>(total(z)), lse = live ? logf(x) : 0.f;
             const bool far = live && !ordinary(x);
             if (SIGMOID) {
-                x = 0.f;
 #pragma unroll
-                for (int i = 0; i < kC; ++i) { z[i] *= rcp(1.f + z[i]); x += z[i]; }
-                x = group_sum<L>(x);
+                for (int i = 0; i < kC / 2; ++i) z[i] = mul2(z[i], rcp_of(add2(z[i], both(1.f))));
+                x = group_sum<L>(total(z));
             }
-            const float inv = live ? __fdividef(1.f, x) : 0.f;
-            if (!live) lse = 0.f;
-#pragma unroll
-            for (int i = 0; i < kC; ++i) z[i] *= inv;
+            const float inv = live && !far ? rcp(x) : 0.f;
             if (__any_sync(kFull, far)) {
-                float again[kC], lse2;
+                float2 again[kC / 2];
+                float lse2;
                 load_row<L, VW>(logits, b.E, sub, far, again);
                 shifted_shares<L, SIGMOID>(again, lse2);
                 if (far) {
                     lse = lse2;
 #pragma unroll
-                    for (int i = 0; i < kC; ++i) z[i] = again[i];
+                    for (int i = 0; i < kC / 2; ++i) { acc[i] = add2(acc[i], again[i]); z[i] = both(0.f); }
                 }
             }
 #pragma unroll
-            for (int i = 0; i < kC; ++i) acc[i] += z[i];
+            for (int i = 0; i < kC / 2; ++i) acc[i] = fma2(z[i], both(inv), acc[i]);
             z2 = fmaf(lse, lse, z2);
         }
         __syncwarp();
@@ -278,27 +304,29 @@ balance_kernel(const BalanceArgs p)
 #pragma unroll
     for (int o = L; o < 32; o <<= 1) {
 #pragma unroll
-        for (int i = 0; i < kC; ++i) acc[i] += __shfl_xor_sync(kFull, acc[i], o);
+        for (int i = 0; i < kC / 2; ++i) {
+            acc[i].x += __shfl_xor_sync(kFull, acc[i].x, o);
+            acc[i].y += __shfl_xor_sync(kFull, acc[i].y, o);
+        }
         z2 += __shfl_xor_sync(kFull, z2, o);
     }
     if (group == 0) {
 #pragma unroll
-        for (int i = 0; i < kC; ++i) s_p[warp][expert_of<L, VW>(sub, i)] = acc[i];
+        for (int i = 0; i < kC; ++i) s_p[warp][expert_of<L, VW>(sub, i)] = i & 1 ? acc[i / 2].y : acc[i / 2].x;
     }
     if (lane == 0) { s_z[warp] = z2; s_n[warp] = tokens; }
     __syncthreads();
-    const int Ep = padded(b.E);
+    const int Ep = padded(b.E), warps = blockDim.x >> 5;
     for (int e = threadIdx.x; e < Ep; e += blockDim.x) {
         float sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) sum += s_p[w][e];
+        for (int w = 0; w < warps; ++w) sum += s_p[w][e];
         s_rec[e] = sum;
         s_rec[Ep + e] = __int_as_float(s_count[e]);
     }
     if (threadIdx.x == 0) {
         float sum = 0.f;
         int n = 0;
-        for (int w = 0; w < kWarps; ++w) { sum += s_z[w]; n += s_n[w]; }
+        for (int w = 0; w < warps; ++w) { sum += s_z[w]; n += s_n[w]; }
         s_rec[2 * Ep] = sum;
         s_rec[2 * Ep + 1] = __int_as_float(n);
     }
@@ -327,7 +355,7 @@ balance_finish_kernel(const BalanceArgs p)
 // One step of a warp: the gradients of the tokens of its groups of L lanes.  FAR: those whose exponentials need a shift (`todo`);
 // otherwise all but those, which are returned.  f: the model's counts if there is one model, else they are looked up.
 template <int L, int VW, bool SIGMOID, bool MULTI, bool FAR, typename TL>
-__device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add, const float (&f1)[kC], float coef1, float z1)
+__device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add, const float2 (&f1)[kC / 2], float coef1, float z1)
 {
     constexpr int J = L < 8 ? 2 : 1;                          // chosen experts of a lane: j = sub and sub + L
     const RouterBatch& b = p.b;
@@ -344,13 +372,15 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
             gw[q] = p.d_w[(size_t)t * b.k + j] * p.scale;
         }
     }
-    float coef = coef1, cz = z1, f[kC];
+    float coef = coef1, cz = z1;
+    float2 f[kC / 2];
     if (MULTI) {
         const float n = live && (p.d_loss || p.d_z) ? (float)max(p.tokens[m], 1) : 1.f;
         coef = live && p.d_loss ? p.d_loss[m] * ((float)b.E / (float)b.k) / n / n : 0.f;
         cz = live && p.d_z ? 2.f * p.d_z[m] / n : 0.f;
     }
-    float e[kC], r[SIGMOID ? kC : 1], s[SIGMOID && FAR ? kC : 1];       // exponentials; 1 - s; s
+    constexpr int kS = SIGMOID ? kC / 2 : 1, kSF = SIGMOID && FAR ? kC / 2 : 1;
+    float2 e[kC / 2], r[kS], s[kSF];                          // exponentials; 1 - s; s
     float inv, lse, share_inv, from = 0.f, ref = 0.f;
     bool far = false;
     load_row<L, VW>(logits, b.E, sub, live, e);
@@ -358,7 +388,7 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
 #pragma unroll
         for (int i = 0; i < kC; ++i) {
             const int at = expert_of<L, VW>(sub, i);
-            f[i] = live && p.d_loss && at < b.E ? (float)p.counts[(size_t)m * b.E + at] : 0.f;
+            reinterpret_cast<float*>(f)[i] = live && p.d_loss && at < b.E ? (float)p.counts[(size_t)m * b.E + at] : 0.f;
         }
     }
     // (a token's choices are as many as its lanes take; their logits are in the caches now)
@@ -375,10 +405,13 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
         const Shifted<L, SIGMOID> x(e);
         if (SIGMOID) {
 #pragma unroll
-            for (int i = 0; i < kC; ++i) { r[i] = sigmoid_from(-clean(e[i]), 0.f); s[i] = x.s[i]; }
+            for (int i = 0; i < kC / 2; ++i) {
+                r[SIGMOID ? i : 0] = make_float2(sigmoid_from(-clean(e[i].x), 0.f), sigmoid_from(-clean(e[i].y), 0.f));
+                s[SIGMOID ? i : 0] = make_float2(x.s[SIGMOID ? 2 * i : 0], x.s[SIGMOID ? 2 * i + 1 : 0]);
+            }
         }
 #pragma unroll
-        for (int i = 0; i < kC; ++i) e[i] = x.e[i];
+        for (int i = 0; i < kC / 2; ++i) e[i] = make_float2(x.e[2 * i], x.e[2 * i + 1]);
         inv = x.inv; lse = x.lse; share_inv = x.share_inv;
         from = x.top > -INFINITY ? x.top : 0.f;
         float best = -INFINITY;
@@ -387,38 +420,45 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
         best = group_max<L>(best);
         if (p.renormalize && best > -INFINITY) ref = SIGMOID ? fminf(best, 0.f) : best;
     } else {
-        float x = 0.f;
 #pragma unroll
-        for (int i = 0; i < kC; ++i) { e[i] = expf(e[i]); x += e[i]; }
-        x = group_sum<L>(x);
+        for (int i = 0; i < kC / 2; ++i) e[i] = exp_of(e[i]);
+        const float x = group_sum<L>(total(e));
         far = live && !ordinary(x);
-        inv = live ? __fdividef(1.f, x) : 0.f;
+        inv = live ? rcp(x) : 0.f;
         lse = live ? logf(x) : 0.f;
         share_inv = inv;
         if (SIGMOID) {
-            x = 0.f;
+            float2 sum = both(0.f);
 #pragma unroll
-            for (int i = 0; i < kC; ++i) { r[i] = rcp(1.f + e[i]); x = fmaf(e[i], r[i], x); }
-            x = group_sum<L>(x);
-            share_inv = live ? __fdividef(1.f, x) : 0.f;
+            for (int i = 0; i < kS; ++i) {
+                r[i] = rcp_of(add2(e[i], both(1.f)));
+                sum = fma2(e[i], r[i], sum);
+            }
+            const float all = group_sum<L>(sum.x + sum.y);    // (a shuffle: not under a condition)
+            share_inv = live ? rcp(all) : 0.f;
         }
     }
-    float d[kC];
+    float2 d[kC / 2];
 #pragma unroll
-    for (int i = 0; i < kC; ++i) d[i] = 0.f;
+    for (int i = 0; i < kC / 2; ++i) d[i] = both(0.f);
     if (p.d_w) {
-        float ws[J], inner[J], sum = 0.f;
+        float ws[J], inner[J], slope[J], sum = 0.f;
 #pragma unroll
         for (int q = 0; q < J; ++q) {
-            const float x = expf(zj[q]);                      // (not used where it is not in range)
-            if (FAR) ws[q] = SIGMOID ? sigmoid_from(zj[q], ref) : (p.renormalize ? expf(zj[q] - ref) : expf(zj[q] - from) * inv);
-            else ws[q] = SIGMOID ? x * rcp(1.f + x) : (p.renormalize ? x : x * inv);
+            if (FAR) {
+                ws[q] = SIGMOID ? sigmoid_from(zj[q], ref) : (p.renormalize ? expf(zj[q] - ref) : expf(zj[q] - from) * inv);
+                slope[q] = SIGMOID ? sigmoid_from(-zj[q], 0.f) : 1.f;
+            } else {
+                const float x = exp_of(both(zj[q])).x;
+                slope[q] = SIGMOID ? rcp(1.f + x) : 1.f;
+                ws[q] = SIGMOID ? x * slope[q] : (p.renormalize ? x : x * inv);
+            }
             sum += ws[q];
         }
         if (p.renormalize) {
             sum = group_sum<L>(sum);
             if (!FAR) far = far || (live && !(sum > 1e-30f));           // (the chosen ones alone are too small)
-            const float over = sum > 0.f ? 1.f / sum : 0.f;
+            const float over = sum > 0.f ? rcp(sum) : 0.f;
             sum = 0.f;
 #pragma unroll
             for (int q = 0; q < J; ++q) { ws[q] *= over; sum = fmaf(gw[q], ws[q], sum); }
@@ -432,24 +472,25 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
             if (!SIGMOID) {                                   // every expert has its share of the whole
                 sum = group_sum<L>(sum) * inv;
 #pragma unroll
-                for (int i = 0; i < kC; ++i) d[i] = -e[i] * sum;
+                for (int i = 0; i < kC / 2; ++i) d[i] = mul2(e[i], both(-sum));
             }
         }
+        // Each choice leaves its number at its expert; a number that another one has written over tells of an expert chosen twice.
+        int* const tag = reinterpret_cast<int*>(add);
 #pragma unroll
         for (int q = 0; q < J; ++q) {
-            if (SIGMOID) inner[q] *= sigmoid_from(-zj[q], 0.f);
-            if (id[q] >= 0) reinterpret_cast<int*>(add)[id[q]] = sub + q * L;
+            inner[q] *= slope[q];
+            if (id[q] >= 0) tag[id[q]] = sub + q * L;
         }
         __syncwarp();
         bool twice = false;
 #pragma unroll
-        for (int q = 0; q < J; ++q) twice |= id[q] >= 0 && reinterpret_cast<int*>(add)[id[q]] != sub + q * L;
-        __syncwarp();
+        for (int q = 0; q < J; ++q) twice |= id[q] >= 0 && tag[id[q]] != sub + q * L;
         if (__any_sync(kFull, twice)) {
-            // an expert that was chosen more than once gets them all, in the order of the choices
-            float total[J];
+            // such an expert gets them all, in the order of the choices
+            float all[J];
 #pragma unroll
-            for (int q = 0; q < J; ++q) total[q] = 0.f;
+            for (int q = 0; q < J; ++q) all[q] = 0.f;
             for (int j = 0; j < b.k; ++j) {
                 int other = __shfl_sync(kFull, id[0], group * L + j % L);
                 float x = __shfl_sync(kFull, inner[0], group * L + j % L);
@@ -459,10 +500,10 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
                     if (j >= L) { other = other1; x = x1; }
                 }
 #pragma unroll
-                for (int q = 0; q < J; ++q) if (other == id[q]) total[q] += x;
+                for (int q = 0; q < J; ++q) if (other == id[q]) all[q] += x;
             }
 #pragma unroll
-            for (int q = 0; q < J; ++q) inner[q] = total[q];
+            for (int q = 0; q < J; ++q) inner[q] = all[q];
         }
 #pragma unroll
         for (int q = 0; q < J; ++q) if (id[q] >= 0) add[id[q]] = inner[q];
@@ -474,10 +515,11 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
 #pragma unroll
                 for (int j = 0; j < VW; j += 4) {
                     const float4 x = *reinterpret_cast<const float4*>(from_add + j);
-                    d[q * VW + j] += x.x; d[q * VW + j + 1] += x.y; d[q * VW + j + 2] += x.z; d[q * VW + j + 3] += x.w;
+                    d[(q * VW + j) / 2] = add2(d[(q * VW + j) / 2], make_float2(x.x, x.y));
+                    d[(q * VW + j) / 2 + 1] = add2(d[(q * VW + j) / 2 + 1], make_float2(x.z, x.w));
                 }
             } else {
-                d[q] += *from_add;
+                reinterpret_cast<float*>(d)[q] += *from_add;
             }
         }
         __syncwarp();
@@ -486,25 +528,26 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
         __syncwarp();
     }
     if (p.d_z) {
-        const float c = cz * inv;
+        if (FAR) {
 #pragma unroll
-        for (int i = 0; i < kC; ++i) d[i] = fmaf(e[i] * c, lse, d[i]);  // (in this order: a share of 0 stays 0)
+            for (int i = 0; i < kC / 2; ++i) d[i] = fma2(mul2(e[i], both(cz * inv)), both(lse), d[i]);      // (in this order: a share of 0 stays 0)
+        } else {
+            const float c = cz * inv * lse;
+#pragma unroll
+            for (int i = 0; i < kC / 2; ++i) d[i] = fma2(e[i], both(c), d[i]);
+        }
     }
     if (p.d_loss) {
-        float mean = 0.f;
+        auto score = [&](int i) { return SIGMOID ? (FAR ? s[kSF > 1 ? i : 0] : mul2(e[i], r[kS > 1 ? i : 0])) : e[i]; };
+        float2 sum = both(0.f);
 #pragma unroll
-        for (int i = 0; i < kC; ++i) {
-            const float score = SIGMOID ? (FAR ? s[SIGMOID && FAR ? i : 0] : e[i] * r[SIGMOID ? i : 0]) : e[i];
-            mean = fmaf(MULTI ? f[i] : f1[i], score, mean);
-        }
-        mean = group_sum<L>(mean) * share_inv;
-        const float c = coef * share_inv;
+        for (int i = 0; i < kC / 2; ++i) sum = fma2(MULTI ? f[i] : f1[i], score(i), sum);
+        const float mean = group_sum<L>(sum.x + sum.y) * share_inv, c = coef * share_inv;
 #pragma unroll
-        for (int i = 0; i < kC; ++i) {
-            const float score = SIGMOID ? (FAR ? s[SIGMOID && FAR ? i : 0] : e[i] * r[SIGMOID ? i : 0]) : e[i];
-            float x = score * c * ((MULTI ? f[i] : f1[i]) - mean);
-            if (SIGMOID) x *= r[i];
-            d[i] += x;
+        for (int i = 0; i < kC / 2; ++i) {
+            float2 x = mul2(score(i), both(c));
+            if (SIGMOID) x = mul2(x, r[kS > 1 ? i : 0]);
+            d[i] = fma2(x, add2(MULTI ? f[i] : f1[i], both(-mean)), d[i]);
         }
     }
     if (t < b.T && (FAR ? todo : !far)) {
@@ -514,7 +557,7 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
             const int e0 = (q * L + sub) * VW, n = b.E - e0;
             TL v[VW];
 #pragma unroll
-            for (int j = 0; j < VW; ++j) v[j] = (TL)(live ? d[q * VW + j] : 0.f);
+            for (int j = 0; j < VW; ++j) v[j] = (TL)(live ? reinterpret_cast<const float*>(d)[q * VW + j] : 0.f);
             if (VW > 1 && n >= VW) {
                 uint4 u;
                 memcpy(&u, v, sizeof(v) < sizeof(u) ? sizeof(v) : sizeof(u));
@@ -530,7 +573,7 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
 template <int L, int VW, bool SIGMOID, typename TL>
 __device__ __noinline__ void grad_step_far(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add)
 {
-    const float none[kC] = {};                                // (looked up: what a call may look into does not stay in registers)
+    const float2 none[kC / 2] = {};                                // (looked up: what a call may look into does not stay in registers)
     grad_step<L, VW, SIGMOID, true, true, TL>(p, t, m, sub, group, todo, add, none, 0.f, 0.f);
 }
 
@@ -547,7 +590,8 @@ gate_grad_kernel(const __grid_constant__ GateGradArgs p)
     __syncwarp();
     pdl_wait();
     pdl_launch_dependents();
-    float f[kC], coef = 0.f, cz = 0.f;
+    float2 f[kC / 2];
+    float coef = 0.f, cz = 0.f;
     if (!MULTI) {
         const float n = p.d_loss || p.d_z ? (float)max(p.tokens[0], 1) : 1.f;
         if (p.d_loss) coef = p.d_loss[0] * ((float)b.E / (float)b.k) / n / n;
@@ -556,7 +600,7 @@ gate_grad_kernel(const __grid_constant__ GateGradArgs p)
 #pragma unroll
     for (int i = 0; i < kC; ++i) {
         const int e = expert_of<L, VW>(sub, i);
-        f[i] = !MULTI && p.d_loss && e < b.E ? (float)p.counts[e] : 0.f;
+        reinterpret_cast<float*>(f)[i] = !MULTI && p.d_loss && e < b.E ? (float)p.counts[e] : 0.f;
     }
     const int steps = (b.T + G - 1) / G;
     for (int step = blockIdx.x * kWarps + warp; step < steps; step += gridDim.x * kWarps) {
@@ -570,23 +614,26 @@ gate_grad_kernel(const __grid_constant__ GateGradArgs p)
 bool wide_rows(const void* p, int64_t ld, int size) { return (uintptr_t)p % 16 == 0 && ld * size % 16 == 0; }
 
 // Tokens that a warp of balance_kernel lists at once (with several models only those of one are summed up), and its blocks per model.
-struct BalanceShape { int chunk, blocks; };
+struct BalanceShape { int chunk, warps, blocks; };
 BalanceShape balance_shape(int T, int E, int M)
 {
     BalanceShape s;
     s.chunk = 32 / (E <= 64 ? 4 : (E <= 128 ? 8 : 16));
-    while (s.chunk < 32 && (M > 1 || T / s.chunk > 148 * 32)) s.chunk *= 2;
-    const int chunks = (T + s.chunk - 1) / s.chunk, all = (chunks + kWarps - 1) / kWarps;
-    int most = 148 * 4 / M;
+    while (s.chunk < 32 && (M > 1 || T / s.chunk > 148 * kSumWarps)) s.chunk *= 2;
+    const int chunks = (T + s.chunk - 1) / s.chunk;
+    // one block finishes by itself; several leave records, which one more launch adds up
+    s.warps = chunks <= kSumWarps ? (chunks < 2 ? 2 : chunks) : (chunks < 148 * 8 ? 8 : kSumWarps);      // (two: a lane for four experts)
+    int most = 148 / M;
     if (most < 1) most = 1;
-    s.blocks = all <= 2 ? 1 : (all < most ? all : most);
+    const int all = (chunks + s.warps - 1) / s.warps;
+    s.blocks = all < 1 ? 1 : (all < most ? all : most);
     return s;
 }
 
 template <int L, int VW, typename TL>
 cudaError_t run_balance(const BalanceArgs& p, cudaStream_t st)
 {
-    const dim3 grid(p.blocks, p.b.M), block(32 * kWarps);
+    const dim3 grid(p.blocks, p.b.M), block(32 * p.warps);
     return p.b.score == MOE_SCORE_SIGMOID ? launch_pdl(balance_kernel<L, VW, true, TL>, grid, block, 0, st, p)
                                           : launch_pdl(balance_kernel<L, VW, false, TL>, grid, block, 0, st, p);
 }
@@ -625,6 +672,7 @@ cudaError_t launch_balance(const BalanceArgs& in, cudaStream_t st)
     const BalanceShape s = balance_shape(b.T, b.E, b.M);
     p.blocks = s.blocks;
     p.chunk = s.chunk;
+    p.warps = s.warps;
     const bool wide = wide_rows(b.logits, b.ld, b.bf16_logits ? 2 : 4);
     const cudaError_t e = FAASMOE_BY_SHAPE(run_balance, b.E, wide, b.bf16_logits, p, st);
     if (e != cudaSuccess || p.blocks == 1) return e;

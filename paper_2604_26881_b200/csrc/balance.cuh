@@ -30,6 +30,7 @@ struct BalanceArgs {
     float* parts;                     // [blocks][M][record]
     int blocks;                       // blocks per model
     int chunk;                        // tokens that a warp lists at once
+    int warps;                        // of a block
 };
 
 struct GateGradArgs {
