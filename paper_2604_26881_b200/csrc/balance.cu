@@ -48,6 +48,10 @@ __device__ __forceinline__ float group_max(float v)
 template <int L, int VW>
 __device__ __forceinline__ int expert_of(int sub, int i) { return ((i / VW) * L + sub) * VW + i % VW; }
 
+// VW logits of a row as one load (VW > 1: rows hold whole vectors of 8 or 16 bytes, on their boundaries).
+template <int VW, typename TL>
+struct alignas(sizeof(TL) * VW) Vec { TL v[VW]; };
+
 // This lane's 16 logits of a row as they are, in pairs, -inf where there is no expert.
 template <int L, int VW, typename TL>
 __device__ __forceinline__ void load_row(const TL* row, int E, int sub, bool live, float2 (&z)[kC / 2])
@@ -55,19 +59,70 @@ __device__ __forceinline__ void load_row(const TL* row, int E, int sub, bool liv
     float* const f = reinterpret_cast<float*>(z);
 #pragma unroll
     for (int q = 0; q < kC / VW; ++q) {
-        const int e0 = (q * L + sub) * VW, n = live ? E - e0 : 0;
-        if (VW > 1 && n >= VW) {
-            const uint4 u = *reinterpret_cast<const uint4*>(row + e0);
-            TL v[VW];
-            memcpy(v, &u, sizeof(v) < sizeof(u) ? sizeof(v) : sizeof(u));
+        const int e0 = (q * L + sub) * VW;
+        if (live && e0 < E) {
+            const Vec<VW, TL> u = *reinterpret_cast<const Vec<VW, TL>*>(row + e0);
 #pragma unroll
-            for (int j = 0; j < VW; ++j) f[q * VW + j] = to_float(v[j]);
+            for (int j = 0; j < VW; ++j) f[q * VW + j] = to_float(u.v[j]);
         } else {
 #pragma unroll
-            for (int j = 0; j < VW; ++j) f[q * VW + j] = j < n ? to_float(row[e0 + j]) : -INFINITY;
+            for (int j = 0; j < VW; ++j) f[q * VW + j] = -INFINITY;
         }
     }
 }
+
+// Rows on their way: a lane's vectors of the next row but one and the next, copied into shared memory (kRowsAhead of them; nothing is
+// copied ahead where VW is 1, where they are loaded when they are needed).
+constexpr int kRowsAhead = 2;
+template <int L, int VW, typename TL>
+struct RowStage {
+    static constexpr int kVecs = kC / VW;
+    static constexpr bool kAhead = VW > 1;
+    Vec<VW, TL>* s;                                           // [ahead][vector][thread]
+    int at = 0;
+    static constexpr size_t bytes(int threads) { return kAhead ? (size_t)kRowsAhead * kC * sizeof(TL) * threads : 0; }
+    __device__ __forceinline__ explicit RowStage(void* shared) : s(reinterpret_cast<Vec<VW, TL>*>(shared) + threadIdx.x) {}
+    __device__ __forceinline__ void ask(const TL* row, int E, int sub, bool there)      // the row after those asked for
+    {
+        if (!kAhead) return;
+#pragma unroll
+        for (int q = 0; q < kVecs; ++q) {
+            const int e0 = (q * L + sub) * VW;
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(s + (at * kVecs + q) * blockDim.x);
+            if (there && e0 < E) {
+                if (sizeof(TL) * VW == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(row + e0) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(row + e0) : "memory");
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        at = at + 1 == kRowsAhead ? 0 : at + 1;
+    }
+    // the oldest row asked for (`at` is its place again); whole rows for all lanes of the warp
+    __device__ __forceinline__ void get(const TL* row, int E, int sub, bool live, float2 (&z)[kC / 2])
+    {
+        if (!kAhead) {
+            load_row<L, VW>(row, E, sub, live, z);
+            return;
+        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRowsAhead - 1) : "memory");
+        __syncwarp();
+        float* const f = reinterpret_cast<float*>(z);
+#pragma unroll
+        for (int q = 0; q < kVecs; ++q) {
+            const Vec<VW, TL> u = s[(at * kVecs + q) * blockDim.x];
+            const bool there = live && (q * L + sub) * VW < E;
+#pragma unroll
+            for (int j = 0; j < VW; ++j) f[q * VW + j] = there ? to_float(u.v[j]) : -INFINITY;
+        }
+    }
+    // expert e of the same row (any lane's, of this lane's token)
+    __device__ __forceinline__ float logit(const TL* row, int e, int sub) const
+    {
+        if (!kAhead) return to_float(row[e]);
+        const int vec = e / VW;
+        return to_float(s[(at * kVecs + vec / L) * (int)blockDim.x + vec % L - sub].v[e % VW]);
+    }
+};
 
 // Model of a token, or -1 if it takes no part.
 __device__ __forceinline__ int model_of(const RouterBatch& b, int t, bool report)
@@ -227,9 +282,9 @@ __device__ __forceinline__ void finish(const BalanceArgs& p, int m, const float*
     }
 }
 
-// blockIdx.y: model; the model's blocks take chunks of up to 32 tokens per warp in turn, list those of the model and sum up 32 / L of
-// them at a time.  A lane keeps the sums of its 16 experts.
-template <int L, int VW, bool SIGMOID, typename TL>
+// blockIdx.y: model; its blocks' warps take the tokens in turn, 32 / L at a time.  MULTI: chunks of 32 tokens, of which those of the
+// model are listed and summed up.  A lane keeps the sums of its 16 experts.
+template <int L, int VW, bool SIGMOID, bool MULTI, typename TL>
 __global__ void __launch_bounds__(32 * kSumWarps, 1)
 balance_kernel(const __grid_constant__ BalanceArgs p)
 {
@@ -252,55 +307,88 @@ balance_kernel(const __grid_constant__ BalanceArgs p)
 #pragma unroll
     for (int i = 0; i < kC / 2; ++i) acc[i] = both(0.f);
     int tokens = 0;
-    const int chunks = (b.T + p.chunk - 1) / p.chunk;
-    for (int chunk = blockIdx.x * (blockDim.x >> 5) + warp; chunk < chunks; chunk += gridDim.x * (blockDim.x >> 5)) {
-        const int t0 = chunk * p.chunk, t = t0 + lane;
-        const bool mine = lane < p.chunk && t < b.T && model_of(b, t, m == 0) == m;
-        const uint32_t set = __ballot_sync(kFull, mine);
-        const int count = __popc(set);
-        tokens += count;
-        if (mine) {
-            s_list[warp][__popc(set & ((1u << lane) - 1))] = (unsigned char)lane;
-            for (int j = 0; j < b.k; ++j) {
-                const int e = b.topk_idx[(size_t)t * b.k + j];
-                if (e >= 0 && e < b.E) atomicAdd(&s_count[e], 1);
-                else if (b.status) atomicOr(b.status, MOE_DEV_BAD_EXPERT);
+    extern __shared__ __align__(16) unsigned char s_rows[];
+    RowStage<L, VW, TL> stage(s_rows);
+    auto count_choice = [&](int e) {
+        if (e >= 0 && e < b.E) atomicAdd(&s_count[e], 1);
+        else if (b.status) atomicOr(b.status, MOE_DEV_BAD_EXPERT);
+    };
+    auto add_token = [&](const TL* logits, bool live, float2 (&z)[kC / 2]) {
+#pragma unroll
+        for (int i = 0; i < kC / 2; ++i) z[i] = exp_of(z[i]);
+        float x = group_sum<L>(total(z)), lse = live ? logf(x) : 0.f;
+        const bool far = live && !ordinary(x);
+        if (SIGMOID) {
+#pragma unroll
+            for (int i = 0; i < kC / 2; ++i) z[i] = mul2(z[i], rcp_of(add2(z[i], both(1.f))));
+            x = group_sum<L>(total(z));
+        }
+        const float inv = live && !far ? rcp(x) : 0.f;
+        if (__any_sync(kFull, far)) {
+            float2 again[kC / 2];
+            float lse2;
+            load_row<L, VW>(logits, b.E, sub, far, again);
+            shifted_shares<L, SIGMOID>(again, lse2);
+            if (far) {
+                lse = lse2;
+#pragma unroll
+                for (int i = 0; i < kC / 2; ++i) { acc[i] = add2(acc[i], again[i]); z[i] = both(0.f); }
             }
         }
-        __syncwarp();
-        for (int base = 0; base < count; base += G) {
-            const bool live = base + group < count;
-            const int row = t0 + (live ? s_list[warp][base + group] : 0);
-            const TL* const logits = (const TL*)b.logits + (size_t)row * b.ld;
+#pragma unroll
+        for (int i = 0; i < kC / 2; ++i) acc[i] = fma2(z[i], both(inv), acc[i]);
+        z2 = fmaf(lse, lse, z2);
+    };
+    const int warps = gridDim.x * (blockDim.x >> 5), me = blockIdx.x * (blockDim.x >> 5) + warp;
+    if (MULTI) {
+        const int chunks = (b.T + 31) / 32;
+        for (int chunk = me; chunk < chunks; chunk += warps) {
+            const int t0 = chunk * 32, t = t0 + lane;
+            const bool mine = t < b.T && model_of(b, t, m == 0) == m;
+            const uint32_t set = __ballot_sync(kFull, mine);
+            const int count = __popc(set);
+            tokens += count;
+            if (mine) s_list[warp][__popc(set & ((1u << lane) - 1))] = (unsigned char)lane;
+            __syncwarp();
+            auto row_of = [&](int base) {
+                const int n = base + group;
+                return (const TL*)b.logits + (size_t)(t0 + (n < count ? s_list[warp][n] : 0)) * b.ld;
+            };
+            for (int r = 0; r < kRowsAhead; ++r) stage.ask(row_of(r * G), b.E, sub, r * G + group < count);
+            if (mine)
+                for (int j = 0; j < b.k; ++j) count_choice(b.topk_idx[(size_t)t * b.k + j]);
+            for (int base = 0; base < count; base += G) {
+                const bool live = base + group < count;
+                const TL* const logits = row_of(base);
+                float2 z[kC / 2];
+                stage.get(logits, b.E, sub, live, z);
+                add_token(logits, live, z);
+                stage.ask(row_of(base + kRowsAhead * G), b.E, sub, base + kRowsAhead * G + group < count);
+            }
+            if (RowStage<L, VW, TL>::kAhead) asm volatile("cp.async.wait_group 0;" ::: "memory");
+            stage.at = 0;
+            __syncwarp();
+        }
+    } else {
+        const int steps = (b.T + G - 1) / G;
+        auto row_of = [&](int step) { return (const TL*)b.logits + (size_t)(step * G + group) * b.ld; };
+        for (int r = 0; r < kRowsAhead; ++r) {
+            const int step = me + r * warps;
+            stage.ask(row_of(step < steps ? step : 0), b.E, sub, step < steps && step * G + group < b.T);
+        }
+        for (int step = me; step < steps; step += warps) {
+            const int t = step * G + group, next = step + kRowsAhead * warps;
+            const bool live = t < b.T && model_of(b, t, sub == 0) == 0;
+            tokens += __popc(__ballot_sync(kFull, live && sub == 0));
+            if (live)
+                for (int j = sub; j < b.k; j += L) count_choice(b.topk_idx[(size_t)t * b.k + j]);
             float2 z[kC / 2];
-            load_row<L, VW>(logits, b.E, sub, live, z);
-#pragma unroll
-            for (int i = 0; i < kC / 2; ++i) z[i] = exp_of(z[i]);
-            float x = group_sum<L>(total(z)), lse = live ? logf(x) : 0.f;
-            const bool far = live && !ordinary(x);
-            if (SIGMOID) {
-#pragma unroll
-                for (int i = 0; i < kC / 2; ++i) z[i] = mul2(z[i], rcp_of(add2(z[i], both(1.f))));
-                x = group_sum<L>(total(z));
-            }
-            const float inv = live && !far ? rcp(x) : 0.f;
-            if (__any_sync(kFull, far)) {
-                float2 again[kC / 2];
-                float lse2;
-                load_row<L, VW>(logits, b.E, sub, far, again);
-                shifted_shares<L, SIGMOID>(again, lse2);
-                if (far) {
-                    lse = lse2;
-#pragma unroll
-                    for (int i = 0; i < kC / 2; ++i) { acc[i] = add2(acc[i], again[i]); z[i] = both(0.f); }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kC / 2; ++i) acc[i] = fma2(z[i], both(inv), acc[i]);
-            z2 = fmaf(lse, lse, z2);
+            stage.get(row_of(step), b.E, sub, live, z);
+            add_token(row_of(step), live, z);
+            stage.ask(row_of(next < steps ? next : 0), b.E, sub, next < steps && next * G + group < b.T);
         }
-        __syncwarp();
     }
+    if (RowStage<L, VW, TL>::kAhead) asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
     for (int o = L; o < 32; o <<= 1) {
 #pragma unroll
@@ -316,17 +404,17 @@ balance_kernel(const __grid_constant__ BalanceArgs p)
     }
     if (lane == 0) { s_z[warp] = z2; s_n[warp] = tokens; }
     __syncthreads();
-    const int Ep = padded(b.E), warps = blockDim.x >> 5;
+    const int Ep = padded(b.E), own = blockDim.x >> 5;
     for (int e = threadIdx.x; e < Ep; e += blockDim.x) {
         float sum = 0.f;
-        for (int w = 0; w < warps; ++w) sum += s_p[w][e];
+        for (int w = 0; w < own; ++w) sum += s_p[w][e];
         s_rec[e] = sum;
         s_rec[Ep + e] = __int_as_float(s_count[e]);
     }
     if (threadIdx.x == 0) {
         float sum = 0.f;
         int n = 0;
-        for (int w = 0; w < warps; ++w) { sum += s_z[w]; n += s_n[w]; }
+        for (int w = 0; w < own; ++w) { sum += s_z[w]; n += s_n[w]; }
         s_rec[2 * Ep] = sum;
         s_rec[2 * Ep + 1] = __int_as_float(n);
     }
@@ -352,26 +440,31 @@ balance_finish_kernel(const BalanceArgs p)
 
 // ---------------------------------------------------------------------------------------------------------------------
 
+// A token's choices, L of them side by side, with their weights' gradients (-1: none).
+template <int L>
+__device__ __forceinline__ void load_choices(const GateGradArgs& p, int t, int m, int sub, int (&id)[L < 8 ? 2 : 1], float (&gw)[L < 8 ? 2 : 1])
+{
+#pragma unroll
+    for (int q = 0; q < (L < 8 ? 2 : 1); ++q) {
+        const int j = sub + q * L;
+        id[q] = -1; gw[q] = 0.f;
+        if (p.d_w && m >= 0 && j < p.b.k) {
+            id[q] = p.b.topk_idx[(size_t)t * p.b.k + j];
+            gw[q] = p.d_w[(size_t)t * p.b.k + j] * p.scale;
+        }
+    }
+}
+
 // One step of a warp: the gradients of the tokens of its groups of L lanes.  FAR: those whose exponentials need a shift (`todo`);
 // otherwise all but those, which are returned.  f: the model's counts if there is one model, else they are looked up.
 template <int L, int VW, bool SIGMOID, bool MULTI, bool FAR, typename TL>
-__device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add, const float2 (&f1)[kC / 2], float coef1, float z1)
+__device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add, const float2 (&f1)[kC / 2], float coef1, float z1,
+                                          RowStage<L, VW, TL>* stage, int (&id)[L < 8 ? 2 : 1], float (&gw)[L < 8 ? 2 : 1])
 {
     constexpr int J = L < 8 ? 2 : 1;                          // chosen experts of a lane: j = sub and sub + L
     const RouterBatch& b = p.b;
     const bool live = m >= 0;
     const TL* const logits = (const TL*)b.logits + (size_t)t * b.ld;
-    int id[J];
-    float gw[J];
-#pragma unroll
-    for (int q = 0; q < J; ++q) {
-        const int j = sub + q * L;
-        id[q] = -1; gw[q] = 0.f;
-        if (p.d_w && live && j < b.k) {
-            id[q] = b.topk_idx[(size_t)t * b.k + j];
-            gw[q] = p.d_w[(size_t)t * b.k + j] * p.scale;
-        }
-    }
     float coef = coef1, cz = z1;
     float2 f[kC / 2];
     if (MULTI) {
@@ -383,7 +476,8 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
     float2 e[kC / 2], r[kS], s[kSF];                          // exponentials; 1 - s; s
     float inv, lse, share_inv, from = 0.f, ref = 0.f;
     bool far = false;
-    load_row<L, VW>(logits, b.E, sub, live, e);
+    if (FAR) load_row<L, VW>(logits, b.E, sub, live, e);
+    else stage->get(logits, b.E, sub, live, e);
     if (MULTI) {
 #pragma unroll
         for (int i = 0; i < kC; ++i) {
@@ -391,7 +485,6 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
             reinterpret_cast<float*>(f)[i] = live && p.d_loss && at < b.E ? (float)p.counts[(size_t)m * b.E + at] : 0.f;
         }
     }
-    // (a token's choices are as many as its lanes take; their logits are in the caches now)
     float zj[J];
 #pragma unroll
     for (int q = 0; q < J; ++q) {
@@ -399,7 +492,7 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
             if (b.status) atomicOr(b.status, MOE_DEV_BAD_EXPERT);
             id[q] = -1;
         }
-        zj[q] = id[q] >= 0 ? to_float(logits[id[q]]) : -INFINITY;
+        zj[q] = id[q] >= 0 ? (FAR ? to_float(logits[id[q]]) : stage->logit(logits, id[q], sub)) : -INFINITY;
     }
     if constexpr (FAR) {
         const Shifted<L, SIGMOID> x(e);
@@ -554,18 +647,11 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
         TL* const row = (TL*)p.d_logits + (size_t)t * p.ld_d;
 #pragma unroll
         for (int q = 0; q < kC / VW; ++q) {
-            const int e0 = (q * L + sub) * VW, n = b.E - e0;
-            TL v[VW];
+            const int e0 = (q * L + sub) * VW;
+            Vec<VW, TL> u;
 #pragma unroll
-            for (int j = 0; j < VW; ++j) v[j] = (TL)(live ? reinterpret_cast<const float*>(d)[q * VW + j] : 0.f);
-            if (VW > 1 && n >= VW) {
-                uint4 u;
-                memcpy(&u, v, sizeof(v) < sizeof(u) ? sizeof(v) : sizeof(u));
-                *reinterpret_cast<uint4*>(row + e0) = u;
-            } else {
-#pragma unroll
-                for (int j = 0; j < VW; ++j) if (j < n) row[e0 + j] = v[j];
-            }
+            for (int j = 0; j < VW; ++j) u.v[j] = (TL)(live ? reinterpret_cast<const float*>(d)[q * VW + j] : 0.f);
+            if (e0 < b.E) *reinterpret_cast<Vec<VW, TL>*>(row + e0) = u;
         }
     }
     return far;
@@ -573,8 +659,11 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
 template <int L, int VW, bool SIGMOID, typename TL>
 __device__ __noinline__ void grad_step_far(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add)
 {
-    const float2 none[kC / 2] = {};                                // (looked up: what a call may look into does not stay in registers)
-    grad_step<L, VW, SIGMOID, true, true, TL>(p, t, m, sub, group, todo, add, none, 0.f, 0.f);
+    const float2 none[kC / 2] = {};                           // (looked up: what a call may look into does not stay in registers)
+    int id[L < 8 ? 2 : 1];
+    float gw[L < 8 ? 2 : 1];
+    load_choices<L>(p, t, m, sub, id, gw);
+    grad_step<L, VW, SIGMOID, true, true, TL>(p, t, m, sub, group, todo, add, none, 0.f, 0.f, nullptr, id, gw);
 }
 
 template <int L, int VW, bool SIGMOID, bool MULTI, typename TL>
@@ -602,60 +691,113 @@ gate_grad_kernel(const __grid_constant__ GateGradArgs p)
         const int e = expert_of<L, VW>(sub, i);
         reinterpret_cast<float*>(f)[i] = !MULTI && p.d_loss && e < b.E ? (float)p.counts[e] : 0.f;
     }
-    const int steps = (b.T + G - 1) / G;
-    for (int step = blockIdx.x * kWarps + warp; step < steps; step += gridDim.x * kWarps) {
-        const int t = step * G + group;
-        const int m = t < b.T ? model_of(b, t, sub == 0) : -1;
-        const bool far = grad_step<L, VW, SIGMOID, MULTI, false, TL>(p, t, m, sub, group, false, add, f, coef, cz);
+    const int steps = (b.T + G - 1) / G, hop = gridDim.x * kWarps;
+    int step = blockIdx.x * kWarps + warp;
+    if (step >= steps) return;
+    extern __shared__ __align__(16) unsigned char s_rows[];
+    RowStage<L, VW, TL> stage(s_rows);
+    auto row_of = [&](int at) { return (const TL*)b.logits + (size_t)(at < steps ? at * G + group : 0) * b.ld; };
+    auto there = [&](int at) { return at < steps && at * G + group < b.T; };
+    for (int r = 0; r < kRowsAhead; ++r) stage.ask(row_of(step + r * hop), b.E, sub, there(step + r * hop));
+    // (rows are asked for two steps ahead, what a token is and its choices one step)
+    int m = there(step) ? model_of(b, step * G + group, sub == 0) : -1;
+    int id[L < 8 ? 2 : 1];
+    float gw[L < 8 ? 2 : 1];
+    load_choices<L>(p, step * G + group, m, sub, id, gw);
+    for (; step < steps; step += hop) {
+        const int t = step * G + group, next = t + hop * G;
+        const int m2 = there(step + hop) ? model_of(b, next, sub == 0) : -1;
+        int id2[L < 8 ? 2 : 1];
+        float gw2[L < 8 ? 2 : 1];
+        load_choices<L>(p, next, m2, sub, id2, gw2);
+        const bool far = grad_step<L, VW, SIGMOID, MULTI, false, TL>(p, t, m, sub, group, false, add, f, coef, cz, &stage, id, gw);
         if (__any_sync(kFull, far)) grad_step_far<L, VW, SIGMOID, TL>(p, t, m, sub, group, far, add);
+        __syncwarp();                                         // (the row's place is free: every lane has read its choices' logits)
+        stage.ask(row_of(step + kRowsAhead * hop), b.E, sub, there(step + kRowsAhead * hop));
+        m = m2;
+#pragma unroll
+        for (int q = 0; q < (L < 8 ? 2 : 1); ++q) { id[q] = id2[q]; gw[q] = gw2[q]; }
     }
+    if (RowStage<L, VW, TL>::kAhead) asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-bool wide_rows(const void* p, int64_t ld, int size) { return (uintptr_t)p % 16 == 0 && ld * size % 16 == 0; }
+// logits of a vector: rows of whole vectors on their boundaries, of 16 bytes or (bf16) of 8, else single ones
+int vector_of(const RouterBatch& b, const void* more, int64_t ld_more)
+{
+    const int size = b.bf16_logits ? 2 : 4;
+    auto fits = [&](const void* q, int64_t ld, int bytes) { return !q || ((uintptr_t)q % bytes == 0 && ld * size % bytes == 0); };
+    for (int bytes = 16; bytes >= 4 * size; bytes /= 2)
+        if (b.E % (bytes / size) == 0 && fits(b.logits, b.ld, bytes) && fits(more, ld_more, bytes)) return bytes / size;
+    return 1;
+}
 
-// Tokens that a warp of balance_kernel lists at once (with several models only those of one are summed up), and its blocks per model.
-struct BalanceShape { int chunk, warps, blocks; };
+// Warps and blocks (per model) of balance_kernel: one block as long as its warps need a step or two, which then writes the outputs
+// itself; beyond, as many as there are SMs, of 32 warps each, which leave records for one more launch.
+struct BalanceShape { int warps, blocks; };
 BalanceShape balance_shape(int T, int E, int M)
 {
+    const int G = M > 1 ? 32 : 32 / (E <= 64 ? 4 : (E <= 128 ? 8 : 16)), steps = (T + G - 1) / G;
     BalanceShape s;
-    s.chunk = 32 / (E <= 64 ? 4 : (E <= 128 ? 8 : 16));
-    while (s.chunk < 32 && (M > 1 || T / s.chunk > 148 * kSumWarps)) s.chunk *= 2;
-    const int chunks = (T + s.chunk - 1) / s.chunk;
-    // one block finishes by itself; several leave records, which one more launch adds up
-    s.warps = chunks <= kSumWarps ? (chunks < 2 ? 2 : chunks) : (chunks < 148 * 8 ? 8 : kSumWarps);      // (two: a lane for four experts)
+    s.warps = steps <= 2 ? 2 : (steps < kSumWarps ? steps : kSumWarps);       // (two: a lane for four experts)
+    if (steps > 2 * kSumWarps && steps < 148 * kSumWarps) s.warps = steps <= 148 * 8 ? 8 : (steps <= 148 * 16 ? 16 : kSumWarps);
     int most = 148 / M;
     if (most < 1) most = 1;
-    const int all = (chunks + s.warps - 1) / s.warps;
-    s.blocks = all < 1 ? 1 : (all < most ? all : most);
+    const int all = steps <= 2 * kSumWarps ? 1 : (steps + s.warps - 1) / s.warps;
+    s.blocks = all < most ? all : most;
     return s;
 }
 
+// the opt-in to large dynamic shared memory is a per-device attribute of a kernel
+template <typename K>
+cudaError_t allow_smem(K kern, size_t bytes, bool (&done)[kMaxDevices])
+{
+    if (bytes <= 8 * 1024) return cudaSuccess;               // (with the static arrays below the 48 KB that need no leave)
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    if (done[dev]) return cudaSuccess;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    if (e == cudaSuccess) done[dev] = true;
+    return e;
+}
+
+template <int L, int VW, bool SIGMOID, bool MULTI, typename TL>
+cudaError_t run_balance_kernel(const BalanceArgs& p, cudaStream_t st)
+{
+    static bool ok[kMaxDevices] = {false};
+    const size_t smem = RowStage<L, VW, TL>::bytes(32 * p.warps);
+    const cudaError_t e = allow_smem(balance_kernel<L, VW, SIGMOID, MULTI, TL>, smem, ok);
+    return e != cudaSuccess ? e : launch_pdl(balance_kernel<L, VW, SIGMOID, MULTI, TL>, dim3(p.blocks, p.b.M), dim3(32 * p.warps), smem, st, p);
+}
 template <int L, int VW, typename TL>
 cudaError_t run_balance(const BalanceArgs& p, cudaStream_t st)
 {
-    const dim3 grid(p.blocks, p.b.M), block(32 * p.warps);
-    return p.b.score == MOE_SCORE_SIGMOID ? launch_pdl(balance_kernel<L, VW, true, TL>, grid, block, 0, st, p)
-                                          : launch_pdl(balance_kernel<L, VW, false, TL>, grid, block, 0, st, p);
+    if (p.b.score == MOE_SCORE_SIGMOID) return p.b.M > 1 ? run_balance_kernel<L, VW, true, true, TL>(p, st) : run_balance_kernel<L, VW, true, false, TL>(p, st);
+    return p.b.M > 1 ? run_balance_kernel<L, VW, false, true, TL>(p, st) : run_balance_kernel<L, VW, false, false, TL>(p, st);
+}
+template <int L, int VW, bool SIGMOID, bool MULTI, typename TL>
+cudaError_t run_grad_kernel(const GateGradArgs& p, cudaStream_t st)
+{
+    static bool ok[kMaxDevices] = {false};
+    const int steps = (p.b.T + 32 / L - 1) / (32 / L), all = (steps + kWarps - 1) / kWarps, most = 148 * 2;
+    const size_t smem = RowStage<L, VW, TL>::bytes(32 * kWarps);
+    const cudaError_t e = allow_smem(gate_grad_kernel<L, VW, SIGMOID, MULTI, TL>, smem, ok);
+    return e != cudaSuccess ? e : launch_pdl(gate_grad_kernel<L, VW, SIGMOID, MULTI, TL>, dim3(all < most ? all : most), dim3(32 * kWarps), smem, st, p);
 }
 template <int L, int VW, typename TL>
 cudaError_t run_grad(const GateGradArgs& p, cudaStream_t st)
 {
-    const int steps = (p.b.T + 32 / L - 1) / (32 / L), all = (steps + kWarps - 1) / kWarps, most = 148 * 4;
-    const dim3 grid(all < most ? all : most), block(32 * kWarps);
-    if (p.b.score == MOE_SCORE_SIGMOID)
-        return p.b.M > 1 ? launch_pdl(gate_grad_kernel<L, VW, true, true, TL>, grid, block, 0, st, p)
-                         : launch_pdl(gate_grad_kernel<L, VW, true, false, TL>, grid, block, 0, st, p);
-    return p.b.M > 1 ? launch_pdl(gate_grad_kernel<L, VW, false, true, TL>, grid, block, 0, st, p)
-                     : launch_pdl(gate_grad_kernel<L, VW, false, false, TL>, grid, block, 0, st, p);
+    if (p.b.score == MOE_SCORE_SIGMOID) return p.b.M > 1 ? run_grad_kernel<L, VW, true, true, TL>(p, st) : run_grad_kernel<L, VW, true, false, TL>(p, st);
+    return p.b.M > 1 ? run_grad_kernel<L, VW, false, true, TL>(p, st) : run_grad_kernel<L, VW, false, false, TL>(p, st);
 }
 // (a macro: the shapes of both kernels)
-#define FAASMOE_BY_SHAPE(run, E, wide, bf, ...)                                                                            \
-    ((E) <= 64 ? ((bf) ? ((wide) ? run<4, 8, bf16>(__VA_ARGS__) : run<4, 1, bf16>(__VA_ARGS__))                            \
-                       : ((wide) ? run<4, 4, float>(__VA_ARGS__) : run<4, 1, float>(__VA_ARGS__)))                         \
-   : (E) <= 128 ? ((bf) ? ((wide) ? run<8, 8, bf16>(__VA_ARGS__) : run<8, 1, bf16>(__VA_ARGS__))                           \
-                        : ((wide) ? run<8, 4, float>(__VA_ARGS__) : run<8, 1, float>(__VA_ARGS__)))                        \
-                : ((bf) ? ((wide) ? run<16, 8, bf16>(__VA_ARGS__) : run<16, 1, bf16>(__VA_ARGS__))                         \
-                        : ((wide) ? run<16, 4, float>(__VA_ARGS__) : run<16, 1, float>(__VA_ARGS__))))
+#define FAASMOE_BY_VECTOR(run, L, vw, bf, ...)                                                                                      \
+    ((bf) ? ((vw) == 8 ? run<L, 8, bf16>(__VA_ARGS__) : (vw) == 4 ? run<L, 4, bf16>(__VA_ARGS__) : run<L, 1, bf16>(__VA_ARGS__))    \
+          : ((vw) == 4 ? run<L, 4, float>(__VA_ARGS__) : run<L, 1, float>(__VA_ARGS__)))
+#define FAASMOE_BY_SHAPE(run, E, vw, bf, ...)                                                                                       \
+    ((E) <= 64 ? FAASMOE_BY_VECTOR(run, 4, vw, bf, __VA_ARGS__)                                                                     \
+               : (E) <= 128 ? FAASMOE_BY_VECTOR(run, 8, vw, bf, __VA_ARGS__) : FAASMOE_BY_VECTOR(run, 16, vw, bf, __VA_ARGS__))
 
 }  // namespace
 
@@ -671,10 +813,9 @@ cudaError_t launch_balance(const BalanceArgs& in, cudaStream_t st)
     const RouterBatch& b = p.b;
     const BalanceShape s = balance_shape(b.T, b.E, b.M);
     p.blocks = s.blocks;
-    p.chunk = s.chunk;
     p.warps = s.warps;
-    const bool wide = wide_rows(b.logits, b.ld, b.bf16_logits ? 2 : 4);
-    const cudaError_t e = FAASMOE_BY_SHAPE(run_balance, b.E, wide, b.bf16_logits, p, st);
+    const int vw = vector_of(b, nullptr, 0);
+    const cudaError_t e = FAASMOE_BY_SHAPE(run_balance, b.E, vw, b.bf16_logits, p, st);
     if (e != cudaSuccess || p.blocks == 1) return e;
     return launch_pdl(balance_finish_kernel, dim3(b.M), dim3(1024), 0, st, p);
 }
@@ -682,9 +823,8 @@ cudaError_t launch_balance(const BalanceArgs& in, cudaStream_t st)
 cudaError_t launch_gate_grad(const GateGradArgs& p, cudaStream_t st)
 {
     const RouterBatch& b = p.b;
-    const int size = b.bf16_logits ? 2 : 4;
-    const bool wide = wide_rows(b.logits, b.ld, size) && wide_rows(p.d_logits, p.ld_d, size);
-    return FAASMOE_BY_SHAPE(run_grad, b.E, wide, b.bf16_logits, p, st);
+    const int vw = vector_of(b, p.d_logits, p.ld_d);
+    return FAASMOE_BY_SHAPE(run_grad, b.E, vw, b.bf16_logits, p, st);
 }
 
 }  // namespace faasmoe

@@ -29,7 +29,6 @@ struct BalanceArgs {
     float* z_loss;                    // [M] or null
     float* parts;                     // [blocks][M][record]
     int blocks;                       // blocks per model
-    int chunk;                        // tokens that a warp lists at once
     int warps;                        // of a block
 };
 
