@@ -81,7 +81,17 @@ struct RowStage {
     Vec<VW, TL>* s;                                           // [ahead][vector][thread]
     int at = 0;
     static constexpr size_t bytes(int threads) { return kAhead ? (size_t)kRowsAhead * kC * sizeof(TL) * threads : 0; }
-    __device__ __forceinline__ explicit RowStage(void* shared) : s(reinterpret_cast<Vec<VW, TL>*>(shared) + threadIdx.x) {}
+    __device__ __forceinline__ RowStage(void* shared, int E, int sub) : s(reinterpret_cast<Vec<VW, TL>*>(shared) + threadIdx.x)
+    {
+        if (!kAhead) return;
+#pragma unroll
+        for (int i = 0; i < kRowsAhead * kVecs; ++i) {        // (experts that are not there are never copied)
+            Vec<VW, TL> none;
+#pragma unroll
+            for (int j = 0; j < VW; ++j) none.v[j] = (TL)(-INFINITY);
+            s[i * blockDim.x] = none;
+        }
+    }
     __device__ __forceinline__ void ask(const TL* row, int E, int sub, bool there)      // the row after those asked for
     {
         if (!kAhead) return;
@@ -97,7 +107,8 @@ struct RowStage {
         asm volatile("cp.async.commit_group;" ::: "memory");
         at = at + 1 == kRowsAhead ? 0 : at + 1;
     }
-    // the oldest row asked for (`at` is its place again); whole rows for all lanes of the warp
+    // The oldest row asked for (`at` is its place again), whole for all lanes of the warp.  A token that is not `live` has some earlier
+    // row's logits here, or its own, and has to be left out of what they are used for.
     __device__ __forceinline__ void get(const TL* row, int E, int sub, bool live, float2 (&z)[kC / 2])
     {
         if (!kAhead) {
@@ -110,9 +121,8 @@ struct RowStage {
 #pragma unroll
         for (int q = 0; q < kVecs; ++q) {
             const Vec<VW, TL> u = s[(at * kVecs + q) * blockDim.x];
-            const bool there = live && (q * L + sub) * VW < E;
 #pragma unroll
-            for (int j = 0; j < VW; ++j) f[q * VW + j] = there ? to_float(u.v[j]) : -INFINITY;
+            for (int j = 0; j < VW; ++j) f[q * VW + j] = to_float(u.v[j]);
         }
     }
     // expert e of the same row (any lane's, of this lane's token)
@@ -226,7 +236,8 @@ constexpr int kFinishMost = 4096;       // floats of a finishing block's table
 // Adds up the records of a model (n of them, `stride` floats apart) in a fixed order and writes its outputs.
 __device__ __forceinline__ void finish(const BalanceArgs& p, int m, const float* rec, int n, size_t stride, float* s_p, int* s_c)
 {
-    __shared__ double s_red[2][32];
+    __shared__ float s_red[32];
+    __shared__ double s_loss[32];
     __shared__ int s_n[32];
     const int E = p.b.E, Ep = padded(E), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     int width = 1;                                            // lanes that share a record: one for four experts
@@ -247,38 +258,41 @@ __device__ __forceinline__ void finish(const BalanceArgs& p, int m, const float*
         *reinterpret_cast<float4*>(s_p + r * Ep + c) = sp;
         *reinterpret_cast<int4*>(s_c + r * Ep + c) = sc;
     }
-    double z = 0;
+    float z = 0.f;
     int tokens = 0;
     for (int x = tid; x < n; x += blockDim.x) {
-        z += (double)rec[x * stride + 2 * Ep];
+        z += rec[x * stride + 2 * Ep];
         tokens += __float_as_int(rec[x * stride + 2 * Ep + 1]);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) { z += __shfl_xor_sync(kFull, z, o); tokens += __shfl_xor_sync(kFull, tokens, o); }
-    if (lane == 0) { s_red[0][warp] = z; s_n[warp] = tokens; }
+    if (lane == 0) { s_red[warp] = z; s_n[warp] = tokens; }
     __syncthreads();
-    z = 0; tokens = 0;
-    for (int w = 0; w < warps; ++w) { z += s_red[0][w]; tokens += s_n[w]; }
-    const double over = tokens > 0 ? 1.0 / tokens : 0.0;
-    double part = 0;
+    z = 0.f; tokens = 0;
+    for (int w = 0; w < warps; ++w) { z += s_red[w]; tokens += s_n[w]; }
+    const float over = tokens > 0 ? 1.f / (float)tokens : 0.f;
+    double part = 0;                                          // (a sum over experts whose counts may be 10^8)
     for (int e = tid; e < E; e += blockDim.x) {
-        double sum = 0;
+        float sum = 0.f;
         int count = 0;
-        for (int i = 0; i < rows; ++i) { sum += (double)s_p[i * Ep + e]; count += s_c[i * Ep + e]; }
+        for (int i = 0; i < rows; ++i) { sum += s_p[i * Ep + e]; count += s_c[i * Ep + e]; }
         p.counts[(size_t)m * E + e] = count;
-        p.mean_prob[(size_t)m * E + e] = (float)(sum * over);
-        part += (double)count * sum * over;
+        sum *= over;
+        p.mean_prob[(size_t)m * E + e] = sum;
+        part += (double)count * (double)sum;
     }
+    if (warp * 32 < E) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(kFull, part, o);
-    if (lane == 0) s_red[1][warp] = part;
+        for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(kFull, part, o);
+        if (lane == 0) s_loss[warp] = part;
+    }
     __syncthreads();
     if (tid == 0) {
         part = 0;
-        for (int w = 0; w < warps; ++w) part += s_red[1][w];
+        for (int w = 0; w < warps && w * 32 < E; ++w) part += s_loss[w];
         p.tokens[m] = tokens;
-        p.loss[m] = (float)(part * over * E / p.b.k);
-        if (p.z_loss) p.z_loss[m] = (float)(z * over);
+        p.loss[m] = (float)part * over * ((float)E / (float)p.b.k);
+        if (p.z_loss) p.z_loss[m] = z * over;
     }
 }
 
@@ -308,36 +322,47 @@ balance_kernel(const __grid_constant__ BalanceArgs p)
     for (int i = 0; i < kC / 2; ++i) acc[i] = both(0.f);
     int tokens = 0;
     extern __shared__ __align__(16) unsigned char s_rows[];
-    RowStage<L, VW, TL> stage(s_rows);
+    RowStage<L, VW, TL> stage(s_rows, b.E, sub);
     auto count_choice = [&](int e) {
         if (e >= 0 && e < b.E) atomicAdd(&s_count[e], 1);
         else if (b.status) atomicOr(b.status, MOE_DEV_BAD_EXPERT);
     };
-    auto add_token = [&](const TL* logits, bool live, float2 (&z)[kC / 2]) {
+    // Rows that need a shift are left out here, and added in a pass of their own behind the others (in the same order every time):
+    // their code would cost the others registers.
+    bool any_far = false;
+    auto add_token = [&](bool live, float2 (&z)[kC / 2]) {
 #pragma unroll
         for (int i = 0; i < kC / 2; ++i) z[i] = exp_of(z[i]);
-        float x = group_sum<L>(total(z)), lse = live ? logf(x) : 0.f;
-        const bool far = live && !ordinary(x);
+        float x = group_sum<L>(total(z));
+        const bool fine = ordinary(x);
+        any_far |= live && !fine;
+        const float lse = live && fine ? __logf(x) : 0.f;
         if (SIGMOID) {
 #pragma unroll
             for (int i = 0; i < kC / 2; ++i) z[i] = mul2(z[i], rcp_of(add2(z[i], both(1.f))));
             x = group_sum<L>(total(z));
         }
-        const float inv = live && !far ? rcp(x) : 0.f;
-        if (__any_sync(kFull, far)) {
-            float2 again[kC / 2];
-            float lse2;
-            load_row<L, VW>(logits, b.E, sub, far, again);
-            shifted_shares<L, SIGMOID>(again, lse2);
-            if (far) {
-                lse = lse2;
+        const float inv = live ? rcp(x) : 0.f;
+        if (fine) {
 #pragma unroll
-                for (int i = 0; i < kC / 2; ++i) { acc[i] = add2(acc[i], again[i]); z[i] = both(0.f); }
-            }
+            for (int i = 0; i < kC / 2; ++i) acc[i] = fma2(z[i], both(inv), acc[i]);
         }
-#pragma unroll
-        for (int i = 0; i < kC / 2; ++i) acc[i] = fma2(z[i], both(inv), acc[i]);
         z2 = fmaf(lse, lse, z2);
+    };
+    auto add_far = [&](const TL* logits, bool live) {
+        float2 z[kC / 2], e[kC / 2];
+        load_row<L, VW>(logits, b.E, sub, live, z);
+#pragma unroll
+        for (int i = 0; i < kC / 2; ++i) e[i] = exp_of(z[i]);
+        const bool far = live && !ordinary(group_sum<L>(total(e)));
+        if (!__any_sync(kFull, far)) return;
+        float lse;
+        shifted_shares<L, SIGMOID>(z, lse);
+        if (far) {
+#pragma unroll
+            for (int i = 0; i < kC / 2; ++i) acc[i] = add2(acc[i], z[i]);
+            z2 = fmaf(lse, lse, z2);
+        }
     };
     const int warps = gridDim.x * (blockDim.x >> 5), me = blockIdx.x * (blockDim.x >> 5) + warp;
     if (MULTI) {
@@ -362,11 +387,15 @@ balance_kernel(const __grid_constant__ BalanceArgs p)
                 const TL* const logits = row_of(base);
                 float2 z[kC / 2];
                 stage.get(logits, b.E, sub, live, z);
-                add_token(logits, live, z);
+                add_token(live, z);
                 stage.ask(row_of(base + kRowsAhead * G), b.E, sub, base + kRowsAhead * G + group < count);
             }
             if (RowStage<L, VW, TL>::kAhead) asm volatile("cp.async.wait_group 0;" ::: "memory");
             stage.at = 0;
+            if (__any_sync(kFull, any_far))
+#pragma unroll 1
+                for (int base = 0; base < count; base += G) add_far(row_of(base), base + group < count);
+            any_far = false;
             __syncwarp();
         }
     } else {
@@ -376,17 +405,35 @@ balance_kernel(const __grid_constant__ BalanceArgs p)
             const int step = me + r * warps;
             stage.ask(row_of(step < steps ? step : 0), b.E, sub, step < steps && step * G + group < b.T);
         }
+        // (rows are asked for two steps ahead, whether a token takes part and its choices one step)
+        constexpr int J = L < 8 ? 2 : 1;
+        int id[J];
+        auto look = [&](int step, int (&ids)[J]) {
+            const int t = step * G + group;
+            const bool live = step < steps && t < b.T && model_of(b, t, sub == 0) == 0;
+#pragma unroll
+            for (int q = 0; q < J; ++q) ids[q] = live && sub + q * L < b.k ? b.topk_idx[(size_t)t * b.k + sub + q * L] : 0;
+            return live;
+        };
+        bool live_next = look(me, id);
         for (int step = me; step < steps; step += warps) {
-            const int t = step * G + group, next = step + kRowsAhead * warps;
-            const bool live = t < b.T && model_of(b, t, sub == 0) == 0;
+            const int next = step + kRowsAhead * warps;
+            const bool live = live_next;
             tokens += __popc(__ballot_sync(kFull, live && sub == 0));
-            if (live)
-                for (int j = sub; j < b.k; j += L) count_choice(b.topk_idx[(size_t)t * b.k + j]);
+#pragma unroll
+            for (int q = 0; q < J; ++q) if (live && sub + q * L < b.k) count_choice(id[q]);
+            live_next = look(step + warps, id);
             float2 z[kC / 2];
             stage.get(row_of(step), b.E, sub, live, z);
-            add_token(row_of(step), live, z);
+            add_token(live, z);
             stage.ask(row_of(next < steps ? next : 0), b.E, sub, next < steps && next * G + group < b.T);
         }
+        if (__any_sync(kFull, any_far))
+#pragma unroll 1
+            for (int step = me; step < steps; step += warps) {
+                const int t = step * G + group;
+                add_far(row_of(step), t < b.T && model_of(b, t, false) == 0);
+            }
     }
     if (RowStage<L, VW, TL>::kAhead) asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
@@ -450,7 +497,7 @@ __device__ __forceinline__ void load_choices(const GateGradArgs& p, int t, int m
         id[q] = -1; gw[q] = 0.f;
         if (p.d_w && m >= 0 && j < p.b.k) {
             id[q] = p.b.topk_idx[(size_t)t * p.b.k + j];
-            gw[q] = p.d_w[(size_t)t * p.b.k + j] * p.scale;
+            gw[q] = p.d_w[(size_t)t * p.b.k + j];             // (not multiplied here: that would wait for it)
         }
     }
 }
@@ -458,7 +505,7 @@ __device__ __forceinline__ void load_choices(const GateGradArgs& p, int t, int m
 // One step of a warp: the gradients of the tokens of its groups of L lanes.  FAR: those whose exponentials need a shift (`todo`);
 // otherwise all but those, which are returned.  f: the model's counts if there is one model, else they are looked up.
 template <int L, int VW, bool SIGMOID, bool MULTI, bool FAR, typename TL>
-__device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add, const float2 (&f1)[kC / 2], float coef1, float z1,
+__device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add, const float* counts1, float coef1, float z1,
                                           RowStage<L, VW, TL>* stage, int (&id)[L < 8 ? 2 : 1], float (&gw)[L < 8 ? 2 : 1])
 {
     constexpr int J = L < 8 ? 2 : 1;                          // chosen experts of a lane: j = sub and sub + L
@@ -466,7 +513,9 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
     const bool live = m >= 0;
     const TL* const logits = (const TL*)b.logits + (size_t)t * b.ld;
     float coef = coef1, cz = z1;
-    float2 f[kC / 2];
+#pragma unroll
+    for (int q = 0; q < J; ++q) gw[q] *= p.scale;
+    float2 f[MULTI ? kC / 2 : 1];
     if (MULTI) {
         const float n = live && (p.d_loss || p.d_z) ? (float)max(p.tokens[m], 1) : 1.f;
         coef = live && p.d_loss ? p.d_loss[m] * ((float)b.E / (float)b.k) / n / n : 0.f;
@@ -517,8 +566,8 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
         for (int i = 0; i < kC / 2; ++i) e[i] = exp_of(e[i]);
         const float x = group_sum<L>(total(e));
         far = live && !ordinary(x);
-        inv = live ? rcp(x) : 0.f;
-        lse = live ? logf(x) : 0.f;
+        inv = rcp(x);
+        lse = __logf(x);
         share_inv = inv;
         if (SIGMOID) {
             float2 sum = both(0.f);
@@ -528,7 +577,7 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
                 sum = fma2(e[i], r[i], sum);
             }
             const float all = group_sum<L>(sum.x + sum.y);    // (a shuffle: not under a condition)
-            share_inv = live ? rcp(all) : 0.f;
+            share_inv = rcp(all);
         }
     }
     float2 d[kC / 2];
@@ -632,15 +681,21 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
     }
     if (p.d_loss) {
         auto score = [&](int i) { return SIGMOID ? (FAR ? s[kSF > 1 ? i : 0] : mul2(e[i], r[kS > 1 ? i : 0])) : e[i]; };
+        // the model's counts (one model: as floats in shared memory)
+        auto count = [&](int i) {
+            if (MULTI) return f[MULTI ? i : 0];
+            if (VW > 1) return *reinterpret_cast<const float2*>(counts1 + expert_of<L, VW>(sub, 2 * i));
+            return make_float2(counts1[expert_of<L, VW>(sub, 2 * i)], counts1[expert_of<L, VW>(sub, 2 * i + 1)]);
+        };
         float2 sum = both(0.f);
 #pragma unroll
-        for (int i = 0; i < kC / 2; ++i) sum = fma2(MULTI ? f[i] : f1[i], score(i), sum);
+        for (int i = 0; i < kC / 2; ++i) sum = fma2(count(i), score(i), sum);
         const float mean = group_sum<L>(sum.x + sum.y) * share_inv, c = coef * share_inv;
 #pragma unroll
         for (int i = 0; i < kC / 2; ++i) {
             float2 x = mul2(score(i), both(c));
             if (SIGMOID) x = mul2(x, r[kS > 1 ? i : 0]);
-            d[i] = fma2(x, add2(MULTI ? f[i] : f1[i], both(-mean)), d[i]);
+            d[i] = fma2(x, add2(count(i), both(-mean)), d[i]);
         }
     }
     if (t < b.T && (FAR ? todo : !far)) {
@@ -659,19 +714,19 @@ __device__ __forceinline__ bool grad_step(const GateGradArgs& p, int t, int m, i
 template <int L, int VW, bool SIGMOID, typename TL>
 __device__ __noinline__ void grad_step_far(const GateGradArgs& p, int t, int m, int sub, int group, bool todo, float* add)
 {
-    const float2 none[kC / 2] = {};                           // (looked up: what a call may look into does not stay in registers)
     int id[L < 8 ? 2 : 1];
     float gw[L < 8 ? 2 : 1];
     load_choices<L>(p, t, m, sub, id, gw);
-    grad_step<L, VW, SIGMOID, true, true, TL>(p, t, m, sub, group, todo, add, none, 0.f, 0.f, nullptr, id, gw);
+    grad_step<L, VW, SIGMOID, true, true, TL>(p, t, m, sub, group, todo, add, nullptr, 0.f, 0.f, nullptr, id, gw);
 }
 
 template <int L, int VW, bool SIGMOID, bool MULTI, typename TL>
-__global__ void __launch_bounds__(32 * kWarps, 2)
+__global__ void __launch_bounds__(32 * kWarps, 3)
 gate_grad_kernel(const __grid_constant__ GateGradArgs p)
 {
     constexpr int G = 32 / L;                                 // tokens of a warp at a time
     __shared__ __align__(16) float s_add[kWarps][G][kC * L];  // what comes by way of the weights, at the chosen experts
+    __shared__ __align__(16) float s_counts[MULTI ? 4 : kC * L];
     const RouterBatch& b = p.b;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane % L, group = lane / L;
     float* const add = s_add[warp][group];
@@ -679,23 +734,19 @@ gate_grad_kernel(const __grid_constant__ GateGradArgs p)
     __syncwarp();
     pdl_wait();
     pdl_launch_dependents();
-    float2 f[kC / 2];
     float coef = 0.f, cz = 0.f;
     if (!MULTI) {
         const float n = p.d_loss || p.d_z ? (float)max(p.tokens[0], 1) : 1.f;
         if (p.d_loss) coef = p.d_loss[0] * ((float)b.E / (float)b.k) / n / n;
         if (p.d_z) cz = 2.f * p.d_z[0] / n;
-    }
-#pragma unroll
-    for (int i = 0; i < kC; ++i) {
-        const int e = expert_of<L, VW>(sub, i);
-        reinterpret_cast<float*>(f)[i] = !MULTI && p.d_loss && e < b.E ? (float)p.counts[e] : 0.f;
+        for (int e = threadIdx.x; e < kC * L; e += blockDim.x) s_counts[e] = p.d_loss && e < b.E ? (float)p.counts[e] : 0.f;
+        __syncthreads();
     }
     const int steps = (b.T + G - 1) / G, hop = gridDim.x * kWarps;
     int step = blockIdx.x * kWarps + warp;
     if (step >= steps) return;
     extern __shared__ __align__(16) unsigned char s_rows[];
-    RowStage<L, VW, TL> stage(s_rows);
+    RowStage<L, VW, TL> stage(s_rows, b.E, sub);
     auto row_of = [&](int at) { return (const TL*)b.logits + (size_t)(at < steps ? at * G + group : 0) * b.ld; };
     auto there = [&](int at) { return at < steps && at * G + group < b.T; };
     for (int r = 0; r < kRowsAhead; ++r) stage.ask(row_of(step + r * hop), b.E, sub, there(step + r * hop));
@@ -710,7 +761,7 @@ gate_grad_kernel(const __grid_constant__ GateGradArgs p)
         int id2[L < 8 ? 2 : 1];
         float gw2[L < 8 ? 2 : 1];
         load_choices<L>(p, next, m2, sub, id2, gw2);
-        const bool far = grad_step<L, VW, SIGMOID, MULTI, false, TL>(p, t, m, sub, group, false, add, f, coef, cz, &stage, id, gw);
+        const bool far = grad_step<L, VW, SIGMOID, MULTI, false, TL>(p, t, m, sub, group, false, add, s_counts, coef, cz, &stage, id, gw);
         if (__any_sync(kFull, far)) grad_step_far<L, VW, SIGMOID, TL>(p, t, m, sub, group, far, add);
         __syncwarp();                                         // (the row's place is free: every lane has read its choices' logits)
         stage.ask(row_of(step + kRowsAhead * hop), b.E, sub, there(step + kRowsAhead * hop));
@@ -731,18 +782,22 @@ int vector_of(const RouterBatch& b, const void* more, int64_t ld_more)
     return 1;
 }
 
-// Warps and blocks (per model) of balance_kernel: one block as long as its warps need a step or two, which then writes the outputs
-// itself; beyond, as many as there are SMs, of 32 warps each, which leave records for one more launch.
+// Warps and blocks (per model) of balance_kernel.  Up to 32 steps of a warp one block does all and writes the outputs itself; beyond,
+// as many blocks as there are SMs leave records, which one more launch adds up (2 to 3 us).  (us, one block of 8 warps / blocks of 4, 8,
+// 16, 32 warps, 148 at most: 128 x 60 4.9 / 6.4 6.8 5.3 6.6; 64 x 256 5.9 / 6.9 7.0 7.6 7.2; 512 x 60 8.0 / 6.6 6.7 7.6 9.6; 4096 x
+// 60 38 / 7.5 7.3 7.5 9.1; 32768 x 60 - / 11.1 11.0 11.4 10.9; 16384 x 256 - / 18.8 16.1 15.9 14.7; 65536 x 256 - / 44 36 32 24.)
 struct BalanceShape { int warps, blocks; };
 BalanceShape balance_shape(int T, int E, int M)
 {
     const int G = M > 1 ? 32 : 32 / (E <= 64 ? 4 : (E <= 128 ? 8 : 16)), steps = (T + G - 1) / G;
     BalanceShape s;
-    s.warps = steps <= 2 ? 2 : (steps < kSumWarps ? steps : kSumWarps);       // (two: a lane for four experts)
-    if (steps > 2 * kSumWarps && steps < 148 * kSumWarps) s.warps = steps <= 148 * 8 ? 8 : (steps <= 148 * 16 ? 16 : kSumWarps);
-    int most = 148 / M;
-    if (most < 1) most = 1;
-    const int all = steps <= 2 * kSumWarps ? 1 : (steps + s.warps - 1) / s.warps;
+    if (steps <= 32) {
+        s.warps = steps <= 2 ? 2 : (steps < 8 ? steps : 8);   // (two: a lane for four experts)
+        s.blocks = 1;
+        return s;
+    }
+    s.warps = steps <= 148 * 4 ? 4 : (steps <= 148 * 8 ? 8 : (steps <= 148 * 16 ? 16 : kSumWarps));
+    const int most = M < 148 ? 148 / M : 1, all = (steps + s.warps - 1) / s.warps;
     s.blocks = all < most ? all : most;
     return s;
 }
@@ -780,7 +835,7 @@ template <int L, int VW, bool SIGMOID, bool MULTI, typename TL>
 cudaError_t run_grad_kernel(const GateGradArgs& p, cudaStream_t st)
 {
     static bool ok[kMaxDevices] = {false};
-    const int steps = (p.b.T + 32 / L - 1) / (32 / L), all = (steps + kWarps - 1) / kWarps, most = 148 * 2;
+    const int steps = (p.b.T + 32 / L - 1) / (32 / L), all = (steps + kWarps - 1) / kWarps, most = 148 * 3;       // (80 registers)
     const size_t smem = RowStage<L, VW, TL>::bytes(32 * kWarps);
     const cudaError_t e = allow_smem(gate_grad_kernel<L, VW, SIGMOID, MULTI, TL>, smem, ok);
     return e != cudaSuccess ? e : launch_pdl(gate_grad_kernel<L, VW, SIGMOID, MULTI, TL>, dim3(all < most ? all : most), dim3(32 * kWarps), smem, st, p);
