@@ -10,6 +10,7 @@
 
 #include "cluster_ptx.cuh"
 #include "project_i8.cuh"
+#include "rows.cuh"
 
 namespace faasmoe {
 
@@ -30,7 +31,8 @@ constexpr int kRows = 128;              // rows of an operand tile of one CTA
 constexpr int kTile = kRows * kRow;     // its bytes
 constexpr int kMaxStages = 8;
 constexpr int kFewThreads = 352;        // warp 0: TMA (weights), 1: MMA, 2..9: epilogue, 10: TMA (tokens)
-constexpr int kMaxSmem = 212 * 1024;
+constexpr int kMaxSmem = 216 * 1024;    // dynamic; with the static arrays below the 227 KB of an SM
+constexpr int kHalfSmem = 108 * 1024;   // dynamic shared memory up to which two CTAs share an SM
 
 // instruction descriptor: int8 x int8 -> int32, K-major operands
 __device__ __forceinline__ uint32_t idesc_i8(int m, int n)
@@ -75,6 +77,7 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
     __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 2];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
+    __shared__ float s_xs[kRows];
     const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * kMaxStages, bar_done = bar_full + 16 * kMaxStages, bar_got = bar_done + 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int S = p.splits, nt = p.nt;
@@ -107,6 +110,22 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
     const uint32_t tmem = s_tmem;
     pdl_wait();
     pdl_launch_dependents();
+
+    // what the outputs are scaled with comes in beside the product: a thread's four (or one) weight rows, all tokens
+    const int vecs = nw / 4, per = kFewThreads / vecs;      // outputs in fours; tokens at a time
+    const int my_vec = threadIdx.x % vecs, my_row = threadIdx.x / vecs, my_n = n0 + rank * nw + 4 * my_vec;
+    float ws[4], add[4];
+    if (S > 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            ws[i] = my_n + i < p.N ? p.w_scale[my_n + i] : 0.f;
+            add[i] = p.bias && my_n + i < p.N ? p.bias[my_n + i] : 0.f;
+        }
+    }
+    if (warp >= 2 && warp < 6) {
+        const int t = threadIdx.x - 64;
+        s_xs[t] = t < rows ? p.x_scale[t0 + t] : 0.f;
+    }
 
     if (warp == 0 || warp == 10) {
         if (lane == 0) {
@@ -154,8 +173,9 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
         // thread <-> weight row (TMEM lane); two groups of four warps take every other 16 tokens each
         const int quarter = warp & 3, half = (warp - 2) >> 2, row = quarter * 32 + lane, n = n0 + row;
         const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
-        float ws = 0.f, bias = 0.f;
-        if (S == 1 && n < p.N) { ws = p.w_scale[n]; bias = p.bias ? p.bias[n] : 0.f; }
+        float scale = 0.f, bias = 0.f;
+        if (S == 1 && n < p.N) { scale = p.w_scale[n]; bias = p.bias ? p.bias[n] : 0.f; }
+        asm volatile("bar.sync 1, 256;" ::: "memory");      // (the tokens' scales are there)
         if (__all_sync(kFull, mbar_wait(bar_done, 0, &s_abort, status))) {
             tc_fence_after();
             int* const dst = own + (row / nw) * pitch + row % nw;
@@ -167,13 +187,17 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) if (c + i < rows) dst[(c + i) * nw] = (int)r[i];
                 } else if (n < p.N) {
+                    float b[16];
+                    if (p.base) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) b[i] = c + i < rows ? load_base(p, t0 + c + i, n) : 0.f;
+                    }
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         if (c + i < rows) {
-                            const int t = t0 + c + i;
-                            float v = (float)(int)r[i] * p.x_scale[t] * ws + bias;
-                            if (p.base) v += load_base(p, t, n);
-                            store_out(p, t, n, v);
+                            float v = fmaf((float)(int)r[i] * s_xs[c + i], scale, bias);
+                            if (p.base) v += b[i];
+                            store_out(p, t0 + c + i, n, v);
                         }
                 }
             }
@@ -194,15 +218,60 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
         __syncwarp();
         cluster_arrive_relaxed();                           // (waited for at the end: nobody leaves while its copies may still be on their way)
         if (!s_abort) {
-            for (int e = threadIdx.x; e < rows * nw; e += kFewThreads) {
-                const int r = e / nw, n = n0 + rank * nw + e % nw, t = t0 + r;
-                if (n >= p.N) continue;
-                int sum = 0;
-                for (int z = 0; z < S; ++z) sum += part[z * nt * nw + e];
-                float v = (float)sum * p.x_scale[t] * p.w_scale[n];
-                if (p.bias) v += p.bias[n];
-                if (p.base) v += load_base(p, t, n);
-                store_out(p, t, n, v);
+            // four neighbouring columns of a token a thread, of every per-th token; bases are asked for two tokens at a time
+            const int esz = p.out_f32 ? 4 : 2;
+            const bool vec = ((uintptr_t)p.out | (uintptr_t)p.base) % (4 * esz) == 0 && p.ldo % 4 == 0 && (!p.base || p.ldbase % 4 == 0) && my_n + 4 <= p.N;
+            if (my_row < per && my_n < p.N) {
+                for (int r0 = my_row; r0 < rows; r0 += 2 * per) {
+                    float v[2][4], b[2][4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int r = r0 + h * per;
+                        if (r >= rows || !p.base) continue;
+                        const size_t at = (size_t)(t0 + r) * p.ldbase + my_n;
+                        if (vec && p.out_f32) {
+                            const float4 f = *reinterpret_cast<const float4*>((const float*)p.base + at);
+                            b[h][0] = f.x; b[h][1] = f.y; b[h][2] = f.z; b[h][3] = f.w;
+                        } else if (vec) {
+                            const uint2 u = *reinterpret_cast<const uint2*>((const bf16*)p.base + at);
+                            b[h][0] = __uint_as_float(u.x << 16); b[h][1] = __uint_as_float(u.x & 0xffff0000u);
+                            b[h][2] = __uint_as_float(u.y << 16); b[h][3] = __uint_as_float(u.y & 0xffff0000u);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) b[h][i] = my_n + i < p.N ? load_base(p, t0 + r, my_n + i) : 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int r = r0 + h * per;
+                        if (r >= rows) continue;
+                        int4 sum = make_int4(0, 0, 0, 0);
+                        for (int z = 0; z < S; ++z) {
+                            const int4 q = *reinterpret_cast<const int4*>(part + (z * nt + r) * nw + 4 * my_vec);
+                            sum.x += q.x; sum.y += q.y; sum.z += q.z; sum.w += q.w;
+                        }
+                        const int s4[4] = {sum.x, sum.y, sum.z, sum.w};
+                        const float xs = s_xs[r];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            v[h][i] = fmaf((float)s4[i] * xs, ws[i], add[i]);
+                            if (p.base) v[h][i] += b[h][i];
+                        }
+                        const size_t at = (size_t)(t0 + r) * p.ldo + my_n;
+                        if (vec && p.out_f32) {
+                            *reinterpret_cast<float4*>((float*)p.out + at) = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
+                        } else if (vec) {
+                            uint2 u;
+                            __nv_bfloat162* const o = reinterpret_cast<__nv_bfloat162*>(&u);
+                            o[0] = __floats2bfloat162_rn(v[h][0], v[h][1]);
+                            o[1] = __floats2bfloat162_rn(v[h][2], v[h][3]);
+                            *reinterpret_cast<uint2*>((bf16*)p.out + at) = u;
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) if (my_n + i < p.N) store_out(p, t0 + r, my_n + i, v[h][i]);
+                        }
+                    }
+                }
             }
         }
         __syncwarp();
@@ -220,82 +289,97 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
 // Many tokens: 256 tokens x 256 weight rows per pair of CTAs (each holds 128 of either), pairs that walk over the tiles, two
 // accumulators of 256 TMEM columns so that a tile's epilogue runs behind the next tile's MMAs.
 constexpr int kManyTile = 256;
-constexpr int kManyStages = 5;
-constexpr int kManyStageBytes = 2 * kTile;
+constexpr int kManySlices = 2;                         // slices of K of a stage: its barriers are waited for half as often
+constexpr int kManyStages = 3;
+constexpr int kManyStageBytes = kManySlices * 2 * kTile;
 constexpr int kManyThreads = 352;                      // warp 0: TMA (weights), 1: MMA, 2..9: epilogue, 10: TMA (tokens)
-constexpr int kOutPitch = 36;                          // floats per row of a warp's staging area (32 columns, 16-byte rows)
+constexpr int kOutCols = 16;                           // columns of a warp's staging area
+constexpr int kOutPitch = kOutCols + 4;                // its floats per row (16-byte rows)
 constexpr int kOutStage = 8 * 32 * kOutPitch * (int)sizeof(float);
 
-// 32 tokens x 32 columns (from row t, column n) by a warp, out of its staging area, where the sums are scaled by their tokens: a
-// row's columns are read, scaled, added to and written by neighbouring lanes.
-template <typename T>
-__device__ __forceinline__ void write_block(const I8Args& p, const float* stage, int t, int n, int lane, bool vec)
+// Stores and loads of 32 bytes (whole sectors of L2) by a thread, or of 16.
+template <int BYTES>
+__device__ __forceinline__ void store_bytes(void* p, const uint32_t* r)
 {
-    constexpr int kPer = 16 / sizeof(T), kLanes = 32 / kPer;    // columns of a 16-byte vector; lanes per row, and vectors per lane
-    if (vec && n + 32 <= p.N) {
-        const int c = (lane % kLanes) * kPer;
-        float ws[kPer], add[kPer];
+    if (BYTES == 32)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+    else
+        asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+
+// 16 columns of a token by its thread (TMEM lane): scaled, added to and written.  A thread's 16 columns are one or two sectors of a
+// row, so they need not be put together with its neighbours' in shared memory, whose bandwidth the MMAs' operands take
+// (through shared memory, in 16-byte vectors of neighbouring lanes: 137 us for 16384 x 2048 -> 5632 instead of %%).
+template <typename T, int BYTES>
+__device__ __forceinline__ void write_columns(const I8Args& p, const uint32_t (&r)[16], float xs, const float* ws, const float* add, T* out, const T* base)
+{
+    float2 v[8];
 #pragma unroll
-        for (int j = 0; j < kPer; j += 4) {
-            const float4 f = __ldg(reinterpret_cast<const float4*>(p.w_scale + n + c + j));
-            ws[j] = f.x; ws[j + 1] = f.y; ws[j + 2] = f.z; ws[j + 3] = f.w;
-            const float4 g = p.bias ? __ldg(reinterpret_cast<const float4*>(p.bias + n + c + j)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            add[j] = g.x; add[j + 1] = g.y; add[j + 2] = g.z; add[j + 3] = g.w;
+    for (int j = 0; j < 4; ++j) {
+        const float4 w = reinterpret_cast<const float4*>(ws)[j];
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p.bias) a = reinterpret_cast<const float4*>(add)[j];
+        v[2 * j] = fma2(mul2(make_float2((float)(int)r[4 * j], (float)(int)r[4 * j + 1]), both(xs)), make_float2(w.x, w.y), make_float2(a.x, a.y));
+        v[2 * j + 1] = fma2(mul2(make_float2((float)(int)r[4 * j + 2], (float)(int)r[4 * j + 3]), both(xs)), make_float2(w.z, w.w), make_float2(a.z, a.w));
+    }
+    constexpr int kWords = 16 * sizeof(T) / 4;
+    uint32_t o[kWords];
+    if (p.base) {
+#pragma unroll
+        for (int j = 0; j < kWords; j += 4) {
+            const uint4 q = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(base) + j);
+            o[j] = q.x; o[j + 1] = q.y; o[j + 2] = q.z; o[j + 3] = q.w;
         }
-        uint4 q[kLanes];
-        if (p.base) {
 #pragma unroll
-            for (int i = 0; i < kLanes; ++i) {
-                const int r = t + i * (32 / kLanes) + lane / kLanes;
-                q[i] = r < p.T ? *reinterpret_cast<const uint4*>((const T*)p.base + (size_t)r * p.ldbase + n + c) : make_uint4(0, 0, 0, 0);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kLanes; ++i) {
-            const int r = i * (32 / kLanes) + lane / kLanes;
-            const float4* from = reinterpret_cast<const float4*>(stage + r * kOutPitch + c);
-            float v[kPer];
-#pragma unroll
-            for (int j = 0; j < kPer / 4; ++j) { const float4 f = from[j]; v[4 * j] = f.x; v[4 * j + 1] = f.y; v[4 * j + 2] = f.z; v[4 * j + 3] = f.w; }
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) v[j] = v[j] * ws[j] + add[j];
-            uint4 o;
-            if constexpr (sizeof(T) == 4) {
-                if (p.base) {
-                    v[0] += __uint_as_float(q[i].x); v[1] += __uint_as_float(q[i].y); v[2] += __uint_as_float(q[i].z); v[3] += __uint_as_float(q[i].w);
-                }
-                o = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-            } else {
-                if (p.base) {
-                    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&q[i]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) { const float2 f = __bfloat1622float2(h[j]); v[2 * j] += f.x; v[2 * j + 1] += f.y; }
-                }
-                __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&o);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-            }
-            if (t + r < p.T) *reinterpret_cast<uint4*>((T*)p.out + (size_t)(t + r) * p.ldo + n + c) = o;
-        }
-    } else if (n + lane < p.N) {
-        // rows that are not on 16-byte boundaries: a row's 32 columns at a time, eight rows' bases on their way at once
-        T* out = (T*)p.out + (size_t)t * p.ldo + n + lane;
-        const T* base = (const T*)p.base + (size_t)t * p.ldbase + n + lane;
-        const float ws = p.w_scale[n + lane], add = p.bias ? p.bias[n + lane] : 0.f;
-        const int rows = min(32, p.T - t);
-#pragma unroll 1
-        for (int r0 = 0; r0 < rows; r0 += 8) {
-            T b[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) b[i] = p.base && r0 + i < rows ? base[(r0 + i) * p.ldbase] : (T)0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (r0 + i < rows) {
-                    const float v = stage[(r0 + i) * kOutPitch + lane] * ws + add;
-                    out[(r0 + i) * p.ldo] = (T)(p.base ? v + (float)b[i] : v);
-                }
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (sizeof(T) == 4) v[j] = add2(v[j], make_float2(__uint_as_float(o[2 * j]), __uint_as_float(o[2 * j + 1])));
+            else v[j] = add2(v[j], make_float2(__uint_as_float(o[j] << 16), __uint_as_float(o[j] & 0xffff0000u)));
         }
     }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (sizeof(T) == 4) { o[2 * j] = __float_as_uint(v[j].x); o[2 * j + 1] = __float_as_uint(v[j].y); }
+        else { const __nv_bfloat162 h = __floats2bfloat162_rn(v[j].x, v[j].y); o[j] = reinterpret_cast<const uint32_t&>(h); }
+    }
+#pragma unroll
+    for (int j = 0; j < kWords; j += BYTES / 4) store_bytes<BYTES>(reinterpret_cast<uint32_t*>(out) + j, o + j);
+}
+
+// 32 tokens x 16 columns (from row t, column n) by a warp, out of its staging area, where the sums are scaled by their tokens: rows that
+// are not on 16-byte boundaries, and a matrix's last columns; two rows at a time, eight of their bases on their way at once.
+template <typename T>
+__device__ __forceinline__ void write_staged(const I8Args& p, const float* stage, int t, int n, int lane)
+{
+    const int c = lane % kOutCols, first = lane / kOutCols;
+    if (n + c >= p.N) return;
+    T* out = (T*)p.out + (size_t)(t + first) * p.ldo + n + c;
+    const T* base = (const T*)p.base + (size_t)(t + first) * p.ldbase + n + c;
+    const float ws = p.w_scale[n + c], add = p.bias ? p.bias[n + c] : 0.f;
+    const int rows = min(32, p.T - t);
+#pragma unroll 1
+    for (int r0 = first; r0 < rows; r0 += 16) {
+        T b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = p.base && r0 + 2 * i < rows ? base[(r0 - first + 2 * i) * p.ldbase] : (T)0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (r0 + 2 * i < rows) {
+                const float v = fmaf(stage[(r0 + 2 * i) * kOutPitch + c], ws, add);
+                out[(r0 - first + 2 * i) * p.ldo] = (T)(p.base ? v + (float)b[i] : v);
+            }
+    }
+}
+
+// The tile that is number i: strips of kStrip token tiles, a strip's tiles column by column, so that the tiles being worked on at one
+// time share their operands both ways (74 of them read 8 strips' tokens and 9 or 10 columns' weights, not all tokens' over again for
+// each column: 16384 tokens of 5632 are 92 MB, more than L2 holds for both of its halves).
+constexpr int kStrip = 8;
+__device__ __forceinline__ void place_of(long long i, int m_tiles, int n_tiles, int& m, int& n)
+{
+    const long long strip = i / ((long long)kStrip * n_tiles);
+    const int rest = (int)(i - strip * kStrip * n_tiles), high = min(kStrip, m_tiles - (int)strip * kStrip);
+    n = rest / high;
+    m = (int)strip * kStrip + rest - n * high;
 }
 
 __global__ void __launch_bounds__(kManyThreads, 1)
@@ -308,6 +392,7 @@ project_i8_many_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
     __shared__ __align__(8) uint64_t s_bars[2 * kManyStages + 4];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
+    __shared__ __align__(16) float s_scales[8][256];        // of a warp's columns: w_scale, bias
     const uint32_t bar_full = smem_u32(s_bars), bar_empty = bar_full + 8 * kManyStages, bar_tfull = bar_full + 16 * kManyStages, bar_tempty = bar_tfull + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
@@ -340,17 +425,20 @@ project_i8_many_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
             uint32_t stage = 0, phase = 0, armed = 0, armed_phase = 0;
             bool ok = true;
             for (long long tile = pair0; tile < total && ok; tile += pairs) {
-                const int n0 = (int)(tile / m_tiles) * kManyTile + rank * kRows, t0 = (int)(tile % m_tiles) * kManyTile + rank * kRows;
-                for (int ks = 0; ks < p.ksteps; ++ks) {
+                int m, n;
+                place_of(tile, m_tiles, n_tiles, m, n);
+                const int n0 = n * kManyTile + rank * kRows, t0 = m * kManyTile + rank * kRows;
+                for (int ks = 0; ks < p.ksteps; ks += kManySlices) {
                     if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, status)) { ok = false; break; }
                     const uint32_t sa = ring + stage * kManyStageBytes, full = bar_full + 8 * stage;
+                    const int slices = min(kManySlices, p.ksteps - ks);
                     if (warp == 0) {
                         armed |= 1u << stage;
                         armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
-                        if (leader) mbar_expect_tx(full, 2 * kManyStageBytes);
-                        tma_load_2d_pair(sa + kTile, &maps.w, full, ks * kRow, n0);
+                        if (leader) mbar_expect_tx(full, slices * 4 * kTile);
+                        for (int q = 0; q < slices; ++q) tma_load_2d_pair(sa + (2 * q + 1) * kTile, &maps.w, full, (ks + q) * kRow, n0);
                     } else {
-                        tma_load_2d_pair(sa, &maps.x, full, ks * kRow, t0);
+                        for (int q = 0; q < slices; ++q) tma_load_2d_pair(sa + 2 * q * kTile, &maps.x, full, (ks + q) * kRow, t0);
                     }
                     if (++stage == (uint32_t)kManyStages) { stage = 0; phase ^= 1; }
                 }
@@ -371,14 +459,19 @@ project_i8_many_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
                 if (!mbar_wait_cluster(bar_tempty + 8 * buf, ((it >> 1) & 1) ^ 1, &s_abort, status)) { ok = false; break; }
                 tc_fence_after();
                 uint32_t acc = 0;
-                for (int ks = 0; ks < p.ksteps; ++ks) {
+                for (int ks = 0; ks < p.ksteps; ks += kManySlices) {
                     if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, status)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t lo_a = smem_desc_lo(ring + stage * kManyStageBytes), lo_b = lo_a + (kTile >> 4);
+                    const uint32_t lo = smem_desc_lo(ring + stage * kManyStageBytes);
 #pragma unroll
-                    for (int kk = 0; kk < kRow / 32; ++kk) {
-                        umma_i8_pair(d, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, acc);
-                        acc = 1;
+                    for (int q = 0; q < kManySlices; ++q) {
+                        if (ks + q >= p.ksteps) break;
+                        const uint32_t lo_a = lo + q * (2 * kTile >> 4), lo_b = lo_a + (kTile >> 4);
+#pragma unroll
+                        for (int kk = 0; kk < kRow / 32; ++kk) {
+                            umma_i8_pair(d, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, acc);
+                            acc = 1;
+                        }
                     }
                     umma_commit_pair(bar_empty + 8 * stage);
                     if (++stage == (uint32_t)kManyStages) { stage = 0; phase ^= 1; }
@@ -392,37 +485,65 @@ project_i8_many_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const uint32_t tempty_leader = map_to_cta(bar_tempty, 0);
         const int esz = p.out_f32 ? 4 : 2;
-        const bool vec = (uintptr_t)p.out % 16 == 0 && p.ldo * esz % 16 == 0 && (!p.base || ((uintptr_t)p.base % 16 == 0 && p.ldbase * esz % 16 == 0)) &&
-                         (uintptr_t)p.w_scale % 16 == 0 && (uintptr_t)p.bias % 16 == 0;
+        // the boundaries that all rows of the outputs (and bases) are on
+        auto rows_on = [&](int bytes) {
+            return (uintptr_t)p.out % bytes == 0 && p.ldo * esz % bytes == 0 && (!p.base || ((uintptr_t)p.base % 16 == 0 && p.ldbase * esz % 16 == 0));
+        };
+        const bool by32 = rows_on(32), by16 = rows_on(16);
         float* const stage = reinterpret_cast<float*>(ring_ptr + kManyStages * kManyStageBytes) + (warp - 2) * 32 * kOutPitch;
+        float* const ws = s_scales[warp - 2], *const add = ws + 128;
         int it = 0;
         for (long long tile = pair0; tile < total; tile += pairs, ++it) {
-            const int n0 = (int)(tile / m_tiles) * kManyTile + half * 128, t = (int)(tile % m_tiles) * kManyTile + (int)rank * kRows + quarter * 32;
+            int m, nt;
+            place_of(tile, m_tiles, n_tiles, m, nt);
+            const int n0 = nt * kManyTile + half * 128, t = m * kManyTile + (int)rank * kRows + quarter * 32;
             const uint32_t buf = it & 1, from = tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16) + half * 128;
             const float xs = t + lane < p.T ? p.x_scale[t + lane] : 0.f;
+#pragma unroll
+            for (int i = lane; i < 128; i += 32) {          // (every lane needs all columns' scales)
+                const bool there = n0 + i < p.N;
+                ws[i] = there ? p.w_scale[n0 + i] : 0.f;
+                if (p.bias) add[i] = there ? p.bias[n0 + i] : 0.f;
+            }
+            __syncwarp();
             if (!__all_sync(kFull, mbar_wait(bar_tfull + 8 * buf, (it >> 1) & 1, &s_abort, status))) break;
             tc_fence_after();
+            const size_t row = (size_t)(t + lane);
 #pragma unroll 1
-            for (int c = 0; c < 128; c += 32) {
-                uint32_t r[32];
+            for (int c = 0; c < 128; c += kOutCols) {
+                uint32_t r[kOutCols];
                 tmem_ld16(from + c, r);
-                tmem_ld16(from + c + 16, r + 16);
                 tmem_ld_wait();
-                if (c == 96) {
+                if (c == 128 - kOutCols) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * buf);
                 }
-                if (n0 + c >= p.N || t >= p.T) continue;
+                const int n = n0 + c;
+                if (n >= p.N || t >= p.T) continue;
+                if (by16 && n + kOutCols <= p.N) {
+                    const size_t at = row * p.ldo + n, from_base = row * p.ldbase + n;
+                    if (t + lane >= p.T) {
+                    } else
+                    if (p.out_f32) {
+                        if (by32) write_columns<float, 32>(p, r, xs, ws + c, add + c, (float*)p.out + at, (const float*)p.base + from_base);
+                        else write_columns<float, 16>(p, r, xs, ws + c, add + c, (float*)p.out + at, (const float*)p.base + from_base);
+                    } else {
+                        if (by32) write_columns<bf16, 32>(p, r, xs, ws + c, add + c, (bf16*)p.out + at, (const bf16*)p.base + from_base);
+                        else write_columns<bf16, 16>(p, r, xs, ws + c, add + c, (bf16*)p.out + at, (const bf16*)p.base + from_base);
+                    }
+                    continue;
+                }
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < kOutCols / 4; ++i)
                     reinterpret_cast<float4*>(stage + lane * kOutPitch)[i] = make_float4((float)(int)r[4 * i] * xs, (float)(int)r[4 * i + 1] * xs,
                                                                                           (float)(int)r[4 * i + 2] * xs, (float)(int)r[4 * i + 3] * xs);
                 __syncwarp();
-                if (p.out_f32) write_block<float>(p, stage, t, n0 + c, lane, vec);
-                else write_block<bf16>(p, stage, t, n0 + c, lane, vec);
+                if (p.out_f32) write_staged<float>(p, stage, t, n, lane);
+                else write_staged<bf16>(p, stage, t, n, lane);
                 __syncwarp();
             }
+            __syncwarp();                                   // (the scales are read)
         }
     }
 
