@@ -23,8 +23,8 @@ __device__ int32_t g_taken;
 __global__ void take_status_kernel() { g_taken = atomicExch(&g_status, 0); }
 
 // TMEM: as in the projection in bf16, the CTAs of clusters that fit one SM together ask for 512 columns at most, so that an
-// allocation never waits for a cluster that waits for it: project_i8_kernel takes 128 columns at most and more than 12288
-// registers (five with 40 a thread do not fit beside one another), project_i8_many_kernel all columns and 198 KB of shared memory.
+// allocation never waits for a cluster that waits for it: project_i8_kernel takes 128 columns at most and 27 of an SM's 64 thousand
+// registers, project_i8_many_kernel all columns and 218 KB of shared memory.
 constexpr uint32_t kFull = 0xffffffffu;
 constexpr int kRow = 128;               // bytes of K of a slice: one row of a swizzled tile
 constexpr int kRows = 128;              // rows of an operand tile of one CTA
@@ -309,7 +309,7 @@ __device__ __forceinline__ void store_bytes(void* p, const uint32_t* r)
 
 // 16 columns of a token by its thread (TMEM lane): scaled, added to and written.  A thread's 16 columns are one or two sectors of a
 // row, so they need not be put together with its neighbours' in shared memory, whose bandwidth the MMAs' operands take
-// (through shared memory, in 16-byte vectors of neighbouring lanes: 137 us for 16384 x 2048 -> 5632 instead of %%).
+// (through shared memory, in 16-byte vectors of neighbouring lanes: 137 us for 16384 x 2048 -> 5632 instead of 133).
 template <typename T, int BYTES>
 __device__ __forceinline__ void write_columns(const I8Args& p, const uint32_t (&r)[16], float xs, const float* ws, const float* add, T* out, const T* base)
 {
@@ -586,6 +586,99 @@ cudaError_t allow_smem(K kern, bool (&done)[kMaxDevices])
 
 int div_up(int a, int b) { return (a + b - 1) / b; }
 
+// How many clusters of `size` CTAs of project_i8_kernel run at once, with one CTA per SM or two (the SMs of a cluster belong to one
+// GPC, so a few of each GPC stay unused).
+int cluster_room(int size, bool two)
+{
+    if (size == 1) return 148 * (two ? 2 : 1);
+    static int room[kMaxDevices][9][2] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return (two ? 256 : 112) / size;
+    int& n = room[dev][size][two];
+    if (n == 0) {
+        static bool allowed[kMaxDevices] = {false};
+        if (allow_smem(project_i8_kernel, allowed) != cudaSuccess) cudaGetLastError();         // (the query asks for that much)
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = size; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cfg.gridDim = dim3(size * 148); cfg.blockDim = dim3(kFewThreads); cfg.dynamicSmemBytes = two ? kHalfSmem : kMaxSmem;
+        cfg.attrs = &attr; cfg.numAttrs = 1;
+        int most = 0;
+        if (cudaOccupancyMaxActiveClusters(&most, project_i8_kernel, &cfg) != cudaSuccess || most < 1) {
+            cudaGetLastError();
+            most = (two ? 256 : 112) / size;                // (no answer: a cautious guess)
+        }
+        n = most;
+    }
+    return n;
+}
+
+// Stages and shared memory (returned) of project_i8_kernel with p.nt tokens a tile and p.splits parts of K; *two: two CTAs share an SM.
+int few_memory(I8Args& p, bool* two)
+{
+    const int stage = kTile + p.nt * kRow, want = div_up(p.ksteps, p.splits);
+    const int own = p.splits > 1 ? p.splits * (p.nt * (kRows / p.splits) + 16) * 4 : 0, got = p.splits > 1 ? p.nt * kRows * 4 : 0;
+    auto stages = [&](int bytes) {                          // the ring, or this CTA's own sums that are put together in it
+        const int room = bytes - 1024 - got;
+        int n = room / stage;
+        if (n > want) n = want;
+        if (n > 6) n = 6;
+        return room < own || n < 0 ? 0 : n;
+    };
+    // (three stages, or all there are, are enough for two CTAs that take turns)
+    const int half = stages(kHalfSmem);
+    *two = half >= 3 || (half >= 1 && half == want);
+    p.n_stages = *two ? half : stages(kMaxSmem);
+    p.scratch = p.n_stages * stage;
+    if (p.scratch < own) p.scratch = own;
+    return p.scratch + got + 1024;
+}
+
+// What a shape costs (us), a model fitted to 350 measured shapes of 1 to 1126 tokens, 1024 to 5632 rows and columns (off by 5 % in the
+// mean): the chain of launch, ids and exchange; slices of K one after the other; a tile's tokens, whose sums are exchanged; and what CTAs
+// that share an SM cost one another.  (us, of tokens a tile / parts of K: 1 token, 5632 -> 2048 16/2 10.2, 16/4 7.2, 16/8 6.1; 128 tokens,
+// 2048 -> 2048 16/4 13.3, 32/2 7.6, 32/4 7.8, 64/4 8.1, 128/4 10.6; 2048 -> 5632 32/1 10.1, 64/1 11.3, 64/2 10.6, 128/2 13.0.)
+float few_cost(I8Args& p, int* smem)
+{
+    bool two;
+    *smem = few_memory(p, &two);
+    if (p.n_stages < 1) return 1e9f;
+    const long long tiles = (long long)div_up(p.N, kRows) * div_up(p.T, p.nt);
+    const int room = cluster_room(p.splits, two), waves = (int)((tiles + room - 1) / room);
+    const float slices = (float)p.ksteps / p.splits;
+    float cost = 3.3f + (p.splits > 1 ? 0.37f : 0.f) + 3.5f * (waves - 1) + waves * (0.3f * slices + 0.0455f * p.nt);
+    if (tiles * p.splits > 148) cost += 0.067f * slices + 0.02f * p.nt + (p.splits == 8 ? 1.9f : (p.splits == 4 ? 0.8f : 0.f));
+    return cost;
+}
+// Tokens a tile and parts of K of the cheapest shape for few tokens; its shared memory and cost.
+int few_geometry(I8Args& p, float* cost)
+{
+    I8Args best = p;
+    int best_smem = 0;
+    *cost = 1e30f;
+    for (int nt = 16; nt <= kRows && (nt == 16 || nt / 2 < p.T); nt *= 2)
+        for (int s = 1; s == 1 || (s <= 8 && p.ksteps >= 2 * s); s *= 2) {
+            if (div_up(p.T, nt) > 65535) continue;          // (a grid's second dimension)
+            I8Args q = p;
+            q.nt = nt; q.splits = s;
+            int smem;
+            const float c = few_cost(q, &smem);
+            if (c < *cost) { *cost = c; best = q; best_smem = smem; }
+        }
+    p = best;
+    p.columns = p.nt <= 32 ? 32 : p.nt;
+    return best_smem;
+}
+// The same for the pairs of CTAs.  (few / many tokens' shape, us: 256 tokens, 2048 -> 2048 9.2 / 11.1, 2048 -> 5632 12.3 / 11.3, 5632 ->
+// 2048 11.9 / 18.8; 512 tokens 10.9 / 11.3, 16.8 / 11.9, 15.8 / 19.2; 1126 tokens 13.4 / 11.9, 31 / 16.8, 22.4 / 20.3.)
+float many_cost(const I8Args& p)
+{
+    const long long tiles = (long long)div_up(p.N, kManyTile) * div_up(p.T, kManyTile);
+    return 6.6f + (float)((tiles + 73) / 74) * 0.275f * p.ksteps;
+}
+
 }  // namespace
 
 cudaError_t take_project_i8_status(int32_t* status_host)
@@ -611,7 +704,9 @@ cudaError_t launch_project_i8(const I8Args& in, cudaStream_t st)
     cfg.attrs = attr; cfg.stream = st;
     I8Maps maps;
 
-    if (p.T > 128) {
+    float cost;
+    const int smem = few_geometry(p, &cost);
+    if (many_cost(p) < cost) {
         cudaError_t e = allow_smem(project_i8_many_kernel, many_ok);
         if (e != cudaSuccess) return e;
         if (!make_map_i8(&maps.x, p.x, p.T, p.K, p.ldx, kRows) || !make_map_i8(&maps.w, p.w, p.N, p.K, p.ldw, kRows)) return cudaErrorInvalidValue;
@@ -624,21 +719,9 @@ cudaError_t launch_project_i8(const I8Args& in, cudaStream_t st)
     }
     cudaError_t e = allow_smem(project_i8_kernel, few_ok);
     if (e != cudaSuccess) return e;
-    p.nt = ((p.T < 128 ? p.T : 128) + 15) & ~15;
-    p.columns = p.nt <= 32 ? 32 : (p.nt <= 64 ? 64 : 128);
-    const int n_tiles = div_up(p.N, kRows), m_tiles = div_up(p.T, p.nt);
-    p.splits = 8;
-    while (p.splits > 1 && ((long long)p.splits * n_tiles * m_tiles > 148 || p.ksteps < 2 * p.splits)) p.splits /= 2;
-    const int stage_bytes = kTile + p.nt * kRow, want = div_up(p.ksteps, p.splits);
-    const int own = p.splits > 1 ? p.splits * (p.nt * (kRows / p.splits) + 16) * 4 : 0, got = p.splits > 1 ? p.nt * kRows * 4 : 0;
-    p.n_stages = (kMaxSmem - 1024 - got) / stage_bytes;
-    if (p.n_stages > 6) p.n_stages = 6;
-    if (p.n_stages > want) p.n_stages = want;
-    p.scratch = p.n_stages * stage_bytes;
-    if (p.scratch < own) p.scratch = own;
     if (!make_map_i8(&maps.x, p.x, p.T, p.K, p.ldx, p.nt) || !make_map_i8(&maps.w, p.w, p.N, p.K, p.ldw, kRows)) return cudaErrorInvalidValue;
-    cfg.gridDim = dim3(n_tiles * p.splits, m_tiles); cfg.blockDim = dim3(kFewThreads);
-    cfg.dynamicSmemBytes = (size_t)p.scratch + got + 1024;
+    cfg.gridDim = dim3(div_up(p.N, kRows) * p.splits, div_up(p.T, p.nt)); cfg.blockDim = dim3(kFewThreads);
+    cfg.dynamicSmemBytes = smem;
     attr[1].val.clusterDim.x = p.splits;
     cfg.numAttrs = p.splits > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, project_i8_kernel, p, maps);
