@@ -86,7 +86,7 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
     const int rows = min(nt, p.T - t0);
     const int nw = kRows / S;                               // weight rows of a CTA
     const int pitch = nt * nw + 16;                         // of an owner's block of sums (16: two owners in a warp meet in no bank)
-    const int stage_bytes = kTile + nt * kRow;
+    const int slice_bytes = kTile + nt * kRow, stage_bytes = p.kb * slice_bytes;
     int* const own = reinterpret_cast<int*>(ring_ptr);      // [owner][token][its weight row], in the ring when its stages are done
     int* const part = reinterpret_cast<int*>(ring_ptr + p.scratch);      // [part][token][own weight row]
     const int k0 = (int)((long long)p.ksteps * rank / S), k1 = (int)((long long)p.ksteps * (rank + 1) / S);
@@ -131,16 +131,17 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
         if (lane == 0) {
             uint32_t stage = 0, phase = 0, armed = 0, armed_phase = 0;
             bool ok = true;
-            for (int ks = k0; ks < k1; ++ks) {
+            for (int ks = k0; ks < k1; ks += p.kb) {
                 if (!mbar_wait(bar_empty + 8 * stage, phase ^ 1, &s_abort, status)) { ok = false; break; }
                 const uint32_t sa = ring + stage * stage_bytes, full = bar_full + 8 * stage;
+                const int slices = min(p.kb, k1 - ks);
                 if (warp == 0) {
                     armed |= 1u << stage;
                     armed_phase = (armed_phase & ~(1u << stage)) | (phase << stage);
-                    mbar_expect_tx(full, stage_bytes);
-                    tma_load_2d(sa, &maps.w, full, ks * kRow, n0);
+                    mbar_expect_tx(full, slices * slice_bytes);
+                    for (int q = 0; q < slices; ++q) tma_load_2d(sa + q * slice_bytes, &maps.w, full, (ks + q) * kRow, n0);
                 } else {
-                    tma_load_2d(sa + kTile, &maps.x, full, ks * kRow, t0);
+                    for (int q = 0; q < slices; ++q) tma_load_2d(sa + q * slice_bytes + kTile, &maps.x, full, (ks + q) * kRow, t0);
                 }
                 if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
             }
@@ -154,14 +155,17 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
             uint32_t stage = 0, phase = 0, acc = 0;
             bool ok = true;
             const uint32_t idesc = idesc_i8(kRows, nt);
-            for (int ks = k0; ks < k1; ++ks) {
+            for (int ks = k0; ks < k1; ks += p.kb) {
                 if (!mbar_wait(bar_full + 8 * stage, phase, &s_abort, status)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t lo_a = smem_desc_lo(ring + stage * stage_bytes), lo_b = lo_a + (kTile >> 4);
+                uint32_t lo_a = smem_desc_lo(ring + stage * stage_bytes);
+                for (int q = min(p.kb, k1 - ks); q > 0; --q, lo_a += slice_bytes >> 4) {
+                    const uint32_t lo_b = lo_a + (kTile >> 4);
 #pragma unroll
-                for (int kk = 0; kk < kRow / 32; ++kk) {
-                    umma_i8(tmem, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, acc);
-                    acc = 1;
+                    for (int kk = 0; kk < kRow / 32; ++kk) {
+                        umma_i8(tmem, smem_desc_pack(lo_a + 2 * kk), smem_desc_pack(lo_b + 2 * kk), idesc, acc);
+                        acc = 1;
+                    }
                 }
                 umma_commit(bar_empty + 8 * stage);
                 if (++stage == (uint32_t)p.n_stages) { stage = 0; phase ^= 1; }
@@ -615,11 +619,13 @@ int cluster_room(int size, bool two)
     return n;
 }
 
-// Stages and shared memory (returned) of project_i8_kernel with p.nt tokens a tile and p.splits parts of K; *two: two CTAs share an SM.
+// Stages and shared memory (returned) of project_i8_kernel with p.nt tokens a tile, p.splits parts of K and p.kb slices a stage; *two: two
+// CTAs share an SM.
 int few_memory(I8Args& p, bool* two)
 {
-    const int stage = kTile + p.nt * kRow, want = div_up(p.ksteps, p.splits);
+    const int slice = kTile + p.nt * kRow, slices = div_up(p.ksteps, p.splits);
     const int own = p.splits > 1 ? p.splits * (p.nt * (kRows / p.splits) + 16) * 4 : 0, got = p.splits > 1 ? p.nt * kRows * 4 : 0;
+    const int stage = p.kb * slice, want = div_up(slices, p.kb), enough = p.kb == 2 ? 2 : 3;
     auto stages = [&](int bytes) {                          // the ring, or this CTA's own sums that are put together in it
         const int room = bytes - 1024 - got;
         int n = room / stage;
@@ -627,9 +633,9 @@ int few_memory(I8Args& p, bool* two)
         if (n > 6) n = 6;
         return room < own || n < 0 ? 0 : n;
     };
-    // (three stages, or all there are, are enough for two CTAs that take turns)
+    // (three slices, or all there are, are enough for two CTAs that take turns)
     const int half = stages(kHalfSmem);
-    *two = half >= 3 || (half >= 1 && half == want);
+    *two = half >= enough || (half >= 1 && half == want);
     p.n_stages = *two ? half : stages(kMaxSmem);
     p.scratch = p.n_stages * stage;
     if (p.scratch < own) p.scratch = own;
@@ -637,9 +643,11 @@ int few_memory(I8Args& p, bool* two)
 }
 
 // What a shape costs (us), a model fitted to 350 measured shapes of 1 to 1126 tokens, 1024 to 5632 rows and columns (off by 5 % in the
-// mean): the chain of launch, ids and exchange; slices of K one after the other; a tile's tokens, whose sums are exchanged; and what CTAs
-// that share an SM cost one another.  (us, of tokens a tile / parts of K: 1 token, 5632 -> 2048 16/2 10.2, 16/4 7.2, 16/8 6.1; 128 tokens,
-// 2048 -> 2048 16/4 13.3, 32/2 7.6, 32/4 7.8, 64/4 8.1, 128/4 10.6; 2048 -> 5632 32/1 10.1, 64/1 11.3, 64/2 10.6, 128/2 13.0.)
+// mean): the chain of launch and exchange; slices of K one after the other (in twos less each: the lanes that load and issue wait and
+// commit half as often, some 300 and 500 cycles each time); a tile's tokens, whose sums are exchanged; and what CTAs that share an SM
+// cost one another.  (us, of tokens a tile / parts of K, slices by one / in twos: 1 token, 5632 -> 2048 16/2 11.9 / 9.3, 16/4 8.2 / 7.0,
+// 16/8 7.0 / 6.4; 128 tokens, 2048 -> 2048 16/4 14.2 / 13.4, 32/2 8.2 / 7.4, 32/4 8.1 / 7.7, 64/4 8.4 / 8.2, 128/4 11.1 / 10.7; 2048 ->
+// 5632 32/1 11.3 / 10.2, 64/1 12.3 / 10.2, 64/2 11.3 / 17.2.)
 float few_cost(I8Args& p, int* smem)
 {
     bool two;
@@ -648,11 +656,11 @@ float few_cost(I8Args& p, int* smem)
     const long long tiles = (long long)div_up(p.N, kRows) * div_up(p.T, p.nt);
     const int room = cluster_room(p.splits, two), waves = (int)((tiles + room - 1) / room);
     const float slices = (float)p.ksteps / p.splits;
-    float cost = 3.3f + (p.splits > 1 ? 0.37f : 0.f) + 3.5f * (waves - 1) + waves * (0.3f * slices + 0.0455f * p.nt);
+    float cost = 3.3f + (p.splits > 1 ? 0.37f : 0.f) + 3.5f * (waves - 1) + waves * ((p.kb == 2 ? 0.21f : 0.3f) * slices + 0.0455f * p.nt);
     if (tiles * p.splits > 148) cost += 0.067f * slices + 0.02f * p.nt + (p.splits == 8 ? 1.9f : (p.splits == 4 ? 0.8f : 0.f));
     return cost;
 }
-// Tokens a tile and parts of K of the cheapest shape for few tokens; its shared memory and cost.
+// Tokens a tile, parts of K and slices a stage of the cheapest shape for few tokens; its shared memory and cost.
 int few_geometry(I8Args& p, float* cost)
 {
     I8Args best = p;
@@ -661,18 +669,20 @@ int few_geometry(I8Args& p, float* cost)
     for (int nt = 16; nt <= kRows && (nt == 16 || nt / 2 < p.T); nt *= 2)
         for (int s = 1; s == 1 || (s <= 8 && p.ksteps >= 2 * s); s *= 2) {
             if (div_up(p.T, nt) > 65535) continue;          // (a grid's second dimension)
-            I8Args q = p;
-            q.nt = nt; q.splits = s;
-            int smem;
-            const float c = few_cost(q, &smem);
-            if (c < *cost) { *cost = c; best = q; best_smem = smem; }
+            for (int kb = 2; kb >= 1; --kb) {
+                I8Args q = p;
+                q.nt = nt; q.splits = s; q.kb = kb;
+                int smem;
+                const float c = few_cost(q, &smem);
+                if (c < *cost) { *cost = c; best = q; best_smem = smem; }
+            }
         }
     p = best;
     p.columns = p.nt <= 32 ? 32 : p.nt;
     return best_smem;
 }
-// The same for the pairs of CTAs.  (few / many tokens' shape, us: 256 tokens, 2048 -> 2048 9.2 / 11.1, 2048 -> 5632 12.3 / 11.3, 5632 ->
-// 2048 11.9 / 18.8; 512 tokens 10.9 / 11.3, 16.8 / 11.9, 15.8 / 19.2; 1126 tokens 13.4 / 11.9, 31 / 16.8, 22.4 / 20.3.)
+// The same for the pairs of CTAs.  (few / many tokens' shape, us: 256 tokens, 2048 -> 2048 8.6 / 11.3, 2048 -> 5632 12.7 / 11.3, 5632 ->
+// 2048 11.9 / 18.8; 512 tokens 10.6 / 11.5, 16.8 / 12.1, 15.8 / 19.2; 1126 tokens 13.5 / 11.9, 31 / 16.8, 21.5 / 20.4.)
 float many_cost(const I8Args& p)
 {
     const long long tiles = (long long)div_up(p.N, kManyTile) * div_up(p.T, kManyTile);

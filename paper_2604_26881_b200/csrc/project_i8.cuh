@@ -22,6 +22,7 @@ struct I8Args {
     int ksteps;                // slices of 128 bytes of K
     int splits;                // few tokens: CTAs of a cluster that share K
     int nt;                    // few tokens: tokens of a tile
+    int kb;                    // few tokens: slices of a stage
     int columns;               // few tokens: TMEM columns
     int n_stages;
     int scratch;               // few tokens: offset of the received sums behind the ring
