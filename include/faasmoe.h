@@ -459,7 +459,7 @@ int64_t moe_project_workspace(int T, int K, int N, int rank, int n_adapters);
 /*
  * Rows as 8-bit integers with one scale each (the tokens of moe_project_i8, and once the rows of its weights), without a context:
  *   scale[t] = max |x[t]| / 127;   q[t] = the fp32 quotient x[t] / scale[t], rounded to the nearest integer (ties to even)
- * x bf16 [T, K], rows ldx apart; q int8 [T, K], rows ldq apart; scale f32 [T].  A row of zeros has scale 0.  A row with an infinity or a
+ * x bf16 [T, K], rows ldx (below 2^31) apart; q int8 [T, K], rows ldq apart; scale f32 [T].  A row of zeros has scale 0.  A row with an infinity or a
  * NaN has a scale that is not finite, and zeros.  1 <= K < 2^24.  Any alignment.  T = 0: nothing is done and the pointers may be NULL.
  */
 int moe_quantize_i8(const void* x, int64_t ldx, int T, int K, int8_t* q, int64_t ldq, float* scale, void* stream);

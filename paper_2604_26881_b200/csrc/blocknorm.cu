@@ -329,7 +329,7 @@ block_norm_kernel(const __grid_constant__ BlockNormArgs p, int W)
         if (n > 0 && wr == 0 && lane == 0) p.q_scale[t] = s.scale;
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (n > v * step) store_i8<VEC>(p.q + (size_t)t * p.ldq + first + v * step, n - v * step, p.vec_q, reinterpret_cast<const float*>(x[v]), s);
+            if (n > v * step) store_i8<VEC>(p.q + (size_t)t * p.ldq + first + v * step, n - v * step, p.vec_q, x[v], s);
     }
 }
 
@@ -774,65 +774,64 @@ cudaError_t launch_grad(const BlockNormArgs& p, const GradShape& g, cudaStream_t
 
 // ---------------------------------------------------------------------------------------------------------------------
 
-// Rows as 8-bit integers.  Up to 16384 columns a row stays in registers; beyond, it is read twice.
+// The largest magnitude of eight bf16 values so far, two by two (bit patterns without their signs are in the order of the magnitudes,
+// a NaN's above infinity's)
+__device__ __forceinline__ uint32_t top_of(uint32_t top, const uint4& v)
+{
+    top = __vmaxu2(top, __vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu));
+    return __vmaxu2(top, __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+}
+
+constexpr int kQuantizeRows = 2;         // rows on their way
+
+// Rows as 8-bit integers.  Up to 16384 columns a row stays in registers; beyond, the rest of it is read twice.
 template <int V, bool VEC>
 __global__ void __launch_bounds__(512)
-quantize_kernel(const QuantizeArgs p, int W)
+quantize_kernel(const __grid_constant__ QuantizeArgs p, int W)
 {
-    __shared__ uint32_t s_top[2][16];
-    pdl_wait();
-    pdl_launch_dependents();
+    __shared__ uint32_t s_top[2][2][kWarpsOfRow];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int row_in_block = warp / W, wr = warp - row_in_block * W;
     const int rows = blockDim.x / (32 * W);
     const int first = (wr * 32 + lane) * 8, step = W * 256;
-    uint4 xv[V];
-    auto fetch = [&](int t) {
-        const int K = t < p.T ? p.K : 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) xv[v] = load8<VEC>(p.x + (size_t)t * p.ldx + first + v * step, K - first - v * step);
-    };
+    const int sets = (p.T + rows - 1) / rows, t_step = gridDim.x * rows;
     int t = blockIdx.x * rows + row_in_block;
-    fetch(t);
+    pdl_wait();
+    pdl_launch_dependents();
+    extern __shared__ __align__(16) uint4 s_feed[];
+    RowFeed<1, V, VEC, kQuantizeRows> feed;
+    feed.src[0] = p.x + first; feed.ld[0] = (uint32_t)p.ldx * 2;
+    feed.start(s_feed, p.K - first, step, p.T, t, t_step);
     int buf = 0;
-    for (int set = blockIdx.x; set * rows < p.T; set += gridDim.x, t += gridDim.x * rows, buf ^= 1) {
-        const bool live = t < p.T;
-        float x[V][8];
-        uint32_t top = 0;
+    for (int set = blockIdx.x; set < sets; set += gridDim.x, t += t_step, buf ^= 1) {
+        const int n = t < p.T ? p.K - first : 0;
+        const bf16* const row = at(p.x, t, (uint32_t)p.ldx * 2) + first;
+        feed.begin();
+        uint32_t two = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            unpack8(xv[v], x[v]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, magnitude(x[v][i]));
-        }
-        if (set + gridDim.x < (p.T + rows - 1) / rows) fetch(t + gridDim.x * rows);
-        if (p.K > V * step)                                   // (one row a block, and more of it than the registers hold)
-            for (int col = first + V * step; live && col < p.K; col += step) {
-                float f[8];
-                unpack8(load8<VEC>(p.x + (size_t)t * p.ldx + col, p.K - col), f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = max(top, magnitude(f[i]));
-            }
-        top = __reduce_max_sync(kFull, top);
+        for (int v = 0; v < V; ++v) two = top_of(two, feed.get(0, v));
+        for (int c = V * step; c < n; c += step) two = top_of(two, load8<VEC>(row + c, n - c));      // (more than the registers hold: one row a block)
+        uint32_t top = __reduce_max_sync(kFull, max(two >> 16, two & 0xffffu));
         if (W > 1) {
-            if (lane == 0) s_top[buf][warp] = top;
+            if (lane == 0) s_top[buf][row_in_block & 1][wr] = top;
             __syncthreads();
-            top = 0;
-            for (int i = 0; i < W; ++i) top = max(top, s_top[buf][row_in_block * W + i]);
+            top = __reduce_max_sync(kFull, lane < W ? s_top[buf][row_in_block & 1][lane] : 0u);
         }
-        const RowScale s = row_scale(__uint_as_float(top) / 127.f);
-        if (live && wr == 0 && lane == 0) p.scale[t] = s.scale;
+        const RowScale s = row_scale(__uint_as_float(top << 16) / 127.f);
+        if (n > 0 && wr == 0 && lane == 0) p.scale[t] = s.scale;
+        int8_t* const q = p.q + (size_t)t * p.ldq + first;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int col = first + v * step, n = live ? p.K - col : 0;
-            if (n > 0) store_i8<VEC>(p.q + (size_t)t * p.ldq + col, n, p.vec_q, x[v], s);
+            float2 x[4];
+            unpack8(feed.get(0, v), x);
+            if (n > v * step) store_i8<VEC>(q + v * step, n - v * step, p.vec_q, x, s);
         }
-        if (p.K > V * step)
-            for (int col = first + V * step; live && col < p.K; col += step) {
-                float f[8];
-                unpack8(load8<VEC>(p.x + (size_t)t * p.ldx + col, p.K - col), f);
-                store_i8<VEC>(p.q + (size_t)t * p.ldq + col, p.K - col, p.vec_q, f, s);
-            }
+        feed.end();
+        for (int c = V * step; c < n; c += step) {
+            float2 x[4];
+            unpack8(load8<VEC>(row + c, n - c), x);
+            store_i8<VEC>(q + c, n - c, p.vec_q, x, s);
+        }
     }
 }
 
@@ -841,7 +840,13 @@ cudaError_t launch_quantize_v(const QuantizeArgs& p, int W, int rows, cudaStream
 {
     const int sets = (p.T + rows - 1) / rows, most = 148 * (32 / (W * rows));
     const dim3 grid(sets < most ? sets : most), block(32 * W * rows);
-    return p.vec ? launch_pdl(quantize_kernel<V, true>, grid, block, 0, st, p, W) : launch_pdl(quantize_kernel<V, false>, grid, block, 0, st, p, W);
+    const size_t smem = p.vec ? feed_bytes(1, V, kQuantizeRows, 32 * W * rows) : 0;
+    static bool ok[kMaxDevices] = {false};
+    if (smem > 40 * 1024) {
+        const cudaError_t e = allow_smem(quantize_kernel<V, true>, ok);
+        if (e != cudaSuccess) return e;
+    }
+    return p.vec ? launch_pdl(quantize_kernel<V, true>, grid, block, smem, st, p, W) : launch_pdl(quantize_kernel<V, false>, grid, block, 0, st, p, W);
 }
 
 }  // namespace
@@ -894,7 +899,9 @@ cudaError_t launch_quantize_i8(const QuantizeArgs& in, cudaStream_t st)
     p.vec = p.K % 8 == 0 && rows16(p.x, p.ldx);
     p.vec_q = al(p.q, 8) && p.ldq % 8 == 0;
     const int vecs = (p.K + 7) / 8;
-    const int V = vecs <= 32 ? 1 : (vecs <= 512 ? 2 : 4);
+    // Vectors per lane: four where there are rows enough for all SMs (16384 x 2048 with 1, 2, 4 and 8: 27, 21, 20 and 21 us; 32 x 2048 with 2, 4
+    // and 8: 1.8, 2.2 and 3.0).
+    const int V = vecs <= 32 ? 1 : (vecs <= 64 || (vecs <= 512 && (p.T < 2048 || !p.vec)) ? 2 : 4);
     int W = (vecs + 32 * V - 1) / (32 * V);
     if (W > 16) W = 16;
     const int rows = W >= 4 ? 1 : 4 / W;

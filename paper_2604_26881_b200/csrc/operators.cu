@@ -274,6 +274,7 @@ int moe_block_norm_backward(const void* block_out, int64_t ld_block, const void*
 int moe_quantize_i8(const void* x, int64_t ldx, int T, int K, int8_t* q, int64_t ldq, float* scale, void* stream)
 {
     if (T < 0 || T > kMaxRows || K < 1 || K > kQuantizeMaxK || ldx < K || ldq < K) return MOE_ERR_SHAPE;
+    if (beyond(ldx)) return MOE_ERR_UNSUPPORTED;
     if (off(x, 2) || off(scale, 4)) return MOE_ERR_SHAPE;
     if (T == 0) return MOE_OK;
     if (!x || !q || !scale) return MOE_ERR_NULL;

@@ -180,6 +180,12 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
         float scale = 0.f, bias = 0.f;
         if (S == 1 && n < p.N) { scale = p.w_scale[n]; bias = p.bias ? p.bias[n] : 0.f; }
         asm volatile("bar.sync 1, 256;" ::: "memory");      // (the tokens' scales are there)
+        float b[16];                                        // (bases of 16 tokens, asked for before the product is there, or before the 16 tokens before them)
+        auto ask = [&](int c) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) b[i] = c + i < rows && n < p.N ? load_base(p, t0 + c + i, n) : 0.f;
+        };
+        if (S == 1 && p.base) ask(half * 16);
         if (__all_sync(kFull, mbar_wait(bar_done, 0, &s_abort, status))) {
             tc_fence_after();
             int* const dst = own + (row / nw) * pitch + row % nw;
@@ -191,18 +197,15 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) if (c + i < rows) dst[(c + i) * nw] = (int)r[i];
                 } else if (n < p.N) {
-                    float b[16];
-                    if (p.base) {
+                    float v[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) b[i] = c + i < rows ? load_base(p, t0 + c + i, n) : 0.f;
+                    for (int i = 0; i < 16; ++i) {
+                        v[i] = fmaf((float)(int)r[i] * s_xs[c + i], scale, bias);
+                        if (p.base) v[i] += b[i];
                     }
+                    if (p.base && c + 32 < rows) ask(c + 32);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (c + i < rows) {
-                            float v = fmaf((float)(int)r[i] * s_xs[c + i], scale, bias);
-                            if (p.base) v += b[i];
-                            store_out(p, t0 + c + i, n, v);
-                        }
+                    for (int i = 0; i < 16; ++i) if (c + i < rows) store_out(p, t0 + c + i, n, v[i]);
                 }
             }
             if (S > 1) fence_async_shared();                // (the sums leave by bulk copies)
@@ -315,7 +318,7 @@ __device__ __forceinline__ void store_bytes(void* p, const uint32_t* r)
 // row, so they need not be put together with its neighbours' in shared memory, whose bandwidth the MMAs' operands take
 // (through shared memory, in 16-byte vectors of neighbouring lanes: 137 us for 16384 x 2048 -> 5632 instead of 133).
 template <typename T, int BYTES>
-__device__ __forceinline__ void write_columns(const I8Args& p, const uint32_t (&r)[16], float xs, const float* ws, const float* add, T* out, const T* base)
+__device__ __forceinline__ void write_columns(const I8Args& p, const uint32_t (&r)[16], float xs, const float* ws, const float* add, T* out, const uint4 (&base)[4])
 {
     float2 v[8];
 #pragma unroll
@@ -330,10 +333,7 @@ __device__ __forceinline__ void write_columns(const I8Args& p, const uint32_t (&
     uint32_t o[kWords];
     if (p.base) {
 #pragma unroll
-        for (int j = 0; j < kWords; j += 4) {
-            const uint4 q = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(base) + j);
-            o[j] = q.x; o[j + 1] = q.y; o[j + 2] = q.z; o[j + 3] = q.w;
-        }
+        for (int j = 0; j < kWords; j += 4) { o[j] = base[j / 4].x; o[j + 1] = base[j / 4].y; o[j + 2] = base[j / 4].z; o[j + 3] = base[j / 4].w; }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if constexpr (sizeof(T) == 4) v[j] = add2(v[j], make_float2(__uint_as_float(o[2 * j]), __uint_as_float(o[2 * j + 1])));
@@ -510,9 +510,18 @@ project_i8_many_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
                 if (p.bias) add[i] = there ? p.bias[n0 + i] : 0.f;
             }
             __syncwarp();
+            // (the bases of the first 16 columns are asked for before the product is there, the others' 16 columns ahead)
+            const size_t row = (size_t)(t + lane);
+            uint4 base[4];
+            auto ask = [&](int n) {
+                if (!p.base || !by16 || n + kOutCols > p.N || t + lane >= p.T) return;
+                const uint4* const from_base = reinterpret_cast<const uint4*>((const char*)p.base + (row * p.ldbase + n) * esz);
+                base[0] = from_base[0]; base[1] = from_base[1];
+                if (p.out_f32) { base[2] = from_base[2]; base[3] = from_base[3]; }
+            };
+            ask(n0);
             if (!__all_sync(kFull, mbar_wait(bar_tfull + 8 * buf, (it >> 1) & 1, &s_abort, status))) break;
             tc_fence_after();
-            const size_t row = (size_t)(t + lane);
 #pragma unroll 1
             for (int c = 0; c < 128; c += kOutCols) {
                 uint32_t r[kOutCols];
@@ -526,15 +535,18 @@ project_i8_many_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
                 const int n = n0 + c;
                 if (n >= p.N || t >= p.T) continue;
                 if (by16 && n + kOutCols <= p.N) {
-                    const size_t at = row * p.ldo + n, from_base = row * p.ldbase + n;
+                    const size_t at = row * p.ldo + n;
+                    uint4 now[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) now[i] = base[i];
+                    if (c + kOutCols < 128) ask(n + kOutCols);
                     if (t + lane >= p.T) {
-                    } else
-                    if (p.out_f32) {
-                        if (by32) write_columns<float, 32>(p, r, xs, ws + c, add + c, (float*)p.out + at, (const float*)p.base + from_base);
-                        else write_columns<float, 16>(p, r, xs, ws + c, add + c, (float*)p.out + at, (const float*)p.base + from_base);
+                    } else if (p.out_f32) {
+                        if (by32) write_columns<float, 32>(p, r, xs, ws + c, add + c, (float*)p.out + at, now);
+                        else write_columns<float, 16>(p, r, xs, ws + c, add + c, (float*)p.out + at, now);
                     } else {
-                        if (by32) write_columns<bf16, 32>(p, r, xs, ws + c, add + c, (bf16*)p.out + at, (const bf16*)p.base + from_base);
-                        else write_columns<bf16, 16>(p, r, xs, ws + c, add + c, (bf16*)p.out + at, (const bf16*)p.base + from_base);
+                        if (by32) write_columns<bf16, 32>(p, r, xs, ws + c, add + c, (bf16*)p.out + at, now);
+                        else write_columns<bf16, 16>(p, r, xs, ws + c, add + c, (bf16*)p.out + at, now);
                     }
                     continue;
                 }
@@ -645,7 +657,7 @@ int few_memory(I8Args& p, bool* two)
 // What a shape costs (us), a model fitted to 350 measured shapes of 1 to 1126 tokens, 1024 to 5632 rows and columns (off by 5 % in the
 // mean): the chain of launch and exchange; slices of K one after the other (in twos less each: the lanes that load and issue wait and
 // commit half as often, some 300 and 500 cycles each time); a tile's tokens, whose sums are exchanged; and what CTAs that share an SM
-// cost one another.  (us, of tokens a tile / parts of K, slices by one / in twos: 1 token, 5632 -> 2048 16/2 11.9 / 9.3, 16/4 8.2 / 7.0,
+// cost one another; without an exchange, outputs that each thread writes one by one.  (us, of tokens a tile / parts of K, slices by one / in twos: 1 token, 5632 -> 2048 16/2 11.9 / 9.3, 16/4 8.2 / 7.0,
 // 16/8 7.0 / 6.4; 128 tokens, 2048 -> 2048 16/4 14.2 / 13.4, 32/2 8.2 / 7.4, 32/4 8.1 / 7.7, 64/4 8.4 / 8.2, 128/4 11.1 / 10.7; 2048 ->
 // 5632 32/1 11.3 / 10.2, 64/1 12.3 / 10.2, 64/2 11.3 / 17.2.)
 float few_cost(I8Args& p, int* smem)
@@ -656,7 +668,7 @@ float few_cost(I8Args& p, int* smem)
     const long long tiles = (long long)div_up(p.N, kRows) * div_up(p.T, p.nt);
     const int room = cluster_room(p.splits, two), waves = (int)((tiles + room - 1) / room);
     const float slices = (float)p.ksteps / p.splits;
-    float cost = 3.3f + (p.splits > 1 ? 0.37f : 0.f) + 3.5f * (waves - 1) + waves * ((p.kb == 2 ? 0.21f : 0.3f) * slices + 0.0455f * p.nt);
+    float cost = 3.3f + (p.splits > 1 ? 0.37f : 1.5f) + 3.5f * (waves - 1) + waves * ((p.kb == 2 ? 0.21f : 0.3f) * slices + 0.0455f * p.nt);
     if (tiles * p.splits > 148) cost += 0.067f * slices + 0.02f * p.nt + (p.splits == 8 ? 1.9f : (p.splits == 4 ? 0.8f : 0.f));
     return cost;
 }
@@ -685,8 +697,9 @@ int few_geometry(I8Args& p, float* cost)
 // 2048 11.9 / 18.8; 512 tokens 10.6 / 11.5, 16.8 / 12.1, 15.8 / 19.2; 1126 tokens 13.5 / 11.9, 31 / 16.8, 21.5 / 20.4.)
 float many_cost(const I8Args& p)
 {
+    // (from 1024 tokens on it is also the shape whose operands come from memory once: 33 us where the other takes 48, weights out of the caches)
     const long long tiles = (long long)div_up(p.N, kManyTile) * div_up(p.T, kManyTile);
-    return 6.6f + (float)((tiles + 73) / 74) * 0.275f * p.ksteps;
+    return (p.T < 1024 ? 6.6f : 5.f) + (float)((tiles + 73) / 74) * 0.275f * p.ksteps;
 }
 
 }  // namespace
