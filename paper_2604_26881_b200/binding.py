@@ -461,13 +461,11 @@ def moe_project(x, w, out, *, base=None, a=None, b=None, scale=None, tenant_id=N
         _check("moe_project", status)
 
 
-def _call(fn, first, *args):
-    """A context-free call, on the device of its first tensor."""
-    status = getattr(_calls or _load_calls(), fn)(first, *args)
-    if status:
-        if status == _OTHER_DEVICE:
-            status = _on_device(fn, first.device, first, *args)
-        _check(fn, status)
+def _again(fn, status, args):
+    """What a context-free call returned that is not 0: another device (again, with that one current), or an error."""
+    if status == _OTHER_DEVICE:
+        status = _on_device(fn, args[0].device, *args)
+    _check(fn, status)
 
 
 def _workspace_on(stream, device, n):
@@ -489,8 +487,11 @@ def moe_block_norm(block_out, residual, h, eps, *, post_weight=None, pre_weight=
     block_out, residual, h, out: bf16 [T, H], rows may be strided; out_q int8 [T, H], q_scale float32 [T]; the weights bf16 [H].
     gate: bf16 [H] (per channel), float32 [T] (per token), bf16 [T, H] (per element) or None; gate_act "none" or "sigmoid".
     post_weight None: block_out is not normed; pre_weight None: only h.  h and out may be block_out, residual or the gate."""
-    _call("moe_block_norm", block_out, residual, h, eps, post_weight, pre_weight, gate, _ACTS[gate_act], residual_scale, block_scale, out,
-          out_q, q_scale, stream)
+    args = (block_out, residual, h, eps, post_weight, pre_weight, gate, _ACTS[gate_act], residual_scale, block_scale, out, out_q,
+            q_scale, stream)
+    status = (_calls or _load_calls()).moe_block_norm(*args)
+    if status:
+        _again("moe_block_norm", status, args)
 
 
 def moe_block_norm_workspace(T, H) -> int:
@@ -511,13 +512,19 @@ def moe_block_norm_backward(block_out, h, eps, *, post_weight=None, pre_weight=N
     allocated for the call on its stream."""
     if stream is not None and workspace is None and block_out.dim() == 2 and block_out.is_cuda:
         workspace = _workspace_on(stream, block_out.device, load_library().moe_block_norm_workspace(*block_out.shape))
-    _call("moe_block_norm_backward", block_out, h, eps, post_weight, pre_weight, gate, _ACTS[gate_act], residual_scale, block_scale, d_out,
-          d_h, d_block, d_residual, d_gate, d_post_weight, d_pre_weight, workspace, stream)
+    args = (block_out, h, eps, post_weight, pre_weight, gate, _ACTS[gate_act], residual_scale, block_scale, d_out, d_h, d_block,
+            d_residual, d_gate, d_post_weight, d_pre_weight, workspace, stream)
+    status = (_calls or _load_calls()).moe_block_norm_backward(*args)
+    if status:
+        _again("moe_block_norm_backward", status, args)
 
 
 def moe_quantize_i8(x, q, scale, *, stream=None):
     """scale[t] = max |x[t]| / 127, q[t] = x[t] / scale[t] to the nearest integer: x bf16 [T, K], q int8 [T, K], scale float32 [T]."""
-    _call("moe_quantize_i8", x, q, scale, stream)
+    args = (x, q, scale, stream)
+    status = (_calls or _load_calls()).moe_quantize_i8(*args)
+    if status:
+        _again("moe_quantize_i8", status, args)
 
 
 def moe_project_i8(x, x_scale, w, w_scale, out, *, bias=None, base=None, status_out=None, stream=None):
@@ -526,7 +533,10 @@ def moe_project_i8(x, x_scale, w, w_scale, out, *, bias=None, base=None, status_
     x int8 [T, K], w int8 [N, K] (rows may be strided, multiples of 16 apart, 16-byte aligned), x_scale float32 [T], w_scale
     float32 [N], bias float32 [N] or None, out float32 or bf16 [T, N], base like out or None.  status_out: int32 [1] on the device;
     without it moe_project_status() tells of a time-out.  Adapters are added by moe_project(x, None, out, base=out, a=..., b=...)."""
-    _call("moe_project_i8", x, x_scale, w, w_scale, out, bias, base, status_out, stream)
+    args = (x, x_scale, w, w_scale, out, bias, base, status_out, stream)
+    status = (_calls or _load_calls()).moe_project_i8(*args)
+    if status:
+        _again("moe_project_i8", status, args)
 
 
 def moe_balance_workspace(T, E, M=1) -> int:
@@ -544,18 +554,24 @@ def moe_balance_loss(logits, topk_idx, counts, tokens, mean_prob, loss, *, score
     logits [T, E] float32 or bf16 (rows may be strided), topk_idx [T, k] int32; counts int32 and mean_prob float32 [M, E], tokens int32,
     loss and z_loss float32 [M].  mask uint8 [T]: 0 for tokens that take no part.  tenant_id [T] and model_of_tenant
     [n_tenants] int32 (device) name a token's model.  workspace: uint8 tensor, by default allocated for the call on its stream."""
-    if stream is not None and workspace is None and logits.dim() == 2 and logits.is_cuda:
+    if stream is not None and workspace is None and logits.dim() == 2 and logits.is_cuda and loss is not None:
         workspace = _workspace_on(stream, logits.device, load_library().moe_balance_workspace(*logits.shape, loss.numel()))
-    _call("moe_balance_loss", logits, topk_idx, counts, tokens, mean_prob, loss, _SCORES[score], z_loss, mask, tenant_id, model_of_tenant,
-          workspace, status_out, stream)
+    args = (logits, topk_idx, counts, tokens, mean_prob, loss, _SCORES[score], z_loss, mask, tenant_id, model_of_tenant, workspace,
+            status_out, stream)
+    status = (_calls or _load_calls()).moe_balance_loss(*args)
+    if status:
+        _again("moe_balance_loss", status, args)
 
 
 def moe_gate_backward(logits, rule, topk_idx, d_logits, *, d_topk_w=None, counts=None, tokens=None, d_loss=None, d_z_loss=None, mask=None,
                       tenant_id=None, model_of_tenant=None, status_out=None, stream=None):
     """Gradient of the logits [T, E] (d_logits, of their type) by way of the chosen weights of `rule` (d_topk_w float32 [T, k]), of the
     balance loss (d_loss float32 [M], with counts and tokens of moe_balance_loss) and of its second loss (d_z_loss float32 [M])."""
-    _call("moe_gate_backward", logits, rule, topk_idx, d_logits, d_topk_w, counts, tokens, d_loss, d_z_loss, mask, tenant_id, model_of_tenant,
-          status_out, stream)
+    args = (logits, rule, topk_idx, d_logits, d_topk_w, counts, tokens, d_loss, d_z_loss, mask, tenant_id, model_of_tenant, status_out,
+            stream)
+    status = (_calls or _load_calls()).moe_gate_backward(*args)
+    if status:
+        _again("moe_gate_backward", status, args)
 
 
 def moe_get_workspace(ctx):

@@ -91,6 +91,7 @@ struct RowStage {
             for (int j = 0; j < VW; ++j) none.v[j] = (TL)(-INFINITY);
             s[i * blockDim.x] = none;
         }
+        __syncwarp();                                         // (before the copies to the same places)
     }
     __device__ __forceinline__ void ask(const TL* row, int E, int sub, bool there)      // the row after those asked for
     {

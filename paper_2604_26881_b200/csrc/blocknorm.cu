@@ -153,11 +153,14 @@ struct RowFeed {
                     }
                 }
             }
-        } else if (!kShared) {
+        } else {                                              // behind the last row: zeros, which add nothing to any sum
 #pragma unroll
             for (int a = 0; a < NA; ++a)
 #pragma unroll
-                for (int v = 0; v < V; ++v) next[kShared ? 0 : a][kShared ? 0 : v] = make_uint4(0, 0, 0, 0);
+                for (int v = 0; v < V; ++v) {
+                    if (kShared) s[((to * NA + a) * V + v) * blockDim.x] = make_uint4(0, 0, 0, 0);
+                    else next[kShared ? 0 : a][kShared ? 0 : v] = make_uint4(0, 0, 0, 0);
+                }
         }
         t += t_step;
         if (kShared) asm volatile("cp.async.commit_group;" ::: "memory");
@@ -168,9 +171,10 @@ struct RowFeed {
         n = columns; step = column_step; T = rows; t = first_t; t_step = row_step; stage = 0;
         s = shared + threadIdx.x;
         if (kShared) {
-            // (what is never copied, columns and matrices that are not there and rows behind the last, reads as zero or is not stored)
+            // (what is never copied, columns and matrices that are not there, reads as zero)
 #pragma unroll
             for (int i = 0; i < D * NA * V; ++i) s[i * blockDim.x] = make_uint4(0, 0, 0, 0);
+            __syncwarp();                                     // (before the copies to the same places)
 #pragma unroll
             for (int d = 0; d < D; ++d) ask(d);
         } else {

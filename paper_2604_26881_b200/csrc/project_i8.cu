@@ -108,6 +108,12 @@ project_i8_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
     if (S > 1) cluster_arrive();                            // (waited for before anything is sent: the peers run and their barriers are there)
     tc_fence_after();
     const uint32_t tmem = s_tmem;
+    // The kernel before this one may still be working on x: the weights' way into L2 need not wait for it (nothing is read before the
+    // wait, and L2 sees what is written later).
+    if (warp == 2 && lane == 0)
+        for (int ks = k0; ks < k1; ++ks)
+            asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(&maps.w), "r"(ks * kRow), "r"(n0) : "memory");
+    __syncwarp();
     pdl_wait();
     pdl_launch_dependents();
 
@@ -604,12 +610,11 @@ int div_up(int a, int b) { return (a + b - 1) / b; }
 
 // How many clusters of `size` CTAs of project_i8_kernel run at once, with one CTA per SM or two (the SMs of a cluster belong to one
 // GPC, so a few of each GPC stay unused).
-int cluster_room(int size, bool two)
+int cluster_room(int size, bool two, int dev)
 {
     if (size == 1) return 148 * (two ? 2 : 1);
     static int room[kMaxDevices][9][2] = {};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return (two ? 256 : 112) / size;
+    if (dev < 0 || dev >= kMaxDevices) return (two ? 256 : 112) / size;
     int& n = room[dev][size][two];
     if (n == 0) {
         static bool allowed[kMaxDevices] = {false};
@@ -660,13 +665,14 @@ int few_memory(I8Args& p, bool* two)
 // cost one another; without an exchange, outputs that each thread writes one by one.  (us, of tokens a tile / parts of K, slices by one / in twos: 1 token, 5632 -> 2048 16/2 11.9 / 9.3, 16/4 8.2 / 7.0,
 // 16/8 7.0 / 6.4; 128 tokens, 2048 -> 2048 16/4 14.2 / 13.4, 32/2 8.2 / 7.4, 32/4 8.1 / 7.7, 64/4 8.4 / 8.2, 128/4 11.1 / 10.7; 2048 ->
 // 5632 32/1 11.3 / 10.2, 64/1 12.3 / 10.2, 64/2 11.3 / 17.2.)
-float few_cost(I8Args& p, int* smem)
+float few_cost(I8Args& p, int dev, int* smem)
 {
     bool two;
     *smem = few_memory(p, &two);
     if (p.n_stages < 1) return 1e9f;
     const long long tiles = (long long)div_up(p.N, kRows) * div_up(p.T, p.nt);
-    const int room = cluster_room(p.splits, two), waves = (int)((tiles + room - 1) / room);
+    const int room = cluster_room(p.splits, two, dev);
+    const float waves = (float)((tiles + room - 1) / room);
     const float slices = (float)p.ksteps / p.splits;
     float cost = 3.3f + (p.splits > 1 ? 0.37f : 1.5f) + 3.5f * (waves - 1) + waves * ((p.kb == 2 ? 0.21f : 0.3f) * slices + 0.0455f * p.nt);
     if (tiles * p.splits > 148) cost += 0.067f * slices + 0.02f * p.nt + (p.splits == 8 ? 1.9f : (p.splits == 4 ? 0.8f : 0.f));
@@ -676,7 +682,8 @@ float few_cost(I8Args& p, int* smem)
 int few_geometry(I8Args& p, float* cost)
 {
     I8Args best = p;
-    int best_smem = 0;
+    int best_smem = 0, dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
     *cost = 1e30f;
     for (int nt = 16; nt <= kRows && (nt == 16 || nt / 2 < p.T); nt *= 2)
         for (int s = 1; s == 1 || (s <= 8 && p.ksteps >= 2 * s); s *= 2) {
@@ -685,7 +692,7 @@ int few_geometry(I8Args& p, float* cost)
                 I8Args q = p;
                 q.nt = nt; q.splits = s; q.kb = kb;
                 int smem;
-                const float c = few_cost(q, &smem);
+                const float c = few_cost(q, dev, &smem);
                 if (c < *cost) { *cost = c; best = q; best_smem = smem; }
             }
         }

@@ -328,6 +328,34 @@ def test_gradients_with_strides_and_alignment(pads, shift):
 
 
 @gpu
+@pytest.mark.parametrize("H", [4097, 8191, 8193, 16383])
+def test_wide_rows_that_are_not_on_16_bytes(H):
+    check_forward(3, H, "element", "sigmoid", q=True, pads=(1, 2, 3, 4, 5, 6))
+    check_forward(3, H, "channel", q=True, shift=1)
+    check_backward(3, H, "element", "sigmoid", pads=(1, 2, 3, 4, 5, 6, 7, 8, 9))
+    check_backward(3, H, "channel", "sigmoid", shift=1)
+
+
+@gpu
+@pytest.mark.parametrize("H", [64, 300, 512, 2048])
+@pytest.mark.parametrize("T", [1, 3, 601, 2371])
+def test_infinite_gradients_stay_in_their_columns(H, T):
+    """A row's infinity is in that row's outputs and that column's sums, whatever rows are worked on beside and behind it."""
+    i = inputs(T, H, "channel")
+    h, d_out, d_h = ((torch.randn(T, H, generator=torch.Generator().manual_seed(s))).to(BF) for s in (1, 2, 3))
+    clean = run_backward(i, h, "channel", "sigmoid", 1.0, 1.0, 1e-6, d_out, d_h)
+    for t in {0, T - 1, T // 2}:
+        d2 = d_h.clone()
+        d2[t, 7] = float("inf")
+        got = run_backward(dict(i, post=None), h, "channel", "sigmoid", 1.0, 1.0, 1e-6, d_out, d2)
+        rows = torch.arange(T) != t
+        cols = torch.arange(H) != 7
+        assert torch.equal(got["residual"].cpu()[rows], clean["residual"].cpu()[rows]) and torch.equal(got["pre"], clean["pre"])
+        assert got["gate"].cpu()[cols].isfinite().all() and got["gate"].cpu()[7].isinf()
+        assert got["y"].cpu()[rows].isfinite().all() and got["residual"].cpu()[t, 7] == float("inf")
+
+
+@gpu
 def test_gradients_against_differences():
     """Of the scalar sum(d_out out) + sum(d_h h) in 64 bits, by central differences with steps of 2^-12 of order-one values."""
     T, H, eps, rs, bs = 3, 40, 1e-3, 0.5, 0.7
