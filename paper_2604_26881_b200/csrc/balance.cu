@@ -7,6 +7,10 @@
 //
 // with (1 - s) only for sigmoid scores and g_w the part that comes by way of the chosen experts' weights w = s, or s over the sum
 // of the chosen s.  A token is taken by 4, 8 or 16 lanes with 16 experts each (up to 64, 128, 256 experts).
+//
+// Long batches are bound by the chains of a step (loads, exponentials, two or three sums over a token's lanes) and by issue, not by
+// the logits' bytes: 65536 x 256 with sigmoid scores and both losses takes 24 us for the loss (67 MB, 10 us of HBM time) and 38 us for
+// the gradient (134 MB, 20 us); 4096 x 60 of four models 13.5 us for both, 32 x 60 3.6 us each: launches and one step.
 #include <float.h>
 
 #include "balance.cuh"
