@@ -131,32 +131,59 @@ __device__ __forceinline__ bf16* at(bf16* p, int t, uint32_t ld_bytes) { return 
 
 // The rows of up to NA matrices that a block works through, each lane's own vectors of them, on their way ahead of time: D rows in
 // shared memory that no other lane touches (asynchronous copies: no registers, and nothing to wait for but the lane's own), or, where
-// rows are not on 16-byte boundaries or D is 0, one row in registers.
+// D is 0, one row in registers.  VEC: rows are on 16-byte boundaries and hold whole vectors.  Otherwise a lane copies the two aligned
+// vectors that its own lies in, as far as they are inside the matrix, and takes its eight elements out of them when they are read.
 template <int NA, int V, bool VEC, int D>
 struct RowFeed {
-    static constexpr bool kShared = VEC && D > 0;
-    static constexpr int kA = kShared ? 1 : NA, kV = kShared ? 1 : V;
+    static constexpr bool kShared = D > 0;
+    static constexpr int kA = kShared ? 1 : NA, kV = kShared ? 1 : V, kHalves = VEC ? 1 : 2;
     const bf16* src[NA];             // this lane's first column of row 0, or null: zeros
     uint32_t ld[NA];
     int n, step, T, t, t_step;       // columns from the lane's first on; the next row to ask for
+    int first;                       // (VEC false) the lane's first column
     uint4* s;
     int stage;
     uint4 cur[kA][kV], next[kA][kV];
 
+    __device__ __forceinline__ uint4* place(int at, int a, int v, int half) const { return s + (((at * NA + a) * V + v) * kHalves + half) * (int)blockDim.x; }
+    __device__ __forceinline__ int shift(int a, int row) const { return (int)(((uint32_t)(uintptr_t)src[a] + (uint32_t)row * ld[a]) & 15u) >> 1; }
+    static __device__ __forceinline__ void copy16(uint4* dst, const void* from)
+    {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(from) : "memory");
+    }
     __device__ __forceinline__ void ask(int to)
     {
         if (t < T) {
 #pragma unroll
             for (int a = 0; a < NA; ++a) {
                 const bf16* const row = at(src[a], t, ld[a]);
+                if (!kShared) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    if (kShared) {
-                        uint4* const dst = s + ((to * NA + a) * V + v) * blockDim.x;
-                        if (src[a] && n > v * step)
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(row + v * step) : "memory");
-                    } else {
-                        next[kShared ? 0 : a][kShared ? 0 : v] = load8<VEC>(row + v * step, src[a] ? n - v * step : 0);
+                    for (int v = 0; v < V; ++v) next[kShared ? 0 : a][kShared ? 0 : v] = load8<VEC>(row + v * step, src[a] ? n - v * step : 0);
+                } else if (VEC) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        if (src[a] && n > v * step) copy16(place(to, a, v, 0), row + v * step);
+                } else if (src[a]) {
+                    const int k = shift(a, t);
+                    // bytes of the matrix in front of this lane's first vector, and up to its end
+                    const uint64_t before = (uint64_t)(uint32_t)t * ld[a] + (uint32_t)(2 * first), all = (uint64_t)(uint32_t)(T - 1) * ld[a] + 2u * (uint32_t)(first + n);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const int m = n - v * step;
+                        if (m <= 0) continue;
+                        const uint64_t off = before + (uint32_t)(2 * v * step);
+                        const char* const from = reinterpret_cast<const char*>(row + v * step) - 2 * k;
+                        if (off >= (uint64_t)(2 * k) && off - 2 * k + (k ? 32 : 16) <= all) {
+                            copy16(place(to, a, v, 0), from);
+                            if (k) copy16(place(to, a, v, kHalves - 1), from + 16);
+                        } else {                              // at the matrix's ends
+                            unsigned short e[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) e[i] = i < m ? reinterpret_cast<const unsigned short*>(row + v * step)[i] : (unsigned short)0;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) reinterpret_cast<unsigned short*>(place(to, a, v, (k + i) >> 3 ? kHalves - 1 : 0))[(k + i) & 7] = e[i];
+                        }
                     }
                 }
             }
@@ -165,22 +192,25 @@ struct RowFeed {
             for (int a = 0; a < NA; ++a)
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    if (kShared) s[((to * NA + a) * V + v) * blockDim.x] = make_uint4(0, 0, 0, 0);
-                    else next[kShared ? 0 : a][kShared ? 0 : v] = make_uint4(0, 0, 0, 0);
+                    if (!kShared) next[kShared ? 0 : a][kShared ? 0 : v] = make_uint4(0, 0, 0, 0);
+                    else {
+#pragma unroll
+                        for (int half = 0; half < kHalves; ++half) *place(to, a, v, half) = make_uint4(0, 0, 0, 0);
+                    }
                 }
         }
         t += t_step;
         if (kShared) asm volatile("cp.async.commit_group;" ::: "memory");
     }
     // src and ld are set; `first_t`: the block's first row for this lane
-    __device__ __forceinline__ void start(uint4* shared, int columns, int column_step, int rows, int first_t, int row_step)
+    __device__ __forceinline__ void start(uint4* shared, int columns, int first_column, int column_step, int rows, int first_t, int row_step)
     {
-        n = columns; step = column_step; T = rows; t = first_t; t_step = row_step; stage = 0;
+        n = columns; first = first_column; step = column_step; T = rows; t = first_t; t_step = row_step; stage = 0;
         s = shared + threadIdx.x;
         if (kShared) {
             // (what is never copied, columns and matrices that are not there, reads as zero)
 #pragma unroll
-            for (int i = 0; i < D * NA * V; ++i) s[i * blockDim.x] = make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < D * NA * V * kHalves; ++i) s[i * blockDim.x] = make_uint4(0, 0, 0, 0);
             __syncwarp();                                     // (before the copies to the same places)
 #pragma unroll
             for (int d = 0; d < D; ++d) ask(d);
@@ -202,7 +232,11 @@ struct RowFeed {
     }
     __device__ __forceinline__ uint4 get(int a, int v) const
     {
-        return kShared ? s[((stage * NA + a) * V + v) * blockDim.x] : cur[kShared ? 0 : a][kShared ? 0 : v];
+        if (!kShared) return cur[kShared ? 0 : a][kShared ? 0 : v];
+        if (VEC) return *place(stage, a, v, 0);
+        const int k = shift(a, t - D * t_step), m = n - v * step;
+        const uint4 x = k ? eight_from(*place(stage, a, v, 0), *place(stage, a, v, kHalves - 1), k) : *place(stage, a, v, 0);
+        return m >= 8 ? x : first_of(x, m);
     }
     __device__ __forceinline__ void end()                     // nothing of this row is read any more
     {
@@ -213,7 +247,7 @@ struct RowFeed {
     }
 };
 // (bytes of shared memory)
-size_t feed_bytes(int NA, int V, int D, int threads) { return (size_t)NA * V * D * 16 * threads; }
+size_t feed_bytes(int NA, int V, bool vec, int D, int threads) { return (size_t)NA * V * (vec ? 1 : 2) * D * 16 * threads; }
 
 // What every row multiplies a column of the block's output with: block_scale, the weight behind the block, a gate per channel.
 template <int V>
@@ -240,7 +274,9 @@ __device__ __forceinline__ void column_factors(const BlockNormArgs& p, int first
     }
 }
 
-constexpr int kForwardRows = 2;          // rows on their way (3 and 4 are no faster)
+// Rows on their way in shared memory (3 and 4 are no faster; 0: one, in registers, where the shared memory does not hold two).
+template <int V, bool VEC>
+constexpr int kForwardRows = VEC || V <= 2 ? 2 : 0;
 
 // W warps per row, V vectors of 8 elements per lane, blockDim / (32 W) rows at a time; a block goes on with every gridDim-th set
 // of rows and has the next sets' loads in flight while it works on this one.  As many blocks as are resident at once, 16 warps an SM
@@ -264,11 +300,11 @@ block_norm_kernel(const __grid_constant__ BlockNormArgs p, int W)
     int t = blockIdx.x * rows + row_in_block;
     const int t_step = gridDim.x * rows;
     extern __shared__ __align__(16) uint4 s_feed[];
-    RowFeed<ELEMENT ? 3 : 2, V, VEC, kForwardRows> feed;
+    RowFeed<ELEMENT ? 3 : 2, V, VEC, kForwardRows<V, VEC>> feed;
     feed.src[0] = p.y + first; feed.ld[0] = (uint32_t)p.ldy * 2;
     feed.src[1] = p.residual + first; feed.ld[1] = (uint32_t)p.ldr * 2;
     if (ELEMENT) { feed.src[ELEMENT ? 2 : 0] = (const bf16*)p.gate + first; feed.ld[ELEMENT ? 2 : 0] = (uint32_t)p.ldg * 2; }
-    feed.start(s_feed, p.H - first, step, p.T, t, t_step);
+    feed.start(s_feed, p.H - first, first, step, p.T, t, t_step);
     const bool token = p.gate_form == MOE_GATE_TOKEN;
     float gt = token && t < p.T ? ((const float*)p.gate)[t] : 1.f;
     bf16* const h = p.h + first;
@@ -310,7 +346,7 @@ block_norm_kernel(const __grid_constant__ BlockNormArgs p, int W)
             }
             const uint4 stored = pack8(x[v]);                 // (rounded: the stream)
             bf16* const dst = at(h, t, (uint32_t)p.ldh * 2) + v * step;
-            if (!VEC) store8<false>(dst, n - v * step, x[v]);
+            if (!VEC) store8_anywhere(dst, n - v * step, stored);
             else if (n > v * step) *reinterpret_cast<uint4*>(dst) = stored;
             unpack8(stored, x[v]);
         }
@@ -365,7 +401,7 @@ cudaError_t launch_one(const BlockNormArgs& p, int W, int rows, cudaStream_t st)
 {
     const int sets = (p.T + rows - 1) / rows, most = 148 * ((V == 1 ? 32 : 16) / (W * rows));
     static bool ok[kMaxDevices] = {false};
-    const size_t smem = VEC ? feed_bytes(ELEMENT ? 3 : 2, V, kForwardRows, 32 * W * rows) : 0;
+    const size_t smem = feed_bytes(ELEMENT ? 3 : 2, V, VEC, kForwardRows<V, VEC>, 32 * W * rows);
     if (smem > 40 * 1024) {
         const cudaError_t e = allow_smem(block_norm_kernel<V, ELEMENT, VEC>, ok);
         if (e != cudaSuccess) return e;
@@ -504,8 +540,8 @@ struct ColumnSums {
 size_t column_sums_bytes(int V, int N, int threads) { return V <= 2 ? 0 : (size_t)N * V * 8 * sizeof(float) * threads; }
 
 // Rows on their way in shared memory (0: one, in registers).
-template <int V>
-constexpr int kGradRows = V <= 2 ? 2 : 0;
+template <int V, bool VEC>
+constexpr int kGradRows = V == 1 ? 2 : (V == 2 ? (VEC ? 2 : 1) : 0);
 
 // One row at a time by W warps, V vectors per lane, blockDim / (32 W) rows at once; a lane keeps the same columns for all of the
 // block's rows and adds up their gradients (of the weights, of a gate per channel), rows in their order.  A row has two
@@ -530,13 +566,13 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
     const int sets = (p.T + rows - 1) / rows, t_step = gridDim.x * rows;
     int t = blockIdx.x * rows + row_in_block;
     extern __shared__ __align__(16) uint4 s_feed[];           // rows on their way, then the columns' sums
-    RowFeed<kElement ? 5 : 4, V, VEC, kGradRows<V>> feed;
+    RowFeed<kElement ? 5 : 4, V, VEC, kGradRows<V, VEC>> feed;
     feed.src[0] = p.y + first; feed.ld[0] = (uint32_t)p.ldy * 2;
     feed.src[1] = p.d_out ? p.h + first : nullptr; feed.ld[1] = (uint32_t)p.ldh * 2;
     feed.src[2] = p.d_out ? p.d_out + first : nullptr; feed.ld[2] = (uint32_t)p.ldout_grad * 2;
     feed.src[3] = p.d_h ? p.d_h + first : nullptr; feed.ld[3] = (uint32_t)p.ldh_grad * 2;
     if (kElement) { feed.src[kElement ? 4 : 0] = (const bf16*)p.gate + first; feed.ld[kElement ? 4 : 0] = (uint32_t)p.ldg * 2; }
-    feed.start(s_feed, p.H - first, step, p.T, t, t_step);
+    feed.start(s_feed, p.H - first, first, step, p.T, t, t_step);
     float gt = GATE == MOE_GATE_TOKEN && t < p.T ? ((const float*)p.gate)[t] : 1.f;
     bf16* const d_y = p.d_y + first;
     bf16* const d_residual = p.d_residual + first;
@@ -564,7 +600,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormArgs p, int W)
             if (GATE == MOE_GATE_CHANNEL) unpack8(column((const bf16*)p.gate, v), gate_w[v]);
         }
     }
-    ColumnSums<V, GATE == MOE_GATE_CHANNEL ? 3 : 2> columns(reinterpret_cast<float4*>(s_feed + (VEC ? kGradRows<V> * (kElement ? 5 : 4) * V * blockDim.x : 0)));  // of d_pre, d_post (without block_scale), d_gate
+    ColumnSums<V, GATE == MOE_GATE_CHANNEL ? 3 : 2> columns(reinterpret_cast<float4*>(s_feed + kGradRows<V, VEC> * (kElement ? 5 : 4) * V * (VEC ? 1 : 2) * blockDim.x));  // of d_pre, d_post (without block_scale), d_gate
     const float over = 1.f / (float)p.H;
     int buf = 0;
     for (int set = blockIdx.x; set < sets; set += gridDim.x, t += t_step, buf ^= 1) {
@@ -768,7 +804,8 @@ cudaError_t launch_grad_gate(const BlockNormArgs& p, const GradShape& g, cudaStr
     static bool ok[2][kMaxDevices] = {{false}, {false}};
     const dim3 grid(g.blocks), block(32 * g.W * g.rows);
     const int threads = 32 * g.W * g.rows;
-    const size_t smem = column_sums_bytes(V, GATE == MOE_GATE_CHANNEL ? 3 : 2, threads) + (p.vec ? feed_bytes(GATE == MOE_GATE_ELEMENT ? 5 : 4, V, kGradRows<V>, threads) : 0);
+    const size_t smem = column_sums_bytes(V, GATE == MOE_GATE_CHANNEL ? 3 : 2, threads) +
+                        feed_bytes(GATE == MOE_GATE_ELEMENT ? 5 : 4, V, p.vec, p.vec ? kGradRows<V, true> : kGradRows<V, false>, threads);
     if (smem > 40 * 1024) {
         const cudaError_t e = p.vec ? allow_smem(block_norm_grad_kernel<V, GATE, true>, ok[1]) : allow_smem(block_norm_grad_kernel<V, GATE, false>, ok[0]);
         if (e != cudaSuccess) return e;
@@ -816,7 +853,7 @@ quantize_kernel(const __grid_constant__ QuantizeArgs p, int W)
     extern __shared__ __align__(16) uint4 s_feed[];
     RowFeed<1, V, VEC, kQuantizeRows> feed;
     feed.src[0] = p.x + first; feed.ld[0] = (uint32_t)p.ldx * 2;
-    feed.start(s_feed, p.K - first, step, p.T, t, t_step);
+    feed.start(s_feed, p.K - first, first, step, p.T, t, t_step);
     int buf = 0;
     for (int set = blockIdx.x; set < sets; set += gridDim.x, t += t_step, buf ^= 1) {
         const int n = t < p.T ? p.K - first : 0;
@@ -855,13 +892,13 @@ cudaError_t launch_quantize_v(const QuantizeArgs& p, int W, int rows, cudaStream
 {
     const int sets = (p.T + rows - 1) / rows, most = 148 * (32 / (W * rows));
     const dim3 grid(sets < most ? sets : most), block(32 * W * rows);
-    const size_t smem = p.vec ? feed_bytes(1, V, kQuantizeRows, 32 * W * rows) : 0;
-    static bool ok[kMaxDevices] = {false};
+    const size_t smem = feed_bytes(1, V, p.vec, kQuantizeRows, 32 * W * rows);
+    static bool ok[2][kMaxDevices] = {{false}, {false}};
     if (smem > 40 * 1024) {
-        const cudaError_t e = allow_smem(quantize_kernel<V, true>, ok);
+        const cudaError_t e = p.vec ? allow_smem(quantize_kernel<V, true>, ok[1]) : allow_smem(quantize_kernel<V, false>, ok[0]);
         if (e != cudaSuccess) return e;
     }
-    return p.vec ? launch_pdl(quantize_kernel<V, true>, grid, block, smem, st, p, W) : launch_pdl(quantize_kernel<V, false>, grid, block, 0, st, p, W);
+    return p.vec ? launch_pdl(quantize_kernel<V, true>, grid, block, smem, st, p, W) : launch_pdl(quantize_kernel<V, false>, grid, block, smem, st, p, W);
 }
 
 }  // namespace
@@ -875,7 +912,7 @@ cudaError_t launch_block_norm(const BlockNormArgs& in, cudaStream_t st)
     p.vec_weight = al(p.post, 16) && al(p.pre, 16) && (p.gate_form != MOE_GATE_CHANNEL || al(p.gate, 16));
     p.vec_q = al(p.q, 8) && p.ldq % 8 == 0;
     const int vecs = (p.H + 7) / 8;
-    const int V = vecs <= 32 || (!p.vec && vecs <= 512) ? 1 : (vecs <= 512 ? 2 : 4);
+    const int V = vecs <= 32 ? 1 : (vecs <= 512 || (!p.vec && vecs <= 1024) ? 2 : 4);
     const int W = (vecs + 32 * V - 1) / (32 * V), rows = W >= 4 ? 1 : 4 / W;
     if (V == 1) return launch_v<1>(p, W, rows, st);
     if (V == 2) return launch_v<2>(p, W, rows, st);

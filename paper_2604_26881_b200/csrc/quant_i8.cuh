@@ -61,7 +61,7 @@ template <bool VEC>
 __device__ __forceinline__ void store_i8(int8_t* dst, int n, bool vec_q, const float2 (&x)[4], const RowScale& s)
 {
     const uint2 o = to_i8x8(x, s);
-    if (VEC && vec_q) {
+    if (vec_q && (VEC || n >= 8)) {
         *reinterpret_cast<uint2*>(dst) = o;
     } else {
 #pragma unroll

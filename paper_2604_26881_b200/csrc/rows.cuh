@@ -85,14 +85,56 @@ __device__ __forceinline__ void store8(bf16* p, int n, const float* f)
     }
 }
 
+__device__ __forceinline__ void store8_anywhere(bf16* p, int n, const uint4& v);
+// (VEC false: all lanes of a warp take part, n elements of this lane, 8 less of the next)
 template <bool VEC>
 __device__ __forceinline__ void store8(bf16* p, int n, const float2* f)
 {
-    if (VEC) {
-        if (n > 0) *reinterpret_cast<uint4*>(p) = pack8(f);
-    } else {
+    if (!VEC) store8_anywhere(p, n, pack8(f));
+    else if (n > 0) *reinterpret_cast<uint4*>(p) = pack8(f);
+}
+
+// Eight of sixteen consecutive elements (two vectors), from element k on (0 .. 7; the same for all lanes).
+__device__ __forceinline__ uint4 eight_from(const uint4& a, const uint4& b, int k)
+{
+    const bool four = k & 4, two = k & 2, one = k & 1;
+    const uint32_t x0 = four ? a.z : a.x, x1 = four ? a.w : a.y, x2 = four ? b.x : a.z, x3 = four ? b.y : a.w, x4 = four ? b.z : b.x, x5 = four ? b.w : b.y;
+    const uint32_t y0 = two ? x1 : x0, y1 = two ? x2 : x1, y2 = two ? x3 : x2, y3 = two ? x4 : x3, y4 = two ? x5 : x4;
+    return make_uint4(one ? __funnelshift_r(y0, y1, 16) : y0, one ? __funnelshift_r(y1, y2, 16) : y1, one ? __funnelshift_r(y2, y3, 16) : y2,
+                      one ? __funnelshift_r(y3, y4, 16) : y3);
+}
+// A vector whose elements from n on read as zero.
+__device__ __forceinline__ uint4 first_of(const uint4& v, int n)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t o[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < n) p[i] = __float2bfloat16_rn(i & 1 ? f[i / 2].y : f[i / 2].x);
+    for (int i = 0; i < 4; ++i) o[i] = 2 * i + 1 < n ? w[i] : (2 * i < n ? w[i] & 0xffffu : 0u);
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+// A row's vectors, one after the other in a warp's lanes, to a row that is on no 16-byte boundary: each lane writes the aligned 16 bytes
+// that its predecessor's last elements and its own first ones make; elements at the ends of the warp's share, and of the row, are
+// written one by one.  All lanes take part; n: elements of this lane (possibly none, the next lane's are 8 less).  (Element by element,
+// each of eight instructions touches all of the warp's lines: 16384 x 2047 forward 216 us.)
+__device__ __forceinline__ void store8_anywhere(bf16* p, int n, const uint4& v)
+{
+    const int s = (int)((uintptr_t)p & 15) >> 1, lane = threadIdx.x & 31;
+    if (s == 0) {
+        if (n >= 8) {
+            *reinterpret_cast<uint4*>(p) = v;
+            return;
+        }
+    } else {
+        const uint4 before = make_uint4(__shfl_up_sync(0xffffffffu, v.x, 1), __shfl_up_sync(0xffffffffu, v.y, 1), __shfl_up_sync(0xffffffffu, v.z, 1),
+                                        __shfl_up_sync(0xffffffffu, v.w, 1));
+        if (lane > 0 && n >= 8 - s) *reinterpret_cast<uint4*>(p - s) = eight_from(before, v, 8 - s);
+    }
+    const bool head = s == 0 || lane == 0 || n < 8 - s, tail = s == 0 || lane == 31 || n < 16 - s;      // not written with a neighbour's
+    if (n > 0 && (head || tail)) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n && (i < 8 - s ? head : tail)) reinterpret_cast<unsigned short*>(p)[i] = (unsigned short)(w[i / 2] >> (16 * (i & 1)));
     }
 }
 
