@@ -359,7 +359,8 @@ balance_kernel(const __grid_constant__ BalanceArgs p)
         load_row<L, VW>(logits, b.E, sub, live, z);
 #pragma unroll
         for (int i = 0; i < kC / 2; ++i) e[i] = exp_of(z[i]);
-        const bool far = live && !ordinary(group_sum<L>(total(e)));
+        const float sum = group_sum<L>(total(e));             // (a shuffle: not under a condition)
+        const bool far = live && !ordinary(sum);
         if (!__any_sync(kFull, far)) return;
         float lse;
         shifted_shares<L, SIGMOID>(z, lse);

@@ -258,6 +258,23 @@ def test_infinities_nan_and_far_logits(score, E, k):
     check_far(z, E, k, score)
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("E,k", [(60, 4), (61, 4), (100, 6), (256, 8)])
+def test_far_logits_of_several_models(E, k, dtype):
+    """Rows that need a shift among others, of every model; masked rows and rows of -inf between them."""
+    g = torch.Generator().manual_seed(5)
+    z = torch.randn(150, E, generator=g)
+    z[::7] -= 90
+    z[3::11] += 75
+    z[5::13] = -float("inf")
+    z[6::17, ::2] = -float("inf")
+    for score in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            check(150, E, k, score, renorm=renorm, z=z, M=3, tenants=5, masked=True, use=("w", "loss"), dtype=dtype)
+            check(150, E, k, score, renorm=renorm, z=z, use=("w", "loss"), dtype=dtype)
+
+
 def check_far(z, E, k, score):
     """Where the second loss is infinite: everything but that."""
     T = z.shape[0]
