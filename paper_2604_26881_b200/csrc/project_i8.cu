@@ -572,6 +572,7 @@ project_i8_many_kernel(const I8Args p, const __grid_constant__ I8Maps maps)
                         if (by32) write_columns<bf16, 32>(p, r, xs, ws + c, add + c, (bf16*)p.out + at, now);
                         else write_columns<bf16, 16>(p, r, xs, ws + c, add + c, (bf16*)p.out + at, now);
                     }
+                    __syncwarp();                           // (the next load is the whole warp's)
                     continue;
                 }
 #pragma unroll
