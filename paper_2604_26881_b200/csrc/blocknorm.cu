@@ -9,8 +9,8 @@
 //
 // Bound by HBM, with the instructions close behind: every element is read and written once, W warps hold a row with up to four
 // 16-byte vectors a lane.  16384 x 2048: 47 us (268 MB, 5.7 TB/s, 0.87 of the measured copy bandwidth), gated element by element 54 us (6.2
-// TB/s); its gradients with a sigmoid gate and both weights' 103 us (537 MB, 5.2 TB/s, 0.79), of a row of 2048 elements 600 instructions
-// a warp.  One token 3.2 us, launch and two sums over the row.  What made it so: rows on their way by asynchronous copies into shared
+// TB/s); its gradients with a sigmoid gate and both weights' 103 us (537 MB, 5.2 TB/s, 0.79), 480 instructions a warp for 256
+// elements.  One token 3.2 us, launch and two sums over the row.  What made it so: rows on their way by asynchronous copies into shared
 // memory instead of registers (16384 x 2048 53 -> 47 us, gradients 132 -> 103), two fp32 operations per instruction and no
 // divisions in the loop (62 -> 53), two barriers a row instead of four and one exponential a gate (gradients 295 -> 160).
 #include "blocknorm.cuh"

@@ -138,8 +138,9 @@ def test_strides_and_alignment(pads, shift):
 
 
 @gpu
-def test_outputs_in_the_place_of_inputs():
-    T, H = 33, 1032
+@pytest.mark.parametrize("H", [1031, 1032, 513, 2047])
+def test_outputs_in_the_place_of_inputs(H):
+    T = 33
     i = inputs(T, H, "element")
     args = dict(post_weight=cuda(i["post"]), pre_weight=cuda(i["pre"]), gate_act="sigmoid")
     y, r, g = cuda(i["y"]), cuda(i["r"]), cuda(i["gate"])
@@ -389,8 +390,9 @@ def test_gradients_against_differences():
 
 
 @gpu
-def test_gradients_in_the_place_of_inputs_are_the_same():
-    T, H = 37, 1032
+@pytest.mark.parametrize("H", [1031, 1032, 513, 2047])
+def test_gradients_in_the_place_of_inputs_are_the_same(H):
+    T = 37
     i = inputs(T, H, "element")
     h, d_out, d_h = ((torch.randn(T, H, generator=torch.Generator().manual_seed(s))).to(BF) for s in (1, 2, 3))
     want = run_backward(i, h, "element", "sigmoid", 0.5, 0.7, 1e-6, d_out, d_h)
